@@ -1,4 +1,5 @@
-"""MI355X-native Caffe-semantics convolution and InnerProduct layers and policy-gradient loss kernels (fp32): thin Python binding over libmi355conv.so.
+"""MI355X-native Caffe-semantics convolution and InnerProduct layers, policy-gradient loss kernels and the operators of a policy over
+tokens (log probabilities, clipping by the gradient norm, 4-bit weights): thin Python binding over libmi355conv.so.
 
 The package holds the HIP sources (``csrc/``), the build step (``build.py``), the ctypes binding
 (``binding.py``: same names as the C entry points, argument marshalling only) and the seeded
@@ -46,4 +47,32 @@ from .pg_binding import (  # noqa: F401
     pg_sigmoid_bottom_diff,
     pg_sigmoid_sample_action,
     pg_softmax_bottom_diff,
+)
+from .lp_binding import (  # noqa: F401
+    LpParams,
+    lp_backward,
+    lp_desc_create,
+    lp_desc_destroy,
+    lp_desc_kernel_names,
+    lp_desc_workspace_bytes,
+    lp_forward,
+    lp_forward_backward,
+)
+from .gn_binding import (  # noqa: F401
+    GnParams,
+    gn_clip,
+    gn_desc_create,
+    gn_desc_destroy,
+    gn_desc_kernel_names,
+    gn_desc_workspace_bytes,
+)
+from .q4_binding import (  # noqa: F401
+    Q4Params,
+    q4_desc_create,
+    q4_desc_destroy,
+    q4_desc_kernel_names,
+    q4_desc_packed_bytes,
+    q4_desc_workspace_bytes,
+    q4_forward,
+    q4_pack,
 )

@@ -1,0 +1,98 @@
+// Vectors of 16 bytes of the element types of mi355dtype.h: loads and stores on the element's own alignment, conversions to and
+// from fp32.
+#pragma once
+
+#include <hip/hip_runtime.h>
+
+#include "mi355dtype.h"
+
+namespace mi355conv {
+
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
+// 16 bytes on a boundary of 2 or 4: one instruction all the same, as global memory takes any alignment.
+struct __attribute__((packed, aligned(2))) Half8Mem {
+  u32x4 v;
+};
+struct __attribute__((packed, aligned(4))) Word4Mem {
+  u32x4 v;
+};
+
+template <int DTYPE>
+struct Elem;
+
+template <>
+struct Elem<MI355_F32> {
+  typedef float T;
+  typedef Word4Mem Mem;
+  static constexpr int VEC = 4;
+  static constexpr uint32_t kLowest = 0xFF800000u;  // -inf in every element of a word
+  static __device__ __forceinline__ float to_float(T x) { return x; }
+  static __device__ __forceinline__ T from_float(float x) { return x; }
+  static __device__ __forceinline__ float get(const u32x4& v, int i) {
+    const uint32_t word = v[i];  // (a bit cast of the vector's element itself would take its first one)
+    return __builtin_bit_cast(float, word);
+  }
+  static __device__ __forceinline__ u32x4 pack(const float (&x)[VEC]) {
+    u32x4 v;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = __builtin_bit_cast(uint32_t, x[i]);
+    return v;
+  }
+};
+
+template <>
+struct Elem<MI355_F16> {
+  typedef _Float16 T;
+  typedef Half8Mem Mem;
+  typedef _Float16 Pair __attribute__((ext_vector_type(2)));
+  static constexpr int VEC = 8;
+  static constexpr uint32_t kLowest = 0xFC00FC00u;
+  static __device__ __forceinline__ float to_float(T x) { return (float)x; }
+  static __device__ __forceinline__ T from_float(float x) { return (T)x; }
+  static __device__ __forceinline__ float get(const u32x4& v, int i) {
+    const uint32_t word = v[i >> 1];
+    const Pair pair = __builtin_bit_cast(Pair, word);
+    return (float)pair[i & 1];
+  }
+  static __device__ __forceinline__ u32x4 pack(const float (&x)[VEC]) {
+    u32x4 v;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = __builtin_bit_cast(uint32_t, Pair{(T)x[2 * i], (T)x[2 * i + 1]});
+    return v;
+  }
+};
+
+template <>
+struct Elem<MI355_BF16> {
+  typedef __bf16 T;
+  typedef Half8Mem Mem;
+  typedef __bf16 Pair __attribute__((ext_vector_type(2)));
+  static constexpr int VEC = 8;
+  static constexpr uint32_t kLowest = 0xFF80FF80u;
+  static __device__ __forceinline__ float to_float(T x) { return (float)x; }
+  static __device__ __forceinline__ T from_float(float x) { return (T)x; }
+  static __device__ __forceinline__ float get(const u32x4& v, int i) {
+    return __builtin_bit_cast(float, i & 1 ? v[i >> 1] & 0xffff0000u : v[i >> 1] << 16);
+  }
+  static __device__ __forceinline__ u32x4 pack(const float (&x)[VEC]) {
+    u32x4 v;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = __builtin_bit_cast(uint32_t, Pair{(T)x[2 * i], (T)x[2 * i + 1]});
+    return v;
+  }
+};
+
+template <class E>
+__device__ __forceinline__ u32x4 load_vec(const typename E::T* at) {
+  return reinterpret_cast<const typename E::Mem*>(at)->v;
+}
+
+template <class E>
+__device__ __forceinline__ void store_vec(typename E::T* at, const u32x4& v) {
+  reinterpret_cast<typename E::Mem*>(at)->v = v;
+}
+
+inline int dtype_bytes(int dtype) { return dtype == MI355_F64 ? 8 : dtype == MI355_F32 ? 4 : 2; }
+
+}  // namespace mi355conv

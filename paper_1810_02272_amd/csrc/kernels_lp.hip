@@ -1,0 +1,825 @@
+// Log probabilities of given tokens over a large vocabulary, with the entropy, the most likely alternatives and the gradient
+// of a loss on them (include/mi355lp.h).
+//
+// With c = scale log2(e) and any reference M, every quantity of a row follows from t_i = c x_i - M:
+//   s = sum 2^t_i      s2 = sum 2^t_i t_i      log2 p_i = t_i - log2 s      H = ln 2 (log2 s - s2 / s)
+//   d_logits_i = 2^t_i (A + B t_i) + [i = token] w scale,   B = -u scale ln 2 / s,   A = scale (-w - u (H - ln 2 log2 s)) / s
+// so one pass finds s and s2 beside a running maximum, and a second one writes the gradient.  M is the maximum's own c x: the same
+// number enters every t_i, so that its rounding cancels.
+#include <float.h>
+#include <hip/hip_runtime.h>
+#include <math.h>
+#include <stdio.h>
+#include <string.h>
+
+#include <algorithm>
+#include <new>
+
+#include "device_utils.h"
+#include "elements.h"
+#include "internal.h"
+#include "mi355lp.h"
+
+struct lp_desc {
+  lp_params_t p;
+  float c;          // scale log2(e)
+  int32_t form;     // of the passes that see a whole row: kWave, kBlock, kWide or kLong
+  int32_t splits;   // parts of a row in different workgroups (1: none)
+  int32_t seg;      // logits of a part
+  size_t ws_bytes;
+  char names[160];
+};
+
+namespace mi355conv {
+
+namespace {
+
+constexpr int kMaxTop = 64;
+constexpr float kLn2 = 0.693147180559945309f;
+
+struct LpArgs {
+  const void* logits;
+  int64_t stride;
+  const int32_t* token;
+  const float *d_logp, *d_entropy;
+  float *logp, *entropy, *stats, *top_logp;
+  int32_t* top_token;
+  void* d_logits;
+  int64_t d_stride;
+  float4* parts;      // [rows][splits]: maximum, s, s2
+  uint64_t* cand;     // [rows][splits][top]: the alternatives of a part
+  int32_t rows, vocab, top, splits, seg;
+  float scale, c;
+};
+
+// What a row's passes share.
+struct RowStat {
+  float M, c;      // t = c x - M
+  float log2s, H;  // log2 s, entropy in nats
+  float step;      // nats per unit of t: ln 2, but for the rows of beyond()
+};
+
+__device__ __forceinline__ float exp2_fast(float t) { return __builtin_amdgcn_exp2f(t); }  // 0 below 2^-126
+
+// t for a product with 2^t, which is 0 where this cuts off: -inf must not meet a 0.
+__device__ __forceinline__ float finite(float t) { return fmaxf(t, -200.f); }
+
+__device__ __forceinline__ float reference(float m, float c) { return fminf(fmaxf(m * c, -FLT_MAX), FLT_MAX); }
+
+// Whether c x leaves fp32 at the row's maximum: a row of nothing but a type's lowest value, or values beyond 2e38.  Neighbouring
+// values are so far apart there that p is shared by those equal to the maximum: t = x - m serves as well, whatever the scale.
+__device__ __forceinline__ bool beyond(float m, float c) { return !(fabsf(m * c) <= FLT_MAX) && m != -INFINITY; }
+
+struct Sums {
+  float m, s, s2;
+};
+
+// Adds what another part of the row has found: relative to that part's own maximum m_t.
+__device__ __forceinline__ void add_part(Sums& a, float M, bool over, float c, float m_t, float s_t, float s2_t) {
+  const float d = reference(m_t, c) - M;
+  const float f = over ? (m_t == a.m ? 1.f : 0.f) : m_t == -INFINITY ? 0.f : exp2_fast(d);
+  a.s += f * s_t;
+  a.s2 += f == 0.f ? 0.f : over ? s2_t : f * (s2_t + d * s_t);
+}
+
+__device__ __forceinline__ RowStat finish(const Sums& a, float c, float scale) {
+  RowStat r;
+  const bool over = beyond(a.m, c);
+  r.c = over ? 1.f : c;
+  r.step = over ? scale : kLn2;
+  r.M = over ? a.m : a.m == -INFINITY ? 0.f : a.m * c;
+  if (a.m == -INFINITY && a.s == 0.f) {  // nothing but -inf
+    r.log2s = INFINITY;
+    r.H = 0.f;
+  } else {
+    r.log2s = log2f(a.s);
+    r.H = kLn2 * (r.log2s - a.s2 / a.s);
+  }
+  return r;
+}
+
+// The natural logarithm of the probability of a logit.
+__device__ __forceinline__ float log_prob(const RowStat& r, float x, float scale) {
+  const float t = fmaf(x, r.c, -r.M);
+  if (t == -INFINITY && x != -INFINITY && r.step == kLn2) return x * scale - r.M * kLn2;  // c x is out of range, scale x may not be
+  return fmaf(r.step, t, -kLn2 * r.log2s);
+}
+
+struct GradScale {
+  float A, B, at_token;
+};
+
+__device__ __forceinline__ GradScale grad_scale(const RowStat& r, float w, float u, float scale) {
+  const float inv = exp2f(-r.log2s) * scale;
+  GradScale g;
+  g.B = -u * kLn2 * inv;
+  g.A = inv * (-w - u * (r.log2s < INFINITY ? r.H - kLn2 * r.log2s : 0.f));
+  if (r.log2s == INFINITY) g.A = g.B = 0.f;
+  g.at_token = w * scale;
+  return g;
+}
+
+__device__ __forceinline__ float wave_max(float v) {
+#pragma unroll
+  for (int d = 32; d >= 1; d >>= 1) v = fmaxf(v, __shfl_xor(v, d, 64));
+  return v;
+}
+
+__device__ __forceinline__ float wave_add(float v) {
+#pragma unroll
+  for (int d = 32; d >= 1; d >>= 1) v += __shfl_xor(v, d, 64);
+  return v;
+}
+
+// The wave's lanes' sums in one, in every lane.
+__device__ __forceinline__ Sums wave_merge(float m, float s, float s2, float c) {
+  Sums a = {wave_max(m), 0.f, 0.f};
+  add_part(a, reference(a.m, c), beyond(a.m, c), c, m, s, s2);
+  a.s = wave_add(a.s);
+  a.s2 = wave_add(a.s2);
+  return a;
+}
+
+// Logits in the order of the alternatives, as unsigned numbers: -0 is 0, NaN the greatest.  With the index below it, each once.
+__device__ __forceinline__ uint32_t order_key(float x) {
+  if (x != x) return 0xFFFFFFFEu;
+  const uint32_t u = x == 0.f ? 0u : __builtin_bit_cast(uint32_t, x);
+  return u & 0x80000000u ? ~u : u | 0x80000000u;
+}
+
+__device__ __forceinline__ float key_value(uint32_t k) {
+  return __builtin_bit_cast(float, k & 0x80000000u ? k ^ 0x80000000u : ~k);
+}
+
+__device__ __forceinline__ uint64_t entry_of(float x, int index) { return (uint64_t)order_key(x) << 32 | (0xFFFFFFFFu - (uint32_t)index); }
+
+// ---- a row in the registers of a team of THREADS threads ----
+// Vector v of a row holds its elements v VEC and on.  A partial one at the end, the tail, is thread 0's: it is loaded so that it ends
+// with the row, and what an earlier vector holds as well is taken out (-inf): every access is inside the row.
+template <class E>
+struct Slot {
+  int base;  // of element 0, negative in rows shorter than a vector
+  int lo;    // elements from here on are this vector's
+};
+
+template <class E>
+__device__ __forceinline__ Slot<E> slot_of(int v, int n) {
+  const int b = v * E::VEC, over = b + E::VEC - n;
+  return over <= 0 ? Slot<E>{b, 0} : Slot<E>{b - over, over};
+}
+
+template <class E>
+__device__ __forceinline__ u32x4 lowest_vec() {
+  return u32x4{E::kLowest, E::kLowest, E::kLowest, E::kLowest};
+}
+
+template <class E>
+__device__ __forceinline__ u32x4 without_first(const u32x4& v, int lo) {
+  u32x4 r = v;
+  constexpr int PER = E::VEC / 4;
+#pragma unroll
+  for (int w = 0; w < 4; ++w) {
+    if (PER == 1) {
+      if (w < lo) r[w] = E::kLowest;
+    } else {
+      if (2 * w < lo) r[w] = (r[w] & 0xffff0000u) | (E::kLowest & 0xffffu);
+      if (2 * w + 1 < lo) r[w] = (r[w] & 0xffffu) | (E::kLowest & 0xffff0000u);
+    }
+  }
+  return r;
+}
+
+// Vector v (v VEC < n), wherever it lies.
+template <class E>
+__device__ __forceinline__ u32x4 row_vec(const typename E::T* row, int v, int n) {
+  const Slot<E> at = slot_of<E>(v, n);
+  if (at.base >= 0) {
+    const u32x4 r = load_vec<E>(row + at.base);
+    return at.lo ? without_first<E>(r, at.lo) : r;
+  }
+  float x[E::VEC];
+#pragma unroll
+  for (int i = 0; i < E::VEC; ++i) x[i] = i >= at.lo ? E::to_float(row[at.base + i]) : -INFINITY;
+  return E::pack(x);
+}
+
+template <class E>
+__device__ __forceinline__ void store_row_vec(typename E::T* row, int v, int n, const float (&x)[E::VEC]) {
+  const Slot<E> at = slot_of<E>(v, n);
+  if (at.lo == 0) {
+    store_vec<E>(row + at.base, E::pack(x));
+    return;
+  }
+#pragma unroll
+  for (int i = 0; i < E::VEC; ++i)
+    if (i >= at.lo) row[at.base + i] = E::from_float(x[i]);
+}
+
+// One vector into a thread's sums.
+template <class E, bool ENT>
+__device__ __forceinline__ void add_vec(const u32x4& r, float c, float& m, float& M, float& s, float& s2) {
+  float x[E::VEC];
+  float most = -INFINITY;
+#pragma unroll
+  for (int i = 0; i < E::VEC; ++i) x[i] = E::get(r, i);
+#pragma unroll
+  for (int i = 0; i < E::VEC; ++i) most = fmaxf(most, x[i]);
+  if (most > m) {
+    const float to = reference(most, c), d = M - to, f = m == -INFINITY ? 0.f : exp2_fast(d);
+    if (ENT) s2 = f == 0.f ? s * 0.f : f * (s2 + d * s);  // (NaN stays)
+    s *= f;
+    M = to;
+    m = most;
+  }
+#pragma unroll
+  for (int i = 0; i < E::VEC; ++i) {
+    const float t = fmaf(x[i], c, -M), e = exp2_fast(t);
+    s += e;
+    if (ENT) s2 = fmaf(e, finite(t), s2);
+  }
+}
+
+template <bool ENT>
+__device__ __forceinline__ float grad_of(float logit, const RowStat& st, const GradScale& g) {
+  const float t = fmaf(logit, st.c, -st.M), e = exp2_fast(t);
+  return e * (ENT ? fmaf(g.B, finite(t), g.A) : g.A);
+}
+
+template <class E, bool ENT>
+__device__ __forceinline__ void grad_vec(const u32x4& r, const RowStat& st, const GradScale& g, float (&x)[E::VEC]) {
+#pragma unroll
+  for (int i = 0; i < E::VEC; ++i) x[i] = grad_of<ENT>(E::get(r, i), st, g);
+}
+
+// Keeps the compiler from carrying what one pass computed from the vectors (unpacked logits, lane masks) to the next one: it would
+// take several times the registers that the vectors themselves do.
+template <int NV>
+__device__ __forceinline__ void forget(u32x4 (&r)[NV]) {
+#pragma unroll
+  for (int j = 0; j < NV; ++j) asm volatile("" : "+v"(r[j]));
+}
+
+__device__ __forceinline__ int forget(int uniform) {
+  asm volatile("" : "+s"(uniform));
+  return uniform;
+}
+
+template <int THREADS>
+__device__ __forceinline__ void team_sync() {
+  if constexpr (THREADS == 64)
+    wave_sync();
+  else
+    __syncthreads();
+}
+
+// Vectors that hold a candidate for a team's alternatives, and candidates.  Where there are more, the alternatives are found one by
+// one.
+template <int THREADS>
+constexpr int kHits = THREADS == 64 ? 128 : 256;
+template <int THREADS>
+constexpr int kCand = 2 * kHits<THREADS>;
+
+template <int THREADS>
+struct TeamLds {
+  u32x4 hit[kHits<THREADS>];
+  float4 sums[THREADS / 64];
+  int hit_at[kHits<THREADS>];
+  uint32_t group_top[64];
+  float bound, at_token;
+  uint32_t hits, count;
+  uint64_t cand[kCand<THREADS>];
+  uint64_t best[THREADS / 64];
+};
+
+// The `top` greatest entries of the row part [first, first + n), out(rank, entry) for each; 0 stands for none.
+// The top-th greatest of 64 groups' maxima bounds the top-th greatest logit from below, so few others pass it: of 128256 normal
+// logits, 24 for 20.  Each that passes is ranked by counting those above it.  Where too many pass (equal logits, all but a few
+// banned), each place is found by a pass over the row.
+template <class E, int THREADS, int NV, class Out>
+__device__ __forceinline__ void team_top(TeamLds<THREADS>& lds, const u32x4 (&r)[NV], const u32x4& tail, const typename E::T* row, int first, int n, int top,
+                                         float m, int tid, Out&& out) {
+  constexpr int VEC = E::VEC, GROUP = THREADS / 64;
+  const int nv = (n + VEC - 1) / VEC, full = n / VEC, lane = tid & 63;
+  float gm = m;
+#pragma unroll
+  for (int d = 1; d < GROUP; d <<= 1) gm = fmaxf(gm, __shfl_xor(gm, d, 64));
+  if (tid % GROUP == 0) lds.group_top[tid / GROUP] = order_key(gm);
+  if (tid == 0) lds.hits = lds.count = 0;
+  team_sync<THREADS>();
+  if (THREADS == 64 || tid < 64) {  // the leading 16 bits of the top-th greatest: a bound all the same
+    const uint32_t k = lds.group_top[lane];
+    uint32_t bound = 0;
+#pragma unroll
+    for (int bit = 31; bit >= 16; --bit) {
+      const uint32_t with = bound | 1u << bit;
+      if (__builtin_popcountll(__ballot(k >= with)) >= top) bound = with;
+    }
+    if (lane == 0) lds.bound = bound <= 0x007FFFFFu ? -INFINITY : key_value(bound);  // key of -inf and the unused ones below it
+  }
+  team_sync<THREADS>();
+  const float bound = lds.bound;
+  auto look = [&](const u32x4& vec, int v) {
+    bool any = false;
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) any |= !(E::get(vec, i) < bound);
+    if (any) {
+      const uint32_t place = atomicAdd(&lds.hits, 1u);
+      if (place < (uint32_t)kHits<THREADS>) {
+        lds.hit[place] = vec;
+        lds.hit_at[place] = v;
+      }
+    }
+  };
+  {
+    const int full_ = forget(full);
+#pragma unroll
+    for (int j = 0; j < NV; ++j)
+      if (j * THREADS < full_ && j * THREADS + tid < full_) look(r[j], j * THREADS + tid);
+  }
+  for (int v = NV * THREADS + tid; v < full; v += THREADS) look(load_vec<E>(row + v * VEC), v);
+  if (full < nv && tid == 0) look(tail, full);
+  team_sync<THREADS>();
+  const int hits = (int)lds.hits;
+  if (hits <= kHits<THREADS>) {
+    for (int i = tid; i < hits * VEC; i += THREADS) {
+      const float x = E::to_float(reinterpret_cast<const typename E::T*>(lds.hit)[i]);
+      const Slot<E> at = slot_of<E>(lds.hit_at[i / VEC], n);
+      if (!(x < bound) && i % VEC >= at.lo) {
+        const uint32_t place = atomicAdd(&lds.count, 1u);
+        if (place < (uint32_t)kCand<THREADS>) lds.cand[place] = entry_of(x, first + at.base + i % VEC);
+      }
+    }
+    team_sync<THREADS>();
+  }
+  const int count = (int)lds.count;
+  if (hits <= kHits<THREADS> && count <= kCand<THREADS>) {
+    for (int i = tid; i < count; i += THREADS) {
+      const uint64_t mine = lds.cand[i];
+      int rank = 0;
+      for (int o = 0; o < count; ++o) rank += lds.cand[o] > mine ? 1 : 0;
+      if (rank < top) out(rank, mine);
+    }
+    for (int i = count + tid; i < top; i += THREADS) out(i, (uint64_t)0);  // a part shorter than that
+    return;
+  }
+  uint64_t last = ~(uint64_t)0;
+  for (int k = 0; k < top; ++k) {
+    uint64_t best = 0;
+    for (int v = tid; v < nv; v += THREADS) {
+      const u32x4 vec = row_vec<E>(row, v, n);
+      const Slot<E> at = slot_of<E>(v, n);
+#pragma unroll
+      for (int i = 0; i < VEC; ++i) {
+        const uint64_t e = entry_of(E::get(vec, i), first + at.base + i);
+        if (i >= at.lo && e < last && e > best) best = e;
+      }
+    }
+#pragma unroll
+    for (int d = 32; d >= 1; d >>= 1) {
+      const uint64_t o = __shfl_xor((unsigned long long)best, d, 64);
+      best = o > best ? o : best;
+    }
+    if constexpr (THREADS > 64) {
+      if (lane == 0) lds.best[tid >> 6] = best;
+      __syncthreads();
+      for (int w = 0; w < THREADS / 64; ++w) best = lds.best[w] > best ? lds.best[w] : best;
+      __syncthreads();
+    }
+    last = best;
+    if (tid == 0) out(k, best);
+  }
+}
+
+enum Mode { kScore, kTrain, kPart };
+
+// A row (kPart: a part of one) is read once, into registers, up to NV vectors a thread; what is beyond them is read again by
+// whatever needs it again.  THREADS 64: a wave for each row, several in a workgroup.
+template <int DTYPE, int THREADS, int NV, Mode MODE, bool ENT>
+__global__ __launch_bounds__(THREADS == 64 ? 256 : THREADS) void lp_row_kernel(LpArgs a) {
+  typedef Elem<DTYPE> E;
+  typedef typename E::T T;
+  constexpr int VEC = E::VEC, WAVES = THREADS / 64;
+  __shared__ TeamLds<THREADS> team_lds[THREADS == 64 ? 4 : 1];
+  TeamLds<THREADS>& lds = team_lds[THREADS == 64 ? threadIdx.x >> 6 : 0];
+  const int tid = THREADS == 64 ? threadIdx.x & 63 : threadIdx.x;
+  const int lane = tid & 63;
+  const int teams = THREADS == 64 ? (int)(gridDim.x * (blockDim.x >> 6)) : (int)gridDim.x;
+  int item = THREADS == 64 ? (int)(blockIdx.x * (blockDim.x >> 6) + (threadIdx.x >> 6)) : (int)blockIdx.x;
+  if constexpr (THREADS == 64) item = __builtin_amdgcn_readfirstlane(item);
+  const int64_t items = MODE == kPart ? (int64_t)a.rows * a.splits : a.rows;
+  for (int64_t it = item; it < items; it += teams) {
+    const int r_ = MODE == kPart ? (int)(it / a.splits) : (int)it;
+    const int first = MODE == kPart ? (int)(it % a.splits) * a.seg : 0;
+    const int n = MODE == kPart ? min(a.seg, a.vocab - first) : a.vocab;
+    const T* const row = static_cast<const T*>(a.logits) + (int64_t)r_ * a.stride + first;
+    const int nv = (n + VEC - 1) / VEC, full = n / VEC;
+    int token = -1;
+    float at_token = 0.f;
+    if (MODE != kPart && a.token) {
+      token = a.token[r_];
+      if ((uint32_t)token >= (uint32_t)a.vocab) token = -1;
+      if (token >= 0) at_token = E::to_float(row[token]);
+    }
+
+    u32x4 r[NV], tail = lowest_vec<E>();
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+      r[j] = lowest_vec<E>();
+      if (j * THREADS < full && j * THREADS + tid < full) r[j] = load_vec<E>(row + (j * THREADS + tid) * VEC);
+    }
+    if (full < nv && tid == 0) tail = row_vec<E>(row, full, n);
+    forget(r);
+
+    float m = -INFINITY, M = 0.f, s = 0.f, s2 = 0.f;
+#pragma unroll
+    for (int j = 0; j < NV; ++j)
+      if (j * THREADS < full) add_vec<E, ENT>(r[j], a.c, m, M, s, s2);
+    for (int v = NV * THREADS + tid; v < full; v += THREADS) add_vec<E, ENT>(load_vec<E>(row + v * VEC), a.c, m, M, s, s2);
+    if (full < nv) add_vec<E, ENT>(tail, a.c, m, M, s, s2);
+
+    forget(r);
+    Sums sum = wave_merge(m, s, s2, a.c);
+    if constexpr (WAVES > 1) {
+      // through shared memory, so that it has arrived before another wave writes over it (d_logits may be logits)
+      if (tid == 0) lds.at_token = at_token;
+      if (lane == 0) lds.sums[tid >> 6] = make_float4(sum.m, sum.s, sum.s2, 0.f);
+      __syncthreads();
+      const float4 p = lane < WAVES ? lds.sums[lane] : make_float4(-INFINITY, 0.f, 0.f, 0.f);
+      sum = wave_merge(p.x, p.y, p.z, a.c);
+      at_token = lds.at_token;
+    }
+    if (beyond(sum.m, a.c)) {  // rare: the same sums of t = x - m
+      float count = 0.f;
+      for (int v = tid; v < nv; v += THREADS) {
+        const u32x4 vec = row_vec<E>(row, v, n);
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) count += exp2_fast(E::get(vec, i) - sum.m);
+      }
+      count = wave_add(count);
+      if constexpr (WAVES > 1) {
+        __syncthreads();
+        if (lane == 0) lds.sums[tid >> 6].x = count;
+        __syncthreads();
+        count = wave_add(lane < WAVES ? lds.sums[lane].x : 0.f);
+      }
+      sum.s = count;
+      sum.s2 = 0.f;
+    }
+
+    if constexpr (MODE == kPart) {
+      if (tid == 0) a.parts[it] = make_float4(sum.m, sum.s, sum.s2, 0.f);
+      if (a.top) {
+        uint64_t* const to = a.cand + it * a.top;
+        team_top<E, THREADS, NV>(lds, r, tail, row, first, n, a.top, m, tid, [&](int rank, uint64_t e) { to[rank] = e; });
+      }
+    } else {
+      const RowStat st = finish(sum, a.c, a.scale);
+      if (tid == 0) {
+        if (a.logp) a.logp[r_] = token >= 0 ? log_prob(st, at_token, a.scale) : 0.f;
+        if (ENT && a.entropy) a.entropy[r_] = st.H;
+        if (MODE == kScore && a.stats) reinterpret_cast<float4*>(a.stats)[r_] = make_float4(st.M, st.log2s, st.H, st.c);
+      }
+      if constexpr (MODE == kScore) {
+        if (a.top) {
+          float* const logp = a.top_logp + (int64_t)r_ * a.top;
+          int32_t* const tok = a.top_token + (int64_t)r_ * a.top;
+          team_top<E, THREADS, NV>(lds, r, tail, row, 0, n, a.top, m, tid, [&](int rank, uint64_t e) {
+            logp[rank] = log_prob(st, key_value((uint32_t)(e >> 32)), a.scale);
+            tok[rank] = (int32_t)(0xFFFFFFFFu - (uint32_t)e);
+          });
+        }
+      } else {
+        const float w = token >= 0 ? a.d_logp[r_] : 0.f, u = ENT && a.d_entropy ? a.d_entropy[r_] : 0.f;
+        const GradScale g = grad_scale(st, w, u, a.scale);
+        T* const to = static_cast<T*>(a.d_logits) + (int64_t)r_ * a.d_stride;
+        const int full_ = forget(full);
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+          if (j * THREADS < full_ && j * THREADS + tid < full_) {
+            float x[VEC];
+            grad_vec<E, ENT>(r[j], st, g, x);
+            store_vec<E>(to + (j * THREADS + tid) * VEC, E::pack(x));
+          }
+        }
+        for (int v = NV * THREADS + tid; v < full; v += THREADS) {
+          float x[VEC];
+          grad_vec<E, ENT>(load_vec<E>(row + v * VEC), st, g, x);
+          store_vec<E>(to + v * VEC, E::pack(x));
+        }
+        if (full < nv && tid == 0) {
+          float x[VEC];
+          grad_vec<E, ENT>(tail, st, g, x);
+          store_row_vec<E>(to, full, n, x);
+        }
+        // the token's own, by the thread that has just written it without
+        if (token >= 0 && tid == (token < full * VEC ? token / VEC % THREADS : 0))
+          to[token] = E::from_float(grad_of<ENT>(at_token, st, g) + g.at_token);
+      }
+    }
+    team_sync<THREADS>();  // the next row's team memory
+  }
+}
+
+// The sums of a row's parts, in every lane of a wave.
+__device__ __forceinline__ Sums merge_parts(const float4* parts, int splits, int lane, float c) {
+  const float4 p = lane < splits ? parts[lane] : make_float4(-INFINITY, 0.f, 0.f, 0.f);
+  return wave_merge(p.x, p.y, p.z, c);
+}
+
+constexpr int kMaxSplits = 64;
+
+// A row's parts in one: a workgroup for each row.
+template <int DTYPE, bool ENT>
+__global__ __launch_bounds__(256) void lp_join_kernel(LpArgs a) {
+  typedef Elem<DTYPE> E;
+  extern __shared__ uint64_t entries[];  // [splits][top]
+  const int row = blockIdx.x, lane = threadIdx.x & 63;
+  const int total = a.splits * a.top;
+  for (int i = threadIdx.x; i < total; i += 256) entries[i] = a.cand[(int64_t)row * total + i];
+  const RowStat st = finish(merge_parts(a.parts + (int64_t)row * a.splits, a.splits, lane, a.c), a.c, a.scale);
+  if (threadIdx.x == 0) {
+    if (a.logp) {
+      const int token = a.token[row];
+      a.logp[row] = (uint32_t)token < (uint32_t)a.vocab
+                        ? log_prob(st, E::to_float(static_cast<const typename E::T*>(a.logits)[(int64_t)row * a.stride + token]), a.scale)
+                        : 0.f;
+    }
+    if (ENT && a.entropy) a.entropy[row] = st.H;
+    if (a.stats) reinterpret_cast<float4*>(a.stats)[row] = make_float4(st.M, st.log2s, st.H, st.c);
+  }
+  __syncthreads();
+  for (int i = threadIdx.x; i < total; i += 256) {
+    const uint64_t mine = entries[i];
+    if (mine == 0) continue;
+    int rank = 0;
+    for (int o = 0; o < total; ++o) rank += entries[o] > mine ? 1 : 0;
+    if (rank < a.top) {
+      a.top_logp[(int64_t)row * a.top + rank] = log_prob(st, key_value((uint32_t)(mine >> 32)), a.scale);
+      a.top_token[(int64_t)row * a.top + rank] = (int32_t)(0xFFFFFFFFu - (uint32_t)mine);
+    }
+  }
+}
+
+// The gradient where the row's statistics are known (PARTS: as parts), kGradVecs vectors a thread.
+constexpr int kGradVecs = 4;
+
+template <int DTYPE, bool ENT, bool PARTS>
+__global__ __launch_bounds__(256) void lp_grad_kernel(LpArgs a, int chunks) {
+  typedef Elem<DTYPE> E;
+  typedef typename E::T T;
+  constexpr int VEC = E::VEC, CHUNK = 256 * VEC * kGradVecs;
+  const int64_t items = (int64_t)a.rows * chunks;
+  for (int64_t it = blockIdx.x; it < items; it += gridDim.x) {
+    const int r_ = (int)(it / chunks), first = (int)(it % chunks) * CHUNK;
+    const int n = min(CHUNK, a.vocab - first), nv = (n + VEC - 1) / VEC;
+    const T* const row = static_cast<const T*>(a.logits) + (int64_t)r_ * a.stride;
+    u32x4 r[kGradVecs];
+#pragma unroll
+    for (int j = 0; j < kGradVecs; ++j) {
+      const int v = j * 256 + (int)threadIdx.x;
+      r[j] = v < nv ? row_vec<E>(row + first, v, n) : lowest_vec<E>();
+    }
+    int token = a.token[r_];
+    if ((uint32_t)token >= (uint32_t)a.vocab) token = -1;
+    // where d_logits is logits, this one is about to be overwritten, by this workgroup
+    const bool mine = token >= first && token < first + n;
+    const float at_token = mine ? E::to_float(row[token]) : 0.f;
+    RowStat st;
+    if constexpr (PARTS) {
+      st = finish(merge_parts(a.parts + (int64_t)r_ * a.splits, a.splits, threadIdx.x & 63, a.c), a.c, a.scale);
+    } else {
+      const float4 q = reinterpret_cast<const float4*>(a.stats)[r_];
+      st = RowStat{q.x, q.w, q.y, q.z, 0.f};
+    }
+    const float w = token >= 0 ? a.d_logp[r_] : 0.f, u = ENT && a.d_entropy ? a.d_entropy[r_] : 0.f;
+    const GradScale g = grad_scale(st, w, u, a.scale);
+    T* const to = static_cast<T*>(a.d_logits) + (int64_t)r_ * a.d_stride + first;
+    const int owner = (token - first) / VEC % 256;
+    float own = 0.f, logp = 0.f;
+    if (mine) {
+      own = grad_of<ENT>(at_token, st, g) + g.at_token;
+      logp = log_prob(st, at_token, a.scale);
+    }
+    asm volatile("" ::"v"(own), "v"(logp));  // the logit has arrived
+    __syncthreads();
+    if (PARTS && threadIdx.x == 0) {
+      if (a.logp && mine) a.logp[r_] = logp;
+      if (a.logp && token < 0 && first == 0) a.logp[r_] = 0.f;
+      if (ENT && a.entropy && first == 0) a.entropy[r_] = st.H;
+    }
+#pragma unroll
+    for (int j = 0; j < kGradVecs; ++j) {
+      const int v = j * 256 + (int)threadIdx.x;
+      if (v < nv) {
+        float x[VEC];
+        grad_vec<E, ENT>(r[j], st, g, x);
+        store_row_vec<E>(to, v, n, x);
+      }
+    }
+    if (mine && (int)threadIdx.x == owner) to[token - first] = E::from_float(own);
+  }
+}
+
+enum Form { kWave, kBlock, kWide, kLong };
+const char* const kFormNames[] = {"wave", "block", "wide", "long"};
+
+constexpr int kWaveVecs = 4, kBlockVecs = 8, kWideVecs = 8, kLongVecs = 20;
+
+constexpr int kPartThreads = 256;
+
+template <int DTYPE, Mode MODE, bool ENT>
+int launch_row(const lp_desc* d, const LpArgs& a, hipStream_t stream) {
+  if (MODE == kPart) {
+    hipLaunchKernelGGL((lp_row_kernel<DTYPE, kPartThreads, kBlockVecs, kPart, ENT>), dim3(a.rows * a.splits), dim3(kPartThreads), 0, stream, a);
+  } else if (d->form == kWave) {
+    const int waves = a.rows >= 2048 ? 4 : 1;
+    hipLaunchKernelGGL((lp_row_kernel<DTYPE, 64, kWaveVecs, MODE, ENT>), dim3(std::min((a.rows + waves - 1) / waves, 1 << 20)), dim3(64 * waves), 0, stream, a);
+  } else if (d->form == kBlock) {
+    hipLaunchKernelGGL((lp_row_kernel<DTYPE, 256, kBlockVecs, MODE, ENT>), dim3(std::min(a.rows, 1 << 20)), dim3(256), 0, stream, a);
+  } else if (d->form == kWide) {
+    hipLaunchKernelGGL((lp_row_kernel<DTYPE, 1024, kWideVecs, MODE, ENT>), dim3(std::min(a.rows, 1 << 20)), dim3(1024), 0, stream, a);
+  } else {
+    hipLaunchKernelGGL((lp_row_kernel<DTYPE, 1024, kLongVecs, MODE, ENT>), dim3(std::min(a.rows, 1 << 20)), dim3(1024), 0, stream, a);
+  }
+  return (int)hipGetLastError();
+}
+
+template <int DTYPE, bool ENT>
+int launch_join(const LpArgs& a, hipStream_t stream) {
+  hipLaunchKernelGGL((lp_join_kernel<DTYPE, ENT>), dim3(a.rows), dim3(256), (size_t)a.splits * a.top * 8, stream, a);
+  return (int)hipGetLastError();
+}
+
+template <int DTYPE, bool ENT, bool PARTS>
+int launch_grad(const LpArgs& a, hipStream_t stream) {
+  constexpr int CHUNK = 256 * Elem<DTYPE>::VEC * kGradVecs;
+  const int chunks = (a.vocab + CHUNK - 1) / CHUNK;
+  hipLaunchKernelGGL((lp_grad_kernel<DTYPE, ENT, PARTS>), dim3((uint32_t)std::min<int64_t>((int64_t)a.rows * chunks, 1 << 22)), dim3(256), 0, stream, a, chunks);
+  return (int)hipGetLastError();
+}
+
+// One of the descriptor's six kinds.
+template <template <int, bool> class Op>
+int by_kind(const lp_desc* d, const LpArgs& a, hipStream_t stream) {
+  const bool ent = d->p.entropy != 0;
+  switch (d->p.dtype) {
+    case MI355_F32: return ent ? Op<MI355_F32, true>::run(d, a, stream) : Op<MI355_F32, false>::run(d, a, stream);
+    case MI355_F16: return ent ? Op<MI355_F16, true>::run(d, a, stream) : Op<MI355_F16, false>::run(d, a, stream);
+    default: return ent ? Op<MI355_BF16, true>::run(d, a, stream) : Op<MI355_BF16, false>::run(d, a, stream);
+  }
+}
+
+template <int DTYPE, bool ENT>
+struct Forward {
+  static int run(const lp_desc* d, const LpArgs& a, hipStream_t stream) {
+    if (d->splits == 1) return launch_row<DTYPE, kScore, ENT>(d, a, stream);
+    const int e = launch_row<DTYPE, kPart, ENT>(d, a, stream);
+    return e ? e : launch_join<DTYPE, ENT>(a, stream);
+  }
+};
+
+template <int DTYPE, bool ENT>
+struct Backward {
+  static int run(const lp_desc*, const LpArgs& a, hipStream_t stream) { return launch_grad<DTYPE, ENT, false>(a, stream); }
+};
+
+template <int DTYPE, bool ENT>
+struct ForwardBackward {
+  static int run(const lp_desc* d, const LpArgs& a, hipStream_t stream) {
+    if (d->splits == 1) return launch_row<DTYPE, kTrain, ENT>(d, a, stream);
+    const int e = launch_row<DTYPE, kPart, ENT>(d, a, stream);
+    return e ? e : launch_grad<DTYPE, ENT, true>(a, stream);
+  }
+};
+
+LpArgs base_args(const lp_desc* d, const void* logits, int64_t stride, const int32_t* token) {
+  LpArgs a = {};
+  a.logits = logits;
+  a.stride = stride;
+  a.token = token;
+  a.rows = d->p.rows;
+  a.vocab = d->p.vocab;
+  a.splits = d->splits;
+  a.seg = d->seg;
+  a.scale = d->p.scale;
+  a.c = d->c;
+  return a;
+}
+
+void place_workspace(const lp_desc* d, LpArgs& a, void* ws) {
+  a.parts = static_cast<float4*>(ws);
+  a.cand = reinterpret_cast<uint64_t*>(a.parts + (size_t)d->p.rows * d->splits);
+}
+
+bool bad_rows(const lp_desc* d, const void* at, int64_t stride) { return !at || (d->p.rows > 1 && stride < d->p.vocab); }
+
+}  // namespace
+
+}  // namespace mi355conv
+
+using namespace mi355conv;
+
+extern "C" {
+
+int lp_desc_create(lp_desc_t** out, const lp_params_t* pp) {
+  if (!out || !pp) return CONV_EINVAL;
+  const lp_params_t p = *pp;
+  if (p.rows < 0 || p.vocab < 1 || (p.dtype != MI355_F32 && p.dtype != MI355_F16 && p.dtype != MI355_BF16)) return CONV_EINVAL;
+  if (p.top < 0 || p.top > kMaxTop || p.top > p.vocab || (p.entropy != 0 && p.entropy != 1)) return CONV_EINVAL;
+  if (!(p.scale >= 0x1p-60f && p.scale <= 0x1p60f)) return CONV_EINVAL;
+  if (p.vocab >= 1 << 30) return CONV_ESHAPE;
+  lp_desc* d = new (std::nothrow) lp_desc;
+  if (!d) return CONV_EINVAL;
+  memset(d, 0, sizeof(*d));
+  d->p = p;
+  d->c = (float)(p.scale * 1.44269504088896340736);
+  const int vec = 16 / dtype_bytes(p.dtype);
+  d->form = p.vocab <= 64 * vec * kWaveVecs ? kWave : p.vocab <= 256 * vec * kBlockVecs ? kBlock : p.vocab <= 1024 * vec * kWideVecs ? kWide : kLong;
+  d->splits = 1;
+  d->seg = p.vocab;
+  if (p.rows > 0 && p.rows < 256 && p.vocab >= 8192) {
+    const int most = 512 / p.rows, least = (p.vocab + 2047) / 2048;
+    int splits = std::max(1, std::min(std::min(most, least), kMaxSplits));
+    if (splits > 1) {
+      d->seg = ((p.vocab + splits - 1) / splits + vec - 1) / vec * vec;
+      d->splits = (p.vocab + d->seg - 1) / d->seg;
+    }
+  }
+  if (d->splits > 1) d->ws_bytes = (size_t)p.rows * d->splits * (16 + 8 * (size_t)p.top);
+  const char* const form = kFormNames[d->form];
+  if (d->splits > 1)
+    snprintf(d->names, sizeof(d->names), "forward=lp_parts(S=%d)+join;backward=lp_grad;forward_backward=lp_parts(S=%d)+grad", d->splits, d->splits);
+  else
+    snprintf(d->names, sizeof(d->names), "forward=lp_row[%s];backward=lp_grad;forward_backward=lp_row[%s]", form, form);
+  *out = d;
+  return CONV_OK;
+}
+
+int lp_desc_destroy(lp_desc_t* d) {
+  if (!d) return CONV_EINVAL;
+  delete d;
+  return CONV_OK;
+}
+
+int lp_desc_workspace_bytes(const lp_desc_t* d, size_t* bytes) {
+  if (!d || !bytes) return CONV_EINVAL;
+  *bytes = d->ws_bytes;
+  return CONV_OK;
+}
+
+const char* lp_desc_kernel_names(const lp_desc_t* d) { return d ? d->names : ""; }
+
+int lp_forward(const lp_desc_t* d, const void* logits, int64_t stride, const int32_t* token, float* logp, float* entropy,
+               float* stats, float* top_logp, int32_t* top_token, void* ws, size_t ws_bytes, void* hip_stream) {
+  if (!d || (token != nullptr) != (logp != nullptr) || (entropy && !d->p.entropy)) return CONV_EINVAL;
+  if (d->p.rows == 0) return CONV_OK;
+  if ((top_logp != nullptr) != (d->p.top > 0) || (top_token != nullptr) != (d->p.top > 0)) return CONV_EINVAL;
+  if (bad_rows(d, logits, stride)) return CONV_EINVAL;
+  if (d->ws_bytes && (!ws || ws_bytes < d->ws_bytes)) return CONV_EWORKSPACE;
+  LpArgs a = base_args(d, logits, stride, token);
+  a.logp = logp;
+  a.entropy = entropy;
+  a.stats = stats;
+  a.top = d->p.top;
+  a.top_logp = top_logp;
+  a.top_token = top_token;
+  place_workspace(d, a, ws);
+  const int e = by_kind<Forward>(d, a, (hipStream_t)hip_stream);
+  return e ? record_hip_error(e) : CONV_OK;
+}
+
+int lp_backward(const lp_desc_t* d, const void* logits, int64_t stride, const int32_t* token, const float* stats,
+                const float* d_logp, const float* d_entropy, void* d_logits, int64_t d_stride, void* hip_stream) {
+  if (!d || (d_entropy && !d->p.entropy)) return CONV_EINVAL;
+  if (d->p.rows == 0) return CONV_OK;
+  if (bad_rows(d, logits, stride) || bad_rows(d, d_logits, d_stride) || !token || !stats || !d_logp) return CONV_EINVAL;
+  LpArgs a = base_args(d, logits, stride, token);
+  a.stats = const_cast<float*>(stats);
+  a.d_logp = d_logp;
+  a.d_entropy = d_entropy;
+  a.d_logits = d_logits;
+  a.d_stride = d_stride;
+  const int e = by_kind<Backward>(d, a, (hipStream_t)hip_stream);
+  return e ? record_hip_error(e) : CONV_OK;
+}
+
+int lp_forward_backward(const lp_desc_t* d, const void* logits, int64_t stride, const int32_t* token, const float* d_logp,
+                        const float* d_entropy, float* logp, float* entropy, void* d_logits, int64_t d_stride, void* ws,
+                        size_t ws_bytes, void* hip_stream) {
+  if (!d || ((d_entropy || entropy) && !d->p.entropy)) return CONV_EINVAL;
+  if (d->p.rows == 0) return CONV_OK;
+  if (bad_rows(d, logits, stride) || bad_rows(d, d_logits, d_stride) || !token || !d_logp) return CONV_EINVAL;
+  if (d->ws_bytes && (!ws || ws_bytes < d->ws_bytes)) return CONV_EWORKSPACE;
+  LpArgs a = base_args(d, logits, stride, token);
+  a.logp = logp;
+  a.entropy = entropy;
+  a.d_logp = d_logp;
+  a.d_entropy = d_entropy;
+  a.d_logits = d_logits;
+  a.d_stride = d_stride;
+  place_workspace(d, a, ws);
+  const int e = by_kind<ForwardBackward>(d, a, (hipStream_t)hip_stream);
+  return e ? record_hip_error(e) : CONV_OK;
+}
+
+}  // extern "C"

@@ -18,6 +18,12 @@
 #include "mi355conv.h"
 #include "mi355ip.h"
 #include "mi355pg.h"
+#include "mi355lp.h"
+#include "mi355gn.h"
+#include "mi355q4.h"
+
+#include <new>
+#include <vector>
 
 namespace {
 
@@ -397,10 +403,206 @@ PyObject* py_ip_plan(PyObject*, PyObject* args) {  // handle, m, k, num_output
   return new_plan(Plan{reinterpret_cast<void*>(handle), {2, {m, k}}, {2, {o, k}}, {2, {m, o}}, {1, {o}}}, kIp);
 }
 
+// ---- log probabilities ----
+
+at::ScalarType scalar_type(int dtype) {
+  return dtype == MI355_F16 ? at::kHalf : dtype == MI355_BF16 ? at::kBFloat16 : dtype == MI355_F64 ? at::kDouble : at::kFloat;
+}
+
+struct LpPlan {
+  const lp_desc_t* desc;
+  int64_t rows, vocab;
+  at::ScalarType type;
+  Shape row, stats, top;
+};
+
+const char kLp[] = "mi355conv.lp_plan", kGn[] = "mi355conv.gn_plan", kQ4[] = "mi355conv.q4_plan";
+
+template <typename P>
+const P* own_plan(PyObject* o, const char* kind) {
+  return PyCapsule_IsValid(o, kind) ? static_cast<const P*>(PyCapsule_GetPointer(o, kind)) : nullptr;
+}
+
+template <typename P>
+void delete_own_plan(PyObject* capsule) {
+  delete static_cast<P*>(PyCapsule_GetPointer(capsule, PyCapsule_GetName(capsule)));
+}
+
+template <typename P>
+PyObject* new_own_plan(P* own, const char* kind) {
+  if (!own) return PyErr_NoMemory();
+  PyObject* c = PyCapsule_New(own, kind, &delete_own_plan<P>);
+  if (!c) delete own;
+  return c;
+}
+
+// Dense rows that may lie apart.
+bool spaced_rows(PyObject* o, const LpPlan& p, void** out, int64_t* stride) {
+  if (!THPVariable_CheckExact(o)) return false;
+  const at::Tensor& t = THPVariable_Unpack(o);
+  if (!t.defined() || !t.has_storage() || !t.is_cuda() || t.layout() != at::kStrided || t.scalar_type() != p.type) return false;
+  if (t.dim() != 2 || t.size(0) != p.rows || t.size(1) != p.vocab) return false;
+  if ((p.vocab > 1 && t.stride(1) != 1) || (p.rows > 1 && t.stride(0) < p.vocab)) return false;
+  *stride = p.rows > 1 ? t.stride(0) : p.vocab;
+  *out = t.data_ptr();
+  return true;
+}
+
+PyObject* py_lp_forward(PyObject*, Args a, Py_ssize_t n) {  // plan, logits, token, logp, entropy, stats, top_logp, top_token, ws, stream
+  return guarded(n, 10, [&]() -> PyObject* {
+    const LpPlan* p = own_plan<LpPlan>(a[0], kLp);
+    void *x, *token, *logp, *h, *stats, *top_logp, *top_token, *ws, *s;
+    int64_t stride;
+    size_t bytes;
+    if (!p || !spaced_rows(a[1], *p, &x, &stride) || !optional_tensor(a[2], kInt, p->row, &token) ||
+        !optional_tensor(a[3], at::kFloat, p->row, &logp) || !optional_tensor(a[4], at::kFloat, p->row, &h) ||
+        !optional_tensor(a[5], at::kFloat, p->stats, &stats) || !optional_tensor(a[6], at::kFloat, p->top, &top_logp) ||
+        !optional_tensor(a[7], kInt, p->top, &top_token) || !workspace(a[8], &ws, &bytes) || !stream(a[9], &s))
+      return nullptr;
+    return released([&] {
+      return lp_forward(p->desc, x, stride, static_cast<int32_t*>(token), static_cast<float*>(logp), static_cast<float*>(h),
+                        static_cast<float*>(stats), static_cast<float*>(top_logp), static_cast<int32_t*>(top_token), ws, bytes, s);
+    });
+  });
+}
+
+PyObject* py_lp_backward(PyObject*, Args a, Py_ssize_t n) {  // plan, logits, token, stats, d_logp, d_entropy, d_logits, stream
+  return guarded(n, 8, [&]() -> PyObject* {
+    const LpPlan* p = own_plan<LpPlan>(a[0], kLp);
+    void *x, *token, *stats, *dl, *dh, *g, *s;
+    int64_t stride, d_stride;
+    if (!p || !spaced_rows(a[1], *p, &x, &stride) || !tensor(a[2], kInt, p->row, &token) || !tensor(a[3], at::kFloat, p->stats, &stats) ||
+        !tensor(a[4], at::kFloat, p->row, &dl) || !optional_tensor(a[5], at::kFloat, p->row, &dh) || !spaced_rows(a[6], *p, &g, &d_stride) ||
+        !stream(a[7], &s))
+      return nullptr;
+    return released([&] {
+      return lp_backward(p->desc, x, stride, static_cast<int32_t*>(token), static_cast<float*>(stats), static_cast<float*>(dl),
+                         static_cast<float*>(dh), g, d_stride, s);
+    });
+  });
+}
+
+// plan, logits, token, d_logp, d_entropy, logp, entropy, d_logits, ws, stream
+PyObject* py_lp_forward_backward(PyObject*, Args a, Py_ssize_t n) {
+  return guarded(n, 10, [&]() -> PyObject* {
+    const LpPlan* p = own_plan<LpPlan>(a[0], kLp);
+    void *x, *token, *dl, *dh, *logp, *h, *g, *ws, *s;
+    int64_t stride, d_stride;
+    size_t bytes;
+    if (!p || !spaced_rows(a[1], *p, &x, &stride) || !tensor(a[2], kInt, p->row, &token) || !tensor(a[3], at::kFloat, p->row, &dl) ||
+        !optional_tensor(a[4], at::kFloat, p->row, &dh) || !optional_tensor(a[5], at::kFloat, p->row, &logp) ||
+        !optional_tensor(a[6], at::kFloat, p->row, &h) || !spaced_rows(a[7], *p, &g, &d_stride) || !workspace(a[8], &ws, &bytes) ||
+        !stream(a[9], &s))
+      return nullptr;
+    return released([&] {
+      return lp_forward_backward(p->desc, x, stride, static_cast<int32_t*>(token), static_cast<float*>(dl), static_cast<float*>(dh),
+                                 static_cast<float*>(logp), static_cast<float*>(h), g, d_stride, ws, bytes, s);
+    });
+  });
+}
+
+PyObject* py_lp_plan(PyObject*, PyObject* args) {  // handle, rows, vocab, dtype, top
+  unsigned long long handle;
+  long long rows, vocab, top;
+  int dtype;
+  if (!PyArg_ParseTuple(args, "KLLiL", &handle, &rows, &vocab, &dtype, &top)) return nullptr;
+  return new_own_plan(new (std::nothrow) LpPlan{reinterpret_cast<const lp_desc_t*>(handle), rows, vocab, scalar_type(dtype), {1, {rows}},
+                                                {2, {rows, 4}}, {2, {rows, top}}}, kLp);
+}
+
+// ---- clipping by the gradient norm ----
+
+struct GnPlan {
+  const gn_desc_t* desc;
+  std::vector<int64_t> counts;
+  std::vector<at::ScalarType> types;
+};
+
+bool tensors(PyObject* o, const GnPlan& p, std::vector<void*>& out) {
+  if (!PyList_CheckExact(o) && !PyTuple_CheckExact(o)) return false;
+  const Py_ssize_t n = PySequence_Fast_GET_SIZE(o);
+  if ((size_t)n != p.counts.size()) return false;
+  PyObject** const items = PySequence_Fast_ITEMS(o);
+  out.resize((size_t)n);
+  for (Py_ssize_t i = 0; i < n; ++i) {
+    if (!THPVariable_CheckExact(items[i])) return false;
+    const at::Tensor& t = THPVariable_Unpack(items[i]);
+    if (!t.defined() || !t.has_storage() || !t.is_cuda() || t.layout() != at::kStrided || t.scalar_type() != p.types[(size_t)i]) return false;
+    if (!t.is_contiguous() || t.numel() != p.counts[(size_t)i]) return false;
+    out[(size_t)i] = t.data_ptr();
+  }
+  return true;
+}
+
+PyObject* py_gn_clip(PyObject*, Args a, Py_ssize_t n) {  // plan, grads, limit, outs, norm, ws, stream
+  return guarded(n, 7, [&]() -> PyObject* {
+    const GnPlan* p = own_plan<GnPlan>(a[0], kGn);
+    const Shape one = {1, {1}};
+    std::vector<void*> grads, outs;
+    double limit;
+    void *norm, *ws, *s;
+    size_t bytes;
+    if (!p || !tensors(a[1], *p, grads) || !number(a[2], &limit) || (a[3] != a[1] && !tensors(a[3], *p, outs)) ||
+        !optional_tensor(a[4], at::kFloat, one, &norm) || !workspace(a[5], &ws, &bytes) || !stream(a[6], &s))
+      return nullptr;
+    void* const* const to = a[3] == a[1] ? grads.data() : outs.data();
+    return released([&] { return gn_clip(p->desc, grads.data(), limit, to, static_cast<float*>(norm), ws, bytes, s); });
+  });
+}
+
+PyObject* py_gn_plan(PyObject*, PyObject* args) {  // handle, counts, dtypes (tuples)
+  unsigned long long handle;
+  PyObject *counts, *dtypes;
+  if (!PyArg_ParseTuple(args, "KO!O!", &handle, &PyTuple_Type, &counts, &PyTuple_Type, &dtypes)) return nullptr;
+  try {
+    GnPlan p = {reinterpret_cast<const gn_desc_t*>(handle), {}, {}};
+    for (Py_ssize_t i = 0; i < PyTuple_GET_SIZE(counts) && i < PyTuple_GET_SIZE(dtypes); ++i) {
+      p.counts.push_back(PyLong_AsLongLong(PyTuple_GET_ITEM(counts, i)));
+      p.types.push_back(scalar_type((int)PyLong_AsLong(PyTuple_GET_ITEM(dtypes, i))));
+    }
+    if (PyErr_Occurred()) return nullptr;
+    return new_own_plan(new GnPlan(p), kGn);
+  } catch (...) {
+    return PyErr_NoMemory();
+  }
+}
+
+// ---- 4-bit weights ----
+
+struct Q4Plan {
+  const q4_desc_t* desc;
+  at::ScalarType type;
+  Shape x, y, bias, packed;
+};
+
+PyObject* py_q4_forward(PyObject*, Args a, Py_ssize_t n) {  // plan, x, packed, bias, y, ws, stream
+  return guarded(n, 7, [&]() -> PyObject* {
+    const Q4Plan* p = own_plan<Q4Plan>(a[0], kQ4);
+    void *x, *packed, *bias, *y, *ws, *s;
+    size_t bytes;
+    if (!p || !tensor(a[1], p->type, p->x, &x) || !tensor(a[2], at::kByte, p->packed, &packed) || !optional_tensor(a[3], p->type, p->bias, &bias) ||
+        !tensor(a[4], p->type, p->y, &y) || !workspace(a[5], &ws, &bytes) || !stream(a[6], &s))
+      return nullptr;
+    return released([&] { return q4_forward(p->desc, x, packed, bias, y, ws, bytes, s); });
+  });
+}
+
+PyObject* py_q4_plan(PyObject*, PyObject* args) {  // handle, m, k, num_output, dtype, packed bytes
+  unsigned long long handle;
+  long long m, k, o, packed;
+  int dtype;
+  if (!PyArg_ParseTuple(args, "KLLLiL", &handle, &m, &k, &o, &dtype, &packed)) return nullptr;
+  return new_own_plan(new (std::nothrow) Q4Plan{reinterpret_cast<const q4_desc_t*>(handle), scalar_type(dtype), {2, {m, k}}, {2, {m, o}}, {1, {o}},
+                                                {1, {packed}}}, kQ4);
+}
+
 #define FAST(name, fn) {name, (PyCFunction)(void (*)(void))(PyObject * (*)(PyObject*, Args, Py_ssize_t)) & fn, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {
     {"conv_plan", py_conv_plan, METH_VARARGS, nullptr},
     {"ip_plan", py_ip_plan, METH_VARARGS, nullptr},
+    {"lp_plan", py_lp_plan, METH_VARARGS, nullptr},
+    {"gn_plan", py_gn_plan, METH_VARARGS, nullptr},
+    {"q4_plan", py_q4_plan, METH_VARARGS, nullptr},
     FAST("conv_forward", py_conv_forward<float>),
     FAST("conv_forward_f64", py_conv_forward<double>),
     FAST("conv_backward_data", py_conv_backward_data<float>),
@@ -419,6 +621,11 @@ PyMethodDef methods[] = {
     FAST("pg_discount_rewards", py_pg_discount_rewards),
     FAST("pg_sigmoid_bottom_diff", py_pg_sigmoid_bottom_diff),
     FAST("pg_softmax_bottom_diff", py_pg_softmax_bottom_diff),
+    FAST("lp_forward", py_lp_forward),
+    FAST("lp_backward", py_lp_backward),
+    FAST("lp_forward_backward", py_lp_forward_backward),
+    FAST("gn_clip", py_gn_clip),
+    FAST("q4_forward", py_q4_forward),
     {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};

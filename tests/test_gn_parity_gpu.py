@@ -1,0 +1,162 @@
+"""The gradient norm and clipping (include/mi355gn.h) against the oracle in 64 bits.
+
+Tolerances: squares and sums are held in fp64, so the norm is off by its rounding to fp32 (2^-24); the factor by its rounding to fp32 (2^-24;
+none for fp64 tensors), the product by its own in fp32 (2^-24) and by the output type's half step."""
+import math
+
+import pytest
+import torch
+
+import paper_1810_02272_amd as lib
+from oracle import tokens
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+F32, F16, BF16, F64 = torch.float32, torch.float16, torch.bfloat16, torch.float64
+
+
+def views(counts, dtypes, apart, first, fill):
+    """Tensors one after the other in a buffer for each type, `apart` elements between them, and the buffers."""
+    size = {t: first + sum(n + apart for n, u in zip(counts, dtypes) if u is t) + 8 for t in set(dtypes)}
+    buffers = {t: torch.full((n,), math.nan, device=DEV, dtype=t) for t, n in size.items()}
+    at = {t: first for t in size}
+    out = []
+    for n, t in zip(counts, dtypes):
+        v = buffers[t][at[t]:at[t] + n]
+        v.copy_(fill(n).to(t))
+        out.append(v)
+        at[t] += n + apart
+    return out, buffers
+
+
+def rest_untouched(tensors, buffers):
+    for t, b in buffers.items():
+        rest = torch.ones_like(b, dtype=torch.bool)
+        for v in tensors:
+            if v.dtype is t:
+                rest[v.storage_offset():v.storage_offset() + v.numel()] = False
+        assert torch.isnan(b[rest]).all()
+
+
+def check(norm, outs, grads, limit):
+    want_norm, want = tokens.clip(grads, limit)
+    assert abs(float(norm) - want_norm) <= 2.0 ** -23 * want_norm
+    for o, w, g in zip(outs, want, grads):
+        if want_norm <= limit:
+            assert torch.equal(o, g)
+            continue
+        eps = torch.finfo(o.dtype).eps
+        small = {F16: 2.0 ** -25, F64: 0.0}.get(o.dtype, 2.0 ** -126)
+        steps = 2.0 ** -51 if o.dtype is F64 else 2.0 ** -23
+        assert bool(((o.double() - w).abs() <= w.abs() * (eps / 2 + steps) + small).all()), (o.dtype, o.numel())
+
+
+ONE = ([1], [F32])
+MIXED = ([5, 0, 1, 4097, 3, 65537, 16, 8, 70000], [F32, BF16, BF16, F16, F64, BF16, F32, F32, F64])
+MANY = ([(i * 37) % 301 for i in range(400)], [(F32, F16, BF16, F64)[i * i % 4] for i in range(400)])
+LARGE = ([3000001, 17, 5000000, 2000003], [BF16, BF16, F32, BF16])
+
+
+@pytest.mark.parametrize("counts,dtypes", [ONE, MIXED, MANY, LARGE], ids=["one", "mixed", "many", "large"])
+@pytest.mark.parametrize("apart,first", [(0, 0), (0, 1), (3, 0), (1, 1)])
+@pytest.mark.parametrize("ratio", [0.3, 0.0, 7.0])
+def test_parity(counts, dtypes, apart, first, ratio):
+    g = torch.Generator(device=DEV).manual_seed(len(counts))
+    fill = lambda n: torch.randn(n, generator=g, device=DEV)
+    grads, grad_buffers = views(counts, dtypes, apart, first, fill)
+    outs, out_buffers = views(counts, dtypes, apart, first, lambda n: torch.full((n,), math.nan, device=DEV))
+    limit = ratio * math.sqrt(sum(counts))
+    d = lib.gn_desc_create(lib.GnParams(counts, dtypes))
+    bytes_ = lib.gn_desc_workspace_bytes(d)
+    ws = torch.full((bytes_ // 4 + 16,), math.nan, device=DEV)
+    norm = torch.full((1,), math.nan, device=DEV)
+    lib.gn_clip(d, grads, limit, outs, norm, ws[:bytes_ // 4])
+    assert torch.isnan(ws[bytes_ // 4:]).all()
+    check(norm, outs, grads, limit)
+    rest_untouched(outs, out_buffers)
+    again = [torch.empty_like(t) for t in outs]
+    lib.gn_clip(d, grads, limit, again, None, ws)        # separate tensors: the sums' order may differ, not the values by more than it
+    check(norm, again, grads, limit)
+    before = [t.clone() for t in grads]
+    lib.gn_clip(d, tuple(grads), limit, None, norm, ws)  # in place
+    check(norm, grads, before, limit)
+    rest_untouched(grads, grad_buffers)
+    assert all(torch.equal(a, b) for a, b in zip(grads, outs))
+
+
+def run(grads, limit):
+    d = lib.gn_desc_create(lib.GnParams([t.numel() for t in grads], [t.dtype for t in grads]))
+    ws = torch.empty(lib.gn_desc_workspace_bytes(d) // 4, device=DEV)
+    norm, outs = torch.empty(1, device=DEV), [torch.empty_like(t) for t in grads]
+    lib.gn_clip(d, grads, limit, outs, norm, ws)
+    return float(norm), outs
+
+
+def test_extremes():
+    big = torch.full((1000,), 1e30, device=DEV)
+    norm, (out,) = run([big], 1.0)
+    assert norm == pytest.approx(1e30 * math.sqrt(1000), rel=1e-6) and torch.allclose(out, torch.full_like(out, 1000 ** -0.5))
+    tiny = torch.full((1000,), 1e-30, device=DEV)
+    norm, (out,) = run([tiny], 1.0)
+    assert norm == pytest.approx(1e-30 * math.sqrt(1000), rel=1e-6) and torch.equal(out, tiny)
+    zero = torch.zeros(77, device=DEV, dtype=BF16)
+    norm, (out,) = run([zero], 0.0)
+    assert norm == 0.0 and torch.equal(out, zero)
+    nan = torch.ones(50, device=DEV)
+    nan[7] = math.nan
+    norm, (out,) = run([nan], 1.0)
+    assert math.isnan(norm) and torch.equal(out.nan_to_num(9.0), nan.nan_to_num(9.0))
+    inf = torch.ones(50, device=DEV)
+    inf[7] = -math.inf
+    norm, (out,) = run([inf], 1.0)
+    assert norm == math.inf and math.isnan(float(out[7])) and float(out[0]) == 0.0
+    norm, (out,) = run([big], math.inf)
+    assert torch.equal(out, big)
+    assert run([], 1.0)[0] == 0.0
+    assert run([torch.empty(0, device=DEV), torch.empty((0, 3), device=DEV, dtype=F16)], 1.0)[0] == 0.0
+
+
+def test_shapes_are_free_and_a_norm_is_that_of_all():
+    grads = [torch.randn(3, 4, 5, device=DEV), torch.randn(7, device=DEV, dtype=F64), torch.randn(64, 64, device=DEV).to(BF16)]
+    norm, outs = run(grads, 2.0)
+    check(norm, outs, grads, 2.0)
+    assert abs(math.sqrt(sum(float(t.double().square().sum()) for t in outs)) - 2.0) < 2.0 * 2.0 ** -8
+
+
+def test_in_a_graph():
+    grads = [torch.randn(1000, device=DEV), torch.randn(333, device=DEV)]
+    d = lib.gn_desc_create(lib.GnParams([1000, 333], [F32, F32]))
+    ws = torch.empty(lib.gn_desc_workspace_bytes(d) // 4, device=DEV)
+    norm, outs = torch.empty(1, device=DEV), [torch.empty_like(t) for t in grads]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    lib.gn_clip(d, grads, 3.0, outs, norm, ws, side)
+    side.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        lib.gn_clip(d, grads, 3.0, outs, norm, ws)
+    for k in range(3):
+        for t in grads:
+            t.normal_()
+        graph.replay()
+        replayed = [norm.clone()] + [t.clone() for t in outs]
+        check(norm, outs, grads, 3.0)
+        lib.gn_clip(d, grads, 3.0, outs, norm, ws)
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(replayed, [norm] + outs))
+
+
+def test_refusals_on_the_device():
+    d = lib.gn_desc_create(lib.GnParams([4, 6], [F32, BF16]))
+    a, b = torch.zeros(4, device=DEV), torch.zeros((2, 3), device=DEV, dtype=BF16)
+    ws = torch.empty(lib.gn_desc_workspace_bytes(d) // 4, device=DEV)
+    lib.gn_clip(d, [a, b], 1.0, ws=ws)
+    lib.gn_clip(d, iter([a, b]) and [a, b], 1, (a, b), None, ws)
+    for grads, limit, outs, space, error in (([a], 1.0, None, ws, ValueError), ([a, b.float()], 1.0, None, ws, TypeError),
+                                             ([a, b[:1]], 1.0, None, ws, ValueError), ([a, b.t()], 1.0, None, ws, TypeError),
+                                             ([a, b.cpu()], 1.0, None, ws, TypeError), ([a, b], -1.0, None, ws, lib.ConvError),
+                                             ([a, b], math.nan, None, ws, lib.ConvError), ([a, None], 1.0, None, ws, lib.ConvError),
+                                             ([a, b], 1.0, [a, None], ws, lib.ConvError), ([a, b], 1.0, None, None, lib.ConvError),
+                                             ([a, b], 1.0, None, ws[:-1], lib.ConvError)):
+        with pytest.raises(error):
+            lib.gn_clip(d, grads, limit, outs, None, space)

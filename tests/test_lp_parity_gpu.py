@@ -1,0 +1,311 @@
+"""Log probabilities of given tokens, entropy, alternatives and gradients (include/mi355lp.h) against the oracle in 64 bits.
+
+Tolerances, with u = 2^-24 (half a step of fp32): a row's sum is at most 256 additions deep in these sizes (per thread, then over lanes,
+waves and parts), each term 2^t has its exponent rounded once (|t| u) and a table's error of 2 u.
+  log p     256 u + 4 u |log p|
+  entropy   256 u (2 + log2 vocab): s2 / s and log2 s, each off by the sums' error
+  gradient  u (300 + 2 |t|) on each of its terms, p |w| and p |u| (|log p| + H + 2 log2 vocab) (the constants' cancellation), two
+            roundings of w at the token, then half a step of the output's type, or of its smallest number
+"""
+import math
+
+import pytest
+import torch
+
+import paper_1810_02272_amd as lib
+from oracle import tokens
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+F32, F16, BF16 = torch.float32, torch.float16, torch.bfloat16
+U = 2.0 ** -24
+INF = math.inf
+
+# rows, vocab, dtype, top, entropy, scale, gap between rows, first element's place in its buffer
+CASES = [
+    (1, 1, F32, 1, 1, 1.0, 0, 0),
+    (3, 2, BF16, 2, 1, 1.0, 0, 1),
+    (5, 7, F16, 3, 1, 0.5, 0, 1),
+    (4, 8, BF16, 8, 0, 1.0, 1, 0),
+    (9, 9, BF16, 1, 1, 2.0, 0, 3),
+    (6, 31, F32, 31, 1, 1.0, 2, 1),
+    (7, 64, F16, 64, 1, 1.0, 0, 0),
+    (300, 65, BF16, 20, 1, 1.0, 0, 0),
+    (17, 511, F32, 32, 1, 1.5, 0, 0),
+    (33, 1000, F32, 0, 0, 1.0, 0, 0),
+    (5, 1024, F32, 5, 1, 1.0, 0, 0),
+    (5, 1025, F32, 5, 1, 1.0, 0, 3),
+    (5, 2048, BF16, 5, 1, 1.0, 0, 0),
+    (2100, 333, F16, 7, 1, 1.0, 5, 0),       # several rows in a workgroup
+    (5, 2049, F16, 40, 1, 0.75, 0, 0),
+    (11, 5000, BF16, 64, 1, 1.0, 8, 0),
+    (270, 8190, F32, 10, 1, 1.0, 2, 2),
+    (260, 16384, BF16, 20, 1, 1.0, 0, 0),
+    (257, 16387, F16, 20, 0, 1.0, 0, 5),
+    (256, 32768, F32, 3, 1, 1.0, 0, 0),
+    (260, 50257, BF16, 20, 1, 1.25, 47, 0),
+    (256, 65539, F16, 32, 1, 1.0, 0, 0),
+    (256, 90001, F32, 20, 1, 1.0, 0, 0),     # beyond a workgroup's registers
+    (256, 128256, BF16, 20, 1, 1.0, 0, 0),
+    (256, 163900, BF16, 5, 0, 1.0, 0, 0),    # beyond a workgroup's registers
+    (1, 8192, BF16, 20, 1, 1.0, 0, 0),       # a row in parts
+    (1, 32000, BF16, 20, 1, 1.0, 0, 0),
+    (2, 10001, F32, 64, 1, 1.0, 3, 1),
+    (3, 160000, F16, 20, 1, 1.0, 0, 0),
+    (64, 50257, BF16, 20, 1, 1.5, 0, 0),
+    (130, 20011, F32, 32, 1, 1.0, 1, 0),
+]
+IDS = ["%dx%d-%s-t%d-e%d-s%g-g%d-o%d" % (c[0], c[1], str(c[2])[6:], *c[3:]) for c in CASES]
+
+
+def spaced(values, dtype, gap, first):
+    """The rows in a buffer of their own with a gap behind each, and the buffer (NaN where no element is)."""
+    rows, vocab = values.shape
+    buffer = torch.full((first + rows * (vocab + gap) + 8,), math.nan, device=DEV, dtype=dtype)
+    view = buffer[first:first + rows * (vocab + gap)].view(rows, vocab + gap)[:, :vocab]
+    view.copy_(values)
+    return view, buffer
+
+
+def untouched(view, buffer):
+    """Whether the buffer still holds NaN wherever the view has no element."""
+    rest = torch.ones_like(buffer, dtype=torch.bool)
+    rest.as_strided(view.shape, view.stride(), view.storage_offset()).fill_(False)
+    return bool(torch.isnan(buffer[rest]).all())
+
+
+def make(case, seed):
+    rows, vocab, dtype, top, entropy, scale, gap, first = case
+    g = torch.Generator(device=DEV).manual_seed(seed)
+    x = torch.randn((rows, vocab), generator=g, device=DEV) * 2.5
+    if vocab > 20:
+        x.masked_fill_(torch.rand((1, vocab), generator=g, device=DEV) < 0.05, -INF)
+    token = torch.randint(vocab, (rows,), generator=g, device=DEV, dtype=torch.int32)
+    if rows > 4:  # rows at which it can go wrong
+        x[1] = -INF                                             # nothing left
+        x[2] = torch.finfo(dtype).min                           # the type's lowest value throughout
+        x[3] = -INF
+        x[3, vocab // 2] = -3.0                                 # one left, and another is asked for
+        x[4] = 0.25                                             # equal throughout
+        token[0], token[3] = -1, 0
+    if rows > 8:
+        x[5] = torch.finfo(dtype).min
+        x[5, vocab - 1] = 2.0
+        x[6, ::2] = 0.0
+        x[6, 1::2] = -0.0
+        x[7] = torch.linspace(-9, 9, vocab, device=DEV)         # the likeliest next to each other
+        token[6], token[7] = vocab, 2 ** 31 - 1
+    if rows > 16:
+        x[9] = torch.linspace(9, -9, vocab, device=DEV)
+        x[10] = -1000.0 + 0.01 * torch.arange(vocab, device=DEV) % 64
+        x[11] += 500.0
+    x, buffer = spaced(x.to(dtype), dtype, gap, first)
+    d_logp = torch.randn(rows, generator=g, device=DEV)
+    d_entropy = torch.randn(rows, generator=g, device=DEV) * 0.1 if entropy else None
+    return x, buffer, token, d_logp, d_entropy
+
+
+def within(got, want, tol, what):
+    got, want = got.double(), want.double()
+    same = (got == want.to(torch.float32)) | ((got - want).abs() <= tol)  # (what fp32 does not reach is an infinity)
+    assert bool(same.all()), (what, float(torch.where(same, 0.0, (got - want).abs()).nan_to_num(INF).max()), int((~same).sum()))
+
+
+def check_rows(logp, h, got_logp, got_h, token, vocab):
+    within(got_logp, tokens.token_logp(logp, token), U * (256 + 4 * tokens.token_logp(logp, token).abs().nan_to_num(0, 0, 0)), "logp")
+    if got_h is not None:
+        within(got_h, h, U * 256 * (2 + math.log2(vocab)), "entropy")
+
+
+def check_gradient(case, x, token, d_logp, d_entropy, got):
+    rows, vocab, dtype, _, _, scale, _, _ = case
+    logp, h = tokens.log_probs(x, scale)
+    p = logp.exp()
+    valid = (token >= 0) & (token < vocab)
+    w = torch.where(valid, d_logp.double(), 0.0).abs()[:, None]
+    inner = torch.where(p == 0, torch.zeros_like(p), p * (logp.abs() + h[:, None] + 2 * math.log2(vocab)))
+    depth = 300 + 2 * logp.abs().clamp(max=200) * 1.5
+    tol = scale * U * depth * (p * w + (inner * d_entropy.double().abs()[:, None] if d_entropy is not None else 0.0))
+    at = torch.where(valid, token, 0).long()[:, None]
+    tol.scatter_add_(1, at, torch.where(valid[:, None], 2 * U * scale * w, 0.0))
+    want = tokens.d_logits(x, token, d_logp, d_entropy, scale)
+    info = torch.finfo(dtype)
+    tol += want.abs() * (info.eps / 2) + (2.0 ** -25 if dtype == F16 else 2.0 ** -126)
+    within(got, want, tol, "d_logits")
+
+
+@pytest.mark.parametrize("case", CASES, ids=IDS)
+def test_parity(case):
+    rows, vocab, dtype, top, entropy, scale, gap, first = case
+    x, x_buffer, token, d_logp, d_entropy = make(case, seed=rows * 7 + vocab)
+    d = lib.lp_desc_create(lib.LpParams(rows, vocab, dtype, top, entropy, scale))
+    print(lib.lp_desc_kernel_names(d), flush=True)
+    ws_bytes = lib.lp_desc_workspace_bytes(d)
+    ws = torch.full((ws_bytes // 4 + 64,), math.nan, device=DEV)
+    nan = lambda *shape: torch.full(shape, math.nan, device=DEV)
+    logp, h, stats = nan(rows), nan(rows) if entropy else None, nan(rows, 4)
+    top_logp = nan(rows, top) if top else None
+    top_token = torch.full((rows, top), -7, device=DEV, dtype=torch.int32) if top else None
+    lib.lp_forward(d, x, token, logp, h, stats, top_logp, top_token, ws[:(ws_bytes + 3) // 4])
+    assert torch.isnan(ws[(ws_bytes + 3) // 4:]).all()
+    want_logp, want_h = tokens.log_probs(x, scale)
+    check_rows(want_logp, want_h, logp, h, token, vocab)
+    if top:
+        index = tokens.top_tokens(x, top)
+        assert torch.equal(top_token.long(), index)
+        want = want_logp.gather(1, index)
+        within(top_logp, want, U * (256 + 4 * want.abs().nan_to_num(0, 0, 0)), "top_logp")
+
+    g, g_buffer = spaced(nan(rows, vocab), dtype, gap // 2, (first + 1) % 4)
+    lib.lp_backward(d, x, token, stats, d_logp, d_entropy, g)
+    check_gradient(case, x, token, d_logp, d_entropy, g)
+    assert untouched(g, g_buffer)
+
+    g2, g2_buffer = spaced(nan(rows, vocab), dtype, gap, first)
+    logp2, h2 = nan(rows), nan(rows) if entropy else None
+    lib.lp_forward_backward(d, x, token, d_logp, d_entropy, logp2, h2, g2, ws)
+    check_rows(want_logp, want_h, logp2, h2, token, vocab)
+    check_gradient(case, x, token, d_logp, d_entropy, g2)
+    assert untouched(g2, g2_buffer)
+
+    # equal calls, equal bits; what is not wanted is left out
+    g3 = torch.empty_like(g2)
+    lib.lp_forward_backward(d, x, token, d_logp, d_entropy, None, None, g3, ws)
+    assert torch.equal(g3, g2)
+    # in place
+    before = x.clone()
+    lib.lp_forward_backward(d, x, token, d_logp, d_entropy, logp2, h2, x, ws)
+    assert torch.equal(x, g2) and untouched(x, x_buffer)
+    check_rows(want_logp, want_h, logp2, h2, token, vocab)
+    x.copy_(before)
+    lib.lp_backward(d, x, token, stats, d_logp, d_entropy, x)
+    assert torch.equal(x, g) and untouched(x, x_buffer)
+
+
+@pytest.mark.parametrize("rows,vocab,dtype", [(6, 300, BF16), (6, 9000, F32), (6, 3000, F16), (260, 17000, BF16), (256, 100000, F32)])
+def test_not_a_number_and_infinity_reach_the_whole_row_and_no_other(rows, vocab, dtype):
+    x = torch.randn((rows, vocab), device=DEV).to(dtype)
+    x[1, vocab // 3] = math.nan
+    x[2, vocab - 1] = INF
+    x[3] = math.nan
+    x[4, 0], x[4, 1:] = -math.nan, -INF
+    token = torch.zeros(rows, dtype=torch.int32, device=DEV)
+    d = lib.lp_desc_create(lib.LpParams(rows, vocab, dtype, 4, 1))
+    ws = torch.empty(lib.lp_desc_workspace_bytes(d) // 4 + 1, device=DEV)
+    logp, h, stats = torch.empty(rows, device=DEV), torch.empty(rows, device=DEV), torch.empty((rows, 4), device=DEV)
+    tl, tt = torch.empty((rows, 4), device=DEV), torch.empty((rows, 4), device=DEV, dtype=torch.int32)
+    lib.lp_forward(d, x, token, logp, h, stats, tl, tt, ws)
+    bad = [1, 2, 3, 4]
+    good = [0] + list(range(5, rows))
+    assert torch.isnan(logp[bad]).all() and torch.isnan(h[bad]).all() and torch.isnan(tl[bad]).all()
+    assert torch.isfinite(logp[good]).all() and torch.isfinite(h[good]).all() and torch.isfinite(tl[good]).all()
+    assert torch.equal(tt.long(), tokens.top_tokens(x, 4))
+    w = torch.ones(rows, device=DEV)
+    g, g2 = torch.empty_like(x), torch.empty_like(x)
+    lib.lp_backward(d, x, token, stats, w, w, g)
+    lib.lp_forward_backward(d, x, token, w, w, logp, h, g2, ws)
+    for t in (g, g2):
+        assert torch.isnan(t[bad]).all() and torch.isfinite(t[good]).all()
+
+
+def test_gradient_against_differences():
+    """Central differences of logp and entropy as the library itself gives them, fp32: a step of 2^-6 leaves h^2 / 6 of a third
+    derivative that is at most 2 (4e-5 of |w| + |u|), and the values' own error over the step, 2^-24 600 / 2^-6 (2.3e-3 for these sizes)."""
+    rows, vocab, step = 8, 40, 2.0 ** -6
+    x = torch.randn((rows, vocab), device=DEV)
+    token = torch.arange(rows, device=DEV, dtype=torch.int32)
+    w, u = torch.randn(rows, device=DEV), torch.randn(rows, device=DEV)
+    one = lib.lp_desc_create(lib.LpParams(rows, vocab, F32, 0, 1))
+    g = torch.empty_like(x)
+    lib.lp_forward_backward(one, x, token, w, u, None, None, g)
+    many = lib.lp_desc_create(lib.LpParams(rows * vocab, vocab, F32, 0, 1))
+
+    def loss(sign):
+        moved = x.repeat_interleave(vocab, 0) + sign * step * torch.eye(vocab, device=DEV).repeat(rows, 1)
+        logp, h = torch.empty(rows * vocab, device=DEV), torch.empty(rows * vocab, device=DEV)
+        lib.lp_forward(many, moved, token.repeat_interleave(vocab), logp, h)
+        return (logp.double().view(rows, vocab) * w[:, None] + h.double().view(rows, vocab) * u[:, None])
+
+    difference = (loss(1) - loss(-1)) / (2 * step)
+    assert float((difference - g.double()).abs().max()) < 3e-3 * float(w.abs().max() + u.abs().max())
+
+
+def test_far_rows():
+    """Rows whose offset passes 2^31 elements."""
+    vocab, stride, rows = 500, (1 << 30) + 24, 3
+    buffer = torch.empty(stride * (rows - 1) + vocab, device=DEV, dtype=BF16)
+    x = buffer.as_strided((rows, vocab), (stride, 1))
+    x.copy_(torch.randn((rows, vocab), device=DEV))
+    token = torch.tensor([3, 499, 7], device=DEV, dtype=torch.int32)
+    w = torch.ones(rows, device=DEV)
+    d = lib.lp_desc_create(lib.LpParams(rows, vocab, BF16, 3, 1))
+    logp, h, stats = torch.empty(rows, device=DEV), torch.empty(rows, device=DEV), torch.empty((rows, 4), device=DEV)
+    tl, tt = torch.empty((rows, 3), device=DEV), torch.empty((rows, 3), device=DEV, dtype=torch.int32)
+    lib.lp_forward(d, x, token, logp, h, stats, tl, tt)
+    check_rows(*tokens.log_probs(x), logp, h, token, vocab)
+    assert torch.equal(tt.long(), tokens.top_tokens(x, 3))
+    case = (rows, vocab, BF16, 3, 1, 1.0, 0, 0)
+    before = x.clone()
+    lib.lp_backward(d, x, token, stats, w, None, x)
+    check_gradient(case, before, token, w, None, x)
+    x.copy_(before)
+    lib.lp_forward_backward(d, x, token, w, w, None, None, x)
+    check_gradient(case, before, token, w, w, x)
+
+
+@pytest.mark.parametrize("rows,vocab", [(300, 1000), (3, 40000)])
+def test_on_another_stream_and_in_a_graph(rows, vocab):
+    """Captured once; replayed with new inputs, eager calls of the same buffers in between."""
+    case = (rows, vocab, BF16, 5, 1, 1.0, 0, 0)
+    x, _, token, w, u = make(case, seed=1)
+    d = lib.lp_desc_create(lib.LpParams(rows, vocab, BF16, 5, 1))
+    ws = torch.empty(lib.lp_desc_workspace_bytes(d) // 4 + 1, device=DEV)
+    logp, h = torch.empty(rows, device=DEV), torch.empty(rows, device=DEV)
+    tl, tt = torch.empty((rows, 5), device=DEV), torch.empty((rows, 5), device=DEV, dtype=torch.int32)
+    g = torch.empty_like(x)
+
+    def step(stream=None):
+        lib.lp_forward(d, x, token, logp, h, None, tl, tt, ws, stream)
+        lib.lp_forward_backward(d, x, token, w, u, None, None, g, ws, stream)
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    step(side)
+    side.synchronize()
+    first = [t.clone() for t in (logp, h, tl, tt, g)]
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for seed in (2, 3, 4):
+        x.copy_(make(case, seed)[0])
+        graph.replay()
+        replayed = [t.clone() for t in (logp, h, tl, tt, g)]
+        step()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(replayed, (logp, h, tl, tt, g)))
+    x.copy_(make(case, 1)[0])
+    graph.replay()
+    assert all(torch.equal(a, b) for a, b in zip(first, (logp, h, tl, tt, g)))
+
+
+def test_refusals_on_the_device():
+    d = lib.lp_desc_create(lib.LpParams(4, 9000, BF16, 2, 1))
+    x = torch.zeros((4, 9000), device=DEV, dtype=BF16)
+    token = torch.zeros(4, device=DEV, dtype=torch.int32)
+    f = lambda *s: torch.empty(s, device=DEV)
+    tl, tt, ws = f(4, 2), torch.empty((4, 2), device=DEV, dtype=torch.int32), f(lib.lp_desc_workspace_bytes(d) // 4)
+    ok = lambda **k: lib.lp_forward(d, **{**dict(logits=x, token=token, logp=f(4), entropy=f(4), stats=None, top_logp=tl, top_token=tt, ws=ws), **k})
+    ok()
+    for wrong, error in ((dict(logits=x.float()), TypeError), (dict(logits=x.t()), ValueError), (dict(logits=x[:, :8999]), ValueError),
+                         (dict(logits=torch.zeros((9000, 4), device=DEV, dtype=BF16).t()), TypeError),
+                         (dict(logits=x[:1].expand(4, 9000)), TypeError), (dict(logits=x.cpu()), TypeError),
+                         (dict(token=token.long()), TypeError), (dict(token=token[:3]), ValueError), (dict(logp=f(5)), ValueError),
+                         (dict(token=None), lib.ConvError), (dict(top_logp=None), lib.ConvError), (dict(ws=None), lib.ConvError),
+                         (dict(ws=ws[:-1]), lib.ConvError), (dict(stats=f(4, 3)), ValueError)):
+        with pytest.raises(error):
+            ok(**wrong)
+    plain = lib.lp_desc_create(lib.LpParams(4, 9000, BF16, 0, 0))
+    with pytest.raises(lib.ConvError):
+        lib.lp_forward(plain, x, token, f(4), f(4), None, None, None, ws)
+    with pytest.raises(lib.ConvError):
+        lib.lp_backward(plain, x, token, f(4, 4), f(4), f(4), torch.empty_like(x))

@@ -1,0 +1,169 @@
+"""Host side of the token policy's operators, without a device: exported names, descriptors, refusals."""
+import ctypes
+import os
+import re
+
+import pytest
+import torch
+
+import paper_1810_02272_amd as lib
+from paper_1810_02272_amd import binding, gn_binding, lp_binding, q4_binding
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+F32, F16, BF16, F64 = torch.float32, torch.float16, torch.bfloat16, torch.float64
+fake = ctypes.c_void_p(256)  # never dereferenced: every call below returns before any launch
+EINVAL, ESHAPE, EWORKSPACE, OK = binding.CONV_EINVAL, binding.CONV_ESHAPE, binding.CONV_EWORKSPACE, binding.CONV_OK
+
+
+@pytest.mark.parametrize("prefix,names", [
+    ("lp", {"desc_create", "desc_destroy", "desc_workspace_bytes", "desc_kernel_names", "forward", "backward", "forward_backward"}),
+    ("gn", {"desc_create", "desc_destroy", "desc_workspace_bytes", "desc_kernel_names", "clip"}),
+    ("q4", {"desc_create", "desc_destroy", "desc_workspace_bytes", "desc_packed_bytes", "desc_kernel_names", "pack", "forward"})])
+def test_every_declared_symbol_is_exported_and_bound(prefix, names):
+    header = open(os.path.join(ROOT, "include", f"mi355{prefix}.h")).read()
+    header = re.sub(r"/\*.*?\*/", "", header, flags=re.S)
+    declared = set(re.findall(rf"\b({prefix}_[a-z0-9_]+)\s*\(", header))
+    assert declared == {f"{prefix}_{n}" for n in names}
+    c = ctypes.CDLL(lib.library_path())
+    for name in declared:
+        assert hasattr(c, name) and hasattr(lib, name), name
+
+
+# ---- log probabilities ----
+
+@pytest.mark.parametrize("bad,status", [(dict(rows=-1), EINVAL), (dict(vocab=0), EINVAL), (dict(top=-1), EINVAL), (dict(top=65), EINVAL),
+                                        (dict(vocab=3, top=4), EINVAL), (dict(entropy=2), EINVAL), (dict(scale=0.0), EINVAL),
+                                        (dict(scale=-1.0), EINVAL), (dict(scale=float("nan")), EINVAL), (dict(scale=float("inf")), EINVAL),
+                                        (dict(vocab=1 << 30), ESHAPE)])
+def test_lp_parameters(bad, status):
+    with pytest.raises(lib.ConvError) as e:
+        lib.lp_desc_create(lib.LpParams(**{**dict(rows=4, vocab=100, dtype=F32, top=2, entropy=1, scale=1.0), **bad}))
+    assert e.value.status == status
+    with pytest.raises(TypeError):
+        lib.lp_desc_create(lib.LpParams(4, 100, F64))
+    with pytest.raises(TypeError):
+        lib.lp_desc_create(lib.LpParams(4, 100, torch.int32))
+
+
+def test_lp_calls():
+    c = lp_binding._load()
+    d = lib.lp_desc_create(lib.LpParams(4, 100, F32, 2, 1))
+    plain = lib.lp_desc_create(lib.LpParams(4, 100, F32, 0, 0))
+    parts = lib.lp_desc_create(lib.LpParams(1, 100000, BF16, 2, 1))
+    none = lib.lp_desc_create(lib.LpParams(0, 100, F32, 2, 1))
+    assert lib.lp_desc_workspace_bytes(parts) > 0 and "parts" in lib.lp_desc_kernel_names(parts)
+    assert lib.lp_desc_workspace_bytes(d) == 0
+    f = fake
+    assert c.lp_desc_create(None, None) == EINVAL and c.lp_desc_destroy(None) == EINVAL and c.lp_desc_workspace_bytes(None, None) == EINVAL
+    assert c.lp_desc_kernel_names(None) == b""
+    assert c.lp_forward(None, f, 100, f, f, f, f, f, f, f, 0, None) == EINVAL
+    assert c.lp_forward(d.handle, None, 100, f, f, f, f, f, f, f, 0, None) == EINVAL      # no logits
+    assert c.lp_forward(d.handle, f, 99, f, f, f, f, f, f, f, 0, None) == EINVAL         # rows overlap
+    assert c.lp_forward(d.handle, f, 100, None, f, f, f, f, f, f, 0, None) == EINVAL     # logp of what
+    assert c.lp_forward(d.handle, f, 100, f, None, f, f, f, f, f, 0, None) == EINVAL
+    assert c.lp_forward(d.handle, f, 100, f, f, f, f, None, f, f, 0, None) == EINVAL     # alternatives: both or neither, as described
+    assert c.lp_forward(d.handle, f, 100, f, f, f, f, f, None, f, 0, None) == EINVAL
+    assert c.lp_forward(d.handle, f, 100, f, f, f, f, None, None, f, 0, None) == EINVAL
+    assert c.lp_forward(plain.handle, f, 100, f, f, None, f, f, f, f, 0, None) == EINVAL
+    assert c.lp_forward(plain.handle, f, 100, f, f, f, f, None, None, f, 0, None) == EINVAL  # entropy of a descriptor without
+    assert c.lp_forward(parts.handle, f, 100000, f, f, f, f, f, f, None, 0, None) == EWORKSPACE
+    assert c.lp_forward(parts.handle, f, 100000, f, f, f, f, f, f, f, 8, None) == EWORKSPACE
+    assert c.lp_forward(none.handle, None, 0, None, None, None, None, None, None, None, 0, None) == OK
+    assert c.lp_backward(None, f, 100, f, f, f, f, f, 100, None) == EINVAL
+    for hole in range(7):
+        args = [f, 100, f, f, f, f, f, 100]
+        at = [0, 1, 2, 3, 4, 6, 7][hole]
+        args[at] = 99 if at in (1, 7) else None
+        assert c.lp_backward(d.handle, *args, None) == EINVAL, at
+    assert c.lp_backward(plain.handle, f, 100, f, f, f, f, f, 100, None) == EINVAL       # d_entropy of a descriptor without
+    assert c.lp_backward(none.handle, None, 0, None, None, None, None, None, 0, None) == OK
+    assert c.lp_forward_backward(None, f, 100, f, f, f, f, f, f, 100, f, 0, None) == EINVAL
+    for at in (0, 1, 2, 3, 7, 8):
+        args = [f, 100, f, f, f, f, f, f, 100]
+        args[at] = 99 if at in (1, 8) else None
+        if at == 7:
+            args[7] = None
+        assert c.lp_forward_backward(d.handle, *args, f, 0, None) == EINVAL, at
+    assert c.lp_forward_backward(plain.handle, f, 100, f, f, f, f, None, f, 100, f, 0, None) == EINVAL
+    assert c.lp_forward_backward(plain.handle, f, 100, f, f, None, f, f, f, 100, f, 0, None) == EINVAL
+    assert c.lp_forward_backward(parts.handle, f, 100000, f, f, f, f, f, f, 100000, None, 0, None) == EWORKSPACE
+
+
+def test_lp_refuses_cpu_tensors():
+    d = lib.lp_desc_create(lib.LpParams(2, 10, F32, 0, 0))
+    x, t = torch.zeros(2, 10), torch.zeros(2, dtype=torch.int32)
+    with pytest.raises(TypeError):
+        lib.lp_forward(d, x, t, torch.zeros(2))
+    with pytest.raises(TypeError):
+        lib.lp_forward_backward(d, x, t, torch.zeros(2), None, None, None, torch.zeros(2, 10))
+
+
+# ---- clipping ----
+
+def test_gn_parameters_and_calls():
+    c = gn_binding._load()
+    for counts, dtypes in (([-1], [F32]), ([1 << 40], [F32]), ([1 << 39, 1 << 39], [F32, F32])):
+        with pytest.raises(lib.ConvError):
+            lib.gn_desc_create(lib.GnParams(counts, dtypes))
+    with pytest.raises(lib.ConvError) as e:
+        lib.gn_desc_create(lib.GnParams([1] * ((1 << 18) + 1), [F32] * ((1 << 18) + 1)))
+    assert e.value.status == ESHAPE
+    with pytest.raises(TypeError):
+        lib.gn_desc_create(lib.GnParams([1], [torch.int32]))
+    with pytest.raises(ValueError):
+        lib.GnParams([1, 2], [F32])
+    for params in (None, gn_binding._CParams(-1, None, None), gn_binding._CParams(2, None, None)):
+        out = ctypes.c_void_p()
+        assert c.gn_desc_create(ctypes.byref(out), ctypes.byref(params) if params else None) == EINVAL
+    bad = gn_binding._CParams(1, (ctypes.c_int64 * 1)(3), (ctypes.c_int32 * 1)(4))
+    assert c.gn_desc_create(ctypes.byref(ctypes.c_void_p()), ctypes.byref(bad)) == EINVAL
+    d = lib.gn_desc_create(lib.GnParams([3, 0], [F32, F64]))
+    bytes_ = lib.gn_desc_workspace_bytes(d)
+    two = (ctypes.c_void_p * 2)(256, None)
+    hole = (ctypes.c_void_p * 2)(None, 256)
+    assert c.gn_desc_destroy(None) == EINVAL and c.gn_desc_workspace_bytes(None, None) == EINVAL and c.gn_desc_kernel_names(None) == b""
+    assert c.gn_clip(None, two, 1.0, two, None, fake, bytes_, None) == EINVAL
+    assert c.gn_clip(d.handle, None, 1.0, two, None, fake, bytes_, None) == EINVAL
+    assert c.gn_clip(d.handle, two, 1.0, None, None, fake, bytes_, None) == EINVAL
+    assert c.gn_clip(d.handle, hole, 1.0, two, None, fake, bytes_, None) == EINVAL
+    assert c.gn_clip(d.handle, two, 1.0, hole, None, fake, bytes_, None) == EINVAL
+    assert c.gn_clip(d.handle, two, -1.0, two, None, fake, bytes_, None) == EINVAL
+    assert c.gn_clip(d.handle, two, float("nan"), two, None, fake, bytes_, None) == EINVAL
+    assert c.gn_clip(d.handle, two, 1.0, two, None, None, 0, None) == EWORKSPACE
+    assert c.gn_clip(d.handle, two, 1.0, two, None, fake, bytes_ - 1, None) == EWORKSPACE
+    with pytest.raises(TypeError):
+        lib.gn_clip(d, [torch.zeros(3), torch.zeros(0, dtype=F64)], 1.0)
+
+
+# ---- 4-bit weights ----
+
+@pytest.mark.parametrize("bad,status", [(dict(m=-1), EINVAL), (dict(k=0), EINVAL), (dict(num_output=0), EINVAL), (dict(group=16), EINVAL),
+                                        (dict(group=0), EINVAL), (dict(bias_term=2), EINVAL), (dict(relu=-1), EINVAL),
+                                        (dict(k=1 << 15, num_output=1 << 15), ESHAPE), (dict(m=1 << 20, k=1 << 10), ESHAPE),
+                                        (dict(m=1 << 20, num_output=1 << 10), ESHAPE)])
+def test_q4_parameters(bad, status):
+    with pytest.raises(lib.ConvError) as e:
+        lib.q4_desc_create(lib.Q4Params(**{**dict(m=2, k=64, num_output=8, dtype=BF16, group=32, bias_term=0, relu=0), **bad}))
+    assert e.value.status == status
+    with pytest.raises(TypeError):
+        lib.q4_desc_create(lib.Q4Params(2, 64, 8, F64))
+
+
+def test_q4_calls():
+    c = q4_binding._load()
+    d = lib.q4_desc_create(lib.Q4Params(2, 64, 8, BF16, 32, 1, 0))
+    plain = lib.q4_desc_create(lib.Q4Params(2, 64, 8, BF16, 32, 0, 0))
+    none = lib.q4_desc_create(lib.Q4Params(0, 64, 8, BF16, 32, 0, 0))
+    assert lib.q4_desc_packed_bytes(d) >= 8 * 64 // 2 and lib.q4_desc_packed_bytes(d) == lib.q4_desc_packed_bytes(none)
+    f, odd = fake, ctypes.c_void_p(264)
+    assert c.q4_desc_create(None, None) == EINVAL and c.q4_desc_destroy(None) == EINVAL
+    assert c.q4_desc_packed_bytes(None, None) == EINVAL and c.q4_desc_workspace_bytes(None, None) == EINVAL
+    assert c.q4_desc_kernel_names(None) == b""
+    assert c.q4_pack(None, f, f, f, None) == EINVAL
+    for args in ((None, f, f), (f, None, f), (f, f, None), (f, f, odd)):
+        assert c.q4_pack(d.handle, *args, None) == EINVAL
+    assert c.q4_forward(None, f, f, f, f, f, 1 << 30, None) == EINVAL
+    for args in ((None, f, f, f), (f, None, f, f), (f, f, None, f), (f, f, f, None), (f, odd, f, f)):
+        assert c.q4_forward(d.handle, *args, f, 1 << 30, None) == EINVAL
+    assert c.q4_forward(plain.handle, f, f, f, f, f, 1 << 30, None) == EINVAL  # bias unexpected
+    assert c.q4_forward(none.handle, None, f, None, None, None, 0, None) == OK
