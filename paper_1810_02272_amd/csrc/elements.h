@@ -93,6 +93,12 @@ __device__ __forceinline__ void store_vec(typename E::T* at, const u32x4& v) {
   reinterpret_cast<typename E::Mem*>(at)->v = v;
 }
 
+// The same for what is not read again soon: it goes around the last-level cache.
+template <class E>
+__device__ __forceinline__ void stream_vec(typename E::T* at, const u32x4& v) {
+  __builtin_nontemporal_store(v, &reinterpret_cast<typename E::Mem*>(at)->v);
+}
+
 inline int dtype_bytes(int dtype) { return dtype == MI355_F64 ? 8 : dtype == MI355_F32 ? 4 : 2; }
 
 }  // namespace mi355conv

@@ -19,6 +19,7 @@
 #include "elements.h"
 #include "internal.h"
 #include "mi355lp.h"
+#include "wave_ops.h"
 
 struct lp_desc {
   lp_params_t p;
@@ -119,24 +120,12 @@ __device__ __forceinline__ GradScale grad_scale(const RowStat& r, float w, float
   return g;
 }
 
-__device__ __forceinline__ float wave_max(float v) {
-#pragma unroll
-  for (int d = 32; d >= 1; d >>= 1) v = fmaxf(v, __shfl_xor(v, d, 64));
-  return v;
-}
-
-__device__ __forceinline__ float wave_add(float v) {
-#pragma unroll
-  for (int d = 32; d >= 1; d >>= 1) v += __shfl_xor(v, d, 64);
-  return v;
-}
-
 // The wave's lanes' sums in one, in every lane.
 __device__ __forceinline__ Sums wave_merge(float m, float s, float s2, float c) {
-  Sums a = {wave_max(m), 0.f, 0.f};
+  Sums a = {wave_most(m), 0.f, 0.f};
   add_part(a, reference(a.m, c), beyond(a.m, c), c, m, s, s2);
-  a.s = wave_add(a.s);
-  a.s2 = wave_add(a.s2);
+  a.s = wave_sum(a.s);
+  a.s2 = wave_sum(a.s2);
   return a;
 }
 
@@ -203,11 +192,19 @@ __device__ __forceinline__ u32x4 row_vec(const typename E::T* row, int v, int n)
   return E::pack(x);
 }
 
-template <class E>
+template <class E, bool STREAM>
+__device__ __forceinline__ void put_vec(typename E::T* at, const u32x4& v) {
+  if constexpr (STREAM)
+    stream_vec<E>(at, v);
+  else
+    store_vec<E>(at, v);
+}
+
+template <class E, bool STREAM>
 __device__ __forceinline__ void store_row_vec(typename E::T* row, int v, int n, const float (&x)[E::VEC]) {
   const Slot<E> at = slot_of<E>(v, n);
   if (at.lo == 0) {
-    store_vec<E>(row + at.base, E::pack(x));
+    put_vec<E, STREAM>(row + at.base, E::pack(x));
     return;
   }
 #pragma unroll
@@ -260,8 +257,36 @@ __device__ __forceinline__ void forget(u32x4 (&r)[NV]) {
 }
 
 __device__ __forceinline__ int forget(int uniform) {
+  uniform = __builtin_amdgcn_readfirstlane(uniform);
   asm volatile("" : "+s"(uniform));
   return uniform;
+}
+
+// Keeps the scheduler from working on many vectors side by side, which takes more registers than there are.
+__device__ __forceinline__ void one_by_one() { __builtin_amdgcn_sched_barrier(0); }
+
+// f(vector, its number) for the thread's vectors of a row that are not among the NV in registers, four loads at a time.
+template <class E, int THREADS, int NV, class F>
+__device__ __forceinline__ void beyond_registers(const typename E::T* row, int full, int tid, F&& f) {
+  for (int v0 = NV * THREADS; v0 < full; v0 += 4 * THREADS) {
+    u32x4 r[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int v = v0 + j * THREADS + tid;
+      if (v < full) r[j] = load_vec<E>(row + (int64_t)v * E::VEC);
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int v = v0 + j * THREADS + tid;
+      if (v < full) f(r[j], v);
+      one_by_one();
+    }
+  }
+}
+
+__device__ __forceinline__ int forget_lane(int per_lane) {
+  asm volatile("" : "+v"(per_lane));
+  return per_lane;
 }
 
 template <int THREADS>
@@ -272,57 +297,78 @@ __device__ __forceinline__ void team_sync() {
     __syncthreads();
 }
 
-// Vectors that hold a candidate for a team's alternatives, and candidates.  Where there are more, the alternatives are found one by
-// one.
+// Vectors that hold a candidate for a team's alternatives.  Where there are more, the alternatives are found one by one.
 template <int THREADS>
-constexpr int kHits = THREADS == 64 ? 128 : 256;
-template <int THREADS>
-constexpr int kCand = 2 * kHits<THREADS>;
+constexpr int kHits = THREADS == 64 ? 64 : 256;
 
 template <int THREADS>
 struct TeamLds {
   u32x4 hit[kHits<THREADS>];
+  uint64_t cand[kHits<THREADS> * 8];
   float4 sums[THREADS / 64];
   int hit_at[kHits<THREADS>];
   uint32_t group_top[64];
   float bound, at_token;
-  uint32_t hits, count;
-  uint64_t cand[kCand<THREADS>];
+  uint32_t hits;
   uint64_t best[THREADS / 64];
 };
 
+// The greatest number that at least `top` of the wave's keys reach, its lower 16 bits cut off: a bound from below all the same.
+__device__ __forceinline__ uint32_t top_bound(uint32_t key, int top) {
+  uint32_t bound = 0;
+#pragma unroll
+  for (int bit = 31; bit >= 16; --bit) {
+    const uint32_t with = bound | 1u << bit;
+    if (__builtin_popcountll(__ballot(key >= with)) >= top) bound = with;
+  }
+  return bound;
+}
+
+// A wave ranks `count` different entries by counting those above each.
+template <class Out>
+__device__ __forceinline__ void rank_entries(const uint64_t* cand, int count, int top, int lane, Out&& out) {
+  if (count <= 64) {
+    const uint64_t mine = lane < count ? cand[lane] : 0;
+    int rank = 0;
+#pragma unroll 4
+    for (int o = 0; o < count; ++o) rank += read_lane(mine, o) > mine ? 1 : 0;
+    if (lane < count && rank < top) out(rank, mine);
+  } else {
+    for (int i = lane; i < count; i += 64) {
+      const uint64_t mine = cand[i];
+      int rank = 0;
+#pragma unroll 8
+      for (int o = 0; o < count; ++o) rank += cand[o] > mine ? 1 : 0;
+      if (rank < top) out(rank, mine);
+    }
+  }
+}
+
 // The `top` greatest entries of the row part [first, first + n), out(rank, entry) for each; 0 stands for none.
 // The top-th greatest of 64 groups' maxima bounds the top-th greatest logit from below, so few others pass it: of 128256 normal
-// logits, 24 for 20.  Each that passes is ranked by counting those above it.  Where too many pass (equal logits, all but a few
-// banned), each place is found by a pass over the row.
+// logits, 24 for 20.  The vectors that hold one are put aside, and one wave ranks the logits in them that pass by counting those above
+// each.  Where too many vectors do (equal logits, all but a few banned), each place is found by a pass over the row.
+// m: the thread's maximum; odd: whether it has met a NaN, which no maximum shows.
 template <class E, int THREADS, int NV, class Out>
-__device__ __forceinline__ void team_top(TeamLds<THREADS>& lds, const u32x4 (&r)[NV], const u32x4& tail, const typename E::T* row, int first, int n, int top,
-                                         float m, int tid, Out&& out) {
+__device__ __forceinline__ void team_top(TeamLds<THREADS>& lds, const u32x4 (&r)[NV], const u32x4& tail, const typename E::T* row, int first,
+                                         int n, int top, float m, bool odd, int tid, Out&& out) {
   constexpr int VEC = E::VEC, GROUP = THREADS / 64;
   const int nv = (n + VEC - 1) / VEC, full = n / VEC, lane = tid & 63;
-  float gm = m;
-#pragma unroll
-  for (int d = 1; d < GROUP; d <<= 1) gm = fmaxf(gm, __shfl_xor(gm, d, 64));
+  const float gm = group_most<GROUP>(m);
   if (tid % GROUP == 0) lds.group_top[tid / GROUP] = order_key(gm);
-  if (tid == 0) lds.hits = lds.count = 0;
+  if (tid == 0) lds.hits = 0;
   team_sync<THREADS>();
   if (THREADS == 64 || tid < 64) {  // the leading 16 bits of the top-th greatest: a bound all the same
-    const uint32_t k = lds.group_top[lane];
-    uint32_t bound = 0;
-#pragma unroll
-    for (int bit = 31; bit >= 16; --bit) {
-      const uint32_t with = bound | 1u << bit;
-      if (__builtin_popcountll(__ballot(k >= with)) >= top) bound = with;
-    }
+    const uint32_t bound = top_bound(lds.group_top[lane], top);
     if (lane == 0) lds.bound = bound <= 0x007FFFFFu ? -INFINITY : key_value(bound);  // key of -inf and the unused ones below it
   }
   team_sync<THREADS>();
   const float bound = lds.bound;
   auto look = [&](const u32x4& vec, int v) {
-    bool any = false;
+    float most = E::get(vec, 0);
 #pragma unroll
-    for (int i = 0; i < VEC; ++i) any |= !(E::get(vec, i) < bound);
-    if (any) {
+    for (int i = 1; i < VEC; ++i) most = __builtin_elementwise_maximum(most, E::get(vec, i));  // NaN if there is one
+    if (!(most < bound)) {
       const uint32_t place = atomicAdd(&lds.hits, 1u);
       if (place < (uint32_t)kHits<THREADS>) {
         lds.hit[place] = vec;
@@ -330,36 +376,38 @@ __device__ __forceinline__ void team_top(TeamLds<THREADS>& lds, const u32x4 (&r)
       }
     }
   };
-  {
-    const int full_ = forget(full);
+  if (!(m < bound) || odd) {
+    const int full_ = forget(full), tid_ = forget_lane(tid);
 #pragma unroll
-    for (int j = 0; j < NV; ++j)
-      if (j * THREADS < full_ && j * THREADS + tid < full_) look(r[j], j * THREADS + tid);
+    for (int j = 0; j < NV; ++j) {
+      if (j * THREADS < full_ && j * THREADS + tid_ < full_) look(r[j], j * THREADS + tid_);
+      one_by_one();
+    }
+    beyond_registers<E, THREADS, NV>(row, full, tid, look);
+    if (full < nv && tid == 0) look(tail, full);
   }
-  for (int v = NV * THREADS + tid; v < full; v += THREADS) look(load_vec<E>(row + v * VEC), v);
-  if (full < nv && tid == 0) look(tail, full);
   team_sync<THREADS>();
-  const int hits = (int)lds.hits;
+  const int hits = __builtin_amdgcn_readfirstlane((int)lds.hits);
   if (hits <= kHits<THREADS>) {
-    for (int i = tid; i < hits * VEC; i += THREADS) {
-      const float x = E::to_float(reinterpret_cast<const typename E::T*>(lds.hit)[i]);
-      const Slot<E> at = slot_of<E>(lds.hit_at[i / VEC], n);
-      if (!(x < bound) && i % VEC >= at.lo) {
-        const uint32_t place = atomicAdd(&lds.count, 1u);
-        if (place < (uint32_t)kCand<THREADS>) lds.cand[place] = entry_of(x, first + at.base + i % VEC);
+    if (THREADS > 64 && tid >= 64) return;
+    int count = 0;
+    for (int i0 = 0; i0 < hits * VEC; i0 += 64) {
+      const int i = i0 + lane;
+      bool pass = false;
+      uint64_t entry = 0;
+      if (i < hits * VEC) {
+        const float x = E::to_float(reinterpret_cast<const typename E::T*>(lds.hit)[i]);
+        const Slot<E> at = slot_of<E>(lds.hit_at[i / VEC], n);
+        pass = !(x < bound) && i % VEC >= at.lo;
+        entry = entry_of(x, first + at.base + i % VEC);
       }
+      const uint64_t mask = __ballot(pass);
+      if (pass) lds.cand[count + __builtin_popcountll(mask & ((1ull << lane) - 1))] = entry;
+      count += (int)__builtin_popcountll(mask);
     }
-    team_sync<THREADS>();
-  }
-  const int count = (int)lds.count;
-  if (hits <= kHits<THREADS> && count <= kCand<THREADS>) {
-    for (int i = tid; i < count; i += THREADS) {
-      const uint64_t mine = lds.cand[i];
-      int rank = 0;
-      for (int o = 0; o < count; ++o) rank += lds.cand[o] > mine ? 1 : 0;
-      if (rank < top) out(rank, mine);
-    }
-    for (int i = count + tid; i < top; i += THREADS) out(i, (uint64_t)0);  // a part shorter than that
+    wave_sync();
+    rank_entries(lds.cand, count, top, lane, out);
+    for (int i = count + lane; i < top; i += 64) out(i, (uint64_t)0);  // a part shorter than that
     return;
   }
   uint64_t last = ~(uint64_t)0;
@@ -394,15 +442,15 @@ enum Mode { kScore, kTrain, kPart };
 
 // A row (kPart: a part of one) is read once, into registers, up to NV vectors a thread; what is beyond them is read again by
 // whatever needs it again.  THREADS 64: a wave for each row, several in a workgroup.
-template <int DTYPE, int THREADS, int NV, Mode MODE, bool ENT>
-__global__ __launch_bounds__(THREADS == 64 ? 256 : THREADS) void lp_row_kernel(LpArgs a) {
+// STREAM: the gradient goes around the last-level cache.
+template <int DTYPE, int THREADS, int NV, Mode MODE, bool ENT, bool STREAM>
+__global__ __launch_bounds__(THREADS == 64 ? 256 : THREADS, THREADS == 64 ? 1 : 4) void lp_row_kernel(LpArgs a) {
   typedef Elem<DTYPE> E;
   typedef typename E::T T;
   constexpr int VEC = E::VEC, WAVES = THREADS / 64;
   __shared__ TeamLds<THREADS> team_lds[THREADS == 64 ? 4 : 1];
   TeamLds<THREADS>& lds = team_lds[THREADS == 64 ? threadIdx.x >> 6 : 0];
-  const int tid = THREADS == 64 ? threadIdx.x & 63 : threadIdx.x;
-  const int lane = tid & 63;
+  const int lane = threadIdx.x & 63;
   const int teams = THREADS == 64 ? (int)(gridDim.x * (blockDim.x >> 6)) : (int)gridDim.x;
   int item = THREADS == 64 ? (int)(blockIdx.x * (blockDim.x >> 6) + (threadIdx.x >> 6)) : (int)blockIdx.x;
   if constexpr (THREADS == 64) item = __builtin_amdgcn_readfirstlane(item);
@@ -410,7 +458,9 @@ __global__ __launch_bounds__(THREADS == 64 ? 256 : THREADS) void lp_row_kernel(L
   for (int64_t it = item; it < items; it += teams) {
     const int r_ = MODE == kPart ? (int)(it / a.splits) : (int)it;
     const int first = MODE == kPart ? (int)(it % a.splits) * a.seg : 0;
-    const int n = MODE == kPart ? min(a.seg, a.vocab - first) : a.vocab;
+    // (nothing that follows from these is worth a register from one row to the next)
+    const int n = forget(MODE == kPart ? min(a.seg, a.vocab - first) : a.vocab);
+    const int tid = forget_lane(THREADS == 64 ? threadIdx.x & 63 : threadIdx.x);
     const T* const row = static_cast<const T*>(a.logits) + (int64_t)r_ * a.stride + first;
     const int nv = (n + VEC - 1) / VEC, full = n / VEC;
     int token = -1;
@@ -433,8 +483,11 @@ __global__ __launch_bounds__(THREADS == 64 ? 256 : THREADS) void lp_row_kernel(L
     float m = -INFINITY, M = 0.f, s = 0.f, s2 = 0.f;
 #pragma unroll
     for (int j = 0; j < NV; ++j)
-      if (j * THREADS < full) add_vec<E, ENT>(r[j], a.c, m, M, s, s2);
-    for (int v = NV * THREADS + tid; v < full; v += THREADS) add_vec<E, ENT>(load_vec<E>(row + v * VEC), a.c, m, M, s, s2);
+      if (j * THREADS < full) {
+        add_vec<E, ENT>(r[j], a.c, m, M, s, s2);
+        one_by_one();
+      }
+    beyond_registers<E, THREADS, NV>(row, full, tid, [&](const u32x4& vec, int) { add_vec<E, ENT>(vec, a.c, m, M, s, s2); });
     if (full < nv) add_vec<E, ENT>(tail, a.c, m, M, s, s2);
 
     forget(r);
@@ -455,12 +508,12 @@ __global__ __launch_bounds__(THREADS == 64 ? 256 : THREADS) void lp_row_kernel(L
 #pragma unroll
         for (int i = 0; i < VEC; ++i) count += exp2_fast(E::get(vec, i) - sum.m);
       }
-      count = wave_add(count);
+      count = wave_sum(count);
       if constexpr (WAVES > 1) {
         __syncthreads();
         if (lane == 0) lds.sums[tid >> 6].x = count;
         __syncthreads();
-        count = wave_add(lane < WAVES ? lds.sums[lane].x : 0.f);
+        count = wave_sum(lane < WAVES ? lds.sums[lane].x : 0.f);
       }
       sum.s = count;
       sum.s2 = 0.f;
@@ -470,7 +523,7 @@ __global__ __launch_bounds__(THREADS == 64 ? 256 : THREADS) void lp_row_kernel(L
       if (tid == 0) a.parts[it] = make_float4(sum.m, sum.s, sum.s2, 0.f);
       if (a.top) {
         uint64_t* const to = a.cand + it * a.top;
-        team_top<E, THREADS, NV>(lds, r, tail, row, first, n, a.top, m, tid, [&](int rank, uint64_t e) { to[rank] = e; });
+        team_top<E, THREADS, NV>(lds, r, tail, row, first, n, a.top, m, s != s, tid, [&](int rank, uint64_t e) { to[rank] = e; });
       }
     } else {
       const RowStat st = finish(sum, a.c, a.scale);
@@ -483,7 +536,7 @@ __global__ __launch_bounds__(THREADS == 64 ? 256 : THREADS) void lp_row_kernel(L
         if (a.top) {
           float* const logp = a.top_logp + (int64_t)r_ * a.top;
           int32_t* const tok = a.top_token + (int64_t)r_ * a.top;
-          team_top<E, THREADS, NV>(lds, r, tail, row, 0, n, a.top, m, tid, [&](int rank, uint64_t e) {
+          team_top<E, THREADS, NV>(lds, r, tail, row, 0, n, a.top, m, s != s, tid, [&](int rank, uint64_t e) {
             logp[rank] = log_prob(st, key_value((uint32_t)(e >> 32)), a.scale);
             tok[rank] = (int32_t)(0xFFFFFFFFu - (uint32_t)e);
           });
@@ -492,24 +545,25 @@ __global__ __launch_bounds__(THREADS == 64 ? 256 : THREADS) void lp_row_kernel(L
         const float w = token >= 0 ? a.d_logp[r_] : 0.f, u = ENT && a.d_entropy ? a.d_entropy[r_] : 0.f;
         const GradScale g = grad_scale(st, w, u, a.scale);
         T* const to = static_cast<T*>(a.d_logits) + (int64_t)r_ * a.d_stride;
-        const int full_ = forget(full);
+        const int full_ = forget(full), tid_ = forget_lane(tid);
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
-          if (j * THREADS < full_ && j * THREADS + tid < full_) {
+          if (j * THREADS < full_ && j * THREADS + tid_ < full_) {
             float x[VEC];
             grad_vec<E, ENT>(r[j], st, g, x);
-            store_vec<E>(to + (j * THREADS + tid) * VEC, E::pack(x));
+            put_vec<E, STREAM>(to + (j * THREADS + tid_) * VEC, E::pack(x));
           }
+          one_by_one();
         }
-        for (int v = NV * THREADS + tid; v < full; v += THREADS) {
+        beyond_registers<E, THREADS, NV>(row, full, tid, [&](const u32x4& vec, int v) {
           float x[VEC];
-          grad_vec<E, ENT>(load_vec<E>(row + v * VEC), st, g, x);
-          store_vec<E>(to + v * VEC, E::pack(x));
-        }
+          grad_vec<E, ENT>(vec, st, g, x);
+          put_vec<E, STREAM>(to + (int64_t)v * VEC, E::pack(x));
+        });
         if (full < nv && tid == 0) {
           float x[VEC];
           grad_vec<E, ENT>(tail, st, g, x);
-          store_row_vec<E>(to, full, n, x);
+          store_row_vec<E, STREAM>(to, full, n, x);
         }
         // the token's own, by the thread that has just written it without
         if (token >= 0 && tid == (token < full * VEC ? token / VEC % THREADS : 0))
@@ -528,42 +582,58 @@ __device__ __forceinline__ Sums merge_parts(const float4* parts, int splits, int
 
 constexpr int kMaxSplits = 64;
 
-// A row's parts in one: a workgroup for each row.
+// A row's parts in one: a workgroup for each row.  Each part's alternatives are in order; the leading ones of all parts, 64 together, give a
+// bound as the groups' maxima do in team_top, and what passes it is ranked by one wave.
 template <int DTYPE, bool ENT>
 __global__ __launch_bounds__(256) void lp_join_kernel(LpArgs a) {
   typedef Elem<DTYPE> E;
-  extern __shared__ uint64_t entries[];  // [splits][top]
+  extern __shared__ uint64_t entries[];  // those that pass, at most [splits][top]
+  __shared__ uint32_t passed;
   const int row = blockIdx.x, lane = threadIdx.x & 63;
   const int total = a.splits * a.top;
-  for (int i = threadIdx.x; i < total; i += 256) entries[i] = a.cand[(int64_t)row * total + i];
+  float at_token = 0.f;
+  int token = -1;
+  if (a.logp) {
+    token = a.token[row];
+    if ((uint32_t)token >= (uint32_t)a.vocab) token = -1;
+    if (token >= 0) at_token = E::to_float(static_cast<const typename E::T*>(a.logits)[(int64_t)row * a.stride + token]);
+  }
+  const uint64_t* const cand = a.cand + (int64_t)row * total;
+  const int part = lane % a.splits, place = lane / a.splits;
+  uint32_t sample = 0;
+  if (place < a.top && (place + 1) * a.splits <= 64) sample = (uint32_t)(cand[part * a.top + place] >> 32);
+  if (threadIdx.x == 0) passed = 0;
   const RowStat st = finish(merge_parts(a.parts + (int64_t)row * a.splits, a.splits, lane, a.c), a.c, a.scale);
   if (threadIdx.x == 0) {
-    if (a.logp) {
-      const int token = a.token[row];
-      a.logp[row] = (uint32_t)token < (uint32_t)a.vocab
-                        ? log_prob(st, E::to_float(static_cast<const typename E::T*>(a.logits)[(int64_t)row * a.stride + token]), a.scale)
-                        : 0.f;
-    }
+    if (a.logp) a.logp[row] = token >= 0 ? log_prob(st, at_token, a.scale) : 0.f;
     if (ENT && a.entropy) a.entropy[row] = st.H;
     if (a.stats) reinterpret_cast<float4*>(a.stats)[row] = make_float4(st.M, st.log2s, st.H, st.c);
   }
+  if (total == 0) return;
+  const uint32_t bound = top_bound(sample, a.top);
   __syncthreads();
-  for (int i = threadIdx.x; i < total; i += 256) {
-    const uint64_t mine = entries[i];
-    if (mine == 0) continue;
-    int rank = 0;
-    for (int o = 0; o < total; ++o) rank += entries[o] > mine ? 1 : 0;
-    if (rank < a.top) {
-      a.top_logp[(int64_t)row * a.top + rank] = log_prob(st, key_value((uint32_t)(mine >> 32)), a.scale);
-      a.top_token[(int64_t)row * a.top + rank] = (int32_t)(0xFFFFFFFFu - (uint32_t)mine);
-    }
+  for (int i0 = 0; i0 < total; i0 += 256) {
+    const int i = i0 + threadIdx.x;
+    const uint64_t mine = i < total ? cand[i] : 0;
+    const bool pass = mine != 0 && (uint32_t)(mine >> 32) >= bound;
+    const uint64_t mask = __ballot(pass);
+    uint32_t at = 0;
+    if (lane == 0 && mask) at = atomicAdd(&passed, (uint32_t)__builtin_popcountll(mask));
+    at = (uint32_t)__builtin_amdgcn_readfirstlane((int)at);
+    if (pass) entries[at + __builtin_popcountll(mask & ((1ull << lane) - 1))] = mine;
   }
+  __syncthreads();
+  if (threadIdx.x >= 64) return;
+  rank_entries(entries, (int)passed, a.top, lane, [&](int rank, uint64_t e) {
+    a.top_logp[(int64_t)row * a.top + rank] = log_prob(st, key_value((uint32_t)(e >> 32)), a.scale);
+    a.top_token[(int64_t)row * a.top + rank] = (int32_t)(0xFFFFFFFFu - (uint32_t)e);
+  });
 }
 
 // The gradient where the row's statistics are known (PARTS: as parts), kGradVecs vectors a thread.
 constexpr int kGradVecs = 4;
 
-template <int DTYPE, bool ENT, bool PARTS>
+template <int DTYPE, bool ENT, bool PARTS, bool STREAM>
 __global__ __launch_bounds__(256) void lp_grad_kernel(LpArgs a, int chunks) {
   typedef Elem<DTYPE> E;
   typedef typename E::T T;
@@ -613,34 +683,41 @@ __global__ __launch_bounds__(256) void lp_grad_kernel(LpArgs a, int chunks) {
       if (v < nv) {
         float x[VEC];
         grad_vec<E, ENT>(r[j], st, g, x);
-        store_row_vec<E>(to, v, n, x);
+        store_row_vec<E, STREAM>(to, v, n, x);
       }
     }
     if (mine && (int)threadIdx.x == owner) to[token - first] = E::from_float(own);
   }
 }
 
-enum Form { kWave, kBlock, kWide, kLong };
-const char* const kFormNames[] = {"wave", "block", "wide", "long"};
+// The team of a whole row.  A wave: no barriers.  Beyond its registers, a workgroup of 256, or of 1024 where there is at most one row for a
+// compute unit, and from its registers on one of 512: two of them share a compute unit, and while one loads the other computes.
+// What 512 threads cannot hold (81920 logits of 16 bits) is read again from the caches.
+enum Form { kWave, kBlock, kSolo, kLong };
+const char* const kFormNames[] = {"wave", "block", "solo", "long"};
 
-constexpr int kWaveVecs = 4, kBlockVecs = 8, kWideVecs = 8, kLongVecs = 20;
+constexpr int kWaveVecs = 4, kBlockVecs = 8, kSoloVecs = 4, kLongVecs = 20;
+constexpr int kUnits = 256;  // compute units
+constexpr int kMostTeams = 1 << 20;
 
-constexpr int kPartThreads = 256;
+template <int DTYPE, int THREADS, int NV, Mode MODE, bool ENT, bool STREAM>
+void launch_team(const LpArgs& a, int blocks, int threads, hipStream_t stream) {
+  hipLaunchKernelGGL((lp_row_kernel<DTYPE, THREADS, NV, MODE, ENT, STREAM>), dim3(std::min(blocks, kMostTeams)), dim3(threads), 0, stream, a);
+}
 
-template <int DTYPE, Mode MODE, bool ENT>
+template <int DTYPE, Mode MODE, bool ENT, bool STREAM>
 int launch_row(const lp_desc* d, const LpArgs& a, hipStream_t stream) {
-  if (MODE == kPart) {
-    hipLaunchKernelGGL((lp_row_kernel<DTYPE, kPartThreads, kBlockVecs, kPart, ENT>), dim3(a.rows * a.splits), dim3(kPartThreads), 0, stream, a);
-  } else if (d->form == kWave) {
-    const int waves = a.rows >= 2048 ? 4 : 1;
-    hipLaunchKernelGGL((lp_row_kernel<DTYPE, 64, kWaveVecs, MODE, ENT>), dim3(std::min((a.rows + waves - 1) / waves, 1 << 20)), dim3(64 * waves), 0, stream, a);
-  } else if (d->form == kBlock) {
-    hipLaunchKernelGGL((lp_row_kernel<DTYPE, 256, kBlockVecs, MODE, ENT>), dim3(std::min(a.rows, 1 << 20)), dim3(256), 0, stream, a);
-  } else if (d->form == kWide) {
-    hipLaunchKernelGGL((lp_row_kernel<DTYPE, 1024, kWideVecs, MODE, ENT>), dim3(std::min(a.rows, 1 << 20)), dim3(1024), 0, stream, a);
-  } else {
-    hipLaunchKernelGGL((lp_row_kernel<DTYPE, 1024, kLongVecs, MODE, ENT>), dim3(std::min(a.rows, 1 << 20)), dim3(1024), 0, stream, a);
-  }
+  const int waves = a.rows >= 2048 ? 4 : 1;
+  if (MODE == kPart)
+    launch_team<DTYPE, 1024, kSoloVecs, kPart, ENT, false>(a, a.rows * a.splits, 1024, stream);
+  else if (d->form == kWave)
+    launch_team<DTYPE, 64, kWaveVecs, MODE, ENT, STREAM>(a, (int)(((int64_t)a.rows + waves - 1) / waves), 64 * waves, stream);
+  else if (d->form == kBlock)
+    launch_team<DTYPE, 256, kBlockVecs, MODE, ENT, STREAM>(a, a.rows, 256, stream);
+  else if (d->form == kSolo)
+    launch_team<DTYPE, 1024, kSoloVecs, MODE, ENT, false>(a, a.rows, 1024, stream);
+  else
+    launch_team<DTYPE, 512, kLongVecs, MODE, ENT, STREAM>(a, a.rows, 512, stream);
   return (int)hipGetLastError();
 }
 
@@ -650,13 +727,17 @@ int launch_join(const LpArgs& a, hipStream_t stream) {
   return (int)hipGetLastError();
 }
 
-template <int DTYPE, bool ENT, bool PARTS>
+template <int DTYPE, bool ENT, bool PARTS, bool STREAM>
 int launch_grad(const LpArgs& a, hipStream_t stream) {
   constexpr int CHUNK = 256 * Elem<DTYPE>::VEC * kGradVecs;
   const int chunks = (a.vocab + CHUNK - 1) / CHUNK;
-  hipLaunchKernelGGL((lp_grad_kernel<DTYPE, ENT, PARTS>), dim3((uint32_t)std::min<int64_t>((int64_t)a.rows * chunks, 1 << 22)), dim3(256), 0, stream, a, chunks);
+  hipLaunchKernelGGL((lp_grad_kernel<DTYPE, ENT, PARTS, STREAM>), dim3((uint32_t)std::min<int64_t>((int64_t)a.rows * chunks, 1 << 22)), dim3(256), 0, stream, a, chunks);
   return (int)hipGetLastError();
 }
+
+// Whether logits and gradient together are more than the last-level cache holds: the gradient then goes around it, and leaves it to the
+// logits that are read a second time and to whoever reads the gradient's end.
+bool streams(const lp_desc* d) { return (double)d->p.rows * d->p.vocab * dtype_bytes(d->p.dtype) * 2 > (double)(256 << 20); }
 
 // One of the descriptor's six kinds.
 template <template <int, bool> class Op>
@@ -672,23 +753,25 @@ int by_kind(const lp_desc* d, const LpArgs& a, hipStream_t stream) {
 template <int DTYPE, bool ENT>
 struct Forward {
   static int run(const lp_desc* d, const LpArgs& a, hipStream_t stream) {
-    if (d->splits == 1) return launch_row<DTYPE, kScore, ENT>(d, a, stream);
-    const int e = launch_row<DTYPE, kPart, ENT>(d, a, stream);
+    if (d->splits == 1) return launch_row<DTYPE, kScore, ENT, false>(d, a, stream);
+    const int e = launch_row<DTYPE, kPart, ENT, false>(d, a, stream);
     return e ? e : launch_join<DTYPE, ENT>(a, stream);
   }
 };
 
 template <int DTYPE, bool ENT>
 struct Backward {
-  static int run(const lp_desc*, const LpArgs& a, hipStream_t stream) { return launch_grad<DTYPE, ENT, false>(a, stream); }
+  static int run(const lp_desc* d, const LpArgs& a, hipStream_t stream) {
+    return streams(d) ? launch_grad<DTYPE, ENT, false, true>(a, stream) : launch_grad<DTYPE, ENT, false, false>(a, stream);
+  }
 };
 
 template <int DTYPE, bool ENT>
 struct ForwardBackward {
   static int run(const lp_desc* d, const LpArgs& a, hipStream_t stream) {
-    if (d->splits == 1) return launch_row<DTYPE, kTrain, ENT>(d, a, stream);
-    const int e = launch_row<DTYPE, kPart, ENT>(d, a, stream);
-    return e ? e : launch_grad<DTYPE, ENT, true>(a, stream);
+    if (d->splits == 1) return streams(d) ? launch_row<DTYPE, kTrain, ENT, true>(d, a, stream) : launch_row<DTYPE, kTrain, ENT, false>(d, a, stream);
+    const int e = launch_row<DTYPE, kPart, ENT, false>(d, a, stream);
+    return e ? e : launch_grad<DTYPE, ENT, true, false>(a, stream);
   }
 };
 
@@ -734,16 +817,18 @@ int lp_desc_create(lp_desc_t** out, const lp_params_t* pp) {
   d->p = p;
   d->c = (float)(p.scale * 1.44269504088896340736);
   const int vec = 16 / dtype_bytes(p.dtype);
-  d->form = p.vocab <= 64 * vec * kWaveVecs ? kWave : p.vocab <= 256 * vec * kBlockVecs ? kBlock : p.vocab <= 1024 * vec * kWideVecs ? kWide : kLong;
+  const int solo = 1024 * vec * kSoloVecs;
+  d->form = p.vocab <= 64 * vec * kWaveVecs                 ? kWave
+            : p.rows <= kUnits && p.vocab <= solo           ? kSolo
+            : p.vocab <= 256 * vec * kBlockVecs             ? kBlock
+                                                            : kLong;
   d->splits = 1;
   d->seg = p.vocab;
-  if (p.rows > 0 && p.rows < 256 && p.vocab >= 8192) {
-    const int most = 512 / p.rows, least = (p.vocab + 2047) / 2048;
-    int splits = std::max(1, std::min(std::min(most, least), kMaxSplits));
-    if (splits > 1) {
-      d->seg = ((p.vocab + splits - 1) / splits + vec - 1) / vec * vec;
-      d->splits = (p.vocab + d->seg - 1) / d->seg;
-    }
+  // Where a compute unit holds no whole row in one pass and two of them or more are left for each, rows are taken in parts.
+  if (p.rows > 0 && 2 * p.rows <= kUnits && p.vocab > solo) {
+    const int splits = std::min(std::min(kUnits / p.rows, (p.vocab + solo / 4 - 1) / (solo / 4)), kMaxSplits);
+    d->seg = ((p.vocab + splits - 1) / splits + vec - 1) / vec * vec;
+    d->splits = (p.vocab + d->seg - 1) / d->seg;
   }
   if (d->splits > 1) d->ws_bytes = (size_t)p.rows * d->splits * (16 + 8 * (size_t)p.top);
   const char* const form = kFormNames[d->form];

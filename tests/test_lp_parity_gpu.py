@@ -54,6 +54,11 @@ CASES = [
     (3, 160000, F16, 20, 1, 1.0, 0, 0),
     (64, 50257, BF16, 20, 1, 1.5, 0, 0),
     (130, 20011, F32, 32, 1, 1.0, 1, 0),
+    (1, 128257, BF16, 64, 1, 1.0, 0, 1),
+    (4, 40009, F32, 20, 1, 0.5, 3, 0),
+    (128, 33000, F16, 20, 1, 1.0, 0, 0),
+    (20, 16385, F32, 20, 1, 1.0, 0, 0),
+    (1, 1000000, F16, 20, 1, 1.0, 0, 0),
 ]
 IDS = ["%dx%d-%s-t%d-e%d-s%g-g%d-o%d" % (c[0], c[1], str(c[2])[6:], *c[3:]) for c in CASES]
 
@@ -289,22 +294,22 @@ def test_on_another_stream_and_in_a_graph(rows, vocab):
 
 
 def test_refusals_on_the_device():
-    d = lib.lp_desc_create(lib.LpParams(4, 9000, BF16, 2, 1))
-    x = torch.zeros((4, 9000), device=DEV, dtype=BF16)
+    d = lib.lp_desc_create(lib.LpParams(4, 90000, BF16, 2, 1))
+    x = torch.zeros((4, 90000), device=DEV, dtype=BF16)
     token = torch.zeros(4, device=DEV, dtype=torch.int32)
     f = lambda *s: torch.empty(s, device=DEV)
     tl, tt, ws = f(4, 2), torch.empty((4, 2), device=DEV, dtype=torch.int32), f(lib.lp_desc_workspace_bytes(d) // 4)
     ok = lambda **k: lib.lp_forward(d, **{**dict(logits=x, token=token, logp=f(4), entropy=f(4), stats=None, top_logp=tl, top_token=tt, ws=ws), **k})
     ok()
-    for wrong, error in ((dict(logits=x.float()), TypeError), (dict(logits=x.t()), ValueError), (dict(logits=x[:, :8999]), ValueError),
-                         (dict(logits=torch.zeros((9000, 4), device=DEV, dtype=BF16).t()), TypeError),
-                         (dict(logits=x[:1].expand(4, 9000)), TypeError), (dict(logits=x.cpu()), TypeError),
+    for wrong, error in ((dict(logits=x.float()), TypeError), (dict(logits=x.t()), ValueError), (dict(logits=x[:, :89999]), ValueError),
+                         (dict(logits=torch.zeros((90000, 4), device=DEV, dtype=BF16).t()), TypeError),
+                         (dict(logits=x[:1].expand(4, 90000)), TypeError), (dict(logits=x.cpu()), TypeError),
                          (dict(token=token.long()), TypeError), (dict(token=token[:3]), ValueError), (dict(logp=f(5)), ValueError),
                          (dict(token=None), lib.ConvError), (dict(top_logp=None), lib.ConvError), (dict(ws=None), lib.ConvError),
                          (dict(ws=ws[:-1]), lib.ConvError), (dict(stats=f(4, 3)), ValueError)):
         with pytest.raises(error):
             ok(**wrong)
-    plain = lib.lp_desc_create(lib.LpParams(4, 9000, BF16, 0, 0))
+    plain = lib.lp_desc_create(lib.LpParams(4, 90000, BF16, 0, 0))
     with pytest.raises(lib.ConvError):
         lib.lp_forward(plain, x, token, f(4), f(4), None, None, None, ws)
     with pytest.raises(lib.ConvError):
