@@ -15,7 +15,7 @@
  * leaves it untouched); otherwise outputs must not overlap inputs.  Tensors that follow each other in memory, as views of one flat
  * buffer do, are taken together; the result does not depend on it but for the order of the sums.
  *
- * Ownership, execution and errors as in mi355conv.h.  Every call only enqueues kernels (two for up to 96 runs of tensors that
+ * The workspace is 16-byte aligned.  Ownership, execution and errors as in mi355conv.h.  Every call only enqueues kernels (two for up to 96 runs of tensors that
  * follow each other, two for each further 96) and may be captured.  Equal calls give equal bits.
  */
 #ifndef MI355GN_H

@@ -25,7 +25,7 @@
  * Sums, maxima and gradients are held in fp32; a gradient is rounded once, to nearest, as it is stored.
  * d_logits may be logits itself (same base and stride); no other output may overlap an input, the workspace or another output.
  *
- * Ownership, execution and errors as in mi355conv.h: caller-owned device memory and workspace, enqueued on the caller's
+ * The workspace is 16-byte aligned.  Ownership, execution and errors as in mi355conv.h: caller-owned device memory and workspace, enqueued on the caller's
  * hipStream_t without synchronising; a conv_status_t comes back, and argument errors are found before anything is enqueued.
  * Every call only enqueues kernels and may be captured.  Results do not depend on timing: equal calls give equal bits.
  * rows == 0 is a no-op.

@@ -16,7 +16,7 @@
  * The packed form depends on k, num_output and group alone: descriptors that agree in these share it.
  * Outputs must not overlap inputs or the workspace.
  *
- * Ownership, execution and errors as in mi355conv.h.  Every call only enqueues kernels and may be captured.  Equal calls
+ * The workspace is 16-byte aligned.  Ownership, execution and errors as in mi355conv.h.  Every call only enqueues kernels and may be captured.  Equal calls
  * give equal bits.  m may be 0: q4_forward is then a no-op.
  */
 #ifndef MI355Q4_H

@@ -290,6 +290,7 @@ int gn_clip(const gn_desc_t* d, const void* const* grads, double limit, void* co
   for (int i = 0; i < d->tensors; ++i)
     if (d->counts[i] > 0 && (!grads[i] || !outs[i])) return CONV_EINVAL;
   if (!ws || ws_bytes < d->ws_bytes) return CONV_EWORKSPACE;
+  if ((uintptr_t)ws & 15u) return CONV_EINVAL;
   const hipStream_t stream = (hipStream_t)hip_stream;
   GnArgs a = {};
   // A chunk is what a workgroup takes at a time: large ones where there is enough for every workgroup.

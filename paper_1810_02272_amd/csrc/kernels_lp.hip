@@ -861,6 +861,7 @@ int lp_forward(const lp_desc_t* d, const void* logits, int64_t stride, const int
   if ((top_logp != nullptr) != (d->p.top > 0) || (top_token != nullptr) != (d->p.top > 0)) return CONV_EINVAL;
   if (bad_rows(d, logits, stride)) return CONV_EINVAL;
   if (d->ws_bytes && (!ws || ws_bytes < d->ws_bytes)) return CONV_EWORKSPACE;
+  if (d->ws_bytes && ((uintptr_t)ws & 15u)) return CONV_EINVAL;
   LpArgs a = base_args(d, logits, stride, token);
   a.logp = logp;
   a.entropy = entropy;
@@ -895,6 +896,7 @@ int lp_forward_backward(const lp_desc_t* d, const void* logits, int64_t stride, 
   if (d->p.rows == 0) return CONV_OK;
   if (bad_rows(d, logits, stride) || bad_rows(d, d_logits, d_stride) || !token || !d_logp) return CONV_EINVAL;
   if (d->ws_bytes && (!ws || ws_bytes < d->ws_bytes)) return CONV_EWORKSPACE;
+  if (d->ws_bytes && ((uintptr_t)ws & 15u)) return CONV_EINVAL;
   LpArgs a = base_args(d, logits, stride, token);
   a.logp = logp;
   a.entropy = entropy;

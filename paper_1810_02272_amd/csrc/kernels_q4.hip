@@ -15,15 +15,23 @@
 
 #include <algorithm>
 #include <new>
+#include <type_traits>
 
 #include "device_utils.h"
 #include "elements.h"
 #include "internal.h"
 #include "mi355q4.h"
 
+#ifndef NT_TILES
+#define NT_TILES 2048
+#define W_GROUPS 2048
+#define KS_BLOCKS 256
+#endif
 struct q4_desc {
   q4_params_t p;
   int32_t tiles, blocks;  // of 16 outputs and 128 inputs
+  int32_t nt, waves;      // tiles of a workgroup, its waves
+  int32_t splits, per_split;  // workgroups that share the inputs of an output, blocks of each
   size_t ws_bytes;
   char names[96];
 };
@@ -32,9 +40,7 @@ namespace mi355conv {
 
 namespace {
 
-typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
-typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 
 constexpr int kTile = 16, kBlockK = 128;
@@ -46,7 +52,10 @@ struct Q4Args {
   const uint16_t* scales;
   const void* bias;
   void* y;
+  u32x4* terms;  // fp32: x as operands (x_terms_kernel)
+  float* parts;  // splits > 1: [splits][m][o]
   int32_t m, k, o, tiles, blocks;
+  int32_t splits, per_split;
   int32_t relu;
 };
 
@@ -94,11 +103,11 @@ struct Operand<MI355_BF16> {
   typedef bf16x8 V;
   static constexpr int TERMS = 1;
   static __device__ __forceinline__ V weights(uint32_t c) {
-    V r;
-    const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, 1.f, 0), b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, 1.f, 1);
-    const bf16x2 d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, 1.f, 2), e = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, 1.f, 3);
-    r[0] = a[0], r[1] = a[1], r[2] = b[0], r[3] = b[1], r[4] = d[0], r[5] = d[1], r[6] = e[0], r[7] = e[1];
-    return r;
+    const u32x4 r = {__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, 1.f, 0)),
+                     __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, 1.f, 1)),
+                     __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, 1.f, 2)),
+                     __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, 1.f, 3))};
+    return __builtin_bit_cast(V, r);
   }
   static __device__ __forceinline__ f32x4 mma(V a, V b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
 };
@@ -108,11 +117,11 @@ struct Operand<MI355_F16> {
   typedef f16x8 V;
   static constexpr int TERMS = 1;
   static __device__ __forceinline__ V weights(uint32_t c) {
-    V r;
-    const f16x2 a = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(c, 1.f, 0), b = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(c, 1.f, 1);
-    const f16x2 d = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(c, 1.f, 2), e = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(c, 1.f, 3);
-    r[0] = a[0], r[1] = a[1], r[2] = b[0], r[3] = b[1], r[4] = d[0], r[5] = d[1], r[6] = e[0], r[7] = e[1];
-    return r;
+    const u32x4 r = {__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(c, 1.f, 0)),
+                     __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(c, 1.f, 1)),
+                     __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(c, 1.f, 2)),
+                     __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(c, 1.f, 3))};
+    return __builtin_bit_cast(V, r);
   }
   static __device__ __forceinline__ f32x4 mma(V a, V b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
 };
@@ -138,122 +147,223 @@ __device__ __forceinline__ void three_terms(float x, uint32_t (&t)[3]) {
   t[2] = __builtin_bit_cast(uint32_t, r2) >> 16;
 }
 
-// Eight consecutive inputs of a row of x from input `at` on, as operands; zeros beyond k.
-template <int DTYPE>
-__device__ __forceinline__ void load_x(const void* x, int64_t row, int at, int k, typename Operand<DTYPE>::V (&v)[Operand<DTYPE>::TERMS]) {
-  typedef Elem<DTYPE> E;
-  typedef typename Operand<DTYPE>::V V;
-  const typename E::T* const p = static_cast<const typename E::T*>(x) + row * k + at;
-  if constexpr (DTYPE == MI355_F32) {
-    float f[8];
-    if (at + 8 <= k) {
-      const u32x4 a = load_vec<E>(p), b = load_vec<E>(p + 4);
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        f[i] = E::get(a, i);
-        f[4 + i] = E::get(b, i);
-      }
-    } else {
-#pragma unroll
-      for (int i = 0; i < 8; ++i) f[i] = at + i < k ? p[i] : 0.f;
-    }
-    uint32_t w[3][4];
+// Row i of a tile of 16 rows of x is row row_place(i) of the instruction's left operand: its results then stand in register i / 4 of the
+// lanes 16 (i % 4) .. + 15, and up to four rows take one register.
+__device__ __forceinline__ int place_row(int place) { return (place & 3) * 4 + (place >> 2); }
+
+// fp32 x as operands: [tile of 16 rows][32 inputs][term][lane], zeros beyond m and k.  One thread for each lane of the three terms.
+__global__ __launch_bounds__(256) void x_terms_kernel(const float* __restrict__ x, u32x4* __restrict__ to, int m, int k, int steps, int64_t lanes) {
+  const int64_t v = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (v >= lanes) return;
+  const int lane = (int)(v & 63);
+  const int64_t ts = v >> 6;
+  const int step = (int)(ts % steps);
+  const int64_t row = ts / steps * 16 + place_row(lane & 15);
+  const int at = 32 * step + 8 * (lane >> 4);
+  float f[8];
+  const float* const p = x + row * k + at;
+  if (row < m && at + 8 <= k) {
+    const u32x4 a = load_vec<Elem<MI355_F32>>(p), b = load_vec<Elem<MI355_F32>>(p + 4);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      uint32_t a[3], b[3];
-      three_terms(f[2 * i], a);
-      three_terms(f[2 * i + 1], b);
-#pragma unroll
-      for (int t = 0; t < 3; ++t) w[t][i] = a[t] | b[t] << 16;
+      f[i] = Elem<MI355_F32>::get(a, i);
+      f[4 + i] = Elem<MI355_F32>::get(b, i);
     }
-#pragma unroll
-    for (int t = 0; t < 3; ++t) v[t] = __builtin_bit_cast(V, u32x4{w[t][0], w[t][1], w[t][2], w[t][3]});
   } else {
-    if (at + 8 <= k) {
-      v[0] = __builtin_bit_cast(V, load_vec<E>(p));
-    } else {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) v[0][i] = at + i < k ? p[i] : (typename E::T)0.f;
-    }
+    for (int i = 0; i < 8; ++i) f[i] = row < m && at + i < k ? p[i] : 0.f;
   }
+  u32x4 w[3];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    uint32_t a[3], b[3];
+    three_terms(f[2 * i], a);
+    three_terms(f[2 * i + 1], b);
+#pragma unroll
+    for (int t = 0; t < 3; ++t) w[t][i] = a[t] | b[t] << 16;
+  }
+#pragma unroll
+  for (int t = 0; t < 3; ++t) to[(ts * 3 + t) * 64 + lane] = w[t];
 }
 
-// MT times 16 rows of x by a tile of 16 outputs in a workgroup, whose waves take the blocks of inputs in turn.
-template <int DTYPE, int MT, int GROUP>
-__global__ __launch_bounds__(256) void q4_kernel(Q4Args a) {
+template <int PER>
+__device__ __forceinline__ void load_scales(const uint16_t* at, float (&scale)[PER]) {
+  uint32_t w[2] = {0, 0};
+  if constexpr (PER == 4) {
+    const uint2 u = *reinterpret_cast<const uint2*>(at);
+    w[0] = u.x, w[1] = u.y;
+  } else if constexpr (PER == 2) {
+    w[0] = *reinterpret_cast<const uint32_t*>(at);
+  } else {
+    w[0] = *at;
+  }
+#pragma unroll
+  for (int g = 0; g < PER; ++g) scale[g] = __builtin_bit_cast(float, g & 1 ? w[g >> 1] & 0xffff0000u : w[g >> 1] << 16);
+}
+
+constexpr int kMostWaves = 8;
+
+// MT times 16 rows of x by NT tiles of 16 outputs in a workgroup; its waves take the blocks of inputs in turn, each on its own, and
+// add up through shared memory at the end: nothing of x is used by two waves.  REGS: result registers that hold rows.
+template <int DTYPE, int MT, int NT, int REGS, int GROUP>
+__global__ __launch_bounds__(kMostWaves * 64) void q4_kernel(Q4Args a) {
   typedef Operand<DTYPE> Op;
   typedef Elem<DTYPE> E;
-  constexpr int PER = kBlockK / GROUP;
-  __shared__ f32x4 parts[4][MT][64];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int tile = blockIdx.x;
-  for (int m0 = blockIdx.y * 64; m0 < a.m; m0 += gridDim.y * 64) {
-    f32x4 acc[MT] = {};
-    for (int b = wave; b < a.blocks; b += 4) {
-      const int64_t tb = (int64_t)tile * a.blocks + b;
-      const u32x4 w = a.codes[tb * 64 + lane];
-      float scale[PER];
+  typedef typename Op::V V;
+  constexpr int PER = kBlockK / GROUP, TERMS = Op::TERMS;
+  __shared__ float parts[kMostWaves][NT * REGS * 64];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), waves = blockDim.x >> 6;
+  const int quarter = lane >> 4;
+  const int groups = (a.tiles + NT - 1) / NT;
+  const int begin = blockIdx.y * a.per_split, end = min(begin + a.per_split, a.blocks);
+  for (int tile0 = blockIdx.x * NT; tile0 < groups * NT; tile0 += gridDim.x * NT) {
+    for (int m0 = 0; m0 < a.m; m0 += 16 * MT) {
+      f32x4 acc[MT][NT] = {};
+      const typename E::T* rows[MT];
+      if constexpr (TERMS == 1) {
 #pragma unroll
-      for (int g = 0; g < PER; ++g) scale[g] = __builtin_bit_cast(float, (uint32_t)a.scales[(tb * kTile + (lane & 15)) * PER + g] << 16);
-      f32x4 sum[MT] = {};
+        for (int t = 0; t < MT; ++t)  // (rows beyond m: the last one's values again, for results that nobody stores)
+          rows[t] = static_cast<const typename E::T*>(a.x) + (int64_t)min(m0 + 16 * t + place_row(lane & 15), a.m - 1) * a.k + 8 * quarter;
+      }
+      auto block = [&](int b, auto guarded) {
+        u32x4 w[NT];
+        float scale[NT][PER];
 #pragma unroll
-      for (int d = 0; d < 4; ++d) {
-        const typename Op::V wv = Op::weights(w[d]);
+        for (int n = 0; n < NT; ++n) {
+          const int64_t tb = (int64_t)min(tile0 + n, a.tiles - 1) * a.blocks + b;
+          w[n] = a.codes[tb * 64 + lane];
+          load_scales<PER>(a.scales + (tb * kTile + (lane & 15)) * PER, scale[n]);
+        }
+        f32x4 sum[MT][NT] = {};
 #pragma unroll
-        for (int t = 0; t < MT; ++t) {
-          const int row = m0 + 16 * t + (lane & 15);
-          typename Op::V x[Op::TERMS] = {};
-          const int at = b * kBlockK + 32 * d + 8 * (lane >> 4);
-          if (row < a.m && at < a.k) load_x<DTYPE>(a.x, row, at, a.k, x);
+        for (int d = 0; d < 4; ++d) {
+          V x[MT][TERMS];
 #pragma unroll
-          for (int i = 0; i < Op::TERMS; ++i) sum[t] = Op::mma(x[i], wv, sum[t]);
-          if ((d + 1) * 32 % GROUP == 0) {
+          for (int t = 0; t < MT; ++t) {
+            if constexpr (TERMS > 1) {
 #pragma unroll
-            for (int r = 0; r < 4; ++r) acc[t][r] = fmaf(sum[t][r], scale[d * 32 / GROUP], acc[t][r]);
-            sum[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+              for (int i = 0; i < TERMS; ++i)
+                x[t][i] = __builtin_bit_cast(V, a.terms[(((int64_t)(m0 / 16 + t) * a.blocks * 4 + b * 4 + d) * TERMS + i) * 64 + lane]);
+            } else {
+              const int at = b * kBlockK + 32 * d;
+              if constexpr (decltype(guarded)::value) {
+                typename E::T f[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) f[i] = at + 8 * quarter + i < a.k ? rows[t][at + i] : (typename E::T)0.f;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) x[t][0][i] = f[i];
+              } else {
+                x[t][0] = __builtin_bit_cast(V, load_vec<E>(rows[t] + at));
+              }
+            }
+          }
+#pragma unroll
+          for (int n = 0; n < NT; ++n) {
+            const V wv = Op::weights(w[n][d]);
+#pragma unroll
+            for (int t = 0; t < MT; ++t) {
+              f32x4 z = d * 32 % GROUP == 0 ? f32x4{0.f, 0.f, 0.f, 0.f} : sum[t][n];
+#pragma unroll
+              for (int i = 0; i < TERMS; ++i) z = Op::mma(x[t][i], wv, z);
+              sum[t][n] = z;
+              if ((d + 1) * 32 % GROUP == 0) {
+#pragma unroll
+                for (int r = 0; r < REGS; ++r) acc[t][n][r] = fmaf(z[r], scale[n][d * 32 / GROUP], acc[t][n][r]);
+              }
+            }
+          }
+        }
+      };
+      const int full = TERMS > 1 ? end : min(end, a.k / kBlockK);
+      int b = begin + wave;
+#pragma unroll 2
+      for (; b < full; b += waves) block(b, std::false_type());
+      if (TERMS == 1 && b < end) block(b, std::true_type());
+
+#pragma unroll
+      for (int t = 0; t < MT; ++t) {
+        __syncthreads();
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+          for (int r = 0; r < REGS; ++r) parts[wave][(n * REGS + r) * 64 + lane] = acc[t][n][r];
+        __syncthreads();
+        for (int i = threadIdx.x; i < NT * REGS * 64; i += blockDim.x) {
+          float v = parts[0][i];
+          for (int p = 1; p < waves; ++p) v += parts[p][i];
+          const int nr = i >> 6, out = (tile0 + nr / REGS) * kTile + (i & 15), row = m0 + 16 * t + 4 * (nr % REGS) + (i >> 4 & 3);
+          if (out >= a.o || row >= a.m) continue;
+          const int64_t at = (int64_t)row * a.o + out;
+          if (a.splits > 1) {
+            a.parts[(int64_t)blockIdx.y * a.m * a.o + at] = v;
+          } else {
+            if (a.bias) v += E::to_float(static_cast<const typename E::T*>(a.bias)[out]);
+            if (a.relu) v = v > 0.f ? v : 0.f;
+            static_cast<typename E::T*>(a.y)[at] = E::from_float(v);
           }
         }
       }
     }
-#pragma unroll
-    for (int t = 0; t < MT; ++t) parts[wave][t][lane] = acc[t];
-    __syncthreads();
-    for (int t = wave; t < MT; t += 4) {
-      const f32x4 z = (parts[0][t][lane] + parts[1][t][lane]) + (parts[2][t][lane] + parts[3][t][lane]);
-      const int out = tile * kTile + (lane & 15);
-      if (out < a.o) {
-        const float bias = a.bias ? E::to_float(static_cast<const typename E::T*>(a.bias)[out]) : 0.f;
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          const int row = m0 + 16 * t + 4 * (lane >> 4) + r;
-          float v = z[r] + bias;
-          if (a.relu) v = v > 0.f ? v : 0.f;
-          if (row < a.m) static_cast<typename E::T*>(a.y)[(int64_t)row * a.o + out] = E::from_float(v);
-        }
-      }
-    }
-    __syncthreads();
   }
 }
 
-template <int DTYPE, int MT>
-void launch_group(const Q4Args& a, int group, hipStream_t stream) {
-  const dim3 grid(a.tiles, std::min((a.m + 63) / 64, 65535)), block(256);
-  switch (group) {
-    case 32: hipLaunchKernelGGL((q4_kernel<DTYPE, MT, 32>), grid, block, 0, stream, a); break;
-    case 64: hipLaunchKernelGGL((q4_kernel<DTYPE, MT, 64>), grid, block, 0, stream, a); break;
-    default: hipLaunchKernelGGL((q4_kernel<DTYPE, MT, 128>), grid, block, 0, stream, a);
+// The splits' sums in one.
+template <int DTYPE>
+__global__ __launch_bounds__(256) void q4_join_kernel(Q4Args a) {
+  typedef Elem<DTYPE> E;
+  const int64_t count = (int64_t)a.m * a.o;
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < count; i += (int64_t)gridDim.x * 256) {
+    float v = a.parts[i];
+    for (int s = 1; s < a.splits; ++s) v += a.parts[s * count + i];
+    if (a.bias) v += E::to_float(static_cast<const typename E::T*>(a.bias)[i % a.o]);
+    if (a.relu) v = v > 0.f ? v : 0.f;
+    static_cast<typename E::T*>(a.y)[i] = E::from_float(v);
+  }
+}
+
+int m_tiles(const q4_desc* d) { return std::max(1, std::min((d->p.m + 15) / 16, 4)); }
+
+size_t terms_bytes(const q4_desc* d) {
+  const size_t tiles = ((size_t)d->p.m + 15) / 16, per = m_tiles(d);
+  return (tiles + per - 1) / per * per * d->blocks * 4 * 3 * 1024;
+}
+
+template <int DTYPE, int MT, int NT, int REGS>
+void launch_group(const q4_desc* d, const Q4Args& a, hipStream_t stream) {
+  const int groups = (d->tiles + NT - 1) / NT;
+  const dim3 grid(std::min(groups, 1 << 22), d->splits), block(64 * d->waves);
+  switch (d->p.group) {
+    case 32: hipLaunchKernelGGL((q4_kernel<DTYPE, MT, NT, REGS, 32>), grid, block, 0, stream, a); break;
+    case 64: hipLaunchKernelGGL((q4_kernel<DTYPE, MT, NT, REGS, 64>), grid, block, 0, stream, a); break;
+    default: hipLaunchKernelGGL((q4_kernel<DTYPE, MT, NT, REGS, 128>), grid, block, 0, stream, a);
   }
 }
 
 template <int DTYPE>
-void launch_rows(const Q4Args& a, int group, hipStream_t stream) {
-  switch (std::min((a.m + 15) / 16, 4)) {
-    case 1: launch_group<DTYPE, 1>(a, group, stream); break;
-    case 2: launch_group<DTYPE, 2>(a, group, stream); break;
-    case 3: launch_group<DTYPE, 3>(a, group, stream); break;
-    default: launch_group<DTYPE, 4>(a, group, stream);
+int launch_forward(const q4_desc* d, const Q4Args& a, hipStream_t stream) {
+  if (DTYPE == MI355_F32) {
+    const int64_t lanes = (int64_t)(terms_bytes(d) / 48);
+    hipLaunchKernelGGL(x_terms_kernel, dim3((uint32_t)((lanes + 255) / 256)), dim3(256), 0, stream, static_cast<const float*>(a.x), a.terms, a.m, a.k,
+                       d->blocks * 4, lanes);
+    const int e = (int)hipGetLastError();
+    if (e) return e;
   }
+  switch (m_tiles(d)) {
+    case 1:
+      if (d->p.m <= 4)
+        d->nt == 1 ? launch_group<DTYPE, 1, 1, 1>(d, a, stream) : launch_group<DTYPE, 1, 2, 1>(d, a, stream);
+      else
+        launch_group<DTYPE, 1, 2, 4>(d, a, stream);
+      break;
+    case 2: launch_group<DTYPE, 2, 4, 4>(d, a, stream); break;
+    case 3: launch_group<DTYPE, 3, 4, 4>(d, a, stream); break;
+    default: launch_group<DTYPE, 4, 4, 4>(d, a, stream);
+  }
+  int e = (int)hipGetLastError();
+  if (e || d->splits == 1) return e;
+  const int64_t count = (int64_t)d->p.m * d->p.num_output;
+  hipLaunchKernelGGL(q4_join_kernel<DTYPE>, dim3((uint32_t)std::min<int64_t>((count + 255) / 256, 4096)), dim3(256), 0, stream, a);
+  return (int)hipGetLastError();
 }
 
 size_t codes_bytes(const q4_desc* d) { return (size_t)d->tiles * d->blocks * 1024; }
@@ -280,7 +390,22 @@ int q4_desc_create(q4_desc_t** out, const q4_params_t* pp) {
   d->p = p;
   d->tiles = (p.num_output + kTile - 1) / kTile;
   d->blocks = (p.k + kBlockK - 1) / kBlockK;
-  snprintf(d->names, sizeof(d->names), "fwd=q4[m%d]", std::min((p.m + 15) / 16, 4) * 16);
+  const int mt = m_tiles(d);
+  d->nt = mt > 1 ? 4 : p.m > 4 ? 2 : d->tiles < NT_TILES ? 1 : 2;
+  const int groups = (d->tiles + d->nt - 1) / d->nt;
+  d->waves = groups >= W_GROUPS ? 4 : 8;
+  d->splits = 1;
+  d->per_split = d->blocks;
+  if (mt > 1) {
+    const int splits = std::max(1, std::min(KS_BLOCKS / groups, d->blocks / d->waves));
+    d->per_split = (d->blocks + splits - 1) / splits;
+    d->splits = (d->blocks + d->per_split - 1) / d->per_split;
+  }
+  if (p.m > 0) {
+    if (p.dtype == MI355_F32) d->ws_bytes += terms_bytes(d);
+    if (d->splits > 1) d->ws_bytes += (size_t)d->splits * p.m * p.num_output * 4;
+  }
+  snprintf(d->names, sizeof(d->names), "fwd=%sq4[m%d,n%d%s](S=%d)", p.dtype == MI355_F32 ? "terms+" : "", 16 * mt, 16 * d->nt, p.m <= 4 ? ",r1" : "", d->splits);
   *out = d;
   return CONV_OK;
 }
@@ -322,6 +447,7 @@ int q4_forward(const q4_desc_t* d, const void* x, const void* packed, const void
   if (d->p.m == 0) return CONV_OK;
   if (!x || !y) return CONV_EINVAL;
   if (d->ws_bytes && (!ws || ws_bytes < d->ws_bytes)) return CONV_EWORKSPACE;
+  if (d->ws_bytes && ((uintptr_t)ws & 15u)) return CONV_EINVAL;
   Q4Args a = {};
   a.x = x;
   a.codes = static_cast<const u32x4*>(packed);
@@ -334,12 +460,15 @@ int q4_forward(const q4_desc_t* d, const void* x, const void* packed, const void
   a.tiles = d->tiles;
   a.blocks = d->blocks;
   a.relu = d->p.relu;
-  switch (d->p.dtype) {
-    case MI355_F32: launch_rows<MI355_F32>(a, d->p.group, (hipStream_t)hip_stream); break;
-    case MI355_F16: launch_rows<MI355_F16>(a, d->p.group, (hipStream_t)hip_stream); break;
-    default: launch_rows<MI355_BF16>(a, d->p.group, (hipStream_t)hip_stream);
-  }
-  const int e = (int)hipGetLastError();
+  a.splits = d->splits;
+  a.per_split = d->per_split;
+  char* const space = static_cast<char*>(ws);
+  a.terms = reinterpret_cast<u32x4*>(space);
+  a.parts = reinterpret_cast<float*>(space + (d->p.dtype == MI355_F32 ? terms_bytes(d) : 0));
+  const hipStream_t stream = (hipStream_t)hip_stream;
+  const int e = d->p.dtype == MI355_F32   ? launch_forward<MI355_F32>(d, a, stream)
+                : d->p.dtype == MI355_F16 ? launch_forward<MI355_F16>(d, a, stream)
+                                          : launch_forward<MI355_BF16>(d, a, stream);
   return e ? record_hip_error(e) : CONV_OK;
 }
 
