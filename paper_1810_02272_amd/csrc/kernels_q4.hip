@@ -22,11 +22,6 @@
 #include "internal.h"
 #include "mi355q4.h"
 
-#ifndef NT_TILES
-#define NT_TILES 2048
-#define W_GROUPS 2048
-#define KS_BLOCKS 256
-#endif
 struct q4_desc {
   q4_params_t p;
   int32_t tiles, blocks;  // of 16 outputs and 128 inputs
@@ -44,6 +39,7 @@ typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 
 constexpr int kTile = 16, kBlockK = 128;
+constexpr int kUnits = 256;  // compute units
 constexpr int64_t kMaxElems = (int64_t)1 << 30;
 
 struct Q4Args {
@@ -201,17 +197,20 @@ __device__ __forceinline__ void load_scales(const uint16_t* at, float (&scale)[P
   for (int g = 0; g < PER; ++g) scale[g] = __builtin_bit_cast(float, g & 1 ? w[g >> 1] & 0xffff0000u : w[g >> 1] << 16);
 }
 
-constexpr int kMostWaves = 8;
+// Waves of a workgroup.  Up to 16 for one tile of rows; the accumulators of more take the registers of 8.
+template <int MT>
+constexpr int kMostWaves = MT == 1 ? 16 : 8;
 
 // MT times 16 rows of x by NT tiles of 16 outputs in a workgroup; its waves take the blocks of inputs in turn, each on its own, and
 // add up through shared memory at the end: nothing of x is used by two waves.  REGS: result registers that hold rows.
 template <int DTYPE, int MT, int NT, int REGS, int GROUP>
-__global__ __launch_bounds__(kMostWaves * 64) void q4_kernel(Q4Args a) {
+__global__ __launch_bounds__(kMostWaves<MT> * 64) void q4_kernel(Q4Args a) {
   typedef Operand<DTYPE> Op;
   typedef Elem<DTYPE> E;
   typedef typename Op::V V;
   constexpr int PER = kBlockK / GROUP, TERMS = Op::TERMS;
-  __shared__ float parts[kMostWaves][NT * REGS * 64];
+  extern __shared__ float parts[];  // [waves][NT * REGS * 64]
+  constexpr int SLOT = NT * REGS * 64;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), waves = blockDim.x >> 6;
   const int quarter = lane >> 4;
   const int groups = (a.tiles + NT - 1) / NT;
@@ -276,7 +275,6 @@ __global__ __launch_bounds__(kMostWaves * 64) void q4_kernel(Q4Args a) {
       };
       const int full = TERMS > 1 ? end : min(end, a.k / kBlockK);
       int b = begin + wave;
-#pragma unroll 2
       for (; b < full; b += waves) block(b, std::false_type());
       if (TERMS == 1 && b < end) block(b, std::true_type());
 
@@ -286,11 +284,11 @@ __global__ __launch_bounds__(kMostWaves * 64) void q4_kernel(Q4Args a) {
 #pragma unroll
         for (int n = 0; n < NT; ++n)
 #pragma unroll
-          for (int r = 0; r < REGS; ++r) parts[wave][(n * REGS + r) * 64 + lane] = acc[t][n][r];
+          for (int r = 0; r < REGS; ++r) parts[wave * SLOT + (n * REGS + r) * 64 + lane] = acc[t][n][r];
         __syncthreads();
-        for (int i = threadIdx.x; i < NT * REGS * 64; i += blockDim.x) {
-          float v = parts[0][i];
-          for (int p = 1; p < waves; ++p) v += parts[p][i];
+        for (int i = threadIdx.x; i < SLOT; i += blockDim.x) {
+          float v = parts[i];
+          for (int p = 1; p < waves; ++p) v += parts[p * SLOT + i];
           const int nr = i >> 6, out = (tile0 + nr / REGS) * kTile + (i & 15), row = m0 + 16 * t + 4 * (nr % REGS) + (i >> 4 & 3);
           if (out >= a.o || row >= a.m) continue;
           const int64_t at = (int64_t)row * a.o + out;
@@ -332,10 +330,11 @@ template <int DTYPE, int MT, int NT, int REGS>
 void launch_group(const q4_desc* d, const Q4Args& a, hipStream_t stream) {
   const int groups = (d->tiles + NT - 1) / NT;
   const dim3 grid(std::min(groups, 1 << 22), d->splits), block(64 * d->waves);
+  const size_t lds = (size_t)d->waves * NT * REGS * 256;  // at most 64 KB
   switch (d->p.group) {
-    case 32: hipLaunchKernelGGL((q4_kernel<DTYPE, MT, NT, REGS, 32>), grid, block, 0, stream, a); break;
-    case 64: hipLaunchKernelGGL((q4_kernel<DTYPE, MT, NT, REGS, 64>), grid, block, 0, stream, a); break;
-    default: hipLaunchKernelGGL((q4_kernel<DTYPE, MT, NT, REGS, 128>), grid, block, 0, stream, a);
+    case 32: hipLaunchKernelGGL((q4_kernel<DTYPE, MT, NT, REGS, 32>), grid, block, lds, stream, a); break;
+    case 64: hipLaunchKernelGGL((q4_kernel<DTYPE, MT, NT, REGS, 64>), grid, block, lds, stream, a); break;
+    default: hipLaunchKernelGGL((q4_kernel<DTYPE, MT, NT, REGS, 128>), grid, block, lds, stream, a);
   }
 }
 
@@ -391,21 +390,26 @@ int q4_desc_create(q4_desc_t** out, const q4_params_t* pp) {
   d->tiles = (p.num_output + kTile - 1) / kTile;
   d->blocks = (p.k + kBlockK - 1) / kBlockK;
   const int mt = m_tiles(d);
-  d->nt = mt > 1 ? 4 : p.m > 4 ? 2 : d->tiles < NT_TILES ? 1 : 2;
+  // Tiles of a workgroup: a load of x serves them all, but where there is less than a wave for each of a compute unit's places they are
+  // workgroups of their own.  Up to four rows, 4096 x 4096: 1 tile 5.1 us, 2 tiles 7.0; 4096 x 128256: 74.4 and 62.3.
+  d->nt = mt > 1 ? 4 : p.m > 4 ? 2 : d->tiles < 8 * kUnits ? 1 : 2;
   const int groups = (d->tiles + d->nt - 1) / d->nt;
-  d->waves = groups >= W_GROUPS ? 4 : 8;
+  // Waves: as many as there may be where a compute unit has one workgroup, four where it has several (8 rows, 4096 x 100000: 4 waves
+  // 58 us, 8 waves 64; 16 rows, 4096 x 4096: 4 waves 12.9, 8 8.9, 16 8.1); at least two blocks for each.
+  d->waves = groups > kUnits ? 4 : mt > 1 || p.m <= 4 ? 8 : 16;
   d->splits = 1;
   d->per_split = d->blocks;
-  if (mt > 1) {
-    const int splits = std::max(1, std::min(KS_BLOCKS / groups, d->blocks / d->waves));
+  if (mt > 1) {  // 48 rows, 9216 x 4096: 1 part 40.8 us, 2 27.7, 4 22.1; 64 rows, 4096 x 8000, 125 groups: 1 part 24.6, 2 20.5, 4 27.5
+    const int splits = std::max(1, std::min(kUnits / groups, d->blocks / d->waves));
     d->per_split = (d->blocks + splits - 1) / splits;
     d->splits = (d->blocks + d->per_split - 1) / d->per_split;
   }
+  d->waves = std::max(1, std::min(d->waves, (d->per_split + 1) / 2));
   if (p.m > 0) {
     if (p.dtype == MI355_F32) d->ws_bytes += terms_bytes(d);
     if (d->splits > 1) d->ws_bytes += (size_t)d->splits * p.m * p.num_output * 4;
   }
-  snprintf(d->names, sizeof(d->names), "fwd=%sq4[m%d,n%d%s](S=%d)", p.dtype == MI355_F32 ? "terms+" : "", 16 * mt, 16 * d->nt, p.m <= 4 ? ",r1" : "", d->splits);
+  snprintf(d->names, sizeof(d->names), "fwd=%sq4[m%d,n%d%s](S=%d,W=%d)", p.dtype == MI355_F32 ? "terms+" : "", 16 * mt, 16 * d->nt, p.m <= 4 ? ",r1" : "", d->splits, d->waves);
   *out = d;
   return CONV_OK;
 }
