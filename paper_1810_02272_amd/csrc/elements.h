@@ -83,6 +83,26 @@ struct Elem<MI355_BF16> {
   }
 };
 
+// fp64 for what only loads, stores and multiplies.
+template <>
+struct Elem<MI355_F64> {
+  typedef double T;
+  struct __attribute__((packed, aligned(8))) Mem {
+    u32x4 v;
+  };
+  static constexpr int VEC = 2;
+  static __device__ __forceinline__ double to_float(T x) { return x; }
+  static __device__ __forceinline__ T from_float(double x) { return x; }
+  static __device__ __forceinline__ double get(const u32x4& v, int i) {
+    const uint64_t word = (uint64_t)v[2 * i + 1] << 32 | v[2 * i];
+    return __builtin_bit_cast(double, word);
+  }
+  static __device__ __forceinline__ u32x4 pack(const double (&x)[VEC]) {
+    const uint64_t a = __builtin_bit_cast(uint64_t, x[0]), b = __builtin_bit_cast(uint64_t, x[1]);
+    return u32x4{(uint32_t)a, (uint32_t)(a >> 32), (uint32_t)b, (uint32_t)(b >> 32)};
+  }
+};
+
 template <class E>
 __device__ __forceinline__ u32x4 load_vec(const typename E::T* at) {
   return reinterpret_cast<const typename E::Mem*>(at)->v;
@@ -93,10 +113,23 @@ __device__ __forceinline__ void store_vec(typename E::T* at, const u32x4& v) {
   reinterpret_cast<typename E::Mem*>(at)->v = v;
 }
 
-// The same for what is not read again soon: it goes around the last-level cache.
-template <class E>
-__device__ __forceinline__ void stream_vec(typename E::T* at, const u32x4& v) {
-  __builtin_nontemporal_store(v, &reinterpret_cast<typename E::Mem*>(at)->v);
+// The same for what is read once, or not read again soon: it goes around the last-level cache.  Measured on 768 MB, 4 vectors a thread in
+// flight: reads 6.1 TB/s through the cache, 6.9 around it; reads and writes 5.2 and 5.3 by 4096 workgroups, 5.4 and 5.9 by 16384.
+// A template argument: of a branch between both the compiler makes one plain access.
+template <class E, bool STREAM>
+__device__ __forceinline__ u32x4 get_vec(const typename E::T* at) {
+  if constexpr (STREAM)
+    return __builtin_nontemporal_load(&reinterpret_cast<const typename E::Mem*>(at)->v);
+  else
+    return load_vec<E>(at);
+}
+
+template <class E, bool STREAM>
+__device__ __forceinline__ void put_vec(typename E::T* at, const u32x4& v) {
+  if constexpr (STREAM)
+    __builtin_nontemporal_store(v, &reinterpret_cast<typename E::Mem*>(at)->v);
+  else
+    store_vec<E>(at, v);
 }
 
 inline int dtype_bytes(int dtype) { return dtype == MI355_F64 ? 8 : dtype == MI355_F32 ? 4 : 2; }

@@ -18,6 +18,7 @@
 #include "elements.h"
 #include "internal.h"
 #include "mi355gn.h"
+#include "wave_ops.h"
 
 struct gn_desc {
   int32_t tensors;
@@ -32,11 +33,18 @@ namespace mi355conv {
 
 namespace {
 
-constexpr int kSegments = 96;      // of one launch: their table is a kernel argument
+// Of one launch: their table is a kernel argument, 3 KB of them; a short one where all fit that (a flat buffer for each type).
+constexpr int kSegments = 96, kFewSegments = 8;
 constexpr int kMaxTensors = 1 << 18;
 constexpr int kThreads = 256;
-constexpr int kBlocks = 2048;      // eight workgroups on each compute unit: partial sums of a call, one a workgroup
+constexpr int kChunk = 16 << 10;   // bytes that a workgroup takes at a time: four vectors a thread
+constexpr int kSumBlocks = 4096, kScaleBlocks = 16384;
 constexpr int kMaxLaunches = (kMaxTensors + kSegments - 1) / kSegments;
+// Up to this many partial sums each workgroup of the second pass adds them up for itself; beyond, a kernel in between does.
+constexpr int kFewParts = 512;
+// Of gradients that the last-level cache (256 MB) does not hold, the first pass reads around it all but this much at the end,
+// where the second pass begins.
+constexpr int64_t kCacheBytes = (int64_t)256 << 20, kKeptBytes = (int64_t)192 << 20;
 
 // Tensors of a type that follow each other in memory.
 struct Segment {
@@ -47,36 +55,46 @@ struct Segment {
   int32_t chunk0;  // chunks of the launch before this segment
 };
 
-struct GnArgs {
-  Segment seg[kSegments];
+struct GnCall {
   int32_t segments, chunks;
-  int32_t chunk_bytes;
+  int32_t kept;        // chunks of this launch from this one on are read through the cache; chunks: all are
   int32_t parts;       // partial sums of the whole call
   int32_t part0;       // of this launch's first workgroup
   int32_t last;        // the launch that writes the norm
+  double limit;
+  double* sums;        // [parts], then the factor where parts > kFewParts
+  float* norm;
+};
+
+template <int SEGMENTS>
+struct GnArgs : GnCall {
+  Segment seg[SEGMENTS];
+};
+
+struct NormArgs {
+  int32_t parts;
   double limit;
   double* sums;
   float* norm;
 };
 
-__device__ __forceinline__ double wave_add(double v) {
-#pragma unroll
-  for (int d = 32; d >= 1; d >>= 1) v += __shfl_xor(v, d, 64);
-  return v;
-}
-
 // The workgroup's sum, in every thread.
-__device__ __forceinline__ double block_add(double v, double (&lds)[kThreads / 64]) {
-  v = wave_add(v);
+template <int THREADS>
+__device__ __forceinline__ double block_sum(double v, double (&lds)[THREADS / 64]) {
+  v = wave_sum(v);
   if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = v;
   __syncthreads();
-  v = (lds[0] + lds[1]) + (lds[2] + lds[3]);
-  __syncthreads();
+  v = 0.;
+#pragma unroll
+  for (int w = 0; w < THREADS / 64; ++w) v += lds[w];
   return v;
 }
 
+__device__ __forceinline__ double factor_of(double norm, double limit) { return norm > limit ? limit / norm : 1.; }
+
 // Which segment a chunk belongs to: the last one that starts at or before it.
-__device__ __forceinline__ int segment_of(const GnArgs& a, int chunk) {
+template <class Args>
+__device__ __forceinline__ int segment_of(const Args& a, int chunk) {
   int lo = 0, hi = a.segments - 1;
   while (lo < hi) {
     const int mid = (lo + hi + 1) >> 1;
@@ -88,146 +106,235 @@ __device__ __forceinline__ int segment_of(const GnArgs& a, int chunk) {
   return lo;
 }
 
-// f(element values of a vector, how many) over the elements [from, to) of a segment.
-template <int DTYPE>
-__device__ __forceinline__ double sum_range(const void* base, int64_t from, int64_t to) {
+// Both passes take a chunk, kChunk bytes or what is left of a segment, as four vectors a thread, all loaded before the first is used,
+// and its last elements one by one.
+template <int DTYPE, bool STREAM, class Vec, class One>
+__device__ __forceinline__ void each(const Segment& s, int64_t from, Vec&& vec, One&& one) {
   typedef Elem<DTYPE> E;
-  const typename E::T* const p = static_cast<const typename E::T*>(base) + from;
-  const int n = (int)(to - from), full = n / E::VEC;
-  double acc[2] = {0., 0.};
-#pragma unroll 4
-  for (int v = threadIdx.x; v < full; v += kThreads) {
-    const u32x4 r = load_vec<E>(p + v * E::VEC);
+  constexpr int VEC = E::VEC, PER = kChunk / 16 / kThreads;
+  const typename E::T* const p = static_cast<const typename E::T*>(s.in) + from;
+  const int64_t left = s.count - from;
+  const int n = left < kChunk / 16 * VEC ? (int)left : kChunk / 16 * VEC, full = n / VEC;
+  u32x4 r[PER];
 #pragma unroll
-    for (int i = 0; i < E::VEC; ++i) {
-      const double x = (double)E::get(r, i);
-      acc[i & 1] = fma(x, x, acc[i & 1]);
-    }
+  for (int j = 0; j < PER; ++j) {
+    const int v = j * kThreads + (int)threadIdx.x;
+    if (v < full) r[j] = get_vec<E, STREAM>(p + v * VEC);
   }
-  for (int i = full * E::VEC + threadIdx.x; i < n; i += kThreads) {
-    const double x = (double)E::to_float(p[i]);
-    acc[0] = fma(x, x, acc[0]);
+#pragma unroll
+  for (int j = 0; j < PER; ++j) {
+    const int v = j * kThreads + (int)threadIdx.x;
+    if (v < full) vec(r[j], from + v * VEC);
   }
+  const int i = full * VEC + (int)threadIdx.x;
+  if (i < n) one(p[i], from + i);
+}
+
+template <int DTYPE, bool STREAM>
+__device__ __forceinline__ double sum_chunk(const Segment& s, int64_t from) {
+  typedef Elem<DTYPE> E;
+  double acc[2] = {0., 0.};
+  each<DTYPE, STREAM>(
+      s, from,
+      [&](const u32x4& r, int64_t) {
+#pragma unroll
+        for (int i = 0; i < E::VEC; ++i) {
+          const double x = (double)E::get(r, i);
+          acc[i & 1] = fma(x, x, acc[i & 1]);
+        }
+      },
+      [&](typename E::T v, int64_t) {
+        const double x = (double)E::to_float(v);
+        acc[0] = fma(x, x, acc[0]);
+      });
   return acc[0] + acc[1];
 }
 
-struct __attribute__((packed, aligned(8))) Pair64Mem {
-  double v[2];
-};
-
-template <>
-__device__ __forceinline__ double sum_range<MI355_F64>(const void* base, int64_t from, int64_t to) {
-  const double* const p = static_cast<const double*>(base) + from;
-  const int n = (int)(to - from), full = n / 2;
-  double acc[2] = {0., 0.};
-#pragma unroll 4
-  for (int v = threadIdx.x; v < full; v += kThreads) {
-    const Pair64Mem r = *reinterpret_cast<const Pair64Mem*>(p + 2 * v);
-    acc[0] = fma(r.v[0], r.v[0], acc[0]);
-    acc[1] = fma(r.v[1], r.v[1], acc[1]);
-  }
-  if ((n & 1) && threadIdx.x == 0) acc[0] = fma(p[n - 1], p[n - 1], acc[0]);
-  return acc[0] + acc[1];
-}
-
-template <int DTYPE>
-__device__ __forceinline__ void scale_range(const void* base, void* out, int64_t from, int64_t to, double factor) {
+template <int DTYPE, bool STREAM_IN, bool STREAM_OUT>
+__device__ __forceinline__ void scale_chunk(const Segment& s, int64_t from, double factor) {
   typedef Elem<DTYPE> E;
-  const typename E::T* const p = static_cast<const typename E::T*>(base) + from;
-  typename E::T* const q = static_cast<typename E::T*>(out) + from;
-  const int n = (int)(to - from), full = n / E::VEC;
-  const float f = (float)factor;
-#pragma unroll 4
-  for (int v = threadIdx.x; v < full; v += kThreads) {
-    const u32x4 r = load_vec<E>(p + v * E::VEC);
-    float x[E::VEC];
+  typedef decltype(E::get(u32x4(), 0)) F;  // fp64 for fp64, fp32 for the others
+  typename E::T* const q = static_cast<typename E::T*>(s.out);
+  const F f = (F)factor;
+  each<DTYPE, STREAM_IN>(
+      s, from,
+      [&](const u32x4& r, int64_t at) {
+        F x[E::VEC];
 #pragma unroll
-    for (int i = 0; i < E::VEC; ++i) x[i] = E::get(r, i) * f;
-    store_vec<E>(q + v * E::VEC, E::pack(x));
-  }
-  for (int i = full * E::VEC + threadIdx.x; i < n; i += kThreads) q[i] = E::from_float(E::to_float(p[i]) * f);
+        for (int i = 0; i < E::VEC; ++i) x[i] = E::get(r, i) * f;
+        put_vec<E, STREAM_OUT>(q + at, E::pack(x));
+      },
+      [&](typename E::T v, int64_t at) { q[at] = E::from_float(E::to_float(v) * f); });
 }
 
-template <>
-__device__ __forceinline__ void scale_range<MI355_F64>(const void* base, void* out, int64_t from, int64_t to, double factor) {
-  const double* const p = static_cast<const double*>(base) + from;
-  double* const q = static_cast<double*>(out) + from;
-  const int n = (int)(to - from), full = n / 2;
-#pragma unroll 4
-  for (int v = threadIdx.x; v < full; v += kThreads) {
-    Pair64Mem r = *reinterpret_cast<const Pair64Mem*>(p + 2 * v);
-    r.v[0] *= factor;
-    r.v[1] *= factor;
-    *reinterpret_cast<Pair64Mem*>(q + 2 * v) = r;
+__device__ __forceinline__ int elem_shift(int dtype) { return dtype == MI355_F64 ? 3 : dtype == MI355_F32 ? 2 : 1; }
+
+template <bool STREAM>
+__device__ __forceinline__ double sum_any(const Segment& s, int64_t from) {
+  switch (s.dtype) {
+    case MI355_F32: return sum_chunk<MI355_F32, STREAM>(s, from);
+    case MI355_F16: return sum_chunk<MI355_F16, STREAM>(s, from);
+    case MI355_BF16: return sum_chunk<MI355_BF16, STREAM>(s, from);
+    default: return sum_chunk<MI355_F64, STREAM>(s, from);
   }
-  if ((n & 1) && threadIdx.x == 0) q[n - 1] = p[n - 1] * factor;
 }
 
-__device__ __forceinline__ int elem_bytes(int dtype) { return dtype == MI355_F64 ? 8 : dtype == MI355_F32 ? 4 : 2; }
+template <bool STREAM_IN, bool STREAM_OUT>
+__device__ __forceinline__ void scale_any(const Segment& s, int64_t from, double factor) {
+  switch (s.dtype) {
+    case MI355_F32: scale_chunk<MI355_F32, STREAM_IN, STREAM_OUT>(s, from, factor); break;
+    case MI355_F16: scale_chunk<MI355_F16, STREAM_IN, STREAM_OUT>(s, from, factor); break;
+    case MI355_BF16: scale_chunk<MI355_BF16, STREAM_IN, STREAM_OUT>(s, from, factor); break;
+    default: scale_chunk<MI355_F64, STREAM_IN, STREAM_OUT>(s, from, factor);
+  }
+}
 
-__global__ __launch_bounds__(kThreads) void gn_sum_kernel(const GnArgs a) {
+template <int SEGMENTS, bool STREAM>
+__global__ __launch_bounds__(kThreads) void gn_sum_kernel(const GnArgs<SEGMENTS> a) {
   __shared__ double lds[kThreads / 64];
   double sum = 0.;
   for (int c = blockIdx.x; c < a.chunks; c += gridDim.x) {
     const Segment& s = a.seg[segment_of(a, c)];
-    const int64_t per = a.chunk_bytes / elem_bytes(s.dtype), from = (int64_t)(c - s.chunk0) * per;
-    const int64_t to = from + per < s.count ? from + per : s.count;
-    switch (s.dtype) {
-      case MI355_F32: sum += sum_range<MI355_F32>(s.in, from, to); break;
-      case MI355_F16: sum += sum_range<MI355_F16>(s.in, from, to); break;
-      case MI355_BF16: sum += sum_range<MI355_BF16>(s.in, from, to); break;
-      default: sum += sum_range<MI355_F64>(s.in, from, to);
-    }
+    const int64_t from = (int64_t)(c - s.chunk0) * (kChunk >> elem_shift(s.dtype));
+    if (STREAM && c < a.kept)
+      sum += sum_any<true>(s, from);
+    else
+      sum += sum_any<false>(s, from);
   }
-  sum = block_add(sum, lds);
+  sum = block_sum<kThreads>(sum, lds);
   if (threadIdx.x == 0) a.sums[a.part0 + blockIdx.x] = sum;
 }
 
-__global__ __launch_bounds__(kThreads) void gn_scale_kernel(const GnArgs a) {
-  __shared__ double lds[kThreads / 64];
+// The norm and the factor of many partial sums.
+__global__ __launch_bounds__(1024) void gn_norm_kernel(const NormArgs a) {
+  __shared__ double lds[16];
   double sum = 0.;
-  for (int i = threadIdx.x; i < a.parts; i += kThreads) sum += a.sums[i];
-  const double norm = sqrt(block_add(sum, lds));
-  if (a.last && a.norm && blockIdx.x == 0 && threadIdx.x == 0) *a.norm = (float)norm;
-  const double factor = norm > a.limit ? a.limit / norm : 1.;
+  for (int i = threadIdx.x; i < a.parts; i += 1024) sum += a.sums[i];
+  const double norm = sqrt(block_sum<1024>(sum, lds));
+  if (threadIdx.x == 0) {
+    if (a.norm) *a.norm = (float)norm;
+    a.sums[a.parts] = factor_of(norm, a.limit);
+  }
+}
+
+template <int SEGMENTS, bool STREAM_IN, bool STREAM_OUT>
+__global__ __launch_bounds__(kThreads) void gn_scale_kernel(const GnArgs<SEGMENTS> a) {
+  __shared__ double lds[kThreads / 64];
+  double factor;
+  if (a.parts > kFewParts) {
+    factor = a.sums[a.parts];
+  } else {
+    double sum = 0.;
+    for (int i = threadIdx.x; i < a.parts; i += kThreads) sum += a.sums[i];
+    const double norm = sqrt(block_sum<kThreads>(sum, lds));
+    if (a.last && a.norm && blockIdx.x == 0 && threadIdx.x == 0) *a.norm = (float)norm;
+    factor = factor_of(norm, a.limit);
+  }
   for (int c0 = blockIdx.x; c0 < a.chunks; c0 += gridDim.x) {
     const int c = a.chunks - 1 - c0;
     const Segment& s = a.seg[segment_of(a, c)];
     if (factor == 1. && s.in == s.out) continue;
-    const int64_t per = a.chunk_bytes / elem_bytes(s.dtype), from = (int64_t)(c - s.chunk0) * per;
-    const int64_t to = from + per < s.count ? from + per : s.count;
-    switch (s.dtype) {
-      case MI355_F32: scale_range<MI355_F32>(s.in, s.out, from, to, factor); break;
-      case MI355_F16: scale_range<MI355_F16>(s.in, s.out, from, to, factor); break;
-      case MI355_BF16: scale_range<MI355_BF16>(s.in, s.out, from, to, factor); break;
-      default: scale_range<MI355_F64>(s.in, s.out, from, to, factor);
-    }
+    const int64_t from = (int64_t)(c - s.chunk0) * (kChunk >> elem_shift(s.dtype));
+    if (STREAM_IN && c < a.kept)
+      scale_any<true, STREAM_OUT>(s, from, factor);
+    else
+      scale_any<false, STREAM_OUT>(s, from, factor);
   }
 }
 
 // The tensors in runs of those that follow each other, from tensor i on: the table of one launch.  Returns the next launch's first.
-int next_launch(const gn_desc* d, const void* const* grads, void* const* outs, int i, int chunk_bytes, GnArgs& a) {
+// (A run goes on where its type's last tensor ended, whatever other types stand between.)
+int next_launch(const gn_desc* d, const void* const* grads, void* const* outs, int i, GnArgs<kSegments>& a) {
   a.segments = a.chunks = 0;
+  Segment* open[4] = {};
   for (; i < d->tensors; ++i) {
     const int64_t n = d->counts[i];
     if (n == 0) continue;
     const int size = dtype_bytes(d->dtypes[i]);
-    Segment* const s = a.segments ? &a.seg[a.segments - 1] : nullptr;
-    if (s && s->dtype == d->dtypes[i] && static_cast<const char*>(s->in) + s->count * size == grads[i] &&
-        static_cast<char*>(s->out) + s->count * size == outs[i]) {
+    Segment* const s = open[d->dtypes[i]];
+    if (s && static_cast<const char*>(s->in) + s->count * size == grads[i] && static_cast<char*>(s->out) + s->count * size == outs[i]) {
       s->count += n;
       continue;
     }
     if (a.segments == kSegments) break;
-    a.seg[a.segments++] = Segment{grads[i], outs[i], n, d->dtypes[i], 0};
+    a.seg[a.segments] = Segment{grads[i], outs[i], n, d->dtypes[i], 0};
+    open[d->dtypes[i]] = &a.seg[a.segments++];
   }
   for (int k = 0; k < a.segments; ++k) {
     Segment& s = a.seg[k];
     s.chunk0 = a.chunks;
-    const int64_t per = chunk_bytes / dtype_bytes(s.dtype);
+    const int64_t per = kChunk / dtype_bytes(s.dtype);
     a.chunks += (int32_t)((s.count + per - 1) / per);
   }
   return i;
+}
+
+GnArgs<kFewSegments> few(const GnArgs<kSegments>& a) {
+  GnArgs<kFewSegments> t;
+  static_cast<GnCall&>(t) = a;
+  std::copy(a.seg, a.seg + kFewSegments, t.seg);
+  return t;
+}
+
+template <bool STREAM>
+void launch_sum(const GnArgs<kSegments>& a, int blocks, hipStream_t stream) {
+  if (a.segments <= kFewSegments)
+    hipLaunchKernelGGL((gn_sum_kernel<kFewSegments, STREAM>), dim3(blocks), dim3(kThreads), 0, stream, few(a));
+  else
+    hipLaunchKernelGGL((gn_sum_kernel<kSegments, STREAM>), dim3(blocks), dim3(kThreads), 0, stream, a);
+}
+
+template <bool STREAM_IN, bool STREAM_OUT>
+void launch_scale(const GnArgs<kSegments>& a, int blocks, hipStream_t stream) {
+  if (a.segments <= kFewSegments)
+    hipLaunchKernelGGL((gn_scale_kernel<kFewSegments, STREAM_IN, STREAM_OUT>), dim3(blocks), dim3(kThreads), 0, stream, few(a));
+  else
+    hipLaunchKernelGGL((gn_scale_kernel<kSegments, STREAM_IN, STREAM_OUT>), dim3(blocks), dim3(kThreads), 0, stream, a);
+}
+
+int run_clip(const gn_desc* d, const void* const* grads, void* const* outs, GnArgs<kSegments>& a, hipStream_t stream) {
+  int launches = 0;
+  int64_t chunks = 0, out_bytes = 0;  // of the outputs in other memory
+  for (int i = 0; i < d->tensors || launches == 0; ++launches) {
+    i = next_launch(d, grads, outs, i, a);
+    chunks += a.chunks;
+    for (int k = 0; k < a.segments; ++k)
+      if (a.seg[k].in != a.seg[k].out) out_bytes += a.seg[k].count * dtype_bytes(a.seg[k].dtype);
+  }
+  const bool stream_in = d->bytes > kCacheBytes, stream_out = d->bytes + out_bytes > kCacheBytes;
+  const int64_t kept = chunks - (stream_in ? kKeptBytes / kChunk : chunks);  // of all chunks, those from here on
+  const int most = std::max(1, kSumBlocks / launches);
+  int64_t before = 0;
+  a.parts = 0;
+  for (int i = 0, k = 0; k < launches; ++k) {
+    if (launches > 1) i = next_launch(d, grads, outs, i, a);
+    a.kept = (int32_t)std::max<int64_t>(0, std::min<int64_t>(kept - before, a.chunks));
+    before += a.chunks;
+    a.part0 = a.parts;
+    const int blocks = std::max(1, std::min(a.chunks, most));
+    a.parts += blocks;
+    stream_in ? launch_sum<true>(a, blocks, stream) : launch_sum<false>(a, blocks, stream);
+    const int e = (int)hipGetLastError();
+    if (e) return e;
+  }
+  if (a.parts > kFewParts) {
+    const NormArgs n = {a.parts, a.limit, a.sums, a.norm};
+    hipLaunchKernelGGL(gn_norm_kernel, dim3(1), dim3(1024), 0, stream, n);
+    const int e = (int)hipGetLastError();
+    if (e) return e;
+  }
+  before = 0;
+  for (int i = 0, k = 0; k < launches; ++k) {
+    if (launches > 1) i = next_launch(d, grads, outs, i, a);
+    a.kept = (int32_t)std::max<int64_t>(0, std::min<int64_t>(kept - before, a.chunks));
+    before += a.chunks;
+    a.last = k == launches - 1;
+    const int blocks = std::max(1, std::min(a.chunks, kScaleBlocks));
+    stream_in ? launch_scale<true, true>(a, blocks, stream) : stream_out ? launch_scale<false, true>(a, blocks, stream) : launch_scale<false, false>(a, blocks, stream);
+    const int e = (int)hipGetLastError();
+    if (e) return e;
+  }
+  return 0;
 }
 
 }  // namespace
@@ -262,7 +369,7 @@ int gn_desc_create(gn_desc_t** out, const gn_params_t* p) {
     std::copy(p->counts, p->counts + p->tensors, d->counts);
     std::copy(p->dtypes, p->dtypes + p->tensors, d->dtypes);
   }
-  d->ws_bytes = (size_t)(kBlocks + kMaxLaunches) * sizeof(double);
+  d->ws_bytes = (size_t)(kSumBlocks + kMaxLaunches + 1) * sizeof(double);
   snprintf(d->names, sizeof(d->names), "clip=gn_sum+gn_scale(T=%d)", d->tensors);
   *out = d;
   return CONV_OK;
@@ -291,38 +398,12 @@ int gn_clip(const gn_desc_t* d, const void* const* grads, double limit, void* co
     if (d->counts[i] > 0 && (!grads[i] || !outs[i])) return CONV_EINVAL;
   if (!ws || ws_bytes < d->ws_bytes) return CONV_EWORKSPACE;
   if ((uintptr_t)ws & 15u) return CONV_EINVAL;
-  const hipStream_t stream = (hipStream_t)hip_stream;
-  GnArgs a = {};
-  // A chunk is what a workgroup takes at a time: large ones where there is enough for every workgroup.
-  a.chunk_bytes = (int32_t)std::min<int64_t>(std::max<int64_t>(d->bytes / kBlocks / 4096 * 4096, 4096), 64 << 10);
-  while (d->bytes / a.chunk_bytes >= 1 << 30) a.chunk_bytes *= 2;
+  GnArgs<kSegments> a = {};
   a.limit = limit;
   a.sums = static_cast<double*>(ws);
   a.norm = norm;
-  int launches = 0;
-  for (int i = 0; i < d->tensors || launches == 0; ++launches) {
-    GnArgs t = a;
-    i = next_launch(d, grads, outs, i, a.chunk_bytes, t);
-  }
-  const int most = std::max(1, kBlocks / launches);
-  a.parts = 0;
-  for (int i = 0, k = 0; k < launches; ++k) {
-    i = next_launch(d, grads, outs, i, a.chunk_bytes, a);
-    a.part0 = a.parts;
-    const int blocks = std::max(1, std::min(a.chunks, most));
-    a.parts += blocks;
-    hipLaunchKernelGGL(gn_sum_kernel, dim3(blocks), dim3(kThreads), 0, stream, a);
-    const int e = (int)hipGetLastError();
-    if (e) return record_hip_error(e);
-  }
-  for (int i = 0, k = 0; k < launches; ++k) {
-    i = next_launch(d, grads, outs, i, a.chunk_bytes, a);
-    a.last = k == launches - 1;
-    hipLaunchKernelGGL(gn_scale_kernel, dim3(std::max(1, std::min(a.chunks, kBlocks))), dim3(kThreads), 0, stream, a);
-    const int e = (int)hipGetLastError();
-    if (e) return record_hip_error(e);
-  }
-  return CONV_OK;
+  const int e = run_clip(d, grads, outs, a, (hipStream_t)hip_stream);
+  return e ? record_hip_error(e) : CONV_OK;
 }
 
 }  // extern "C"

@@ -179,25 +179,17 @@ __device__ __forceinline__ u32x4 without_first(const u32x4& v, int lo) {
 }
 
 // Vector v (v VEC < n), wherever it lies.
-template <class E>
+template <class E, bool STREAM = false>
 __device__ __forceinline__ u32x4 row_vec(const typename E::T* row, int v, int n) {
   const Slot<E> at = slot_of<E>(v, n);
   if (at.base >= 0) {
-    const u32x4 r = load_vec<E>(row + at.base);
+    const u32x4 r = get_vec<E, STREAM>(row + at.base);
     return at.lo ? without_first<E>(r, at.lo) : r;
   }
   float x[E::VEC];
 #pragma unroll
   for (int i = 0; i < E::VEC; ++i) x[i] = i >= at.lo ? E::to_float(row[at.base + i]) : -INFINITY;
   return E::pack(x);
-}
-
-template <class E, bool STREAM>
-__device__ __forceinline__ void put_vec(typename E::T* at, const u32x4& v) {
-  if constexpr (STREAM)
-    stream_vec<E>(at, v);
-  else
-    store_vec<E>(at, v);
 }
 
 template <class E, bool STREAM>
@@ -442,7 +434,7 @@ enum Mode { kScore, kTrain, kPart };
 
 // A row (kPart: a part of one) is read once, into registers, up to NV vectors a thread; what is beyond them is read again by
 // whatever needs it again.  THREADS 64: a wave for each row, several in a workgroup.
-// STREAM: the gradient goes around the last-level cache.
+// STREAM: what is read and written once goes around the last-level cache.
 template <int DTYPE, int THREADS, int NV, Mode MODE, bool ENT, bool STREAM>
 __global__ __launch_bounds__(THREADS == 64 ? 256 : THREADS, THREADS == 64 ? 1 : 4) void lp_row_kernel(LpArgs a) {
   typedef Elem<DTYPE> E;
@@ -475,7 +467,7 @@ __global__ __launch_bounds__(THREADS == 64 ? 256 : THREADS, THREADS == 64 ? 1 : 
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
       r[j] = lowest_vec<E>();
-      if (j * THREADS < full && j * THREADS + tid < full) r[j] = load_vec<E>(row + (j * THREADS + tid) * VEC);
+      if (j * THREADS < full && j * THREADS + tid < full) r[j] = get_vec<E, STREAM>(row + (j * THREADS + tid) * VEC);
     }
     if (full < nv && tid == 0) tail = row_vec<E>(row, full, n);
     forget(r);
@@ -647,7 +639,7 @@ __global__ __launch_bounds__(256) void lp_grad_kernel(LpArgs a, int chunks) {
 #pragma unroll
     for (int j = 0; j < kGradVecs; ++j) {
       const int v = j * 256 + (int)threadIdx.x;
-      r[j] = v < nv ? row_vec<E>(row + first, v, n) : lowest_vec<E>();
+      r[j] = v < nv ? row_vec<E, STREAM>(row + first, v, n) : lowest_vec<E>();
     }
     int token = a.token[r_];
     if ((uint32_t)token >= (uint32_t)a.vocab) token = -1;
@@ -735,9 +727,9 @@ int launch_grad(const LpArgs& a, hipStream_t stream) {
   return (int)hipGetLastError();
 }
 
-// Whether logits and gradient together are more than the last-level cache holds: the gradient then goes around it, and leaves it to the
-// logits that are read a second time and to whoever reads the gradient's end.
-bool streams(const lp_desc* d) { return (double)d->p.rows * d->p.vocab * dtype_bytes(d->p.dtype) * 2 > (double)(256 << 20); }
+// Whether the logits, or they and the gradient, are more than the last-level cache (256 MB) holds: they then go around it, and leave it to
+// what is read a second time.  Training on 4096 x 128256: 455 us through it, 442 with the gradient around it, STREAMED with both.
+bool streams(const lp_desc* d, int blobs) { return (double)d->p.rows * d->p.vocab * dtype_bytes(d->p.dtype) * blobs > (double)(256 << 20); }
 
 // One of the descriptor's six kinds.
 template <template <int, bool> class Op>
@@ -753,7 +745,7 @@ int by_kind(const lp_desc* d, const LpArgs& a, hipStream_t stream) {
 template <int DTYPE, bool ENT>
 struct Forward {
   static int run(const lp_desc* d, const LpArgs& a, hipStream_t stream) {
-    if (d->splits == 1) return launch_row<DTYPE, kScore, ENT, false>(d, a, stream);
+    if (d->splits == 1) return streams(d, 1) ? launch_row<DTYPE, kScore, ENT, true>(d, a, stream) : launch_row<DTYPE, kScore, ENT, false>(d, a, stream);
     const int e = launch_row<DTYPE, kPart, ENT, false>(d, a, stream);
     return e ? e : launch_join<DTYPE, ENT>(a, stream);
   }
@@ -762,14 +754,14 @@ struct Forward {
 template <int DTYPE, bool ENT>
 struct Backward {
   static int run(const lp_desc* d, const LpArgs& a, hipStream_t stream) {
-    return streams(d) ? launch_grad<DTYPE, ENT, false, true>(a, stream) : launch_grad<DTYPE, ENT, false, false>(a, stream);
+    return streams(d, 2) ? launch_grad<DTYPE, ENT, false, true>(a, stream) : launch_grad<DTYPE, ENT, false, false>(a, stream);
   }
 };
 
 template <int DTYPE, bool ENT>
 struct ForwardBackward {
   static int run(const lp_desc* d, const LpArgs& a, hipStream_t stream) {
-    if (d->splits == 1) return streams(d) ? launch_row<DTYPE, kTrain, ENT, true>(d, a, stream) : launch_row<DTYPE, kTrain, ENT, false>(d, a, stream);
+    if (d->splits == 1) return streams(d, 2) ? launch_row<DTYPE, kTrain, ENT, true>(d, a, stream) : launch_row<DTYPE, kTrain, ENT, false>(d, a, stream);
     const int e = launch_row<DTYPE, kPart, ENT, false>(d, a, stream);
     return e ? e : launch_grad<DTYPE, ENT, true, false>(a, stream);
   }
