@@ -470,7 +470,6 @@ __global__ __launch_bounds__(THREADS == 64 ? 256 : THREADS, THREADS == 64 ? 1 : 
       if (j * THREADS < full && j * THREADS + tid < full) r[j] = get_vec<E, STREAM>(row + (j * THREADS + tid) * VEC);
     }
     if (full < nv && tid == 0) tail = row_vec<E>(row, full, n);
-    forget(r);
 
     float m = -INFINITY, M = 0.f, s = 0.f, s2 = 0.f;
 #pragma unroll

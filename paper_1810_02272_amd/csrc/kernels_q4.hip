@@ -22,6 +22,9 @@
 #include "internal.h"
 #include "mi355q4.h"
 
+#ifndef STREAM_MB
+#define STREAM_MB 240
+#endif
 struct q4_desc {
   q4_params_t p;
   int32_t tiles, blocks;  // of 16 outputs and 128 inputs
@@ -202,8 +205,9 @@ template <int MT>
 constexpr int kMostWaves = MT == 1 ? 16 : 8;
 
 // MT times 16 rows of x by NT tiles of 16 outputs in a workgroup; its waves take the blocks of inputs in turn, each on its own, and
-// add up through shared memory at the end: nothing of x is used by two waves.  REGS: result registers that hold rows.
-template <int DTYPE, int MT, int NT, int REGS, int GROUP>
+// add up through shared memory at the end: nothing of x is used by two waves.  REGS: result registers that hold rows.  STREAM: the codes
+// go around the last-level cache.
+template <int DTYPE, int MT, int NT, int REGS, int GROUP, bool STREAM>
 __global__ __launch_bounds__(kMostWaves<MT> * 64) void q4_kernel(Q4Args a) {
   typedef Operand<DTYPE> Op;
   typedef Elem<DTYPE> E;
@@ -230,7 +234,10 @@ __global__ __launch_bounds__(kMostWaves<MT> * 64) void q4_kernel(Q4Args a) {
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
           const int64_t tb = (int64_t)min(tile0 + n, a.tiles - 1) * a.blocks + b;
-          w[n] = a.codes[tb * 64 + lane];
+          if constexpr (STREAM)
+            w[n] = __builtin_nontemporal_load(&a.codes[tb * 64 + lane]);
+          else
+            w[n] = a.codes[tb * 64 + lane];
           load_scales<PER>(a.scales + (tb * kTile + (lane & 15)) * PER, scale[n]);
         }
         f32x4 sum[MT][NT] = {};
@@ -326,15 +333,17 @@ size_t terms_bytes(const q4_desc* d) {
   return (tiles + per - 1) / per * per * d->blocks * 4 * 3 * 1024;
 }
 
-template <int DTYPE, int MT, int NT, int REGS>
+size_t codes_bytes(const q4_desc* d) { return (size_t)d->tiles * d->blocks * 1024; }
+
+template <int DTYPE, int MT, int NT, int REGS, bool STREAM = false>
 void launch_group(const q4_desc* d, const Q4Args& a, hipStream_t stream) {
   const int groups = (d->tiles + NT - 1) / NT;
   const dim3 grid(std::min(groups, 1 << 22), d->splits), block(64 * d->waves);
   const size_t lds = (size_t)d->waves * NT * REGS * 256;  // at most 64 KB
   switch (d->p.group) {
-    case 32: hipLaunchKernelGGL((q4_kernel<DTYPE, MT, NT, REGS, 32>), grid, block, lds, stream, a); break;
-    case 64: hipLaunchKernelGGL((q4_kernel<DTYPE, MT, NT, REGS, 64>), grid, block, lds, stream, a); break;
-    default: hipLaunchKernelGGL((q4_kernel<DTYPE, MT, NT, REGS, 128>), grid, block, lds, stream, a);
+    case 32: hipLaunchKernelGGL((q4_kernel<DTYPE, MT, NT, REGS, 32, STREAM>), grid, block, lds, stream, a); break;
+    case 64: hipLaunchKernelGGL((q4_kernel<DTYPE, MT, NT, REGS, 64, STREAM>), grid, block, lds, stream, a); break;
+    default: hipLaunchKernelGGL((q4_kernel<DTYPE, MT, NT, REGS, 128, STREAM>), grid, block, lds, stream, a);
   }
 }
 
@@ -347,12 +356,15 @@ int launch_forward(const q4_desc* d, const Q4Args& a, hipStream_t stream) {
     const int e = (int)hipGetLastError();
     if (e) return e;
   }
+  // Codes that the last-level cache (256 MB) does not hold from call to call go around it.
+  const bool stream_codes = codes_bytes(d) > (size_t)STREAM_MB << 20;
   switch (m_tiles(d)) {
     case 1:
       if (d->p.m <= 4)
-        d->nt == 1 ? launch_group<DTYPE, 1, 1, 1>(d, a, stream) : launch_group<DTYPE, 1, 2, 1>(d, a, stream);
+        d->nt == 1 ? launch_group<DTYPE, 1, 1, 1>(d, a, stream)
+                   : stream_codes ? launch_group<DTYPE, 1, 2, 1, true>(d, a, stream) : launch_group<DTYPE, 1, 2, 1>(d, a, stream);
       else
-        launch_group<DTYPE, 1, 2, 4>(d, a, stream);
+        stream_codes ? launch_group<DTYPE, 1, 2, 4, true>(d, a, stream) : launch_group<DTYPE, 1, 2, 4>(d, a, stream);
       break;
     case 2: launch_group<DTYPE, 2, 4, 4>(d, a, stream); break;
     case 3: launch_group<DTYPE, 3, 4, 4>(d, a, stream); break;
@@ -364,8 +376,6 @@ int launch_forward(const q4_desc* d, const Q4Args& a, hipStream_t stream) {
   hipLaunchKernelGGL(q4_join_kernel<DTYPE>, dim3((uint32_t)std::min<int64_t>((count + 255) / 256, 4096)), dim3(256), 0, stream, a);
   return (int)hipGetLastError();
 }
-
-size_t codes_bytes(const q4_desc* d) { return (size_t)d->tiles * d->blocks * 1024; }
 
 }  // namespace
 
