@@ -22,9 +22,6 @@
 #include "internal.h"
 #include "mi355q4.h"
 
-#ifndef STREAM_MB
-#define STREAM_MB 240
-#endif
 struct q4_desc {
   q4_params_t p;
   int32_t tiles, blocks;  // of 16 outputs and 128 inputs
@@ -223,14 +220,16 @@ __global__ __launch_bounds__(kMostWaves<MT> * 64) void q4_kernel(Q4Args a) {
     for (int m0 = 0; m0 < a.m; m0 += 16 * MT) {
       f32x4 acc[MT][NT] = {};
       const typename E::T* rows[MT];
+      int from[MT];  // fp32: the lane whose operand is read, the tile's first row's where there is no row
+#pragma unroll
+      for (int t = 0; t < MT; ++t) from[t] = m0 + 16 * t + place_row(lane & 15) < a.m ? lane : lane & 48;
       if constexpr (TERMS == 1) {
 #pragma unroll
         for (int t = 0; t < MT; ++t)  // (rows beyond m: the last one's values again, for results that nobody stores)
           rows[t] = static_cast<const typename E::T*>(a.x) + (int64_t)min(m0 + 16 * t + place_row(lane & 15), a.m - 1) * a.k + 8 * quarter;
       }
-      auto block = [&](int b, auto guarded) {
-        u32x4 w[NT];
-        float scale[NT][PER];
+      // A block's codes and scales; its operands of inputs 32 d and on (GUARDED: zeros beyond k); their products.
+      auto load_codes = [&](int b, u32x4(&w)[NT], float(&scale)[NT][PER]) {
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
           const int64_t tb = (int64_t)min(tile0 + n, a.tiles - 1) * a.blocks + b;
@@ -240,50 +239,107 @@ __global__ __launch_bounds__(kMostWaves<MT> * 64) void q4_kernel(Q4Args a) {
             w[n] = a.codes[tb * 64 + lane];
           load_scales<PER>(a.scales + (tb * kTile + (lane & 15)) * PER, scale[n]);
         }
-        f32x4 sum[MT][NT] = {};
+      };
+      auto load_x = [&](int b, int d, V(&x)[MT][TERMS], auto guarded) {
 #pragma unroll
-        for (int d = 0; d < 4; ++d) {
-          V x[MT][TERMS];
+        for (int t = 0; t < MT; ++t) {
+          if constexpr (TERMS > 1) {
 #pragma unroll
-          for (int t = 0; t < MT; ++t) {
-            if constexpr (TERMS > 1) {
+            for (int i = 0; i < TERMS; ++i)
+              x[t][i] = __builtin_bit_cast(V, a.terms[(((int64_t)(m0 / 16 + t) * a.blocks * 4 + b * 4 + d) * TERMS + i) * 64 + from[t]]);
+          } else {
+            const int at = b * kBlockK + 32 * d;
+            if constexpr (decltype(guarded)::value) {
+              typename E::T f[8];
 #pragma unroll
-              for (int i = 0; i < TERMS; ++i)
-                x[t][i] = __builtin_bit_cast(V, a.terms[(((int64_t)(m0 / 16 + t) * a.blocks * 4 + b * 4 + d) * TERMS + i) * 64 + lane]);
+              for (int i = 0; i < 8; ++i) f[i] = at + 8 * quarter + i < a.k ? rows[t][at + i] : (typename E::T)0.f;
+#pragma unroll
+              for (int i = 0; i < 8; ++i) x[t][0][i] = f[i];
             } else {
-              const int at = b * kBlockK + 32 * d;
-              if constexpr (decltype(guarded)::value) {
-                typename E::T f[8];
-#pragma unroll
-                for (int i = 0; i < 8; ++i) f[i] = at + 8 * quarter + i < a.k ? rows[t][at + i] : (typename E::T)0.f;
-#pragma unroll
-                for (int i = 0; i < 8; ++i) x[t][0][i] = f[i];
-              } else {
-                x[t][0] = __builtin_bit_cast(V, load_vec<E>(rows[t] + at));
-              }
-            }
-          }
-#pragma unroll
-          for (int n = 0; n < NT; ++n) {
-            const V wv = Op::weights(w[n][d]);
-#pragma unroll
-            for (int t = 0; t < MT; ++t) {
-              f32x4 z = d * 32 % GROUP == 0 ? f32x4{0.f, 0.f, 0.f, 0.f} : sum[t][n];
-#pragma unroll
-              for (int i = 0; i < TERMS; ++i) z = Op::mma(x[t][i], wv, z);
-              sum[t][n] = z;
-              if ((d + 1) * 32 % GROUP == 0) {
-#pragma unroll
-                for (int r = 0; r < REGS; ++r) acc[t][n][r] = fmaf(z[r], scale[n][d * 32 / GROUP], acc[t][n][r]);
-              }
+              x[t][0] = __builtin_bit_cast(V, load_vec<E>(rows[t] + at));
             }
           }
         }
       };
+      f32x4 sum[MT][NT];
+      auto multiply = [&](int d, const u32x4(&w)[NT], const float(&scale)[NT][PER], const V(&x)[MT][TERMS]) {
+        V wv[NT];
+#pragma unroll
+        for (int n = 0; n < NT; ++n) wv[n] = Op::weights(w[n][d]);
+        // (term by term: an instruction that adds to the one before it would wait for it)
+#pragma unroll
+        for (int i = 0; i < TERMS; ++i)
+#pragma unroll
+          for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int t = 0; t < MT; ++t)
+              sum[t][n] = Op::mma(x[t][i], wv[n], i == 0 && d * 32 % GROUP == 0 ? f32x4{0.f, 0.f, 0.f, 0.f} : sum[t][n]);
+        if ((d + 1) * 32 % GROUP == 0) {
+#pragma unroll
+          for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int t = 0; t < MT; ++t)
+#pragma unroll
+              for (int r = 0; r < REGS; ++r) acc[t][n][r] = fmaf(sum[t][n][r], scale[n][d * 32 / GROUP], acc[t][n][r]);
+        }
+      };
+      u32x4 w[NT];
+      float scale[NT][PER];
       const int full = TERMS > 1 ? end : min(end, a.k / kBlockK);
       int b = begin + wave;
-      for (; b < full; b += waves) block(b, std::false_type());
-      if (TERMS == 1 && b < end) block(b, std::true_type());
+      if constexpr (MT == 2 || MT == 3) {
+        // Two waves on a SIMD do not hide a load: operands are asked for two steps ahead, codes one block ahead.  (64 rows leave no
+        // registers for that.  64 x 4096 -> 8000: 20.8 us without, 23.4 with; 48 x 12000 -> 500: 18.8 without, 15.9 with.)
+        if (b < full) {
+          V x[2][MT][TERMS];
+          load_codes(b, w, scale);
+          load_x(b, 0, x[0], std::false_type());
+          load_x(b, 1, x[1], std::false_type());
+          for (; b < full; b += waves) {
+            const int next = b + waves < full ? b + waves : b;  // (the last one's again)
+            u32x4 next_w[NT];
+            float next_scale[NT][PER];
+            multiply(0, w, scale, x[0]);
+            load_x(b, 2, x[0], std::false_type());
+            __builtin_amdgcn_sched_barrier(0);
+            multiply(1, w, scale, x[1]);
+            load_x(b, 3, x[1], std::false_type());
+            load_codes(next, next_w, next_scale);
+            __builtin_amdgcn_sched_barrier(0);
+            multiply(2, w, scale, x[0]);
+            load_x(next, 0, x[0], std::false_type());
+            __builtin_amdgcn_sched_barrier(0);
+            multiply(3, w, scale, x[1]);
+            load_x(next, 1, x[1], std::false_type());
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+              w[n] = next_w[n];
+#pragma unroll
+              for (int g = 0; g < PER; ++g) scale[n][g] = next_scale[n][g];
+            }
+          }
+        }
+      } else {
+        for (; b < full; b += waves) {
+          load_codes(b, w, scale);
+#pragma unroll
+          for (int d = 0; d < 4; ++d) {
+            V x[MT][TERMS];
+            load_x(b, d, x, std::false_type());
+            multiply(d, w, scale, x);
+          }
+        }
+      }
+      if (TERMS == 1 && b < end) {
+        load_codes(b, w, scale);
+#pragma unroll
+        for (int d = 0; d < 4; ++d) {
+          V x[MT][TERMS];
+          load_x(b, d, x, std::true_type());
+          multiply(d, w, scale, x);
+        }
+      }
 
 #pragma unroll
       for (int t = 0; t < MT; ++t) {
@@ -295,6 +351,7 @@ __global__ __launch_bounds__(kMostWaves<MT> * 64) void q4_kernel(Q4Args a) {
         __syncthreads();
         for (int i = threadIdx.x; i < SLOT; i += blockDim.x) {
           float v = parts[i];
+#pragma unroll 4
           for (int p = 1; p < waves; ++p) v += parts[p * SLOT + i];
           const int nr = i >> 6, out = (tile0 + nr / REGS) * kTile + (i & 15), row = m0 + 16 * t + 4 * (nr % REGS) + (i >> 4 & 3);
           if (out >= a.o || row >= a.m) continue;
@@ -312,15 +369,20 @@ __global__ __launch_bounds__(kMostWaves<MT> * 64) void q4_kernel(Q4Args a) {
   }
 }
 
-// The splits' sums in one.
+// The splits' sums in one: a workgroup for 256 outputs of a row.
 template <int DTYPE>
 __global__ __launch_bounds__(256) void q4_join_kernel(Q4Args a) {
   typedef Elem<DTYPE> E;
+  const int out = blockIdx.x * 256 + threadIdx.x;
+  if (out >= a.o) return;
   const int64_t count = (int64_t)a.m * a.o;
-  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < count; i += (int64_t)gridDim.x * 256) {
+  const float bias = a.bias ? E::to_float(static_cast<const typename E::T*>(a.bias)[out]) : 0.f;
+  for (int row = blockIdx.y; row < a.m; row += gridDim.y) {
+    const int64_t i = (int64_t)row * a.o + out;
     float v = a.parts[i];
+#pragma unroll 4
     for (int s = 1; s < a.splits; ++s) v += a.parts[s * count + i];
-    if (a.bias) v += E::to_float(static_cast<const typename E::T*>(a.bias)[i % a.o]);
+    v += bias;
     if (a.relu) v = v > 0.f ? v : 0.f;
     static_cast<typename E::T*>(a.y)[i] = E::from_float(v);
   }
@@ -347,6 +409,11 @@ void launch_group(const q4_desc* d, const Q4Args& a, hipStream_t stream) {
   }
 }
 
+// Tiles of a workgroup for up to four rows and many outputs.  4096 x 128256: bf16 2 tiles 58.7 us, 4 65.7; fp32, whose operands are three
+// times as many loads, 95.4 and 67.6.
+template <int DTYPE>
+constexpr int kManyTiles = DTYPE == MI355_F32 ? 4 : 2;
+
 template <int DTYPE>
 int launch_forward(const q4_desc* d, const Q4Args& a, hipStream_t stream) {
   if (DTYPE == MI355_F32) {
@@ -357,14 +424,15 @@ int launch_forward(const q4_desc* d, const Q4Args& a, hipStream_t stream) {
     if (e) return e;
   }
   // Codes that the last-level cache (256 MB) does not hold from call to call go around it.
-  const bool stream_codes = codes_bytes(d) > (size_t)STREAM_MB << 20;
+  const bool stream_codes = codes_bytes(d) > (size_t)240 << 20;
   switch (m_tiles(d)) {
     case 1:
       if (d->p.m <= 4)
         d->nt == 1 ? launch_group<DTYPE, 1, 1, 1>(d, a, stream)
-                   : stream_codes ? launch_group<DTYPE, 1, 2, 1, true>(d, a, stream) : launch_group<DTYPE, 1, 2, 1>(d, a, stream);
+                   : stream_codes ? launch_group<DTYPE, 1, kManyTiles<DTYPE>, 1, true>(d, a, stream) : launch_group<DTYPE, 1, kManyTiles<DTYPE>, 1>(d, a, stream);
       else
-        stream_codes ? launch_group<DTYPE, 1, 2, 4, true>(d, a, stream) : launch_group<DTYPE, 1, 2, 4>(d, a, stream);
+        d->nt == 2 ? launch_group<DTYPE, 1, 2, 4>(d, a, stream)
+                   : stream_codes ? launch_group<DTYPE, 1, 4, 4, true>(d, a, stream) : launch_group<DTYPE, 1, 4, 4>(d, a, stream);
       break;
     case 2: launch_group<DTYPE, 2, 4, 4>(d, a, stream); break;
     case 3: launch_group<DTYPE, 3, 4, 4>(d, a, stream); break;
@@ -372,8 +440,7 @@ int launch_forward(const q4_desc* d, const Q4Args& a, hipStream_t stream) {
   }
   int e = (int)hipGetLastError();
   if (e || d->splits == 1) return e;
-  const int64_t count = (int64_t)d->p.m * d->p.num_output;
-  hipLaunchKernelGGL(q4_join_kernel<DTYPE>, dim3((uint32_t)std::min<int64_t>((count + 255) / 256, 4096)), dim3(256), 0, stream, a);
+  hipLaunchKernelGGL(q4_join_kernel<DTYPE>, dim3((d->p.num_output + 255) / 256, std::min(d->p.m, 65535)), dim3(256), 0, stream, a);
   return (int)hipGetLastError();
 }
 
@@ -400,9 +467,11 @@ int q4_desc_create(q4_desc_t** out, const q4_params_t* pp) {
   d->tiles = (p.num_output + kTile - 1) / kTile;
   d->blocks = (p.k + kBlockK - 1) / kBlockK;
   const int mt = m_tiles(d);
-  // Tiles of a workgroup: a load of x serves them all, but where there is less than a wave for each of a compute unit's places they are
-  // workgroups of their own.  Up to four rows, 4096 x 4096: 1 tile 5.1 us, 2 tiles 7.0; 4096 x 128256: 74.4 and 62.3.
-  d->nt = mt > 1 ? 4 : p.m > 4 ? 2 : d->tiles < 8 * kUnits ? 1 : 2;
+  // Tiles of a workgroup: a load of x serves them all, but where there are few of them they are workgroups of their own.  One row,
+  // 4096 x 4096 (256 tiles): 1 tile 5.1 us, 2 tiles 7.0; 4096 x 128256 (8016): 74.4 and 62.3.  16 rows, 4096 x 20000 (1250): 2 tiles 16.7 us,
+  // 4 16.2; 4096 x 30000: 23.2 and 19.1; 4096 x 128256: 103 and 64.
+  const int many = p.dtype == MI355_F32 ? kManyTiles<MI355_F32> : kManyTiles<MI355_BF16>;
+  d->nt = mt > 1 ? 4 : p.m > 4 ? (d->tiles < 4 * kUnits ? 2 : 4) : d->tiles < 8 * kUnits ? 1 : many;
   const int groups = (d->tiles + d->nt - 1) / d->nt;
   // Waves: as many as there may be where a compute unit has one workgroup, four where it has several (8 rows, 4096 x 100000: 4 waves
   // 58 us, 8 waves 64; 16 rows, 4096 x 4096: 4 waves 12.9, 8 8.9, 16 8.1); at least two blocks for each.
