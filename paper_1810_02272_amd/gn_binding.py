@@ -8,7 +8,7 @@ from dataclasses import dataclass
 import torch
 
 from . import binding as _b
-from .lp_binding import _dtype
+from .lp_binding import DTYPES
 
 _ready = False
 
@@ -20,7 +20,7 @@ class GnParams:
     dtypes: tuple
 
     def __post_init__(self):
-        object.__setattr__(self, "counts", tuple(int(n) for n in self.counts))
+        object.__setattr__(self, "counts", tuple(map(int, self.counts)))
         object.__setattr__(self, "dtypes", tuple(self.dtypes))
         if len(self.counts) != len(self.dtypes):
             raise ValueError("one type for each count")
@@ -64,7 +64,9 @@ class GnDesc:
 
 def gn_desc_create(params: GnParams) -> GnDesc:
     n = len(params.counts)
-    codes = [_dtype(t, (0, 1, 2, 3)) for t in params.dtypes]
+    codes = list(map(DTYPES.get, params.dtypes))
+    if None in codes:
+        raise TypeError(f"dtypes: {params.dtypes[codes.index(None)]} is not among those of this operator")
     c = _CParams(n, (ctypes.c_int64 * n)(*params.counts), (ctypes.c_int32 * n)(*codes))
     out = ctypes.c_void_p()
     _b._check(_load().gn_desc_create(ctypes.byref(out), ctypes.byref(c)), "gn_desc_create")
