@@ -706,7 +706,7 @@ int launch_row(const lp_desc* d, const LpArgs& a, hipStream_t stream) {
   else if (d->form == kBlock)
     launch_team<DTYPE, 256, kBlockVecs, MODE, ENT, STREAM>(a, a.rows, 256, stream);
   else if (d->form == kSolo)
-    launch_team<DTYPE, 1024, kSoloVecs, MODE, ENT, false>(a, a.rows, 1024, stream);
+    launch_team<DTYPE, 1024, kSoloVecs, MODE, ENT, false>(a, a.rows, 1024, stream);  // (at most 32 MB)
   else
     launch_team<DTYPE, 512, kLongVecs, MODE, ENT, STREAM>(a, a.rows, 512, stream);
   return (int)hipGetLastError();
@@ -727,7 +727,7 @@ int launch_grad(const LpArgs& a, hipStream_t stream) {
 }
 
 // Whether the logits, or they and the gradient, are more than the last-level cache (256 MB) holds: they then go around it, and leave it to
-// what is read a second time.  Training on 4096 x 128256: 455 us through it, 442 with the gradient around it, STREAMED with both.
+// what is read a second time.  Training on 4096 x 128256: 455 us through it, 442 with the gradient around it, 419 with both.
 bool streams(const lp_desc* d, int blobs) { return (double)d->p.rows * d->p.vocab * dtype_bytes(d->p.dtype) * blobs > (double)(256 << 20); }
 
 // One of the descriptor's six kinds.
@@ -823,10 +823,13 @@ int lp_desc_create(lp_desc_t** out, const lp_params_t* pp) {
   }
   if (d->splits > 1) d->ws_bytes = (size_t)p.rows * d->splits * (16 + 8 * (size_t)p.top);
   const char* const form = kFormNames[d->form];
+  auto around = [&](int blobs) { return d->form != kSolo && streams(d, blobs) ? ",stream" : ""; };
   if (d->splits > 1)
-    snprintf(d->names, sizeof(d->names), "forward=lp_parts(S=%d)+join;backward=lp_grad;forward_backward=lp_parts(S=%d)+grad", d->splits, d->splits);
+    snprintf(d->names, sizeof(d->names), "forward=lp_parts(S=%d)+join;backward=lp_grad%s;forward_backward=lp_parts(S=%d)+grad", d->splits,
+             streams(d, 2) ? "[stream]" : "", d->splits);
   else
-    snprintf(d->names, sizeof(d->names), "forward=lp_row[%s];backward=lp_grad;forward_backward=lp_row[%s]", form, form);
+    snprintf(d->names, sizeof(d->names), "forward=lp_row[%s%s];backward=lp_grad%s;forward_backward=lp_row[%s%s]", form, around(1), streams(d, 2) ? "[stream]" : "",
+             form, around(2));
   *out = d;
   return CONV_OK;
 }

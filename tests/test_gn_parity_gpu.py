@@ -54,6 +54,7 @@ def check(norm, outs, grads, limit):
 ONE = ([1], [F32])
 MIXED = ([5, 0, 1, 4097, 3, 65537, 16, 8, 70000], [F32, BF16, BF16, F16, F64, BF16, F32, F32, F64])
 MANY = ([(i * 37) % 301 for i in range(400)], [(F32, F16, BF16, F64)[i * i % 4] for i in range(400)])
+HUGE = ([70000001, 3, 40000000], [BF16, F32, F32])  # more than the last-level cache holds
 LARGE = ([3000001, 17, 5000000, 2000003], [BF16, BF16, F32, BF16])
 
 
@@ -82,6 +83,12 @@ def test_parity(counts, dtypes, apart, first, ratio):
     check(norm, grads, before, limit)
     rest_untouched(grads, grad_buffers)
     assert all(torch.equal(a, b) for a, b in zip(grads, outs))
+
+
+@pytest.mark.parametrize("first", [0, 1])
+@pytest.mark.parametrize("ratio", [0.3, 7.0])
+def test_more_than_the_cache_holds(first, ratio):
+    test_parity(*HUGE, 0, first, ratio)
 
 
 def run(grads, limit):

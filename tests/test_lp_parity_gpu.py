@@ -41,6 +41,7 @@ CASES = [
     (11, 5000, BF16, 64, 1, 1.0, 8, 0),
     (270, 8190, F32, 10, 1, 1.0, 2, 2),
     (260, 16384, BF16, 20, 1, 1.0, 0, 0),
+    (300, 9001, F16, 20, 1, 1.0, 0, 3),
     (257, 16387, F16, 20, 0, 1.0, 0, 5),
     (256, 32768, F32, 3, 1, 1.0, 0, 0),
     (260, 50257, BF16, 20, 1, 1.25, 47, 0),
@@ -59,6 +60,9 @@ CASES = [
     (128, 33000, F16, 20, 1, 1.0, 0, 0),
     (20, 16385, F32, 20, 1, 1.0, 0, 0),
     (1, 1000000, F16, 20, 1, 1.0, 0, 0),
+    (70001, 2000, BF16, 3, 1, 1.0, 0, 0),    # more than the last-level cache holds
+    (20001, 8001, BF16, 3, 1, 1.0, 0, 0),
+    (1100, 128256, BF16, 20, 1, 1.0, 0, 0),
 ]
 IDS = ["%dx%d-%s-t%d-e%d-s%g-g%d-o%d" % (c[0], c[1], str(c[2])[6:], *c[3:]) for c in CASES]
 

@@ -29,6 +29,41 @@ def test_every_declared_symbol_is_exported_and_bound(prefix, names):
         assert hasattr(c, name) and hasattr(lib, name), name
 
 
+# ---- every variant is run by some GPU parity case ----
+
+def test_lp_variants_have_parity_cases():
+    import test_lp_parity_gpu as t
+    seen = set()
+    for rows, vocab, dtype, top, entropy, scale, _, _ in t.CASES:
+        for v in lib.lp_desc_kernel_names(lib.lp_desc_create(lib.LpParams(rows, vocab, dtype, top, entropy, scale))).split(";"):
+            seen.add((re.sub(r"S=\d+", "S", v), dtype))
+    for dtype in (F32, F16, BF16):
+        for form in ("wave", "block", "solo", "long"):
+            for which in ("forward", "forward_backward"):
+                assert (f"{which}=lp_row[{form}]", dtype) in seen
+        assert ("forward=lp_parts(S)+join", dtype) in seen and ("forward_backward=lp_parts(S)+grad", dtype) in seen
+        assert ("backward=lp_grad", dtype) in seen
+    for form in ("wave", "block", "long"):  # one type: the others' differ in the conversions alone
+        assert (f"forward=lp_row[{form},stream]", BF16) in seen and (f"forward_backward=lp_row[{form},stream]", BF16) in seen
+    assert ("backward=lp_grad[stream]", BF16) in seen
+
+
+def test_q4_variants_have_parity_cases():
+    import test_q4_parity_gpu as t
+    seen = set()
+    for m, k, o, dtype, group, bias, relu in t.CASES:
+        name = lib.q4_desc_kernel_names(lib.q4_desc_create(lib.Q4Params(m, k, o, dtype, group, bias, relu)))
+        shape, splits = re.fullmatch(r"fwd=(?:terms\+)?q4\[(.*)\]\(S=(\d+),W=\d+\)", name).groups()
+        seen.add((shape, int(splits) > 1, dtype is F32))
+    for wide in (False, True):
+        for shape in ("m16,n16,r1", "m16,n64,r1" if wide else "m16,n32,r1", "m16,n32", "m16,n64", "m32,n64", "m48,n64", "m64,n64"):
+            assert (shape, False, wide) in seen, (shape, wide)
+        assert any(s and f is wide for _, s, f in seen)
+    for shape in ("m16,n32,r1,stream", "m16,n64,stream"):
+        assert (shape, False, False) in seen
+    assert ("m16,n64,r1,stream", False, True) in seen
+
+
 # ---- log probabilities ----
 
 @pytest.mark.parametrize("bad,status", [(dict(rows=-1), EINVAL), (dict(vocab=0), EINVAL), (dict(top=-1), EINVAL), (dict(top=65), EINVAL),
