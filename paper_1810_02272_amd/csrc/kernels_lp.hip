@@ -436,7 +436,7 @@ enum Mode { kScore, kTrain, kPart };
 // whatever needs it again.  THREADS 64: a wave for each row, several in a workgroup.
 // STREAM: what is read and written once goes around the last-level cache.
 template <int DTYPE, int THREADS, int NV, Mode MODE, bool ENT, bool STREAM>
-__global__ __launch_bounds__(THREADS == 64 ? 256 : THREADS, THREADS == 64 ? 1 : 4) void lp_row_kernel(LpArgs a) {
+__global__ __launch_bounds__(THREADS == 64 ? 256 : THREADS, THREADS == 64 ? 1 : NV > 20 ? 3 : 4) void lp_row_kernel(LpArgs a) {
   typedef Elem<DTYPE> E;
   typedef typename E::T T;
   constexpr int VEC = E::VEC, WAVES = THREADS / 64;
@@ -681,13 +681,24 @@ __global__ __launch_bounds__(256) void lp_grad_kernel(LpArgs a, int chunks) {
   }
 }
 
-// The team of a whole row.  A wave: no barriers.  Beyond its registers, a workgroup of 256, or of 1024 where there is at most one row for a
-// compute unit, and from its registers on one of 512: two of them share a compute unit, and while one loads the other computes.
-// What 512 threads cannot hold (81920 logits of 16 bits) is read again from the caches.
-enum Form { kWave, kBlock, kSolo, kLong };
-const char* const kFormNames[] = {"wave", "block", "solo", "long"};
+// The team of a whole row: the smallest whose registers hold it, as several share a compute unit and one loads while another computes,
+// and as a wave needs no barriers.  us, this team and the next larger one (rows x vocab):
+//   wave4    8000 x 2000 bf16, 20 alternatives 17.4, 256 threads 33.3; training 17.8, 27.1
+//   wave8    8000 x 3900 bf16, 20 alternatives 25.4, block8 40.1; training on 8000 x 3000 28.2, 37.6
+//   block8   3000 x 12000 bf16, 20 alternatives 27.4, block16 32.0; 512 threads 47
+//   block16  1000 x 30000 bf16, 20 alternatives 23.5, 512 threads 25.1; training on 3000 x 30000 73.2, 77.7
+//   block26  8000 x 50257 f16 163, 512 threads 185; training on 2000 x 50257 90.0, 93.9
+//   long     training on 4096 x 128256 bf16: 512 threads 453, 1024 with 20 vectors 485, with 7 (most of a row read again) 470
+// Where there is at most one row for a compute unit, 1024 threads: 1 x 32000 8.7 us, in parts 11.0; 200 x 30000 trained 9.8, in parts 15.
+// What the long team cannot hold (81920 logits of 16 bits) is read again from the caches.
+enum Form { kWave4, kWave8, kSolo, kBlock8, kBlock16, kBlock26, kLong };
+const char* const kFormNames[] = {"wave4", "wave8", "solo", "block8", "block16", "block26", "long"};
 
-constexpr int kWaveVecs = 4, kBlockVecs = 8, kSoloVecs = 4, kLongVecs = 20;
+constexpr int kSoloVecs = 4, kLongVecs = 20;
+
+// Whether three block26 teams on a compute unit finish before two long ones: they take 7/8 of the time for a row where all places are taken,
+// but a last round that is not full costs more.  777 x 50257: block26 32.4 us, long 30.7; 300 rows 20.6, 19.9; 2000 rows trained 90.0, 93.9.
+bool dense(int64_t rows) { return (rows + 767) / 768 * 21 <= (rows + 511) / 512 * 16; }
 constexpr int kUnits = 256;  // compute units
 constexpr int kMostTeams = 1 << 20;
 
@@ -701,10 +712,16 @@ int launch_row(const lp_desc* d, const LpArgs& a, hipStream_t stream) {
   const int waves = a.rows >= 2048 ? 4 : 1;
   if (MODE == kPart)
     launch_team<DTYPE, 1024, kSoloVecs, kPart, ENT, false>(a, a.rows * a.splits, 1024, stream);
-  else if (d->form == kWave)
-    launch_team<DTYPE, 64, kWaveVecs, MODE, ENT, STREAM>(a, (int)(((int64_t)a.rows + waves - 1) / waves), 64 * waves, stream);
-  else if (d->form == kBlock)
-    launch_team<DTYPE, 256, kBlockVecs, MODE, ENT, STREAM>(a, a.rows, 256, stream);
+  else if (d->form == kWave4)
+    launch_team<DTYPE, 64, 4, MODE, ENT, STREAM>(a, (int)(((int64_t)a.rows + waves - 1) / waves), 64 * waves, stream);
+  else if (d->form == kWave8)
+    launch_team<DTYPE, 64, 8, MODE, ENT, STREAM>(a, (int)(((int64_t)a.rows + waves - 1) / waves), 64 * waves, stream);
+  else if (d->form == kBlock8)
+    launch_team<DTYPE, 256, 8, MODE, ENT, STREAM>(a, a.rows, 256, stream);
+  else if (d->form == kBlock16)
+    launch_team<DTYPE, 256, 16, MODE, ENT, STREAM>(a, a.rows, 256, stream);
+  else if (d->form == kBlock26)
+    launch_team<DTYPE, 256, 26, MODE, ENT, STREAM>(a, a.rows, 256, stream);
   else if (d->form == kSolo)
     launch_team<DTYPE, 1024, kSoloVecs, MODE, ENT, false>(a, a.rows, 1024, stream);  // (at most 32 MB)
   else
@@ -809,13 +826,17 @@ int lp_desc_create(lp_desc_t** out, const lp_params_t* pp) {
   d->c = (float)(p.scale * 1.44269504088896340736);
   const int vec = 16 / dtype_bytes(p.dtype);
   const int solo = 1024 * vec * kSoloVecs;
-  d->form = p.vocab <= 64 * vec * kWaveVecs                 ? kWave
-            : p.rows <= kUnits && p.vocab <= solo           ? kSolo
-            : p.vocab <= 256 * vec * kBlockVecs             ? kBlock
-                                                            : kLong;
+  d->form = p.vocab <= 64 * vec * 4                   ? kWave4
+            : p.rows <= kUnits && p.vocab <= solo     ? kSolo
+            : p.vocab <= 64 * vec * 8                 ? kWave8
+            : p.vocab <= 256 * vec * 8                ? kBlock8
+            : p.vocab <= 256 * vec * 16               ? kBlock16
+            : p.vocab <= 256 * vec * 26 && dense(p.rows) ? kBlock26
+                                                      : kLong;
   d->splits = 1;
   d->seg = p.vocab;
-  // Where a compute unit holds no whole row in one pass and two of them or more are left for each, rows are taken in parts.
+  // Where a workgroup of 1024 cannot hold a row and there are two compute units or more for each, rows are taken in parts: 64 x 128256
+  // with 20 alternatives 14.4 us, whole rows 24.2; 8 x 128256 12.0, 23.2; 200 x 50257, one part, 15.0, and 14.7 in two.
   if (p.rows > 0 && 2 * p.rows <= kUnits && p.vocab > solo) {
     const int splits = std::min(std::min(kUnits / p.rows, (p.vocab + solo / 4 - 1) / (solo / 4)), kMaxSplits);
     d->seg = ((p.vocab + splits - 1) / splits + vec - 1) / vec * vec;

@@ -42,6 +42,14 @@ CASES = [
     (270, 8190, F32, 10, 1, 1.0, 2, 2),
     (260, 16384, BF16, 20, 1, 1.0, 0, 0),
     (300, 9001, F16, 20, 1, 1.0, 0, 3),
+    (300, 2050, BF16, 20, 1, 1.0, 0, 0),
+    (2049, 4096, F16, 20, 1, 1.0, 1, 1),
+    (300, 1999, F32, 20, 1, 1.0, 0, 0),
+    (300, 32768, BF16, 20, 1, 1.0, 0, 0),
+    (300, 9000, F32, 20, 1, 1.0, 0, 2),
+    (600, 40001, F16, 20, 1, 1.0, 0, 0),
+    (600, 26624, F32, 64, 1, 1.0, 0, 0),
+    (300, 90003, F16, 64, 1, 1.0, 0, 1),
     (257, 16387, F16, 20, 0, 1.0, 0, 5),
     (256, 32768, F32, 3, 1, 1.0, 0, 0),
     (260, 50257, BF16, 20, 1, 1.25, 47, 0),
@@ -62,6 +70,9 @@ CASES = [
     (1, 1000000, F16, 20, 1, 1.0, 0, 0),
     (70001, 2000, BF16, 3, 1, 1.0, 0, 0),    # more than the last-level cache holds
     (20001, 8001, BF16, 3, 1, 1.0, 0, 0),
+    (40001, 3999, BF16, 3, 1, 1.0, 0, 0),
+    (6001, 30001, BF16, 3, 1, 1.0, 0, 0),
+    (3001, 50257, BF16, 3, 1, 1.0, 0, 0),
     (1100, 128256, BF16, 20, 1, 1.0, 0, 0),
 ]
 IDS = ["%dx%d-%s-t%d-e%d-s%g-g%d-o%d" % (c[0], c[1], str(c[2])[6:], *c[3:]) for c in CASES]
@@ -191,7 +202,8 @@ def test_parity(case):
     assert torch.equal(x, g) and untouched(x, x_buffer)
 
 
-@pytest.mark.parametrize("rows,vocab,dtype", [(6, 300, BF16), (6, 9000, F32), (6, 3000, F16), (260, 17000, BF16), (256, 100000, F32)])
+@pytest.mark.parametrize("rows,vocab,dtype", [(6, 300, BF16), (6, 9000, F32), (6, 3000, F16), (260, 17000, BF16), (256, 100000, F32), (300, 3000, F16),
+                                              (300, 8000, BF16), (600, 40000, BF16), (6, 70000, BF16)])
 def test_not_a_number_and_infinity_reach_the_whole_row_and_no_other(rows, vocab, dtype):
     x = torch.randn((rows, vocab), device=DEV).to(dtype)
     x[1, vocab // 3] = math.nan

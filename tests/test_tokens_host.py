@@ -38,12 +38,12 @@ def test_lp_variants_have_parity_cases():
         for v in lib.lp_desc_kernel_names(lib.lp_desc_create(lib.LpParams(rows, vocab, dtype, top, entropy, scale))).split(";"):
             seen.add((re.sub(r"S=\d+", "S", v), dtype))
     for dtype in (F32, F16, BF16):
-        for form in ("wave", "block", "solo", "long"):
+        for form in ("wave4", "wave8", "solo", "block8", "block16", "block26", "long"):
             for which in ("forward", "forward_backward"):
                 assert (f"{which}=lp_row[{form}]", dtype) in seen
         assert ("forward=lp_parts(S)+join", dtype) in seen and ("forward_backward=lp_parts(S)+grad", dtype) in seen
         assert ("backward=lp_grad", dtype) in seen
-    for form in ("wave", "block", "long"):  # one type: the others' differ in the conversions alone
+    for form in ("wave4", "wave8", "block8", "block16", "block26", "long"):  # one type: the others' differ in the conversions alone
         assert (f"forward=lp_row[{form},stream]", BF16) in seen and (f"forward_backward=lp_row[{form},stream]", BF16) in seen
     assert ("backward=lp_grad[stream]", BF16) in seen
 
