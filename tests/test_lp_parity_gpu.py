@@ -52,7 +52,7 @@ CASES = [
     (300, 90003, F16, 64, 1, 1.0, 0, 1),
     (257, 16387, F16, 20, 0, 1.0, 0, 5),
     (256, 32768, F32, 3, 1, 1.0, 0, 0),
-    (260, 50257, BF16, 20, 1, 1.25, 47, 0),
+    (520, 50257, BF16, 20, 1, 1.25, 47, 0),
     (256, 65539, F16, 32, 1, 1.0, 0, 0),
     (256, 90001, F32, 20, 1, 1.0, 0, 0),     # beyond a workgroup's registers
     (256, 128256, BF16, 20, 1, 1.0, 0, 0),
