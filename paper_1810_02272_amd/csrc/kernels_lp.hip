@@ -57,7 +57,7 @@ struct LpArgs {
 struct RowStat {
   float M, c;      // t = c x - M
   float log2s, H;  // log2 s, entropy in nats
-  float step;      // nats per unit of t: ln 2, but for the rows of beyond()
+  float step;      // nats per unit of t
 };
 
 __device__ __forceinline__ float exp2_fast(float t) { return __builtin_amdgcn_exp2f(t); }  // 0 below 2^-126
@@ -65,11 +65,17 @@ __device__ __forceinline__ float exp2_fast(float t) { return __builtin_amdgcn_ex
 // t for a product with 2^t, which is 0 where this cuts off: -inf must not meet a 0.
 __device__ __forceinline__ float finite(float t) { return fmaxf(t, -200.f); }
 
-__device__ __forceinline__ float reference(float m, float c) { return fminf(fmaxf(m * c, -FLT_MAX), FLT_MAX); }
+// M is c x of a maximum, rounded to fp32: t there is the rounding, at most 32 up to 2^30.  Maxima below that range (large finite masks
+// throughout) take its end for M, and leave sums of 0; beyond() takes care of those that are a row's.
+constexpr float kMostReference = 0x1p30f;
 
-// Whether c x leaves fp32 at the row's maximum: a row of nothing but a type's lowest value, or values beyond 2e38.  Neighbouring
-// values are so far apart there that p is shared by those equal to the maximum: t = x - m serves as well, whatever the scale.
-__device__ __forceinline__ bool beyond(float m, float c) { return !(fabsf(m * c) <= FLT_MAX) && m != -INFINITY; }
+__device__ __forceinline__ float reference(float m, float c) { return fminf(fmaxf(m * c, -kMostReference), kMostReference); }
+
+// Whether a row's maximum is beyond that range.  Different values are then so far apart (2^-24 of c m, 64, at least) that p is shared by
+// those equal to the maximum, and t may be P (x - m) with a power of two P for c: P m is exact, and so is the difference.
+__device__ __forceinline__ bool beyond(float m, float c) { return !(fabsf(m * c) <= kMostReference) && m != -INFINITY; }
+
+__device__ __forceinline__ float power_for(float m, float c) { return ldexpf(1.f, min(ilogbf(c) + 1, 126 - ilogbf(m))); }
 
 struct Sums {
   float m, s, s2;
@@ -86,9 +92,9 @@ __device__ __forceinline__ void add_part(Sums& a, float M, bool over, float c, f
 __device__ __forceinline__ RowStat finish(const Sums& a, float c, float scale) {
   RowStat r;
   const bool over = beyond(a.m, c);
-  r.c = over ? 1.f : c;
-  r.step = over ? scale : kLn2;
-  r.M = over ? a.m : a.m == -INFINITY ? 0.f : a.m * c;
+  r.c = over ? power_for(a.m, c) : c;
+  r.step = over ? scale / r.c : kLn2;
+  r.M = a.m == -INFINITY ? 0.f : a.m * r.c;
   if (a.m == -INFINITY && a.s == 0.f) {  // nothing but -inf
     r.log2s = INFINITY;
     r.H = 0.f;
@@ -102,8 +108,12 @@ __device__ __forceinline__ RowStat finish(const Sums& a, float c, float scale) {
 // The natural logarithm of the probability of a logit.
 __device__ __forceinline__ float log_prob(const RowStat& r, float x, float scale) {
   const float t = fmaf(x, r.c, -r.M);
-  if (t == -INFINITY && x != -INFINITY && r.step == kLn2) return x * scale - r.M * kLn2;  // c x is out of range, scale x may not be
+  if (t == -INFINITY && x != -INFINITY) return x * scale - r.M / r.c * scale;  // c x is out of range, scale x may not be
   return fmaf(r.step, t, -kLn2 * r.log2s);
+}
+
+__device__ __forceinline__ void put_stats(float* to, const RowStat& r) {
+  store_vec<Elem<MI355_F32>>(to, Elem<MI355_F32>::pack({r.M, r.log2s, r.H, r.c}));
 }
 
 struct GradScale {
@@ -492,12 +502,13 @@ __global__ __launch_bounds__(THREADS == 64 ? 256 : THREADS, THREADS == 64 ? 1 : 
       sum = wave_merge(p.x, p.y, p.z, a.c);
       at_token = lds.at_token;
     }
-    if (beyond(sum.m, a.c)) {  // rare: the same sums of t = x - m
+    if (beyond(sum.m, a.c)) {  // rare: the sums again, with that row's t
+      const float P = power_for(sum.m, a.c), M = sum.m * P;
       float count = 0.f;
       for (int v = tid; v < nv; v += THREADS) {
         const u32x4 vec = row_vec<E>(row, v, n);
 #pragma unroll
-        for (int i = 0; i < VEC; ++i) count += exp2_fast(E::get(vec, i) - sum.m);
+        for (int i = 0; i < VEC; ++i) count += exp2_fast(fmaf(E::get(vec, i), P, -M));
       }
       count = wave_sum(count);
       if constexpr (WAVES > 1) {
@@ -521,7 +532,7 @@ __global__ __launch_bounds__(THREADS == 64 ? 256 : THREADS, THREADS == 64 ? 1 : 
       if (tid == 0) {
         if (a.logp) a.logp[r_] = token >= 0 ? log_prob(st, at_token, a.scale) : 0.f;
         if (ENT && a.entropy) a.entropy[r_] = st.H;
-        if (MODE == kScore && a.stats) reinterpret_cast<float4*>(a.stats)[r_] = make_float4(st.M, st.log2s, st.H, st.c);
+        if (MODE == kScore && a.stats) put_stats(a.stats + 4 * (int64_t)r_, st);
       }
       if constexpr (MODE == kScore) {
         if (a.top) {
@@ -598,7 +609,7 @@ __global__ __launch_bounds__(256) void lp_join_kernel(LpArgs a) {
   if (threadIdx.x == 0) {
     if (a.logp) a.logp[row] = token >= 0 ? log_prob(st, at_token, a.scale) : 0.f;
     if (ENT && a.entropy) a.entropy[row] = st.H;
-    if (a.stats) reinterpret_cast<float4*>(a.stats)[row] = make_float4(st.M, st.log2s, st.H, st.c);
+    if (a.stats) put_stats(a.stats + 4 * (int64_t)row, st);
   }
   if (total == 0) return;
   const uint32_t bound = top_bound(sample, a.top);
@@ -649,8 +660,8 @@ __global__ __launch_bounds__(256) void lp_grad_kernel(LpArgs a, int chunks) {
     if constexpr (PARTS) {
       st = finish(merge_parts(a.parts + (int64_t)r_ * a.splits, a.splits, threadIdx.x & 63, a.c), a.c, a.scale);
     } else {
-      const float4 q = reinterpret_cast<const float4*>(a.stats)[r_];
-      st = RowStat{q.x, q.w, q.y, q.z, 0.f};
+      const float* const q = a.stats + 4 * (int64_t)r_;
+      st = RowStat{q[0], q[3], q[1], q[2], 0.f};
     }
     const float w = token >= 0 ? a.d_logp[r_] : 0.f, u = ENT && a.d_entropy ? a.d_entropy[r_] : 0.f;
     const GradScale g = grad_scale(st, w, u, a.scale);

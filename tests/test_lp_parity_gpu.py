@@ -202,6 +202,57 @@ def test_parity(case):
     assert torch.equal(x, g) and untouched(x, x_buffer)
 
 
+@pytest.mark.parametrize("scale", [1.0, 1.5, 0.37, 2.0 ** 20])
+@pytest.mark.parametrize("vocab", [500, 3000, 9001, 40000, 70001])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_large_finite_logits(dtype, vocab, scale):
+    """Masks of -1e9 and on, throughout a row, in a run that some threads see nothing but, and next to each other; large positive
+    logits; differences of one step of the type at either end of the range."""
+    rows = 24
+    x = torch.randn((rows, vocab), device=DEV) * 2
+    for r, mask in enumerate((-1e9, -1e10, -3e15, -1e20, -1e30, -3e38)):
+        x[r] = mask                                  # throughout
+        x[6 + r] = mask
+        x[6 + r, -3:] = torch.tensor([1.0, 2.0, 0.5], device=DEV)  # all but three
+        x[12 + r, : vocab // 2] = mask               # half
+    x[18] = 1e9
+    x[18, 7] = 1.1e9
+    x[19, 3] = 3e38
+    x[20] = -1e30
+    x[20, : vocab // 3] = -1.01e30
+    x[21] *= 1e8
+    x[22] = -3e8
+    x = x.to(dtype)
+    x[23] = -1e25
+    x[23, 5] = torch.nextafter(x[23, 5].cpu(), torch.tensor(0.0, dtype=dtype)).to(DEV)
+    token = torch.randint(vocab, (rows,), device=DEV, dtype=torch.int32)
+    token[18], token[23] = 7, 5
+    w, u = torch.randn(rows, device=DEV), torch.randn(rows, device=DEV) * 0.1
+    want_logp, want_h = tokens.log_probs(x, scale)
+    case = (rows, vocab, dtype, 5, 1, scale, 0, 0)
+    for copies in (1, 30):  # 30: teams of rows that many
+        n = rows * copies
+        many = x.repeat(copies, 1)
+        d = lib.lp_desc_create(lib.LpParams(n, vocab, dtype, 5, 1, scale))
+        print(lib.lp_desc_kernel_names(d), flush=True)
+        ws = torch.empty(lib.lp_desc_workspace_bytes(d) // 4 + 1, device=DEV)
+        logp, h, stats = torch.empty(n, device=DEV), torch.empty(n, device=DEV), torch.empty((n, 4), device=DEV)
+        tl, tt = torch.empty((n, 5), device=DEV), torch.empty((n, 5), device=DEV, dtype=torch.int32)
+        lib.lp_forward(d, many, token.repeat(copies), logp, h, stats, tl, tt, ws)
+        g, g2, logp2, h2 = torch.empty_like(many), torch.empty_like(many), torch.empty_like(logp), torch.empty_like(h)
+        lib.lp_backward(d, many, token.repeat(copies), stats, w.repeat(copies), u.repeat(copies), g)
+        lib.lp_forward_backward(d, many, token.repeat(copies), w.repeat(copies), u.repeat(copies), logp2, h2, g2, ws)
+        for at in (slice(0, rows), slice(n - rows, n)):
+            check_rows(want_logp, want_h, logp[at], h[at], token, vocab)
+            check_rows(want_logp, want_h, logp2[at], h2[at], token, vocab)
+            index = tokens.top_tokens(x, 5)
+            assert torch.equal(tt[at].long(), index)
+            want = want_logp.gather(1, index)
+            within(tl[at], want, U * (256 + 4 * want.abs()), "top_logp")
+            check_gradient(case, x, token, w, u, g[at])
+            check_gradient(case, x, token, w, u, g2[at])
+
+
 @pytest.mark.parametrize("rows,vocab,dtype", [(6, 300, BF16), (6, 9000, F32), (6, 3000, F16), (260, 17000, BF16), (256, 100000, F32), (300, 3000, F16),
                                               (300, 8000, BF16), (600, 40000, BF16), (6, 70000, BF16)])
 def test_not_a_number_and_infinity_reach_the_whole_row_and_no_other(rows, vocab, dtype):
