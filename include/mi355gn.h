@@ -12,7 +12,8 @@
  *
  * Layouts: tensor i is counts[i] contiguous elements of dtypes[i] in DEVICE memory, on the element's own alignment; the arrays of
  * pointers are HOST memory and are read before the call returns.  outs[i] may be grads[i] itself (a factor of 1 then
- * leaves it untouched); otherwise outputs must not overlap inputs.  Tensors that follow each other in memory, as views of one flat
+ * leaves it untouched); otherwise outputs must not overlap inputs.  No tensor
+ * may share memory with another one of the list.  Tensors that follow each other in memory, as views of one flat
  * buffer do, are taken together; the result does not depend on it but for the order of the sums.
  *
  * The workspace is 16-byte aligned.  Ownership, execution and errors as in mi355conv.h.  Every call only enqueues kernels (two for up to 96 runs of tensors that

@@ -326,9 +326,26 @@ __device__ __forceinline__ uint32_t top_bound(uint32_t key, int top) {
   return bound;
 }
 
-// A wave ranks `count` different entries by counting those above each.
+// A wave ranks `count` different entries by counting those above each.  Of more than 64 (short rows, that no bound has been found for) it
+// first keeps those that pass a bound from 64 shares of them.
 template <class Out>
-__device__ __forceinline__ void rank_entries(const uint64_t* cand, int count, int top, int lane, Out&& out) {
+__device__ __forceinline__ void rank_entries(uint64_t* cand, int count, int top, int lane, Out&& out) {
+  if (count > 64) {
+    uint32_t most = 0;
+    for (int i = lane; i < count; i += 64) most = max(most, (uint32_t)(cand[i] >> 32));
+    const uint32_t bound = top_bound(most, top);
+    int kept = 0;
+    for (int i0 = 0; i0 < count; i0 += 64) {
+      const uint64_t mine = cand[min(i0 + lane, count - 1)];
+      const bool pass = i0 + lane < count && (uint32_t)(mine >> 32) >= bound;
+      const uint64_t mask = __ballot(pass);
+      wave_sync();
+      if (pass) cand[kept + __builtin_popcountll(mask & ((1ull << lane) - 1))] = mine;
+      wave_sync();
+      kept += (int)__builtin_popcountll(mask);
+    }
+    count = kept;
+  }
   if (count <= 64) {
     const uint64_t mine = lane < count ? cand[lane] : 0;
     int rank = 0;
@@ -359,8 +376,10 @@ __device__ __forceinline__ void team_top(TeamLds<THREADS>& lds, const u32x4 (&r)
   const float gm = group_most<GROUP>(m);
   if (tid % GROUP == 0) lds.group_top[tid / GROUP] = order_key(gm);
   if (tid == 0) lds.hits = 0;
+  if (tid == 0) lds.bound = -INFINITY;
   team_sync<THREADS>();
-  if (THREADS == 64 || tid < 64) {  // the leading 16 bits of the top-th greatest: a bound all the same
+  // (where all vectors may be put aside, a bound from them one by one is the better one, and comes with the ranking)
+  if (nv > kHits<THREADS> && (THREADS == 64 || tid < 64)) {  // the leading 16 bits of the top-th greatest: a bound all the same
     const uint32_t bound = top_bound(lds.group_top[lane], top);
     if (lane == 0) lds.bound = bound <= 0x007FFFFFu ? -INFINITY : key_value(bound);  // key of -inf and the unused ones below it
   }
@@ -450,8 +469,8 @@ __global__ __launch_bounds__(THREADS == 64 ? 256 : THREADS, THREADS == 64 ? 1 : 
   typedef Elem<DTYPE> E;
   typedef typename E::T T;
   constexpr int VEC = E::VEC, WAVES = THREADS / 64;
-  __shared__ TeamLds<THREADS> team_lds[THREADS == 64 ? 4 : 1];
-  TeamLds<THREADS>& lds = team_lds[THREADS == 64 ? threadIdx.x >> 6 : 0];
+  extern __shared__ u32x4 team_memory[];  // TeamLds for each team, but where a wave trains
+  TeamLds<THREADS>& lds = reinterpret_cast<TeamLds<THREADS>*>(team_memory)[THREADS == 64 ? threadIdx.x >> 6 : 0];
   const int lane = threadIdx.x & 63;
   const int teams = THREADS == 64 ? (int)(gridDim.x * (blockDim.x >> 6)) : (int)gridDim.x;
   int item = THREADS == 64 ? (int)(blockIdx.x * (blockDim.x >> 6) + (threadIdx.x >> 6)) : (int)blockIdx.x;
@@ -715,7 +734,8 @@ constexpr int kMostTeams = 1 << 20;
 
 template <int DTYPE, int THREADS, int NV, Mode MODE, bool ENT, bool STREAM>
 void launch_team(const LpArgs& a, int blocks, int threads, hipStream_t stream) {
-  hipLaunchKernelGGL((lp_row_kernel<DTYPE, THREADS, NV, MODE, ENT, STREAM>), dim3(std::min(blocks, kMostTeams)), dim3(threads), 0, stream, a);
+  const size_t lds = MODE == kTrain && THREADS == 64 ? 0 : sizeof(TeamLds<THREADS>) * (threads / THREADS);
+  hipLaunchKernelGGL((lp_row_kernel<DTYPE, THREADS, NV, MODE, ENT, STREAM>), dim3(std::min(blocks, kMostTeams)), dim3(threads), lds, stream, a);
 }
 
 template <int DTYPE, Mode MODE, bool ENT, bool STREAM>

@@ -26,6 +26,7 @@ struct q4_desc {
   q4_params_t p;
   int32_t tiles, blocks;  // of 16 outputs and 128 inputs
   int32_t nt, waves;      // tiles of a workgroup, its waves
+  int32_t prepared;       // fp32 x is laid out as operands before
   int32_t splits, per_split;  // workgroups that share the inputs of an output, blocks of each
   size_t ws_bytes;
   char names[96];
@@ -149,6 +150,29 @@ __device__ __forceinline__ void three_terms(float x, uint32_t (&t)[3]) {
   t[2] = __builtin_bit_cast(uint32_t, r2) >> 16;
 }
 
+// Eight consecutive values of x as operands.
+template <int DTYPE>
+__device__ __forceinline__ void load_operand(const typename Elem<DTYPE>::T* p, typename Operand<DTYPE>::V (&v)[Operand<DTYPE>::TERMS]) {
+  typedef Elem<DTYPE> E;
+  typedef typename Operand<DTYPE>::V V;
+  if constexpr (DTYPE == MI355_F32) {
+    const u32x4 h[2] = {load_vec<E>(p), load_vec<E>(p + 4)};
+    u32x4 w[3];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      uint32_t a[3], b[3];
+      three_terms(E::get(h[i >> 1], 2 * i & 3), a);
+      three_terms(E::get(h[i >> 1], (2 * i & 3) + 1), b);
+#pragma unroll
+      for (int t = 0; t < 3; ++t) w[t][i] = a[t] | b[t] << 16;
+    }
+#pragma unroll
+    for (int t = 0; t < 3; ++t) v[t] = __builtin_bit_cast(V, w[t]);
+  } else {
+    v[0] = __builtin_bit_cast(V, load_vec<E>(p));
+  }
+}
+
 // Row i of a tile of 16 rows of x is row row_place(i) of the instruction's left operand: its results then stand in register i / 4 of the
 // lanes 16 (i % 4) .. + 15, and up to four rows take one register.
 __device__ __forceinline__ int place_row(int place) { return (place & 3) * 4 + (place >> 2); }
@@ -175,17 +199,10 @@ __global__ __launch_bounds__(256) void x_terms_kernel(const float* __restrict__ 
 #pragma unroll
     for (int i = 0; i < 8; ++i) f[i] = row < m && at + i < k ? p[i] : 0.f;
   }
-  u32x4 w[3];
+  bf16x8 w[3];
+  load_operand<MI355_F32>(f, w);
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    uint32_t a[3], b[3];
-    three_terms(f[2 * i], a);
-    three_terms(f[2 * i + 1], b);
-#pragma unroll
-    for (int t = 0; t < 3; ++t) w[t][i] = a[t] | b[t] << 16;
-  }
-#pragma unroll
-  for (int t = 0; t < 3; ++t) to[(ts * 3 + t) * 64 + lane] = w[t];
+  for (int t = 0; t < 3; ++t) to[(ts * 3 + t) * 64 + lane] = __builtin_bit_cast(u32x4, w[t]);
 }
 
 template <int PER>
@@ -210,7 +227,8 @@ constexpr int kMostWaves = MT == 1 ? 16 : 8;
 // MT times 16 rows of x by NT tiles of 16 outputs in a workgroup; its waves take the blocks of inputs in turn, each on its own, and
 // add up through shared memory at the end: nothing of x is used by two waves.  REGS: result registers that hold rows.  STREAM: the codes
 // go around the last-level cache.
-template <int DTYPE, int MT, int NT, int REGS, int GROUP, bool STREAM>
+// PREPARED: x comes as operands (x_terms_kernel).
+template <int DTYPE, int MT, int NT, int REGS, int GROUP, bool STREAM, bool PREPARED>
 __global__ __launch_bounds__(kMostWaves<MT> * 64) void q4_kernel(Q4Args a) {
   typedef Operand<DTYPE> Op;
   typedef Elem<DTYPE> E;
@@ -229,7 +247,7 @@ __global__ __launch_bounds__(kMostWaves<MT> * 64) void q4_kernel(Q4Args a) {
       int from[MT];  // fp32: the lane whose operand is read, the tile's first row's where there is no row
 #pragma unroll
       for (int t = 0; t < MT; ++t) from[t] = m0 + 16 * t + place_row(lane & 15) < a.m ? lane : lane & 48;
-      if constexpr (TERMS == 1) {
+      if constexpr (!PREPARED) {
 #pragma unroll
         for (int t = 0; t < MT; ++t)  // (rows beyond m: the last one's values again, for results that nobody stores)
           rows[t] = static_cast<const typename E::T*>(a.x) + (int64_t)min(m0 + 16 * t + place_row(lane & 15), a.m - 1) * a.k + 8 * quarter;
@@ -249,20 +267,22 @@ __global__ __launch_bounds__(kMostWaves<MT> * 64) void q4_kernel(Q4Args a) {
       auto load_x = [&](int b, int d, V(&x)[MT][TERMS], auto guarded) {
 #pragma unroll
         for (int t = 0; t < MT; ++t) {
-          if constexpr (TERMS > 1) {
+          if constexpr (PREPARED) {
 #pragma unroll
             for (int i = 0; i < TERMS; ++i)
               x[t][i] = __builtin_bit_cast(V, a.terms[(((int64_t)(m0 / 16 + t) * a.blocks * 4 + b * 4 + d) * TERMS + i) * 64 + from[t]]);
           } else {
-            const int at = b * kBlockK + 32 * d;
-            if constexpr (decltype(guarded)::value) {
+            const int at = b * kBlockK + 32 * d, left = decltype(guarded)::value ? a.k - at - 8 * quarter : 8;
+            if (left >= 8) {
+              load_operand<DTYPE>(rows[t] + at, x[t]);
+            } else {
+              // (loads of the last input in the place of those beyond it: none waits for a branch)
               typename E::T f[8];
 #pragma unroll
-              for (int i = 0; i < 8; ++i) f[i] = at + 8 * quarter + i < a.k ? rows[t][at + i] : (typename E::T)0.f;
+              for (int i = 0; i < 8; ++i) f[i] = rows[t][min(at + i, a.k - 1 - 8 * quarter)];
 #pragma unroll
-              for (int i = 0; i < 8; ++i) x[t][0][i] = f[i];
-            } else {
-              x[t][0] = __builtin_bit_cast(V, load_vec<E>(rows[t] + at));
+              for (int i = 0; i < 8; ++i) f[i] = i < left ? f[i] : (typename E::T)0.f;
+              load_operand<DTYPE>(f, x[t]);
             }
           }
         }
@@ -291,7 +311,7 @@ __global__ __launch_bounds__(kMostWaves<MT> * 64) void q4_kernel(Q4Args a) {
       };
       u32x4 w[NT];
       float scale[NT][PER];
-      const int full = TERMS > 1 ? end : min(end, a.k / kBlockK);
+      const int full = PREPARED ? end : min(end, a.k / kBlockK);
       int b = begin + wave;
       if constexpr (MT == 2 || MT == 3) {
         // Two waves on a SIMD do not hide a load: operands are asked for two steps ahead, codes one block ahead.  (64 rows leave no
@@ -337,12 +357,12 @@ __global__ __launch_bounds__(kMostWaves<MT> * 64) void q4_kernel(Q4Args a) {
           }
         }
       }
-      if (TERMS == 1 && b < end) {
+      if (!PREPARED && b < end) {
         load_codes(b, w, scale);
 #pragma unroll
         for (int d = 0; d < 4; ++d) {
-          V x[MT][TERMS];
-          load_x(b, d, x, std::true_type());
+          V x[MT][TERMS] = {};
+          if (b * kBlockK + 32 * d < a.k) load_x(b, d, x, std::true_type());
           multiply(d, w, scale, x);
         }
       }
@@ -403,15 +423,15 @@ size_t terms_bytes(const q4_desc* d) {
 
 size_t codes_bytes(const q4_desc* d) { return (size_t)d->tiles * d->blocks * 1024; }
 
-template <int DTYPE, int MT, int NT, int REGS, bool STREAM = false>
+template <int DTYPE, int MT, int NT, int REGS, bool STREAM = false, bool PREPARED = DTYPE == MI355_F32>
 void launch_group(const q4_desc* d, const Q4Args& a, hipStream_t stream) {
   const int groups = (d->tiles + NT - 1) / NT;
   const dim3 grid(std::min(groups, 1 << 22), d->splits), block(64 * d->waves);
   const size_t lds = (size_t)d->waves * NT * REGS * 256;  // at most 64 KB
   switch (d->p.group) {
-    case 32: hipLaunchKernelGGL((q4_kernel<DTYPE, MT, NT, REGS, 32, STREAM>), grid, block, lds, stream, a); break;
-    case 64: hipLaunchKernelGGL((q4_kernel<DTYPE, MT, NT, REGS, 64, STREAM>), grid, block, lds, stream, a); break;
-    default: hipLaunchKernelGGL((q4_kernel<DTYPE, MT, NT, REGS, 128, STREAM>), grid, block, lds, stream, a);
+    case 32: hipLaunchKernelGGL((q4_kernel<DTYPE, MT, NT, REGS, 32, STREAM, PREPARED>), grid, block, lds, stream, a); break;
+    case 64: hipLaunchKernelGGL((q4_kernel<DTYPE, MT, NT, REGS, 64, STREAM, PREPARED>), grid, block, lds, stream, a); break;
+    default: hipLaunchKernelGGL((q4_kernel<DTYPE, MT, NT, REGS, 128, STREAM, PREPARED>), grid, block, lds, stream, a);
   }
 }
 
@@ -426,7 +446,7 @@ constexpr int kManyTiles = DTYPE == MI355_F32 ? 4 : 2;
 
 template <int DTYPE>
 int launch_forward(const q4_desc* d, const Q4Args& a, hipStream_t stream) {
-  if (DTYPE == MI355_F32) {
+  if (d->prepared) {
     const int64_t lanes = (int64_t)(terms_bytes(d) / 48);
     hipLaunchKernelGGL(x_terms_kernel, dim3((uint32_t)((lanes + 255) / 256)), dim3(256), 0, stream, static_cast<const float*>(a.x), a.terms, a.m, a.k,
                        d->blocks * 4, lanes);
@@ -437,10 +457,10 @@ int launch_forward(const q4_desc* d, const Q4Args& a, hipStream_t stream) {
   switch (m_tiles(d)) {
     case 1:
       if (d->p.m <= 4)
-        d->nt == 1 ? launch_group<DTYPE, 1, 1, 1>(d, a, stream)
+        d->nt == 1 ? d->prepared ? launch_group<DTYPE, 1, 1, 1>(d, a, stream) : launch_group<DTYPE, 1, 1, 1, false, false>(d, a, stream)
                    : stream_codes ? launch_group<DTYPE, 1, kManyTiles<DTYPE>, 1, true>(d, a, stream) : launch_group<DTYPE, 1, kManyTiles<DTYPE>, 1>(d, a, stream);
       else
-        d->nt == 2 ? launch_group<DTYPE, 1, 2, 4>(d, a, stream)
+        d->nt == 2 ? d->prepared ? launch_group<DTYPE, 1, 2, 4>(d, a, stream) : launch_group<DTYPE, 1, 2, 4, false, false>(d, a, stream)
                    : stream_codes ? launch_group<DTYPE, 1, 4, 4, true>(d, a, stream) : launch_group<DTYPE, 1, 4, 4>(d, a, stream);
       break;
     case 2: launch_group<DTYPE, 2, 4, 4>(d, a, stream); break;
@@ -493,11 +513,14 @@ int q4_desc_create(q4_desc_t** out, const q4_params_t* pp) {
     d->splits = (d->blocks + d->per_split - 1) / d->per_split;
   }
   d->waves = std::max(1, std::min(d->waves, (d->per_split + 1) / 2));
+  // fp32 x is cut into its terms once, by a launch of its own, but where little is cut: 4 x 76 -> 104 5.4 us, prepared 7.8; 5 x 2251 -> 45 9.0 and
+  // 8.7, 1 x 4096 -> 4096 12.3 and 10.5.
+  d->prepared = p.dtype == MI355_F32 && (mt > 1 || groups > kUnits || d->blocks > 8);
   if (p.m > 0) {
-    if (p.dtype == MI355_F32) d->ws_bytes += terms_bytes(d);
+    if (d->prepared) d->ws_bytes += terms_bytes(d);
     if (d->splits > 1) d->ws_bytes += (size_t)d->splits * p.m * p.num_output * 4;
   }
-  snprintf(d->names, sizeof(d->names), "fwd=%sq4[m%d,n%d%s%s](S=%d,W=%d)", p.dtype == MI355_F32 ? "terms+" : "", 16 * mt, 16 * d->nt, p.m <= 4 ? ",r1" : "", streams(d) && d->nt > 1 ? ",stream" : "", d->splits, d->waves);
+  snprintf(d->names, sizeof(d->names), "fwd=%sq4[m%d,n%d%s%s](S=%d,W=%d)", d->prepared ? "terms+" : "", 16 * mt, 16 * d->nt, p.m <= 4 ? ",r1" : "", streams(d) && d->nt > 1 ? ",stream" : "", d->splits, d->waves);
   *out = d;
   return CONV_OK;
 }
@@ -557,7 +580,7 @@ int q4_forward(const q4_desc_t* d, const void* x, const void* packed, const void
   a.per_split = d->per_split;
   char* const space = static_cast<char*>(ws);
   a.terms = reinterpret_cast<u32x4*>(space);
-  a.parts = reinterpret_cast<float*>(space + (d->p.dtype == MI355_F32 ? terms_bytes(d) : 0));
+  a.parts = reinterpret_cast<float*>(space + (d->prepared ? terms_bytes(d) : 0));
   const hipStream_t stream = (hipStream_t)hip_stream;
   const int e = d->p.dtype == MI355_F32   ? launch_forward<MI355_F32>(d, a, stream)
                 : d->p.dtype == MI355_F16 ? launch_forward<MI355_F16>(d, a, stream)

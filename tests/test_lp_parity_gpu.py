@@ -302,6 +302,26 @@ def test_gradient_against_differences():
     assert float((difference - g.double()).abs().max()) < 3e-3 * float(w.abs().max() + u.abs().max())
 
 
+def test_more_rows_than_teams():
+    rows, vocab = (1 << 22) + 77, 9  # four to a workgroup, 2^20 workgroups
+    x = torch.randn((rows, vocab), device=DEV).to(BF16)
+    token = torch.randint(vocab, (rows,), device=DEV, dtype=torch.int32)
+    w, u = torch.randn(rows, device=DEV), torch.randn(rows, device=DEV)
+    d = lib.lp_desc_create(lib.LpParams(rows, vocab, BF16, 2, 1))
+    logp, h, stats = torch.empty(rows, device=DEV), torch.empty(rows, device=DEV), torch.empty((rows, 4), device=DEV)
+    tl, tt = torch.empty((rows, 2), device=DEV), torch.empty((rows, 2), device=DEV, dtype=torch.int32)
+    lib.lp_forward(d, x, token, logp, h, stats, tl, tt)
+    check_rows(*tokens.log_probs(x), logp, h, token, vocab)
+    assert torch.equal(tt.long(), tokens.top_tokens(x, 2))
+    case = (rows, vocab, BF16, 2, 1, 1.0, 0, 0)
+    g = torch.empty_like(x)
+    lib.lp_backward(d, x, token, stats, w, u, g)
+    check_gradient(case, x, token, w, u, g)
+    g.fill_(math.nan)
+    lib.lp_forward_backward(d, x, token, w, u, logp, h, g)
+    check_gradient(case, x, token, w, u, g)
+
+
 def test_far_rows():
     """Rows whose offset passes 2^31 elements."""
     vocab, stride, rows = 500, (1 << 30) + 24, 3
