@@ -460,7 +460,8 @@ int launch_forward(const q4_desc* d, const Q4Args& a, hipStream_t stream) {
         d->nt == 1 ? d->prepared ? launch_group<DTYPE, 1, 1, 1>(d, a, stream) : launch_group<DTYPE, 1, 1, 1, false, false>(d, a, stream)
                    : stream_codes ? launch_group<DTYPE, 1, kManyTiles<DTYPE>, 1, true>(d, a, stream) : launch_group<DTYPE, 1, kManyTiles<DTYPE>, 1>(d, a, stream);
       else
-        d->nt == 2 ? d->prepared ? launch_group<DTYPE, 1, 2, 4>(d, a, stream) : launch_group<DTYPE, 1, 2, 4, false, false>(d, a, stream)
+        d->nt == 1 ? d->prepared ? launch_group<DTYPE, 1, 1, 4>(d, a, stream) : launch_group<DTYPE, 1, 1, 4, false, false>(d, a, stream)
+        : d->nt == 2 ? d->prepared ? launch_group<DTYPE, 1, 2, 4>(d, a, stream) : launch_group<DTYPE, 1, 2, 4, false, false>(d, a, stream)
                    : stream_codes ? launch_group<DTYPE, 1, 4, 4, true>(d, a, stream) : launch_group<DTYPE, 1, 4, 4>(d, a, stream);
       break;
     case 2: launch_group<DTYPE, 2, 4, 4>(d, a, stream); break;
@@ -499,11 +500,15 @@ int q4_desc_create(q4_desc_t** out, const q4_params_t* pp) {
   // Tiles of a workgroup: a load of x serves them all, but where there are few of them they are workgroups of their own.  One row,
   // 4096 x 4096 (256 tiles): 1 tile 5.1 us, 2 tiles 7.0; 4096 x 128256 (8016): 74.4 and 62.3.  16 rows, 4096 x 20000 (1250): 2 tiles 16.7 us,
   // 4 16.2; 4096 x 30000: 23.2 and 19.1; 4096 x 128256: 103 and 64.
-  const int many = p.dtype == MI355_F32 ? kManyTiles<MI355_F32> : kManyTiles<MI355_BF16>;
-  d->nt = mt > 1 ? 4 : p.m > 4 ? (d->tiles < 4 * kUnits ? 2 : 4) : d->tiles < 8 * kUnits ? 1 : many;
+  const bool wide = p.dtype == MI355_F32;  // (1 x 4096 -> 30000 fp32, 1875 tiles: 1 tile 35.5 us, 4 24.4)
+  d->nt = mt > 1                                       ? 4
+          : p.m > 4                                    ? (d->tiles <= kUnits ? 1 : d->tiles < 4 * kUnits ? 2 : 4)
+          : d->tiles < (wide ? 4 : 8) * kUnits         ? 1
+          : wide                                       ? kManyTiles<MI355_F32>
+                                                       : kManyTiles<MI355_BF16>;
   const int groups = (d->tiles + d->nt - 1) / d->nt;
   // Waves: as many as there may be where a compute unit has one workgroup, four where it has several (8 rows, 4096 x 100000: 4 waves
-  // 58 us, 8 waves 64; 16 rows, 4096 x 4096: 4 waves 12.9, 8 8.9, 16 8.1); at least two blocks for each.
+  // 58 us, 8 waves 64; 16 rows, 4096 x 4096: 4 waves 12.9, 8 8.9, 16 8.1); at least two blocks for each then.
   d->waves = groups > kUnits ? 4 : mt > 1 || p.m <= 4 ? 8 : 16;
   d->splits = 1;
   d->per_split = d->blocks;
@@ -512,10 +517,10 @@ int q4_desc_create(q4_desc_t** out, const q4_params_t* pp) {
     d->per_split = (d->blocks + splits - 1) / splits;
     d->splits = (d->blocks + d->per_split - 1) / d->per_split;
   }
-  d->waves = std::max(1, std::min(d->waves, (d->per_split + 1) / 2));
+  d->waves = std::max(1, std::min(d->waves, groups > kUnits ? (d->per_split + 1) / 2 : d->per_split));
   // fp32 x is cut into its terms once, by a launch of its own, but where little is cut: 4 x 76 -> 104 5.4 us, prepared 7.8; 5 x 2251 -> 45 9.0 and
   // 8.7, 1 x 4096 -> 4096 12.3 and 10.5.
-  d->prepared = p.dtype == MI355_F32 && (mt > 1 || groups > kUnits || d->blocks > 8);
+  d->prepared = p.dtype == MI355_F32 && (d->nt == 4 || groups > kUnits || d->blocks > 8);
   if (p.m > 0) {
     if (d->prepared) d->ws_bytes += terms_bytes(d);
     if (d->splits > 1) d->ws_bytes += (size_t)d->splits * p.m * p.num_output * 4;

@@ -21,7 +21,8 @@ CASES = [
     (1, 129, 31, BF16, 128, 0, 0), (4, 1000, 100, F16, 64, 1, 1), (1, 4096, 4096, BF16, 128, 0, 0), (1, 4095, 777, BF16, 32, 1, 0),
     (15, 2047, 65, F32, 64, 0, 0), (16, 2048, 64, BF16, 32, 0, 0), (17, 640, 300, F16, 128, 1, 1), (31, 999, 2000, BF16, 64, 1, 1),
     (33, 12288, 40, BF16, 64, 0, 0), (48, 9216, 256, F32, 64, 1, 1), (49, 500, 1111, F32, 32, 0, 0), (64, 1536, 512, F16, 32, 0, 1),
-    (2, 96, 33000, BF16, 32, 1, 0), (1, 64, 33000, F32, 64, 0, 0), (3, 130, 33000, F16, 128, 1, 1), (16, 200, 17000, F32, 64, 0, 0),
+    (9, 700, 5000, BF16, 64, 1, 0), (12, 300, 6000, F32, 32, 0, 0), (7, 900, 5000, F32, 64, 1, 1), (58, 161, 3467, BF16, 64, 0, 0), (14, 4337, 1534, F16, 32, 0, 1),
+    (9, 2000, 400, F32, 128, 0, 0), (6, 200, 16384, F32, 64, 0, 0), (2, 200, 16384, F32, 64, 0, 0), (2, 96, 33000, BF16, 32, 1, 0), (1, 64, 33000, F32, 64, 0, 0), (3, 130, 33000, F16, 128, 1, 1), (16, 200, 17000, F32, 64, 0, 0),
     (20, 300, 500, F32, 32, 1, 0), (40, 300, 500, F32, 32, 0, 1), (32, 9000, 70, F32, 128, 0, 0), (64, 9000, 70, BF16, 128, 1, 0), (48, 300, 20000, F16, 32, 0, 0),
     (1, 4096, 128256, BF16, 32, 0, 0), (6, 4096, 128257, F16, 128, 1, 0), (1, 4090, 128256, F32, 64, 0, 0),
     (64, 771, 129, F32, 128, 1, 0), (65, 260, 50, BF16, 32, 1, 0), (200, 96, 33, F32, 32, 0, 1), (1, 12287, 9, F32, 32, 1, 0), (8, 160, 30000, BF16, 32, 1, 0),

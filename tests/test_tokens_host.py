@@ -53,12 +53,16 @@ def test_q4_variants_have_parity_cases():
     seen = set()
     for m, k, o, dtype, group, bias, relu in t.CASES:
         name = lib.q4_desc_kernel_names(lib.q4_desc_create(lib.Q4Params(m, k, o, dtype, group, bias, relu)))
-        shape, splits = re.fullmatch(r"fwd=(?:terms\+)?q4\[(.*)\]\(S=(\d+),W=\d+\)", name).groups()
+        terms, shape, splits = re.fullmatch(r"fwd=(terms\+)?q4\[(.*)\]\(S=(\d+),W=\d+\)", name).groups()
+        if dtype is F32 and not terms:
+            seen.add(("direct", shape))
         seen.add((shape, int(splits) > 1, dtype is F32))
     for wide in (False, True):
-        for shape in ("m16,n16,r1", "m16,n64,r1" if wide else "m16,n32,r1", "m16,n32", "m16,n64", "m32,n64", "m48,n64", "m64,n64"):
+        for shape in ("m16,n16,r1", "m16,n64,r1" if wide else "m16,n32,r1", "m16,n16", "m16,n32", "m16,n64", "m32,n64", "m48,n64", "m64,n64"):
             assert (shape, False, wide) in seen, (shape, wide)
-        assert any(s and f is wide for _, s, f in seen)
+        assert any(len(s) == 3 and s[1] and s[2] is wide for s in seen)
+    assert ("direct", "m16,n16,r1") in seen and ("direct", "m16,n16") in seen
+    seen = {s for s in seen if len(s) == 3}
     for shape in ("m16,n32,r1,stream", "m16,n64,stream"):
         assert (shape, False, False) in seen
     assert ("m16,n64,r1,stream", False, True) in seen
