@@ -16,8 +16,9 @@
  * may share memory with another one of the list.  Tensors that follow each other in memory, as views of one flat
  * buffer do, are taken together; the result does not depend on it but for the order of the sums.
  *
- * The workspace is 16-byte aligned.  Ownership, execution and errors as in mi355conv.h.  Every call only enqueues kernels (two for up to 96 runs of tensors that
- * follow each other, two for each further 96) and may be captured.  Equal calls give equal bits.
+ * The workspace is 16-byte aligned.  Ownership, execution and errors as in mi355conv.h.  Every call only enqueues kernels (a pass each for
+ * the sum and the product, of one launch for up to 96 runs of tensors that follow each other, and one between them for many partial
+ * sums) and may be captured.  Equal calls give equal bits.
  */
 #ifndef MI355GN_H
 #define MI355GN_H

@@ -456,13 +456,18 @@ int launch_forward(const q4_desc* d, const Q4Args& a, hipStream_t stream) {
   const bool stream_codes = streams(d);
   switch (m_tiles(d)) {
     case 1:
-      if (d->p.m <= 4)
-        d->nt == 1 ? d->prepared ? launch_group<DTYPE, 1, 1, 1>(d, a, stream) : launch_group<DTYPE, 1, 1, 1, false, false>(d, a, stream)
-                   : stream_codes ? launch_group<DTYPE, 1, kManyTiles<DTYPE>, 1, true>(d, a, stream) : launch_group<DTYPE, 1, kManyTiles<DTYPE>, 1>(d, a, stream);
-      else
-        d->nt == 1 ? d->prepared ? launch_group<DTYPE, 1, 1, 4>(d, a, stream) : launch_group<DTYPE, 1, 1, 4, false, false>(d, a, stream)
-        : d->nt == 2 ? d->prepared ? launch_group<DTYPE, 1, 2, 4>(d, a, stream) : launch_group<DTYPE, 1, 2, 4, false, false>(d, a, stream)
-                   : stream_codes ? launch_group<DTYPE, 1, 4, 4, true>(d, a, stream) : launch_group<DTYPE, 1, 4, 4>(d, a, stream);
+      if (d->p.m <= 4) {
+        if (d->nt == 1)
+          d->prepared ? launch_group<DTYPE, 1, 1, 1>(d, a, stream) : launch_group<DTYPE, 1, 1, 1, false, false>(d, a, stream);
+        else
+          stream_codes ? launch_group<DTYPE, 1, kManyTiles<DTYPE>, 1, true>(d, a, stream) : launch_group<DTYPE, 1, kManyTiles<DTYPE>, 1>(d, a, stream);
+      } else if (d->nt == 1) {
+        d->prepared ? launch_group<DTYPE, 1, 1, 4>(d, a, stream) : launch_group<DTYPE, 1, 1, 4, false, false>(d, a, stream);
+      } else if (d->nt == 2) {
+        d->prepared ? launch_group<DTYPE, 1, 2, 4>(d, a, stream) : launch_group<DTYPE, 1, 2, 4, false, false>(d, a, stream);
+      } else {
+        stream_codes ? launch_group<DTYPE, 1, 4, 4, true>(d, a, stream) : launch_group<DTYPE, 1, 4, 4>(d, a, stream);
+      }
       break;
     case 2: launch_group<DTYPE, 2, 4, 4>(d, a, stream); break;
     case 3: launch_group<DTYPE, 3, 4, 4>(d, a, stream); break;
@@ -525,7 +530,7 @@ int q4_desc_create(q4_desc_t** out, const q4_params_t* pp) {
     if (d->prepared) d->ws_bytes += terms_bytes(d);
     if (d->splits > 1) d->ws_bytes += (size_t)d->splits * p.m * p.num_output * 4;
   }
-  snprintf(d->names, sizeof(d->names), "fwd=%sq4[m%d,n%d%s%s](S=%d,W=%d)", d->prepared ? "terms+" : "", 16 * mt, 16 * d->nt, p.m <= 4 ? ",r1" : "", streams(d) && d->nt > 1 ? ",stream" : "", d->splits, d->waves);
+  snprintf(d->names, sizeof(d->names), "fwd=%sq4[m%d,n%d%s%s](S=%d,W=%d)", d->prepared ? "terms+" : "", 16 * mt, 16 * d->nt, p.m <= 4 ? ",r1" : "", streams(d) && d->nt > (p.m <= 4 ? 1 : 2) ? ",stream" : "", d->splits, d->waves);
   *out = d;
   return CONV_OK;
 }
