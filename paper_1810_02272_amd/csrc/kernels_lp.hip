@@ -81,10 +81,11 @@ struct Sums {
   float m, s, s2;
 };
 
-// Adds what another part of the row has found: relative to that part's own maximum m_t.
+// Adds what another part of the row has found: relative to that part's own maximum m_t.  A part that lies beyond the range in a row that
+// does not is 2^-64 of it at most (beyond), and its sums may be relative to another number than the range's end: nothing of it is added.
 __device__ __forceinline__ void add_part(Sums& a, float M, bool over, float c, float m_t, float s_t, float s2_t) {
   const float d = reference(m_t, c) - M;
-  const float f = over ? (m_t == a.m ? 1.f : 0.f) : m_t == -INFINITY ? 0.f : exp2_fast(d);
+  const float f = over ? (m_t == a.m ? 1.f : 0.f) : m_t * c < -kMostReference ? 0.f : exp2_fast(d);
   a.s += f * s_t;
   a.s2 += f == 0.f ? 0.f : over ? s2_t : f * (s2_t + d * s_t);
 }

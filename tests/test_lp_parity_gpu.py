@@ -401,3 +401,63 @@ def test_refusals_on_the_device():
         lib.lp_forward(plain, x, token, f(4), f(4), None, None, None, ws)
     with pytest.raises(lib.ConvError):
         lib.lp_backward(plain, x, token, f(4, 4), f(4), f(4), torch.empty_like(x))
+
+
+def exponents_that_round_to(reference, scale, dtype):
+    """Values of the type, next to each other, whose product with scale log2(e), as the kernels round it to fp32, is `reference`."""
+    c = (torch.tensor(scale, dtype=F32).double() * 1.44269504088896340736).to(F32)
+    x = torch.tensor(reference / float(c)).to(dtype)
+    found = []
+    for toward in (-INF, INF):
+        at = x
+        for _ in range(8):
+            found.append(float(at))
+            at = torch.nextafter(at, torch.tensor(toward, dtype=dtype))
+    return sorted({v for v in found if float(torch.tensor(v, dtype=F32) * c) == reference})
+
+
+@pytest.mark.parametrize("dtype,scale,vocab", [(F32, 1.0, 40000), (F32, 1.0, 17001), (F32, 0.37, 70001), (F32, 2.0 ** 20, 40000), (BF16, math.log(2), 70001),
+                                               (BF16, 2.0 ** -40 * math.log(2), 40000), (BF16, 2.0 ** -40 * math.log(2), 128256)])
+def test_largest_logit_at_the_end_of_the_references(dtype, scale, vocab):
+    """Rows whose largest exponent is the least that a reference holds, -2^30, among masks beyond it: alone, several, in the first and the last
+    part of a row, with masks one step of the type below; and rows of nothing but such masks."""
+    best = exponents_that_round_to(-2.0 ** 30, scale, dtype)
+    assert best
+    below = float(torch.nextafter(torch.tensor(best[0], dtype=dtype), torch.tensor(-INF, dtype=dtype)))
+    rows = 6 + len(best)
+    x = torch.full((rows, vocab), -1e30, device=DEV)
+    x[0, 0] = best[-1]
+    x[1, vocab - 1] = best[-1]
+    x[2, ::vocab // 3] = best[-1]
+    x[3], x[3, vocab // 2] = below, best[-1]
+    x[4] = below
+    x[5, : vocab // 2], x[5, 7] = below, best[0]
+    for r, value in enumerate(best):
+        x[6 + r, 11 * r] = value
+    x = x.to(dtype)
+    token = torch.zeros(rows, device=DEV, dtype=torch.int32)
+    token[1], token[5] = vocab - 1, 7
+    want_logp, want_h = tokens.log_probs(x, scale)
+    w, u = torch.randn(rows, device=DEV), torch.randn(rows, device=DEV) * 0.1
+    case = (rows, vocab, dtype, 5, 1, scale, 0, 0)
+    for copies in (1, 50):  # rows in parts, and teams of a whole row
+        n = rows * copies
+        many, tokens_ = x.repeat(copies, 1), token.repeat(copies)
+        d = lib.lp_desc_create(lib.LpParams(n, vocab, dtype, 5, 1, scale))
+        print(lib.lp_desc_kernel_names(d), flush=True)
+        ws = torch.empty(lib.lp_desc_workspace_bytes(d) // 4 + 1, device=DEV)
+        logp, h, stats = torch.empty(n, device=DEV), torch.empty(n, device=DEV), torch.empty((n, 4), device=DEV)
+        tl, tt = torch.empty((n, 5), device=DEV), torch.empty((n, 5), device=DEV, dtype=torch.int32)
+        lib.lp_forward(d, many, tokens_, logp, h, stats, tl, tt, ws)
+        g, g2, logp2, h2 = torch.empty_like(many), torch.empty_like(many), torch.empty_like(logp), torch.empty_like(h)
+        lib.lp_backward(d, many, tokens_, stats, w.repeat(copies), u.repeat(copies), g)
+        lib.lp_forward_backward(d, many, tokens_, w.repeat(copies), u.repeat(copies), logp2, h2, g2, ws)
+        for at in (slice(0, rows), slice(n - rows, n)):
+            check_rows(want_logp, want_h, logp[at], h[at], token, vocab)
+            check_rows(want_logp, want_h, logp2[at], h2[at], token, vocab)
+            index = tokens.top_tokens(x, 5)
+            assert torch.equal(tt[at].long(), index)
+            want = want_logp.gather(1, index)
+            within(tl[at], want, U * (256 + 4 * want.abs()), "top_logp")
+            check_gradient(case, x, token, w, u, g[at])
+            check_gradient(case, x, token, w, u, g2[at])
