@@ -109,7 +109,7 @@ __device__ __forceinline__ RowStat finish(const Sums& a, float c, float scale) {
 // The natural logarithm of the probability of a logit.
 __device__ __forceinline__ float log_prob(const RowStat& r, float x, float scale) {
   const float t = fmaf(x, r.c, -r.M);
-  if (t == -INFINITY && x != -INFINITY) return x * scale - r.M / r.c * scale;  // c x is out of range, scale x may not be
+  if (t == -INFINITY && x != -INFINITY) return x * scale - r.M / r.c * scale - kLn2 * r.log2s;  // c x is out of range, scale x may not be
   return fmaf(r.step, t, -kLn2 * r.log2s);
 }
 

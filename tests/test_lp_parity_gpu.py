@@ -461,3 +461,28 @@ def test_largest_logit_at_the_end_of_the_references(dtype, scale, vocab):
             within(tl[at], want, U * (256 + 4 * want.abs()), "top_logp")
             check_gradient(case, x, token, w, u, g[at])
             check_gradient(case, x, token, w, u, g2[at])
+
+
+@pytest.mark.parametrize("rows,vocab,dtype", [(6, 300, BF16), (6, 9000, F32), (6, 3000, F16), (260, 17000, BF16), (256, 100000, F32), (300, 3000, F16),
+                                              (300, 8000, BF16), (600, 40000, BF16), (6, 70000, BF16), (6, 17000, F32)])
+def test_not_a_number_reaches_masked_tokens(rows, vocab, dtype):
+    """Tokens and alternatives at masks of the type's lowest value, whose product with the scale leaves fp32, in rows with a NaN or +inf."""
+    x = torch.randn((rows, vocab), device=DEV).to(dtype)
+    lowest = torch.finfo(dtype).min
+    for r, odd in ((1, math.nan), (2, INF), (3, math.nan)):
+        x[r] = lowest
+        x[r, vocab // 3] = odd
+    x[1, 1] = 5.0
+    token = torch.zeros(rows, dtype=torch.int32, device=DEV)
+    token[1], token[2], token[3] = 2, vocab - 1, 0
+    d = lib.lp_desc_create(lib.LpParams(rows, vocab, dtype, 4, 1))
+    print(lib.lp_desc_kernel_names(d), flush=True)
+    ws = torch.empty(lib.lp_desc_workspace_bytes(d) // 4 + 1, device=DEV)
+    logp, logp2, h = torch.empty(rows, device=DEV), torch.empty(rows, device=DEV), torch.empty(rows, device=DEV)
+    tl, tt = torch.empty((rows, 4), device=DEV), torch.empty((rows, 4), device=DEV, dtype=torch.int32)
+    lib.lp_forward(d, x, token, logp, h, None, tl, tt, ws)
+    lib.lp_forward_backward(d, x, token, torch.ones(rows, device=DEV), None, logp2, None, torch.empty_like(x), ws)
+    good = [0] + list(range(4, rows))
+    for t in (logp, logp2, tl):
+        assert torch.isnan(t[1:4]).all() and torch.isfinite(t[good]).all()
+    assert torch.equal(tt.long(), tokens.top_tokens(x, 4))
