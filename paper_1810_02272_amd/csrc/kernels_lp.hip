@@ -869,7 +869,7 @@ int lp_desc_create(lp_desc_t** out, const lp_params_t* pp) {
   d->seg = p.vocab;
   // Where a workgroup of 1024 cannot hold a row and there are two compute units or more for each, rows are taken in parts: 64 x 128256
   // with 20 alternatives 14.4 us, whole rows 24.2; 8 x 128256 12.0, 23.2; 200 x 50257, one part, 15.0, and 14.7 in two.
-  if (p.rows > 0 && 2 * p.rows <= kUnits && p.vocab > solo) {
+  if (p.rows > 0 && p.rows <= kUnits / 2 && p.vocab > solo) {
     const int splits = std::min(std::min(kUnits / p.rows, (p.vocab + solo / 4 - 1) / (solo / 4)), kMaxSplits);
     d->seg = ((p.vocab + splits - 1) / splits + vec - 1) / vec * vec;
     d->splits = (p.vocab + d->seg - 1) / d->seg;

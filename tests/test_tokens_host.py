@@ -128,6 +128,13 @@ def test_lp_calls():
     assert c.lp_forward_backward(parts.handle, f, 100000, f, f, f, f, f, f, 100000, None, 0, None) == EWORKSPACE
 
 
+@pytest.mark.parametrize("rows", [1 << 22, (1 << 30) - 1, 1 << 30, (1 << 30) + 64, (1 << 31) - 1])
+@pytest.mark.parametrize("vocab", [1, 40000, 200000, (1 << 30) - 1])
+def test_lp_descriptors_of_any_number_of_rows(rows, vocab):
+    d = lib.lp_desc_create(lib.LpParams(rows, vocab, BF16, min(vocab, 64), 1))
+    assert "parts" not in lib.lp_desc_kernel_names(d) and lib.lp_desc_workspace_bytes(d) == 0
+
+
 def test_lp_refuses_cpu_tensors():
     d = lib.lp_desc_create(lib.LpParams(2, 10, F32, 0, 0))
     x, t = torch.zeros(2, 10), torch.zeros(2, dtype=torch.int32)
