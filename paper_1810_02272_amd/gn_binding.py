@@ -8,7 +8,7 @@ from dataclasses import dataclass
 import torch
 
 from . import binding as _b
-from .lp_binding import DTYPES
+from .lp_binding import DTYPES, _fits
 
 _ready = False
 
@@ -67,7 +67,8 @@ def gn_desc_create(params: GnParams) -> GnDesc:
     codes = list(map(DTYPES.get, params.dtypes))
     if None in codes:
         raise TypeError(f"dtypes: {params.dtypes[codes.index(None)]} is not among those of this operator")
-    c = _CParams(n, (ctypes.c_int64 * n)(*params.counts), (ctypes.c_int32 * n)(*codes))
+    counts = [_fits(count, 64, "gn_desc_create") for count in params.counts]
+    c = _CParams(n, (ctypes.c_int64 * n)(*counts), (ctypes.c_int32 * n)(*codes))
     out = ctypes.c_void_p()
     _b._check(_load().gn_desc_create(ctypes.byref(out), ctypes.byref(c)), "gn_desc_create")
     desc = GnDesc(out.value, params)

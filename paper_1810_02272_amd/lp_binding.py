@@ -56,6 +56,14 @@ def _dtype(dtype, allowed) -> int:
     return code
 
 
+def _fits(value, bits, where) -> int:
+    """An integer for a C field of so many bits: ctypes would take its lowest ones."""
+    value = int(value)
+    if not -1 << bits - 1 <= value < 1 << bits - 1:
+        raise _b.ConvError(_b.CONV_ESHAPE if value > 0 else _b.CONV_EINVAL, where)
+    return value
+
+
 class LpDesc:
     """Owner of an lp_desc_t*; destroyed with the Python object (or lp_desc_destroy)."""
 
@@ -72,7 +80,8 @@ class LpDesc:
 
 
 def lp_desc_create(params: LpParams) -> LpDesc:
-    c = _CParams(int(params.rows), int(params.vocab), _dtype(params.dtype, (0, 1, 2)), int(params.top), int(params.entropy),
+    fits = lambda value: _fits(value, 32, "lp_desc_create")
+    c = _CParams(fits(params.rows), fits(params.vocab), _dtype(params.dtype, (0, 1, 2)), fits(params.top), fits(params.entropy),
                  float(params.scale))
     out = ctypes.c_void_p()
     _b._check(_load().lp_desc_create(ctypes.byref(out), ctypes.byref(c)), "lp_desc_create")

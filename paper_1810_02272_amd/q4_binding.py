@@ -8,7 +8,7 @@ from dataclasses import dataclass
 import torch
 
 from . import binding as _b
-from .lp_binding import _dtype
+from .lp_binding import _dtype, _fits
 
 _ready = False
 
@@ -66,7 +66,8 @@ class Q4Desc:
 
 def q4_desc_create(params: Q4Params) -> Q4Desc:
     p = params
-    c = _CParams(int(p.m), int(p.k), int(p.num_output), _dtype(p.dtype, (0, 1, 2)), int(p.group), int(p.bias_term), int(p.relu))
+    fits = lambda value: _fits(value, 32, "q4_desc_create")
+    c = _CParams(fits(p.m), fits(p.k), fits(p.num_output), _dtype(p.dtype, (0, 1, 2)), fits(p.group), fits(p.bias_term), fits(p.relu))
     out = ctypes.c_void_p()
     _b._check(_load().q4_desc_create(ctypes.byref(out), ctypes.byref(c)), "q4_desc_create")
     desc = Q4Desc(out.value, params)

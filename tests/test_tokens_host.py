@@ -213,3 +213,21 @@ def test_q4_calls():
         assert c.q4_forward(d.handle, *args, f, 1 << 30, None) == EINVAL
     assert c.q4_forward(plain.handle, f, f, f, f, f, 1 << 30, None) == EINVAL  # bias unexpected
     assert c.q4_forward(none.handle, None, f, None, None, None, 0, None) == OK
+
+
+@pytest.mark.parametrize("create,params,field", [(lib.lp_desc_create, dict(rows=4, vocab=100, top=2), f) for f in ("rows", "vocab", "top", "entropy")] +
+                         [(lib.q4_desc_create, dict(m=2, k=64, num_output=8), f) for f in ("m", "k", "num_output", "group", "bias_term", "relu")])
+def test_parameters_beyond_32_bits_are_refused(create, params, field):
+    make = lib.LpParams if create is lib.lp_desc_create else lib.Q4Params
+    plain = getattr(make(**params), field)
+    for value, status in ((plain + (1 << 32), ESHAPE), (plain + (1 << 64), ESHAPE), (plain - (1 << 32), EINVAL)):
+        with pytest.raises(lib.ConvError) as e:
+            create(make(**{**params, field: value}))
+        assert e.value.status == status
+
+
+def test_gn_counts_beyond_64_bits_are_refused():
+    for count, status in (((1 << 64) + 1, ESHAPE), (1 - (1 << 64), EINVAL)):
+        with pytest.raises(lib.ConvError) as e:
+            lib.gn_desc_create(lib.GnParams([3, count], [F32, F32]))
+        assert e.value.status == status
