@@ -107,6 +107,8 @@ def _pointers(tensors, params, name):
 
 def gn_clip(desc, grads, limit, outs=None, norm=None, ws=None, stream=None) -> None:
     """outs=None: in place."""
+    if not isinstance(grads, (list, tuple)):
+        grads = list(grads)  # an iterator is read once, also where the outputs are the gradients
     if outs is None:
         outs = grads
     status = _b._marshal.gn_clip(desc._plan, grads, limit, outs, norm, ws, stream)

@@ -167,3 +167,15 @@ def test_refusals_on_the_device():
                                              ([a, b], 1.0, None, ws[:-1], lib.ConvError)):
         with pytest.raises(error):
             lib.gn_clip(d, grads, limit, outs, None, space)
+
+
+def test_gradients_from_an_iterator():
+    grads = [torch.randn(300, device=DEV), torch.randn((2, 3), device=DEV).to(BF16)]
+    d = lib.gn_desc_create(lib.GnParams([300, 6], [F32, BF16]))
+    ws, norm = torch.empty(lib.gn_desc_workspace_bytes(d) // 4, device=DEV), torch.empty(1, device=DEV)
+    before = [t.clone() for t in grads]
+    lib.gn_clip(d, iter(grads), 3.0, None, norm, ws)
+    check(norm, grads, before, 3.0)
+    outs = [torch.empty_like(t) for t in grads]
+    lib.gn_clip(d, (t for t in before), 3.0, (t for t in outs), norm, ws)
+    check(norm, outs, before, 3.0)

@@ -231,3 +231,13 @@ def test_gn_counts_beyond_64_bits_are_refused():
         with pytest.raises(lib.ConvError) as e:
             lib.gn_desc_create(lib.GnParams([3, count], [F32, F32]))
         assert e.value.status == status
+
+
+def test_gn_reads_an_iterator_of_gradients_once():
+    d = lib.gn_desc_create(lib.GnParams([0, 0], [F32, BF16]))  # of no elements: they may be absent
+    for grads in ([None, None], (None, None), iter([None, None]), (t for t in (None, None))):
+        with pytest.raises(lib.ConvError) as e:
+            lib.gn_clip(d, grads, 1.0, stream=0)
+        assert e.value.status == EWORKSPACE  # every tensor found, in place
+    with pytest.raises(ValueError):
+        lib.gn_clip(d, iter([None]), 1.0, stream=0)
