@@ -6,8 +6,8 @@
  *   out  = factor g,   factor = limit / norm where norm > limit, else 1
  *
  * the step that Caffe's solvers take between accumulating parameter diffs (the paper's Appendix A and B) and applying them.
- * Squares and sums are held in fp64; the factor is held in fp64 for fp64 tensors and rounded to fp32 for the others, whose product
- * with it is rounded once more, to the tensor's type.  A norm of +inf has the factor 0 (so an infinite gradient becomes NaN
+ * Squares and sums are held in fp64; the factor is held in fp64 for fp64 tensors and rounded to 24 bits for the others (of any size,
+ * also below fp32's normal numbers), whose product with it is rounded to fp32 and once more to the tensor's type.  A norm of +inf has the factor 0 (so an infinite gradient becomes NaN
  * and the others 0); one that is NaN compares as not above the limit, and the gradients stay as they are.
  *
  * Layouts: tensor i is counts[i] contiguous elements of dtypes[i] in DEVICE memory, on the element's own alignment; the arrays of

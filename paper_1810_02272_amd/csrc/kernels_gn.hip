@@ -150,21 +150,38 @@ __device__ __forceinline__ double sum_chunk(const Segment& s, int64_t from) {
   return acc[0] + acc[1];
 }
 
+// A factor in fp64, or in fp32, whose normal numbers do not reach as far down: below them it is a number of all 24 bits times a power of
+// two, applied one after the other (3e38 clipped to 1 came out 5e-6 off by a subnormal factor, 1e25 to 1e-20 as zeros).
+template <typename F>
+struct Factor {
+  F f;
+  __device__ __forceinline__ explicit Factor(double factor) : f(factor) {}
+  __device__ __forceinline__ F times(F x) const { return x * f; }
+};
+
+template <>
+struct Factor<float> {
+  float f;
+  int e = 0;  // (an instruction a value that is not seen beside the memory's time)
+  __device__ __forceinline__ explicit Factor(double factor) { f = (float)(factor < (double)FLT_MIN ? frexp(factor, &e) : factor); }
+  __device__ __forceinline__ float times(float x) const { return ldexpf(x * f, e); }
+};
+
 template <int DTYPE, bool STREAM_IN, bool STREAM_OUT>
 __device__ __forceinline__ void scale_chunk(const Segment& s, int64_t from, double factor) {
   typedef Elem<DTYPE> E;
   typedef decltype(E::get(u32x4(), 0)) F;  // fp64 for fp64, fp32 for the others
   typename E::T* const q = static_cast<typename E::T*>(s.out);
-  const F f = (F)factor;
+  const Factor<F> f(factor);
   each<DTYPE, STREAM_IN>(
       s, from,
       [&](const u32x4& r, int64_t at) {
         F x[E::VEC];
 #pragma unroll
-        for (int i = 0; i < E::VEC; ++i) x[i] = E::get(r, i) * f;
+        for (int i = 0; i < E::VEC; ++i) x[i] = f.times(E::get(r, i));
         put_vec<E, STREAM_OUT>(q + at, E::pack(x));
       },
-      [&](typename E::T v, int64_t at) { q[at] = E::from_float(E::to_float(v) * f); });
+      [&](typename E::T v, int64_t at) { q[at] = E::from_float(f.times(E::to_float(v))); });
 }
 
 __device__ __forceinline__ int elem_shift(int dtype) { return dtype == MI355_F64 ? 3 : dtype == MI355_F32 ? 2 : 1; }

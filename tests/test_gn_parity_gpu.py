@@ -179,3 +179,36 @@ def test_gradients_from_an_iterator():
     outs = [torch.empty_like(t) for t in grads]
     lib.gn_clip(d, (t for t in before), 3.0, (t for t in outs), norm, ws)
     check(norm, outs, before, 3.0)
+
+
+def scaled_clip(grads, limit):
+    """(norm, outputs) in 64 bits, the squares taken of values over the greatest: none overflows or vanishes."""
+    most = max(float(g.double().abs().max()) for g in grads)
+    norm = most * math.sqrt(math.fsum(float((g.double() / most).square().sum()) for g in grads))
+    factor = lambda g: g.double() / norm * limit if norm > limit else g.double()  # (limit / norm itself may be out of range)
+    return norm, [factor(g) for g in grads]
+
+
+def check_scaled(grads, limit):
+    norm, outs = run(grads, limit)
+    want_norm, want = scaled_clip(grads, limit)
+    assert norm == pytest.approx(float(torch.tensor(want_norm, dtype=F64).float()), rel=2.0 ** -23, abs=2.0 ** -149)
+    for o, w, g in zip(outs, want, grads):
+        if want_norm <= limit:
+            assert torch.equal(o, g)
+            continue
+        info = torch.finfo(o.dtype)
+        steps = 2.0 ** -50 if o.dtype is F64 else 2.0 ** -23  # fp64: the norm's sum and root, the factor, the product; here in the oracle too
+        bound = w.abs() * (info.eps / 2 + steps) + (2.0 ** -25 if o.dtype is F16 else 2.0 ** -126 if o.dtype is not F64 else 0.0)
+        assert bool(((o.double() - w).abs() <= bound).all()), (o.dtype, o.numel())
+
+
+@pytest.mark.parametrize("size,limit", [(3e38, 1.0), (1e30, 1e-15), (1e25, 1e-20), (1e38, 1e-3), (1e20, 1e-18)])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_factors_below_the_normal_range(dtype, size, limit):
+    """The limit over the norm is subnormal in fp32, or less; the products are not."""
+    g = torch.Generator(device=DEV).manual_seed(1)
+    sign = lambda n: torch.randint(2, (n,), generator=g, device=DEV) * 2.0 - 1.0
+    check_scaled([(sign(1000) * size).to(dtype), (torch.rand(4099, generator=g, device=DEV) * size).to(dtype)], limit)
+    check_scaled([(torch.rand(70001, generator=g, device=DEV) * size).to(dtype), torch.randn(77, generator=g, device=DEV).to(F16),
+                  torch.randn(500, generator=g, device=DEV, dtype=F64) * size], limit)
