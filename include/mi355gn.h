@@ -6,9 +6,11 @@
  *   out  = factor g,   factor = limit / norm where norm > limit, else 1
  *
  * the step that Caffe's solvers take between accumulating parameter diffs (the paper's Appendix A and B) and applying them.
- * Squares and sums are held in fp64; the factor is held in fp64 for fp64 tensors and rounded to 24 bits for the others (of any size,
- * also below fp32's normal numbers), whose product with it is rounded to fp32 and once more to the tensor's type.  A norm of +inf has the factor 0 (so an infinite gradient becomes NaN
- * and the others 0); one that is NaN compares as not above the limit, and the gradients stay as they are.
+ * Squares and sums are held in fp64, and no square of a finite gradient overflows or vanishes.  The factor is held in fp64 for
+ * fp64 tensors (below 2^-1022 with the bits that such numbers have) and rounded to 24 bits for the others, of any size, also
+ * below fp32's normal numbers; their product with it is rounded to fp32 and once more to the tensor's type.  A norm of +inf (an
+ * infinite gradient, or fp64 gradients whose norm itself is beyond fp64) has the factor 0, so an infinite gradient becomes NaN
+ * and the others 0; one that is NaN compares as not above the limit, and the gradients stay as they are.
  *
  * Layouts: tensor i is counts[i] contiguous elements of dtypes[i] in DEVICE memory, on the element's own alignment; the arrays of
  * pointers are HOST memory and are read before the call returns.  outs[i] may be grads[i] itself (a factor of 1 then

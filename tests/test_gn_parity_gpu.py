@@ -212,3 +212,38 @@ def test_factors_below_the_normal_range(dtype, size, limit):
     check_scaled([(sign(1000) * size).to(dtype), (torch.rand(4099, generator=g, device=DEV) * size).to(dtype)], limit)
     check_scaled([(torch.rand(70001, generator=g, device=DEV) * size).to(dtype), torch.randn(77, generator=g, device=DEV).to(F16),
                   torch.randn(500, generator=g, device=DEV, dtype=F64) * size], limit)
+
+
+@pytest.mark.parametrize("exponent", [300, 200, 160, -100, -160, -200, -290])
+@pytest.mark.parametrize("ratio", [0.3, 3.0])
+def test_fp64_gradients_whose_squares_leave_the_range(exponent, ratio):
+    g = torch.Generator(device=DEV).manual_seed(2)
+    r = lambda n: torch.randn(n, generator=g, device=DEV, dtype=F64) * 10.0 ** exponent
+    for n in (1, 3, 1001, 2000003):
+        check_scaled([r(n)], ratio * math.sqrt(n) * 10.0 ** exponent)
+    check_scaled([r(5000), torch.randn(333, generator=g, device=DEV), r(77)], ratio * math.sqrt(5077) * 10.0 ** exponent)
+
+
+@pytest.mark.parametrize("at", [478, 479, 480, 481, 482, -478, -479, -480, -481, -482])
+def test_fp64_gradients_of_two_ranges_count_alike(at):
+    """Magnitudes on both sides of a power of two, each a good part of the norm."""
+    g = torch.Generator(device=DEV).manual_seed(3)
+    t = torch.ldexp(torch.rand(3001, generator=g, device=DEV, dtype=F64) * 3 + 0.25, torch.tensor(at, device=DEV)).contiguous()
+    check_scaled([t[:1000], t[1000:], torch.zeros(5, device=DEV)], 2.0 ** at)
+    check_scaled([t, torch.ones(3, device=DEV)], 2.0 ** at)
+
+
+def test_fp64_infinities_and_zeros():
+    zero = torch.zeros(77, device=DEV, dtype=F64)
+    norm, (out,) = run([zero], 0.0)
+    assert norm == 0.0 and torch.equal(out, zero)
+    big = torch.full((50,), 1e300, device=DEV, dtype=F64)
+    for bad in (math.inf, -math.inf):
+        big[7] = bad
+        norm, (out,) = run([big], 1.0)
+        assert norm == math.inf and math.isnan(float(out[7])) and float(out[0]) == 0.0
+    for size in (1e300, 1.0, 1e-300):
+        nan = torch.full((50,), size, device=DEV, dtype=F64)
+        nan[7] = math.nan
+        norm, (out,) = run([nan], 1.0)
+        assert math.isnan(norm) and torch.equal(out.nan_to_num(9.0), nan.nan_to_num(9.0))
