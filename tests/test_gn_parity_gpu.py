@@ -247,3 +247,20 @@ def test_fp64_infinities_and_zeros():
         nan[7] = math.nan
         norm, (out,) = run([nan], 1.0)
         assert math.isnan(norm) and torch.equal(out.nan_to_num(9.0), nan.nan_to_num(9.0))
+
+
+# Every kernel beyond the small sizes above: tables of up to 8 and up to 96 runs, with fp64 tensors and without, the sum around the cache, the
+# product with reads, or writes alone, around it; what the second pass finds in the cache over several launches.
+FEW_OUT = ([20000003, 30000001, 17], [F32, BF16, F32])
+FEW_HUGE = ([30000001, 5, 20000003], [F64, F32, BF16])
+MANY_OUT = ([1200003 + 1000 * i for i in range(40)], [(F32, BF16)[i % 3 == 2] for i in range(40)])
+MANY_HUGE = ([8000009 + 16 * i for i in range(12)], [(F32, F32, F64, BF16)[i % 4] for i in range(12)])
+LAUNCHES = ([600011 + (i * 37) % 301 for i in range(250)], [(F32, BF16)[i % 5 == 4] for i in range(250)])
+EVERY_TYPE = ([(i * 53) % 1009 for i in range(130)], [(F32, F16, BF16, F64)[i % 4] for i in range(130)])
+LARGE_CASES = [(FEW_OUT, 0), (FEW_HUGE, 0), (MANY_OUT, 3), (MANY_HUGE, 5), (LAUNCHES, 1), (EVERY_TYPE, 1)]
+
+
+@pytest.mark.parametrize("case,apart", LARGE_CASES, ids=["few-out", "few-huge", "many-out", "many-huge", "launches", "every-type"])
+@pytest.mark.parametrize("ratio", [0.3, 7.0])
+def test_large_calls(case, apart, ratio):
+    test_parity(*case, apart, 1, ratio)

@@ -241,3 +241,24 @@ def test_gn_reads_an_iterator_of_gradients_once():
         assert e.value.status == EWORKSPACE  # every tensor found, in place
     with pytest.raises(ValueError):
         lib.gn_clip(d, iter([None]), 1.0, stream=0)
+
+
+def test_gn_variants_have_parity_cases():
+    """The kernels go by the runs of tensors that follow each other (8 and 96 to a launch), by fp64 tensors, and by the bytes of the gradients, and
+    of them and outputs elsewhere, against the 256 MB of the last-level cache."""
+    import test_gn_parity_gpu as t
+    size = {F32: 4, F16: 2, BF16: 2, F64: 8}
+    sums, scales, launches = set(), set(), 0
+    for (counts, dtypes), apart in [(c, a) for c in (t.ONE, t.MIXED, t.MANY, t.LARGE) for a in (0, 3)] + [(t.HUGE, 0)] + t.LARGE_CASES:
+        used = [(n, d) for n, d in zip(counts, dtypes) if n]
+        runs = len(used) if apart else len({d for _, d in used})
+        read = sum(n * size[d] for n, d in used)
+        table = [8 if min(96, runs - first) <= 8 else 96 for first in range(0, runs, 96)]
+        sums |= {(k, read > 1 << 28, F64 in dtypes) for k in table}
+        for written in (read, 0):  # outputs elsewhere, in place
+            scales |= {(k, read > 1 << 28, read + written > 1 << 28) for k in table}
+        if read > 1 << 28:
+            launches = max(launches, len(table))
+    assert sums == {(k, stream, wide) for k in (8, 96) for stream in (False, True) for wide in (False, True)}
+    assert scales == {(k, *s) for k in (8, 96) for s in ((False, False), (False, True), (True, True))}
+    assert launches > 2
