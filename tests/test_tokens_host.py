@@ -249,7 +249,7 @@ def test_gn_variants_have_parity_cases():
     import test_gn_parity_gpu as t
     size = {F32: 4, F16: 2, BF16: 2, F64: 8}
     sums, scales, launches = set(), set(), 0
-    for (counts, dtypes), apart in [(c, a) for c in (t.ONE, t.MIXED, t.MANY, t.LARGE) for a in (0, 3)] + [(t.HUGE, 0)] + t.LARGE_CASES:
+    for (counts, dtypes), apart in [(c, a) for c in (t.ONE, t.MIXED, t.MANY, t.LARGE) for a in (0, 3)] + [(t.HUGE, 0), (t.EVERY_TYPE, 1)] + t.LARGE_CASES:
         used = [(n, d) for n, d in zip(counts, dtypes) if n]
         runs = len(used) if apart else len({d for _, d in used})
         read = sum(n * size[d] for n, d in used)
