@@ -167,3 +167,16 @@ def test_refusals_on_the_device():
             lib.q4_forward(d, **{**dict(x=x, packed=packed, bias=b, y=y, ws=ws), **wrong})
     none = lib.q4_desc_create(lib.Q4Params(0, 40, 9, BF16, 32, 0, 0))
     lib.q4_forward(none, x[:0], packed, None, y[:0], ws)
+
+
+# fp32 rows laid out as operands beforehand in each of the small shapes, for each group; batches of many 64s of rows.
+MORE_CASES = [
+    (1, 4096, 4096, F32, 64, 0, 0), (3, 1500, 500, F32, 32, 1, 0), (4, 2000, 777, F32, 128, 0, 1), (16, 3001, 600, F32, 32, 0, 0), (5, 1300, 1000, F32, 64, 1, 1),
+    (8, 4096, 8000, F32, 64, 1, 0), (5, 130, 9000, F32, 32, 0, 0), (16, 2047, 5001, F32, 128, 0, 1), (7, 1500, 4100, F32, 32, 1, 0),
+    (512, 96, 333, F32, 32, 1, 0), (1000, 640, 300, BF16, 128, 1, 1), (130, 300, 3001, F16, 64, 0, 0), (257, 1111, 70, F32, 64, 0, 0), (2049, 130, 40, BF16, 32, 0, 0),
+]
+
+
+@pytest.mark.parametrize("case", MORE_CASES, ids=["%dx%d-%d-%s-g%d-b%d-r%d" % (c[0], c[1], c[2], str(c[3])[6:], *c[4:]) for c in MORE_CASES])
+def test_more_shapes(case):
+    test_parity(case)

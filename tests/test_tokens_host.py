@@ -262,3 +262,21 @@ def test_gn_variants_have_parity_cases():
     assert sums == {(k, stream, wide) for k in (8, 96) for stream in (False, True) for wide in (False, True)}
     assert scales == {(k, *s) for k in (8, 96) for s in ((False, False), (False, True), (True, True))}
     assert launches > 2
+
+
+def test_q4_variants_have_parity_cases_prepared_and_direct():
+    """Each shape that fp32 rows may take as they are and as operands laid out before, of each group size; batches beyond 64 rows of each type."""
+    import test_q4_parity_gpu as t
+    name = lambda m, k, o, dtype, group: lib.q4_desc_kernel_names(lib.q4_desc_create(lib.Q4Params(m, k, o, dtype, group)))
+    key = lambda text: re.sub(r"\(S=\d+,W=\d+\)", "", text)
+    cases = t.CASES + t.MORE_CASES
+    seen = {(key(name(*c[:5])), c[3]) for c in cases}
+    for m in (1, 4, 5, 16, 17, 33, 49, 64):  # what the library selects over a wide range
+        for k in (32, 100, 1024, 1025, 4096, 12000):
+            for o in (8, 100, 4096, 4097, 8000, 16384, 20000, 33000):
+                for dtype in (F32, F16, BF16):
+                    n = key(name(m, k, o, dtype, 64))
+                    assert (n, dtype) in seen or dtype is not F32 and (n, BF16 if dtype is F16 else F16) in seen, (n, dtype, m, k, o)
+    prepared = {(key(name(*c[:5])), c[4]) for c in t.MORE_CASES if c[3] is F32 and c[0] <= 16}
+    assert prepared >= {(f"fwd=terms+q4[{shape}]", group) for shape in ("m16,n16,r1", "m16,n32") for group in (32, 64, 128)}
+    assert {c[3] for c in cases if c[0] > 64} == {F32, F16, BF16}
