@@ -6,7 +6,8 @@
  *   z[n][o] = bias[o] + sum_i x[n][i] w[o][i];   y = relu ? max(z, 0) : z
  *   value(c) for c = 0 .. 15:  0 0.5 1 1.5 2 3 4 6  -0 -0.5 -1 -1.5 -2 -3 -4 -6     (one sign, two exponent, one mantissa bit)
  * Products with x are exact and summed in fp32 inside each group, the groups' sums times their scales in fp32; fp32 x takes part with all
- * of its 24 bits.  One rounding to y's type at the end.
+ * of its 24 bits, but for those below 2^-133 (of inputs below 2^-110).  One rounding to y's type at the end.  A group's sum is taken before its scale: it stays in
+ * fp32's range where |x| <= 2^118, and may be infinite or NaN beyond, whatever the scale.
  *
  * Layouts, dense row-major DEVICE memory:
  *   x [m][k], bias [num_output], y [m][num_output]: the descriptor's type (fp32, fp16, bf16), on the element's own alignment

@@ -134,7 +134,8 @@ struct Operand<MI355_F32> : Operand<MI355_BF16> {
   static constexpr int TERMS = 3;
 };
 
-// An fp32 value's terms: its leading 8 bits, the next 8, the last 8, each cut off and so exact.  What is not finite is the first term's.
+// An fp32 value's terms: its leading 8 bits, the next 8, the last 8, each cut off and so exact, but for bits below 2^-133, bf16's last.  What is
+// not finite is the first term's.
 __device__ __forceinline__ void three_terms(float x, uint32_t (&t)[3]) {
   const uint32_t u = __builtin_bit_cast(uint32_t, x);
   if ((u & 0x7F800000u) == 0x7F800000u) {

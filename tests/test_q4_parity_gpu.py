@@ -180,3 +180,36 @@ MORE_CASES = [
 @pytest.mark.parametrize("case", MORE_CASES, ids=["%dx%d-%d-%s-g%d-b%d-r%d" % (c[0], c[1], c[2], str(c[3])[6:], *c[4:]) for c in MORE_CASES])
 def test_more_shapes(case):
     test_parity(case)
+
+
+@pytest.mark.parametrize("m", [1, 20])
+@pytest.mark.parametrize("dtype,size,scale", [(F32, 2.0 ** -100, 2.0 ** 60), (F32, 2.0 ** -112, 2.0 ** 60), (F32, 2.0 ** -122, 2.0 ** 60),
+                                              (F32, 2.0 ** -128, 2.0 ** 70), (F32, 2.0 ** -140, 2.0 ** 80), (BF16, 2.0 ** -124, 2.0 ** 60),
+                                              (BF16, 2.0 ** -130, 2.0 ** 70), (F16, 2.0 ** -14, 2.0 ** 8), (F16, 2.0 ** -21, 2.0 ** 12)])
+def test_small_and_subnormal_inputs(m, dtype, size, scale):
+    """As the others' bound, and what lies below 2^-133 of each fp32 input (2^-133 of it at most) times its weight."""
+    case = (m, 1500, 40, dtype, 64, 0, 0)
+    x, codes, scales, _ = make(case)
+    x, scales = (x.double() * size).to(dtype), (scales.double() * scale).to(BF16)
+    y = run(case, x, codes, scales, None)
+    want = tokens.q4_forward(x, codes, scales, None, 1500, 64, 0)
+    weights = tokens.q4_weights(codes, scales, 1500, 64).abs()
+    tol = x.double().abs() @ weights.t().contiguous() * (1500 / 32 + 160) * 2.0 ** -24 + want.abs() * (torch.finfo(dtype).eps / 2 + 2.0 ** -23)
+    tol += (weights.sum(1) * 2.0 ** -133 if dtype is F32 else 0.0) + (2.0 ** -25 if dtype is F16 else 2.0 ** -126)
+    if dtype is not F32 or size > 2.0 ** -124:  # (below, what an fp32 input loses is a good part of it, or all)
+        assert float(want.abs().max()) > 16 * float(tol.max())
+    assert bool(((y.double() - want).abs() <= tol).all())
+
+
+@pytest.mark.parametrize("group", [32, 64, 128])
+@pytest.mark.parametrize("dtype,size,scale", [(F32, 2.0 ** 118, 2.0 ** -16), (BF16, 2.0 ** 118, 2.0 ** -16), (F16, 65504.0, 2.0 ** -12)])
+def test_large_inputs(dtype, size, scale, group):
+    """The greatest sums that the header promises: every input as large as it may be, weights of 6 and -6 scaled down, one sign and both."""
+    case = (3, 512, 40, dtype, group, 0, 0)
+    x, codes, scales, _ = make(case)
+    x = torch.where(x > 0, size, -size).to(dtype)
+    x[0] = size
+    codes[:20], codes[20:] = 0x77, 0xF7
+    scales = torch.full_like(scales, scale)
+    scales[:, 1::2] = -scale / 2
+    check(case, x, codes, scales, None, run(case, x, codes, scales, None))
