@@ -741,23 +741,25 @@ void launch_team(const LpArgs& a, int blocks, int threads, hipStream_t stream) {
 
 template <int DTYPE, Mode MODE, bool ENT, bool STREAM>
 int launch_row(const lp_desc* d, const LpArgs& a, hipStream_t stream) {
-  const int waves = a.rows >= 2048 ? 4 : 1;
-  if (MODE == kPart)
+  if constexpr (MODE == kPart) {
     launch_team<DTYPE, 1024, kSoloVecs, kPart, ENT, false>(a, a.rows * a.splits, 1024, stream);
-  else if (d->form == kWave4)
-    launch_team<DTYPE, 64, 4, MODE, ENT, STREAM>(a, (int)(((int64_t)a.rows + waves - 1) / waves), 64 * waves, stream);
-  else if (d->form == kWave8)
-    launch_team<DTYPE, 64, 8, MODE, ENT, STREAM>(a, (int)(((int64_t)a.rows + waves - 1) / waves), 64 * waves, stream);
-  else if (d->form == kBlock8)
-    launch_team<DTYPE, 256, 8, MODE, ENT, STREAM>(a, a.rows, 256, stream);
-  else if (d->form == kBlock16)
-    launch_team<DTYPE, 256, 16, MODE, ENT, STREAM>(a, a.rows, 256, stream);
-  else if (d->form == kBlock26)
-    launch_team<DTYPE, 256, 26, MODE, ENT, STREAM>(a, a.rows, 256, stream);
-  else if (d->form == kSolo)
-    launch_team<DTYPE, 1024, kSoloVecs, MODE, ENT, false>(a, a.rows, 1024, stream);  // (at most 32 MB)
-  else
-    launch_team<DTYPE, 512, kLongVecs, MODE, ENT, STREAM>(a, a.rows, 512, stream);
+  } else {
+    const int waves = a.rows >= 2048 ? 4 : 1;
+    if (d->form == kWave4)
+      launch_team<DTYPE, 64, 4, MODE, ENT, STREAM>(a, (int)(((int64_t)a.rows + waves - 1) / waves), 64 * waves, stream);
+    else if (d->form == kWave8)
+      launch_team<DTYPE, 64, 8, MODE, ENT, STREAM>(a, (int)(((int64_t)a.rows + waves - 1) / waves), 64 * waves, stream);
+    else if (d->form == kBlock8)
+      launch_team<DTYPE, 256, 8, MODE, ENT, STREAM>(a, a.rows, 256, stream);
+    else if (d->form == kBlock16)
+      launch_team<DTYPE, 256, 16, MODE, ENT, STREAM>(a, a.rows, 256, stream);
+    else if (d->form == kBlock26)
+      launch_team<DTYPE, 256, 26, MODE, ENT, STREAM>(a, a.rows, 256, stream);
+    else if (d->form == kSolo)
+      launch_team<DTYPE, 1024, kSoloVecs, MODE, ENT, false>(a, a.rows, 1024, stream);  // (at most 32 MB)
+    else
+      launch_team<DTYPE, 512, kLongVecs, MODE, ENT, STREAM>(a, a.rows, 512, stream);
+  }
   return (int)hipGetLastError();
 }
 

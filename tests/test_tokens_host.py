@@ -280,3 +280,13 @@ def test_q4_variants_have_parity_cases_prepared_and_direct():
     prepared = {(key(name(*c[:5])), c[4]) for c in t.MORE_CASES if c[3] is F32 and c[0] <= 16}
     assert prepared >= {(f"fwd=terms+q4[{shape}]", group) for shape in ("m16,n16,r1", "m16,n32") for group in (32, 64, 128)}
     assert {c[3] for c in cases if c[0] > 64} == {F32, F16, BF16}
+
+
+def test_lp_row_kernels_of_parts_are_those_that_are_launched():
+    """Parts of a row are taken by workgroups of 1024 threads, through the cache; the library holds no kernel of them for another team."""
+    with open(lib.library_path(), "rb") as f:
+        built = re.findall(rb"lp_row_kernelILi(\d)ELi(\d+)ELi(\d+)ELN\w*?4ModeE(\d)ELb([01])ELb([01])E", f.read())
+    kernels = {tuple(map(int, k)) for k in built}  # type, threads, vectors, mode (2: a part), entropy, stream
+    assert {k for k in kernels if k[3] == 2} == {(t, 1024, 4, 2, e, 0) for t in (0, 1, 2) for e in (0, 1)}
+    teams = {(64, 4), (64, 8), (256, 8), (256, 16), (256, 26), (512, 20)}
+    assert {k[1:3] + k[5:] for k in kernels if k[3] < 2} == {(*team, stream) for team in teams for stream in (0, 1)} | {(1024, 4, 0)}
