@@ -52,7 +52,7 @@ typedef struct {
 typedef struct lp_desc lp_desc_t;
 
 /* Validates p, picks kernels and sizes the workspace; touches no device.  *out is written only on success.
- * CONV_ESHAPE: vocab out of range, or a workspace of 2^40 bytes or more. */
+ * CONV_ESHAPE: vocab of 2^30 or more. */
 int lp_desc_create(lp_desc_t** out, const lp_params_t* p);
 int lp_desc_destroy(lp_desc_t* d);
 /* Largest workspace any pass of this descriptor needs, in bytes (may be 0). */

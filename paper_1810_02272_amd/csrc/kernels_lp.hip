@@ -24,7 +24,7 @@
 struct lp_desc {
   lp_params_t p;
   float c;          // scale log2(e)
-  int32_t form;     // of the passes that see a whole row: kWave, kBlock, kWide or kLong
+  int32_t form;     // of the passes that see a whole row (Form)
   int32_t splits;   // parts of a row in different workgroups (1: none)
   int32_t seg;      // logits of a part
   size_t ws_bytes;
