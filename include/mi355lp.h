@@ -21,7 +21,8 @@
  * Types and layouts: logits and d_logits in the descriptor's type (fp32, fp16, bf16), rows `stride` elements apart
  * (stride >= vocab where there is more than one row) and dense inside, on the element's own alignment; everything else is dense fp32 or int32:
  *   token int32 [rows]   logp, entropy, d_logp, d_entropy [rows]   stats [rows][4]   top_logp, top_token (int32) [rows][top]
- * stats is what lp_forward leaves for lp_backward (reference exponent, log2 of the sum, entropy, exponent factor).
+ * stats is what lp_forward leaves for lp_backward (reference exponent, log2 of the sum, entropy, exponent factor): of the same logits, by a
+ * descriptor of the same vocab, dtype and scale.  The entropy is NaN if that descriptor's is 0: a gradient through it is then NaN, one without it as usual.
  * Sums, maxima and gradients are held in fp32; a gradient is rounded once, to nearest, as it is stored.
  * d_logits may be logits itself (same base and stride); no other output may overlap an input, the workspace or another output.
  *
@@ -64,7 +65,7 @@ const char* lp_desc_kernel_names(const lp_desc_t* d);
  * NULL together.  top_logp and top_token are NULL exactly when top == 0. */
 int lp_forward(const lp_desc_t* d, const void* logits, int64_t stride, const int32_t* token, float* logp, float* entropy,
                float* stats, float* top_logp, int32_t* top_token, void* ws, size_t ws_bytes, void* hip_stream);
-/* stats from lp_forward on the same logits.  d_entropy is NULL if the descriptor's entropy is 0 and may be NULL otherwise. */
+/* stats from lp_forward on the same logits, as above.  d_entropy is NULL if the descriptor's entropy is 0 and may be NULL otherwise. */
 int lp_backward(const lp_desc_t* d, const void* logits, int64_t stride, const int32_t* token, const float* stats,
                 const float* d_logp, const float* d_entropy, void* d_logits, int64_t d_stride, void* hip_stream);
 /* Both at once, where the derivatives are known before the call; logp and entropy may be NULL (not wanted). */

@@ -113,8 +113,9 @@ __device__ __forceinline__ float log_prob(const RowStat& r, float x, float scale
   return fmaf(r.step, t, -kLn2 * r.log2s);
 }
 
+template <bool ENT>
 __device__ __forceinline__ void put_stats(float* to, const RowStat& r) {
-  store_vec<Elem<MI355_F32>>(to, Elem<MI355_F32>::pack({r.M, r.log2s, r.H, r.c}));
+  store_vec<Elem<MI355_F32>>(to, Elem<MI355_F32>::pack({r.M, r.log2s, ENT ? r.H : NAN, r.c}));  // (without s2, H is not one)
 }
 
 struct GradScale {
@@ -552,7 +553,7 @@ __global__ __launch_bounds__(THREADS == 64 ? 256 : THREADS, THREADS == 64 ? 1 : 
       if (tid == 0) {
         if (a.logp) a.logp[r_] = token >= 0 ? log_prob(st, at_token, a.scale) : 0.f;
         if (ENT && a.entropy) a.entropy[r_] = st.H;
-        if (MODE == kScore && a.stats) put_stats(a.stats + 4 * (int64_t)r_, st);
+        if (MODE == kScore && a.stats) put_stats<ENT>(a.stats + 4 * (int64_t)r_, st);
       }
       if constexpr (MODE == kScore) {
         if (a.top) {
@@ -629,7 +630,7 @@ __global__ __launch_bounds__(256) void lp_join_kernel(LpArgs a) {
   if (threadIdx.x == 0) {
     if (a.logp) a.logp[row] = token >= 0 ? log_prob(st, at_token, a.scale) : 0.f;
     if (ENT && a.entropy) a.entropy[row] = st.H;
-    if (a.stats) put_stats(a.stats + 4 * (int64_t)row, st);
+    if (a.stats) put_stats<ENT>(a.stats + 4 * (int64_t)row, st);
   }
   if (total == 0) return;
   const uint32_t bound = top_bound(sample, a.top);
@@ -681,7 +682,7 @@ __global__ __launch_bounds__(256) void lp_grad_kernel(LpArgs a, int chunks) {
       st = finish(merge_parts(a.parts + (int64_t)r_ * a.splits, a.splits, threadIdx.x & 63, a.c), a.c, a.scale);
     } else {
       const float* const q = a.stats + 4 * (int64_t)r_;
-      st = RowStat{q[0], q[3], q[1], q[2], 0.f};
+      st = RowStat{q[0], q[3], q[1], ENT && a.d_entropy ? q[2] : 0.f, 0.f};
     }
     const float w = token >= 0 ? a.d_logp[r_] : 0.f, u = ENT && a.d_entropy ? a.d_entropy[r_] : 0.f;
     const GradScale g = grad_scale(st, w, u, a.scale);

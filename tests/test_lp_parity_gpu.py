@@ -486,3 +486,25 @@ def test_not_a_number_reaches_masked_tokens(rows, vocab, dtype):
     for t in (logp, logp2, tl):
         assert torch.isnan(t[1:4]).all() and torch.isfinite(t[good]).all()
     assert torch.equal(tt.long(), tokens.top_tokens(x, 4))
+
+
+@pytest.mark.parametrize("rows,vocab", [(40, 300), (3, 40000), (600, 30000)])
+def test_statistics_without_entropy(rows, vocab):
+    """By a descriptor without entropy: gradients through log p alone are right by either kind of descriptor, those through the entropy are NaN,
+    not numbers of something else."""
+    case = (rows, vocab, F32, 0, 1, 1.0, 0, 0)
+    x, _, token, w, u = make(case, seed=4)
+    plain, full = (lib.lp_desc_create(lib.LpParams(rows, vocab, F32, 0, e)) for e in (0, 1))
+    ws = torch.empty(max(lib.lp_desc_workspace_bytes(d) for d in (plain, full)) // 4 + 1, device=DEV)
+    logp, stats, g = torch.empty(rows, device=DEV), torch.empty((rows, 4), device=DEV), torch.empty_like(x)
+    lib.lp_forward(plain, x, token, logp, None, stats, None, None, ws)
+    for d in (plain, full):
+        g.fill_(math.nan)
+        lib.lp_backward(d, x, token, stats, w, None, g)
+        check_gradient(case, x, token, w, None, g)
+    lib.lp_backward(full, x, token, stats, w, u, g)
+    some = (x > -INF).sum(1) > 0  # (a row of nothing but -inf has no gradient through the entropy)
+    assert torch.isnan(g[some]).all()
+    lib.lp_forward(full, x, token, logp, None, stats, None, None, ws)
+    lib.lp_backward(full, x, token, stats, w, u, g)
+    check_gradient(case, x, token, w, u, g)
