@@ -424,6 +424,8 @@ size_t terms_bytes(const q4_desc* d) {
 
 size_t codes_bytes(const q4_desc* d) { return (size_t)d->tiles * d->blocks * 1024; }
 
+size_t packed_bytes(const q4_desc* d) { return codes_bytes(d) + (size_t)d->tiles * d->blocks * kTile * (kBlockK / d->p.group) * 2; }
+
 template <int DTYPE, int MT, int NT, int REGS, bool STREAM = false, bool PREPARED = DTYPE == MI355_F32>
 void launch_group(const q4_desc* d, const Q4Args& a, hipStream_t stream) {
   const int groups = (d->tiles + NT - 1) / NT;
@@ -436,9 +438,11 @@ void launch_group(const q4_desc* d, const Q4Args& a, hipStream_t stream) {
   }
 }
 
-// Codes that the last-level cache (256 MB) does not hold from call to call go around it: 1 x 4096 x 128256 61.9 -> 57.8 us.  (Batches of
-// more than 16 rows are not bound by them.)
-bool streams(const q4_desc* d) { return d->p.m <= 16 && codes_bytes(d) > (size_t)240 << 20; }
+// Codes of weights that the last-level cache (256 MB) does not hold from call to call go around it.  us through it and around it, one row of 4096
+// bf16: weights that it does not hold at the call, as after other layers' work, 60.7 and 56.1 (282 MB packed), 64.1 and 59.0 (254), 50.1
+// and 45.3 (226); the same weights call after call 70.9 and 65.3 (330), 53.9 and 56.1 (282), 46.2 and 58.2 (254), 35.6 and 45.0 (226): from
+// 256 MB on what they lose is less and less, and what they gain is not.  (Batches of more than 16 rows are not bound by the codes.)
+bool streams(const q4_desc* d) { return d->p.m <= 16 && packed_bytes(d) > (size_t)256 << 20; }
 
 // Tiles of a workgroup for up to four rows and many outputs.  4096 x 128256: bf16 2 tiles 58.7 us, 4 65.7; fp32, whose operands are three
 // times as many loads, 95.4 and 67.6.
@@ -550,7 +554,7 @@ int q4_desc_workspace_bytes(const q4_desc_t* d, size_t* bytes) {
 
 int q4_desc_packed_bytes(const q4_desc_t* d, size_t* bytes) {
   if (!d || !bytes) return CONV_EINVAL;
-  *bytes = codes_bytes(d) + (size_t)d->tiles * d->blocks * kTile * (kBlockK / d->p.group) * 2;
+  *bytes = packed_bytes(d);
   return CONV_OK;
 }
 

@@ -290,3 +290,15 @@ def test_lp_row_kernels_of_parts_are_those_that_are_launched():
     assert {k for k in kernels if k[3] == 2} == {(t, 1024, 4, 2, e, 0) for t in (0, 1, 2) for e in (0, 1)}
     teams = {(64, 4), (64, 8), (256, 8), (256, 16), (256, 26), (512, 20)}
     assert {k[1:3] + k[5:] for k in kernels if k[3] < 2} == {(*team, stream) for team in teams for stream in (0, 1)} | {(1024, 4, 0)}
+
+
+@pytest.mark.parametrize("group", [32, 64, 128])
+def test_q4_codes_go_around_the_cache_by_the_packed_size(group):
+    """As the logits and gradients of the other operators do: where there is more than the 256 MB that the last-level cache holds."""
+    seen = set()
+    for o in range(100000, 136000, 512):
+        d = lib.q4_desc_create(lib.Q4Params(1, 4096, o, BF16, group))
+        large = lib.q4_desc_packed_bytes(d) > 1 << 28
+        assert ("stream" in lib.q4_desc_kernel_names(d)) == large, o
+        seen.add(large)
+    assert seen == {False, True}
