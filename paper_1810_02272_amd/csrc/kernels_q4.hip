@@ -42,6 +42,7 @@ typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 constexpr int kTile = 16, kBlockK = 128;
 constexpr int kUnits = 256;  // compute units
 constexpr int64_t kMaxElems = (int64_t)1 << 30;
+constexpr int64_t kMostBlocks = 1 << 22;  // of 256 threads: a launch has fewer than 2^32
 
 struct Q4Args {
   const void* x;
@@ -62,38 +63,38 @@ template <bool WORDS>
 __global__ __launch_bounds__(256) void q4_pack_kernel(const uint8_t* __restrict__ codes, const uint16_t* __restrict__ scales,
                                                       u32x4* __restrict__ to, uint16_t* __restrict__ to_scales, int k, int o, int blocks,
                                                       int64_t vectors, int group) {
-  const int64_t v = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  if (v >= vectors) return;
-  const int lane = (int)(v & 63);
-  const int64_t tb = v >> 6;
-  const int tile = (int)(tb / blocks), block = (int)(tb % blocks);
-  const int row = tile * kTile + (lane & 15), stride = (k + 1) / 2;
-  u32x4 w = {0, 0, 0, 0};
-  if (row < o) {
+  for (int64_t v = (int64_t)blockIdx.x * 256 + threadIdx.x; v < vectors; v += (int64_t)gridDim.x * 256) {
+    const int lane = (int)(v & 63);
+    const int64_t tb = v >> 6;
+    const int tile = (int)(tb / blocks), block = (int)(tb % blocks);
+    const int row = tile * kTile + (lane & 15), stride = (k + 1) / 2;
+    u32x4 w = {0, 0, 0, 0};
+    if (row < o) {
 #pragma unroll
-    for (int d = 0; d < 4; ++d) {
-      const int at = block * kBlockK + 32 * d + 8 * (lane >> 4);
-      if constexpr (WORDS) {
-        if (at < k) w[d] = *reinterpret_cast<const uint32_t*>(codes + (int64_t)row * stride + at / 2);
-        continue;
-      }
+      for (int d = 0; d < 4; ++d) {
+        const int at = block * kBlockK + 32 * d + 8 * (lane >> 4);
+        if constexpr (WORDS) {
+          if (at < k) w[d] = *reinterpret_cast<const uint32_t*>(codes + (int64_t)row * stride + at / 2);
+          continue;
+        }
 #pragma unroll
-      for (int b = 0; b < 4; ++b) {
-        const int i = at + 2 * b;
-        if (i < k) {
-          uint32_t c = codes[(int64_t)row * stride + i / 2];
-          if (i + 1 >= k) c &= 15u;
-          w[d] |= c << (8 * b);
+        for (int b = 0; b < 4; ++b) {
+          const int i = at + 2 * b;
+          if (i < k) {
+            uint32_t c = codes[(int64_t)row * stride + i / 2];
+            if (i + 1 >= k) c &= 15u;
+            w[d] |= c << (8 * b);
+          }
         }
       }
     }
-  }
-  to[v] = w;
-  const int per = kBlockK / group, groups = (k + group - 1) / group;
-  if (lane < 16) {
-    for (int g = 0; g < per; ++g) {
-      const int at = block * per + g;
-      to_scales[(tb * kTile + lane) * per + g] = row < o && at < groups ? scales[(int64_t)row * groups + at] : 0;
+    to[v] = w;
+    const int per = kBlockK / group, groups = (k + group - 1) / group;
+    if (lane < 16) {
+      for (int g = 0; g < per; ++g) {
+        const int at = block * per + g;
+        to_scales[(tb * kTile + lane) * per + g] = row < o && at < groups ? scales[(int64_t)row * groups + at] : 0;
+      }
     }
   }
 }
@@ -180,30 +181,30 @@ __device__ __forceinline__ int place_row(int place) { return (place & 3) * 4 + (
 
 // fp32 x as operands: [tile of 16 rows][32 inputs][term][lane], zeros beyond m and k.  One thread for each lane of the three terms.
 __global__ __launch_bounds__(256) void x_terms_kernel(const float* __restrict__ x, u32x4* __restrict__ to, int m, int k, int steps, int64_t lanes) {
-  const int64_t v = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  if (v >= lanes) return;
-  const int lane = (int)(v & 63);
-  const int64_t ts = v >> 6;
-  const int step = (int)(ts % steps);
-  const int64_t row = ts / steps * 16 + place_row(lane & 15);
-  const int at = 32 * step + 8 * (lane >> 4);
-  float f[8];
-  const float* const p = x + row * k + at;
-  if (row < m && at + 8 <= k) {
-    const u32x4 a = load_vec<Elem<MI355_F32>>(p), b = load_vec<Elem<MI355_F32>>(p + 4);
+  for (int64_t v = (int64_t)blockIdx.x * 256 + threadIdx.x; v < lanes; v += (int64_t)gridDim.x * 256) {
+    const int lane = (int)(v & 63);
+    const int64_t ts = v >> 6;
+    const int step = (int)(ts % steps);
+    const int64_t row = ts / steps * 16 + place_row(lane & 15);
+    const int at = 32 * step + 8 * (lane >> 4);
+    float f[8];
+    const float* const p = x + row * k + at;
+    if (row < m && at + 8 <= k) {
+      const u32x4 a = load_vec<Elem<MI355_F32>>(p), b = load_vec<Elem<MI355_F32>>(p + 4);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      f[i] = Elem<MI355_F32>::get(a, i);
-      f[4 + i] = Elem<MI355_F32>::get(b, i);
+      for (int i = 0; i < 4; ++i) {
+        f[i] = Elem<MI355_F32>::get(a, i);
+        f[4 + i] = Elem<MI355_F32>::get(b, i);
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) f[i] = row < m && at + i < k ? p[i] : 0.f;
     }
-  } else {
+    bf16x8 w[3];
+    load_operand<MI355_F32>(f, w);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) f[i] = row < m && at + i < k ? p[i] : 0.f;
+    for (int t = 0; t < 3; ++t) to[(ts * 3 + t) * 64 + lane] = __builtin_bit_cast(u32x4, w[t]);
   }
-  bf16x8 w[3];
-  load_operand<MI355_F32>(f, w);
-#pragma unroll
-  for (int t = 0; t < 3; ++t) to[(ts * 3 + t) * 64 + lane] = __builtin_bit_cast(u32x4, w[t]);
 }
 
 template <int PER>
@@ -453,7 +454,7 @@ template <int DTYPE>
 int launch_forward(const q4_desc* d, const Q4Args& a, hipStream_t stream) {
   if (d->prepared) {
     const int64_t lanes = (int64_t)(terms_bytes(d) / 48);
-    hipLaunchKernelGGL(x_terms_kernel, dim3((uint32_t)((lanes + 255) / 256)), dim3(256), 0, stream, static_cast<const float*>(a.x), a.terms, a.m, a.k,
+    hipLaunchKernelGGL(x_terms_kernel, dim3((uint32_t)std::min((lanes + 255) / 256, kMostBlocks)), dim3(256), 0, stream, static_cast<const float*>(a.x), a.terms, a.m, a.k,
                        d->blocks * 4, lanes);
     const int e = (int)hipGetLastError();
     if (e) return e;
@@ -564,7 +565,7 @@ int q4_pack(const q4_desc_t* d, const uint8_t* codes, const uint16_t* scales, vo
   if (!d || !codes || !scales || !packed || ((uintptr_t)packed & 15u)) return CONV_EINVAL;
   const int64_t vectors = (int64_t)d->tiles * d->blocks * 64;
   const bool words = d->p.k % 8 == 0 && ((uintptr_t)codes & 3u) == 0;
-  hipLaunchKernelGGL(words ? q4_pack_kernel<true> : q4_pack_kernel<false>, dim3((uint32_t)((vectors + 255) / 256)), dim3(256), 0, (hipStream_t)hip_stream, codes, scales,
+  hipLaunchKernelGGL(words ? q4_pack_kernel<true> : q4_pack_kernel<false>, dim3((uint32_t)std::min((vectors + 255) / 256, kMostBlocks)), dim3(256), 0, (hipStream_t)hip_stream, codes, scales,
                      static_cast<u32x4*>(packed), reinterpret_cast<uint16_t*>(static_cast<char*>(packed) + codes_bytes(d)), d->p.k, d->p.num_output,
                      d->blocks, vectors, d->p.group);
   const int e = (int)hipGetLastError();

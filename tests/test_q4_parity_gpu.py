@@ -213,3 +213,19 @@ def test_large_inputs(dtype, size, scale, group):
     scales = torch.full_like(scales, scale)
     scales[:, 1::2] = -scale / 2
     check(case, x, codes, scales, None, run(case, x, codes, scales, None))
+
+
+def test_as_many_outputs_as_there_may_be():
+    """2^30 - 1 outputs of one input: 2^32 vectors of packed codes (64 GB), more than a launch has threads."""
+    o = (1 << 30) - 1
+    d = lib.q4_desc_create(lib.Q4Params(1, 1, o, BF16, 128, 0, 0))
+    g = torch.Generator(device=DEV).manual_seed(5)
+    codes = torch.randint(16, (o, 1), generator=g, device=DEV, dtype=torch.uint8)
+    scales = torch.ones((o, 1), device=DEV, dtype=BF16)
+    packed = torch.empty(lib.q4_desc_packed_bytes(d), device=DEV, dtype=torch.uint8)
+    lib.q4_pack(d, codes, scales, packed)
+    y = torch.full((1, o), math.nan, device=DEV, dtype=BF16)
+    lib.q4_forward(d, torch.full((1, 1), 2.0, device=DEV, dtype=BF16), packed, None, y)
+    value = 2 * tokens.q4_values(torch.arange(16, device=DEV, dtype=torch.uint8)[:, None], 1)[:, 0].to(BF16)
+    for at in range(0, o, 1 << 26):
+        assert torch.equal(y[0, at:at + (1 << 26)], value[codes[at:at + (1 << 26), 0].int()]), at
