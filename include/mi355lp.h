@@ -21,8 +21,9 @@
  * Types and layouts: logits and d_logits in the descriptor's type (fp32, fp16, bf16), rows `stride` elements apart
  * (stride >= vocab where there is more than one row) and dense inside, on the element's own alignment; everything else is dense fp32 or int32:
  *   token int32 [rows]   logp, entropy, d_logp, d_entropy [rows]   stats [rows][4]   top_logp, top_token (int32) [rows][top]
- * stats is what lp_forward leaves for lp_backward (reference exponent, log2 of the sum, entropy, exponent factor): of the same logits, by a
- * descriptor of the same vocab, dtype and scale.  The entropy is NaN if that descriptor's is 0: a gradient through it is then NaN, one without it as usual.
+ * stats is what lp_forward leaves for lp_backward (reference exponent, log2 of the sum, entropy, exponent factor): of the same logits, by
+ * a descriptor of the same vocab, dtype and scale.  The entropy is NaN if that descriptor's is 0: a gradient through it is then NaN, one
+ * without it as usual.
  * Sums, maxima and gradients are held in fp32; a gradient is rounded once, to nearest, as it is stored.
  * d_logits may be logits itself (same base and stride); no other output may overlap an input, the workspace or another output.
  *

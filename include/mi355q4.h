@@ -6,8 +6,10 @@
  *   z[n][o] = bias[o] + sum_i x[n][i] w[o][i];   y = relu ? max(z, 0) : z
  *   value(c) for c = 0 .. 15:  0 0.5 1 1.5 2 3 4 6  -0 -0.5 -1 -1.5 -2 -3 -4 -6     (one sign, two exponent, one mantissa bit)
  * Products with x are exact and summed in fp32 inside each group, the groups' sums times their scales in fp32; fp32 x takes part with all
- * of its 24 bits, but for those below 2^-133 (of inputs below 2^-110).  One rounding to y's type at the end.  A group's sum is taken before its scale: it stays in
- * fp32's range where |x| <= 2^118, and may be infinite or NaN beyond, whatever the scale.
+ * of its 24 bits, but for those below 2^-133 (of inputs below 2^-110).  One rounding to y's type at the end.  A group's sum is taken
+ * before its scale: it stays in fp32's range where |x| <= 2^118, and may be infinite or NaN beyond, whatever the scale.
+ *
+ * Made for batches of up to 64 rows, which read the weights once.  Larger ones are taken 64 rows at a time.
  *
  * Layouts, dense row-major DEVICE memory:
  *   x [m][k], bias [num_output], y [m][num_output]: the descriptor's type (fp32, fp16, bf16), on the element's own alignment
@@ -17,8 +19,8 @@
  * The packed form depends on k, num_output and group alone: descriptors that agree in these share it.
  * Outputs must not overlap inputs or the workspace.
  *
- * The workspace is 16-byte aligned.  Ownership, execution and errors as in mi355conv.h.  Every call only enqueues kernels and may be captured.  Equal calls
- * give equal bits.  m may be 0: q4_forward is then a no-op.
+ * The workspace is 16-byte aligned.  Ownership, execution and errors as in mi355conv.h.  Every call only enqueues kernels and may be
+ * captured.  Equal calls give equal bits.  m may be 0: q4_forward is then a no-op.
  */
 #ifndef MI355Q4_H
 #define MI355Q4_H

@@ -1,8 +1,10 @@
 // The norm over many tensors and clipping by it (include/mi355gn.h): a pass that sums squares, and one that multiplies.
 //
 // Bound by memory: every gradient is read twice and written once (in place and unclipped: read once).  The factor needs all squares
-// first, so what the second pass reads again comes from memory but for what the last-level cache (256 MB) still holds; it
-// walks the gradients from their end, where that is.
+// first, so what the second pass reads again comes from memory but for what the last-level cache (256 MB) still holds; a launch of
+// it (up to 96 runs of tensors) walks its gradients from their end, where that is.  Several launches go from the first on, as those of
+// the first pass do; what is in the cache is then the last ones', and waits there, as the others' reads and writes go around it.  242
+// tensors of their own memory, 708 MB clipped: 325.5 us, as views of one buffer 314.7 (one state's buffers call after call).
 // The squares are summed in fp64, whose multiply-add runs at fp32's rate on this chip: no square of an fp32 value overflows or
 // vanishes in it.  Those of fp64 values may: the large and the small ones have sums of their own, of squares of scaled values (Squares).
 #include <float.h>
@@ -45,7 +47,7 @@ constexpr int kMostParts = kSumBlocks + kMaxLaunches;
 // Up to this many partial sums each workgroup of the second pass adds them up for itself; beyond, a kernel in between does.
 constexpr int kFewParts = 512;
 // Of gradients that the last-level cache (256 MB) does not hold, the first pass reads around it all but this much at the end,
-// where the second pass begins.
+// where the second pass begins, or which it leaves alone until then.
 constexpr int64_t kCacheBytes = (int64_t)256 << 20, kKeptBytes = (int64_t)192 << 20;
 
 // Tensors of a type that follow each other in memory.

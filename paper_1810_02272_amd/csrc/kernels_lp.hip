@@ -720,9 +720,10 @@ __global__ __launch_bounds__(256) void lp_grad_kernel(LpArgs a, int chunks) {
 //   block8   3000 x 12000 bf16, 20 alternatives 27.4, block16 32.0; 512 threads 47
 //   block16  1000 x 30000 bf16, 20 alternatives 23.5, 512 threads 25.1; training on 3000 x 30000 73.2, 77.7
 //   block26  8000 x 50257 f16 163, 512 threads 185; training on 2000 x 50257 90.0, 93.9
-//   long     training on 4096 x 128256 bf16: 512 threads 453, 1024 with 20 vectors 485, with 7 (most of a row read again) 470
+//   long     training on 4096 x 128256 bf16, through the cache: 512 threads 453, 1024 with 20 vectors 485, with 7 (most of a row read again) 470
 // Where there is at most one row for a compute unit, 1024 threads: 1 x 32000 8.7 us, in parts 11.0; 200 x 30000 trained 9.8, in parts 15.
-// What the long team cannot hold (81920 logits of 16 bits) is read again from the caches.
+// What the long team cannot hold (81920 logits of 16 bits) is read again from the caches.  (Its kernels that score 16-bit rows keep 8 bytes a
+// thread in scratch memory.)
 enum Form { kWave4, kWave8, kSolo, kBlock8, kBlock16, kBlock26, kLong };
 const char* const kFormNames[] = {"wave4", "wave8", "solo", "block8", "block16", "block26", "long"};
 
@@ -779,7 +780,7 @@ int launch_grad(const LpArgs& a, hipStream_t stream) {
 }
 
 // Whether the logits, or they and the gradient, are more than the last-level cache (256 MB) holds: they then go around it, and leave it to
-// what is read a second time.  Training on 4096 x 128256: 455 us through it, 442 with the gradient around it, 419 with both.
+// what is read a second time.  Training on 4096 x 128256: 455 us through it, 442 with the gradient around it, 417 with both.
 bool streams(const lp_desc* d, int blobs) { return (double)d->p.rows * d->p.vocab * dtype_bytes(d->p.dtype) * blobs > (double)(256 << 20); }
 
 // One of the descriptor's six kinds.
