@@ -729,9 +729,13 @@ const char* const kFormNames[] = {"wave4", "wave8", "solo", "block8", "block16",
 
 constexpr int kSoloVecs = 4, kLongVecs = 20;
 
-// Whether three block26 teams on a compute unit finish before two long ones: they take 7/8 of the time for a row where all places are taken,
-// but a last round that is not full costs more.  777 x 50257: block26 32.4 us, long 30.7; 300 rows 20.6, 19.9; 2000 rows trained 90.0, 93.9.
-bool dense(int64_t rows) { return (rows + 767) / 768 * 21 <= (rows + 511) / 512 * 16; }
+// Whether three block26 teams on a compute unit finish before two long ones: they take 5/6 of the time for a row where all places are taken,
+// but a last round that is not full costs more.  us, block26 and long, rows of 50257 fp16 with 20 alternatives, of 36000 bf16 trained, of 24000 fp32
+// trained, the same logits from call to call:
+//    300 rows  21.2 20.6,  18.3 17.8,  16.1 15.7      777 rows  32.6 34.1,  28.7 29.6,  33.2 32.3      2400 rows  71.7 86.7,  70.3 70.7,  84.8 82.1
+//    700 rows  27.3 29.1,  25.1 25.6,  22.8 28.3     1300 rows  42.6 48.5,  48.6 50.1,  56.4 54.5      8000 rows   190  245,   216  214,   273  262
+// Of 132 calls of 257 to 8000 rows the slower one is taken in 19, by 7 % at most.
+bool dense(int64_t rows) { return (rows + 767) / 768 * 20 <= (rows + 511) / 512 * 16; }
 constexpr int kUnits = 256;  // compute units
 constexpr int kMostTeams = 1 << 20;
 

@@ -302,3 +302,10 @@ def test_q4_codes_go_around_the_cache_by_the_packed_size(group):
         assert ("stream" in lib.q4_desc_kernel_names(d)) == large, o
         seen.add(large)
     assert seen == {False, True}
+
+
+def test_lp_long_rows_take_the_denser_team_from_a_thousand_rows_on():
+    """Three teams on a compute unit: measured faster, or as fast within 7 %, for any number of rows beyond 1024 (at 2400 they were not taken)."""
+    team = lambda rows: re.search(r"forward=lp_row\[(\w+)", lib.lp_desc_kernel_names(lib.lp_desc_create(lib.LpParams(rows, 50257, BF16, 20, 1)))).group(1)
+    assert {team(rows) for rows in range(1025, 9000, 7)} == {"block26"}
+    assert team(512) == "long" and team(768) == "block26" and team(777) == "long"
