@@ -292,3 +292,15 @@ def test_every_type_over_several_launches(ratio):
         assert bool(((o.double() - w).abs() <= w.abs() * steps + small).all()), (o.dtype, o.numel())
     lib.gn_clip(d, grads, limit, None, norm, ws)  # in place
     assert all(torch.equal(a, b) for a, b in zip(grads, outs))
+
+
+@pytest.mark.parametrize("size", [1e-300, 1e-200, 1e-30, 1.0, 1e200])
+def test_fp64_value_among_zeros(size):
+    """One value, wherever it stands, among zeros of both signs: the norm is its size."""
+    n = 2 * 2048 + 3  # two chunks and an odd end
+    for at in (0, 1, 2, 511, 2047, 2048, 4095, n - 3, n - 2, n - 1):
+        t = torch.zeros(n, device=DEV, dtype=F64)
+        t[1::2] = -0.0
+        t[at] = -size
+        check_scaled([t], size / 4)
+        check_scaled([t], size * 4)
