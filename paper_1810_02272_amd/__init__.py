@@ -1,5 +1,5 @@
 """MI355X-native Caffe-semantics convolution and InnerProduct layers, policy-gradient loss kernels and the operators of a policy over
-tokens (log probabilities, clipping by the gradient norm, 4-bit weights): thin Python binding over libmi355conv.so.
+tokens (drawing them, log probabilities, clipping by the gradient norm, 4-bit weights, layers in 8-bit integers): thin Python binding over libmi355conv.so.
 
 The package holds the HIP sources (``csrc/``), the build step (``build.py``), the ctypes binding
 (``binding.py``: same names as the C entry points, argument marshalling only) and the seeded
@@ -75,4 +75,25 @@ from .q4_binding import (  # noqa: F401
     q4_desc_workspace_bytes,
     q4_forward,
     q4_pack,
+)
+from .sm_binding import (  # noqa: F401
+    SmParams,
+    sm_desc_create,
+    sm_desc_destroy,
+    sm_desc_kernel_names,
+    sm_desc_workspace_bytes,
+    sm_sample,
+)
+from .i8_binding import (  # noqa: F401
+    I8Params,
+    i8_backward_data,
+    i8_backward_filter,
+    i8_desc_create,
+    i8_desc_destroy,
+    i8_desc_kernel_names,
+    i8_desc_row_bytes,
+    i8_desc_workspace_bytes,
+    i8_forward,
+    i8_pack,
+    i8_quantise,
 )

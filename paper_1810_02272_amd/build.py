@@ -13,8 +13,8 @@ MARSHAL = os.path.join(_HERE, "_marshal.so")  # Python extension over LIB (csrc/
 SOURCES = ["api.cpp", "api_ip.cpp", "kernels_corr.hip", "kernels_corr_patch.hip", "kernels_corr_thin.hip",
            "kernels_small.hip", "kernels_corr_split.hip", "kernels_wgrad_split.hip", "kernels_wgrad.hip", "kernels_bias.hip",
            "kernels_ip.hip", "kernels_pg.hip", "kernels_f64.hip", "kernels_direct.hip", "static_workspace.hip",
-           "kernels_lp.hip", "kernels_gn.hip", "kernels_q4.hip"]
-HEADERS = ["internal.h", "device_utils.h", "corr_epilogue.h", "split_bf16.h", "split_f16.h", "elements.h", "wave_ops.h"]
+           "kernels_lp.hip", "kernels_gn.hip", "kernels_q4.hip", "kernels_sm.hip", "kernels_i8.hip"]
+HEADERS = ["internal.h", "device_utils.h", "corr_epilogue.h", "split_bf16.h", "split_f16.h", "elements.h", "wave_ops.h", "rows.h"]
 
 HIPCC_FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared",
@@ -55,7 +55,7 @@ def is_stale() -> bool:
     t = min(os.path.getmtime(LIB), os.path.getmtime(MARSHAL))
     deps = [os.path.join(CSRC, s) for s in SOURCES + HEADERS + ["marshal.cpp"]] + [
         os.path.join(_ROOT, "include", h) for h in ("mi355conv.h", "mi355ip.h", "mi355pg.h", "mi355dtype.h", "mi355lp.h", "mi355gn.h",
-                                                         "mi355q4.h")]
+                                                         "mi355q4.h", "mi355sm.h", "mi355i8.h")]
     return any(os.path.getmtime(d) > t for d in deps)
 
 

@@ -1,0 +1,835 @@
+// The InnerProduct layer in 8-bit integers, and its gradients from activations kept in 8 bits (include/mi355i8.h).
+//
+// Forward: sum_i c[n][i] v[o][i] by the integer matrix instructions, exact in 32 bits in any order; then s_n t_o, bias, ReLU, one rounding.
+// Gradients: the scale of a row is on the side of dz in both,
+//   dw[o][i] = sum_n (dz[n][o] s_n) c[n][i]      dx[n][i] = sum_o (dz[n][o] t_o) v[o][i]
+// so the codes go into the bf16 matrix instructions as they are (whole numbers up to 127 are bf16's) and dz times the scale as terms that make it
+// up: a bf16 dz and a scale of 8 bits have products of 16, two terms; others are rounded to fp32's 24, three terms.
+#include <hip/hip_runtime.h>
+#include <stdio.h>
+#include <string.h>
+
+#include <algorithm>
+#include <new>
+#include <type_traits>
+
+#include "device_utils.h"
+#include "elements.h"
+#include "internal.h"
+#include "mi355i8.h"
+#include "wave_ops.h"
+
+struct i8_desc {
+  i8_params_t p;
+  int64_t row;             // bytes of a row of codes
+  int32_t fwd;             // FwdForm
+  int32_t filter_tile, filter_splits, filter_per;  // backward filter: tile (rows and columns), workgroups that share a sum, steps of each
+  int32_t data_tile, data_splits, data_per;        // backward data
+  int32_t waves;           // of the forward pass by rows
+  size_t ws_bytes;
+  char names[192];
+};
+
+namespace mi355conv {
+
+namespace {
+
+typedef int i32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+
+constexpr int kRowUnit = 128;          // bytes that a row of codes is a multiple of
+constexpr int kMostInputs = 133120;    // 127^2 times this fits 32 bits
+constexpr int kUnits = 256;            // compute units
+constexpr int64_t kMaxElems = (int64_t)1 << 30;
+
+enum FwdForm { kRows, kTile128, kTile256 };
+
+// ---- rows to 8 bits ----
+
+// The smallest number of 8 significant bits whose 127-fold reaches most, at least 2^-126; NaN where most is not finite.  The quotient is
+// rounded to nearest: cut to 8 bits it is that number or the one below (127 times 8 bits are exact).
+__device__ __forceinline__ float scale_for(float most) {
+  if (!(most < INFINITY)) return NAN;
+  const uint32_t down = __builtin_bit_cast(uint32_t, most / 127.f) & 0xffff0000u;
+  const float lo = __builtin_bit_cast(float, down);
+  return fmaxf(127.f * lo >= most ? lo : __builtin_bit_cast(float, down + 0x10000u), 0x1p-126f);
+}
+
+// The whole number nearest x / s, the even one of two.  x times the rounded reciprocal is within 2^-15 of the quotient; x - q s is exact in fp32
+// (a multiple of the smaller one's last bit, not more than s), and says which side of a half x is on.
+__device__ __forceinline__ int code_of(float x, float s, float inverse) {
+  float q = rintf(x * inverse);
+  const float left = fmaf(-q, s, x), twice = 2.f * fabsf(left);
+  if (twice > s || (twice == s && ((int)q & 1))) q += copysignf(1.f, left);
+  return (int)q;
+}
+
+// THREADS threads for a row: its largest magnitude, then the codes, from registers for up to NV vectors a thread, read again beyond.  Bound by
+// memory.  THREADS 64: a wave for each row, four in a workgroup.
+template <int DTYPE, int THREADS, int NV>
+__global__ __launch_bounds__(256) void i8_quantise_kernel(const void* __restrict__ x, int8_t* __restrict__ codes, float* __restrict__ scales, int rows,
+                                                          int k, int64_t row_bytes) {
+  typedef Elem<DTYPE> E;
+  typedef typename E::T T;
+  constexpr int VEC = E::VEC;
+  __shared__ uint32_t most_of[4];
+  const int tid = THREADS == 64 ? threadIdx.x & 63 : threadIdx.x, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int step = THREADS == 64 ? gridDim.x * 4 : gridDim.x;
+  const int vectors = (int)(row_bytes / VEC);
+  for (int64_t r = THREADS == 64 ? (int64_t)blockIdx.x * 4 + wave : blockIdx.x; r < rows; r += step) {
+    const T* const from = static_cast<const T*>(x) + r * k;
+    auto load = [&](int v) {
+      const int at = v * VEC;
+      if (at + VEC <= k) return load_vec<E>(from + at);
+      float f[VEC];
+#pragma unroll
+      for (int i = 0; i < VEC; ++i) f[i] = at + i < k ? E::to_float(from[at + i]) : 0.f;
+      return E::pack(f);
+    };
+    uint32_t most = 0;  // as the bits of a magnitude: NaN is above infinity
+    auto look = [&](const u32x4& vec) {
+#pragma unroll
+      for (int i = 0; i < VEC; ++i) most = max(most, __builtin_bit_cast(uint32_t, E::get(vec, i)) & 0x7fffffffu);
+    };
+    u32x4 held[NV];
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+      held[j] = u32x4{0, 0, 0, 0};
+      if (j * THREADS + tid < vectors) held[j] = load(j * THREADS + tid);
+    }
+#pragma unroll
+    for (int j = 0; j < NV; ++j) look(held[j]);
+    for (int v = NV * THREADS + tid; v < vectors; v += THREADS) look(load(v));
+    most = (uint32_t)wave_reduce((int)most, 0, [](int a, int b) { return max(a, b); });
+    if constexpr (THREADS > 64) {
+      __syncthreads();
+      if (lane == 0) most_of[wave] = most;
+      __syncthreads();
+      most = max(max(most_of[0], most_of[1]), max(most_of[2], most_of[3]));
+    }
+    const float s = scale_for(__builtin_bit_cast(float, most)), inverse = 1.f / s;
+    const bool finite = s < INFINITY;
+    if (tid == 0) scales[r] = s;
+    int8_t* const to = codes + r * row_bytes;
+    auto put = [&](const u32x4& vec, int v) {
+      uint32_t w[VEC / 4];
+#pragma unroll
+      for (int i = 0; i < VEC / 4; ++i) {
+        uint32_t word = 0;
+#pragma unroll
+        for (int b = 0; b < 4; ++b) word |= ((uint32_t)code_of(E::get(vec, 4 * i + b), s, inverse) & 255u) << (8 * b);
+        w[i] = finite ? word : 0u;
+      }
+      if constexpr (VEC == 8)
+        *reinterpret_cast<uint2*>(to + (int64_t)v * 8) = make_uint2(w[0], w[1]);
+      else
+        *reinterpret_cast<uint32_t*>(to + (int64_t)v * 4) = w[0];
+    };
+#pragma unroll
+    for (int j = 0; j < NV; ++j)
+      if (j * THREADS + tid < vectors) put(held[j], j * THREADS + tid);
+    for (int v = NV * THREADS + tid; v < vectors; v += THREADS) put(load(v), v);
+  }
+}
+
+template <int DTYPE>
+int launch_quantise(const void* x, int8_t* codes, float* scales, int rows, int k, int64_t row, hipStream_t stream) {
+  const int64_t vectors = row / Elem<DTYPE>::VEC;
+  if (vectors <= 64 * 4)
+    hipLaunchKernelGGL((i8_quantise_kernel<DTYPE, 64, 4>), dim3((uint32_t)(((int64_t)rows + 3) / 4)), dim3(256), 0, stream, x, codes, scales, rows, k, row);
+  else
+    hipLaunchKernelGGL((i8_quantise_kernel<DTYPE, 256, 4>), dim3(std::min(rows, 1 << 22)), dim3(256), 0, stream, x, codes, scales, rows, k, row);
+  return (int)hipGetLastError();
+}
+
+int quantise(const i8_desc* d, const void* x, int8_t* codes, float* scales, int rows, hipStream_t stream) {
+  switch (d->p.dtype) {
+    case MI355_F32: return launch_quantise<MI355_F32>(x, codes, scales, rows, d->p.k, d->row, stream);
+    case MI355_F16: return launch_quantise<MI355_F16>(x, codes, scales, rows, d->p.k, d->row, stream);
+    default: return launch_quantise<MI355_BF16>(x, codes, scales, rows, d->p.k, d->row, stream);
+  }
+}
+
+// ---- forward ----
+
+struct FwdArgs {
+  const int8_t *codes, *w_codes;
+  const float *scale, *w_scale;
+  const void* bias;
+  void* y;
+  int64_t row;
+  int32_t m, o, relu;
+};
+
+// One result: the scales one after the other, as their product may leave fp32 where the result does not.
+__device__ __forceinline__ float finish(int sum, float s, float t, float bias, int relu) {
+  const float z = fmaf((float)sum * s, t, bias);
+  return relu ? (z > 0.f ? z : 0.f) : z;
+}
+
+// 16 MT rows by 16 outputs in a workgroup, whose waves take the inputs in turn, 128 at a time, and add up through shared memory: nothing is used by two
+// waves, and operands come from memory as the instructions take them, 16 inputs of a row or an output a lane.
+template <int DTYPE, int MT>
+__global__ __launch_bounds__(1024) void i8_rows_kernel(FwdArgs a) {
+  typedef Elem<DTYPE> E;
+  extern __shared__ int parts[];  // [waves][MT * 256]
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), waves = blockDim.x >> 6;
+  const int o0 = blockIdx.x * 16, blocks = (int)(a.row / kRowUnit);
+  const int8_t* const w = a.w_codes + (int64_t)min(o0 + (lane & 15), a.o - 1) * a.row + 16 * (lane >> 4);
+  for (int m0 = blockIdx.y * 16 * MT; m0 < a.m; m0 += gridDim.y * 16 * MT) {
+    const int8_t* x[MT];
+#pragma unroll
+    for (int t = 0; t < MT; ++t) x[t] = a.codes + (int64_t)min(m0 + 16 * t + (lane & 15), a.m - 1) * a.row + 16 * (lane >> 4);
+    i32x4 acc[MT] = {};
+    for (int b = wave; b < blocks; b += waves) {
+      i32x4 wv[2], xv[MT][2];
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        wv[h] = *reinterpret_cast<const i32x4*>(w + b * kRowUnit + 64 * h);
+#pragma unroll
+        for (int t = 0; t < MT; ++t) xv[t][h] = *reinterpret_cast<const i32x4*>(x[t] + b * kRowUnit + 64 * h);
+      }
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int t = 0; t < MT; ++t) acc[t] = __builtin_amdgcn_mfma_i32_16x16x64_i8(wv[h], xv[t][h], acc[t], 0, 0, 0);
+    }
+    __syncthreads();
+#pragma unroll
+    for (int t = 0; t < MT; ++t)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) parts[(wave * MT + t) * 256 + r * 64 + lane] = acc[t][r];  // output 4 (lane / 16) + r, row lane % 16
+    __syncthreads();
+    for (int i = threadIdx.x; i < MT * 256; i += blockDim.x) {
+      // (consecutive threads: consecutive outputs of a row)
+      const int t = i >> 8, n = m0 + 16 * t + (i >> 4 & 15), out = o0 + (i & 15);
+      if (n >= a.m || out >= a.o) continue;
+      const int at = t * 256 + (i & 3) * 64 + ((i & 15) >> 2) * 16 + (i >> 4 & 15);
+      int sum = 0;
+      for (int p = 0; p < waves; ++p) sum += parts[p * MT * 256 + at];
+      const float bias = a.bias ? E::to_float(static_cast<const typename E::T*>(a.bias)[out]) : 0.f;
+      static_cast<typename E::T*>(a.y)[(int64_t)n * a.o + out] = E::from_float(finish(sum, a.scale[n], a.w_scale[out], bias, a.relu));
+    }
+  }
+}
+
+typedef const __attribute__((address_space(1))) uint32_t* GlobalPtr;
+typedef __attribute__((address_space(3))) uint32_t* LdsPtr;
+
+template <class E>
+__device__ __forceinline__ void store_four(typename E::T* at, const float (&v)[4]) {
+  if constexpr (E::VEC == 4) {
+    store_vec<E>(at, E::pack(v));
+  } else {
+    struct __attribute__((packed, aligned(2))) Four {
+      u32x2 v;
+    };
+    const u32x4 w = E::pack({v[0], v[1], v[2], v[3], 0.f, 0.f, 0.f, 0.f});
+    reinterpret_cast<Four*>(at)->v = u32x2{w[0], w[1]};
+  }
+}
+
+// Tiles in the order in which the compute units of an XCD, which share an L2, take them: eight rows of tiles by all columns.
+__device__ __forceinline__ void tile_place(int tiles_m, int tiles_n, int& tm, int& tn) {
+  const int id = (int)xcd_contiguous_block_id(), band = 8 * tiles_n, first = id / band * 8, high = min(8, tiles_m - first);
+  tm = first + id % band % high;
+  tn = id % band / high;
+}
+
+// Of 64 neighbouring columns, the one that stands at place p of shared memory: lane l of the instructions then holds columns 4 l .. 4 l + 3 in four of
+// its tiles, and stores them together.
+__device__ __forceinline__ int column_at(int p) { return (p & ~63) + 4 * (p & 15) + (p >> 4 & 3); }
+
+// WM x WN waves, each 64 rows of x by 16 NT outputs.  128 inputs at a time go straight into shared memory, one step ahead, as rows of 8 pieces of 16
+// bytes whose order is turned from row to row, so that neither side meets a bank twice.
+template <int DTYPE, int WM, int WN, int NT>
+__global__ __launch_bounds__(WM * WN * 64, 2) void i8_tile_kernel(FwdArgs a) {
+  typedef Elem<DTYPE> E;
+  constexpr int THREADS = WM * WN * 64, BM = WM * 64, BN = WN * NT * 16, ROWS = BM + BN, LOADS = ROWS * 8 / THREADS;
+  __shared__ __attribute__((aligned(16))) int8_t lds[2][ROWS * kRowUnit];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), wm = wave / WN, wn = wave % WN;
+  int tm, tn;
+  tile_place((a.m + BM - 1) / BM, (a.o + BN - 1) / BN, tm, tn);
+  const int m0 = tm * BM, o0 = tn * BN, steps = (int)(a.row / kRowUnit);
+  const int8_t* from[LOADS];
+#pragma unroll
+  for (int j = 0; j < LOADS; ++j) {
+    const int at = j * THREADS + (int)threadIdx.x, r = at >> 3, piece = (at & 7) ^ (r & 7);
+    from[j] = (r < BM ? a.codes + (int64_t)min(m0 + r, a.m - 1) * a.row : a.w_codes + (int64_t)min(o0 + column_at(r - BM), a.o - 1) * a.row) + 16 * piece;
+  }
+  auto load = [&](int step, int buffer) {
+#pragma unroll
+    for (int j = 0; j < LOADS; ++j)
+      __builtin_amdgcn_global_load_lds((GlobalPtr)(from[j] + (int64_t)step * kRowUnit), (LdsPtr)&lds[buffer][(j * THREADS + wave * 64) * 16], 16, 0, 0);
+  };
+  i32x4 acc[4][NT] = {};
+  load(0, 0);
+  for (int s = 0; s < steps; ++s) {
+    __builtin_amdgcn_s_waitcnt(0x0F70);  // vmcnt(0): this wave's pieces are in shared memory
+    __syncthreads();                     // everybody's are, and nobody reads the other buffer any more
+    if (s + 1 < steps) load(s + 1, (s + 1) & 1);
+    const int8_t* const base = lds[s & 1];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      i32x4 x[4], w[NT];
+      const int piece = 4 * h + (lane >> 4);
+#pragma unroll
+      for (int t = 0; t < 4; ++t) x[t] = *reinterpret_cast<const i32x4*>(base + (wm * 64 + t * 16 + (lane & 15)) * kRowUnit + 16 * (piece ^ (lane & 7)));
+#pragma unroll
+      for (int t = 0; t < NT; ++t)
+        w[t] = *reinterpret_cast<const i32x4*>(base + (BM + wn * NT * 16 + t * 16 + (lane & 15)) * kRowUnit + 16 * (piece ^ (lane & 7)));
+#pragma unroll
+      for (int t = 0; t < 4; ++t)
+#pragma unroll
+        for (int u = 0; u < NT; ++u) acc[t][u] = __builtin_amdgcn_mfma_i32_16x16x64_i8(x[t], w[u], acc[t][u], 0, 0, 0);
+    }
+  }
+#pragma unroll
+  for (int g = 0; g < NT / 4; ++g) {
+    const int out = o0 + wn * NT * 16 + g * 64 + 4 * (lane & 15);
+    if (out >= a.o) continue;
+    float t[4], bias[4];
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const int at = min(out + q, a.o - 1);
+      t[q] = a.w_scale[at];
+      bias[q] = a.bias ? E::to_float(static_cast<const typename E::T*>(a.bias)[at]) : 0.f;
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const int n = m0 + wm * 64 + i * 16 + 4 * (lane >> 4) + r;
+        if (n >= a.m) continue;
+        const float s = a.scale[n];
+        float v[4];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) v[q] = finish(acc[i][4 * g + q][r], s, t[q], bias[q], a.relu);
+        typename E::T* const to = static_cast<typename E::T*>(a.y) + (int64_t)n * a.o + out;
+        if (out + 4 <= a.o) {
+          store_four<E>(to, v);
+        } else {
+          for (int q = 0; q < a.o - out; ++q) to[q] = E::from_float(v[q]);
+        }
+      }
+  }
+}
+
+template <int DTYPE>
+int launch_forward(const i8_desc* d, const FwdArgs& a, hipStream_t stream) {
+  const int m = d->p.m, o = d->p.num_output;
+  if (d->fwd == kTile256) {
+    hipLaunchKernelGGL((i8_tile_kernel<DTYPE, 4, 2, 8>), dim3((m + 255) / 256 * ((o + 255) / 256)), dim3(512), 0, stream, a);
+  } else if (d->fwd == kTile128) {
+    hipLaunchKernelGGL((i8_tile_kernel<DTYPE, 2, 2, 4>), dim3((m + 127) / 128 * ((o + 127) / 128)), dim3(256), 0, stream, a);
+  } else {
+    const int mt = std::min(4, (m + 15) / 16);
+    const dim3 grid((o + 15) / 16, std::min((m + 16 * mt - 1) / (16 * mt), 65535)), block(64 * d->waves);
+    const size_t lds = (size_t)d->waves * mt * 1024;  // at most 64 KB
+    switch (mt) {
+      case 1: hipLaunchKernelGGL((i8_rows_kernel<DTYPE, 1>), grid, block, lds, stream, a); break;
+      case 2: hipLaunchKernelGGL((i8_rows_kernel<DTYPE, 2>), grid, block, lds, stream, a); break;
+      case 3: hipLaunchKernelGGL((i8_rows_kernel<DTYPE, 3>), grid, block, lds, stream, a); break;
+      default: hipLaunchKernelGGL((i8_rows_kernel<DTYPE, 4>), grid, block, lds, stream, a);
+    }
+  }
+  return (int)hipGetLastError();
+}
+
+// ---- gradients ----
+
+struct BwdArgs {
+  const int8_t* codes;  // [reduction][row]
+  const float* scale;   // [reduction]
+  const void* dz;       // [n][o]
+  void* out;            // filter: dw; data: dx
+  float* db;            // filter, may be null
+  float* parts;         // splits > 1: [splits][rows][k], then [splits][o] of db
+  float* db_parts;
+  int64_t row;
+  int32_t n, o, k;
+  int32_t per;          // steps of a split
+  float beta;
+};
+
+constexpr int kStep = 32;  // terms of the sums that a step takes
+
+// Values as bf16 terms, two at a time: the rounded value, what is left of it rounded, and so on.
+template <int TERMS>
+__device__ __forceinline__ void pair_terms(float a, float b, uint32_t (&w)[TERMS]) {
+  typedef __bf16 Pair __attribute__((ext_vector_type(2)));
+#pragma unroll
+  for (int t = 0; t < TERMS; ++t) {
+    w[t] = __builtin_bit_cast(uint32_t, Pair{(__bf16)a, (__bf16)b});
+    if (t + 1 < TERMS) {
+      a -= __builtin_bit_cast(float, w[t] << 16);
+      b -= __builtin_bit_cast(float, w[t] & 0xffff0000u);
+    }
+  }
+}
+
+// TILE rows of the result (filter: outputs, data: rows of x) by TILE inputs.  Both factors are made into bf16 operands on the way from memory to
+// shared memory, where the 8 terms of the sum that a lane of the matrix instructions takes lie together: a thread takes 8 terms of two
+// neighbouring rows or columns, so that turning them costs nothing beside the conversion.  The next step's values are on their way
+// in registers while the instructions work on this one's.
+// Waves of 64 rows by 16 NT inputs.
+template <int DTYPE, bool FILTER, int TILE>
+__global__ __launch_bounds__(TILE == 256 ? 512 : 256, 2) void i8_gradient_kernel(BwdArgs a) {
+  typedef Elem<DTYPE> E;
+  typedef typename E::T T;
+  constexpr int THREADS = TILE == 256 ? 512 : 256, WN = 2, NT = TILE / (16 * WN), TERMS = DTYPE == MI355_BF16 ? 2 : 3;
+  // pieces of 16 bytes: [term][group of 8 terms of the sum][row], and the same of the codes; what is added keeps the threads that write on banks of
+  // their own
+  constexpr int A_GROUP = TILE + 4, B_GROUP = TILE + TILE / 8, A_TERM = 4 * A_GROUP, BUFFER = TERMS * A_TERM + 4 * B_GROUP;
+  __shared__ __attribute__((aligned(16))) u32x4 lds[2][BUFFER];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), wm = wave / WN, wn = wave % WN;
+  const int rows = FILTER ? a.o : a.n, depth = FILTER ? a.n : a.o;
+  int tm, tn;
+  tile_place((rows + TILE - 1) / TILE, (a.k + TILE - 1) / TILE, tm, tn);
+  const int r0 = tm * TILE, i0 = tn * TILE;
+  const int first = blockIdx.y * a.per, steps = min(a.per, (depth + kStep - 1) / kStep - first);
+
+  // codes: inputs 2 p, 2 p + 1 of group g; filter: dz of outputs 2 p, 2 p + 1 the same way
+  const int g = __builtin_amdgcn_readfirstlane(tid / (TILE / 2)), p = tid % (TILE / 2);
+  const int col = (int)min((int64_t)i0 + 2 * p, a.row - 2);
+  const bool inside = r0 + TILE <= rows;
+  const bool sum_bias = FILTER && a.db && tn == 0;
+  // data: 8 terms of rows (tid / 4) and on, THREADS / 4 apart
+  constexpr int DATA_ROWS = FILTER ? 1 : TILE * 4 / THREADS;
+  typedef typename std::conditional<DTYPE == MI355_F32, u32x2, uint32_t>::type Two;
+  Two za[8];                    // filter
+  u32x4 zd[DATA_ROWS][DTYPE == MI355_F32 ? 2 : 1];  // data
+  float s[8];
+  uint16_t c[8];
+  float bias[2] = {0.f, 0.f};
+
+  auto load = [&](int step) {
+    const int d0 = (first + step) * kStep + 8 * g;
+    const int8_t* const at = a.codes + (int64_t)d0 * a.row + col;
+    if (d0 + 8 <= depth) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) c[j] = *reinterpret_cast<const uint16_t*>(at + j * a.row);
+    } else {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) c[j] = *reinterpret_cast<const uint16_t*>(a.codes + (int64_t)min(d0 + j, depth - 1) * a.row + col);
+    }
+    if constexpr (FILTER) {
+      const T* const z = static_cast<const T*>(a.dz);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const int n = min(d0 + j, depth - 1);
+        s[j] = a.scale[n];
+        if (inside) {
+          struct __attribute__((packed, aligned(sizeof(T)))) Mem {
+            Two v;
+          };
+          za[j] = reinterpret_cast<const Mem*>(z + (int64_t)n * a.o + r0 + 2 * p)->v;
+        } else {
+          const T* const row = z + (int64_t)n * a.o;
+          const T lo = row[min(r0 + 2 * p, a.o - 1)], hi = row[min(r0 + 2 * p + 1, a.o - 1)];
+          if constexpr (DTYPE == MI355_F32)
+            za[j] = u32x2{__builtin_bit_cast(uint32_t, lo), __builtin_bit_cast(uint32_t, hi)};
+          else
+            za[j] = (uint32_t)__builtin_bit_cast(uint16_t, lo) | (uint32_t)__builtin_bit_cast(uint16_t, hi) << 16;
+        }
+      }
+      if (d0 + 8 > depth) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+          if (d0 + j >= depth) {
+            za[j] = Two{};
+            s[j] = 0.f;
+          }
+      }
+    } else {
+      const int at_o = (first + step) * kStep + 8 * (tid & 3);
+      if (at_o + 8 <= depth) {
+        const u32x4 s0 = load_vec<Elem<MI355_F32>>(a.scale + at_o), s1 = load_vec<Elem<MI355_F32>>(a.scale + at_o + 4);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) s[j] = Elem<MI355_F32>::get(j < 4 ? s0 : s1, j & 3);
+      } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) s[j] = at_o + j < depth ? a.scale[at_o + j] : 0.f;
+      }
+#pragma unroll
+      for (int i = 0; i < DATA_ROWS; ++i) {
+        const T* const z = static_cast<const T*>(a.dz) + (int64_t)min(r0 + tid / 4 + i * (THREADS / 4), rows - 1) * a.o;
+        if (at_o + 8 <= depth) {
+          zd[i][0] = load_vec<E>(z + at_o);
+          if constexpr (DTYPE == MI355_F32) zd[i][1] = load_vec<E>(z + at_o + 4);
+        } else {
+          float f[8];
+#pragma unroll
+          for (int j = 0; j < 8; ++j) f[j] = at_o + j < depth ? E::to_float(z[at_o + j]) : 0.f;
+          if constexpr (DTYPE == MI355_F32) {
+            zd[i][0] = E::pack({f[0], f[1], f[2], f[3]});
+            zd[i][1] = E::pack({f[4], f[5], f[6], f[7]});
+          } else {
+            zd[i][0] = E::pack(f);
+          }
+        }
+      }
+    }
+  };
+
+  auto put = [&](int buffer) {
+    u32x4* const A = lds[buffer];
+    u32x4* const B = A + TERMS * A_TERM;
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      u32x4 w;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        uint32_t two[1];
+        pair_terms<1>((float)(int8_t)(c[2 * j] >> 8 * e), (float)(int8_t)(c[2 * j + 1] >> 8 * e), two);
+        w[j] = two[0];
+      }
+      const int i = 2 * p + e, place = (i & ~63) + (i & 3) * 16 + (i >> 2 & 15);  // column_at(place) = i
+      B[g * B_GROUP + place + 2 * (place >> 4)] = w;
+    }
+    if constexpr (FILTER) {
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        float v[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          if constexpr (DTYPE == MI355_F32)
+            v[j] = E::get(u32x4{za[j][0], za[j][1], 0, 0}, e);
+          else
+            v[j] = E::get(u32x4{za[j], 0, 0, 0}, e);
+        }
+        if (sum_bias) {
+#pragma unroll
+          for (int j = 0; j < 8; ++j) bias[e] += v[j];
+        }
+        u32x4 w[TERMS];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          uint32_t two[TERMS];
+          pair_terms<TERMS>(v[2 * j] * s[2 * j], v[2 * j + 1] * s[2 * j + 1], two);
+#pragma unroll
+          for (int t = 0; t < TERMS; ++t) w[t][j] = two[t];
+        }
+#pragma unroll
+        for (int t = 0; t < TERMS; ++t) A[t * A_TERM + g * A_GROUP + 2 * p + e] = w[t];
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < DATA_ROWS; ++i) {
+        u32x4 w[TERMS];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          uint32_t two[TERMS];
+          constexpr int PER = E::VEC;
+          pair_terms<TERMS>(E::get(zd[i][2 * j / PER], 2 * j % PER) * s[2 * j], E::get(zd[i][2 * j / PER], 2 * j % PER + 1) * s[2 * j + 1], two);
+#pragma unroll
+          for (int t = 0; t < TERMS; ++t) w[t][j] = two[t];
+        }
+#pragma unroll
+        for (int t = 0; t < TERMS; ++t) A[t * A_TERM + (tid & 3) * A_GROUP + tid / 4 + i * (THREADS / 4)] = w[t];
+      }
+    }
+  };
+
+  f32x4 acc[4][NT] = {};
+  if (steps > 0) {
+    load(0);
+    put(0);
+  }
+  __syncthreads();
+  for (int step = 0; step < steps; ++step) {
+    const bool more = step + 1 < steps;
+    if (more) load(step + 1);
+    const u32x4* const A = lds[step & 1] + (lane >> 4) * A_GROUP + wm * 64 + (lane & 15);
+    const u32x4* const B = lds[step & 1] + TERMS * A_TERM + (lane >> 4) * B_GROUP + wn * NT * 18 + (lane & 15);
+    bf16x8 w[NT];
+#pragma unroll
+    for (int u = 0; u < NT; ++u) w[u] = __builtin_bit_cast(bf16x8, B[u * 18]);
+#pragma unroll
+    for (int t = 0; t < TERMS; ++t) {
+      bf16x8 x[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) x[i] = __builtin_bit_cast(bf16x8, A[t * A_TERM + 16 * i]);
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int u = 0; u < NT; ++u) acc[i][u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x[i], w[u], acc[i][u], 0, 0, 0);
+    }
+    if (more) put((step + 1) & 1);
+    __syncthreads();
+  }
+
+  const bool split = gridDim.y > 1;
+  if (sum_bias) {  // the four groups' sums of each output
+    float* const sums = reinterpret_cast<float*>(lds);
+    sums[g * TILE + 2 * p] = bias[0];
+    sums[g * TILE + 2 * p + 1] = bias[1];
+    __syncthreads();
+    if (tid < TILE && r0 + tid < a.o) {
+      const float v = (sums[tid] + sums[TILE + tid]) + (sums[2 * TILE + tid] + sums[3 * TILE + tid]);
+      if (split)
+        a.db_parts[(int64_t)blockIdx.y * a.o + r0 + tid] = v;
+      else
+        a.db[r0 + tid] = a.beta == 0.f ? v : a.db[r0 + tid] + v;
+    }
+  }
+#pragma unroll
+  for (int h = 0; h < NT / 4; ++h) {
+    const int at = i0 + wn * NT * 16 + h * 64 + 4 * (lane & 15);
+    if (at >= a.k) continue;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const int to_row = r0 + wm * 64 + i * 16 + 4 * (lane >> 4) + r;
+        if (to_row >= rows) continue;
+        float v[4];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) v[q] = acc[i][4 * h + q][r];
+        const int64_t place = (int64_t)to_row * a.k + at;
+        const int count = min(4, a.k - at);
+        if (split || FILTER) {
+          typedef Elem<MI355_F32> F;
+          float* const to = split ? a.parts + (int64_t)blockIdx.y * rows * a.k + place : static_cast<float*>(a.out) + place;
+          const bool add = !split && a.beta != 0.f;
+          if (count == 4) {
+            if (add) {
+              const u32x4 old = load_vec<F>(to);
+#pragma unroll
+              for (int q = 0; q < 4; ++q) v[q] += F::get(old, q);
+            }
+            store_vec<F>(to, F::pack(v));
+          } else {
+            for (int q = 0; q < count; ++q) to[q] = add ? to[q] + v[q] : v[q];
+          }
+        } else {
+          T* const to = static_cast<T*>(a.out) + place;
+          if (count == 4) {
+            store_four<E>(to, v);
+          } else {
+            for (int q = 0; q < count; ++q) to[q] = E::from_float(v[q]);
+          }
+        }
+      }
+  }
+}
+
+// The splits' sums in one, four elements a thread; beta as the kernels take it.
+template <class E>
+__global__ __launch_bounds__(256) void i8_join_kernel(const float* __restrict__ parts, typename E::T* __restrict__ out, int64_t count, int splits, float beta) {
+  typedef Elem<MI355_F32> F;
+  for (int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4; i < count; i += (int64_t)gridDim.x * 1024) {
+    float v[4];
+    if (i + 4 <= count) {
+      u32x4 w = load_vec<F>(parts + i);
+#pragma unroll
+      for (int q = 0; q < 4; ++q) v[q] = F::get(w, q);
+#pragma unroll 4
+      for (int s = 1; s < splits; ++s) {
+        w = load_vec<F>(parts + s * count + i);
+#pragma unroll
+        for (int q = 0; q < 4; ++q) v[q] += F::get(w, q);
+      }
+      if (beta != 0.f) {
+#pragma unroll
+        for (int q = 0; q < 4; ++q) v[q] += E::to_float(out[i + q]);
+      }
+      store_four<E>(out + i, v);
+    } else {
+      for (int64_t j = i; j < count; ++j) {
+        float sum = parts[j];
+        for (int s = 1; s < splits; ++s) sum += parts[s * count + j];
+        out[j] = E::from_float(beta != 0.f ? E::to_float(out[j]) + sum : sum);
+      }
+    }
+  }
+}
+
+template <class E>
+int launch_join(const float* parts, void* out, int64_t count, int splits, float beta, hipStream_t stream) {
+  hipLaunchKernelGGL(i8_join_kernel<E>, dim3((uint32_t)std::min<int64_t>((count + 1023) / 1024, 1 << 20)), dim3(256), 0, stream, parts,
+                     static_cast<typename E::T*>(out), count, splits, beta);
+  return (int)hipGetLastError();
+}
+
+template <int DTYPE, bool FILTER>
+int launch_gradient(const BwdArgs& a, int tile, int splits, hipStream_t stream) {
+  const int rows = FILTER ? a.o : a.n;
+  const dim3 grid((uint32_t)(((int64_t)rows + tile - 1) / tile * (((int64_t)a.k + tile - 1) / tile)), splits);
+  if (tile == 256)
+    hipLaunchKernelGGL((i8_gradient_kernel<DTYPE, FILTER, 256>), grid, dim3(512), 0, stream, a);
+  else
+    hipLaunchKernelGGL((i8_gradient_kernel<DTYPE, FILTER, 128>), grid, dim3(256), 0, stream, a);
+  int e = (int)hipGetLastError();
+  if (e || splits == 1) return e;
+  const int64_t count = (int64_t)rows * a.k;
+  if constexpr (FILTER) {
+    e = launch_join<Elem<MI355_F32>>(a.parts, a.out, count, splits, a.beta, stream);
+    return e || !a.db ? e : launch_join<Elem<MI355_F32>>(a.db_parts, a.db, a.o, splits, a.beta, stream);
+  } else {
+    return launch_join<Elem<DTYPE>>(a.parts, a.out, count, splits, 0.f, stream);
+  }
+}
+
+template <bool FILTER>
+int gradient(const i8_desc* d, const BwdArgs& a, hipStream_t stream) {
+  const int tile = FILTER ? d->filter_tile : d->data_tile, splits = FILTER ? d->filter_splits : d->data_splits;
+  switch (d->p.dtype) {
+    case MI355_F32: return launch_gradient<MI355_F32, FILTER>(a, tile, splits, stream);
+    case MI355_F16: return launch_gradient<MI355_F16, FILTER>(a, tile, splits, stream);
+    default: return launch_gradient<MI355_BF16, FILTER>(a, tile, splits, stream);
+  }
+}
+
+__global__ __launch_bounds__(256) void i8_clear_kernel(float* to, int64_t count) {
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < count; i += (int64_t)gridDim.x * 256) to[i] = 0.f;
+}
+
+int clear(float* to, int64_t count, hipStream_t stream) {
+  hipLaunchKernelGGL(i8_clear_kernel, dim3((uint32_t)std::min<int64_t>((count + 255) / 256, 1 << 16)), dim3(256), 0, stream, to, count);
+  return (int)hipGetLastError();
+}
+
+int64_t tiles_of(int64_t rows, int64_t columns, int tile) { return (rows + tile - 1) / tile * ((columns + tile - 1) / tile); }
+
+// The tile of a gradient, and the workgroups that share a sum.
+void plan_gradient(int64_t rows, int64_t k, int64_t depth, int32_t& tile, int32_t& splits, int32_t& per) {
+  const int64_t steps = std::max<int64_t>(1, (depth + kStep - 1) / kStep);
+  tile = tiles_of(rows, k, 256) >= kUnits / 2 ? 256 : 128;
+  const int64_t tiles = std::max<int64_t>(1, tiles_of(rows, k, tile)), places = tile == 256 ? 1 : 2 * kUnits;
+  splits = (int32_t)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(places / tiles, steps / 8), 64));
+  per = (int32_t)((steps + splits - 1) / splits);
+  splits = (int32_t)((steps + per - 1) / per);
+}
+
+bool workspace_missing(const i8_desc* d, const void* ws, size_t bytes, int& status) {
+  if (!d->ws_bytes) return false;
+  status = !ws || bytes < d->ws_bytes ? CONV_EWORKSPACE : ((uintptr_t)ws & 15u) ? CONV_EINVAL : CONV_OK;
+  return status != CONV_OK;
+}
+
+bool misaligned(const void* p) { return ((uintptr_t)p & 15u) != 0; }
+
+}  // namespace
+
+}  // namespace mi355conv
+
+using namespace mi355conv;
+
+extern "C" {
+
+int i8_desc_create(i8_desc_t** out, const i8_params_t* pp) {
+  if (!out || !pp) return CONV_EINVAL;
+  const i8_params_t p = *pp;
+  if (p.m < 0 || p.k < 1 || p.num_output < 1 || (p.dtype != MI355_F32 && p.dtype != MI355_F16 && p.dtype != MI355_BF16)) return CONV_EINVAL;
+  if ((p.bias_term != 0 && p.bias_term != 1) || (p.relu != 0 && p.relu != 1)) return CONV_EINVAL;
+  const int64_t M = p.m, K = p.k, O = p.num_output;
+  if (K > kMostInputs || M * K >= kMaxElems || O * K >= kMaxElems || M * O >= kMaxElems) return CONV_ESHAPE;
+  i8_desc* d = new (std::nothrow) i8_desc;
+  if (!d) return CONV_EINVAL;
+  memset(d, 0, sizeof(*d));
+  d->p = p;
+  d->row = (K + kRowUnit - 1) / kRowUnit * kRowUnit;
+  d->fwd = M <= 64 || tiles_of(M, O, 128) < kUnits / 4 ? kRows : tiles_of(M, O, 256) >= kUnits / 2 ? kTile256 : kTile128;
+  d->waves = (int32_t)std::max<int64_t>(1, std::min<int64_t>(tiles_of(M, O, 16) > 4 * kUnits ? 4 : 16, d->row / kRowUnit));
+  plan_gradient(O, K, M, d->filter_tile, d->filter_splits, d->filter_per);
+  plan_gradient(M, K, O, d->data_tile, d->data_splits, d->data_per);
+  if (M > 0) {
+    if (d->filter_splits > 1) d->ws_bytes = (size_t)d->filter_splits * (O * K + O) * 4;
+    if (d->data_splits > 1) d->ws_bytes = std::max(d->ws_bytes, (size_t)d->data_splits * M * K * 4);
+  }
+  char fwd[32];
+  if (d->fwd == kRows)
+    snprintf(fwd, sizeof(fwd), "i8_rows[m%d](W=%d)", 16 * std::max(1, std::min(4, (p.m + 15) / 16)), d->waves);
+  else
+    snprintf(fwd, sizeof(fwd), "i8_tile[%d]", d->fwd == kTile256 ? 256 : 128);
+  snprintf(d->names, sizeof(d->names), "fwd=%s;bwd_filter=i8_gradient[%d](S=%d);bwd_data=i8_gradient[%d](S=%d)", fwd, d->filter_tile, d->filter_splits,
+           d->data_tile, d->data_splits);
+  *out = d;
+  return CONV_OK;
+}
+
+int i8_desc_destroy(i8_desc_t* d) {
+  if (!d) return CONV_EINVAL;
+  delete d;
+  return CONV_OK;
+}
+
+int i8_desc_workspace_bytes(const i8_desc_t* d, size_t* bytes) {
+  if (!d || !bytes) return CONV_EINVAL;
+  *bytes = d->ws_bytes;
+  return CONV_OK;
+}
+
+int i8_desc_row_bytes(const i8_desc_t* d, size_t* bytes) {
+  if (!d || !bytes) return CONV_EINVAL;
+  *bytes = (size_t)d->row;
+  return CONV_OK;
+}
+
+const char* i8_desc_kernel_names(const i8_desc_t* d) { return d ? d->names : ""; }
+
+int i8_pack(const i8_desc_t* d, const void* w, int8_t* w_codes, float* w_scale, void* hip_stream) {
+  if (!d || !w || !w_codes || !w_scale || misaligned(w_codes)) return CONV_EINVAL;
+  const int e = quantise(d, w, w_codes, w_scale, d->p.num_output, (hipStream_t)hip_stream);
+  return e ? record_hip_error(e) : CONV_OK;
+}
+
+int i8_quantise(const i8_desc_t* d, const void* x, int8_t* codes, float* scale, void* hip_stream) {
+  if (!d) return CONV_EINVAL;
+  if (d->p.m == 0) return CONV_OK;
+  if (!x || !codes || !scale || misaligned(codes)) return CONV_EINVAL;
+  const int e = quantise(d, x, codes, scale, d->p.m, (hipStream_t)hip_stream);
+  return e ? record_hip_error(e) : CONV_OK;
+}
+
+int i8_forward(const i8_desc_t* d, const void* x, const int8_t* w_codes, const float* w_scale, const void* bias, void* y,
+               int8_t* codes, float* scale, void* ws, size_t ws_bytes, void* hip_stream) {
+  (void)ws, (void)ws_bytes;
+  if (!d || !w_codes || !w_scale || misaligned(w_codes) || (d->p.bias_term != 0) != (bias != nullptr)) return CONV_EINVAL;
+  if (d->p.m == 0) return CONV_OK;
+  if (!y || !codes || !scale || misaligned(codes)) return CONV_EINVAL;
+  const hipStream_t stream = (hipStream_t)hip_stream;
+  int e = x ? quantise(d, x, codes, scale, d->p.m, stream) : 0;
+  if (e) return record_hip_error(e);
+  const FwdArgs a = {codes, w_codes, scale, w_scale, bias, y, d->row, d->p.m, d->p.num_output, d->p.relu};
+  e = d->p.dtype == MI355_F32   ? launch_forward<MI355_F32>(d, a, stream)
+      : d->p.dtype == MI355_F16 ? launch_forward<MI355_F16>(d, a, stream)
+                                : launch_forward<MI355_BF16>(d, a, stream);
+  return e ? record_hip_error(e) : CONV_OK;
+}
+
+int i8_backward_filter(const i8_desc_t* d, const int8_t* codes, const float* scale, const void* dz, float* dw, float* db, float beta,
+                       void* ws, size_t ws_bytes, void* hip_stream) {
+  if (!d || !dw || (db && !d->p.bias_term) || (beta != 0.f && beta != 1.f)) return CONV_EINVAL;
+  const hipStream_t stream = (hipStream_t)hip_stream;
+  const int64_t O = d->p.num_output, K = d->p.k;
+  if (d->p.m == 0) {
+    if (beta != 0.f) return CONV_OK;
+    int e = clear(dw, O * K, stream);
+    if (!e && db) e = clear(db, O, stream);
+    return e ? record_hip_error(e) : CONV_OK;
+  }
+  int status = CONV_OK;
+  if (!codes || !scale || !dz || misaligned(codes)) return CONV_EINVAL;
+  if (workspace_missing(d, ws, ws_bytes, status)) return status;
+  float* const parts = static_cast<float*>(ws);
+  const BwdArgs a = {codes, scale, dz, dw, db, parts, parts + d->filter_splits * O * K, d->row, d->p.m, d->p.num_output, d->p.k, d->filter_per, beta};
+  const int e = gradient<true>(d, a, stream);
+  return e ? record_hip_error(e) : CONV_OK;
+}
+
+int i8_backward_data(const i8_desc_t* d, const int8_t* w_codes, const float* w_scale, const void* dz, void* dx, void* ws,
+                     size_t ws_bytes, void* hip_stream) {
+  if (!d || !w_codes || !w_scale || misaligned(w_codes)) return CONV_EINVAL;
+  if (d->p.m == 0) return CONV_OK;
+  int status = CONV_OK;
+  if (!dz || !dx) return CONV_EINVAL;
+  if (workspace_missing(d, ws, ws_bytes, status)) return status;
+  const BwdArgs a = {w_codes, w_scale, dz, dx, nullptr, static_cast<float*>(ws), nullptr, d->row, d->p.m, d->p.num_output, d->p.k, d->data_per, 0.f};
+  const int e = gradient<false>(d, a, (hipStream_t)hip_stream);
+  return e ? record_hip_error(e) : CONV_OK;
+}
+
+}  // extern "C"

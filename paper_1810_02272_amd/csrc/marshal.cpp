@@ -21,6 +21,8 @@
 #include "mi355lp.h"
 #include "mi355gn.h"
 #include "mi355q4.h"
+#include "mi355sm.h"
+#include "mi355i8.h"
 
 #include <new>
 #include <vector>
@@ -596,6 +598,120 @@ PyObject* py_q4_plan(PyObject*, PyObject* args) {  // handle, m, k, num_output, 
                                                 {1, {packed}}}, kQ4);
 }
 
+// ---- drawing tokens ----
+
+struct SmPlan {
+  const sm_desc_t* desc;
+  LpPlan rows;  // the logits' shape and type
+};
+
+const char kSm[] = "mi355conv.sm_plan", kI8[] = "mi355conv.i8_plan";
+
+PyObject* py_sm_sample(PyObject*, Args a, Py_ssize_t n) {  // plan, logits, u, scale, top_k, top_p, min_p, token, logp, ws, stream
+  return guarded(n, 11, [&]() -> PyObject* {
+    const SmPlan* p = own_plan<SmPlan>(a[0], kSm);
+    void *x, *u, *scale, *top_k, *top_p, *min_p, *token, *logp, *ws, *s;
+    int64_t stride;
+    size_t bytes;
+    if (!p || !spaced_rows(a[1], p->rows, &x, &stride) || !tensor(a[2], at::kFloat, p->rows.row, &u) ||
+        !optional_tensor(a[3], at::kFloat, p->rows.row, &scale) || !optional_tensor(a[4], kInt, p->rows.row, &top_k) ||
+        !optional_tensor(a[5], at::kFloat, p->rows.row, &top_p) || !optional_tensor(a[6], at::kFloat, p->rows.row, &min_p) ||
+        !tensor(a[7], kInt, p->rows.row, &token) || !optional_tensor(a[8], at::kFloat, p->rows.row, &logp) || !workspace(a[9], &ws, &bytes) ||
+        !stream(a[10], &s))
+      return nullptr;
+    return released([&] {
+      return sm_sample(p->desc, x, stride, static_cast<float*>(u), static_cast<float*>(scale), static_cast<int32_t*>(top_k),
+                       static_cast<float*>(top_p), static_cast<float*>(min_p), static_cast<int32_t*>(token), static_cast<float*>(logp), ws,
+                       bytes, s);
+    });
+  });
+}
+
+PyObject* py_sm_plan(PyObject*, PyObject* args) {  // handle, rows, vocab, dtype
+  unsigned long long handle;
+  long long rows, vocab;
+  int dtype;
+  if (!PyArg_ParseTuple(args, "KLLi", &handle, &rows, &vocab, &dtype)) return nullptr;
+  return new_own_plan(new (std::nothrow) SmPlan{reinterpret_cast<const sm_desc_t*>(handle),
+                                                LpPlan{nullptr, rows, vocab, scalar_type(dtype), {1, {rows}}, {}, {}}}, kSm);
+}
+
+// ---- 8-bit integers ----
+
+struct I8Plan {
+  const i8_desc_t* desc;
+  at::ScalarType type;
+  Shape x, w, y, codes, w_codes, rows, outputs;
+};
+
+PyObject* py_i8_quantise(PyObject*, Args a, Py_ssize_t n) {  // plan, x, codes, scale, stream
+  return guarded(n, 5, [&]() -> PyObject* {
+    const I8Plan* p = own_plan<I8Plan>(a[0], kI8);
+    void *x, *codes, *scale, *s;
+    if (!p || !tensor(a[1], p->type, p->x, &x) || !tensor(a[2], at::kChar, p->codes, &codes) || !tensor(a[3], at::kFloat, p->rows, &scale) ||
+        !stream(a[4], &s))
+      return nullptr;
+    return released([&] { return i8_quantise(p->desc, x, static_cast<int8_t*>(codes), static_cast<float*>(scale), s); });
+  });
+}
+
+PyObject* py_i8_forward(PyObject*, Args a, Py_ssize_t n) {  // plan, x, w_codes, w_scale, bias, y, codes, scale, ws, stream
+  return guarded(n, 10, [&]() -> PyObject* {
+    const I8Plan* p = own_plan<I8Plan>(a[0], kI8);
+    void *x, *w_codes, *w_scale, *bias, *y, *codes, *scale, *ws, *s;
+    size_t bytes;
+    if (!p || !optional_tensor(a[1], p->type, p->x, &x) || !tensor(a[2], at::kChar, p->w_codes, &w_codes) ||
+        !tensor(a[3], at::kFloat, p->outputs, &w_scale) || !optional_tensor(a[4], p->type, p->outputs, &bias) ||
+        !tensor(a[5], p->type, p->y, &y) || !tensor(a[6], at::kChar, p->codes, &codes) || !tensor(a[7], at::kFloat, p->rows, &scale) ||
+        !workspace(a[8], &ws, &bytes) || !stream(a[9], &s))
+      return nullptr;
+    return released([&] {
+      return i8_forward(p->desc, x, static_cast<int8_t*>(w_codes), static_cast<float*>(w_scale), bias, y, static_cast<int8_t*>(codes),
+                        static_cast<float*>(scale), ws, bytes, s);
+    });
+  });
+}
+
+PyObject* py_i8_backward_filter(PyObject*, Args a, Py_ssize_t n) {  // plan, codes, scale, dz, dw, db, beta, ws, stream
+  return guarded(n, 9, [&]() -> PyObject* {
+    const I8Plan* p = own_plan<I8Plan>(a[0], kI8);
+    void *codes, *scale, *dz, *dw, *db, *ws, *s;
+    double beta;
+    size_t bytes;
+    if (!p || !tensor(a[1], at::kChar, p->codes, &codes) || !tensor(a[2], at::kFloat, p->rows, &scale) || !tensor(a[3], p->type, p->y, &dz) ||
+        !tensor(a[4], at::kFloat, p->w, &dw) || !optional_tensor(a[5], at::kFloat, p->outputs, &db) || !number(a[6], &beta) ||
+        !workspace(a[7], &ws, &bytes) || !stream(a[8], &s))
+      return nullptr;
+    return released([&] {
+      return i8_backward_filter(p->desc, static_cast<int8_t*>(codes), static_cast<float*>(scale), dz, static_cast<float*>(dw),
+                                static_cast<float*>(db), (float)beta, ws, bytes, s);
+    });
+  });
+}
+
+PyObject* py_i8_backward_data(PyObject*, Args a, Py_ssize_t n) {  // plan, w_codes, w_scale, dz, dx, ws, stream
+  return guarded(n, 7, [&]() -> PyObject* {
+    const I8Plan* p = own_plan<I8Plan>(a[0], kI8);
+    void *w_codes, *w_scale, *dz, *dx, *ws, *s;
+    size_t bytes;
+    if (!p || !tensor(a[1], at::kChar, p->w_codes, &w_codes) || !tensor(a[2], at::kFloat, p->outputs, &w_scale) ||
+        !tensor(a[3], p->type, p->y, &dz) || !tensor(a[4], p->type, p->x, &dx) || !workspace(a[5], &ws, &bytes) || !stream(a[6], &s))
+      return nullptr;
+    return released([&] {
+      return i8_backward_data(p->desc, static_cast<int8_t*>(w_codes), static_cast<float*>(w_scale), dz, dx, ws, bytes, s);
+    });
+  });
+}
+
+PyObject* py_i8_plan(PyObject*, PyObject* args) {  // handle, m, k, num_output, dtype, bytes of a row of codes
+  unsigned long long handle;
+  long long m, k, o, row;
+  int dtype;
+  if (!PyArg_ParseTuple(args, "KLLLiL", &handle, &m, &k, &o, &dtype, &row)) return nullptr;
+  return new_own_plan(new (std::nothrow) I8Plan{reinterpret_cast<const i8_desc_t*>(handle), scalar_type(dtype), {2, {m, k}}, {2, {o, k}},
+                                                {2, {m, o}}, {2, {m, row}}, {2, {o, row}}, {1, {m}}, {1, {o}}}, kI8);
+}
+
 #define FAST(name, fn) {name, (PyCFunction)(void (*)(void))(PyObject * (*)(PyObject*, Args, Py_ssize_t)) & fn, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {
     {"conv_plan", py_conv_plan, METH_VARARGS, nullptr},
@@ -603,6 +719,8 @@ PyMethodDef methods[] = {
     {"lp_plan", py_lp_plan, METH_VARARGS, nullptr},
     {"gn_plan", py_gn_plan, METH_VARARGS, nullptr},
     {"q4_plan", py_q4_plan, METH_VARARGS, nullptr},
+    {"sm_plan", py_sm_plan, METH_VARARGS, nullptr},
+    {"i8_plan", py_i8_plan, METH_VARARGS, nullptr},
     FAST("conv_forward", py_conv_forward<float>),
     FAST("conv_forward_f64", py_conv_forward<double>),
     FAST("conv_backward_data", py_conv_backward_data<float>),
@@ -626,6 +744,11 @@ PyMethodDef methods[] = {
     FAST("lp_forward_backward", py_lp_forward_backward),
     FAST("gn_clip", py_gn_clip),
     FAST("q4_forward", py_q4_forward),
+    FAST("sm_sample", py_sm_sample),
+    FAST("i8_quantise", py_i8_quantise),
+    FAST("i8_forward", py_i8_forward),
+    FAST("i8_backward_filter", py_i8_backward_filter),
+    FAST("i8_backward_data", py_i8_backward_data),
     {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};

@@ -1,0 +1,335 @@
+"""The InnerProduct layer in 8-bit integers (include/mi355i8.h) against the oracle in 64 bits.
+
+Codes and scales are whole numbers of 8 bits and have to be equal.  Tolerances:
+forward: the sum is exact; its conversion, the product with s and the last multiply-add round once each (2^-24 of the product twice, of the
+result once), then half a step of the output's type.
+gradients: dz times a scale is exact for bf16 and rounded once to fp32 otherwise; an instruction adds 32 products of a term (at most 32 roundings of its
+own products' size) to the sum (one of the sum's size).  With T terms and a depth of N that is below (32 + T N / 32 + splits + 4) 2^-24 of the sum of
+the terms' magnitudes; then half a step of the output's type.  The bias gradient adds N numbers one by one at most."""
+import math
+
+import pytest
+import torch
+
+import paper_1810_02272_amd as lib
+from oracle import tokens
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+F32, F16, BF16 = torch.float32, torch.float16, torch.bfloat16
+U = 2.0 ** -24
+
+# m, k, o, dtype, bias, relu
+CASES = [
+    (1, 1, 1, BF16, 0, 0), (1, 1, 1, F32, 1, 1), (1, 7, 3, F16, 1, 0), (2, 127, 16, BF16, 1, 1), (3, 128, 17, F32, 0, 0), (5, 129, 33, F16, 0, 1),
+    (16, 1000, 100, BF16, 1, 0), (17, 2049, 65, F32, 1, 1), (1, 4096, 4096, BF16, 0, 0), (1, 4095, 20000, BF16, 1, 0), (33, 300, 257, F16, 1, 0), (48, 9216, 512, F32, 1, 1),
+    (64, 640, 1000, BF16, 0, 0), (65, 640, 130, F32, 0, 1), (100, 999, 333, F32, 0, 0), (129, 511, 77, BF16, 1, 0), (200, 33, 1, F16, 1, 0), (1, 33, 300, F32, 0, 0),
+    (1500, 200, 900, F32, 1, 1), (1100, 129, 1030, BF16, 1, 0), (2001, 257, 777, F16, 0, 0), (4096, 300, 2100, BF16, 1, 1), (4099, 260, 2050, F16, 1, 0), (3000, 130, 3001, F32, 0, 0),
+    (256, 4096, 1000, F32, 1, 0), (1999, 1111, 777, F16, 1, 0), (3333, 96, 130, BF16, 1, 0), (31, 2900, 2900, BF16, 1, 0), (40, 2900, 3100, F32, 0, 0), (64, 3001, 2900, F16, 1, 0),
+    (3001, 2900, 70, BF16, 0, 0), (3000, 2901, 50, F32, 0, 0), (2999, 2900, 64, F16, 0, 0), (900, 2900, 2048, BF16, 1, 0), (5000, 128, 31, F32, 1, 1), (2, 60000, 5, BF16, 0, 0), (3, 133120, 4, F32, 0, 0),
+]
+
+
+def make(case, seed=0):
+    m, k, o, dtype, bias, relu = case
+    g = torch.Generator(device=DEV).manual_seed(seed + m * k + o)
+    random = lambda *shape: torch.randn(shape, generator=g, device=DEV)
+    x = (random(m, k) * torch.exp(random(m, 1))).to(dtype)
+    w = (random(o, k) * torch.exp(0.5 * random(o, 1)) / math.sqrt(k)).to(dtype)
+    return x, w, random(o).to(dtype) if bias else None, random(m, o).to(dtype)
+
+
+class Layer:
+    """Every call's outputs lie between guards, and is made twice."""
+
+    def __init__(self, case):
+        m, k, o, dtype, bias, relu = self.case = case
+        self.d = lib.i8_desc_create(lib.I8Params(m, k, o, dtype, bias, relu))
+        print(lib.i8_desc_kernel_names(self.d), flush=True)
+        self.row = lib.i8_desc_row_bytes(self.d)
+        assert self.row % 128 == 0 and 0 <= self.row - k < 128
+        self.ws = torch.full((lib.i8_desc_workspace_bytes(self.d) // 4 + 16,), math.nan, device=DEV)
+
+    def space(self):
+        size = (lib.i8_desc_workspace_bytes(self.d) + 3) // 4
+        return self.ws[:size]
+
+    @staticmethod
+    def guarded(shape, dtype, first=0):
+        n = math.prod(shape)
+        fill = 0x55 if dtype is torch.int8 else math.nan
+        buffer = torch.full((first + n + 64,), fill, device=DEV, dtype=dtype)
+        return buffer, buffer[first:first + n].view(shape)
+
+    @staticmethod
+    def untouched(buffer, n, first=0):
+        for t in (buffer[:first], buffer[first + n:]):
+            assert bool((t == 0x55).all() if t.dtype is torch.int8 else torch.isnan(t).all())
+
+    def eight(self, x, pack=False):
+        b, codes = self.guarded((x.shape[0], self.row), torch.int8)
+        s, scale = self.guarded((x.shape[0],), F32)
+        (lib.i8_pack if pack else lib.i8_quantise)(self.d, x, codes, scale)
+        self.untouched(b, codes.numel())
+        self.untouched(s, scale.numel())
+        return codes, scale
+
+    def forward(self, x, w_codes, w_scale, bias, first=0):
+        m, k, o, dtype = self.case[:4]
+        codes, scale = torch.empty((m, self.row), device=DEV, dtype=torch.int8), torch.empty(m, device=DEV)
+        b, y = self.guarded((m, o), dtype, first)
+        lib.i8_forward(self.d, x, w_codes, w_scale, bias, y, codes, scale, self.space())
+        self.untouched(b, m * o, first)
+        again = torch.empty_like(y)
+        lib.i8_forward(self.d, None, w_codes, w_scale, bias, again, codes, scale, self.space())
+        assert torch.equal(again.nan_to_num(7.0), y.nan_to_num(7.0))
+        return y, codes, scale
+
+    def filter(self, codes, scale, dz, want_db=True):
+        m, k, o, dtype, bias, relu = self.case
+        b, dw = self.guarded((o, k), F32)
+        c, db = self.guarded((o,), F32) if bias and want_db else (None, None)
+        lib.i8_backward_filter(self.d, codes, scale, dz, dw, db, 0.0, self.space())
+        self.untouched(b, o * k)
+        more, more_db = dw.clone(), None if db is None else db.clone()
+        lib.i8_backward_filter(self.d, codes, scale, dz, more, more_db, 1.0, self.space())
+        assert torch.equal((dw + dw).nan_to_num(7.0), more.nan_to_num(7.0))  # twice a number is exact
+        if db is not None:
+            self.untouched(c, o)
+            assert torch.equal((db + db).nan_to_num(7.0), more_db.nan_to_num(7.0))
+        return dw, db
+
+    def data(self, w_codes, w_scale, dz):
+        m, k, o, dtype = self.case[:4]
+        b, dx = self.guarded((m, k), dtype)
+        lib.i8_backward_data(self.d, w_codes, w_scale, dz, dx, self.space())
+        self.untouched(b, m * k)
+        again = torch.empty_like(dx)
+        lib.i8_backward_data(self.d, w_codes, w_scale, dz, again, self.space())
+        assert torch.equal(dx.nan_to_num(7.0), again.nan_to_num(7.0))
+        return dx
+
+    def splits(self, which):
+        part = [v for v in lib.i8_desc_kernel_names(self.d).split(";") if v.startswith(which)][0]
+        return int(part.split("S=")[1].rstrip(")"))
+
+
+def check_eight(x, codes, scale):
+    want_codes, want_scale = tokens.eight_bits(x)
+    assert torch.equal(scale.double().nan_to_num(7.0), want_scale.nan_to_num(7.0))
+    assert torch.equal(codes[:, :x.shape[1]].double(), want_codes)
+    assert bool((codes[:, x.shape[1]:] == 0).all())
+
+
+def half_step(want, dtype):
+    if dtype is F32:
+        return want.abs() * 0 + 2.0 ** -149
+    return want.abs() * (torch.finfo(dtype).eps / 2) + (2.0 ** -25 if dtype is F16 else 2.0 ** -134)
+
+
+def within(got, want, tol):
+    off = (got.double() - want).abs()
+    assert bool((off <= tol).all()), (float(off.max()), int((off > tol).sum()), float((off / tol).max()))
+
+
+def check_forward(case, codes, scale, w_codes, w_scale, bias, y):
+    m, k, o, dtype, _, relu = case
+    codes, w_codes = codes[:, :k], w_codes[:, :k]
+    want = tokens.i8_forward(codes, scale, w_codes, w_scale, bias, relu)
+    product = tokens.i8_forward(codes, scale, w_codes, w_scale, None, 0).abs()
+    within(y, want, product * 2.01 * U + want.abs() * 1.01 * U + half_step(want, dtype) * 1.01)
+
+
+def terms(dtype):
+    return 2 if dtype is BF16 else 3
+
+
+def check_filter(case, layer, codes, scale, dz, dw, db):
+    m, k, o, dtype = case[:4]
+    want, want_db = tokens.i8_backward_filter(codes[:, :k], scale, dz)
+    size, size_db = tokens.i8_backward_filter(codes[:, :k].abs(), scale, dz.abs())
+    s = layer.splits("bwd_filter")
+    within(dw, want, size * (36 + terms(dtype) * m / 32 + s) * U * 1.02 + 2.0 ** -126)
+    if db is not None:
+        within(db, want_db, size_db * (m + 4) * U + 2.0 ** -149)
+
+
+def check_data(case, layer, w_codes, w_scale, dz, dx):
+    m, k, o, dtype = case[:4]
+    want = tokens.i8_backward_data(w_codes[:, :k], w_scale, dz)
+    size = tokens.i8_backward_data(w_codes[:, :k].abs(), w_scale, dz.abs())
+    s = layer.splits("bwd_data")
+    within(dx, want, size * (36 + terms(dtype) * o / 32 + s) * U * 1.02 + half_step(want, dtype) * 1.02 + 2.0 ** -126)
+
+
+@pytest.mark.parametrize("case", CASES, ids=["%dx%d-%d-%s-b%d-r%d" % (c[0], c[1], c[2], str(c[3])[6:], *c[4:]) for c in CASES])
+def test_parity(case):
+    x, w, bias, dz = make(case)
+    layer = Layer(case)
+    w_codes, w_scale = layer.eight(w, pack=True)
+    check_eight(w, w_codes, w_scale)
+    codes, scale = layer.eight(x)
+    check_eight(x, codes, scale)
+    y, kept, kept_scale = layer.forward(x, w_codes, w_scale, bias)
+    assert torch.equal(kept, codes) and torch.equal(kept_scale, scale)
+    check_forward(case, codes, scale, w_codes, w_scale, bias, y)
+    dw, db = layer.filter(codes, scale, dz)
+    check_filter(case, layer, codes, scale, dz, dw, db)
+    check_data(case, layer, w_codes, w_scale, dz, layer.data(w_codes, w_scale, dz))
+
+
+@pytest.mark.parametrize("dtype", [F32, F16, BF16])
+@pytest.mark.parametrize("m", [3, 1030])
+def test_unaligned_blobs(dtype, m):
+    case = (m, 263, 1027 if m > 3 else 47, dtype, 1, 0)
+    x, w, bias, dz = make(case)
+    place = lambda t: torch.cat([t.new_zeros(1), t.reshape(-1)])[1:].view(t.shape)
+    x, w, bias, dz = place(x), place(w), place(bias), place(dz)
+    layer = Layer(case)
+    w_codes, w_scale = layer.eight(w, pack=True)
+    w_scale = place(w_scale)
+    y, codes, scale = layer.forward(x, w_codes, w_scale, bias, first=1)
+    scale = place(scale)
+    check_eight(x, codes, scale)
+    check_forward(case, codes, scale, w_codes, w_scale, bias, y)
+    dw, db = layer.filter(codes, scale, dz)
+    check_filter(case, layer, codes, scale, dz, dw, db)
+    check_data(case, layer, w_codes, w_scale, dz, layer.data(w_codes, w_scale, dz))
+
+
+@pytest.mark.parametrize("dtype", [F32, F16, BF16])
+@pytest.mark.parametrize("k", [40, 3000])
+def test_codes_at_halves_and_ends(dtype, k):
+    """Halves go to the even whole number, rows of zeros stay zeros, subnormal and the largest rows have scales that hold them."""
+    info = torch.finfo(dtype)
+    x = torch.zeros((12, k), device=DEV, dtype=dtype)
+    halves = torch.arange(k, device=DEV) % 40
+    x[0] = (halves - 20 + 0.5).to(dtype)
+    x[0, 0] = 127  # scale 1
+    x[1] = x[0] * 2.0 ** -8
+    x[2, 1] = info.max
+    x[3] = -info.max
+    x[4, k - 1] = info.smallest_normal
+    x[5, 0] = info.smallest_normal * info.eps  # the smallest number there is
+    x[6] = torch.randn(k, device=DEV).to(dtype)
+    x[7] = torch.randn(k, device=DEV).to(dtype) * info.smallest_normal * 8
+    x[8, :4] = torch.tensor([1.0, -1.0, 0.5, -0.5], device=DEV, dtype=dtype)
+    x[9] = -0.0
+    x[10] = info.max / 255
+    x[11, 0], x[11, 1] = 127.5, 63.75
+    layer = Layer((12, k, 1, dtype, 0, 0))
+    codes, scale = layer.eight(x)
+    check_eight(x, codes, scale)
+    assert float(scale[0]) == 1.0 and bool((codes[0, 1:k].double() % 2 == 0).all())
+
+
+@pytest.mark.parametrize("dtype", [F32, F16, BF16])
+@pytest.mark.parametrize("m", [20, 1200])
+def test_not_a_number_and_infinity_stay_in_their_rows(dtype, m):
+    case = (m, 200, 1100 if m > 20 else 40, dtype, 1, 0)
+    x, w, bias, dz = make(case)
+    x[3, 5], x[7, 150], x[18, 0] = math.nan, math.inf, -math.inf
+    w[9, 3] = math.nan
+    layer = Layer(case)
+    w_codes, w_scale = layer.eight(w, pack=True)
+    y, codes, scale = layer.forward(x, w_codes, w_scale, bias)
+    check_eight(x, codes, scale)
+    bad = torch.zeros(m, device=DEV, dtype=torch.bool)
+    bad[[3, 7, 18]] = True
+    other = torch.arange(case[2], device=DEV) != 9
+    assert torch.isnan(y[bad]).all() and torch.isnan(y[:, 9]).all()
+    assert torch.isfinite(y[~bad][:, other]).all()
+    dz[4, 2] = math.nan  # a gradient's stays with its output, and its row
+    dw, db = layer.filter(*layer.eight(torch.nan_to_num(x, 0.0, 1.0, 1.0)), dz)
+    assert torch.isnan(dw[2]).all() and torch.isnan(db[2]) and torch.isfinite(dw[torch.arange(case[2], device=DEV) != 2]).all()
+    dx = layer.data(*layer.eight(torch.nan_to_num(w, 0.0), pack=True), dz)
+    assert torch.isnan(dx[4]).all() and torch.isfinite(dx[torch.arange(m, device=DEV) != 4]).all()
+
+
+@pytest.mark.parametrize("dtype", [F32, F16, BF16])
+def test_gradients_take_all_bits_of_dz(dtype):
+    """Two rows whose dz differ in the last bit, under codes 1 and -1 and a scale of 255 / 128: what is left comes out exactly."""
+    layer = Layer((2, 1, 1, dtype, 0, 0))
+    codes = torch.zeros((2, layer.row), device=DEV, dtype=torch.int8)
+    codes[0, 0], codes[1, 0] = 1, -1
+    scale = torch.full((2,), 255 / 128 if dtype is not F32 else 1.0, device=DEV)
+    step = torch.finfo(dtype).eps
+    dz = torch.tensor([[1.0 + step], [1.0]], device=DEV, dtype=dtype)
+    dw, _ = layer.filter(codes, scale, dz)
+    assert float(dw) == step * float(scale[0])
+    layer = Layer((1, 1, 2, dtype, 0, 0))
+    dx = layer.data(codes, scale, dz.t().contiguous())
+    assert float(dx) == step * float(scale[0])
+
+
+def test_gradients_agree_with_differences():
+    """fp32: of a sum of outputs of the layer, by the codes' and the bias's change."""
+    case = (6, 20, 5, F32, 1, 0)
+    x, w, bias, dz = make(case)
+    layer = Layer(case)
+    w_codes, w_scale = layer.eight(w, pack=True)
+    codes, scale = layer.eight(x)
+    dw, db = layer.filter(codes, scale, dz)
+    dx = layer.data(w_codes, w_scale, dz)
+    loss = lambda c, wc: float((tokens.i8_forward(c[:, :20], scale, wc[:, :20], w_scale, bias, 0) * dz.double()).sum())
+    for n, i in ((0, 0), (5, 19), (2, 7)):
+        c = codes.clone().short()
+        c[n, i] += 1  # x moves by its row's scale
+        assert abs((loss(c, w_codes) - loss(codes, w_codes)) - float(dx[n, i]) * float(scale[n])) <= 1e-4
+    for o, i in ((0, 0), (4, 19), (2, 7)):
+        c = w_codes.clone().short()
+        c[o, i] += 1
+        assert abs((loss(codes, c) - loss(codes, w_codes)) - float(dw[o, i]) * float(w_scale[o])) <= 1e-4
+
+
+@pytest.mark.parametrize("beta", [0.0, 1.0])
+def test_no_rows(beta):
+    d = lib.i8_desc_create(lib.I8Params(0, 70, 33, BF16, 1, 0))
+    dw, db = torch.full((33, 70), 3.0, device=DEV), torch.full((33,), 3.0, device=DEV)
+    empty = lambda *s, t=F32: torch.empty(s, device=DEV, dtype=t)
+    codes, scale, dz = empty(0, 128, t=torch.int8), empty(0), empty(0, 33, t=BF16)
+    lib.i8_quantise(d, empty(0, 70, t=BF16), codes, scale)
+    lib.i8_forward(d, empty(0, 70, t=BF16), empty(33, 128, t=torch.int8), empty(33), empty(33, t=BF16), dz, codes, scale)
+    lib.i8_backward_data(d, empty(33, 128, t=torch.int8), empty(33), dz, empty(0, 70, t=BF16))
+    lib.i8_backward_filter(d, codes, scale, dz, dw, db, beta)
+    assert bool((dw == 3.0 * beta).all()) and bool((db == 3.0 * beta).all())
+
+
+@pytest.mark.parametrize("case", [(1, 500, 300, BF16, 1, 0), (40, 3000, 700, F16, 1, 1), (1300, 400, 900, F32, 1, 0)])
+def test_other_streams_and_graphs(case):
+    m, k, o, dtype, _, _ = case
+    x, w, bias, dz = make(case)
+    layer = Layer(case)
+    w_codes, w_scale = layer.eight(w, pack=True)
+    t = lambda *shape, d=dtype: torch.empty(shape, device=DEV, dtype=d)
+    outs = (t(m, o), t(m, layer.row, d=torch.int8), t(m, d=F32), t(o, k, d=F32), t(o, d=F32), t(m, k))
+    y, codes, scale, dw, db, dx = outs
+    ws = layer.space()
+
+    def step(stream=None):
+        lib.i8_forward(layer.d, x, w_codes, w_scale, bias, y, codes, scale, ws, stream)
+        lib.i8_backward_filter(layer.d, codes, scale, dz, dw, db, 0.0, ws, stream)
+        lib.i8_backward_data(layer.d, w_codes, w_scale, dz, dx, ws, stream)
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    step(side)
+    side.synchronize()
+    first = [v.clone() for v in outs]
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for i in range(3):
+        if i:
+            x.normal_()
+            dz.normal_()
+        for v in outs:
+            v.zero_()
+        graph.replay()
+        replayed = [v.clone() for v in outs]
+        step()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(replayed, outs))
+        if i == 0:
+            assert all(torch.equal(a, b) for a, b in zip(first, outs))
+        check_filter(case, layer, codes, scale, dz, dw, db)

@@ -1,0 +1,220 @@
+"""Drawing tokens (include/mi355sm.h) against the oracle in 64 bits.
+
+Tokens are whole numbers and have to be equal: weights and sums are held in 64 bits on both sides, and none of these inputs has a border within
+2^-40 of the whole of u or p, but for those made to meet one exactly, with weights that are powers of two.  Log probabilities: an exponent of 64
+bits, a logarithm and one rounding to fp32, half a step (2^-24 relative)."""
+import math
+
+import pytest
+import torch
+
+import paper_1810_02272_amd as lib
+from oracle import tokens
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+F32, F16, BF16 = torch.float32, torch.float16, torch.bfloat16
+I32 = torch.int32
+
+# rows, vocab, dtype, stride, spread of the logits
+CASES = [
+    (1, 1, F32, 1, 1.0), (1, 1, BF16, 1, 1.0), (3, 2, F16, 5, 1.0), (5, 7, BF16, 7, 2.0), (64, 8, F32, 8, 2.0), (33, 9, F16, 11, 2.0), (200, 64, BF16, 64, 3.0),
+    (50, 255, F32, 300, 1.0), (40, 1000, F16, 1001, 3.0), (60, 4096, F32, 4096, 2.0), (30, 4097, F32, 4097, 2.0), (30, 8192, BF16, 8192, 3.0), (20, 8193, F16, 8193, 3.0),
+    (10, 32000, BF16, 32000, 2.0), (6, 50257, F16, 50304, 4.0), (4, 65537, BF16, 65537, 1.0), (3, 131072, BF16, 131073, 3.0), (2, 128256, F32, 128256, 2.0),
+    (2, 160001, F16, 160001, 2.0), (1, 700000, BF16, 700000, 3.0), (300, 3000, BF16, 3000, 0.1), (12, 20000, BF16, 20000, 0.02), (600, 128, BF16, 128, 3.0),
+]
+SCALES, KS = (0.25, 0.75, 1.0, 1.25, 3.0), (0, 0, 1, 2, 5, 40, 1000, 5000, 1 << 30, -3)
+PS, QS = (1.0, 1.0, 0.0, 0.3, 0.9, 0.95, 0.999, 2.0), (0.0, 0.0, 0.01, 0.1, 0.7, 1.0, 3.0, -1.0)
+
+
+def make(case, seed=0):
+    rows, vocab, dtype, stride, spread = case
+    g = torch.Generator(device=DEV).manual_seed(seed + rows * vocab)
+    x = torch.full((rows, stride), math.nan, device=DEV, dtype=dtype)
+    z = torch.randn((rows, vocab), generator=g, device=DEV) * spread
+    x[:, :vocab] = (z - 0.6 * torch.log1p(torch.rand((rows, vocab), generator=g, device=DEV) * vocab)).to(dtype)
+    pick = lambda values, t=F32: torch.tensor(values, device=DEV, dtype=t)[torch.randint(len(values), (rows,), generator=g, device=DEV)]
+    return x[:, :vocab], torch.rand(rows, generator=g, device=DEV), pick(SCALES), pick(KS, I32), pick(PS), pick(QS)
+
+
+def run(x, u, scale=None, top_k=None, top_p=None, min_p=None, want_logp=True):
+    rows, vocab = x.shape
+    d = lib.sm_desc_create(lib.SmParams(rows, vocab, x.dtype))
+    print(lib.sm_desc_kernel_names(d), flush=True)
+    size = lib.sm_desc_workspace_bytes(d)
+    ws = torch.full(((size + 3) // 4 + 16,), math.nan, device=DEV)
+    token, logp = torch.full((rows + 8,), -77, device=DEV, dtype=I32), torch.full((rows + 8,), 55.0, device=DEV)
+    call = lambda t, l: lib.sm_sample(d, x, u, scale, top_k, top_p, min_p, t, l, ws[:(size + 3) // 4])
+    call(token[:rows], logp[:rows])
+    assert bool((token[rows:] == -77).all()) and bool((logp[rows:] == 55.0).all()) and bool(torch.isnan(ws[(size + 3) // 4:]).all())
+    again = torch.empty_like(token[:rows])
+    call(again, None)
+    assert torch.equal(again, token[:rows])
+    return token[:rows], logp[:rows]
+
+
+def full(rows, value, t=F32):
+    return torch.full((rows,), value, device=DEV, dtype=t)
+
+
+def check(got, x, u, scale=None, top_k=None, top_p=None, min_p=None):
+    rows = x.shape[0]
+    token, logp = got
+    want, want_logp = tokens.draw(x, u, full(rows, 1.0) if scale is None else scale, full(rows, 0, I32) if top_k is None else top_k,
+                                  full(rows, 1.0) if top_p is None else top_p, full(rows, 0.0) if min_p is None else min_p)
+    assert torch.equal(token, want), [(int(r), int(token[r]), int(want[r])) for r in (token != want).nonzero()[:5, 0]]
+    assert bool(((logp.double() - want_logp).abs() <= want_logp.abs() * 1.01 * 2.0 ** -24 + 2.0 ** -45).all())
+
+
+@pytest.mark.parametrize("case", CASES, ids=["%dx%d-%s-%d-%g" % (c[0], c[1], str(c[2])[6:], c[3], c[4]) for c in CASES])
+def test_parity(case):
+    x, u, scale, k, p, q = make(case)
+    for limits in ((None, None, None, None), (scale, None, None, None), (scale, k, None, None), (scale, None, p, None), (None, None, None, q),
+                   (scale, k, p, None), (scale, k, p, q)):
+        check(run(x, u, *limits), x, u, *limits)
+
+
+@pytest.mark.parametrize("dtype", [F32, F16, BF16])
+def test_against_the_definition_token_by_token(dtype):
+    x, u, scale, k, p, q = make((120, 37, dtype, 40, 2.0), seed=4)
+    x[5, 3:] = -math.inf
+    x[6, :36] = -math.inf
+    x[7] = 0.5
+    x[8, ::2], x[8, 1::2] = 0.0, -0.0
+    token, logp = run(x, u, scale, k, p, q)
+    for r in range(120):
+        want = tokens.draw_row(x[r].cpu(), float(u[r]), float(scale[r]), int(k[r]), float(p[r]), float(q[r]))
+        assert int(token[r]) == want[0], r
+        assert abs(float(logp[r]) - want[1]) <= 1e-6 * (1 + abs(want[1]))
+
+
+@pytest.mark.parametrize("dtype", [F32, F16, BF16])
+@pytest.mark.parametrize("vocab", [1, 6, 5000, 70000])
+def test_rows_without_a_distribution_and_bad_parameters(dtype, vocab):
+    rows = 16
+    x = torch.randn((rows, vocab), device=DEV).to(dtype)
+    u, scale, k, p, q = full(rows, 0.5), full(rows, 1.0), full(rows, 3, I32), full(rows, 0.9), full(rows, 0.1)
+    x[0], x[1, vocab - 1], x[2, 0] = -math.inf, math.nan, math.inf
+    x[3], x[4] = math.nan, math.inf
+    scale[5], scale[6], scale[7], scale[8] = 0.0, math.nan, -1.0, math.inf
+    u[9], u[10], u[11] = -0.001, 1.001, math.nan
+    p[12], q[13] = math.nan, math.nan
+    scale[14] = 2.0 ** 61
+    token, logp = run(x, u, scale, k, p, q)
+    assert bool((token[:15] == -1).all()) and int(token[15]) >= 0
+    assert float(logp[0]) == -math.inf and bool(torch.isnan(logp[1:15]).all()) and math.isfinite(float(logp[15]))
+
+
+@pytest.mark.parametrize("dtype", [F32, F16, BF16])
+@pytest.mark.parametrize("vocab", [3, 1000, 33000, 140000])
+def test_banned_tokens_are_never_drawn(dtype, vocab):
+    rows = 40
+    x = torch.randn((rows, vocab), device=DEV).to(dtype)
+    allowed = torch.randint(vocab, (rows,), device=DEV)
+    x.fill_(-math.inf)
+    x[torch.arange(rows, device=DEV), allowed] = 1.0
+    u = torch.linspace(0, 1, rows, device=DEV)
+    for limits in ((None, None, None, None), (None, full(rows, 2, I32), None, None), (None, None, full(rows, 0.5), None), (None, full(rows, 2, I32), full(rows, 0.99), full(rows, 0.5))):
+        token, logp = run(x, u, *limits)
+        assert torch.equal(token, allowed.int()) and bool((logp == 0).all())
+    low = torch.finfo(dtype).min
+    x = torch.where(x == 1.0, x, torch.full_like(x, low))  # finite masks
+    token, _ = run(x, u, full(rows, 1.0), full(rows, 2, I32), full(rows, 0.99), full(rows, 0.0))
+    assert torch.equal(token, allowed.int())
+
+
+@pytest.mark.parametrize("vocab", [4, 64, 1024, 4096, 65536, 131072])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_equal_logits_go_by_their_indices(vocab, dtype):
+    """Weights of 1: every sum is exact, and u or p may meet a border."""
+    rows = 9
+    x = torch.full((rows, vocab), 2.5, device=DEV, dtype=dtype)
+    u = torch.arange(rows, device=DEV) / 8.0
+    token, logp = run(x, u)
+    want = torch.clamp((u * vocab).floor(), max=vocab - 1).int()
+    assert torch.equal(token, want) and bool((logp.double() + math.log(vocab)).abs().max() <= 1e-6)
+    token, logp = run(x, u, None, full(rows, vocab // 2, I32))
+    assert torch.equal(token, torch.clamp((u * (vocab // 2)).floor(), max=vocab // 2 - 1).int())
+    token, logp = run(x, u, None, None, full(rows, 0.25))
+    assert torch.equal(token, torch.clamp((u * (vocab // 4)).floor(), max=vocab // 4 - 1).int())
+    token, logp = run(x, u, None, full(rows, vocab // 2, I32), full(rows, 0.5), full(rows, 1.0))
+    assert torch.equal(token, torch.clamp((u * (vocab // 4)).floor(), max=vocab // 4 - 1).int())
+    assert bool((logp.double() + math.log(vocab // 4)).abs().max() <= 1e-6)
+
+
+@pytest.mark.parametrize("vocab", [40, 3000, 90000])
+def test_ties_at_the_last_place(vocab):
+    """Two values; the limits cut within the smaller one."""
+    rows = 8
+    x = torch.full((rows, vocab), 0.0, device=DEV, dtype=BF16)
+    x[:, vocab // 3] = 1.0
+    u = torch.linspace(0, 1, rows, device=DEV)
+    for k in (1, 2, vocab // 2, vocab - 1):
+        check(run(x, u, None, full(rows, k, I32)), x, u, None, full(rows, k, I32))
+    for p in (0.001, 0.37, 0.5):
+        check(run(x, u, None, None, full(rows, p)), x, u, None, None, full(rows, p))
+        check(run(x, u, None, full(rows, vocab - 2, I32), full(rows, p)), x, u, None, full(rows, vocab - 2, I32), full(rows, p))
+
+
+@pytest.mark.parametrize("vocab", [50, 5000, 100000])
+def test_logits_that_differ_in_their_last_bits(vocab):
+    """fp32 logits closer to each other than their distance from the maximum can tell; and far apart."""
+    rows = 6
+    g = torch.Generator(device=DEV).manual_seed(vocab)
+    x = torch.full((rows, vocab), 1.0, device=DEV) + torch.randint(0, 60, (rows, vocab), generator=g, device=DEV) * 2.0 ** -23
+    x[:, 7] = 100.0
+    x[3:] = torch.randn((3, vocab), generator=g, device=DEV) * torch.tensor([[1e4], [1e-30], [1e30]], device=DEV)
+    u, k = torch.rand(rows, generator=g, device=DEV), full(rows, vocab // 2, I32)
+    scale = torch.tensor([2.0 ** -6, 0.03, 1.0, 1e-4, 2.0 ** 60, 2.0 ** -60], device=DEV)
+    for limits in ((scale, k, None, None), (scale, None, full(rows, 0.7), None), (scale, k, full(rows, 0.7), None)):
+        check(run(x, u, *limits), x, u, *limits)
+
+
+def test_every_token_comes_as_often_as_it_should():
+    vocab, rows = 10, 4096
+    row = torch.randn(vocab, device=DEV)
+    u = (torch.arange(rows, device=DEV) + 0.5) / rows
+    token, logp = run(row.expand(rows, vocab).contiguous(), u)
+    p = torch.softmax(row.double(), 0)
+    assert bool(((torch.bincount(token.long(), minlength=vocab) / rows - p).abs() <= 2 / rows).all())
+    assert bool((logp.double() - torch.log(p)[token.long()]).abs().max() <= 1e-6)
+
+
+@pytest.mark.parametrize("dtype", [F32, F16, BF16])
+def test_unaligned_rows_other_streams_and_graphs(dtype):
+    rows, vocab = 21, 9001
+    space = torch.randn(rows * 9003 + 1, device=DEV).to(dtype)
+    x = torch.as_strided(space, (rows, vocab), (9003, 1), 1)
+    _, u, scale, k, p, q = make((rows, vocab, dtype, vocab, 1.0))
+    d = lib.sm_desc_create(lib.SmParams(rows, vocab, dtype))
+    ws = torch.empty(lib.sm_desc_workspace_bytes(d) // 4 + 1, device=DEV)
+    token, logp = torch.empty(rows, device=DEV, dtype=I32), torch.empty(rows, device=DEV)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    lib.sm_sample(d, x, u, scale, k, p, q, token, logp, ws, side)
+    side.synchronize()
+    check((token, logp), x, u, scale, k, p, q)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        lib.sm_sample(d, x, u, scale, k, p, q, token, logp, ws)
+    for _ in range(3):
+        space.normal_()
+        u.uniform_()
+        k.copy_(k.roll(1))
+        graph.replay()
+        replayed = token.clone()
+        lib.sm_sample(d, x, u, scale, k, p, q, token, logp, ws)
+        torch.cuda.synchronize()
+        assert torch.equal(replayed, token)
+        check((token, logp), x, u, scale, k, p, q)
+
+
+def test_no_rows_and_far_rows():
+    d = lib.sm_desc_create(lib.SmParams(0, 100, F32))
+    lib.sm_sample(d, torch.empty((0, 100), device=DEV), torch.empty(0, device=DEV), None, None, None, None, torch.empty(0, device=DEV, dtype=I32))
+    x = torch.empty((2, 5000), device=DEV, dtype=BF16)  # rows more than 2^32 bytes apart
+    space = torch.zeros((1 << 31) + 6000, device=DEV, dtype=BF16)
+    far = torch.as_strided(space, (2, 5000), ((1 << 31) + 500, 1))
+    far[0, 11], far[1, 4999] = 50.0, 50.0
+    token, _ = run(far, full(2, 0.5))
+    assert token.tolist() == [11, 4999]
