@@ -1,8 +1,12 @@
 // Drawing tokens under a temperature, top-k, top-p and min-p from given uniform numbers (include/mi355sm.h).
 //
-// What is kept of a row is what its cut keeps, x > value or x = value and index <= last, and what min-p keeps: top-k and top-p only move the
-// cut.  Its place is found by a histogram of the distances below the maximum, finer ones of a bin that holds many logits, and an exact order of the
-// few of the last bin.  The token is then found from the weights' sums in the order of the indices: over groups of vectors, vectors, lanes, elements.
+// A first launch reads the rows once, in segments, and leaves each segment's maximum and sum of weights.  Where there is no limit the second one
+// finds the segment that the uniform number falls on, and the token in it.
+// What is kept under limits is what a cut keeps, x > value or x = value and index <= last, and what min-p keeps: top-k and top-p only move the
+// cut.  The second launch puts the logits near the maximum in a list, in the order of their indices; the cut's place in it is found by a histogram of the
+// distances below the maximum, finer ones of a bin that holds many, and an exact order of the few of the last bin; the token by the
+// sums of the list's weights.  Where the list does not hold what is kept, the same runs over the row itself.
+// Rows of a single segment take one launch, from shared memory.
 //
 // Weights are 64 bits wide: with 128256 tokens borders lie 2^-17 of the whole apart, and a uniform number falls within fp32's error of one in
 // every hundredth row.  exp(scale (x - m)) = 2^(n / 32) 2^(r / 32) with n a whole number and |r| <= 1/2: the 32 roots of 2 and a polynomial.
@@ -25,13 +29,23 @@
 
 struct sm_desc {
   sm_params_t p;
-  int32_t large;  // a team of 1024 threads for a row, not 256
+  int32_t segments;  // of a row (1: one launch)
+  int32_t chunks;    // of a segment
+  int32_t shift;     // weights as whole numbers: 2^shift, so that a row's sum stays below 2^62
+  size_t ws_bytes;
   char names[64];
 };
 
 namespace mi355conv {
 
 namespace {
+
+// What the first launch leaves of a segment: its largest logit (infinity if there is a NaN or an infinity), the least finite one, and the sum of
+// weights relative to its largest.
+struct Part {
+  float most, least;
+  double sum;
+};
 
 struct SmArgs {
   const void* logits;
@@ -40,14 +54,19 @@ struct SmArgs {
   const int32_t* top_k;
   int32_t* token;
   float* logp;
-  int32_t rows, vocab;
-  int32_t shift;  // weights as whole numbers: 2^shift, so that a row's sum stays below 2^62
+  Part* parts;  // [rows][segments]
+  float* tops;  // [rows][segments][kTops]: maxima of a segment's groups of threads
+  int32_t rows, vocab, segments, chunks, shift;
 };
 
-constexpr int kBins = 1024;       // of a histogram
-constexpr int kList = 1024;       // logits that are put in order
-constexpr int kGroups = 16;       // of a row's vectors, whose sums stand side by side
-constexpr float kNear = 8.f;      // nats below the maximum that the first histogram looks at: weights from 3e-4 on
+constexpr int kBins = 1024;     // of a histogram
+constexpr int kSorted = 1024;   // logits that are put in order
+constexpr int kList = 4096;     // logits near the maximum
+constexpr int kGroups = 16;     // of vectors, whose sums stand side by side
+constexpr int kTops = 16;       // groups of threads of a segment
+constexpr int kChunkVecs = 4;   // vectors of a thread of the first launch
+constexpr int kMostSegments = 256;
+constexpr float kNear = 8.f;    // nats below the maximum that the list holds: weights from 3e-4 on
 
 // 2^(i / 32), computed to 60 digits and rounded.
 __device__ const double kRoots[32] = {
@@ -99,104 +118,231 @@ __device__ __forceinline__ uint64_t wave_scan(uint64_t v) {
   return v + move_words(v, 5);
 }
 
-template <int THREADS, int HELD>
-struct TeamLds {
-  static constexpr int WAVES = THREADS / 64;
-  u32x4 held[HELD * THREADS];  // the row's first vectors, each read by the thread that wrote it
-  double part[kGroups][WAVES];
-  double root[32];
-  double sum[WAVES];
-  uint64_t whole[WAVES];
-  uint64_t list[kList];
-  uint64_t weight[kBins];
-  int count[kBins];
-  float most[WAVES], least[WAVES];
-  int number[WAVES];
-  uint32_t listed;
-  int found, before, inside;
-  double result;
-};
+// exp of the difference to the row's or segment's largest logit.
+struct Exponential {
+  const double* root;  // in shared memory
+  double top, c32;
 
-struct Cut {
-  float value;
-  int last;
-};
-
-template <int DTYPE, int THREADS, int HELD>
-struct Team {
-  typedef Elem<DTYPE> E;
-  typedef typename E::T T;
-  typedef TeamLds<THREADS, HELD> Lds;
-  static constexpr int VEC = E::VEC, WAVES = THREADS / 64;
-
-  Lds& lds;
-  const T* row;
-  int n, nv, rounds, tid, lane, wave, shift;
-  float m, scale;  // the maximum
-  double top, c32, q;
-  Cut cut;
-
-  __device__ u32x4 vec(int j) const {
-    const int v = j * THREADS + tid;
-    if (j < HELD) return lds.held[v];
-    return v < nv ? row_vec<E>(row, v, n) : lowest_vec<E>();
+  __device__ __forceinline__ void set(float largest, float scale) {
+    top = largest;
+    c32 = (double)scale * (32 * 1.44269504088896340736);
   }
 
-  // f(vector, its number) for this thread's vectors of the rounds [j0, j1), four loads at a time.
-  template <class F>
-  __device__ __forceinline__ void each(int j0, int j1, F&& f) const {
-    for (int j = j0; j < j1; j += 4) {
-      u32x4 x[4];
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-        if (j + i < j1) x[i] = vec(j + i);
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-        if (j + i < j1) {
-          f(x[i], (j + i) * THREADS + tid);
-          __builtin_amdgcn_sched_barrier(0);  // (vectors side by side would take more registers than there are)
-        }
-    }
-  }
-
-  __device__ __forceinline__ double weight(float x) const {
+  __device__ __forceinline__ double operator()(float x) const {
     const double t = fmax(((double)x - top) * c32, -36000.);  // (2^-1125 is 0)
     const double whole = rint(t), r = t - whole;
     const int i = (int)whole;
     constexpr double L = 0.69314718055994530942 / 32;
-    double p = L * L * L * L * L / 120;
+    double p = L * L * L * L * L / 120;  // the next term is below 2^-48.7
     p = fma(p, r, L * L * L * L / 24);
     p = fma(p, r, L * L * L / 6);
     p = fma(p, r, L * L / 2);
     p = fma(p, r, L);
     p = fma(p, r, 1.);
-    return ldexp(lds.root[i & 31] * p, i >> 5);
+    return ldexp(root[i & 31] * p, i >> 5);
+  }
+};
+
+template <int THREADS>
+struct Shared {
+  static constexpr int WAVES = THREADS / 64;
+  double root[32];
+  double sum[WAVES];
+  float most[WAVES], least[WAVES];
+};
+
+// Over the team, in the same order every time.
+template <int THREADS>
+__device__ __forceinline__ double team_sum(Shared<THREADS>& lds, double v) {
+  constexpr int WAVES = THREADS / 64;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  v = wave_sum(v);
+  __syncthreads();
+  if (lane == 0) lds.sum[wave] = v;
+  __syncthreads();
+  double all = lds.sum[0];
+#pragma unroll
+  for (int w = 1; w < WAVES; ++w) all += lds.sum[w];
+  return all;
+}
+
+template <int THREADS>
+__device__ __forceinline__ void team_range(Shared<THREADS>& lds, float& most, float& least) {
+  constexpr int WAVES = THREADS / 64;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  most = wave_most(most);
+  least = -wave_most(-least);
+  __syncthreads();
+  if (lane == 0) {
+    lds.most[wave] = most;
+    lds.least[wave] = least;
+  }
+  __syncthreads();
+  most = lds.most[0], least = lds.least[0];
+#pragma unroll
+  for (int w = 1; w < WAVES; ++w) {
+    most = fmaxf(most, lds.most[w]);
+    least = fminf(least, lds.least[w]);
+  }
+}
+
+__device__ __forceinline__ bool scale_is_good(float scale) { return scale >= 0x1p-60f && scale <= 0x1p60f; }
+
+// Vectors of a row [from, from + 256 kChunkVecs), thread by thread, into its range.
+template <class E>
+__device__ __forceinline__ void load_chunk(const typename E::T* row, int from, int nv, int n, u32x4 (&x)[kChunkVecs]) {
+#pragma unroll
+  for (int j = 0; j < kChunkVecs; ++j) {
+    const int v = from + j * 256 + (int)threadIdx.x;
+    x[j] = v < nv ? row_vec<E>(row, v, n) : lowest_vec<E>();
+  }
+}
+
+template <class E>
+__device__ __forceinline__ void chunk_range(const u32x4 (&x)[kChunkVecs], float& most, float& least) {
+  bool bad = false;
+#pragma unroll
+  for (int j = 0; j < kChunkVecs; ++j)
+#pragma unroll
+    for (int i = 0; i < E::VEC; ++i) {
+      const float logit = E::get(x[j], i);
+      bad |= !(logit < INFINITY);
+      most = fmaxf(most, logit);
+      least = logit > -INFINITY ? fminf(least, logit) : least;
+    }
+  if (bad) most = INFINITY;
+}
+
+template <class E>
+__device__ __forceinline__ double chunk_sum(const u32x4 (&x)[kChunkVecs], const Exponential& weight) {
+  double s = 0.;
+#pragma unroll
+  for (int j = 0; j < kChunkVecs; ++j) {
+#pragma unroll
+    for (int i = 0; i < E::VEC; ++i) s += weight(E::get(x[j], i));
+    __builtin_amdgcn_sched_barrier(0);  // (vectors side by side would take more registers than there are)
+  }
+  return s;
+}
+
+// The first launch: a workgroup for each segment.
+template <int DTYPE>
+__global__ __launch_bounds__(256) void sm_sums_kernel(SmArgs a) {
+  typedef Elem<DTYPE> E;
+  __shared__ Shared<256> lds;
+  const int tid = threadIdx.x;
+  if (tid < 32) lds.root[tid] = kRoots[tid];
+  const int n = a.vocab, nv = (n + E::VEC - 1) / E::VEC;
+  const int64_t items = (int64_t)a.rows * a.segments;
+  for (int64_t it = blockIdx.x; it < items; it += gridDim.x) {
+    const int r = (int)(it / a.segments), segment = (int)(it % a.segments);
+    const typename E::T* const row = static_cast<const typename E::T*>(a.logits) + (int64_t)r * a.stride;
+    const float scale = a.scale ? a.scale[r] : 1.f;
+    Exponential weight = {lds.root};
+    weight.set(0.f, scale_is_good(scale) ? scale : 1.f);
+    float most = -INFINITY, least = INFINITY, mine = -INFINITY;
+    double sum = 0.;
+    for (int c = 0; c < a.chunks; ++c) {
+      u32x4 x[kChunkVecs];
+      load_chunk<E>(row, (segment * a.chunks + c) * 256 * kChunkVecs, nv, n, x);
+      float here = -INFINITY;
+      chunk_range<E>(x, here, least);
+      mine = fmaxf(mine, here);
+      float all = here, all_least = least;
+      team_range<256>(lds, all, all_least);
+      if (all > most) {
+        if (most > -INFINITY && all < INFINITY) {
+          weight.top = all;
+          sum *= weight(most);
+        }
+        most = all;
+        weight.top = all;
+      }
+      least = all_least;
+      if (fabsf(most) < INFINITY) sum += chunk_sum<E>(x, weight);
+    }
+    const float top = group_most<16>(mine);
+    if ((tid & 15) == 0) a.tops[it * kTops + tid / 16] = top;
+    sum = team_sum<256>(lds, sum);
+    if (tid == 0) a.parts[it] = Part{most, least, sum};
+  }
+}
+
+struct Cut {
+  float value;
+  int last;  // an index of the row, or a place in the list
+};
+
+template <int THREADS, bool LIMITED, bool HELD>
+struct RowLds : Shared<THREADS> {
+  static constexpr int WAVES = THREADS / 64;
+  u32x4 held[HELD ? 256 * kChunkVecs : 1];  // rows of one segment
+  double part[kGroups][WAVES];
+  double segment[HELD ? 1 : kMostSegments];
+  uint64_t sorted[LIMITED ? kSorted : 1];
+  uint64_t weights[LIMITED ? kBins : 1];
+  int count[LIMITED ? kBins : 1];
+  float value[LIMITED ? kList : 1];  // the list: logits near the maximum and their indices, in the order of these
+  int index[LIMITED ? kList : 1];
+  uint64_t whole[WAVES];
+  int number[WAVES];
+  uint32_t places;
+  int found, before, inside;
+};
+
+template <int DTYPE, int THREADS, bool LIMITED, bool HELD>
+struct Team {
+  typedef Elem<DTYPE> E;
+  typedef typename E::T T;
+  typedef RowLds<THREADS, LIMITED, HELD> Lds;
+  static constexpr int VEC = E::VEC, WAVES = THREADS / 64, SHARE = kList / WAVES;  // of the list, for each wave
+
+  Lds& lds;
+  const T* row;
+  int n, nv, tid, lane, wave, shift;
+  float m, scale;  // the maximum
+  Exponential weight;
+  Cut cut;
+
+  __device__ __forceinline__ u32x4 vec(int v) const {
+    if constexpr (HELD) return lds.held[v];
+    return v < nv ? row_vec<E>(row, v, n) : lowest_vec<E>();
   }
 
-  __device__ __forceinline__ bool keeps(float x, int index) const { return x > cut.value || (x == cut.value && index <= cut.last); }
+  __device__ __forceinline__ bool keeps(float x, int at) const { return x > cut.value || (x == cut.value && at <= cut.last); }
 
   __device__ __forceinline__ float distance(float x) const { return fminf((m - x) * scale, FLT_MAX); }
 
-  // The sum over the team, in the same order every time.
-  __device__ double team_sum(double v) {
-    v = wave_sum(v);
-    __syncthreads();
-    if (lane == 0) lds.sum[wave] = v;
-    __syncthreads();
-    return wave_sum(lane < WAVES ? lds.sum[lane] : 0.);
+  // f(logit, index) for the elements of a vector, in order; compactly, two at a time.
+  template <class F>
+  __device__ __forceinline__ void elements(u32x4 x, int v, F&& f) const {
+    const Slot<E> at = slot_of<E>(v, n);
+#pragma unroll 1
+    for (int w = 0; w < 4; ++w) {
+      const u32x4 first = {x[0], 0, 0, 0};
+#pragma unroll
+      for (int i = 0; i < VEC / 4; ++i) f(E::get(first, i), at.base + w * (VEC / 4) + i);
+      x = u32x4{x[1], x[2], x[3], x[0]};
+    }
   }
 
-  __device__ void team_range(float& most, float& least) {
-    most = wave_most(most);
-    least = -wave_most(-least);
-    __syncthreads();
-    if (lane == 0) {
-      lds.most[wave] = most;
-      lds.least[wave] = least;
+  // The same for the whole row (LIST: what the list holds, with places for indices), by all threads.
+  template <bool LIST, class F>
+  __device__ __forceinline__ void each(int entries, F&& f) const {
+    if constexpr (LIST) {
+      for (int i = tid; i < entries; i += THREADS) f(lds.value[i], i);
+    } else {
+      for (int v0 = 0; v0 < nv; v0 += 4 * THREADS) {
+        u32x4 x[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) x[j] = v0 + j * THREADS + tid < nv ? vec(v0 + j * THREADS + tid) : lowest_vec<E>();
+#pragma unroll 1
+        for (int j = 0; j < 4; ++j) {
+          elements(x[0], v0 + j * THREADS + tid, f);
+          x[0] = x[1], x[1] = x[2], x[2] = x[3];
+        }
+      }
     }
-    __syncthreads();
-    most = wave_most(lane < WAVES ? lds.most[lane] : -INFINITY);
-    least = -wave_most(lane < WAVES ? -lds.least[lane] : -INFINITY);
   }
 
   // The groups' sums stand in the lanes: the first group with which they pass `target`, or the last one of any weight; target becomes what is left of
@@ -217,15 +363,23 @@ struct Team {
     return chosen;
   }
 
-  // The index of the first logit with which the sum of of(logit, index) passes the target: u times the whole (FRACTION), or as given.
+  // The same by a scan over 64 lanes.
+  __device__ static int pick_lane(double mine, double& target) {
+    const double up_to = wave_scan(mine);
+    const uint64_t some = __ballot(mine > 0.), passed = __ballot(mine > 0. && up_to > target);
+    const int chosen = passed ? __builtin_ctzll(passed) : 63 - __builtin_clzll(some | 1);
+    target -= read_lane(up_to - mine, chosen);
+    return chosen;
+  }
+
+  // The index of the first logit of the vectors [from, to) with which the sum of of(logit, index) passes the target: u times the whole
+  // (FRACTION), or as given.
   template <bool FRACTION, class W>
-  __device__ int locate(double target, W&& of, double& whole) {
-    int j0 = 0, j1 = rounds, place = 0;
-    auto of_vec = [&](const u32x4& x, int v) {
-      const Slot<E> at = slot_of<E>(v, n);
+  __device__ int locate(int from, int to, double target, W&& of, double& whole) {
+    int j0 = 0, j1 = (to - from + THREADS - 1) / THREADS, place = 0;
+    auto of_vec = [&](int v) {
       double s = 0.;
-#pragma unroll
-      for (int i = 0; i < VEC; ++i) s += of(E::get(x, i), at.base + i);
+      if (v < to) elements(vec(v), v, [&](float x, int at) { s += of(x, at); });
       return s;
     };
     bool first = FRACTION;
@@ -234,7 +388,7 @@ struct Team {
       __syncthreads();
       for (int g = 0; g < groups; ++g) {
         double s = 0.;
-        each(j0 + g * per, min(j0 + (g + 1) * per, j1), [&](const u32x4& x, int v) { s += of_vec(x, v); });
+        for (int j = j0 + g * per; j < min(j0 + (g + 1) * per, j1); ++j) s += of_vec(from + j * THREADS + tid);
         s = wave_sum(s);
         if (lane == 0) lds.part[g][wave] = s;
       }
@@ -256,25 +410,20 @@ struct Team {
       }
     }
     if (wave == place) {
-      const u32x4 x = vec(j0);
-      const int v = j0 * THREADS + tid;
-      const double mine = of_vec(x, v), up_to = wave_scan(mine);
-      const uint64_t some = __ballot(mine > 0.), passed = __ballot(mine > 0. && up_to > target);
-      const int at_lane = passed ? __builtin_ctzll(passed) : 63 - __builtin_clzll(some | 1);
+      const int v = from + j0 * THREADS + tid;
+      const int at_lane = pick_lane(of_vec(v), target);
       if (lane == at_lane) {
-        const Slot<E> at = slot_of<E>(v, n);
-        double sum = up_to - mine;
-        int index = at.base + VEC - 1;
+        double sum = 0.;
+        int index = 0;
         bool done = false;
-#pragma unroll
-        for (int i = 0; i < VEC; ++i) {
-          const double w = of(E::get(x, i), at.base + i);
+        elements(vec(v), v, [&](float x, int at) {
+          const double w = of(x, at);
           sum += w;
           if (w > 0. && !done) {
-            index = at.base + i;
+            index = at;
             done = sum > target;
           }
-        }
+        });
         lds.found = index;
       }
     }
@@ -282,28 +431,40 @@ struct Team {
     return lds.found;
   }
 
-  // The first `entries` of the list in descending order.
-  __device__ void sort_list(int entries) {
-    int size = 2;
+  // lds.sorted in descending order: by a wave where they are few, which counts those above each.
+  __device__ void sort(int entries) {
+    __syncthreads();
+    if (entries <= 64) {
+      if (wave == 0) {
+        const uint64_t mine = lane < entries ? lds.sorted[lane] : 0;
+        int rank = 0;
+        for (int o = 0; o < entries; ++o) rank += read_lane(mine, o) > mine ? 1 : 0;
+        wave_sync();
+        if (lane < entries) lds.sorted[rank] = mine;
+      }
+      __syncthreads();
+      return;
+    }
+    int size = 128;
     while (size < entries) size *= 2;
-    for (int i = entries + tid; i < size; i += THREADS) lds.list[i] = 0;
+    for (int i = entries + tid; i < size; i += THREADS) lds.sorted[i] = 0;
     for (int k = 2; k <= size; k *= 2)
       for (int j = k / 2; j > 0; j /= 2) {
         __syncthreads();
         for (int i = tid; i < size / 2; i += THREADS) {
           const int a = 2 * i - (i & (j - 1)), b = a + j;
-          const uint64_t x = lds.list[a], y = lds.list[b];
+          const uint64_t x = lds.sorted[a], y = lds.sorted[b];
           if ((x < y) == ((a & k) == 0)) {
-            lds.list[a] = y;
-            lds.list[b] = x;
+            lds.sorted[a] = y;
+            lds.sorted[b] = x;
           }
         }
       }
     __syncthreads();
   }
 
-  // The bin in which the counts (WEIGHT: the weights) pass the target, counted from `carry` on: its number, or -1; lds.before and lds.inside are
-  // the count before it and its own.  carry goes on to the end of the bins.
+  // The first bin with which the counts (WEIGHT: the weights) reach the target, counted from `carry` on: its number, or -1 (`surely`: the last bin that
+  // holds any); lds.before and lds.inside are the count before it and its own.  The carries go on to the end of the bins.
   template <bool WEIGHT>
   __device__ int find_bin(uint64_t target, uint64_t& carry, int& count_carry, bool surely) {
     constexpr int PER = kBins / THREADS;
@@ -313,7 +474,7 @@ struct Team {
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
       counts[i] = lds.count[tid * PER + i];
-      values[i] = WEIGHT ? lds.weight[tid * PER + i] : (uint64_t)counts[i];
+      values[i] = WEIGHT ? lds.weights[tid * PER + i] : (uint64_t)counts[i];
       count += counts[i];
       value += values[i];
     }
@@ -323,7 +484,10 @@ struct Team {
       lds.number[wave] = count_to;
       lds.whole[wave] = value_to;
     }
-    if (tid == 0) lds.found = INT_MAX;
+    if (tid == 0) {
+      lds.found = INT_MAX;
+      lds.places = 0;
+    }
     __syncthreads();
     int count_before = count_carry, count_all = count_carry;
     uint64_t before = carry, all = carry;
@@ -336,41 +500,23 @@ struct Team {
       count_all += lds.number[w];
       all += lds.whole[w];
     }
+    if (surely && all < target) target = all;  // (a rounding)
     count_before += count_to - count;
     before += value_to - value;
-    int mine = INT_MAX, last = -1, mine_before = 0, mine_count = 0;
+    int mine = INT_MAX, mine_before = 0, mine_count = 0;
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
       before += values[i];
-      if (counts[i] > 0) {
-        last = tid * PER + i;
-        if (mine == INT_MAX && before >= target) {
-          mine = last;
-          mine_before = count_before;
-          mine_count = counts[i];
-        }
+      if (mine == INT_MAX && counts[i] > 0 && before >= target) {
+        mine = tid * PER + i;
+        mine_before = count_before;
+        mine_count = counts[i];
       }
       count_before += counts[i];
     }
     if (mine != INT_MAX) atomicMin(&lds.found, mine);
     __syncthreads();
-    int found = lds.found;
-    if (found == INT_MAX && surely) {  // (a rounding: the last bin that holds any)
-      __syncthreads();
-      if (tid == 0) lds.found = -1;
-      __syncthreads();
-      if (last >= 0) atomicMax(&lds.found, last);
-      __syncthreads();
-      found = lds.found;
-      if (found == last && found >= 0) {
-        mine = found;
-        mine_count = lds.count[found];
-        mine_before = count_before - mine_count;
-#pragma unroll
-        for (int i = 0; i < PER; ++i)
-          if (tid * PER + i > found) mine_before -= counts[i];
-      }
-    }
+    const int found = lds.found;
     if (mine == found && mine != INT_MAX) {
       lds.before = mine_before;
       lds.inside = mine_count;
@@ -385,140 +531,147 @@ struct Team {
     __syncthreads();
     for (int i = tid; i < kBins; i += THREADS) {
       lds.count[i] = 0;
-      lds.weight[i] = 0;
+      lds.weights[i] = 0;
     }
-    if (tid == 0) lds.listed = 0;
     __syncthreads();
   }
 
   __device__ __forceinline__ uint64_t fixed(double w) const { return (uint64_t)ldexp(w, shift); }
 
-  // Moves the cut to where the counts (WEIGHT: the weights) of what it keeps reach the target, in descending order.  least: the least finite logit.
   template <bool WEIGHT>
-  __device__ void find_cut(double target, float least) {
+  __device__ __forceinline__ void count_in(int b, float logit) {
+    atomicAdd(&lds.count[b], 1);
+    if (WEIGHT) atomicAdd((unsigned long long*)&lds.weights[b], (unsigned long long)fixed(weight(logit)));
+  }
+
+  // Moves the cut to where the counts (WEIGHT: the weights) of what it keeps reach the target, in descending order.  least: the least finite logit.
+  // False where they do not reach it.
+  template <bool WEIGHT, bool LIST>
+  __device__ bool find_cut(double target, float least, int entries) {
     // the first histograms: by distance, near the maximum, then beyond
     const float end = distance(least);
     float from = 0.f, per = 0.f;
     uint64_t carry = 0;
     int count_carry = 0, bin = -1;
     for (int phase = 0; phase < 2 && bin < 0; ++phase) {
-      const float to = phase == 0 ? fminf(kNear, end) : end;
       if (phase == 1 && end <= kNear) break;
+      const float to = phase == 0 ? fminf(kNear, end) : end;
       from = phase == 0 ? 0.f : kNear;
       per = to > from ? fminf(kBins / (to - from), FLT_MAX) : 0.f;
       clear_bins();
-      each(0, rounds, [&](const u32x4& x, int v) {
-        const Slot<E> at = slot_of<E>(v, n);
-#pragma unroll
-        for (int i = 0; i < VEC; ++i) {
-          const float logit = E::get(x, i), d = distance(logit);
-          if (logit > -INFINITY && (phase == 0 ? d <= to : d > from) && keeps(logit, at.base + i)) {
-            const int b = min((int)((d - from) * per), kBins - 1);
-            atomicAdd(&lds.count[b], 1);
-            if (WEIGHT) atomicAdd((unsigned long long*)&lds.weight[b], (unsigned long long)fixed(weight(logit)));
-          }
-        }
+      each<LIST>(entries, [&](float logit, int at) {
+        const float d = distance(logit);
+        if (logit > -INFINITY && (phase == 0 ? d <= to : d > from) && keeps(logit, at)) count_in<WEIGHT>(min((int)((d - from) * per), kBins - 1), logit);
       });
       bin = find_bin<WEIGHT>(WEIGHT ? fixed(target) : (uint64_t)target, carry, count_carry, false);
     }
-    if (bin < 0) return;  // all that there is
+    if (bin < 0) return false;
     bool by_key = false;
-    uint32_t high = 0;  // by key: bins of (high - key) >> bits
+    uint32_t high = 0, low = 0;  // by key: bins of (high - key) >> bits
     int bits = 0, above = lds.before, inside = lds.inside;
     const bool far = from > 0.f;
-    uint32_t low = 0;
-    while (bin >= 0) {
-      // what the bin holds: in the list if it is few; their range; the weight above them
-      __syncthreads();
-      if (tid == 0) lds.listed = 0;
-      __syncthreads();
+    for (;;) {
+      // what the bin holds: to be sorted if it is few; their range; the weight above them
       float most = -INFINITY, least_in = INFINITY;
       double sum = 0.;
-      each(0, rounds, [&](const u32x4& x, int v) {
-        const Slot<E> at = slot_of<E>(v, n);
-#pragma unroll
-        for (int i = 0; i < VEC; ++i) {
-          const float logit = E::get(x, i);
-          if (!(logit > -INFINITY) || !keeps(logit, at.base + i)) continue;
-          int side;  // below 0: above the bin
-          if (by_key) {
-            const uint32_t key = order_key(logit);
-            side = key > high ? -1 : key < low ? 1 : (int)((high - key) >> bits) - bin;
-          } else {
-            const float d = distance(logit);
-            const bool other = far ? d <= from : d > kNear;
-            side = other ? (far ? -1 : 1) : min((int)((d - from) * per), kBins - 1) - bin;
-          }
-          if (WEIGHT && side < 0) sum += weight(logit);
-          if (side == 0) {
-            most = fmaxf(most, logit);
-            least_in = fminf(least_in, logit);
-            if (inside <= kList) {
-              const uint32_t place = atomicAdd(&lds.listed, 1u);
-              if (place < (uint32_t)kList) lds.list[place] = entry_of(logit, at.base + i);
-            }
+      each<LIST>(entries, [&](float logit, int at) {
+        if (!(logit > -INFINITY) || !keeps(logit, at)) return;
+        int side;  // below 0: above the bin
+        if (by_key) {
+          const uint32_t key = order_key(logit);
+          side = key > high ? -1 : key < low ? 1 : (int)((high - key) >> bits) - bin;
+        } else {
+          const float d = distance(logit);
+          side = (far ? d <= from : d > kNear) ? (far ? -1 : 1) : min((int)((d - from) * per), kBins - 1) - bin;
+        }
+        if (WEIGHT && side < 0) sum += weight(logit);
+        if (side == 0) {
+          most = fmaxf(most, logit);
+          least_in = fminf(least_in, logit);
+          if (inside <= kSorted) {
+            const uint32_t place = atomicAdd(&lds.places, 1u);
+            if (place < (uint32_t)kSorted) lds.sorted[place] = entry_of(logit, at);
           }
         }
       });
-      if (WEIGHT) sum = team_sum(sum);
-      if (inside <= kList) {
-        __syncthreads();
-        sort_list(inside);
+      if (WEIGHT) sum = team_sum<THREADS>(lds, sum);
+      if (inside <= kSorted) {
+        sort(inside);
         int place = (int)target - above - 1;
-        if (WEIGHT) place = list_place(inside, sum, target);
-        place = max(0, min(place, inside - 1));
-        const uint64_t entry = lds.list[place];
+        if (WEIGHT) place = sorted_place(inside, sum, target);
+        const uint64_t entry = lds.sorted[max(0, min(place, inside - 1))];
         cut.value = key_value((uint32_t)(entry >> 32));
         cut.last = (int)(0xFFFFFFFFu - (uint32_t)entry);
-        return;
+        return true;
       }
-      team_range(most, least_in);
+      team_range<THREADS>(lds, most, least_in);
       if (most == least_in) {  // equal ones: by their indices
         double order = target - above;
         if (WEIGHT) order = fmin(fmax(ceil((target - sum) / weight(most)), 1.), (double)inside);
         const Cut kept = cut;
-        double whole;
-        const int index = locate<false>(order - 0.5, [&](float x, int at) { return x == most && keeps(x, at) ? 1. : 0.; }, whole);
+        cut.last = nth_equal<LIST>(most, (int)order, entries);
         cut.value = most;
-        cut.last = most == kept.value ? min(index, kept.last) : index;
-        return;
+        if (most == kept.value) cut.last = min(cut.last, kept.last);
+        return true;
       }
-      const uint32_t next_high = order_key(most), next_low = order_key(least_in);
       by_key = true;
-      high = next_high;
-      low = next_low;
+      high = order_key(most);
+      low = order_key(least_in);
       bits = max(0, 32 - __builtin_clz(high - low) - 10);
       clear_bins();
-      each(0, rounds, [&](const u32x4& x, int v) {
-        const Slot<E> at = slot_of<E>(v, n);
-#pragma unroll
-        for (int i = 0; i < VEC; ++i) {
-          const float logit = E::get(x, i);
-          const uint32_t key = order_key(logit);
-          if (key <= high && key >= low && keeps(logit, at.base + i)) {
-            const int b = (int)((high - key) >> bits);
-            atomicAdd(&lds.count[b], 1);
-            if (WEIGHT) atomicAdd((unsigned long long*)&lds.weight[b], (unsigned long long)fixed(weight(logit)));
-          }
-        }
+      each<LIST>(entries, [&](float logit, int at) {
+        const uint32_t key = order_key(logit);
+        if (key <= high && key >= low && keeps(logit, at)) count_in<WEIGHT>((int)((high - key) >> bits), logit);
       });
-      uint64_t none = 0;
-      int count_above = above;
-      if (!WEIGHT) none = (uint64_t)above;
-      bin = find_bin<WEIGHT>(WEIGHT ? fixed(fmax(target - sum, 0.)) : (uint64_t)target, none, count_above, true);
+      uint64_t before = WEIGHT ? 0 : (uint64_t)above;
+      int count_before = above;
+      bin = find_bin<WEIGHT>(WEIGHT ? fixed(fmax(target - sum, 0.)) : (uint64_t)target, before, count_before, true);
+      if (bin < 0) return false;
       above = lds.before;
       inside = lds.inside;
     }
   }
 
-  // The list's first place with which the weights reach the target, counted from `sum` on.
-  __device__ int list_place(int entries, double sum, double target) {
-    constexpr int PER = kList / THREADS;
+  // The index of the order-th (from 1) of the logits that equal x, all of which the cut keeps.
+  template <bool LIST>
+  __device__ int nth_equal(float x, int order, int entries) {
+    if constexpr (LIST) {  // places in turns of the team
+      int before = 0;
+      for (int i0 = 0; i0 < entries; i0 += THREADS) {
+        const bool mine = i0 + tid < entries && lds.value[i0 + tid] == x;
+        const uint64_t mask = __ballot(mine);
+        __syncthreads();
+        if (lane == 0) lds.number[wave] = (int)__builtin_popcountll(mask);
+        __syncthreads();
+        int here = before + (int)__builtin_popcountll(mask & ((2ull << lane) - 1));
+#pragma unroll
+        for (int w = 0; w < WAVES; ++w) {
+          if (w < wave) here += lds.number[w];
+          before += lds.number[w];
+        }
+        if (mine && here == order) lds.found = i0 + tid;
+      }
+      __syncthreads();
+      return lds.found;
+    } else {
+      double whole;
+      return locate<false>(0, nv, order - 0.5, [&](float logit, int at) { return logit == x && keeps(logit, at) ? 1. : 0.; }, whole);
+    }
+  }
+
+  // The first place of lds.sorted with which the weights reach the target, counted from `sum` on.
+  __device__ int sorted_place(int entries, double sum, double target) {
+    if (entries <= 64) {
+      const double w = lane < entries ? weight(key_value((uint32_t)(lds.sorted[lane] >> 32))) : 0.;
+      const uint64_t reached = __ballot(lane < entries && sum + wave_scan(w) >= target);
+      return reached ? __builtin_ctzll(reached) : entries - 1;
+    }
+    constexpr int PER = kSorted / THREADS;
     double w[PER], mine = 0.;
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
       const int at = tid * PER + i;
-      w[i] = at < entries ? weight(key_value((uint32_t)(lds.list[at] >> 32))) : 0.;
+      w[i] = at < entries ? weight(key_value((uint32_t)(lds.sorted[at] >> 32))) : 0.;
       mine += w[i];
     }
     const double to = wave_scan(mine);
@@ -541,53 +694,179 @@ struct Team {
     __syncthreads();
     return lds.found;
   }
+
+  // Logits from `bound` on into the list, in the order of their indices: each wave takes a part of the row and fills a part of the list, which are then
+  // moved together.  The number of them, or -1 where a wave found more than its part holds.
+  __device__ int fill_list(float bound) {
+    const int per = ((nv + WAVES - 1) / WAVES + 63) / 64 * 64, to = min(nv, (wave + 1) * per);
+    int mine = 0;
+    __syncthreads();
+    for (int v0 = wave * per; v0 < to && mine <= SHARE; v0 += 4 * 64) {
+      u32x4 x[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) x[j] = v0 + j * 64 + lane < to ? vec(v0 + j * 64 + lane) : lowest_vec<E>();
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        uint32_t mask = 0;
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) mask |= E::get(x[j], i) >= bound ? 1u << i : 0u;
+        if (__ballot(mask != 0) == 0) continue;
+        const int count = __builtin_popcount(mask), up_to = wave_scan(count);
+        int place = mine + up_to - count;
+        const Slot<E> at = slot_of<E>(v0 + j * 64 + lane, n);
+#pragma unroll
+        for (int i = 0; i < VEC; ++i)
+          if (mask >> i & 1) {
+            if (place < SHARE) {
+              lds.value[wave * SHARE + place] = E::get(x[j], i);
+              lds.index[wave * SHARE + place] = at.base + i;
+            }
+            ++place;
+          }
+        mine += read_lane(up_to, 63);
+      }
+    }
+    if (lane == 0) lds.number[wave] = mine;
+    __syncthreads();
+    int before = 0, all = 0;
+    bool over = false;
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) {
+      const int count = lds.number[w];
+      over |= count > SHARE;
+      before += w < wave ? count : 0;
+      all += count;
+    }
+    if (over) return -1;
+    float value[SHARE / 64];
+    int index[SHARE / 64];
+#pragma unroll
+    for (int i = 0; i < SHARE / 64; ++i)
+      if (i * 64 + lane < mine) {
+        value[i] = lds.value[wave * SHARE + i * 64 + lane];
+        index[i] = lds.index[wave * SHARE + i * 64 + lane];
+      }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < SHARE / 64; ++i)
+      if (i * 64 + lane < mine) {
+        lds.value[before + i * 64 + lane] = value[i];
+        lds.index[before + i * 64 + lane] = index[i];
+      }
+    __syncthreads();
+    return all;
+  }
+
+  // The sum of the weights that the cut keeps.
+  template <bool LIST>
+  __device__ double kept_sum(int entries) {
+    double sum = 0.;
+    each<LIST>(entries, [&](float logit, int at) {
+      if (keeps(logit, at)) sum += weight(logit);
+    });
+    return team_sum<THREADS>(lds, sum);
+  }
+
+  // The place in the list of the token.
+  __device__ int locate_in_list(double u, double q, int entries, double& whole) {
+    // each thread a run of the list
+    const int per = (entries + THREADS - 1) / THREADS, from = min(tid * per, entries), to = min(from + per, entries);
+    auto of = [&](int i) {
+      const float x = lds.value[i];
+      const double w = keeps(x, i) ? weight(x) : 0.;
+      return w >= q ? w : 0.;
+    };
+    double mine = 0.;
+    for (int i = from; i < to; ++i) mine += of(i);
+    const double sum = wave_sum(mine);
+    __syncthreads();
+    if (lane == 0) lds.part[0][wave] = sum;
+    __syncthreads();
+    const double s = lane < WAVES ? lds.part[0][lane] : 0.;
+    whole = wave_sum(s);
+    double target = u * whole;
+    const int place = pick(s, WAVES, target);
+    if (wave == place) {
+      const int at_lane = pick_lane(mine, target);
+      if (lane == at_lane) {
+        double reached = 0.;
+        int chosen = from;
+        for (int i = from; i < to; ++i) {
+          const double w = of(i);
+          reached += w;
+          if (w > 0.) {
+            chosen = i;
+            if (reached > target) break;
+          }
+        }
+        lds.found = chosen;
+      }
+    }
+    __syncthreads();
+    return lds.found;
+  }
+
+  // A bound that at least k logits reach, from the maxima of `groups` groups: the leading 16 bits of the k-th largest one, where every lane takes
+  // the larger ones of four shares of them.
+  __device__ float bound_of(const float* tops, int groups, int k) {
+    if (min(groups, 256) < k) return -INFINITY;
+    uint32_t keys[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      float most = -INFINITY;
+      for (int g = i * 64 + lane; g < groups; g += 256) most = fmaxf(most, tops[g]);
+      keys[i] = order_key(most);
+    }
+    uint32_t bound = 0;
+    for (int bit = 31; bit >= 16; --bit) {
+      const uint32_t with = bound | 1u << bit;
+      int count = 0;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) count += (int)__builtin_popcountll(__ballot(keys[i] >= with));
+      if (count >= k) bound = with;
+    }
+    return bound <= 0x007FFFFFu ? -INFINITY : key_value(bound);  // (the key of -inf and the unused ones below it)
+  }
 };
 
-// A row for a team of threads, which reads it once from memory and keeps its first HELD vectors a thread in shared memory.
-template <int DTYPE, int THREADS, int HELD>
+// The second launch (HELD: the only one, of rows of one segment): a team for each row.
+template <int DTYPE, int THREADS, bool LIMITED, bool HELD>
 __global__ __launch_bounds__(THREADS) void sm_row_kernel(SmArgs a) {
   typedef Elem<DTYPE> E;
-  typedef Team<DTYPE, THREADS, HELD> Rows;
-  __shared__ TeamLds<THREADS, HELD> lds;
+  __shared__ RowLds<THREADS, LIMITED, HELD> lds;
   const int tid = threadIdx.x;
   if (tid < 32) lds.root[tid] = kRoots[tid];
   for (int r = blockIdx.x; r < a.rows; r += gridDim.x) {
-    Rows t = {lds};
+    Team<DTYPE, THREADS, LIMITED, HELD> t = {lds};
     t.tid = tid;
     t.lane = tid & 63;
     t.wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     t.row = static_cast<const typename E::T*>(a.logits) + (int64_t)r * a.stride;
     t.n = a.vocab;
     t.nv = (a.vocab + E::VEC - 1) / E::VEC;
-    t.rounds = (t.nv + THREADS - 1) / THREADS;
     t.shift = a.shift;
-    const float scale = a.scale ? a.scale[r] : 1.f, u = a.u[r], p = a.top_p ? a.top_p[r] : 1.f, q = a.min_p ? a.min_p[r] : 0.f;
-    const int k = a.top_k ? a.top_k[r] : 0;
+    const float scale = a.scale ? a.scale[r] : 1.f, u = a.u[r];
+    const float p = LIMITED && a.top_p ? a.top_p[r] : 1.f, q = LIMITED && a.min_p ? a.min_p[r] : 0.f;
+    const int k = LIMITED && a.top_k ? a.top_k[r] : 0;
+    const bool bad = !scale_is_good(scale) || !(u >= 0.f && u <= 1.f) || p != p || q != q;
+    const Part* const parts = a.parts + (int64_t)r * a.segments;
 
     __syncthreads();  // the row before this one
     float most = -INFINITY, least = INFINITY;
-    bool bad = !(scale >= 0x1p-60f && scale <= 0x1p60f) || !(u >= 0.f && u <= 1.f) || p != p || q != q;
-    for (int j0 = 0; j0 < t.rounds; j0 += 4) {
-      u32x4 x[4];
+    u32x4 x[kChunkVecs];
+    Part part = {-INFINITY, INFINITY, 0.};
+    if constexpr (HELD) {
+      load_chunk<E>(t.row, 0, t.nv, t.n, x);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int v = (j0 + i) * THREADS + tid;
-        x[i] = v < t.nv ? row_vec<E>(t.row, v, t.n) : lowest_vec<E>();
-      }
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        if (j0 + i < HELD) lds.held[(j0 + i) * THREADS + tid] = x[i];
-#pragma unroll
-        for (int e = 0; e < E::VEC; ++e) {
-          const float logit = E::get(x[i], e);
-          bad |= !(logit < INFINITY);
-          most = fmaxf(most, logit);
-          least = logit > -INFINITY ? fminf(least, logit) : least;
-        }
-      }
+      for (int j = 0; j < kChunkVecs; ++j) lds.held[j * 256 + tid] = x[j];
+      chunk_range<E>(x, most, least);
+    } else if (tid < a.segments) {
+      part = parts[tid];
+      most = part.most;
+      least = part.least;
     }
     if (bad) most = INFINITY;
-    t.team_range(most, least);
+    team_range<THREADS>(lds, most, least);
     if (!(fabsf(most) < INFINITY)) {
       if (tid == 0) {
         a.token[r] = -1;
@@ -596,36 +875,107 @@ __global__ __launch_bounds__(THREADS) void sm_row_kernel(SmArgs a) {
       continue;
     }
     t.m = most;
-    t.top = most;
     t.scale = scale;
-    t.c32 = (double)scale * (32 * 1.44269504088896340736);
-    t.q = fmin((double)q, 1.);
+    t.weight.root = lds.root;
+    t.weight.set(most, scale);
     t.cut = Cut{-INFINITY, INT_MAX};
-    if (k > 0 && k < t.n) t.template find_cut<false>((double)k, least);
-    if (p < 1.f) {
-      double sum = 0.;
-      t.each(0, t.rounds, [&](const u32x4& x, int v) {
-        const Slot<E> at = slot_of<E>(v, t.n);
-#pragma unroll
-        for (int i = 0; i < E::VEC; ++i) {
-          const float logit = E::get(x, i);
-          if (t.keeps(logit, at.base + i)) sum += t.weight(logit);
+    double whole = 0.;
+    int token = -1;
+
+    if constexpr (LIMITED) {
+      const double least_weight = fmin((double)q, 1.);
+      const bool by_count = k > 0 && k < t.n, by_weight = p < 1.f;
+      double all = 0.;
+      if (by_weight && !by_count) {
+        if constexpr (HELD)
+          all = team_sum<THREADS>(lds, chunk_sum<E>(x, t.weight));
+        else
+          all = team_sum<THREADS>(lds, tid < a.segments ? part.sum * t.weight(part.most) : 0.);
+      }
+      // what the list has to hold: all that min-p keeps, or k logits, or those near the maximum; rows of one segment fit it as they are
+      float bound = -INFINITY;
+      bool complete = false;  // all that min-p keeps
+      if (by_count || by_weight || q > 0.f) {
+        bound = most - kNear / scale;
+        if (by_count && !HELD) bound = fmaxf(bound, t.bound_of(a.tops + (int64_t)r * a.segments * kTops, a.segments * kTops, k));
+        if (q > 0.f) {
+          const float low = most + (logf(fminf(q, 1.f)) * 1.00001f - 1e-5f) / scale;  // (below the border, whatever the roundings)
+          const float lower = low - fabsf(low) * 1e-6f;
+          complete = lower >= bound;
+          bound = fmaxf(bound, lower);
         }
-      });
-      t.template find_cut<true>(fmax(t.team_sum(sum) * (double)p, 0.), least);
-    }
-    double whole;
-    const int token = t.template locate<true>(
-        (double)u,
-        [&](float x, int at) {
-          double w = 0.;
-          if (t.keeps(x, at)) {
-            w = t.weight(x);
-            w = w >= t.q ? w : 0.;
+        bound = fminf(fmaxf(bound, -FLT_MAX), most);
+      }
+      int entries = -1;
+      if (bound > -INFINITY) entries = t.fill_list(bound);
+      if (entries >= 0) {
+        bool enough = by_count || by_weight || complete;
+        const float lowest = bound;
+        if (by_count) {
+          if (k < entries)
+            enough = t.template find_cut<false, true>((double)k, lowest, entries);
+          else
+            enough = k == entries || complete;
+        }
+        if (enough && by_weight) {
+          const double kept = t.template kept_sum<true>(entries), target = fmax((by_count ? kept : all) * (double)p, 0.);
+          if (by_count && k > entries)
+            enough = false;  // (the weight of k logits is not known)
+          else if (target <= kept)
+            t.template find_cut<true, true>(target, lowest, entries);
+          else
+            enough = complete;
+        }
+        if (enough)
+          token = lds.index[t.locate_in_list((double)u, least_weight, entries, whole)];
+        else
+          t.cut = Cut{-INFINITY, INT_MAX};
+      }
+      if (token < 0) {
+        if (by_count) t.template find_cut<false, false>((double)k, least, 0);
+        if (by_weight) t.template find_cut<true, false>(fmax((by_count ? t.template kept_sum<false>(0) : all) * (double)p, 0.), least, 0);
+        token = t.template locate<true>(
+            0, t.nv, (double)u,
+            [&](float logit, int at) {
+              const double w = t.keeps(logit, at) ? t.weight(logit) : 0.;
+              return w >= least_weight ? w : 0.;
+            },
+            whole);
+      }
+    } else {
+      auto plain = [&](float logit, int) { return t.weight(logit); };
+      if constexpr (HELD) {
+        token = t.template locate<true>(0, t.nv, (double)u, plain, whole);
+      } else {
+        if (tid < kMostSegments) lds.segment[tid] = tid < a.segments ? part.sum * t.weight(part.most) : 0.;
+        __syncthreads();
+        double four[4], mine = 0.;  // of four segments
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          four[i] = lds.segment[4 * t.lane + i];
+          mine += four[i];
+        }
+        whole = wave_sum(mine);
+        double target = (double)u * whole;
+        const int lane = t.pick_lane(mine, target);
+        double before = 0., sum = 0.;
+        int chosen = 0;
+        bool done = false;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const double s = read_lane(four[i], lane);
+          if (s > 0. && !done) {
+            chosen = i;
+            before = sum;
+            sum += s;
+            done = sum > target;
           }
-          return w;
-        },
-        whole);
+        }
+        const int per = a.chunks * 256 * kChunkVecs, from = (4 * lane + chosen) * per;
+        double ignored;
+        token = t.template locate<false>(from, min(from + per, t.nv), target - before, plain, ignored);
+      }
+    }
     if (tid == 0) {
       a.token[r] = token;
       if (a.logp) a.logp[r] = (float)log(t.weight(E::to_float(t.row[token])) / whole);
@@ -633,14 +983,23 @@ __global__ __launch_bounds__(THREADS) void sm_row_kernel(SmArgs a) {
   }
 }
 
+template <int DTYPE, bool LIMITED>
+int launch_rows(const sm_desc* d, const SmArgs& a, hipStream_t stream) {
+  const dim3 grid(std::min(a.rows, 1 << 20));
+  if (d->segments == 1 && d->chunks == 1) {
+    hipLaunchKernelGGL((sm_row_kernel<DTYPE, 256, LIMITED, true>), grid, dim3(256), 0, stream, a);
+    return (int)hipGetLastError();
+  }
+  hipLaunchKernelGGL(sm_sums_kernel<DTYPE>, dim3((uint32_t)std::min<int64_t>((int64_t)a.rows * a.segments, 1 << 22)), dim3(256), 0, stream, a);
+  const int e = (int)hipGetLastError();
+  if (e) return e;
+  hipLaunchKernelGGL((sm_row_kernel<DTYPE, LIMITED ? 512 : 256, LIMITED, false>), grid, dim3(LIMITED ? 512 : 256), 0, stream, a);
+  return (int)hipGetLastError();
+}
+
 template <int DTYPE>
 int launch(const sm_desc* d, const SmArgs& a, hipStream_t stream) {
-  const dim3 grid(std::min(a.rows, 1 << 20));
-  if (d->large)
-    hipLaunchKernelGGL((sm_row_kernel<DTYPE, 1024, 8>), grid, dim3(1024), 0, stream, a);
-  else
-    hipLaunchKernelGGL((sm_row_kernel<DTYPE, 256, 4>), grid, dim3(256), 0, stream, a);
-  return (int)hipGetLastError();
+  return a.top_k || a.top_p || a.min_p ? launch_rows<DTYPE, true>(d, a, stream) : launch_rows<DTYPE, false>(d, a, stream);
 }
 
 }  // namespace
@@ -660,8 +1019,14 @@ int sm_desc_create(sm_desc_t** out, const sm_params_t* pp) {
   if (!d) return CONV_EINVAL;
   memset(d, 0, sizeof(*d));
   d->p = p;
-  d->large = p.vocab > 256 * 4 * 16 / dtype_bytes(p.dtype);
-  snprintf(d->names, sizeof(d->names), "sample=sm_row[%d]", d->large ? 1024 : 256);
+  const int64_t chunk = 256 * kChunkVecs * 16 / dtype_bytes(p.dtype), chunks = (p.vocab + chunk - 1) / chunk;  // of logits
+  d->chunks = (int32_t)((chunks + kMostSegments - 1) / kMostSegments);
+  d->segments = (int32_t)((chunks + d->chunks - 1) / d->chunks);
+  int bits = 0;
+  while (((int64_t)1 << bits) < p.vocab) ++bits;
+  d->shift = 61 - bits;
+  if (p.rows > 0 && chunks > 1) d->ws_bytes = (size_t)p.rows * d->segments * (sizeof(Part) + kTops * sizeof(float));
+  snprintf(d->names, sizeof(d->names), d->segments > 1 ? "sample=sm_sums+sm_row(S=%d)" : "sample=sm_row(S=%d)", d->segments);
   *out = d;
   return CONV_OK;
 }
@@ -674,7 +1039,7 @@ int sm_desc_destroy(sm_desc_t* d) {
 
 int sm_desc_workspace_bytes(const sm_desc_t* d, size_t* bytes) {
   if (!d || !bytes) return CONV_EINVAL;
-  *bytes = 0;
+  *bytes = d->ws_bytes;
   return CONV_OK;
 }
 
@@ -682,13 +1047,14 @@ const char* sm_desc_kernel_names(const sm_desc_t* d) { return d ? d->names : "";
 
 int sm_sample(const sm_desc_t* d, const void* logits, int64_t stride, const float* u, const float* scale, const int32_t* top_k,
               const float* top_p, const float* min_p, int32_t* token, float* logp, void* ws, size_t ws_bytes, void* hip_stream) {
-  (void)ws, (void)ws_bytes;
   if (!d) return CONV_EINVAL;
   if (d->p.rows == 0) return CONV_OK;
   if (!logits || !u || !token || (d->p.rows > 1 && stride < d->p.vocab)) return CONV_EINVAL;
-  int bits = 0;
-  while (((int64_t)1 << bits) < d->p.vocab) ++bits;
-  const SmArgs a = {logits, stride, u, scale, top_p, min_p, top_k, token, logp, d->p.rows, d->p.vocab, 61 - bits};
+  if (d->ws_bytes && (!ws || ws_bytes < d->ws_bytes)) return CONV_EWORKSPACE;
+  if (d->ws_bytes && ((uintptr_t)ws & 15u)) return CONV_EINVAL;
+  Part* const parts = static_cast<Part*>(ws);
+  const SmArgs a = {logits, stride, u, scale, top_p, min_p, top_k, token, logp, parts, reinterpret_cast<float*>(parts + (size_t)d->p.rows * d->segments),
+                    d->p.rows, d->p.vocab, d->segments, d->chunks, d->shift};
   const hipStream_t stream = (hipStream_t)hip_stream;
   const int e = d->p.dtype == MI355_F32   ? launch<MI355_F32>(d, a, stream)
                 : d->p.dtype == MI355_F16 ? launch<MI355_F16>(d, a, stream)
