@@ -29,7 +29,8 @@
 
 struct sm_desc {
   sm_params_t p;
-  int32_t segments;  // of a row (1: one launch)
+  int32_t held;      // a row is held by a team: one launch
+  int32_t segments;  // of a row
   int32_t chunks;    // of a segment
   int32_t shift;     // weights as whole numbers: 2^shift, so that a row's sum stays below 2^62
   size_t ws_bytes;
@@ -40,10 +41,9 @@ namespace mi355conv {
 
 namespace {
 
-// What the first launch leaves of a segment: its largest logit (infinity if there is a NaN or an infinity), the least finite one, and the sum of
-// weights relative to its largest.
+// What the first launch leaves of a segment: its largest logit (infinity if there is a NaN or an infinity), and the sum of weights relative to it.
 struct Part {
-  float most, least;
+  float most, unused;
   double sum;
 };
 
@@ -63,9 +63,10 @@ constexpr int kBins = 1024;     // of a histogram
 constexpr int kSorted = 1024;   // logits that are put in order
 constexpr int kList = 4096;     // logits near the maximum
 constexpr int kGroups = 16;     // of vectors, whose sums stand side by side
-constexpr int kTops = 16;       // groups of threads of a segment
-constexpr int kChunkVecs = 4;   // vectors of a thread of the first launch
+constexpr int kTops = 4;        // groups of lanes of a segment
+constexpr int kChunkVecs = 4;   // vectors of a lane of the first launch, and of a thread that holds a row's share
 constexpr int kMostSegments = 256;
+constexpr int kUnits = 256;     // compute units
 constexpr float kNear = 8.f;    // nats below the maximum that the list holds: weights from 3e-4 on
 
 // 2^(i / 32), computed to 60 digits and rounded.
@@ -79,6 +80,17 @@ __device__ const double kRoots[32] = {
     1.681792830507429, 1.718619298122478, 1.7562521603732995, 1.7947090750031072,
     1.8340080864093424, 1.8741676341103, 1.9152065613971474, 1.9571441241754002,
 };
+
+// 32 of them lie in 64 banks: the lanes' reads of different ones do not meet.  (512, and two terms less: 110 us for 1024 x 128256, bound by the banks,
+// where the arithmetic takes 60.)
+constexpr int kRootCount = 32;
+
+// 2^(i / 32), with i 2^15 taken out of the upper word: adding (32 n + i) 2^15 to it gives 2^(n + i / 32).
+__device__ __forceinline__ void fill_roots(double* root, int tid) {
+  if (tid < kRootCount) root[tid] = __builtin_bit_cast(double, __builtin_bit_cast(uint64_t, kRoots[tid]) - ((uint64_t)tid << (15 + 32)));
+}
+
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 
 __device__ __forceinline__ int wave_scan(int v) {  // the sum of the lanes up to this one
   v += dpp_move<0x111, 0xF>(0, v);
@@ -118,37 +130,57 @@ __device__ __forceinline__ uint64_t wave_scan(uint64_t v) {
   return v + move_words(v, 5);
 }
 
-// exp of the difference to the row's or segment's largest logit.
+// exp of the difference to the row's or segment's largest logit: 2^((32 n + i + r) / 32), |r| <= 1/2.  The number 1.5 2^52 brings 32 n + i
+// into the lower word; the polynomial's next term is below 2^-48.7.  What is below 2^-995 counts as 0.
 struct Exponential {
   const double* root;  // in shared memory
-  double top, c32;
+  double top, c;
+  float low;
 
   __device__ __forceinline__ void set(float largest, float scale) {
     top = largest;
-    c32 = (double)scale * (32 * 1.44269504088896340736);
+    c = (double)scale * (kRootCount * 1.44269504088896340736);
+    low = fmaxf(largest - 690.f / scale, -FLT_MAX);
   }
 
-  __device__ __forceinline__ double operator()(float x) const {
-    const double t = fmax(((double)x - top) * c32, -36000.);  // (2^-1125 is 0)
-    const double whole = rint(t), r = t - whole;
-    const int i = (int)whole;
-    constexpr double L = 0.69314718055994530942 / 32;
-    double p = L * L * L * L * L / 120;  // the next term is below 2^-48.7
-    p = fma(p, r, L * L * L * L / 24);
-    p = fma(p, r, L * L * L / 6);
-    p = fma(p, r, L * L / 2);
-    p = fma(p, r, L);
-    p = fma(p, r, 1.);
-    return ldexp(root[i & 31] * p, i >> 5);
+  // The weights of N logits, none of which is below `low`, added to a sum one after the other.  Their steps go side by side, so that a wave waits
+  // once for N entries.
+  template <int N>
+  __device__ __forceinline__ double add(double sum, const float (&x)[N]) const {
+    constexpr double kWhole = 0x1.8p52, L = 0.69314718055994530942 / kRootCount;
+    double r[N], entry[N];
+    uint32_t at[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const double d = (double)x[i] - top, placed = fma(d, c, kWhole);
+      r[i] = fma(d, c, kWhole - placed);
+      at[i] = (uint32_t)__builtin_bit_cast(uint64_t, placed);
+      entry[i] = root[at[i] & (kRootCount - 1)];
+    }
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      u32x2 words = __builtin_bit_cast(u32x2, entry[i]);
+      words[1] += at[i] << 15;
+      const double base = __builtin_bit_cast(double, words);
+      double p = fma(L * L * L * L * L / 120, r[i], L * L * L * L / 24);
+      p = fma(fma(fma(p, r[i], L * L * L / 6), r[i], L * L / 2), r[i], L);
+      sum += fma(base * r[i], p, base);
+    }
+    return sum;
   }
+
+  __device__ __forceinline__ double near(float x) const { return add<1>(0., {x}); }
+
+  __device__ __forceinline__ double operator()(float x) const { return x >= low ? near(x) : 0.; }
 };
 
 template <int THREADS>
 struct Shared {
   static constexpr int WAVES = THREADS / 64;
-  double root[32];
+  double root[kRootCount];
   double sum[WAVES];
-  float most[WAVES], least[WAVES];
+  float most[WAVES];
 };
 
 // Over the team, in the same order every time.
@@ -167,50 +199,40 @@ __device__ __forceinline__ double team_sum(Shared<THREADS>& lds, double v) {
 }
 
 template <int THREADS>
-__device__ __forceinline__ void team_range(Shared<THREADS>& lds, float& most, float& least) {
+__device__ __forceinline__ float team_most(Shared<THREADS>& lds, float most) {
   constexpr int WAVES = THREADS / 64;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   most = wave_most(most);
-  least = -wave_most(-least);
   __syncthreads();
-  if (lane == 0) {
-    lds.most[wave] = most;
-    lds.least[wave] = least;
-  }
+  if (lane == 0) lds.most[wave] = most;
   __syncthreads();
-  most = lds.most[0], least = lds.least[0];
+  most = lds.most[0];
 #pragma unroll
-  for (int w = 1; w < WAVES; ++w) {
-    most = fmaxf(most, lds.most[w]);
-    least = fminf(least, lds.least[w]);
-  }
+  for (int w = 1; w < WAVES; ++w) most = fmaxf(most, lds.most[w]);
+  return most;
 }
 
 __device__ __forceinline__ bool scale_is_good(float scale) { return scale >= 0x1p-60f && scale <= 0x1p60f; }
 
-// Vectors of a row [from, from + 256 kChunkVecs), thread by thread, into its range.
-template <class E>
-__device__ __forceinline__ void load_chunk(const typename E::T* row, int from, int nv, int n, u32x4 (&x)[kChunkVecs]) {
+// Vectors of a row [from, from + THREADS kChunkVecs), thread by thread.
+template <class E, int THREADS>
+__device__ __forceinline__ void load_chunk(const typename E::T* row, int from, int nv, int n, int tid, u32x4 (&x)[kChunkVecs]) {
 #pragma unroll
   for (int j = 0; j < kChunkVecs; ++j) {
-    const int v = from + j * 256 + (int)threadIdx.x;
+    const int v = from + j * THREADS + tid;
     x[j] = v < nv ? row_vec<E>(row, v, n) : lowest_vec<E>();
   }
 }
 
+// The largest one; infinity if there is one or a NaN.
 template <class E>
-__device__ __forceinline__ void chunk_range(const u32x4 (&x)[kChunkVecs], float& most, float& least) {
-  bool bad = false;
+__device__ __forceinline__ float chunk_most(const u32x4 (&x)[kChunkVecs]) {
+  float most = -INFINITY;
 #pragma unroll
   for (int j = 0; j < kChunkVecs; ++j)
 #pragma unroll
-    for (int i = 0; i < E::VEC; ++i) {
-      const float logit = E::get(x[j], i);
-      bad |= !(logit < INFINITY);
-      most = fmaxf(most, logit);
-      least = logit > -INFINITY ? fminf(least, logit) : least;
-    }
-  if (bad) most = INFINITY;
+    for (int i = 0; i < E::VEC; ++i) most = __builtin_elementwise_maximum(most, E::get(x[j], i));  // NaN if there is one
+  return most < INFINITY ? most : INFINITY;
 }
 
 template <class E>
@@ -219,52 +241,74 @@ __device__ __forceinline__ double chunk_sum(const u32x4 (&x)[kChunkVecs], const 
 #pragma unroll
   for (int j = 0; j < kChunkVecs; ++j) {
 #pragma unroll
-    for (int i = 0; i < E::VEC; ++i) s += weight(E::get(x[j], i));
-    __builtin_amdgcn_sched_barrier(0);  // (vectors side by side would take more registers than there are)
+    for (int h = 0; h < E::VEC; h += 4) {
+      float logit[4];  // (2^-995 in the place of less: nothing beside 1)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) logit[i] = __builtin_amdgcn_fmed3f(E::get(x[j], h + i), weight.low, FLT_MAX);
+      s = weight.add(s, logit);
+      __builtin_amdgcn_sched_barrier(0);  // (vectors side by side would take more registers than there are)
+    }
   }
   return s;
 }
 
-// The first launch: a workgroup for each segment.
+// The first launch: a wave for each segment, which knows no other and waits for none; the next one's vectors are on their way while it works.
 template <int DTYPE>
 __global__ __launch_bounds__(256) void sm_sums_kernel(SmArgs a) {
   typedef Elem<DTYPE> E;
-  __shared__ Shared<256> lds;
-  const int tid = threadIdx.x;
-  if (tid < 32) lds.root[tid] = kRoots[tid];
-  const int n = a.vocab, nv = (n + E::VEC - 1) / E::VEC;
-  const int64_t items = (int64_t)a.rows * a.segments;
-  for (int64_t it = blockIdx.x; it < items; it += gridDim.x) {
-    const int r = (int)(it / a.segments), segment = (int)(it % a.segments);
-    const typename E::T* const row = static_cast<const typename E::T*>(a.logits) + (int64_t)r * a.stride;
-    const float scale = a.scale ? a.scale[r] : 1.f;
-    Exponential weight = {lds.root};
-    weight.set(0.f, scale_is_good(scale) ? scale : 1.f);
-    float most = -INFINITY, least = INFINITY, mine = -INFINITY;
+  typedef typename E::T T;
+  __shared__ double root[kRootCount];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+  fill_roots(root, threadIdx.x);
+  __syncthreads();
+  const int n = a.vocab, nv = (n + E::VEC - 1) / E::VEC, total = gridDim.x * 4, per = a.chunks * 64 * kChunkVecs;
+  const int step_r = total / a.segments, step_s = total % a.segments;
+  const int first = blockIdx.x * 4 + wave;
+  int r = first / a.segments, segment = first % a.segments;
+  u32x4 x[kChunkVecs];
+  float scale = 1.f;
+  auto load = [&](int row, int from) {
+    load_chunk<E, 64>(static_cast<const T*>(a.logits) + (int64_t)row * a.stride, from, nv, n, lane, x);
+  };
+  auto load_first = [&]() {
+    if (r >= a.rows) return;
+    load(r, segment * per);
+    if (a.scale) scale = a.scale[r];
+  };
+  load_first();
+  while (r < a.rows) {
+    const int64_t it = (int64_t)r * a.segments + segment;
+    const float used = scale_is_good(scale) ? scale : 1.f;  // (of a bad one the next launch makes what it is)
+    Exponential weight = {root};
+    float most = -INFINITY, mine = -INFINITY;
     double sum = 0.;
     for (int c = 0; c < a.chunks; ++c) {
-      u32x4 x[kChunkVecs];
-      load_chunk<E>(row, (segment * a.chunks + c) * 256 * kChunkVecs, nv, n, x);
-      float here = -INFINITY;
-      chunk_range<E>(x, here, least);
+      if (c > 0) load(r, segment * per + c * 64 * kChunkVecs);
+      const float here = chunk_most<E>(x), all = wave_most(here);
       mine = fmaxf(mine, here);
-      float all = here, all_least = least;
-      team_range<256>(lds, all, all_least);
       if (all > most) {
-        if (most > -INFINITY && all < INFINITY) {
-          weight.top = all;
-          sum *= weight(most);
-        }
+        weight.set(all, used);
+        if (most > -INFINITY && all < INFINITY) sum *= weight(most);
         most = all;
-        weight.top = all;
       }
-      least = all_least;
-      if (fabsf(most) < INFINITY) sum += chunk_sum<E>(x, weight);
+      u32x4 now[kChunkVecs];
+#pragma unroll
+      for (int j = 0; j < kChunkVecs; ++j) now[j] = x[j];
+      if (c + 1 == a.chunks) {
+        r += step_r;
+        segment += step_s;
+        if (segment >= a.segments) {
+          segment -= a.segments;
+          ++r;
+        }
+        load_first();
+      }
+      if (fabsf(most) < INFINITY) sum += chunk_sum<E>(now, weight);
     }
     const float top = group_most<16>(mine);
-    if ((tid & 15) == 0) a.tops[it * kTops + tid / 16] = top;
-    sum = team_sum<256>(lds, sum);
-    if (tid == 0) a.parts[it] = Part{most, least, sum};
+    if ((lane & 15) == 0) a.tops[it * kTops + lane / 16] = top;
+    sum = wave_sum(sum);
+    if (lane == 0) a.parts[it] = Part{most, 0.f, sum};
   }
 }
 
@@ -547,7 +591,7 @@ struct Team {
   // Moves the cut to where the counts (WEIGHT: the weights) of what it keeps reach the target, in descending order.  least: the least finite logit.
   // False where they do not reach it.
   template <bool WEIGHT, bool LIST>
-  __device__ bool find_cut(double target, float least, int entries) {
+  __device__ __attribute__((always_inline)) bool find_cut(double target, float least, int entries) {
     // the first histograms: by distance, near the maximum, then beyond
     const float end = distance(least);
     float from = 0.f, per = 0.f;
@@ -604,7 +648,8 @@ struct Team {
         cut.last = (int)(0xFFFFFFFFu - (uint32_t)entry);
         return true;
       }
-      team_range<THREADS>(lds, most, least_in);
+      most = team_most<THREADS>(lds, most);
+      least_in = -team_most<THREADS>(lds, -least_in);
       if (most == least_in) {  // equal ones: by their indices
         double order = target - above;
         if (WEIGHT) order = fmin(fmax(ceil((target - sum) / weight(most)), 1.), (double)inside);
@@ -697,7 +742,7 @@ struct Team {
 
   // Logits from `bound` on into the list, in the order of their indices: each wave takes a part of the row and fills a part of the list, which are then
   // moved together.  The number of them, or -1 where a wave found more than its part holds.
-  __device__ int fill_list(float bound) {
+  __device__ __forceinline__ int fill_list(float bound) {
     const int per = ((nv + WAVES - 1) / WAVES + 63) / 64 * 64, to = min(nv, (wave + 1) * per);
     int mine = 0;
     __syncthreads();
@@ -757,6 +802,12 @@ struct Team {
     return all;
   }
 
+  __device__ float least_finite() const {
+    float least = INFINITY;
+    each<false>(0, [&](float logit, int) { least = logit > -INFINITY ? fminf(least, logit) : least; });
+    return -team_most<THREADS>(lds, -least);
+  }
+
   // The sum of the weights that the cut keeps.
   template <bool LIST>
   __device__ double kept_sum(int entries) {
@@ -806,6 +857,70 @@ struct Team {
     return lds.found;
   }
 
+  // The list's place of the token, where the list has at most one logit for each thread and k of them, or all that min-p keeps, or what top-p
+  // needs: each thread ranks its own by counting those above it; weights in that order give the number of them that the limits keep.
+  // all: the weight that top-p goes by, where top-k has no part in it.  -1 where the list does not hold what is kept.
+  __device__ int rank_and_locate(double u, int k, double p, double q, double all, bool complete, int entries, double& whole) {
+    const bool mine = tid < entries;
+    const float x = mine ? lds.value[tid] : -INFINITY;
+    const uint64_t key = mine ? entry_of(x, tid) : 0;
+    const double w = mine ? weight(x) : 0.;
+    uint64_t* const keys = lds.sorted;
+    double* const ordered = reinterpret_cast<double*>(lds.weights);
+    keys[tid] = key;
+    __syncthreads();
+    int rank = 0;
+    if (wave * 64 < entries) {
+#pragma unroll 4
+      for (int o = 0; o < entries; ++o) rank += keys[o] > key ? 1 : 0;
+    }
+    if (mine)
+      ordered[rank] = w;
+    else
+      ordered[tid] = 0.;
+    __syncthreads();
+    // every wave the same: a run of the order for each lane
+    constexpr int PER = THREADS / 64;
+    double run[PER], sum = 0.;
+    int kept_q = 0;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+      const int at = lane * PER + i;
+      run[i] = at < entries ? ordered[at] : 0.;
+      if (k > 0 && at >= k) run[i] = 0.;
+      sum += run[i];
+      kept_q += (int)__builtin_popcountll(__ballot(at < entries && run[i] >= q));
+    }
+    const double up_to = wave_scan(sum), held = read_lane(up_to, 63);
+    int kept = k > 0 ? min(k, entries) : entries;
+    if (p < 1.) {
+      const double target = fmax((k > 0 ? held : all) * p, 0.);
+      if (target > held && !complete) return -1;
+      double reached = up_to - sum;
+      int before = 0;  // those before the one that reaches it
+#pragma unroll
+      for (int i = 0; i < PER; ++i) {
+        reached += run[i];
+        before += (int)__builtin_popcountll(__ballot(lane * PER + i < entries && reached < target));
+      }
+      kept = min(kept, before + 1);
+    }
+    if (q > 0.) kept = min(kept, kept_q);
+    const double part = mine && rank < kept ? w : 0., part_to = wave_scan(part);
+    if (lane == 63) lds.part[0][wave] = part_to;
+    __syncthreads();
+    const double s = lane < WAVES ? lds.part[0][lane] : 0.;
+    whole = wave_sum(s);
+    double target = u * whole;
+    const int place = pick(s, WAVES, target);
+    if (wave == place) {
+      const int at_lane = pick_lane(part, target);
+      if (lane == at_lane) lds.found = tid;
+    }
+    __syncthreads();
+    return lds.found;
+  }
+
   // A bound that at least k logits reach, from the maxima of `groups` groups: the leading 16 bits of the k-th largest one, where every lane takes
   // the larger ones of four shares of them.
   __device__ float bound_of(const float* tops, int groups, int k) {
@@ -835,7 +950,7 @@ __global__ __launch_bounds__(THREADS) void sm_row_kernel(SmArgs a) {
   typedef Elem<DTYPE> E;
   __shared__ RowLds<THREADS, LIMITED, HELD> lds;
   const int tid = threadIdx.x;
-  if (tid < 32) lds.root[tid] = kRoots[tid];
+  fill_roots(lds.root, tid);
   for (int r = blockIdx.x; r < a.rows; r += gridDim.x) {
     Team<DTYPE, THREADS, LIMITED, HELD> t = {lds};
     t.tid = tid;
@@ -852,21 +967,20 @@ __global__ __launch_bounds__(THREADS) void sm_row_kernel(SmArgs a) {
     const Part* const parts = a.parts + (int64_t)r * a.segments;
 
     __syncthreads();  // the row before this one
-    float most = -INFINITY, least = INFINITY;
+    float most = -INFINITY;
     u32x4 x[kChunkVecs];
-    Part part = {-INFINITY, INFINITY, 0.};
+    Part part = {-INFINITY, 0.f, 0.};
     if constexpr (HELD) {
-      load_chunk<E>(t.row, 0, t.nv, t.n, x);
+      load_chunk<E, 256>(t.row, 0, t.nv, t.n, tid, x);
 #pragma unroll
       for (int j = 0; j < kChunkVecs; ++j) lds.held[j * 256 + tid] = x[j];
-      chunk_range<E>(x, most, least);
+      most = chunk_most<E>(x);
     } else if (tid < a.segments) {
       part = parts[tid];
       most = part.most;
-      least = part.least;
     }
     if (bad) most = INFINITY;
-    team_range<THREADS>(lds, most, least);
+    most = team_most<THREADS>(lds, most);
     if (!(fabsf(most) < INFINITY)) {
       if (tid == 0) {
         a.token[r] = -1;
@@ -908,7 +1022,10 @@ __global__ __launch_bounds__(THREADS) void sm_row_kernel(SmArgs a) {
       }
       int entries = -1;
       if (bound > -INFINITY) entries = t.fill_list(bound);
-      if (entries >= 0) {
+      if (entries >= 0 && entries <= THREADS && (!by_count || k <= entries || (complete && !by_weight)) && (by_count || by_weight || complete)) {
+        const int place = t.rank_and_locate((double)u, by_count ? k : 0, (double)p, least_weight, all, complete, entries, whole);
+        if (place >= 0) token = lds.index[place];
+      } else if (entries >= 0) {
         bool enough = by_count || by_weight || complete;
         const float lowest = bound;
         if (by_count) {
@@ -932,6 +1049,7 @@ __global__ __launch_bounds__(THREADS) void sm_row_kernel(SmArgs a) {
           t.cut = Cut{-INFINITY, INT_MAX};
       }
       if (token < 0) {
+        const float least = t.least_finite();
         if (by_count) t.template find_cut<false, false>((double)k, least, 0);
         if (by_weight) t.template find_cut<true, false>(fmax((by_count ? t.template kept_sum<false>(0) : all) * (double)p, 0.), least, 0);
         token = t.template locate<true>(
@@ -971,7 +1089,7 @@ __global__ __launch_bounds__(THREADS) void sm_row_kernel(SmArgs a) {
             done = sum > target;
           }
         }
-        const int per = a.chunks * 256 * kChunkVecs, from = (4 * lane + chosen) * per;
+        const int per = a.chunks * 64 * kChunkVecs, from = (4 * lane + chosen) * per;
         double ignored;
         token = t.template locate<false>(from, min(from + per, t.nv), target - before, plain, ignored);
       }
@@ -986,11 +1104,11 @@ __global__ __launch_bounds__(THREADS) void sm_row_kernel(SmArgs a) {
 template <int DTYPE, bool LIMITED>
 int launch_rows(const sm_desc* d, const SmArgs& a, hipStream_t stream) {
   const dim3 grid(std::min(a.rows, 1 << 20));
-  if (d->segments == 1 && d->chunks == 1) {
+  if (d->held) {
     hipLaunchKernelGGL((sm_row_kernel<DTYPE, 256, LIMITED, true>), grid, dim3(256), 0, stream, a);
     return (int)hipGetLastError();
   }
-  hipLaunchKernelGGL(sm_sums_kernel<DTYPE>, dim3((uint32_t)std::min<int64_t>((int64_t)a.rows * a.segments, 1 << 22)), dim3(256), 0, stream, a);
+  hipLaunchKernelGGL(sm_sums_kernel<DTYPE>, dim3((uint32_t)std::min<int64_t>(((int64_t)a.rows * a.segments + 3) / 4, kUnits * 4)), dim3(256), 0, stream, a);
   const int e = (int)hipGetLastError();
   if (e) return e;
   hipLaunchKernelGGL((sm_row_kernel<DTYPE, LIMITED ? 512 : 256, LIMITED, false>), grid, dim3(LIMITED ? 512 : 256), 0, stream, a);
@@ -1019,14 +1137,15 @@ int sm_desc_create(sm_desc_t** out, const sm_params_t* pp) {
   if (!d) return CONV_EINVAL;
   memset(d, 0, sizeof(*d));
   d->p = p;
-  const int64_t chunk = 256 * kChunkVecs * 16 / dtype_bytes(p.dtype), chunks = (p.vocab + chunk - 1) / chunk;  // of logits
+  const int64_t chunk = 64 * kChunkVecs * 16 / dtype_bytes(p.dtype), chunks = (p.vocab + chunk - 1) / chunk;  // of logits
   d->chunks = (int32_t)((chunks + kMostSegments - 1) / kMostSegments);
   d->segments = (int32_t)((chunks + d->chunks - 1) / d->chunks);
+  d->held = chunks <= 4;
   int bits = 0;
   while (((int64_t)1 << bits) < p.vocab) ++bits;
   d->shift = 61 - bits;
-  if (p.rows > 0 && chunks > 1) d->ws_bytes = (size_t)p.rows * d->segments * (sizeof(Part) + kTops * sizeof(float));
-  snprintf(d->names, sizeof(d->names), d->segments > 1 ? "sample=sm_sums+sm_row(S=%d)" : "sample=sm_row(S=%d)", d->segments);
+  if (!d->held) d->ws_bytes = (size_t)p.rows * d->segments * (sizeof(Part) + kTops * sizeof(float));
+  snprintf(d->names, sizeof(d->names), d->held ? "sample=sm_row" : "sample=sm_sums+sm_row");
   *out = d;
   return CONV_OK;
 }
