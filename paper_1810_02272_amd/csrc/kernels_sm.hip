@@ -67,6 +67,7 @@ constexpr int kTops = 4;        // groups of lanes of a segment
 constexpr int kChunkVecs = 4;   // vectors of a lane of the first launch, and of a thread that holds a row's share
 constexpr int kMostSegments = 256;
 constexpr int kUnits = 256;     // compute units
+constexpr int kAhead = 8;        // vectors that a thread asks for at a time
 constexpr float kNear = 8.f;    // nats below the maximum that the list holds: weights from 3e-4 on
 
 // 2^(i / 32), computed to 60 digits and rounded.
@@ -215,12 +216,15 @@ __device__ __forceinline__ float team_most(Shared<THREADS>& lds, float most) {
 __device__ __forceinline__ bool scale_is_good(float scale) { return scale >= 0x1p-60f && scale <= 0x1p60f; }
 
 // Vectors of a row [from, from + THREADS kChunkVecs), thread by thread.
-template <class E, int THREADS>
+template <class E, int THREADS, bool LONG>
 __device__ __forceinline__ void load_chunk(const typename E::T* row, int from, int nv, int n, int tid, u32x4 (&x)[kChunkVecs]) {
 #pragma unroll
   for (int j = 0; j < kChunkVecs; ++j) {
     const int v = from + j * THREADS + tid;
-    x[j] = v < nv ? row_vec<E>(row, v, n) : lowest_vec<E>();
+    if constexpr (LONG)
+      x[j] = long_row_vec<E>(row, v, nv, n);
+    else
+      x[j] = v < nv ? row_vec<E>(row, v, n) : lowest_vec<E>();
   }
 }
 
@@ -268,7 +272,7 @@ __global__ __launch_bounds__(256) void sm_sums_kernel(SmArgs a) {
   u32x4 x[kChunkVecs];
   float scale = 1.f;
   auto load = [&](int row, int from) {
-    load_chunk<E, 64>(static_cast<const T*>(a.logits) + (int64_t)row * a.stride, from, nv, n, lane, x);
+    load_chunk<E, 64, true>(static_cast<const T*>(a.logits) + (int64_t)row * a.stride, from, nv, n, lane, x);
   };
   auto load_first = [&]() {
     if (r >= a.rows) return;
@@ -341,7 +345,12 @@ struct Team {
   typedef RowLds<THREADS, LIMITED, HELD> Lds;
   static constexpr int VEC = E::VEC, WAVES = THREADS / 64, SHARE = kList / WAVES;  // of the list, for each wave
 
-  Lds& lds;
+  // (a function's own shared memory: a reference kept in the team would make every access a generic one)
+  static __device__ __forceinline__ Lds& memory() {
+    __shared__ Lds lds;
+    return lds;
+  }
+
   const T* row;
   int n, nv, tid, lane, wave, shift;
   float m, scale;  // the maximum
@@ -349,8 +358,8 @@ struct Team {
   Cut cut;
 
   __device__ __forceinline__ u32x4 vec(int v) const {
-    if constexpr (HELD) return lds.held[v];
-    return v < nv ? row_vec<E>(row, v, n) : lowest_vec<E>();
+    if constexpr (HELD) return v < nv ? memory().held[v] : lowest_vec<E>();
+    return long_row_vec<E>(row, v, nv, n);
   }
 
   __device__ __forceinline__ bool keeps(float x, int at) const { return x > cut.value || (x == cut.value && at <= cut.last); }
@@ -374,16 +383,17 @@ struct Team {
   template <bool LIST, class F>
   __device__ __forceinline__ void each(int entries, F&& f) const {
     if constexpr (LIST) {
-      for (int i = tid; i < entries; i += THREADS) f(lds.value[i], i);
+      for (int i = tid; i < entries; i += THREADS) f(memory().value[i], i);
     } else {
-      for (int v0 = 0; v0 < nv; v0 += 4 * THREADS) {
-        u32x4 x[4];
+      for (int v0 = 0; v0 < nv; v0 += kAhead * THREADS) {
+        u32x4 x[kAhead];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) x[j] = v0 + j * THREADS + tid < nv ? vec(v0 + j * THREADS + tid) : lowest_vec<E>();
+        for (int j = 0; j < kAhead; ++j) x[j] = vec(v0 + j * THREADS + tid);
 #pragma unroll 1
-        for (int j = 0; j < 4; ++j) {
+        for (int j = 0; j < min(kAhead, (nv - v0 + THREADS - 1) / THREADS); ++j) {
           elements(x[0], v0 + j * THREADS + tid, f);
-          x[0] = x[1], x[1] = x[2], x[2] = x[3];
+#pragma unroll
+          for (int i = 0; i + 1 < kAhead; ++i) x[i] = x[i + 1];
         }
       }
     }
@@ -391,7 +401,7 @@ struct Team {
 
   // The groups' sums stand in the lanes: the first group with which they pass `target`, or the last one of any weight; target becomes what is left of
   // it before that group.
-  __device__ static int pick(double s, int groups, double& target) {
+  static __device__ __forceinline__ int pick(double s, int groups, double& target) {
     double sum = 0., before = 0.;
     int chosen = 0;
     for (int g = 0; g < groups; ++g) {
@@ -408,7 +418,7 @@ struct Team {
   }
 
   // The same by a scan over 64 lanes.
-  __device__ static int pick_lane(double mine, double& target) {
+  static __device__ __forceinline__ int pick_lane(double mine, double& target) {
     const double up_to = wave_scan(mine);
     const uint64_t some = __ballot(mine > 0.), passed = __ballot(mine > 0. && up_to > target);
     const int chosen = passed ? __builtin_ctzll(passed) : 63 - __builtin_clzll(some | 1);
@@ -419,7 +429,7 @@ struct Team {
   // The index of the first logit of the vectors [from, to) with which the sum of of(logit, index) passes the target: u times the whole
   // (FRACTION), or as given.
   template <bool FRACTION, class W>
-  __device__ int locate(int from, int to, double target, W&& of, double& whole) {
+  __device__ __forceinline__ int locate(int from, int to, double target, W&& of, double& whole) {
     int j0 = 0, j1 = (to - from + THREADS - 1) / THREADS, place = 0;
     auto of_vec = [&](int v) {
       double s = 0.;
@@ -434,12 +444,12 @@ struct Team {
         double s = 0.;
         for (int j = j0 + g * per; j < min(j0 + (g + 1) * per, j1); ++j) s += of_vec(from + j * THREADS + tid);
         s = wave_sum(s);
-        if (lane == 0) lds.part[g][wave] = s;
+        if (lane == 0) memory().part[g][wave] = s;
       }
       __syncthreads();
       double s = 0.;
       if (lane < groups)
-        for (int w = 0; w < WAVES; ++w) s += lds.part[lane][w];
+        for (int w = 0; w < WAVES; ++w) s += memory().part[lane][w];
       if (first) {
         whole = wave_sum(s);
         target *= whole;
@@ -449,7 +459,7 @@ struct Team {
       j0 += g * per;
       j1 = min(j0 + per, j1);
       if (per == 1) {
-        place = pick(lane < WAVES ? lds.part[g][lane] : 0., WAVES, target);
+        place = pick(lane < WAVES ? memory().part[g][lane] : 0., WAVES, target);
         break;
       }
     }
@@ -468,39 +478,39 @@ struct Team {
             done = sum > target;
           }
         });
-        lds.found = index;
+        memory().found = index;
       }
     }
     __syncthreads();
-    return lds.found;
+    return memory().found;
   }
 
-  // lds.sorted in descending order: by a wave where they are few, which counts those above each.
-  __device__ void sort(int entries) {
+  // memory().sorted in descending order: by a wave where they are few, which counts those above each.
+  __device__ __forceinline__ void sort(int entries) {
     __syncthreads();
     if (entries <= 64) {
       if (wave == 0) {
-        const uint64_t mine = lane < entries ? lds.sorted[lane] : 0;
+        const uint64_t mine = lane < entries ? memory().sorted[lane] : 0;
         int rank = 0;
         for (int o = 0; o < entries; ++o) rank += read_lane(mine, o) > mine ? 1 : 0;
         wave_sync();
-        if (lane < entries) lds.sorted[rank] = mine;
+        if (lane < entries) memory().sorted[rank] = mine;
       }
       __syncthreads();
       return;
     }
     int size = 128;
     while (size < entries) size *= 2;
-    for (int i = entries + tid; i < size; i += THREADS) lds.sorted[i] = 0;
+    for (int i = entries + tid; i < size; i += THREADS) memory().sorted[i] = 0;
     for (int k = 2; k <= size; k *= 2)
       for (int j = k / 2; j > 0; j /= 2) {
         __syncthreads();
         for (int i = tid; i < size / 2; i += THREADS) {
           const int a = 2 * i - (i & (j - 1)), b = a + j;
-          const uint64_t x = lds.sorted[a], y = lds.sorted[b];
+          const uint64_t x = memory().sorted[a], y = memory().sorted[b];
           if ((x < y) == ((a & k) == 0)) {
-            lds.sorted[a] = y;
-            lds.sorted[b] = x;
+            memory().sorted[a] = y;
+            memory().sorted[b] = x;
           }
         }
       }
@@ -508,29 +518,29 @@ struct Team {
   }
 
   // The first bin with which the counts (WEIGHT: the weights) reach the target, counted from `carry` on: its number, or -1 (`surely`: the last bin that
-  // holds any); lds.before and lds.inside are the count before it and its own.  The carries go on to the end of the bins.
+  // holds any); memory().before and memory().inside are the count before it and its own.  The carries go on to the end of the bins.
   template <bool WEIGHT>
-  __device__ int find_bin(uint64_t target, uint64_t& carry, int& count_carry, bool surely) {
+  __device__ __forceinline__ int find_bin(uint64_t target, uint64_t& carry, int& count_carry, bool surely) {
     constexpr int PER = kBins / THREADS;
     __syncthreads();
     int counts[PER], count = 0;
     uint64_t values[PER], value = 0;
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
-      counts[i] = lds.count[tid * PER + i];
-      values[i] = WEIGHT ? lds.weights[tid * PER + i] : (uint64_t)counts[i];
+      counts[i] = memory().count[tid * PER + i];
+      values[i] = WEIGHT ? memory().weights[tid * PER + i] : (uint64_t)counts[i];
       count += counts[i];
       value += values[i];
     }
     const int count_to = wave_scan(count);
     const uint64_t value_to = wave_scan(value);
     if (lane == 63) {
-      lds.number[wave] = count_to;
-      lds.whole[wave] = value_to;
+      memory().number[wave] = count_to;
+      memory().whole[wave] = value_to;
     }
     if (tid == 0) {
-      lds.found = INT_MAX;
-      lds.places = 0;
+      memory().found = INT_MAX;
+      memory().places = 0;
     }
     __syncthreads();
     int count_before = count_carry, count_all = count_carry;
@@ -538,11 +548,11 @@ struct Team {
 #pragma unroll
     for (int w = 0; w < WAVES; ++w) {
       if (w < wave) {
-        count_before += lds.number[w];
-        before += lds.whole[w];
+        count_before += memory().number[w];
+        before += memory().whole[w];
       }
-      count_all += lds.number[w];
-      all += lds.whole[w];
+      count_all += memory().number[w];
+      all += memory().whole[w];
     }
     if (surely && all < target) target = all;  // (a rounding)
     count_before += count_to - count;
@@ -558,12 +568,12 @@ struct Team {
       }
       count_before += counts[i];
     }
-    if (mine != INT_MAX) atomicMin(&lds.found, mine);
+    if (mine != INT_MAX) atomicMin(&memory().found, mine);
     __syncthreads();
-    const int found = lds.found;
+    const int found = memory().found;
     if (mine == found && mine != INT_MAX) {
-      lds.before = mine_before;
-      lds.inside = mine_count;
+      memory().before = mine_before;
+      memory().inside = mine_count;
     }
     __syncthreads();
     carry = all;
@@ -571,11 +581,11 @@ struct Team {
     return found == INT_MAX ? -1 : found;
   }
 
-  __device__ void clear_bins() {
+  __device__ __forceinline__ void clear_bins() {
     __syncthreads();
     for (int i = tid; i < kBins; i += THREADS) {
-      lds.count[i] = 0;
-      lds.weights[i] = 0;
+      memory().count[i] = 0;
+      memory().weights[i] = 0;
     }
     __syncthreads();
   }
@@ -584,36 +594,54 @@ struct Team {
 
   template <bool WEIGHT>
   __device__ __forceinline__ void count_in(int b, float logit) {
-    atomicAdd(&lds.count[b], 1);
-    if (WEIGHT) atomicAdd((unsigned long long*)&lds.weights[b], (unsigned long long)fixed(weight(logit)));
+    atomicAdd(&memory().count[b], 1);
+    if (WEIGHT) atomicAdd((unsigned long long*)&memory().weights[b], (unsigned long long)fixed(weight(logit)));
   }
 
   // Moves the cut to where the counts (WEIGHT: the weights) of what it keeps reach the target, in descending order.  least: the least finite logit.
-  // False where they do not reach it.
+  // [bracket.x, bracket.y]: distances between which it is likely to be (bracket.y = 0: not known).  False where they do not reach it.
   template <bool WEIGHT, bool LIST>
-  __device__ __attribute__((always_inline)) bool find_cut(double target, float least, int entries) {
-    // the first histograms: by distance, near the maximum, then beyond
+  __device__ __forceinline__ bool find_cut(double target, float least, int entries, float2 bracket) {
+    // histograms by distance: of the bracket, then near the maximum, then beyond; d of (from, to]
     const float end = distance(least);
-    float from = 0.f, per = 0.f;
+    float from = -1.f, to = -1.f, start = 0.f, per = 0.f;
+    double above_sum = 0.;
+    int bin = -1, count_carry = 0;
     uint64_t carry = 0;
-    int count_carry = 0, bin = -1;
-    for (int phase = 0; phase < 2 && bin < 0; ++phase) {
-      if (phase == 1 && end <= kNear) break;
-      const float to = phase == 0 ? fminf(kNear, end) : end;
-      from = phase == 0 ? 0.f : kNear;
-      per = to > from ? fminf(kBins / (to - from), FLT_MAX) : 0.f;
+    for (int phase = bracket.y > 0.f ? 0 : 1; phase < 3 && bin < 0; ++phase) {
+      from = phase == 0 ? bracket.x : phase == 1 ? -1.f : kNear;
+      to = phase == 0 ? bracket.y : phase == 1 ? fminf(kNear, end) : end;
+      if (phase == 2 && end <= kNear) break;
+      start = fmaxf(from, 0.f);
+      per = to > start ? fminf(kBins / (to - start), FLT_MAX) : 0.f;
       clear_bins();
+      double sum = 0.;
+      int count = 0;
       each<LIST>(entries, [&](float logit, int at) {
         const float d = distance(logit);
-        if (logit > -INFINITY && (phase == 0 ? d <= to : d > from) && keeps(logit, at)) count_in<WEIGHT>(min((int)((d - from) * per), kBins - 1), logit);
+        if (!(d <= to) || !(logit > -INFINITY) || !keeps(logit, at)) return;
+        if (d > from) {
+          count_in<WEIGHT>(min((int)((d - start) * per), kBins - 1), logit);
+        } else {
+          ++count;
+          if (WEIGHT) sum += weight(logit);
+        }
       });
-      bin = find_bin<WEIGHT>(WEIGHT ? fixed(target) : (uint64_t)target, carry, count_carry, false);
+      above_sum = 0.;
+      count_carry = 0;
+      carry = 0;
+      if (from >= 0.f) {
+        count_carry = (int)team_sum<THREADS>(memory(), (double)count);
+        if (WEIGHT) above_sum = team_sum<THREADS>(memory(), sum);
+        carry = WEIGHT ? fixed(above_sum) : (uint64_t)count_carry;
+      }
+      if (carry < (WEIGHT ? fixed(target) : (uint64_t)target) || from < 0.f)
+        bin = find_bin<WEIGHT>(WEIGHT ? fixed(target) : (uint64_t)target, carry, count_carry, false);
     }
     if (bin < 0) return false;
     bool by_key = false;
     uint32_t high = 0, low = 0;  // by key: bins of (high - key) >> bits
-    int bits = 0, above = lds.before, inside = lds.inside;
-    const bool far = from > 0.f;
+    int bits = 0, above = memory().before, inside = memory().inside;
     for (;;) {
       // what the bin holds: to be sorted if it is few; their range; the weight above them
       float most = -INFINITY, least_in = INFINITY;
@@ -626,30 +654,31 @@ struct Team {
           side = key > high ? -1 : key < low ? 1 : (int)((high - key) >> bits) - bin;
         } else {
           const float d = distance(logit);
-          side = (far ? d <= from : d > kNear) ? (far ? -1 : 1) : min((int)((d - from) * per), kBins - 1) - bin;
+          if (d <= from) return;  // these are in above_sum
+          side = d > to ? 1 : min((int)((d - start) * per), kBins - 1) - bin;
         }
         if (WEIGHT && side < 0) sum += weight(logit);
         if (side == 0) {
           most = fmaxf(most, logit);
           least_in = fminf(least_in, logit);
           if (inside <= kSorted) {
-            const uint32_t place = atomicAdd(&lds.places, 1u);
-            if (place < (uint32_t)kSorted) lds.sorted[place] = entry_of(logit, at);
+            const uint32_t place = atomicAdd(&memory().places, 1u);
+            if (place < (uint32_t)kSorted) memory().sorted[place] = entry_of(logit, at);
           }
         }
       });
-      if (WEIGHT) sum = team_sum<THREADS>(lds, sum);
+      if (WEIGHT) sum = team_sum<THREADS>(memory(), sum) + (by_key ? 0. : above_sum);
       if (inside <= kSorted) {
         sort(inside);
         int place = (int)target - above - 1;
         if (WEIGHT) place = sorted_place(inside, sum, target);
-        const uint64_t entry = lds.sorted[max(0, min(place, inside - 1))];
+        const uint64_t entry = memory().sorted[max(0, min(place, inside - 1))];
         cut.value = key_value((uint32_t)(entry >> 32));
         cut.last = (int)(0xFFFFFFFFu - (uint32_t)entry);
         return true;
       }
-      most = team_most<THREADS>(lds, most);
-      least_in = -team_most<THREADS>(lds, -least_in);
+      most = team_most<THREADS>(memory(), most);
+      least_in = -team_most<THREADS>(memory(), -least_in);
       if (most == least_in) {  // equal ones: by their indices
         double order = target - above;
         if (WEIGHT) order = fmin(fmax(ceil((target - sum) / weight(most)), 1.), (double)inside);
@@ -672,42 +701,42 @@ struct Team {
       int count_before = above;
       bin = find_bin<WEIGHT>(WEIGHT ? fixed(fmax(target - sum, 0.)) : (uint64_t)target, before, count_before, true);
       if (bin < 0) return false;
-      above = lds.before;
-      inside = lds.inside;
+      above = memory().before;
+      inside = memory().inside;
     }
   }
 
   // The index of the order-th (from 1) of the logits that equal x, all of which the cut keeps.
   template <bool LIST>
-  __device__ int nth_equal(float x, int order, int entries) {
+  __device__ __forceinline__ int nth_equal(float x, int order, int entries) {
     if constexpr (LIST) {  // places in turns of the team
       int before = 0;
       for (int i0 = 0; i0 < entries; i0 += THREADS) {
-        const bool mine = i0 + tid < entries && lds.value[i0 + tid] == x;
+        const bool mine = i0 + tid < entries && memory().value[i0 + tid] == x;
         const uint64_t mask = __ballot(mine);
         __syncthreads();
-        if (lane == 0) lds.number[wave] = (int)__builtin_popcountll(mask);
+        if (lane == 0) memory().number[wave] = (int)__builtin_popcountll(mask);
         __syncthreads();
         int here = before + (int)__builtin_popcountll(mask & ((2ull << lane) - 1));
 #pragma unroll
         for (int w = 0; w < WAVES; ++w) {
-          if (w < wave) here += lds.number[w];
-          before += lds.number[w];
+          if (w < wave) here += memory().number[w];
+          before += memory().number[w];
         }
-        if (mine && here == order) lds.found = i0 + tid;
+        if (mine && here == order) memory().found = i0 + tid;
       }
       __syncthreads();
-      return lds.found;
+      return memory().found;
     } else {
       double whole;
       return locate<false>(0, nv, order - 0.5, [&](float logit, int at) { return logit == x && keeps(logit, at) ? 1. : 0.; }, whole);
     }
   }
 
-  // The first place of lds.sorted with which the weights reach the target, counted from `sum` on.
-  __device__ int sorted_place(int entries, double sum, double target) {
+  // The first place of memory().sorted with which the weights reach the target, counted from `sum` on.
+  __device__ __forceinline__ int sorted_place(int entries, double sum, double target) {
     if (entries <= 64) {
-      const double w = lane < entries ? weight(key_value((uint32_t)(lds.sorted[lane] >> 32))) : 0.;
+      const double w = lane < entries ? weight(key_value((uint32_t)(memory().sorted[lane] >> 32))) : 0.;
       const uint64_t reached = __ballot(lane < entries && sum + wave_scan(w) >= target);
       return reached ? __builtin_ctzll(reached) : entries - 1;
     }
@@ -716,28 +745,28 @@ struct Team {
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
       const int at = tid * PER + i;
-      w[i] = at < entries ? weight(key_value((uint32_t)(lds.sorted[at] >> 32))) : 0.;
+      w[i] = at < entries ? weight(key_value((uint32_t)(memory().sorted[at] >> 32))) : 0.;
       mine += w[i];
     }
     const double to = wave_scan(mine);
-    if (tid == 0) lds.found = entries - 1;
-    if (lane == 63) lds.sum[wave] = to;
+    if (tid == 0) memory().found = entries - 1;
+    if (lane == 63) memory().sum[wave] = to;
     __syncthreads();
 #pragma unroll
     for (int o = 0; o < WAVES; ++o)
-      if (o < wave) sum += lds.sum[o];
+      if (o < wave) sum += memory().sum[o];
     sum += to - mine;
     bool done = false;
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
       sum += w[i];
       if (!done && tid * PER + i < entries && sum >= target) {
-        atomicMin(&lds.found, tid * PER + i);
+        atomicMin(&memory().found, tid * PER + i);
         done = true;
       }
     }
     __syncthreads();
-    return lds.found;
+    return memory().found;
   }
 
   // Logits from `bound` on into the list, in the order of their indices: each wave takes a part of the row and fills a part of the list, which are then
@@ -746,12 +775,12 @@ struct Team {
     const int per = ((nv + WAVES - 1) / WAVES + 63) / 64 * 64, to = min(nv, (wave + 1) * per);
     int mine = 0;
     __syncthreads();
-    for (int v0 = wave * per; v0 < to && mine <= SHARE; v0 += 4 * 64) {
-      u32x4 x[4];
+    for (int v0 = wave * per; v0 < to && mine <= SHARE; v0 += kAhead * 64) {
+      u32x4 x[kAhead];
 #pragma unroll
-      for (int j = 0; j < 4; ++j) x[j] = v0 + j * 64 + lane < to ? vec(v0 + j * 64 + lane) : lowest_vec<E>();
+      for (int j = 0; j < kAhead; ++j) x[j] = vec(v0 + j * 64 + lane < to ? v0 + j * 64 + lane : nv);
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
+      for (int j = 0; j < kAhead; ++j) {
         uint32_t mask = 0;
 #pragma unroll
         for (int i = 0; i < VEC; ++i) mask |= E::get(x[j], i) >= bound ? 1u << i : 0u;
@@ -763,21 +792,21 @@ struct Team {
         for (int i = 0; i < VEC; ++i)
           if (mask >> i & 1) {
             if (place < SHARE) {
-              lds.value[wave * SHARE + place] = E::get(x[j], i);
-              lds.index[wave * SHARE + place] = at.base + i;
+              memory().value[wave * SHARE + place] = E::get(x[j], i);
+              memory().index[wave * SHARE + place] = at.base + i;
             }
             ++place;
           }
         mine += read_lane(up_to, 63);
       }
     }
-    if (lane == 0) lds.number[wave] = mine;
+    if (lane == 0) memory().number[wave] = mine;
     __syncthreads();
     int before = 0, all = 0;
     bool over = false;
 #pragma unroll
     for (int w = 0; w < WAVES; ++w) {
-      const int count = lds.number[w];
+      const int count = memory().number[w];
       over |= count > SHARE;
       before += w < wave ? count : 0;
       all += count;
@@ -788,42 +817,115 @@ struct Team {
 #pragma unroll
     for (int i = 0; i < SHARE / 64; ++i)
       if (i * 64 + lane < mine) {
-        value[i] = lds.value[wave * SHARE + i * 64 + lane];
-        index[i] = lds.index[wave * SHARE + i * 64 + lane];
+        value[i] = memory().value[wave * SHARE + i * 64 + lane];
+        index[i] = memory().index[wave * SHARE + i * 64 + lane];
       }
     __syncthreads();
 #pragma unroll
     for (int i = 0; i < SHARE / 64; ++i)
       if (i * 64 + lane < mine) {
-        lds.value[before + i * 64 + lane] = value[i];
-        lds.index[before + i * 64 + lane] = index[i];
+        memory().value[before + i * 64 + lane] = value[i];
+        memory().index[before + i * 64 + lane] = index[i];
       }
     __syncthreads();
     return all;
   }
 
-  __device__ float least_finite() const {
+  // Where the k-th logit, or (k = 0) the place up to which the weights reach p of `all`, is likely to lie: distances that are likely before and
+  // after it, from every so many-th vector, and in `likely` about how many logits lie up to the second.  Weights beyond a place are those of
+  // many small ones, which a share of the row shows well.
+  __device__ __forceinline__ float2 estimate(int k, double p, double all, int& likely) {
+    constexpr float kPer = kBins / 32.f;  // 32 nats
+    const int stride = max(1, nv / THREADS), v = tid * stride;
+    const float share = (float)nv / (float)min(THREADS, (nv + stride - 1) / stride);
+    clear_bins();
+    if (v < nv)
+      elements(vec(v), v, [&](float logit, int) {
+        if (logit > -INFINITY) atomicAdd(&memory().count[(int)fminf(distance(logit) * kPer, kBins - 1.f)], 1);
+      });
+    __syncthreads();
+    // the last bin first: what lies beyond a bin
+    constexpr int PER = kBins / THREADS;
+    float value[PER], mine = 0.f;
+    int counts[PER], count = 0;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+      const int bin = kBins - 1 - (tid * PER + i);
+      counts[i] = memory().count[bin];
+      value[i] = (float)counts[i] * __expf(-(float)bin / kPer);
+      mine += value[i];
+      count += counts[i];
+    }
+    const int count_to = wave_scan(count);
+    const double value_to = wave_scan((double)mine);
+    if (lane == 63) {
+      memory().number[wave] = count_to;
+      memory().sum[wave] = value_to;
+    }
+    if (tid == 0) {
+      memory().before = kBins;
+      memory().found = 0;
+      memory().inside = 0;
+    }
+    __syncthreads();
+    int beyond = count_to - count, total = 0;
+    double weight_beyond = value_to - mine;
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) {
+      if (w < wave) {
+        beyond += memory().number[w];
+        weight_beyond += memory().sum[w];
+      }
+      total += memory().number[w];
+    }
+    // the first bin up to which there is surely not enough left out, the last one up to which there surely is
+    const double left = all * (1. - p) / share;
+    int low = kBins, high = 0, high_count = 0;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+      const int bin = kBins - 1 - (tid * PER + i), up_to = total - beyond;  // logits up to this bin's end
+      const bool enough = k > 0 ? up_to * share >= 1.4f * k + 8.f * share : weight_beyond <= 0.7 * left;
+      const bool short_of = k > 0 ? up_to * share < 0.7f * k - 8.f * share : weight_beyond > 1.4 * left;
+      if (!short_of) low = bin;
+      if (!enough && high == 0) {
+        high = bin + 1;
+        high_count = up_to;
+      }
+      beyond += counts[i];
+      weight_beyond += value[i];
+    }
+    if (low < kBins) atomicMin(&memory().before, low);
+    if (high > 0) atomicMax(&memory().found, high);
+    __syncthreads();
+    if (high > 0 && high == memory().found) memory().inside = high_count;
+    const int a = memory().before, b = memory().found + 1;
+    __syncthreads();
+    likely = (int)fminf(memory().inside * share, 1e9f);
+    return make_float2(a / kPer, b / kPer);
+  }
+
+  __device__ __forceinline__ float least_finite() const {
     float least = INFINITY;
     each<false>(0, [&](float logit, int) { least = logit > -INFINITY ? fminf(least, logit) : least; });
-    return -team_most<THREADS>(lds, -least);
+    return -team_most<THREADS>(memory(), -least);
   }
 
   // The sum of the weights that the cut keeps.
   template <bool LIST>
-  __device__ double kept_sum(int entries) {
+  __device__ __forceinline__ double kept_sum(int entries) {
     double sum = 0.;
     each<LIST>(entries, [&](float logit, int at) {
       if (keeps(logit, at)) sum += weight(logit);
     });
-    return team_sum<THREADS>(lds, sum);
+    return team_sum<THREADS>(memory(), sum);
   }
 
   // The place in the list of the token.
-  __device__ int locate_in_list(double u, double q, int entries, double& whole) {
+  __device__ __forceinline__ int locate_in_list(double u, double q, int entries, double& whole) {
     // each thread a run of the list
     const int per = (entries + THREADS - 1) / THREADS, from = min(tid * per, entries), to = min(from + per, entries);
     auto of = [&](int i) {
-      const float x = lds.value[i];
+      const float x = memory().value[i];
       const double w = keeps(x, i) ? weight(x) : 0.;
       return w >= q ? w : 0.;
     };
@@ -831,9 +933,9 @@ struct Team {
     for (int i = from; i < to; ++i) mine += of(i);
     const double sum = wave_sum(mine);
     __syncthreads();
-    if (lane == 0) lds.part[0][wave] = sum;
+    if (lane == 0) memory().part[0][wave] = sum;
     __syncthreads();
-    const double s = lane < WAVES ? lds.part[0][lane] : 0.;
+    const double s = lane < WAVES ? memory().part[0][lane] : 0.;
     whole = wave_sum(s);
     double target = u * whole;
     const int place = pick(s, WAVES, target);
@@ -850,23 +952,23 @@ struct Team {
             if (reached > target) break;
           }
         }
-        lds.found = chosen;
+        memory().found = chosen;
       }
     }
     __syncthreads();
-    return lds.found;
+    return memory().found;
   }
 
   // The list's place of the token, where the list has at most one logit for each thread and k of them, or all that min-p keeps, or what top-p
   // needs: each thread ranks its own by counting those above it; weights in that order give the number of them that the limits keep.
   // all: the weight that top-p goes by, where top-k has no part in it.  -1 where the list does not hold what is kept.
-  __device__ int rank_and_locate(double u, int k, double p, double q, double all, bool complete, int entries, double& whole) {
+  __device__ __forceinline__ int rank_and_locate(double u, int k, double p, double q, double all, bool complete, int entries, double& whole) {
     const bool mine = tid < entries;
-    const float x = mine ? lds.value[tid] : -INFINITY;
+    const float x = mine ? memory().value[tid] : -INFINITY;
     const uint64_t key = mine ? entry_of(x, tid) : 0;
     const double w = mine ? weight(x) : 0.;
-    uint64_t* const keys = lds.sorted;
-    double* const ordered = reinterpret_cast<double*>(lds.weights);
+    uint64_t* const keys = memory().sorted;
+    double* const ordered = reinterpret_cast<double*>(memory().weights);
     keys[tid] = key;
     __syncthreads();
     int rank = 0;
@@ -907,23 +1009,23 @@ struct Team {
     }
     if (q > 0.) kept = min(kept, kept_q);
     const double part = mine && rank < kept ? w : 0., part_to = wave_scan(part);
-    if (lane == 63) lds.part[0][wave] = part_to;
+    if (lane == 63) memory().part[0][wave] = part_to;
     __syncthreads();
-    const double s = lane < WAVES ? lds.part[0][lane] : 0.;
+    const double s = lane < WAVES ? memory().part[0][lane] : 0.;
     whole = wave_sum(s);
     double target = u * whole;
     const int place = pick(s, WAVES, target);
     if (wave == place) {
       const int at_lane = pick_lane(part, target);
-      if (lane == at_lane) lds.found = tid;
+      if (lane == at_lane) memory().found = tid;
     }
     __syncthreads();
-    return lds.found;
+    return memory().found;
   }
 
   // A bound that at least k logits reach, from the maxima of `groups` groups: the leading 16 bits of the k-th largest one, where every lane takes
   // the larger ones of four shares of them.
-  __device__ float bound_of(const float* tops, int groups, int k) {
+  __device__ __forceinline__ float bound_of(const float* tops, int groups, int k) {
     if (min(groups, 256) < k) return -INFINITY;
     uint32_t keys[4];
 #pragma unroll
@@ -948,11 +1050,12 @@ struct Team {
 template <int DTYPE, int THREADS, bool LIMITED, bool HELD>
 __global__ __launch_bounds__(THREADS) void sm_row_kernel(SmArgs a) {
   typedef Elem<DTYPE> E;
-  __shared__ RowLds<THREADS, LIMITED, HELD> lds;
+  typedef Team<DTYPE, THREADS, LIMITED, HELD> Rows;
+  typename Rows::Lds& lds = Rows::memory();
   const int tid = threadIdx.x;
   fill_roots(lds.root, tid);
   for (int r = blockIdx.x; r < a.rows; r += gridDim.x) {
-    Team<DTYPE, THREADS, LIMITED, HELD> t = {lds};
+    Rows t;
     t.tid = tid;
     t.lane = tid & 63;
     t.wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -971,7 +1074,7 @@ __global__ __launch_bounds__(THREADS) void sm_row_kernel(SmArgs a) {
     u32x4 x[kChunkVecs];
     Part part = {-INFINITY, 0.f, 0.};
     if constexpr (HELD) {
-      load_chunk<E, 256>(t.row, 0, t.nv, t.n, tid, x);
+      load_chunk<E, 256, false>(t.row, 0, t.nv, t.n, tid, x);
 #pragma unroll
       for (int j = 0; j < kChunkVecs; ++j) lds.held[j * 256 + tid] = x[j];
       most = chunk_most<E>(x);
@@ -1006,22 +1109,30 @@ __global__ __launch_bounds__(THREADS) void sm_row_kernel(SmArgs a) {
         else
           all = team_sum<THREADS>(lds, tid < a.segments ? part.sum * t.weight(part.most) : 0.);
       }
-      // what the list has to hold: all that min-p keeps, or k logits, or those near the maximum; rows of one segment fit it as they are
-      float bound = -INFINITY;
-      bool complete = false;  // all that min-p keeps
-      if (by_count || by_weight || q > 0.f) {
-        bound = most - kNear / scale;
+      // what the list has to hold: k logits, or what makes up p of the weight, or all that min-p keeps
+      float bound = -FLT_MAX;
+      float2 bracket = {0.f, 0.f};
+      int likely = 0;
+      if (by_count || by_weight) {
         if (by_count && !HELD) bound = fmaxf(bound, t.bound_of(a.tops + (int64_t)r * a.segments * kTops, a.segments * kTops, k));
-        if (q > 0.f) {
-          const float low = most + (logf(fminf(q, 1.f)) * 1.00001f - 1e-5f) / scale;  // (below the border, whatever the roundings)
-          const float lower = low - fabsf(low) * 1e-6f;
-          complete = lower >= bound;
-          bound = fmaxf(bound, lower);
+        if (bound == -FLT_MAX) {
+          bracket = t.estimate(by_count ? k : 0, (double)p, all, likely);
+          bound = most - bracket.y / scale;
         }
-        bound = fminf(fmaxf(bound, -FLT_MAX), most);
       }
+      bool complete = !by_count && !by_weight;  // all that min-p keeps
+      if (q > 0.f) {
+        const float low = most + (logf(fminf(q, 1.f)) * 1.00001f - 1e-5f) / scale;  // (below the border, whatever the roundings)
+        const float lower = low - fabsf(low) * 1e-6f;
+        if (complete || lower >= bound) {
+          complete = true;
+          likely = 0;
+          bound = lower;
+        }
+      }
+      bound = fminf(fmaxf(bound, -FLT_MAX), most);
       int entries = -1;
-      if (bound > -INFINITY) entries = t.fill_list(bound);
+      if ((by_count || by_weight || q > 0.f) && likely <= kList) entries = t.fill_list(bound);
       if (entries >= 0 && entries <= THREADS && (!by_count || k <= entries || (complete && !by_weight)) && (by_count || by_weight || complete)) {
         const int place = t.rank_and_locate((double)u, by_count ? k : 0, (double)p, least_weight, all, complete, entries, whole);
         if (place >= 0) token = lds.index[place];
@@ -1030,7 +1141,7 @@ __global__ __launch_bounds__(THREADS) void sm_row_kernel(SmArgs a) {
         const float lowest = bound;
         if (by_count) {
           if (k < entries)
-            enough = t.template find_cut<false, true>((double)k, lowest, entries);
+            enough = t.template find_cut<false, true>((double)k, lowest, entries, make_float2(0.f, 0.f));
           else
             enough = k == entries || complete;
         }
@@ -1039,7 +1150,7 @@ __global__ __launch_bounds__(THREADS) void sm_row_kernel(SmArgs a) {
           if (by_count && k > entries)
             enough = false;  // (the weight of k logits is not known)
           else if (target <= kept)
-            t.template find_cut<true, true>(target, lowest, entries);
+            t.template find_cut<true, true>(target, lowest, entries, make_float2(0.f, 0.f));
           else
             enough = complete;
         }
@@ -1050,8 +1161,8 @@ __global__ __launch_bounds__(THREADS) void sm_row_kernel(SmArgs a) {
       }
       if (token < 0) {
         const float least = t.least_finite();
-        if (by_count) t.template find_cut<false, false>((double)k, least, 0);
-        if (by_weight) t.template find_cut<true, false>(fmax((by_count ? t.template kept_sum<false>(0) : all) * (double)p, 0.), least, 0);
+        if (by_count) t.template find_cut<false, false>((double)k, least, 0, bracket);
+        if (by_weight) t.template find_cut<true, false>(fmax((by_count ? t.template kept_sum<false>(0) : all) * (double)p, 0.), least, 0, by_count ? make_float2(0.f, 0.f) : bracket);
         token = t.template locate<true>(
             0, t.nv, (double)u,
             [&](float logit, int at) {

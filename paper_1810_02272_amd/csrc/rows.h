@@ -70,6 +70,14 @@ __device__ __forceinline__ u32x4 row_vec(const typename E::T* row, int v, int n)
   return E::pack(x);
 }
 
+// The same of a row of at least a vector, and -inf throughout beyond its last one: one load, whatever v is.
+template <class E>
+__device__ __forceinline__ u32x4 long_row_vec(const typename E::T* row, int v, int nv, int n) {
+  const Slot<E> at = slot_of<E>(min(v, nv - 1), n);
+  const u32x4 r = load_vec<E>(row + at.base);
+  return v >= nv ? lowest_vec<E>() : at.lo ? without_first<E>(r, at.lo) : r;
+}
+
 template <int THREADS>
 __device__ __forceinline__ void team_sync() {
   if constexpr (THREADS == 64)
