@@ -61,7 +61,7 @@ struct SmArgs {
 
 constexpr int kBins = 1024;     // of a histogram
 constexpr int kSorted = 1024;   // logits that are put in order
-constexpr int kList = 4096;     // logits near the maximum
+constexpr int kList = 12288;    // logits near the maximum that a long row's list holds
 constexpr int kGroups = 16;     // of vectors, whose sums stand side by side
 constexpr int kTops = 4;        // groups of lanes of a segment
 constexpr int kChunkVecs = 4;   // vectors of a lane of the first launch, and of a thread that holds a row's share
@@ -321,6 +321,9 @@ struct Cut {
   int last;  // an index of the row, or a place in the list
 };
 
+template <bool HELD>
+constexpr int kListed = HELD ? 2048 : kList;  // (rows that a team holds are few passes away)
+
 template <int THREADS, bool LIMITED, bool HELD>
 struct RowLds : Shared<THREADS> {
   static constexpr int WAVES = THREADS / 64;
@@ -330,8 +333,8 @@ struct RowLds : Shared<THREADS> {
   uint64_t sorted[LIMITED ? kSorted : 1];
   uint64_t weights[LIMITED ? kBins : 1];
   int count[LIMITED ? kBins : 1];
-  float value[LIMITED ? kList : 1];  // the list: logits near the maximum and their indices, in the order of these
-  int index[LIMITED ? kList : 1];
+  float value[LIMITED ? kListed<HELD> : 1];  // the list: logits near the maximum and their indices, in the order of these, in a part for each wave
+  int index[LIMITED ? kListed<HELD> : 1];
   uint64_t whole[WAVES];
   int number[WAVES];
   uint32_t places;
@@ -343,7 +346,7 @@ struct Team {
   typedef Elem<DTYPE> E;
   typedef typename E::T T;
   typedef RowLds<THREADS, LIMITED, HELD> Lds;
-  static constexpr int VEC = E::VEC, WAVES = THREADS / 64, SHARE = kList / WAVES;  // of the list, for each wave
+  static constexpr int VEC = E::VEC, WAVES = THREADS / 64, SHARE = kListed<HELD> / WAVES;  // of the list, for each wave
 
   // (a function's own shared memory: a reference kept in the team would make every access a generic one)
   static __device__ __forceinline__ Lds& memory() {
@@ -356,6 +359,7 @@ struct Team {
   float m, scale;  // the maximum
   Exponential weight;
   Cut cut;
+  int part_end[WAVES];  // of the list's parts, one after the other
 
   __device__ __forceinline__ u32x4 vec(int v) const {
     if constexpr (HELD) return v < nv ? memory().held[v] : lowest_vec<E>();
@@ -365,6 +369,14 @@ struct Team {
   __device__ __forceinline__ bool keeps(float x, int at) const { return x > cut.value || (x == cut.value && at <= cut.last); }
 
   __device__ __forceinline__ float distance(float x) const { return fminf((m - x) * scale, FLT_MAX); }
+
+  // Where the i-th of the list stands.
+  __device__ __forceinline__ int place_of(int i) const {
+    int place = i;
+#pragma unroll
+    for (int w = 0; w < WAVES - 1; ++w) place += i >= part_end[w] ? SHARE - (part_end[w] - (w ? part_end[w - 1] : 0)) : 0;
+    return place;
+  }
 
   // f(logit, index) for the elements of a vector, in order; compactly, two at a time.
   template <class F>
@@ -383,7 +395,7 @@ struct Team {
   template <bool LIST, class F>
   __device__ __forceinline__ void each(int entries, F&& f) const {
     if constexpr (LIST) {
-      for (int i = tid; i < entries; i += THREADS) f(memory().value[i], i);
+      for (int i = tid; i < entries; i += THREADS) f(memory().value[place_of(i)], i);
     } else {
       for (int v0 = 0; v0 < nv; v0 += kAhead * THREADS) {
         u32x4 x[kAhead];
@@ -593,9 +605,9 @@ struct Team {
   __device__ __forceinline__ uint64_t fixed(double w) const { return (uint64_t)ldexp(w, shift); }
 
   template <bool WEIGHT>
-  __device__ __forceinline__ void count_in(int b, float logit) {
+  __device__ __forceinline__ void count_in(int b, double w) {
     atomicAdd(&memory().count[b], 1);
-    if (WEIGHT) atomicAdd((unsigned long long*)&memory().weights[b], (unsigned long long)fixed(weight(logit)));
+    if (WEIGHT) atomicAdd((unsigned long long*)&memory().weights[b], (unsigned long long)fixed(w));
   }
 
   // Moves the cut to where the counts (WEIGHT: the weights) of what it keeps reach the target, in descending order.  least: the least finite logit.
@@ -620,11 +632,12 @@ struct Team {
       each<LIST>(entries, [&](float logit, int at) {
         const float d = distance(logit);
         if (!(d <= to) || !(logit > -INFINITY) || !keeps(logit, at)) return;
+        const double w = WEIGHT ? weight(logit) : 0.;
         if (d > from) {
-          count_in<WEIGHT>(min((int)((d - start) * per), kBins - 1), logit);
+          count_in<WEIGHT>(min((int)((d - start) * per), kBins - 1), w);
         } else {
           ++count;
-          if (WEIGHT) sum += weight(logit);
+          sum += w;
         }
       });
       above_sum = 0.;
@@ -695,7 +708,7 @@ struct Team {
       clear_bins();
       each<LIST>(entries, [&](float logit, int at) {
         const uint32_t key = order_key(logit);
-        if (key <= high && key >= low && keeps(logit, at)) count_in<WEIGHT>((int)((high - key) >> bits), logit);
+        if (key <= high && key >= low && keeps(logit, at)) count_in<WEIGHT>((int)((high - key) >> bits), WEIGHT ? weight(logit) : 0.);
       });
       uint64_t before = WEIGHT ? 0 : (uint64_t)above;
       int count_before = above;
@@ -712,7 +725,7 @@ struct Team {
     if constexpr (LIST) {  // places in turns of the team
       int before = 0;
       for (int i0 = 0; i0 < entries; i0 += THREADS) {
-        const bool mine = i0 + tid < entries && memory().value[i0 + tid] == x;
+        const bool mine = i0 + tid < entries && memory().value[place_of(i0 + tid)] == x;
         const uint64_t mask = __ballot(mine);
         __syncthreads();
         if (lane == 0) memory().number[wave] = (int)__builtin_popcountll(mask);
@@ -769,18 +782,18 @@ struct Team {
     return memory().found;
   }
 
-  // Logits from `bound` on into the list, in the order of their indices: each wave takes a part of the row and fills a part of the list, which are then
-  // moved together.  The number of them, or -1 where a wave found more than its part holds.
+  // Logits from `bound` on into the list, in the order of their indices: each wave takes a part of the row and fills a part of the list.  The number of them, or -1 where a wave found more than its part holds.
   __device__ __forceinline__ int fill_list(float bound) {
     const int per = ((nv + WAVES - 1) / WAVES + 63) / 64 * 64, to = min(nv, (wave + 1) * per);
     int mine = 0;
     __syncthreads();
-    for (int v0 = wave * per; v0 < to && mine <= SHARE; v0 += kAhead * 64) {
-      u32x4 x[kAhead];
+    constexpr int AHEAD = HELD ? 4 : 16;
+    for (int v0 = wave * per; v0 < to && mine <= SHARE; v0 += AHEAD * 64) {
+      u32x4 x[AHEAD];
 #pragma unroll
-      for (int j = 0; j < kAhead; ++j) x[j] = vec(v0 + j * 64 + lane < to ? v0 + j * 64 + lane : nv);
+      for (int j = 0; j < AHEAD; ++j) x[j] = vec(v0 + j * 64 + lane < to ? v0 + j * 64 + lane : nv);
 #pragma unroll
-      for (int j = 0; j < kAhead; ++j) {
+      for (int j = 0; j < AHEAD; ++j) {
         uint32_t mask = 0;
 #pragma unroll
         for (int i = 0; i < VEC; ++i) mask |= E::get(x[j], i) >= bound ? 1u << i : 0u;
@@ -802,33 +815,16 @@ struct Team {
     }
     if (lane == 0) memory().number[wave] = mine;
     __syncthreads();
-    int before = 0, all = 0;
+    int all = 0;
     bool over = false;
 #pragma unroll
     for (int w = 0; w < WAVES; ++w) {
-      const int count = memory().number[w];
+      const int count = __builtin_amdgcn_readfirstlane(memory().number[w]);
       over |= count > SHARE;
-      before += w < wave ? count : 0;
       all += count;
+      part_end[w] = all;
     }
-    if (over) return -1;
-    float value[SHARE / 64];
-    int index[SHARE / 64];
-#pragma unroll
-    for (int i = 0; i < SHARE / 64; ++i)
-      if (i * 64 + lane < mine) {
-        value[i] = memory().value[wave * SHARE + i * 64 + lane];
-        index[i] = memory().index[wave * SHARE + i * 64 + lane];
-      }
-    __syncthreads();
-#pragma unroll
-    for (int i = 0; i < SHARE / 64; ++i)
-      if (i * 64 + lane < mine) {
-        memory().value[before + i * 64 + lane] = value[i];
-        memory().index[before + i * 64 + lane] = index[i];
-      }
-    __syncthreads();
-    return all;
+    return over ? -1 : all;
   }
 
   // Where the k-th logit, or (k = 0) the place up to which the weights reach p of `all`, is likely to lie: distances that are likely before and
@@ -925,7 +921,7 @@ struct Team {
     // each thread a run of the list
     const int per = (entries + THREADS - 1) / THREADS, from = min(tid * per, entries), to = min(from + per, entries);
     auto of = [&](int i) {
-      const float x = memory().value[i];
+      const float x = memory().value[place_of(i)];
       const double w = keeps(x, i) ? weight(x) : 0.;
       return w >= q ? w : 0.;
     };
@@ -964,7 +960,7 @@ struct Team {
   // all: the weight that top-p goes by, where top-k has no part in it.  -1 where the list does not hold what is kept.
   __device__ __forceinline__ int rank_and_locate(double u, int k, double p, double q, double all, bool complete, int entries, double& whole) {
     const bool mine = tid < entries;
-    const float x = mine ? memory().value[tid] : -INFINITY;
+    const float x = mine ? memory().value[place_of(tid)] : -INFINITY;
     const uint64_t key = mine ? entry_of(x, tid) : 0;
     const double w = mine ? weight(x) : 0.;
     uint64_t* const keys = memory().sorted;
@@ -1115,7 +1111,9 @@ __global__ __launch_bounds__(THREADS) void sm_row_kernel(SmArgs a) {
       int likely = 0;
       if (by_count || by_weight) {
         if (by_count && !HELD) bound = fmaxf(bound, t.bound_of(a.tops + (int64_t)r * a.segments * kTops, a.segments * kTops, k));
-        if (bound == -FLT_MAX) {
+        if (!by_count && q > 0.f && all <= (double)q * kListed<HELD>) {
+          // what min-p keeps is few: each of them has a share q of the weight or more
+        } else if (bound == -FLT_MAX) {
           bracket = t.estimate(by_count ? k : 0, (double)p, all, likely);
           bound = most - bracket.y / scale;
         }
@@ -1124,7 +1122,7 @@ __global__ __launch_bounds__(THREADS) void sm_row_kernel(SmArgs a) {
       if (q > 0.f) {
         const float low = most + (logf(fminf(q, 1.f)) * 1.00001f - 1e-5f) / scale;  // (below the border, whatever the roundings)
         const float lower = low - fabsf(low) * 1e-6f;
-        if (complete || lower >= bound) {
+        if (complete || (lower >= bound && !(by_count && by_weight))) {  // (the weight of k logits is that of all of them)
           complete = true;
           likely = 0;
           bound = lower;
@@ -1132,10 +1130,10 @@ __global__ __launch_bounds__(THREADS) void sm_row_kernel(SmArgs a) {
       }
       bound = fminf(fmaxf(bound, -FLT_MAX), most);
       int entries = -1;
-      if ((by_count || by_weight || q > 0.f) && likely <= kList) entries = t.fill_list(bound);
+      if ((by_count || by_weight || q > 0.f) && likely <= kListed<HELD>) entries = t.fill_list(bound);
       if (entries >= 0 && entries <= THREADS && (!by_count || k <= entries || (complete && !by_weight)) && (by_count || by_weight || complete)) {
         const int place = t.rank_and_locate((double)u, by_count ? k : 0, (double)p, least_weight, all, complete, entries, whole);
-        if (place >= 0) token = lds.index[place];
+        if (place >= 0) token = lds.index[t.place_of(place)];
       } else if (entries >= 0) {
         bool enough = by_count || by_weight || complete;
         const float lowest = bound;
@@ -1155,7 +1153,7 @@ __global__ __launch_bounds__(THREADS) void sm_row_kernel(SmArgs a) {
             enough = complete;
         }
         if (enough)
-          token = lds.index[t.locate_in_list((double)u, least_weight, entries, whole)];
+          token = lds.index[t.place_of(t.locate_in_list((double)u, least_weight, entries, whole))];
         else
           t.cut = Cut{-INFINITY, INT_MAX};
       }
