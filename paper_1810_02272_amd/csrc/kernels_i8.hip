@@ -370,18 +370,19 @@ __device__ __forceinline__ void pair_terms(float a, float b, uint32_t (&w)[TERMS
 }
 
 // TILE rows of the result (filter: outputs, data: rows of x) by TILE inputs.  Both factors are made into bf16 operands on the way from memory to
-// shared memory, where the 8 terms of the sum that a lane of the matrix instructions takes lie together: a thread takes 8 terms of two
-// neighbouring rows or columns, so that turning them costs nothing beside the conversion.  The next step's values are on their way
-// in registers while the instructions work on this one's.
+// shared memory, where the 8 terms of the sum that a lane of the matrix instructions takes lie together.  Half of the waves do it for dz, half for
+// the codes: a lane takes 8 terms of four neighbouring rows or columns, so that turning them costs nothing beside the conversion.  The next step's values
+// are asked for before the instructions on this one's first term and converted after them: a compute unit's matrix and vector units are then
+// both busy, with waves that are at different places.
 // Waves of 64 rows by 16 NT inputs.
 template <int DTYPE, bool FILTER, int TILE>
 __global__ __launch_bounds__(TILE == 256 ? 512 : 256, 2) void i8_gradient_kernel(BwdArgs a) {
   typedef Elem<DTYPE> E;
   typedef typename E::T T;
-  constexpr int THREADS = TILE == 256 ? 512 : 256, WN = 2, NT = TILE / (16 * WN), TERMS = DTYPE == MI355_BF16 ? 2 : 3;
-  // pieces of 16 bytes: [term][group of 8 terms of the sum][row], and the same of the codes; what is added keeps the threads that write on banks of
-  // their own
-  constexpr int A_GROUP = TILE + 4, B_GROUP = TILE + TILE / 8, A_TERM = 4 * A_GROUP, BUFFER = TERMS * A_TERM + 4 * B_GROUP;
+  constexpr int THREADS = TILE == 256 ? 512 : 256, HALF = THREADS / 2, WN = 2, NT = TILE / (16 * WN), TERMS = DTYPE == MI355_BF16 ? 2 : 3;
+  // pieces of 16 bytes: [term][group of 8 terms of the sum][place], and the same of the codes; two are left out after every 16, and four
+  // after a group, so that the lanes that write meet no bank twice
+  constexpr int GROUP = TILE + TILE / 8 + 4, TERM = 4 * GROUP, BUFFER = (TERMS + 1) * TERM;
   __shared__ __attribute__((aligned(16))) u32x4 lds[2][BUFFER];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), wm = wave / WN, wn = wave % WN;
   const int rows = FILTER ? a.o : a.n, depth = FILTER ? a.n : a.o;
@@ -389,119 +390,126 @@ __global__ __launch_bounds__(TILE == 256 ? 512 : 256, 2) void i8_gradient_kernel
   tile_place((rows + TILE - 1) / TILE, (a.k + TILE - 1) / TILE, tm, tn);
   const int r0 = tm * TILE, i0 = tn * TILE;
   const int first = blockIdx.y * a.per, steps = min(a.per, (depth + kStep - 1) / kStep - first);
-
-  // codes: inputs 2 p, 2 p + 1 of group g; filter: dz of outputs 2 p, 2 p + 1 the same way
-  const int g = __builtin_amdgcn_readfirstlane(tid / (TILE / 2)), p = tid % (TILE / 2);
-  const int col = (int)min((int64_t)i0 + 2 * p, a.row - 2);
-  const bool inside = r0 + TILE <= rows;
   const bool sum_bias = FILTER && a.db && tn == 0;
-  // data: 8 terms of rows (tid / 4) and on, THREADS / 4 apart
-  constexpr int DATA_ROWS = FILTER ? 1 : TILE * 4 / THREADS;
-  typedef typename std::conditional<DTYPE == MI355_F32, u32x2, uint32_t>::type Two;
-  Two za[8];                    // filter
-  u32x4 zd[DATA_ROWS][DTYPE == MI355_F32 ? 2 : 1];  // data
-  float s[8];
-  uint16_t c[8];
-  float bias[2] = {0.f, 0.f};
 
-  auto load = [&](int step) {
+  const bool of_dz = wave < HALF / 64;
+  const int half = of_dz ? tid : tid - HALF, g = half / (TILE / 4), p = half % (TILE / 4);  // group, four rows or columns 4 p ..
+  const int at4 = (p >> 4) * 72 + (p & 15);  // the place of the first of them: of 64 neighbours, 4 l + q stands at 16 q + l (and the pieces left out)
+  const int col = (int)min((int64_t)i0 + 4 * p, a.row - 4);
+  const bool inside = r0 + TILE <= rows;
+  constexpr int DATA_ROWS = TILE * 4 / HALF;  // data: 8 terms of rows half / 4 and on, HALF / 4 apart
+  constexpr int WORDS = DTYPE == MI355_F32 ? 4 : 2;
+  typedef typename std::conditional<DTYPE == MI355_F32, u32x4, u32x2>::type Four;
+  struct __attribute__((packed, aligned(sizeof(T)))) FourMem {
+    Four v;
+  };
+  float s[8];
+  float bias[4] = {0.f, 0.f, 0.f, 0.f};
+  f32x4 acc[4][NT] = {};
+
+  struct Filter {  // what is on its way
+    Four z[8];
+  };
+  struct Data {
+    u32x4 z[DATA_ROWS][DTYPE == MI355_F32 ? 2 : 1];
+  };
+  typename std::conditional<FILTER, Filter, Data>::type raw;
+  uint32_t c[8];
+
+  auto load_codes = [&](int step) {
     const int d0 = (first + step) * kStep + 8 * g;
-    const int8_t* const at = a.codes + (int64_t)d0 * a.row + col;
-    if (d0 + 8 <= depth) {
+    const int8_t* const at = a.codes + col;
 #pragma unroll
-      for (int j = 0; j < 8; ++j) c[j] = *reinterpret_cast<const uint16_t*>(at + j * a.row);
+    for (int j = 0; j < 8; ++j) c[j] = *reinterpret_cast<const uint32_t*>(at + (int64_t)min(d0 + j, depth - 1) * a.row);
+  };
+  auto load_scales = [&](int d0) {
+    if (d0 + 8 <= depth) {
+      const u32x4 s0 = load_vec<Elem<MI355_F32>>(a.scale + d0), s1 = load_vec<Elem<MI355_F32>>(a.scale + d0 + 4);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) s[j] = Elem<MI355_F32>::get(j < 4 ? s0 : s1, j & 3);
     } else {
 #pragma unroll
-      for (int j = 0; j < 8; ++j) c[j] = *reinterpret_cast<const uint16_t*>(a.codes + (int64_t)min(d0 + j, depth - 1) * a.row + col);
+      for (int j = 0; j < 8; ++j) s[j] = d0 + j < depth ? a.scale[d0 + j] : 0.f;
     }
+  };
+  auto load_dz = [&](int step) {
     if constexpr (FILTER) {
+      const int d0 = (first + step) * kStep + 8 * g;
+      load_scales(d0);
       const T* const z = static_cast<const T*>(a.dz);
+      if (inside) {
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const int n = min(d0 + j, depth - 1);
-        s[j] = a.scale[n];
-        if (inside) {
-          struct __attribute__((packed, aligned(sizeof(T)))) Mem {
-            Two v;
-          };
-          za[j] = reinterpret_cast<const Mem*>(z + (int64_t)n * a.o + r0 + 2 * p)->v;
-        } else {
-          const T* const row = z + (int64_t)n * a.o;
-          const T lo = row[min(r0 + 2 * p, a.o - 1)], hi = row[min(r0 + 2 * p + 1, a.o - 1)];
-          if constexpr (DTYPE == MI355_F32)
-            za[j] = u32x2{__builtin_bit_cast(uint32_t, lo), __builtin_bit_cast(uint32_t, hi)};
-          else
-            za[j] = (uint32_t)__builtin_bit_cast(uint16_t, lo) | (uint32_t)__builtin_bit_cast(uint16_t, hi) << 16;
+        for (int j = 0; j < 8; ++j) raw.z[j] = reinterpret_cast<const FourMem*>(z + (int64_t)min(d0 + j, depth - 1) * a.o + r0 + 4 * p)->v;
+      } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const T* const row = z + (int64_t)min(d0 + j, depth - 1) * a.o;
+          float f[E::VEC];
+#pragma unroll
+          for (int q = 0; q < E::VEC; ++q) f[q] = q < 4 ? E::to_float(row[min(r0 + 4 * p + q, a.o - 1)]) : 0.f;
+          const u32x4 v = E::pack(f);
+#pragma unroll
+          for (int w = 0; w < WORDS; ++w) raw.z[j][w] = v[w];
         }
       }
       if (d0 + 8 > depth) {
 #pragma unroll
         for (int j = 0; j < 8; ++j)
-          if (d0 + j >= depth) {
-            za[j] = Two{};
-            s[j] = 0.f;
-          }
+          if (d0 + j >= depth) raw.z[j] = Four{};
       }
     } else {
-      const int at_o = (first + step) * kStep + 8 * (tid & 3);
-      if (at_o + 8 <= depth) {
-        const u32x4 s0 = load_vec<Elem<MI355_F32>>(a.scale + at_o), s1 = load_vec<Elem<MI355_F32>>(a.scale + at_o + 4);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) s[j] = Elem<MI355_F32>::get(j < 4 ? s0 : s1, j & 3);
-      } else {
-#pragma unroll
-        for (int j = 0; j < 8; ++j) s[j] = at_o + j < depth ? a.scale[at_o + j] : 0.f;
-      }
+      const int d0 = (first + step) * kStep + 8 * (half & 3);
+      load_scales(d0);
 #pragma unroll
       for (int i = 0; i < DATA_ROWS; ++i) {
-        const T* const z = static_cast<const T*>(a.dz) + (int64_t)min(r0 + tid / 4 + i * (THREADS / 4), rows - 1) * a.o;
-        if (at_o + 8 <= depth) {
-          zd[i][0] = load_vec<E>(z + at_o);
-          if constexpr (DTYPE == MI355_F32) zd[i][1] = load_vec<E>(z + at_o + 4);
+        const T* const z = static_cast<const T*>(a.dz) + (int64_t)min(r0 + half / 4 + i * (HALF / 4), rows - 1) * a.o;
+        if (d0 + 8 <= depth) {
+          raw.z[i][0] = load_vec<E>(z + d0);
+          if constexpr (DTYPE == MI355_F32) raw.z[i][1] = load_vec<E>(z + d0 + 4);
         } else {
           float f[8];
 #pragma unroll
-          for (int j = 0; j < 8; ++j) f[j] = at_o + j < depth ? E::to_float(z[at_o + j]) : 0.f;
+          for (int j = 0; j < 8; ++j) f[j] = d0 + j < depth ? E::to_float(z[d0 + j]) : 0.f;
           if constexpr (DTYPE == MI355_F32) {
-            zd[i][0] = E::pack({f[0], f[1], f[2], f[3]});
-            zd[i][1] = E::pack({f[4], f[5], f[6], f[7]});
+            raw.z[i][0] = E::pack({f[0], f[1], f[2], f[3]});
+            raw.z[i][1] = E::pack({f[4], f[5], f[6], f[7]});
           } else {
-            zd[i][0] = E::pack(f);
+            raw.z[i][0] = E::pack(f);
           }
         }
       }
     }
   };
-
-  auto put = [&](int buffer) {
-    u32x4* const A = lds[buffer];
-    u32x4* const B = A + TERMS * A_TERM;
+  auto put_codes = [&](u32x4* buffer) {
+    u32x4* const to = buffer + TERMS * TERM + g * GROUP + at4;
 #pragma unroll
-    for (int e = 0; e < 2; ++e) {
+    for (int q = 0; q < 4; ++q) {
       u32x4 w;
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         uint32_t two[1];
-        pair_terms<1>((float)(int8_t)(c[2 * j] >> 8 * e), (float)(int8_t)(c[2 * j + 1] >> 8 * e), two);
+        pair_terms<1>((float)(int8_t)(c[2 * j] >> 8 * q), (float)(int8_t)(c[2 * j + 1] >> 8 * q), two);
         w[j] = two[0];
       }
-      const int i = 2 * p + e, place = (i & ~63) + (i & 3) * 16 + (i >> 2 & 15);  // column_at(place) = i
-      B[g * B_GROUP + place + 2 * (place >> 4)] = w;
+      to[18 * q] = w;
     }
+  };
+  auto put_dz = [&](u32x4* buffer) {
     if constexpr (FILTER) {
+      u32x4* const to = buffer + g * GROUP + at4;
 #pragma unroll
-      for (int e = 0; e < 2; ++e) {
+      for (int q = 0; q < 4; ++q) {
         float v[8];
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-          if constexpr (DTYPE == MI355_F32)
-            v[j] = E::get(u32x4{za[j][0], za[j][1], 0, 0}, e);
-          else
-            v[j] = E::get(u32x4{za[j], 0, 0, 0}, e);
+          u32x4 z = {};
+#pragma unroll
+          for (int w = 0; w < WORDS; ++w) z[w] = raw.z[j][w];
+          v[j] = E::get(z, q);
         }
         if (sum_bias) {
 #pragma unroll
-          for (int j = 0; j < 8; ++j) bias[e] += v[j];
+          for (int j = 0; j < 8; ++j) bias[q] += v[j];
         }
         u32x4 w[TERMS];
 #pragma unroll
@@ -512,7 +520,7 @@ __global__ __launch_bounds__(TILE == 256 ? 512 : 256, 2) void i8_gradient_kernel
           for (int t = 0; t < TERMS; ++t) w[t][j] = two[t];
         }
 #pragma unroll
-        for (int t = 0; t < TERMS; ++t) A[t * A_TERM + g * A_GROUP + 2 * p + e] = w[t];
+        for (int t = 0; t < TERMS; ++t) to[t * TERM + 18 * q] = w[t];
       }
     } else {
 #pragma unroll
@@ -522,49 +530,63 @@ __global__ __launch_bounds__(TILE == 256 ? 512 : 256, 2) void i8_gradient_kernel
         for (int j = 0; j < 4; ++j) {
           uint32_t two[TERMS];
           constexpr int PER = E::VEC;
-          pair_terms<TERMS>(E::get(zd[i][2 * j / PER], 2 * j % PER) * s[2 * j], E::get(zd[i][2 * j / PER], 2 * j % PER + 1) * s[2 * j + 1], two);
+          pair_terms<TERMS>(E::get(raw.z[i][2 * j / PER], 2 * j % PER) * s[2 * j], E::get(raw.z[i][2 * j / PER], 2 * j % PER + 1) * s[2 * j + 1], two);
 #pragma unroll
           for (int t = 0; t < TERMS; ++t) w[t][j] = two[t];
         }
+        const int row = half / 4 + i * (HALF / 4);
 #pragma unroll
-        for (int t = 0; t < TERMS; ++t) A[t * A_TERM + (tid & 3) * A_GROUP + tid / 4 + i * (THREADS / 4)] = w[t];
+        for (int t = 0; t < TERMS; ++t) buffer[t * TERM + (half & 3) * GROUP + row + 2 * (row >> 4)] = w[t];
       }
     }
   };
 
-  f32x4 acc[4][NT] = {};
-  if (steps > 0) {
+  // Both kinds of waves take the same steps, and meet at the same barriers.
+  auto work = [&](auto&& load, auto&& put) {
     load(0);
-    put(0);
-  }
-  __syncthreads();
-  for (int step = 0; step < steps; ++step) {
-    const bool more = step + 1 < steps;
-    if (more) load(step + 1);
-    const u32x4* const A = lds[step & 1] + (lane >> 4) * A_GROUP + wm * 64 + (lane & 15);
-    const u32x4* const B = lds[step & 1] + TERMS * A_TERM + (lane >> 4) * B_GROUP + wn * NT * 18 + (lane & 15);
-    bf16x8 w[NT];
-#pragma unroll
-    for (int u = 0; u < NT; ++u) w[u] = __builtin_bit_cast(bf16x8, B[u * 18]);
-#pragma unroll
-    for (int t = 0; t < TERMS; ++t) {
-      bf16x8 x[4];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) x[i] = __builtin_bit_cast(bf16x8, A[t * A_TERM + 16 * i]);
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int u = 0; u < NT; ++u) acc[i][u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x[i], w[u], acc[i][u], 0, 0, 0);
-    }
-    if (more) put((step + 1) & 1);
+    put(lds[0]);
     __syncthreads();
+    for (int step = 0; step < steps; ++step) {
+      const bool more = step + 1 < steps;
+      if (more) load(step + 1);
+      __builtin_amdgcn_sched_barrier(0);
+      const u32x4* const A = lds[step & 1] + (lane >> 4) * GROUP + wm * 72 + (lane & 15);
+      const u32x4* const B = lds[step & 1] + TERMS * TERM + (lane >> 4) * GROUP + wn * NT * 18 + (lane & 15);
+      bf16x8 w[NT];
+#pragma unroll
+      for (int u = 0; u < NT; ++u) w[u] = __builtin_bit_cast(bf16x8, B[u * 18]);
+#pragma unroll
+      for (int t = 0; t < TERMS; ++t) {
+        bf16x8 x[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[i] = __builtin_bit_cast(bf16x8, A[t * TERM + 18 * i]);
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+          for (int u = 0; u < NT; ++u) acc[i][u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x[i], w[u], acc[i][u], 0, 0, 0);
+        if (t + 2 == TERMS) {
+          __builtin_amdgcn_sched_barrier(0);
+          if (more) put(lds[(step + 1) & 1]);
+          __builtin_amdgcn_sched_barrier(0);
+        }
+      }
+      __syncthreads();
+    }
+  };
+  if (steps > 0) {
+    if (of_dz)
+      work(load_dz, put_dz);
+    else
+      work(load_codes, put_codes);
   }
 
   const bool split = gridDim.y > 1;
   if (sum_bias) {  // the four groups' sums of each output
     float* const sums = reinterpret_cast<float*>(lds);
-    sums[g * TILE + 2 * p] = bias[0];
-    sums[g * TILE + 2 * p + 1] = bias[1];
+    if (of_dz) {
+#pragma unroll
+      for (int q = 0; q < 4; ++q) sums[g * TILE + 4 * p + q] = bias[q];
+    }
     __syncthreads();
     if (tid < TILE && r0 + tid < a.o) {
       const float v = (sums[tid] + sums[TILE + tid]) + (sums[2 * TILE + tid] + sums[3 * TILE + tid]);
@@ -582,7 +604,7 @@ __global__ __launch_bounds__(TILE == 256 ? 512 : 256, 2) void i8_gradient_kernel
     for (int i = 0; i < 4; ++i)
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
-        const int to_row = r0 + wm * 64 + i * 16 + 4 * (lane >> 4) + r;
+        const int in_tile = 4 * (lane >> 4) + r, to_row = r0 + wm * 64 + (FILTER ? 4 * in_tile + i : 16 * i + in_tile);  // (filter: as the places go)
         if (to_row >= rows) continue;
         float v[4];
 #pragma unroll
