@@ -26,6 +26,7 @@ struct i8_desc {
   int32_t filter_tile, filter_splits, filter_per;  // backward filter: tile (rows and columns), workgroups that share a sum, steps of each
   int32_t data_tile, data_splits, data_per;        // backward data
   int32_t waves;           // of the forward pass by rows
+  int32_t token;           // few rows are brought to 8 bits by the workgroups that multiply them
   size_t ws_bytes;
   char names[192];
 };
@@ -68,12 +69,12 @@ __device__ __forceinline__ int code_of(float x, float s, float inverse) {
 // THREADS threads for a row: its largest magnitude, then the codes, from registers for up to NV vectors a thread, read again beyond.  Bound by
 // memory.  THREADS 64: a wave for each row, four in a workgroup.
 template <int DTYPE, int THREADS, int NV>
-__global__ __launch_bounds__(256) void i8_quantise_kernel(const void* __restrict__ x, int8_t* __restrict__ codes, float* __restrict__ scales, int rows,
+__global__ __launch_bounds__(THREADS == 64 ? 256 : THREADS) void i8_quantise_kernel(const void* __restrict__ x, int8_t* __restrict__ codes, float* __restrict__ scales, int rows,
                                                           int k, int64_t row_bytes) {
   typedef Elem<DTYPE> E;
   typedef typename E::T T;
   constexpr int VEC = E::VEC;
-  __shared__ uint32_t most_of[4];
+  __shared__ uint32_t most_of[16];
   const int tid = THREADS == 64 ? threadIdx.x & 63 : threadIdx.x, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int step = THREADS == 64 ? gridDim.x * 4 : gridDim.x;
   const int vectors = (int)(row_bytes / VEC);
@@ -106,7 +107,8 @@ __global__ __launch_bounds__(256) void i8_quantise_kernel(const void* __restrict
       __syncthreads();
       if (lane == 0) most_of[wave] = most;
       __syncthreads();
-      most = max(max(most_of[0], most_of[1]), max(most_of[2], most_of[3]));
+#pragma unroll
+      for (int w = 0; w < THREADS / 64; ++w) most = max(most, most_of[w]);
     }
     const float s = scale_for(__builtin_bit_cast(float, most)), inverse = 1.f / s;
     const bool finite = s < INFINITY;
@@ -138,6 +140,8 @@ int launch_quantise(const void* x, int8_t* codes, float* scales, int rows, int k
   const int64_t vectors = row / Elem<DTYPE>::VEC;
   if (vectors <= 64 * 4)
     hipLaunchKernelGGL((i8_quantise_kernel<DTYPE, 64, 4>), dim3((uint32_t)(((int64_t)rows + 3) / 4)), dim3(256), 0, stream, x, codes, scales, rows, k, row);
+  else if (vectors > 256 * 4 && rows <= 2 * kUnits)  // (48 x 9216 fp32: 256 threads 7.6 us, 1024 @Q)
+    hipLaunchKernelGGL((i8_quantise_kernel<DTYPE, 1024, 4>), dim3(rows), dim3(1024), 0, stream, x, codes, scales, rows, k, row);
   else
     hipLaunchKernelGGL((i8_quantise_kernel<DTYPE, 256, 4>), dim3(std::min(rows, 1 << 22)), dim3(256), 0, stream, x, codes, scales, rows, k, row);
   return (int)hipGetLastError();
@@ -168,11 +172,28 @@ __device__ __forceinline__ float finish(int sum, float s, float t, float bias, i
   return relu ? (z > 0.f ? z : 0.f) : z;
 }
 
+// What the waves of a workgroup have found for 16 MT rows and 16 outputs, [waves][MT * 256] in `parts`, into the results.
+template <class E, int MT>
+__device__ __forceinline__ void join_waves(const FwdArgs& a, const int* parts, int waves, int m0, int o0, const float* scale) {
+  for (int i = threadIdx.x; i < MT * 256; i += blockDim.x) {
+    // (consecutive threads: consecutive outputs of a row)
+    const int t = i >> 8, n = m0 + 16 * t + (i >> 4 & 15), out = o0 + (i & 15);
+    if (n >= a.m || out >= a.o) continue;
+    const int at = t * 256 + (i & 3) * 64 + ((i & 15) >> 2) * 16 + (i >> 4 & 15);
+    int sum = 0;
+#pragma unroll 4
+    for (int p = 0; p < waves; ++p) sum += parts[p * MT * 256 + at];
+    const float bias = a.bias ? E::to_float(static_cast<const typename E::T*>(a.bias)[out]) : 0.f;
+    static_cast<typename E::T*>(a.y)[(int64_t)n * a.o + out] = E::from_float(finish(sum, scale[n], a.w_scale[out], bias, a.relu));
+  }
+}
+
 // 16 MT rows by 16 outputs in a workgroup, whose waves take the inputs in turn, 128 at a time, and add up through shared memory: nothing is used by two
-// waves, and operands come from memory as the instructions take them, 16 inputs of a row or an output a lane.
+// waves, and operands come from memory as the instructions take them, 16 inputs of a row or an output a lane, those of AHEAD turns at a time.
 template <int DTYPE, int MT>
 __global__ __launch_bounds__(1024) void i8_rows_kernel(FwdArgs a) {
   typedef Elem<DTYPE> E;
+  constexpr int AHEAD = MT == 1 ? 4 : 2;
   extern __shared__ int parts[];  // [waves][MT * 256]
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), waves = blockDim.x >> 6;
   const int o0 = blockIdx.x * 16, blocks = (int)(a.row / kRowUnit);
@@ -182,36 +203,127 @@ __global__ __launch_bounds__(1024) void i8_rows_kernel(FwdArgs a) {
 #pragma unroll
     for (int t = 0; t < MT; ++t) x[t] = a.codes + (int64_t)min(m0 + 16 * t + (lane & 15), a.m - 1) * a.row + 16 * (lane >> 4);
     i32x4 acc[MT] = {};
-    for (int b = wave; b < blocks; b += waves) {
-      i32x4 wv[2], xv[MT][2];
+    auto turn = [&](int b0, auto count) {
+      constexpr int N = decltype(count)::value;
+      i32x4 wv[N][2], xv[N][MT][2];
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        wv[h] = *reinterpret_cast<const i32x4*>(w + b * kRowUnit + 64 * h);
+      for (int i = 0; i < N; ++i)
 #pragma unroll
-        for (int t = 0; t < MT; ++t) xv[t][h] = *reinterpret_cast<const i32x4*>(x[t] + b * kRowUnit + 64 * h);
-      }
+        for (int h = 0; h < 2; ++h) {
+          const int at = (b0 + i * waves) * kRowUnit + 64 * h;
+          wv[i][h] = *reinterpret_cast<const i32x4*>(w + at);
 #pragma unroll
-      for (int h = 0; h < 2; ++h)
+          for (int t = 0; t < MT; ++t) xv[i][t][h] = *reinterpret_cast<const i32x4*>(x[t] + at);
+        }
 #pragma unroll
-        for (int t = 0; t < MT; ++t) acc[t] = __builtin_amdgcn_mfma_i32_16x16x64_i8(wv[h], xv[t][h], acc[t], 0, 0, 0);
+      for (int i = 0; i < N; ++i)
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+          for (int t = 0; t < MT; ++t) acc[t] = __builtin_amdgcn_mfma_i32_16x16x64_i8(wv[i][h], xv[i][t][h], acc[t], 0, 0, 0);
+    };
+    int b = wave;
+    for (; b + (AHEAD - 1) * waves < blocks; b += AHEAD * waves) turn(b, std::integral_constant<int, AHEAD>());
+    if (AHEAD == 4 && b + waves < blocks) {
+      turn(b, std::integral_constant<int, 2>());
+      b += 2 * waves;
     }
+    if (b < blocks) turn(b, std::integral_constant<int, 1>());
     __syncthreads();
 #pragma unroll
     for (int t = 0; t < MT; ++t)
 #pragma unroll
       for (int r = 0; r < 4; ++r) parts[(wave * MT + t) * 256 + r * 64 + lane] = acc[t][r];  // output 4 (lane / 16) + r, row lane % 16
     __syncthreads();
-    for (int i = threadIdx.x; i < MT * 256; i += blockDim.x) {
-      // (consecutive threads: consecutive outputs of a row)
-      const int t = i >> 8, n = m0 + 16 * t + (i >> 4 & 15), out = o0 + (i & 15);
-      if (n >= a.m || out >= a.o) continue;
-      const int at = t * 256 + (i & 3) * 64 + ((i & 15) >> 2) * 16 + (i >> 4 & 15);
-      int sum = 0;
-      for (int p = 0; p < waves; ++p) sum += parts[p * MT * 256 + at];
-      const float bias = a.bias ? E::to_float(static_cast<const typename E::T*>(a.bias)[out]) : 0.f;
-      static_cast<typename E::T*>(a.y)[(int64_t)n * a.o + out] = E::from_float(finish(sum, a.scale[n], a.w_scale[out], bias, a.relu));
+    join_waves<E, MT>(a, parts, waves, m0, o0, a.scale);
+  }
+}
+
+// Few rows that are not yet in 8 bits: every workgroup makes them so for itself, while its weights are on their way, and the first one leaves them for the
+// caller.  Rows of codes in shared memory; a wave keeps up to kTokenAhead turns of weights in registers.
+constexpr int kTokenRows = 4, kTokenBytes = 32768, kTokenAhead = 4;
+
+template <int DTYPE>
+__global__ __launch_bounds__(1024) void i8_token_kernel(FwdArgs a, const void* __restrict__ x, int8_t* __restrict__ codes, float* __restrict__ scales, int k) {
+  typedef Elem<DTYPE> E;
+  typedef typename E::T T;
+  constexpr int VEC = E::VEC;
+  extern __shared__ __attribute__((aligned(16))) int8_t rows[];  // [m][row], then [waves][256] of sums
+  __shared__ uint32_t most_of[kTokenRows][16];
+  __shared__ float scale[kTokenRows];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), waves = blockDim.x >> 6;
+  const int o0 = blockIdx.x * 16, blocks = (int)(a.row / kRowUnit), row = (int)a.row, vectors = row / VEC;
+  const int8_t* const w = a.w_codes + (int64_t)min(o0 + (lane & 15), a.o - 1) * a.row + 16 * (lane >> 4);
+  i32x4 wv[kTokenAhead][2] = {};
+#pragma unroll
+  for (int i = 0; i < kTokenAhead; ++i)
+    if (wave + i * waves < blocks) {
+#pragma unroll
+      for (int h = 0; h < 2; ++h) wv[i][h] = *reinterpret_cast<const i32x4*>(w + (wave + i * waves) * kRowUnit + 64 * h);
+    }
+  auto load = [&](int n, int v) {
+    const T* const from = static_cast<const T*>(x) + (int64_t)n * k;
+    const int at = v * VEC;
+    if (at + VEC <= k) return load_vec<E>(from + at);
+    float f[VEC];
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) f[i] = at + i < k ? E::to_float(from[at + i]) : 0.f;
+    return E::pack(f);
+  };
+  for (int n = 0; n < a.m; ++n) {
+    uint32_t most = 0;
+    for (int v = tid; v < vectors; v += blockDim.x) {
+      const u32x4 vec = load(n, v);
+#pragma unroll
+      for (int i = 0; i < VEC; ++i) most = max(most, __builtin_bit_cast(uint32_t, E::get(vec, i)) & 0x7fffffffu);
+    }
+    most = (uint32_t)wave_reduce((int)most, 0, [](int p, int q) { return max(p, q); });
+    if (lane == 0) most_of[n][wave] = most;
+  }
+  __syncthreads();
+  for (int n = 0; n < a.m; ++n) {
+    uint32_t most = 0;
+    for (int p = 0; p < waves; ++p) most = max(most, most_of[n][p]);
+    const float s = scale_for(__builtin_bit_cast(float, most)), inverse = 1.f / s;
+    const bool finite = s < INFINITY;
+    if (tid == 0) {
+      scale[n] = s;
+      if (blockIdx.x == 0) scales[n] = s;
+    }
+    for (int v = tid; v < vectors; v += blockDim.x) {
+      const u32x4 vec = load(n, v);
+#pragma unroll
+      for (int i = 0; i < VEC / 4; ++i) {
+        uint32_t word = 0;
+#pragma unroll
+        for (int b = 0; b < 4; ++b) word |= ((uint32_t)code_of(E::get(vec, 4 * i + b), s, inverse) & 255u) << (8 * b);
+        if (!finite) word = 0;
+        reinterpret_cast<uint32_t*>(rows + n * row)[v * (VEC / 4) + i] = word;
+        if (blockIdx.x == 0) reinterpret_cast<uint32_t*>(codes + (int64_t)n * row)[v * (VEC / 4) + i] = word;
+      }
     }
   }
+  __syncthreads();
+  const int8_t* const mine = rows + min(lane & 15, a.m - 1) * row + 16 * (lane >> 4);
+  i32x4 acc = {0, 0, 0, 0};
+  auto multiply = [&](int b, const i32x4(&v)[2]) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(v[h], *reinterpret_cast<const i32x4*>(mine + b * kRowUnit + 64 * h), acc, 0, 0, 0);
+  };
+#pragma unroll
+  for (int i = 0; i < kTokenAhead; ++i)
+    if (wave + i * waves < blocks) multiply(wave + i * waves, wv[i]);
+  for (int b = wave + kTokenAhead * waves; b < blocks; b += waves) {
+    i32x4 v[2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) v[h] = *reinterpret_cast<const i32x4*>(w + b * kRowUnit + 64 * h);
+    multiply(b, v);
+  }
+  int* const parts = reinterpret_cast<int*>(rows + a.m * row);
+#pragma unroll
+  for (int r = 0; r < 4; ++r) parts[wave * 256 + r * 64 + lane] = acc[r];
+  __syncthreads();
+  join_waves<E, 1>(a, parts, waves, 0, o0, scale);
 }
 
 typedef const __attribute__((address_space(1))) uint32_t* GlobalPtr;
@@ -317,8 +429,16 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void i8_tile_kernel(FwdArgs a) {
 }
 
 template <int DTYPE>
-int launch_forward(const i8_desc* d, const FwdArgs& a, hipStream_t stream) {
+int launch_forward(const i8_desc* d, const FwdArgs& a, const void* x, int8_t* codes, float* scales, hipStream_t stream) {
   const int m = d->p.m, o = d->p.num_output;
+  if (x && d->token) {
+    hipLaunchKernelGGL(i8_token_kernel<DTYPE>, dim3((o + 15) / 16), dim3(64 * d->waves), (size_t)(m * d->row + d->waves * 1024), stream, a, x, codes, scales, d->p.k);
+    return (int)hipGetLastError();
+  }
+  if (x) {
+    const int e = launch_quantise<DTYPE>(x, codes, scales, m, d->p.k, d->row, stream);
+    if (e) return e;
+  }
   if (d->fwd == kTile256) {
     hipLaunchKernelGGL((i8_tile_kernel<DTYPE, 4, 2, 8>), dim3((m + 255) / 256 * ((o + 255) / 256)), dim3(512), 0, stream, a);
   } else if (d->fwd == kTile128) {
@@ -374,8 +494,11 @@ __device__ __forceinline__ void pair_terms(float a, float b, uint32_t (&w)[TERMS
 // the codes: a lane takes 8 terms of four neighbouring rows or columns, so that turning them costs nothing beside the conversion.  The next step's values
 // are asked for before the instructions on this one's first term and converted after them: a compute unit's matrix and vector units are then
 // both busy, with waves that are at different places.
+// Every load is in range and none waits for a branch: the last terms of a sum that are fewer than 8 come as the last 8, with zeros for those that the
+// groups before hold, and the last outputs that are fewer than four as the last four, each to its own place.  SLOW: sums or rows too short
+// for that, one by one.
 // Waves of 64 rows by 16 NT inputs.
-template <int DTYPE, bool FILTER, int TILE>
+template <int DTYPE, bool FILTER, int TILE, bool SLOW>
 __global__ __launch_bounds__(TILE == 256 ? 512 : 256, 2) void i8_gradient_kernel(BwdArgs a) {
   typedef Elem<DTYPE> E;
   typedef typename E::T T;
@@ -394,109 +517,123 @@ __global__ __launch_bounds__(TILE == 256 ? 512 : 256, 2) void i8_gradient_kernel
 
   const bool of_dz = wave < HALF / 64;
   const int half = of_dz ? tid : tid - HALF, g = half / (TILE / 4), p = half % (TILE / 4);  // group, four rows or columns 4 p ..
-  const int at4 = (p >> 4) * 72 + (p & 15);  // the place of the first of them: of 64 neighbours, 4 l + q stands at 16 q + l (and the pieces left out)
+  // the place of a row or column: of 64 neighbours, 4 l + q stands at 16 q + l (and the pieces left out)
+  auto place_of = [](int i) { return (i >> 6) * 72 + (i & 3) * 18 + (i >> 2 & 15); };
   const int col = (int)min((int64_t)i0 + 4 * p, a.row - 4);
-  const bool inside = r0 + TILE <= rows;
+  const int out = SLOW ? r0 + 4 * p : min(r0 + 4 * p, rows - 4);  // filter
+  int places[4];
+#pragma unroll
+  for (int q = 0; q < 4; ++q) places[q] = !FILTER || !of_dz ? place_of(4 * p + q) : out + q >= r0 ? place_of(out + q - r0) : GROUP - 1;  // (another tile's: nobody reads it)
+  // the first term of a group's 8 in a step, and how many of them are not the group's
+  auto first_of = [&](int step, int group, int& skip) {
+    const int d0 = (first + step) * kStep + 8 * group, from = max(0, min(d0, depth - 8));
+    skip = d0 - from;
+    return from;
+  };
   constexpr int DATA_ROWS = TILE * 4 / HALF;  // data: 8 terms of rows half / 4 and on, HALF / 4 apart
   constexpr int WORDS = DTYPE == MI355_F32 ? 4 : 2;
   typedef typename std::conditional<DTYPE == MI355_F32, u32x4, u32x2>::type Four;
   struct __attribute__((packed, aligned(sizeof(T)))) FourMem {
     Four v;
   };
-  float s[8];
   float bias[4] = {0.f, 0.f, 0.f, 0.f};
   f32x4 acc[4][NT] = {};
 
-  struct Filter {  // what is on its way
+  struct Filter {
     Four z[8];
   };
   struct Data {
     u32x4 z[DATA_ROWS][DTYPE == MI355_F32 ? 2 : 1];
   };
-  typename std::conditional<FILTER, Filter, Data>::type raw;
-  uint32_t c[8];
+  struct Way {  // what is on its way
+    typename std::conditional<FILTER, Filter, Data>::type raw;
+    float s[8];
+    uint32_t c[8];
+    int skip;
+  };
 
-  auto load_codes = [&](int step) {
-    const int d0 = (first + step) * kStep + 8 * g;
-    const int8_t* const at = a.codes + col;
+  auto load_codes = [&](Way& way, int step) {
+    const int from = first_of(step, g, way.skip);
+    const int8_t* const at = a.codes + (int64_t)from * a.row + col;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) c[j] = *reinterpret_cast<const uint32_t*>(at + (int64_t)min(d0 + j, depth - 1) * a.row);
+    for (int j = 0; j < 8; ++j) way.c[j] = *reinterpret_cast<const uint32_t*>(at + (int64_t)(SLOW ? min(j, depth - 1 - from) : j) * a.row);
   };
-  auto load_scales = [&](int d0) {
-    if (d0 + 8 <= depth) {
-      const u32x4 s0 = load_vec<Elem<MI355_F32>>(a.scale + d0), s1 = load_vec<Elem<MI355_F32>>(a.scale + d0 + 4);
+  auto load_dz = [&](Way& way, int step) {
+    const int from = first_of(step, FILTER ? g : half & 3, way.skip);
 #pragma unroll
-      for (int j = 0; j < 8; ++j) s[j] = Elem<MI355_F32>::get(j < 4 ? s0 : s1, j & 3);
-    } else {
-#pragma unroll
-      for (int j = 0; j < 8; ++j) s[j] = d0 + j < depth ? a.scale[d0 + j] : 0.f;
-    }
-  };
-  auto load_dz = [&](int step) {
+    for (int j = 0; j < 8; ++j) way.s[j] = a.scale[SLOW ? min(from + j, depth - 1) : from + j];
     if constexpr (FILTER) {
-      const int d0 = (first + step) * kStep + 8 * g;
-      load_scales(d0);
-      const T* const z = static_cast<const T*>(a.dz);
-      if (inside) {
+      const T* const z = static_cast<const T*>(a.dz) + (int64_t)from * a.o + (SLOW ? 0 : out);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) raw.z[j] = reinterpret_cast<const FourMem*>(z + (int64_t)min(d0 + j, depth - 1) * a.o + r0 + 4 * p)->v;
-      } else {
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          const T* const row = z + (int64_t)min(d0 + j, depth - 1) * a.o;
+      for (int j = 0; j < 8; ++j) {
+        if constexpr (SLOW) {
+          const T* const row = z + (int64_t)min(j, depth - 1 - from) * a.o;
           float f[E::VEC];
 #pragma unroll
-          for (int q = 0; q < E::VEC; ++q) f[q] = q < 4 ? E::to_float(row[min(r0 + 4 * p + q, a.o - 1)]) : 0.f;
+          for (int q = 0; q < E::VEC; ++q) f[q] = q < 4 ? E::to_float(row[min(out + q, a.o - 1)]) : 0.f;
           const u32x4 v = E::pack(f);
 #pragma unroll
-          for (int w = 0; w < WORDS; ++w) raw.z[j][w] = v[w];
+          for (int w = 0; w < WORDS; ++w) way.raw.z[j][w] = v[w];
+        } else {
+          way.raw.z[j] = reinterpret_cast<const FourMem*>(z + (int64_t)j * a.o)->v;
         }
       }
-      if (d0 + 8 > depth) {
-#pragma unroll
-        for (int j = 0; j < 8; ++j)
-          if (d0 + j >= depth) raw.z[j] = Four{};
-      }
     } else {
-      const int d0 = (first + step) * kStep + 8 * (half & 3);
-      load_scales(d0);
 #pragma unroll
       for (int i = 0; i < DATA_ROWS; ++i) {
-        const T* const z = static_cast<const T*>(a.dz) + (int64_t)min(r0 + half / 4 + i * (HALF / 4), rows - 1) * a.o;
-        if (d0 + 8 <= depth) {
-          raw.z[i][0] = load_vec<E>(z + d0);
-          if constexpr (DTYPE == MI355_F32) raw.z[i][1] = load_vec<E>(z + d0 + 4);
-        } else {
+        const T* const z = static_cast<const T*>(a.dz) + (int64_t)min(r0 + half / 4 + i * (HALF / 4), rows - 1) * a.o + from;
+        if constexpr (SLOW) {
           float f[8];
 #pragma unroll
-          for (int j = 0; j < 8; ++j) f[j] = d0 + j < depth ? E::to_float(z[d0 + j]) : 0.f;
+          for (int j = 0; j < 8; ++j) f[j] = E::to_float(z[min(j, depth - 1 - from)]);
           if constexpr (DTYPE == MI355_F32) {
-            raw.z[i][0] = E::pack({f[0], f[1], f[2], f[3]});
-            raw.z[i][1] = E::pack({f[4], f[5], f[6], f[7]});
+            way.raw.z[i][0] = E::pack({f[0], f[1], f[2], f[3]});
+            way.raw.z[i][1] = E::pack({f[4], f[5], f[6], f[7]});
           } else {
-            raw.z[i][0] = E::pack(f);
+            way.raw.z[i][0] = E::pack(f);
           }
+        } else {
+          way.raw.z[i][0] = load_vec<E>(z);
+          if constexpr (DTYPE == MI355_F32) way.raw.z[i][1] = load_vec<E>(z + 4);
         }
       }
     }
   };
-  auto put_codes = [&](u32x4* buffer) {
-    u32x4* const to = buffer + TERMS * TERM + g * GROUP + at4;
+  auto put_codes = [&](const Way& way, u32x4* buffer) {
+    u32x4* const to = buffer + TERMS * TERM + g * GROUP;
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
       u32x4 w;
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         uint32_t two[1];
-        pair_terms<1>((float)(int8_t)(c[2 * j] >> 8 * q), (float)(int8_t)(c[2 * j + 1] >> 8 * q), two);
+        pair_terms<1>((float)(int8_t)(way.c[2 * j] >> 8 * q), (float)(int8_t)(way.c[2 * j + 1] >> 8 * q), two);
         w[j] = two[0];
       }
-      to[18 * q] = w;
+      to[places[q]] = w;
     }
   };
-  auto put_dz = [&](u32x4* buffer) {
+  // The 8 terms' dz, zeros for those that are not the group's, whatever they hold.
+  auto keep_own = [&](const Way& way, float (&v)[8]) {
+    if (way.skip > 0 || SLOW) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[j] = j >= way.skip && j < depth ? v[j] : 0.f;
+    }
+  };
+  auto terms_of = [&](const Way& way, float (&v)[8], u32x4 (&w)[TERMS]) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] *= way.s[j];
+    keep_own(way, v);  // (their scales may be NaN)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      uint32_t two[TERMS];
+      pair_terms<TERMS>(v[2 * j], v[2 * j + 1], two);
+#pragma unroll
+      for (int t = 0; t < TERMS; ++t) w[t][j] = two[t];
+    }
+  };
+  auto put_dz = [&](const Way& way, u32x4* buffer) {
     if constexpr (FILTER) {
-      u32x4* const to = buffer + g * GROUP + at4;
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
         float v[8];
@@ -504,36 +641,27 @@ __global__ __launch_bounds__(TILE == 256 ? 512 : 256, 2) void i8_gradient_kernel
         for (int j = 0; j < 8; ++j) {
           u32x4 z = {};
 #pragma unroll
-          for (int w = 0; w < WORDS; ++w) z[w] = raw.z[j][w];
+          for (int i = 0; i < WORDS; ++i) z[i] = way.raw.z[j][i];
           v[j] = E::get(z, q);
         }
         if (sum_bias) {
+          keep_own(way, v);
 #pragma unroll
           for (int j = 0; j < 8; ++j) bias[q] += v[j];
         }
         u32x4 w[TERMS];
+        terms_of(way, v, w);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          uint32_t two[TERMS];
-          pair_terms<TERMS>(v[2 * j] * s[2 * j], v[2 * j + 1] * s[2 * j + 1], two);
-#pragma unroll
-          for (int t = 0; t < TERMS; ++t) w[t][j] = two[t];
-        }
-#pragma unroll
-        for (int t = 0; t < TERMS; ++t) to[t * TERM + 18 * q] = w[t];
+        for (int t = 0; t < TERMS; ++t) buffer[t * TERM + g * GROUP + places[q]] = w[t];
       }
     } else {
 #pragma unroll
       for (int i = 0; i < DATA_ROWS; ++i) {
+        float v[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = E::get(way.raw.z[i][j / E::VEC], j % E::VEC);
         u32x4 w[TERMS];
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          uint32_t two[TERMS];
-          constexpr int PER = E::VEC;
-          pair_terms<TERMS>(E::get(raw.z[i][2 * j / PER], 2 * j % PER) * s[2 * j], E::get(raw.z[i][2 * j / PER], 2 * j % PER + 1) * s[2 * j + 1], two);
-#pragma unroll
-          for (int t = 0; t < TERMS; ++t) w[t][j] = two[t];
-        }
+        terms_of(way, v, w);
         const int row = half / 4 + i * (HALF / 4);
 #pragma unroll
         for (int t = 0; t < TERMS; ++t) buffer[t * TERM + (half & 3) * GROUP + row + 2 * (row >> 4)] = w[t];
@@ -542,35 +670,64 @@ __global__ __launch_bounds__(TILE == 256 ? 512 : 256, 2) void i8_gradient_kernel
   };
 
   // Both kinds of waves take the same steps, and meet at the same barriers.
-  auto work = [&](auto&& load, auto&& put) {
-    load(0);
-    put(lds[0]);
-    __syncthreads();
-    for (int step = 0; step < steps; ++step) {
-      const bool more = step + 1 < steps;
-      if (more) load(step + 1);
-      __builtin_amdgcn_sched_barrier(0);
-      const u32x4* const A = lds[step & 1] + (lane >> 4) * GROUP + wm * 72 + (lane & 15);
-      const u32x4* const B = lds[step & 1] + TERMS * TERM + (lane >> 4) * GROUP + wn * NT * 18 + (lane & 15);
-      bf16x8 w[NT];
+  auto products = [&](int step, auto&& between) {
+    const u32x4* const A = lds[step & 1] + (lane >> 4) * GROUP + wm * 72 + (lane & 15);
+    const u32x4* const B = lds[step & 1] + TERMS * TERM + (lane >> 4) * GROUP + wn * NT * 18 + (lane & 15);
+    bf16x8 w[NT];
 #pragma unroll
-      for (int u = 0; u < NT; ++u) w[u] = __builtin_bit_cast(bf16x8, B[u * 18]);
+    for (int u = 0; u < NT; ++u) w[u] = __builtin_bit_cast(bf16x8, B[u * 18]);
 #pragma unroll
-      for (int t = 0; t < TERMS; ++t) {
-        bf16x8 x[4];
+    for (int t = 0; t < TERMS; ++t) {
+      bf16x8 x[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) x[i] = __builtin_bit_cast(bf16x8, A[t * TERM + 18 * i]);
+      for (int i = 0; i < 4; ++i) x[i] = __builtin_bit_cast(bf16x8, A[t * TERM + 18 * i]);
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
+      for (int i = 0; i < 4; ++i)
 #pragma unroll
-          for (int u = 0; u < NT; ++u) acc[i][u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x[i], w[u], acc[i][u], 0, 0, 0);
-        if (t + 2 == TERMS) {
-          __builtin_amdgcn_sched_barrier(0);
-          if (more) put(lds[(step + 1) & 1]);
-          __builtin_amdgcn_sched_barrier(0);
-        }
+        for (int u = 0; u < NT; ++u) acc[i][u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x[i], w[u], acc[i][u], 0, 0, 0);
+      if (t + 2 == TERMS) {
+        __builtin_amdgcn_sched_barrier(0);
+        between();
+        __builtin_amdgcn_sched_barrier(0);
       }
+    }
+    __syncthreads();
+  };
+  auto work = [&](auto&& load, auto&& put) {
+    if constexpr (TILE == 256) {
+      Way way;
+      load(way, 0);
+      put(way, lds[0]);
       __syncthreads();
+      for (int step = 0; step < steps; ++step) {
+        const bool more = step + 1 < steps;
+        if (more) load(way, step + 1);
+        __builtin_amdgcn_sched_barrier(0);
+        products(step, [&]() {
+          if (more) put(way, lds[(step + 1) & 1]);
+        });
+      }
+    } else {
+      // The small tile's registers hold two steps: few workgroups and short sums leave a step's loads no time otherwise.  (Loads beyond the last
+      // step are the last one's again.)
+      Way one, two;
+      load(one, 0);
+      put(one, lds[0]);
+      load(one, min(1, steps - 1));
+      __syncthreads();
+      for (int step = 0; step < steps; step += 2) {
+        load(two, min(step + 2, steps - 1));
+        __builtin_amdgcn_sched_barrier(0);
+        products(step, [&]() {
+          if (step + 1 < steps) put(one, lds[1]);
+        });
+        if (step + 1 == steps) break;
+        load(one, min(step + 3, steps - 1));
+        __builtin_amdgcn_sched_barrier(0);
+        products(step + 1, [&]() {
+          if (step + 2 < steps) put(two, lds[0]);
+        });
+      }
     }
   };
   if (steps > 0) {
@@ -585,7 +742,8 @@ __global__ __launch_bounds__(TILE == 256 ? 512 : 256, 2) void i8_gradient_kernel
     float* const sums = reinterpret_cast<float*>(lds);
     if (of_dz) {
 #pragma unroll
-      for (int q = 0; q < 4; ++q) sums[g * TILE + 4 * p + q] = bias[q];
+      for (int q = 0; q < 4; ++q)
+        if (out + q >= r0 && out + q < r0 + TILE) sums[g * TILE + out + q - r0] = bias[q];
     }
     __syncthreads();
     if (tid < TILE && r0 + tid < a.o) {
@@ -639,59 +797,66 @@ __global__ __launch_bounds__(TILE == 256 ? 512 : 256, 2) void i8_gradient_kernel
 
 // The splits' sums in one, four elements a thread; beta as the kernels take it.
 template <class E>
-__global__ __launch_bounds__(256) void i8_join_kernel(const float* __restrict__ parts, typename E::T* __restrict__ out, int64_t count, int splits, float beta) {
+__device__ __forceinline__ void join_four(const float* parts, typename E::T* out, int64_t count, int splits, float beta, int64_t i) {
   typedef Elem<MI355_F32> F;
-  for (int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4; i < count; i += (int64_t)gridDim.x * 1024) {
-    float v[4];
-    if (i + 4 <= count) {
-      u32x4 w = load_vec<F>(parts + i);
+  float v[4];
+  if (i + 4 <= count) {
+    u32x4 w = load_vec<F>(parts + i);
 #pragma unroll
-      for (int q = 0; q < 4; ++q) v[q] = F::get(w, q);
+    for (int q = 0; q < 4; ++q) v[q] = F::get(w, q);
 #pragma unroll 4
-      for (int s = 1; s < splits; ++s) {
-        w = load_vec<F>(parts + s * count + i);
+    for (int s = 1; s < splits; ++s) {
+      w = load_vec<F>(parts + s * count + i);
 #pragma unroll
-        for (int q = 0; q < 4; ++q) v[q] += F::get(w, q);
-      }
-      if (beta != 0.f) {
+      for (int q = 0; q < 4; ++q) v[q] += F::get(w, q);
+    }
+    if (beta != 0.f) {
 #pragma unroll
-        for (int q = 0; q < 4; ++q) v[q] += E::to_float(out[i + q]);
-      }
-      store_four<E>(out + i, v);
-    } else {
-      for (int64_t j = i; j < count; ++j) {
-        float sum = parts[j];
-        for (int s = 1; s < splits; ++s) sum += parts[s * count + j];
-        out[j] = E::from_float(beta != 0.f ? E::to_float(out[j]) + sum : sum);
-      }
+      for (int q = 0; q < 4; ++q) v[q] += E::to_float(out[i + q]);
+    }
+    store_four<E>(out + i, v);
+  } else {
+    for (int64_t j = i; j < count; ++j) {
+      float sum = parts[j];
+      for (int s = 1; s < splits; ++s) sum += parts[s * count + j];
+      out[j] = E::from_float(beta != 0.f ? E::to_float(out[j]) + sum : sum);
     }
   }
 }
 
+// Of the result, and by the last workgroups of the bias gradient (bias_count 0: none).
 template <class E>
-int launch_join(const float* parts, void* out, int64_t count, int splits, float beta, hipStream_t stream) {
-  hipLaunchKernelGGL(i8_join_kernel<E>, dim3((uint32_t)std::min<int64_t>((count + 1023) / 1024, 1 << 20)), dim3(256), 0, stream, parts,
-                     static_cast<typename E::T*>(out), count, splits, beta);
-  return (int)hipGetLastError();
+__global__ __launch_bounds__(256) void i8_join_kernel(const float* __restrict__ parts, typename E::T* __restrict__ out, int64_t count, const float* __restrict__ bias_parts,
+                                                      float* __restrict__ bias_out, int64_t bias_count, int splits, float beta, int blocks) {
+  if ((int)blockIdx.x >= blocks) {
+    const int64_t i = ((int64_t)(blockIdx.x - blocks) * 256 + threadIdx.x) * 4;
+    if (i < bias_count) join_four<Elem<MI355_F32>>(bias_parts, bias_out, bias_count, splits, beta, i);
+    return;
+  }
+  for (int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4; i < count; i += (int64_t)blocks * 1024) join_four<E>(parts, out, count, splits, beta, i);
 }
+
+// Whether a gradient's sums or rows are too short for loads of 8 terms of four outputs.
+bool slow(int64_t rows, int64_t depth, bool filter) { return depth < 8 || (filter && rows < 4); }
 
 template <int DTYPE, bool FILTER>
 int launch_gradient(const BwdArgs& a, int tile, int splits, hipStream_t stream) {
   const int rows = FILTER ? a.o : a.n;
   const dim3 grid((uint32_t)(((int64_t)rows + tile - 1) / tile * (((int64_t)a.k + tile - 1) / tile)), splits);
-  if (tile == 256)
-    hipLaunchKernelGGL((i8_gradient_kernel<DTYPE, FILTER, 256>), grid, dim3(512), 0, stream, a);
+  if (slow(rows, FILTER ? a.n : a.o, FILTER))
+    hipLaunchKernelGGL((i8_gradient_kernel<DTYPE, FILTER, 128, true>), grid, dim3(256), 0, stream, a);
+  else if (tile == 256)
+    hipLaunchKernelGGL((i8_gradient_kernel<DTYPE, FILTER, 256, false>), grid, dim3(512), 0, stream, a);
   else
-    hipLaunchKernelGGL((i8_gradient_kernel<DTYPE, FILTER, 128>), grid, dim3(256), 0, stream, a);
-  int e = (int)hipGetLastError();
+    hipLaunchKernelGGL((i8_gradient_kernel<DTYPE, FILTER, 128, false>), grid, dim3(256), 0, stream, a);
+  const int e = (int)hipGetLastError();
   if (e || splits == 1) return e;
-  const int64_t count = (int64_t)rows * a.k;
-  if constexpr (FILTER) {
-    e = launch_join<Elem<MI355_F32>>(a.parts, a.out, count, splits, a.beta, stream);
-    return e || !a.db ? e : launch_join<Elem<MI355_F32>>(a.db_parts, a.db, a.o, splits, a.beta, stream);
-  } else {
-    return launch_join<Elem<DTYPE>>(a.parts, a.out, count, splits, 0.f, stream);
-  }
+  typedef typename std::conditional<FILTER, Elem<MI355_F32>, Elem<DTYPE>>::type Out;
+  const int64_t count = (int64_t)rows * a.k, bias_count = FILTER && a.db ? a.o : 0;
+  const int blocks = (int)std::min<int64_t>((count + 1023) / 1024, 1 << 20), bias_blocks = (int)((bias_count + 1023) / 1024);
+  hipLaunchKernelGGL(i8_join_kernel<Out>, dim3(blocks + bias_blocks), dim3(256), 0, stream, a.parts, static_cast<typename Out::T*>(a.out), count, a.db_parts, a.db,
+                     bias_count, splits, a.beta, blocks);
+  return (int)hipGetLastError();
 }
 
 template <bool FILTER>
@@ -716,9 +881,9 @@ int clear(float* to, int64_t count, hipStream_t stream) {
 int64_t tiles_of(int64_t rows, int64_t columns, int tile) { return (rows + tile - 1) / tile * ((columns + tile - 1) / tile); }
 
 // The tile of a gradient, and the workgroups that share a sum.
-void plan_gradient(int64_t rows, int64_t k, int64_t depth, int32_t& tile, int32_t& splits, int32_t& per) {
+void plan_gradient(int64_t rows, int64_t k, int64_t depth, bool filter, int32_t& tile, int32_t& splits, int32_t& per) {
   const int64_t steps = std::max<int64_t>(1, (depth + kStep - 1) / kStep);
-  tile = tiles_of(rows, k, 256) >= kUnits / 2 ? 256 : 128;
+  tile = tiles_of(rows, k, 256) >= kUnits / 2 && !slow(rows, depth, filter) ? 256 : 128;
   const int64_t tiles = std::max<int64_t>(1, tiles_of(rows, k, tile)), places = tile == 256 ? 1 : 2 * kUnits;
   splits = (int32_t)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(places / tiles, steps / 8), 64));
   per = (int32_t)((steps + splits - 1) / splits);
@@ -755,19 +920,20 @@ int i8_desc_create(i8_desc_t** out, const i8_params_t* pp) {
   d->row = (K + kRowUnit - 1) / kRowUnit * kRowUnit;
   d->fwd = M <= 64 || tiles_of(M, O, 128) < kUnits / 4 ? kRows : tiles_of(M, O, 256) >= kUnits / 2 ? kTile256 : kTile128;
   d->waves = (int32_t)std::max<int64_t>(1, std::min<int64_t>(tiles_of(M, O, 16) > 4 * kUnits ? 4 : 16, d->row / kRowUnit));
-  plan_gradient(O, K, M, d->filter_tile, d->filter_splits, d->filter_per);
-  plan_gradient(M, K, O, d->data_tile, d->data_splits, d->data_per);
+  d->token = d->fwd == kRows && M <= kTokenRows && M * d->row <= kTokenBytes;
+  plan_gradient(O, K, M, true, d->filter_tile, d->filter_splits, d->filter_per);
+  plan_gradient(M, K, O, false, d->data_tile, d->data_splits, d->data_per);
   if (M > 0) {
     if (d->filter_splits > 1) d->ws_bytes = (size_t)d->filter_splits * (O * K + O) * 4;
     if (d->data_splits > 1) d->ws_bytes = std::max(d->ws_bytes, (size_t)d->data_splits * M * K * 4);
   }
-  char fwd[32];
+  char fwd[48];
   if (d->fwd == kRows)
-    snprintf(fwd, sizeof(fwd), "i8_rows[m%d](W=%d)", 16 * std::max(1, std::min(4, (p.m + 15) / 16)), d->waves);
+    snprintf(fwd, sizeof(fwd), "%si8_rows[m%d](W=%d)", d->token ? "i8_token/" : "", 16 * std::max(1, std::min(4, (p.m + 15) / 16)), d->waves);
   else
     snprintf(fwd, sizeof(fwd), "i8_tile[%d]", d->fwd == kTile256 ? 256 : 128);
-  snprintf(d->names, sizeof(d->names), "fwd=%s;bwd_filter=i8_gradient[%d](S=%d);bwd_data=i8_gradient[%d](S=%d)", fwd, d->filter_tile, d->filter_splits,
-           d->data_tile, d->data_splits);
+  snprintf(d->names, sizeof(d->names), "fwd=%s;bwd_filter=i8_gradient[%d%s](S=%d);bwd_data=i8_gradient[%d%s](S=%d)", fwd, d->filter_tile, slow(O, M, true) ? ",slow" : "",
+           d->filter_splits, d->data_tile, slow(M, O, false) ? ",slow" : "", d->data_splits);
   *out = d;
   return CONV_OK;
 }
@@ -813,12 +979,10 @@ int i8_forward(const i8_desc_t* d, const void* x, const int8_t* w_codes, const f
   if (d->p.m == 0) return CONV_OK;
   if (!y || !codes || !scale || misaligned(codes)) return CONV_EINVAL;
   const hipStream_t stream = (hipStream_t)hip_stream;
-  int e = x ? quantise(d, x, codes, scale, d->p.m, stream) : 0;
-  if (e) return record_hip_error(e);
   const FwdArgs a = {codes, w_codes, scale, w_scale, bias, y, d->row, d->p.m, d->p.num_output, d->p.relu};
-  e = d->p.dtype == MI355_F32   ? launch_forward<MI355_F32>(d, a, stream)
-      : d->p.dtype == MI355_F16 ? launch_forward<MI355_F16>(d, a, stream)
-                                : launch_forward<MI355_BF16>(d, a, stream);
+  const int e = d->p.dtype == MI355_F32   ? launch_forward<MI355_F32>(d, a, x, codes, scale, stream)
+                : d->p.dtype == MI355_F16 ? launch_forward<MI355_F16>(d, a, x, codes, scale, stream)
+                                          : launch_forward<MI355_BF16>(d, a, x, codes, scale, stream);
   return e ? record_hip_error(e) : CONV_OK;
 }
 
