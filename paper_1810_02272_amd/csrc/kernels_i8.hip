@@ -885,7 +885,7 @@ void plan_gradient(int64_t rows, int64_t k, int64_t depth, bool filter, int32_t&
   const int64_t steps = std::max<int64_t>(1, (depth + kStep - 1) / kStep);
   tile = tiles_of(rows, k, 256) >= kUnits / 2 && !slow(rows, depth, filter) ? 256 : 128;
   const int64_t tiles = std::max<int64_t>(1, tiles_of(rows, k, tile)), places = tile == 256 ? 1 : 2 * kUnits;
-  splits = (int32_t)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(places / tiles, steps / 8), 64));
+  splits = (int32_t)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(places / tiles, steps / (tiles <= kUnits / 2 ? 4 : 8)), 64));
   per = (int32_t)((steps + splits - 1) / splits);
   splits = (int32_t)((steps + per - 1) / per);
 }

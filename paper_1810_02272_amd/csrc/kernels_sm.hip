@@ -70,25 +70,31 @@ constexpr int kUnits = 256;     // compute units
 constexpr int kAhead = 8;        // vectors that a thread asks for at a time
 constexpr float kNear = 8.f;    // nats below the maximum that the list holds: weights from 3e-4 on
 
-// 2^(i / 32), computed to 60 digits and rounded.
-__device__ const double kRoots[32] = {
-    1.0, 1.0218971486541166, 1.0442737824274138, 1.0671404006768237,
-    1.0905077326652577, 1.1143867425958924, 1.1387886347566916, 1.1637248587775775,
-    1.189207115002721, 1.215247359980469, 1.241857812073484, 1.2690509571917332,
-    1.2968395546510096, 1.3252366431597413, 1.3542555469368927, 1.383909881963832,
-    1.4142135623730951, 1.4451808069770467, 1.4768261459394993, 1.5091644275934228,
-    1.5422108254079407, 1.5759808451078865, 1.6104903319492543, 1.645755478153965,
-    1.681792830507429, 1.718619298122478, 1.7562521603732995, 1.7947090750031072,
-    1.8340080864093424, 1.8741676341103, 1.9152065613971474, 1.9571441241754002,
+// 2^(i / 64), computed to 60 digits and rounded.
+constexpr int kRootCount = 64, kRootBits = 6;
+__device__ const double kRoots[kRootCount] = {
+    1.0, 1.0108892860517005, 1.0218971486541166, 1.0330248790212284,
+    1.0442737824274138, 1.0556451783605572, 1.0671404006768237, 1.0787607977571199,
+    1.0905077326652577, 1.102382583307841, 1.1143867425958924, 1.1265216186082418,
+    1.1387886347566916, 1.1511892299529827, 1.1637248587775775, 1.1763969916502812,
+    1.189207115002721, 1.202156731452703, 1.215247359980469, 1.22848053610687,
+    1.241857812073484, 1.255380757024691, 1.2690509571917332, 1.2828700160787783,
+    1.2968395546510096, 1.3109612115247644, 1.3252366431597413, 1.339667524053303,
+    1.3542555469368927, 1.3690024229745905, 1.383909881963832, 1.3989796725383112,
+    1.4142135623730951, 1.42961333839197, 1.4451808069770467, 1.460917794180647,
+    1.4768261459394993, 1.4929077282912648, 1.5091644275934228, 1.5255981507445384,
+    1.5422108254079407, 1.559004400237837, 1.5759808451078865, 1.593142151342267,
+    1.6104903319492543, 1.6280274218573478, 1.645755478153965, 1.6636765803267364,
+    1.681792830507429, 1.7001063537185235, 1.718619298122478, 1.7373338352737062,
+    1.7562521603732995, 1.7753764925265212, 1.7947090750031072, 1.8142521755003989,
+    1.8340080864093424, 1.8539791250833855, 1.8741676341103, 1.8945759815869656,
+    1.9152065613971474, 1.9360617934922943, 1.9571441241754002, 1.978456026387951,
 };
 
-// 32 of them lie in 64 banks: the lanes' reads of different ones do not meet.  (512, and two terms less: 110 us for 1024 x 128256, bound by the banks,
-// where the arithmetic takes 60.)
-constexpr int kRootCount = 32;
-
-// 2^(i / 32), with i 2^15 taken out of the upper word: adding (32 n + i) 2^15 to it gives 2^(n + i / 32).
+// In shared memory with i 2^14 taken out of the upper word: adding (64 n + i) 2^14 to it gives 2^(n + i / 64).  (512 of them, and a term less: the lanes'
+// reads meet in the banks, 110 us for 1024 x 128256; 32, and a term more: 106.)
 __device__ __forceinline__ void fill_roots(double* root, int tid) {
-  if (tid < kRootCount) root[tid] = __builtin_bit_cast(double, __builtin_bit_cast(uint64_t, kRoots[tid]) - ((uint64_t)tid << (15 + 32)));
+  if (tid < kRootCount) root[tid] = __builtin_bit_cast(double, __builtin_bit_cast(uint64_t, kRoots[tid]) - ((uint64_t)tid << (20 - kRootBits + 32)));
 }
 
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
@@ -131,8 +137,8 @@ __device__ __forceinline__ uint64_t wave_scan(uint64_t v) {
   return v + move_words(v, 5);
 }
 
-// exp of the difference to the row's or segment's largest logit: 2^((32 n + i + r) / 32), |r| <= 1/2.  The number 1.5 2^52 brings 32 n + i
-// into the lower word; the polynomial's next term is below 2^-48.7.  What is below 2^-995 counts as 0.
+// exp of the difference to the row's or segment's largest logit: 2^((64 n + i + r) / 64), |r| <= 1/2.  The number 1.5 2^52 brings 64 n + i
+// into the lower word; the polynomial's next term is below 2^-44.5.  What is below 2^-995 counts as 0.
 struct Exponential {
   const double* root;  // in shared memory
   double top, c;
@@ -144,11 +150,14 @@ struct Exponential {
     low = fmaxf(largest - 690.f / scale, -FLT_MAX);
   }
 
+  static constexpr double kWhole = 0x1.8p52;
+
   // The weights of N logits, none of which is below `low`, added to a sum one after the other.  Their steps go side by side, so that a wave waits
-  // once for N entries.
+  // once for N entries.  Ten operations in 64 bits a logit take most of the time.  (One of them is the difference, which makes the largest one's weight
+  // 1 exactly, and so sums of equal ones exact.)
   template <int N>
   __device__ __forceinline__ double add(double sum, const float (&x)[N]) const {
-    constexpr double kWhole = 0x1.8p52, L = 0.69314718055994530942 / kRootCount;
+    constexpr double L = 0.69314718055994530942 / kRootCount;
     double r[N], entry[N];
     uint32_t at[N];
 #pragma unroll
@@ -162,11 +171,10 @@ struct Exponential {
 #pragma unroll
     for (int i = 0; i < N; ++i) {
       u32x2 words = __builtin_bit_cast(u32x2, entry[i]);
-      words[1] += at[i] << 15;
-      const double base = __builtin_bit_cast(double, words);
-      double p = fma(L * L * L * L * L / 120, r[i], L * L * L * L / 24);
-      p = fma(fma(fma(p, r[i], L * L * L / 6), r[i], L * L / 2), r[i], L);
-      sum += fma(base * r[i], p, base);
+      words[1] += at[i] << (20 - kRootBits);
+      double p = fma(L * L * L * L / 24, r[i], L * L * L / 6);
+      p = fma(fma(fma(p, r[i], L * L / 2), r[i], L), r[i], 1.);
+      sum = fma(__builtin_bit_cast(double, words), p, sum);
     }
     return sum;
   }
@@ -216,15 +224,12 @@ __device__ __forceinline__ float team_most(Shared<THREADS>& lds, float most) {
 __device__ __forceinline__ bool scale_is_good(float scale) { return scale >= 0x1p-60f && scale <= 0x1p60f; }
 
 // Vectors of a row [from, from + THREADS kChunkVecs), thread by thread.
-template <class E, int THREADS, bool LONG>
+template <class E, int THREADS>
 __device__ __forceinline__ void load_chunk(const typename E::T* row, int from, int nv, int n, int tid, u32x4 (&x)[kChunkVecs]) {
 #pragma unroll
   for (int j = 0; j < kChunkVecs; ++j) {
     const int v = from + j * THREADS + tid;
-    if constexpr (LONG)
-      x[j] = long_row_vec<E>(row, v, nv, n);
-    else
-      x[j] = v < nv ? row_vec<E>(row, v, n) : lowest_vec<E>();
+    x[j] = v < nv ? row_vec<E>(row, v, n) : lowest_vec<E>();
   }
 }
 
@@ -272,7 +277,8 @@ __global__ __launch_bounds__(256) void sm_sums_kernel(SmArgs a) {
   u32x4 x[kChunkVecs];
   float scale = 1.f;
   auto load = [&](int row, int from) {
-    load_chunk<E, 64, true>(static_cast<const T*>(a.logits) + (int64_t)row * a.stride, from, nv, n, lane, x);
+#pragma unroll
+    for (int j = 0; j < kChunkVecs; ++j) x[j] = begin_row_vec<E>(static_cast<const T*>(a.logits) + (int64_t)row * a.stride, from + j * 64 + lane, nv, n);
   };
   auto load_first = [&]() {
     if (r >= a.rows) return;
@@ -287,17 +293,22 @@ __global__ __launch_bounds__(256) void sm_sums_kernel(SmArgs a) {
     float most = -INFINITY, mine = -INFINITY;
     double sum = 0.;
     for (int c = 0; c < a.chunks; ++c) {
-      if (c > 0) load(r, segment * per + c * 64 * kChunkVecs);
-      const float here = chunk_most<E>(x), all = wave_most(here);
+      const int from = segment * per + c * 64 * kChunkVecs;
+      if (c > 0) load(r, from);
+      u32x4 now[kChunkVecs];
+#pragma unroll
+      for (int j = 0; j < kChunkVecs; ++j) now[j] = x[j];
+      if ((from + 64 * kChunkVecs) * E::VEC > n) {
+#pragma unroll
+        for (int j = 0; j < kChunkVecs; ++j) now[j] = end_row_vec<E>(now[j], from + j * 64 + lane, nv, n);
+      }
+      const float here = chunk_most<E>(now), all = wave_most(here);
       mine = fmaxf(mine, here);
       if (all > most) {
         weight.set(all, used);
         if (most > -INFINITY && all < INFINITY) sum *= weight(most);
         most = all;
       }
-      u32x4 now[kChunkVecs];
-#pragma unroll
-      for (int j = 0; j < kChunkVecs; ++j) now[j] = x[j];
       if (c + 1 == a.chunks) {
         r += step_r;
         segment += step_s;
@@ -1070,7 +1081,7 @@ __global__ __launch_bounds__(THREADS) void sm_row_kernel(SmArgs a) {
     u32x4 x[kChunkVecs];
     Part part = {-INFINITY, 0.f, 0.};
     if constexpr (HELD) {
-      load_chunk<E, 256, false>(t.row, 0, t.nv, t.n, tid, x);
+      load_chunk<E, 256>(t.row, 0, t.nv, t.n, tid, x);
 #pragma unroll
       for (int j = 0; j < kChunkVecs; ++j) lds.held[j * 256 + tid] = x[j];
       most = chunk_most<E>(x);

@@ -70,12 +70,22 @@ __device__ __forceinline__ u32x4 row_vec(const typename E::T* row, int v, int n)
   return E::pack(x);
 }
 
-// The same of a row of at least a vector, and -inf throughout beyond its last one: one load, whatever v is.
+// The same of a row of at least a vector, and -inf throughout beyond its last one: one load, whatever v is; and apart, for those who do something
+// else while it is on its way.
+template <class E>
+__device__ __forceinline__ u32x4 begin_row_vec(const typename E::T* row, int v, int nv, int n) {
+  return load_vec<E>(row + slot_of<E>(min(v, nv - 1), n).base);
+}
+
+template <class E>
+__device__ __forceinline__ u32x4 end_row_vec(const u32x4& r, int v, int nv, int n) {
+  const int lo = slot_of<E>(v, n).lo;
+  return v >= nv ? lowest_vec<E>() : lo ? without_first<E>(r, lo) : r;
+}
+
 template <class E>
 __device__ __forceinline__ u32x4 long_row_vec(const typename E::T* row, int v, int nv, int n) {
-  const Slot<E> at = slot_of<E>(min(v, nv - 1), n);
-  const u32x4 r = load_vec<E>(row + at.base);
-  return v >= nv ? lowest_vec<E>() : at.lo ? without_first<E>(r, at.lo) : r;
+  return end_row_vec<E>(begin_row_vec<E>(row, v, nv, n), v, nv, n);
 }
 
 template <int THREADS>
