@@ -66,6 +66,54 @@ __device__ __forceinline__ int code_of(float x, float s, float inverse) {
   return (int)q;
 }
 
+// A vector's codes, four a word.  x / s plus 1.5 2^23 has the whole number in its last byte, and is one off at most, where x is as far from it as
+// half a step or farther: hardly ever, and then all are looked at closely.
+template <class E>
+__device__ __forceinline__ void codes_of(const u32x4& vec, float s, float inverse, uint32_t (&w)[E::VEC / 4]) {
+  float x[E::VEC], most = 0.f;
+  uint32_t c[E::VEC];
+#pragma unroll
+  for (int i = 0; i < E::VEC; ++i) {
+    x[i] = E::get(vec, i);
+    const float placed = fmaf(x[i], inverse, 0x1.8p23f), q = placed - 0x1.8p23f;
+    c[i] = __builtin_bit_cast(uint32_t, placed);
+    most = fmaxf(most, fabsf(fmaf(-q, s, x[i])));
+  }
+  if (!(most < 0.5f * s)) {
+#pragma unroll
+    for (int i = 0; i < E::VEC; ++i) c[i] = (uint32_t)code_of(x[i], s, inverse);
+  }
+#pragma unroll
+  for (int i = 0; i < E::VEC / 4; ++i) {
+    const uint32_t lo = __builtin_amdgcn_perm(c[4 * i + 1], c[4 * i], 0x0c0c0400u), hi = __builtin_amdgcn_perm(c[4 * i + 3], c[4 * i + 2], 0x04000c0cu);
+    w[i] = s < INFINITY ? lo | hi : 0u;
+  }
+}
+
+// The largest magnitude of a thread's vectors, as bits: of both halves of a word side by side where an element is 16 bits.  NaN is above infinity.
+template <int DTYPE>
+struct Most {
+  typedef unsigned short Pair __attribute__((ext_vector_type(2)));
+  uint32_t most = 0;
+
+  __device__ __forceinline__ void look(const u32x4& vec) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const uint32_t word = vec[i];
+      if constexpr (DTYPE == MI355_F32)
+        most = max(most, word & 0x7fffffffu);
+      else
+        most = __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(Pair, most), __builtin_bit_cast(Pair, word & 0x7fff7fffu)));
+    }
+  }
+
+  __device__ __forceinline__ uint32_t magnitude() const {  // fp32's bits
+    if constexpr (DTYPE == MI355_F32) return most;
+    const u32x4 both = {most, 0, 0, 0};
+    return max(__builtin_bit_cast(uint32_t, Elem<DTYPE>::get(both, 0)), __builtin_bit_cast(uint32_t, Elem<DTYPE>::get(both, 1)));
+  }
+};
+
 // THREADS threads for a row: its largest magnitude, then the codes, from registers for up to NV vectors a thread, read again beyond.  Bound by
 // memory.  THREADS 64: a wave for each row, four in a workgroup.
 template <int DTYPE, int THREADS, int NV>
@@ -88,11 +136,7 @@ __global__ __launch_bounds__(THREADS == 64 ? 256 : THREADS) void i8_quantise_ker
       for (int i = 0; i < VEC; ++i) f[i] = at + i < k ? E::to_float(from[at + i]) : 0.f;
       return E::pack(f);
     };
-    uint32_t most = 0;  // as the bits of a magnitude: NaN is above infinity
-    auto look = [&](const u32x4& vec) {
-#pragma unroll
-      for (int i = 0; i < VEC; ++i) most = max(most, __builtin_bit_cast(uint32_t, E::get(vec, i)) & 0x7fffffffu);
-    };
+    Most<DTYPE> seen;
     u32x4 held[NV];
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
@@ -100,9 +144,9 @@ __global__ __launch_bounds__(THREADS == 64 ? 256 : THREADS) void i8_quantise_ker
       if (j * THREADS + tid < vectors) held[j] = load(j * THREADS + tid);
     }
 #pragma unroll
-    for (int j = 0; j < NV; ++j) look(held[j]);
-    for (int v = NV * THREADS + tid; v < vectors; v += THREADS) look(load(v));
-    most = (uint32_t)wave_reduce((int)most, 0, [](int a, int b) { return max(a, b); });
+    for (int j = 0; j < NV; ++j) seen.look(held[j]);
+    for (int v = NV * THREADS + tid; v < vectors; v += THREADS) seen.look(load(v));
+    uint32_t most = (uint32_t)wave_reduce((int)seen.magnitude(), 0, [](int a, int b) { return max(a, b); });
     if constexpr (THREADS > 64) {
       __syncthreads();
       if (lane == 0) most_of[wave] = most;
@@ -111,18 +155,11 @@ __global__ __launch_bounds__(THREADS == 64 ? 256 : THREADS) void i8_quantise_ker
       for (int w = 0; w < THREADS / 64; ++w) most = max(most, most_of[w]);
     }
     const float s = scale_for(__builtin_bit_cast(float, most)), inverse = 1.f / s;
-    const bool finite = s < INFINITY;
     if (tid == 0) scales[r] = s;
     int8_t* const to = codes + r * row_bytes;
     auto put = [&](const u32x4& vec, int v) {
       uint32_t w[VEC / 4];
-#pragma unroll
-      for (int i = 0; i < VEC / 4; ++i) {
-        uint32_t word = 0;
-#pragma unroll
-        for (int b = 0; b < 4; ++b) word |= ((uint32_t)code_of(E::get(vec, 4 * i + b), s, inverse) & 255u) << (8 * b);
-        w[i] = finite ? word : 0u;
-      }
+      codes_of<E>(vec, s, inverse, w);
       if constexpr (VEC == 8)
         *reinterpret_cast<uint2*>(to + (int64_t)v * 8) = make_uint2(w[0], w[1]);
       else
@@ -271,13 +308,9 @@ __global__ __launch_bounds__(1024) void i8_token_kernel(FwdArgs a, const void* _
     return E::pack(f);
   };
   for (int n = 0; n < a.m; ++n) {
-    uint32_t most = 0;
-    for (int v = tid; v < vectors; v += blockDim.x) {
-      const u32x4 vec = load(n, v);
-#pragma unroll
-      for (int i = 0; i < VEC; ++i) most = max(most, __builtin_bit_cast(uint32_t, E::get(vec, i)) & 0x7fffffffu);
-    }
-    most = (uint32_t)wave_reduce((int)most, 0, [](int p, int q) { return max(p, q); });
+    Most<DTYPE> seen;
+    for (int v = tid; v < vectors; v += blockDim.x) seen.look(load(n, v));
+    const uint32_t most = (uint32_t)wave_reduce((int)seen.magnitude(), 0, [](int p, int q) { return max(p, q); });
     if (lane == 0) most_of[n][wave] = most;
   }
   __syncthreads();
@@ -285,21 +318,17 @@ __global__ __launch_bounds__(1024) void i8_token_kernel(FwdArgs a, const void* _
     uint32_t most = 0;
     for (int p = 0; p < waves; ++p) most = max(most, most_of[n][p]);
     const float s = scale_for(__builtin_bit_cast(float, most)), inverse = 1.f / s;
-    const bool finite = s < INFINITY;
     if (tid == 0) {
       scale[n] = s;
       if (blockIdx.x == 0) scales[n] = s;
     }
     for (int v = tid; v < vectors; v += blockDim.x) {
-      const u32x4 vec = load(n, v);
+      uint32_t w[VEC / 4];
+      codes_of<E>(load(n, v), s, inverse, w);
 #pragma unroll
       for (int i = 0; i < VEC / 4; ++i) {
-        uint32_t word = 0;
-#pragma unroll
-        for (int b = 0; b < 4; ++b) word |= ((uint32_t)code_of(E::get(vec, 4 * i + b), s, inverse) & 255u) << (8 * b);
-        if (!finite) word = 0;
-        reinterpret_cast<uint32_t*>(rows + n * row)[v * (VEC / 4) + i] = word;
-        if (blockIdx.x == 0) reinterpret_cast<uint32_t*>(codes + (int64_t)n * row)[v * (VEC / 4) + i] = word;
+        reinterpret_cast<uint32_t*>(rows + n * row)[v * (VEC / 4) + i] = w[i];
+        if (blockIdx.x == 0) reinterpret_cast<uint32_t*>(codes + (int64_t)n * row)[v * (VEC / 4) + i] = w[i];
       }
     }
   }
