@@ -152,9 +152,9 @@ def test_i8_variants_have_parity_cases():
                                   lib.i8_desc_kernel_names(lib.i8_desc_create(lib.I8Params(m, k, o, dtype))).split(";")}
     seen = set().union(*(key(*c[:4]) for c in t.CASES))
     for dtype in (F32, F16, BF16):
-        for m in (1, 16, 17, 33, 64, 65, 200, 1000, 1500, 4096, 8192):  # what the library selects over a wide range
-            for k in (32, 100, 1024, 4096, 12000):
-                for o in (1, 8, 100, 1000, 2000, 4096, 12000):
+        for m in (1, 3, 4, 5, 16, 17, 33, 64, 65, 200, 1000, 1500, 4096, 8192):  # what the library selects over a wide range
+            for k in (32, 100, 1024, 4096, 12000, 40000):
+                for o in (1, 3, 4, 8, 100, 1000, 2000, 4096, 12000):
                     assert key(m, k, o, dtype) <= seen, (m, k, o, key(m, k, o, dtype) - seen)
 
 

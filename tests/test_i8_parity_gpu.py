@@ -27,6 +27,8 @@ CASES = [
     (1500, 200, 900, F32, 1, 1), (1100, 129, 1030, BF16, 1, 0), (2001, 257, 777, F16, 0, 0), (4096, 300, 2100, BF16, 1, 1), (4099, 260, 2050, F16, 1, 0), (3000, 130, 3001, F32, 0, 0),
     (256, 4096, 1000, F32, 1, 0), (1999, 1111, 777, F16, 1, 0), (3333, 96, 130, BF16, 1, 0), (31, 2900, 2900, BF16, 1, 0), (40, 2900, 3100, F32, 0, 0), (64, 3001, 2900, F16, 1, 0),
     (3001, 2900, 70, BF16, 0, 0), (3000, 2901, 50, F32, 0, 0), (2999, 2900, 64, F16, 0, 0), (900, 2900, 2048, BF16, 1, 0), (5000, 128, 31, F32, 1, 1), (2, 60000, 5, BF16, 0, 0), (3, 133120, 4, F32, 0, 0),
+    (20, 130, 40, F16, 0, 0), (7, 4097, 4100, F32, 1, 0), (2, 96, 5, F16, 1, 0), (40, 513, 6, BF16, 1, 0), (3000, 131, 3, F32, 1, 0), (2999, 260, 2, F16, 1, 0),
+    (3001, 140, 1, BF16, 1, 0), (8, 300, 8, BF16, 1, 0), (9, 257, 9, F16, 1, 0), (130, 129, 259, BF16, 1, 0), (131, 200, 387, F16, 1, 0), (133, 64, 130, F32, 1, 0),
 ]
 
 

@@ -156,6 +156,21 @@ def test_ties_at_the_last_place(vocab):
         check(run(x, u, None, full(rows, vocab - 2, I32), full(rows, p)), x, u, None, full(rows, vocab - 2, I32), full(rows, p))
 
 
+@pytest.mark.parametrize("dtype", [F32, F16, BF16])
+@pytest.mark.parametrize("vocab,spread", [(8000, 1.0), (40000, 0.3), (128256, 0.5), (128256, 2.5)])
+def test_limits_that_keep_few_many_and_most(vocab, spread, dtype):
+    """What is kept is ranked, found in a list, or found in the row itself: from a few tokens to nearly all, by each limit and by two of them; with
+    a share of banned tokens."""
+    rows = 12
+    x, u, *_ = make((rows, vocab, dtype, vocab, spread), seed=5)
+    x = x.masked_fill(torch.rand((1, vocab), generator=torch.Generator(device=DEV).manual_seed(1), device=DEV) < 0.1, -math.inf)
+    ks = torch.tensor([1, 7, 60, 250, 400, 700, 1500, 4000, 7000, vocab // 3, vocab - 5, vocab // 2], device=DEV, dtype=I32)
+    ps = torch.tensor([0.001, 0.05, 0.2, 0.4, 0.6, 0.8, 0.9, 0.95, 0.99, 0.999, 0.99999, 0.5], device=DEV)
+    qs = torch.tensor([0.9, 0.5, 0.2, 0.1, 0.05, 0.02, 0.01, 0.003, 1e-3, 1e-4, 1e-6, 1e-30], device=DEV)
+    for limits in ((ks, None, None), (None, ps, None), (None, None, qs), (ks, ps.flip(0), None), (ks, None, qs.flip(0)), (None, ps, qs.flip(0)), (ks.flip(0), ps, qs)):
+        check(run(x, u, None, *limits), x, u, None, *limits)
+
+
 @pytest.mark.parametrize("vocab", [50, 5000, 100000])
 def test_logits_that_differ_in_their_last_bits(vocab):
     """fp32 logits closer to each other than their distance from the maximum can tell; and far apart."""
