@@ -177,7 +177,7 @@ int launch_quantise(const void* x, int8_t* codes, float* scales, int rows, int k
   const int64_t vectors = row / Elem<DTYPE>::VEC;
   if (vectors <= 64 * 4)
     hipLaunchKernelGGL((i8_quantise_kernel<DTYPE, 64, 4>), dim3((uint32_t)(((int64_t)rows + 3) / 4)), dim3(256), 0, stream, x, codes, scales, rows, k, row);
-  else if (vectors > 256 * 4 && rows <= 2 * kUnits)  // (48 x 9216 fp32: 256 threads 7.6 us, 1024 @Q)
+  else if (vectors > 256 * 4 && rows <= 2 * kUnits)  // (48 x 9216 fp32: 256 threads 7.6 us, 1024 4.8)
     hipLaunchKernelGGL((i8_quantise_kernel<DTYPE, 1024, 4>), dim3(rows), dim3(1024), 0, stream, x, codes, scales, rows, k, row);
   else
     hipLaunchKernelGGL((i8_quantise_kernel<DTYPE, 256, 4>), dim3(std::min(rows, 1 << 22)), dim3(256), 0, stream, x, codes, scales, rows, k, row);
@@ -502,7 +502,7 @@ struct BwdArgs {
   float beta;
 };
 
-constexpr int kStep = 32;  // terms of the sums that a step takes
+constexpr int step_of(int tile) { return tile == 64 ? 64 : 32; }  // terms of the sums that a step takes
 
 // Values as bf16 terms, two at a time: the rounded value, what is left of it rounded, and so on.
 template <int TERMS>
@@ -526,22 +526,23 @@ __device__ __forceinline__ void pair_terms(float a, float b, uint32_t (&w)[TERMS
 // Every load is in range and none waits for a branch: the last terms of a sum that are fewer than 8 come as the last 8, with zeros for those that the
 // groups before hold, and the last outputs that are fewer than four as the last four, each to its own place.  SLOW: sums or rows too short
 // for that, one by one.
-// Waves of 64 rows by 16 NT inputs.
+// Waves of 16 MT rows by 16 NT inputs.
 template <int DTYPE, bool FILTER, int TILE, bool SLOW>
 __global__ __launch_bounds__(TILE == 256 ? 512 : 256, 2) void i8_gradient_kernel(BwdArgs a) {
   typedef Elem<DTYPE> E;
   typedef typename E::T T;
-  constexpr int THREADS = TILE == 256 ? 512 : 256, HALF = THREADS / 2, WN = 2, NT = TILE / (16 * WN), TERMS = DTYPE == MI355_BF16 ? 2 : 3;
+  constexpr int THREADS = TILE == 256 ? 512 : 256, HALF = THREADS / 2, WN = TILE == 64 ? 1 : 2, MT = TILE == 64 ? 1 : 4, NT = TILE / (16 * WN);
+  constexpr int TERMS = DTYPE == MI355_BF16 ? 2 : 3, STEP = step_of(TILE), GROUPS = STEP / 8;
   // pieces of 16 bytes: [term][group of 8 terms of the sum][place], and the same of the codes; two are left out after every 16, and four
   // after a group, so that the lanes that write meet no bank twice
-  constexpr int GROUP = TILE + TILE / 8 + 4, TERM = 4 * GROUP, BUFFER = (TERMS + 1) * TERM;
+  constexpr int GROUP = TILE + TILE / 8 + 4, TERM = GROUPS * GROUP, BUFFER = (TERMS + 1) * TERM;
   __shared__ __attribute__((aligned(16))) u32x4 lds[2][BUFFER];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), wm = wave / WN, wn = wave % WN;
   const int rows = FILTER ? a.o : a.n, depth = FILTER ? a.n : a.o;
   int tm, tn;
   tile_place((rows + TILE - 1) / TILE, (a.k + TILE - 1) / TILE, tm, tn);
   const int r0 = tm * TILE, i0 = tn * TILE;
-  const int first = blockIdx.y * a.per, steps = min(a.per, (depth + kStep - 1) / kStep - first);
+  const int first = blockIdx.y * a.per, steps = min(a.per, (depth + STEP - 1) / STEP - first);
   const bool sum_bias = FILTER && a.db && tn == 0;
 
   const bool of_dz = wave < HALF / 64;
@@ -555,18 +556,18 @@ __global__ __launch_bounds__(TILE == 256 ? 512 : 256, 2) void i8_gradient_kernel
   for (int q = 0; q < 4; ++q) places[q] = !FILTER || !of_dz ? place_of(4 * p + q) : out + q >= r0 ? place_of(out + q - r0) : GROUP - 1;  // (another tile's: nobody reads it)
   // the first term of a group's 8 in a step, and how many of them are not the group's
   auto first_of = [&](int step, int group, int& skip) {
-    const int d0 = (first + step) * kStep + 8 * group, from = max(0, min(d0, depth - 8));
+    const int d0 = (first + step) * STEP + 8 * group, from = max(0, min(d0, depth - 8));
     skip = d0 - from;
     return from;
   };
-  constexpr int DATA_ROWS = TILE * 4 / HALF;  // data: 8 terms of rows half / 4 and on, HALF / 4 apart
+  constexpr int DATA_ROWS = TILE * GROUPS / HALF;  // data: 8 terms of rows half / GROUPS and on, HALF / GROUPS apart
   constexpr int WORDS = DTYPE == MI355_F32 ? 4 : 2;
   typedef typename std::conditional<DTYPE == MI355_F32, u32x4, u32x2>::type Four;
   struct __attribute__((packed, aligned(sizeof(T)))) FourMem {
     Four v;
   };
   float bias[4] = {0.f, 0.f, 0.f, 0.f};
-  f32x4 acc[4][NT] = {};
+  f32x4 acc[MT][NT] = {};
 
   struct Filter {
     Four z[8];
@@ -588,7 +589,7 @@ __global__ __launch_bounds__(TILE == 256 ? 512 : 256, 2) void i8_gradient_kernel
     for (int j = 0; j < 8; ++j) way.c[j] = *reinterpret_cast<const uint32_t*>(at + (int64_t)(SLOW ? min(j, depth - 1 - from) : j) * a.row);
   };
   auto load_dz = [&](Way& way, int step) {
-    const int from = first_of(step, FILTER ? g : half & 3, way.skip);
+    const int from = first_of(step, FILTER ? g : half % GROUPS, way.skip);
 #pragma unroll
     for (int j = 0; j < 8; ++j) way.s[j] = a.scale[SLOW ? min(from + j, depth - 1) : from + j];
     if constexpr (FILTER) {
@@ -610,7 +611,7 @@ __global__ __launch_bounds__(TILE == 256 ? 512 : 256, 2) void i8_gradient_kernel
     } else {
 #pragma unroll
       for (int i = 0; i < DATA_ROWS; ++i) {
-        const T* const z = static_cast<const T*>(a.dz) + (int64_t)min(r0 + half / 4 + i * (HALF / 4), rows - 1) * a.o + from;
+        const T* const z = static_cast<const T*>(a.dz) + (int64_t)min(r0 + half / GROUPS + i * (HALF / GROUPS), rows - 1) * a.o + from;
         if constexpr (SLOW) {
           float f[8];
 #pragma unroll
@@ -691,33 +692,36 @@ __global__ __launch_bounds__(TILE == 256 ? 512 : 256, 2) void i8_gradient_kernel
         for (int j = 0; j < 8; ++j) v[j] = E::get(way.raw.z[i][j / E::VEC], j % E::VEC);
         u32x4 w[TERMS];
         terms_of(way, v, w);
-        const int row = half / 4 + i * (HALF / 4);
+        const int row = half / GROUPS + i * (HALF / GROUPS);
 #pragma unroll
-        for (int t = 0; t < TERMS; ++t) buffer[t * TERM + (half & 3) * GROUP + row + 2 * (row >> 4)] = w[t];
+        for (int t = 0; t < TERMS; ++t) buffer[t * TERM + half % GROUPS * GROUP + row + 2 * (row >> 4)] = w[t];
       }
     }
   };
 
   // Both kinds of waves take the same steps, and meet at the same barriers.
   auto products = [&](int step, auto&& between) {
-    const u32x4* const A = lds[step & 1] + (lane >> 4) * GROUP + wm * 72 + (lane & 15);
-    const u32x4* const B = lds[step & 1] + TERMS * TERM + (lane >> 4) * GROUP + wn * NT * 18 + (lane & 15);
-    bf16x8 w[NT];
 #pragma unroll
-    for (int u = 0; u < NT; ++u) w[u] = __builtin_bit_cast(bf16x8, B[u * 18]);
+    for (int part = 0; part < STEP / 32; ++part) {
+      const u32x4* const A = lds[step & 1] + (4 * part + (lane >> 4)) * GROUP + wm * MT * 18 + (lane & 15);
+      const u32x4* const B = lds[step & 1] + TERMS * TERM + (4 * part + (lane >> 4)) * GROUP + wn * NT * 18 + (lane & 15);
+      bf16x8 w[NT];
 #pragma unroll
-    for (int t = 0; t < TERMS; ++t) {
-      bf16x8 x[4];
+      for (int u = 0; u < NT; ++u) w[u] = __builtin_bit_cast(bf16x8, B[u * 18]);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) x[i] = __builtin_bit_cast(bf16x8, A[t * TERM + 18 * i]);
+      for (int t = 0; t < TERMS; ++t) {
+        bf16x8 x[MT];
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
+        for (int i = 0; i < MT; ++i) x[i] = __builtin_bit_cast(bf16x8, A[t * TERM + 18 * i]);
 #pragma unroll
-        for (int u = 0; u < NT; ++u) acc[i][u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x[i], w[u], acc[i][u], 0, 0, 0);
-      if (t + 2 == TERMS) {
-        __builtin_amdgcn_sched_barrier(0);
-        between();
-        __builtin_amdgcn_sched_barrier(0);
+        for (int i = 0; i < MT; ++i)
+#pragma unroll
+          for (int u = 0; u < NT; ++u) acc[i][u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x[i], w[u], acc[i][u], 0, 0, 0);
+        if (part + 1 == STEP / 32 && t + 2 == TERMS) {
+          __builtin_amdgcn_sched_barrier(0);
+          between();
+          __builtin_amdgcn_sched_barrier(0);
+        }
       }
     }
     __syncthreads();
@@ -767,7 +771,7 @@ __global__ __launch_bounds__(TILE == 256 ? 512 : 256, 2) void i8_gradient_kernel
   }
 
   const bool split = gridDim.y > 1;
-  if (sum_bias) {  // the four groups' sums of each output
+  if (sum_bias) {  // the groups' sums of each output
     float* const sums = reinterpret_cast<float*>(lds);
     if (of_dz) {
 #pragma unroll
@@ -776,7 +780,9 @@ __global__ __launch_bounds__(TILE == 256 ? 512 : 256, 2) void i8_gradient_kernel
     }
     __syncthreads();
     if (tid < TILE && r0 + tid < a.o) {
-      const float v = (sums[tid] + sums[TILE + tid]) + (sums[2 * TILE + tid] + sums[3 * TILE + tid]);
+      float v = sums[tid];
+#pragma unroll
+      for (int i = 1; i < GROUPS; ++i) v += sums[i * TILE + tid];
       if (split)
         a.db_parts[(int64_t)blockIdx.y * a.o + r0 + tid] = v;
       else
@@ -788,10 +794,11 @@ __global__ __launch_bounds__(TILE == 256 ? 512 : 256, 2) void i8_gradient_kernel
     const int at = i0 + wn * NT * 16 + h * 64 + 4 * (lane & 15);
     if (at >= a.k) continue;
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
+    for (int i = 0; i < MT; ++i)
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
-        const int in_tile = 4 * (lane >> 4) + r, to_row = r0 + wm * 64 + (FILTER ? 4 * in_tile + i : 16 * i + in_tile);  // (filter: as the places go)
+        const int in_tile = 4 * (lane >> 4) + r, tile = wm * MT + i;  // of 16 rows; filter: as the places go
+        const int to_row = r0 + (FILTER ? (tile >> 2) * 64 + 4 * in_tile + (tile & 3) : 16 * tile + in_tile);
         if (to_row >= rows) continue;
         float v[4];
 #pragma unroll
@@ -874,8 +881,10 @@ int launch_gradient(const BwdArgs& a, int tile, int splits, hipStream_t stream) 
   const dim3 grid((uint32_t)(((int64_t)rows + tile - 1) / tile * (((int64_t)a.k + tile - 1) / tile)), splits);
   if (slow(rows, FILTER ? a.n : a.o, FILTER))
     hipLaunchKernelGGL((i8_gradient_kernel<DTYPE, FILTER, 128, true>), grid, dim3(256), 0, stream, a);
-  else if (tile == 256)
-    hipLaunchKernelGGL((i8_gradient_kernel<DTYPE, FILTER, 256, false>), grid, dim3(512), 0, stream, a);
+  else if (tile == 256) {
+    if constexpr (FILTER || DTYPE != MI355_F32) hipLaunchKernelGGL((i8_gradient_kernel<DTYPE, FILTER, 256, false>), grid, dim3(512), 0, stream, a);
+  } else if (tile == 64)
+    hipLaunchKernelGGL((i8_gradient_kernel<DTYPE, FILTER, 64, false>), grid, dim3(256), 0, stream, a);
   else
     hipLaunchKernelGGL((i8_gradient_kernel<DTYPE, FILTER, 128, false>), grid, dim3(256), 0, stream, a);
   const int e = (int)hipGetLastError();
@@ -909,10 +918,17 @@ int clear(float* to, int64_t count, hipStream_t stream) {
 
 int64_t tiles_of(int64_t rows, int64_t columns, int tile) { return (rows + tile - 1) / tile * ((columns + tile - 1) / tile); }
 
-// The tile of a gradient, and the workgroups that share a sum.
-void plan_gradient(int64_t rows, int64_t k, int64_t depth, bool filter, int32_t& tile, int32_t& splits, int32_t& per) {
-  const int64_t steps = std::max<int64_t>(1, (depth + kStep - 1) / kStep);
-  tile = tiles_of(rows, k, 256) >= kUnits / 2 && !slow(rows, depth, filter) ? 256 : 128;
+// The tile of a gradient, and the workgroups that share a sum.  A tile of 256 has a compute unit to itself, of 128 half of one; a round of the former takes
+// 1.4 times as long as one of the latter where dz is two terms, 1.7 to 1.9 where it is three, 2.3 for dx in fp32, whose kernel keeps 152 bytes a lane in
+// scratch memory (us, 256 and 128: dw of 8192 x 4096 -> 4096 bf16 483, 683, fp16 812, 961, fp32 1124, 1199; dx of the same 451, 630; 852, 903; 1232, 1083; dw of
+// 8192 x 4096 -> 2048 bf16, half a round, 456, 359).  Where a tile of 128 leaves half of the units without work, 64: dx of 100 x 999 <- 333 fp32 10.3, with
+// 128 17.4; of 512 x 333 <- 150 fp32 6.8, 12.5; dw of 2000 x 512 -> 512 bf16 17.0, 18.7, of 1999 x 1111 -> 777 fp16 40.4, 38.3; of 1000 x 2000 -> 1000 bf16, 128 tiles of
+// 128, 30.0, 30.7; of 64 x 4096 -> 4096 bf16 33.1, 21.8.
+void plan_gradient(int64_t rows, int64_t k, int64_t depth, int dtype, bool filter, int32_t& tile, int32_t& splits, int32_t& per) {
+  const int64_t large = (tiles_of(rows, k, 256) + kUnits - 1) / kUnits, medium = (tiles_of(rows, k, 128) + 2 * kUnits - 1) / (2 * kUnits);  // rounds
+  const double round = dtype == MI355_BF16 ? 1.43 : filter || dtype == MI355_F16 ? 1.85 : 2.3;
+  tile = slow(rows, depth, filter) ? 128 : tiles_of(rows, k, 128) < kUnits / 2 ? 64 : round * large < medium ? 256 : 128;
+  const int64_t step = step_of(tile), steps = std::max<int64_t>(1, (depth + step - 1) / step);
   const int64_t tiles = std::max<int64_t>(1, tiles_of(rows, k, tile)), places = tile == 256 ? 1 : 2 * kUnits;
   splits = (int32_t)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(places / tiles, steps / (tiles <= kUnits / 2 ? 4 : 8)), 64));
   per = (int32_t)((steps + splits - 1) / splits);
@@ -950,8 +966,8 @@ int i8_desc_create(i8_desc_t** out, const i8_params_t* pp) {
   d->fwd = M <= 64 || tiles_of(M, O, 128) < kUnits / 4 ? kRows : tiles_of(M, O, 256) >= kUnits / 2 ? kTile256 : kTile128;
   d->waves = (int32_t)std::max<int64_t>(1, std::min<int64_t>(tiles_of(M, O, 16) > 4 * kUnits ? 4 : 16, d->row / kRowUnit));
   d->token = d->fwd == kRows && M <= kTokenRows && M * d->row <= kTokenBytes;
-  plan_gradient(O, K, M, true, d->filter_tile, d->filter_splits, d->filter_per);
-  plan_gradient(M, K, O, false, d->data_tile, d->data_splits, d->data_per);
+  plan_gradient(O, K, M, p.dtype, true, d->filter_tile, d->filter_splits, d->filter_per);
+  plan_gradient(M, K, O, p.dtype, false, d->data_tile, d->data_splits, d->data_per);
   if (M > 0) {
     if (d->filter_splits > 1) d->ws_bytes = (size_t)d->filter_splits * (O * K + O) * 4;
     if (d->data_splits > 1) d->ws_bytes = std::max(d->ws_bytes, (size_t)d->data_splits * M * K * 4);
