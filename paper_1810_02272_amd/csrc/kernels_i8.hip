@@ -43,6 +43,7 @@ constexpr int kRowUnit = 128;          // bytes that a row of codes is a multipl
 constexpr int kMostInputs = 133120;    // 127^2 times this fits 32 bits
 constexpr int kUnits = 256;            // compute units
 constexpr int64_t kMaxElems = (int64_t)1 << 30;
+constexpr int kMostBlocks = 1 << 21;   // of up to 1024 threads: a launch has fewer than 2^32
 
 enum FwdForm { kRows, kTile128, kTile256 };
 
@@ -176,11 +177,11 @@ template <int DTYPE>
 int launch_quantise(const void* x, int8_t* codes, float* scales, int rows, int k, int64_t row, hipStream_t stream) {
   const int64_t vectors = row / Elem<DTYPE>::VEC;
   if (vectors <= 64 * 4)
-    hipLaunchKernelGGL((i8_quantise_kernel<DTYPE, 64, 4>), dim3((uint32_t)(((int64_t)rows + 3) / 4)), dim3(256), 0, stream, x, codes, scales, rows, k, row);
+    hipLaunchKernelGGL((i8_quantise_kernel<DTYPE, 64, 4>), dim3((uint32_t)std::min<int64_t>(((int64_t)rows + 3) / 4, kMostBlocks)), dim3(256), 0, stream, x, codes, scales, rows, k, row);
   else if (vectors > 256 * 4 && rows <= 2 * kUnits)  // (48 x 9216 fp32: 256 threads 7.6 us, 1024 4.8)
     hipLaunchKernelGGL((i8_quantise_kernel<DTYPE, 1024, 4>), dim3(rows), dim3(1024), 0, stream, x, codes, scales, rows, k, row);
   else
-    hipLaunchKernelGGL((i8_quantise_kernel<DTYPE, 256, 4>), dim3(std::min(rows, 1 << 22)), dim3(256), 0, stream, x, codes, scales, rows, k, row);
+    hipLaunchKernelGGL((i8_quantise_kernel<DTYPE, 256, 4>), dim3(std::min(rows, kMostBlocks)), dim3(256), 0, stream, x, codes, scales, rows, k, row);
   return (int)hipGetLastError();
 }
 
@@ -233,9 +234,10 @@ __global__ __launch_bounds__(1024) void i8_rows_kernel(FwdArgs a) {
   constexpr int AHEAD = MT == 1 ? 4 : 2;
   extern __shared__ int parts[];  // [waves][MT * 256]
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), waves = blockDim.x >> 6;
-  const int o0 = blockIdx.x * 16, blocks = (int)(a.row / kRowUnit);
-  const int8_t* const w = a.w_codes + (int64_t)min(o0 + (lane & 15), a.o - 1) * a.row + 16 * (lane >> 4);
-  for (int m0 = blockIdx.y * 16 * MT; m0 < a.m; m0 += gridDim.y * 16 * MT) {
+  const int blocks = (int)(a.row / kRowUnit), tiles = (a.o + 15) / 16, groups = (a.m + 16 * MT - 1) / (16 * MT);
+  for (int64_t item = blockIdx.x; item < (int64_t)tiles * groups; item += gridDim.x) {
+    const int o0 = (int)(item % tiles) * 16, m0 = (int)(item / tiles) * 16 * MT;
+    const int8_t* const w = a.w_codes + (int64_t)min(o0 + (lane & 15), a.o - 1) * a.row + 16 * (lane >> 4);
     const int8_t* x[MT];
 #pragma unroll
     for (int t = 0; t < MT; ++t) x[t] = a.codes + (int64_t)min(m0 + 16 * t + (lane & 15), a.m - 1) * a.row + 16 * (lane >> 4);
@@ -289,15 +291,20 @@ __global__ __launch_bounds__(1024) void i8_token_kernel(FwdArgs a, const void* _
   __shared__ uint32_t most_of[kTokenRows][16];
   __shared__ float scale[kTokenRows];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), waves = blockDim.x >> 6;
-  const int o0 = blockIdx.x * 16, blocks = (int)(a.row / kRowUnit), row = (int)a.row, vectors = row / VEC;
-  const int8_t* const w = a.w_codes + (int64_t)min(o0 + (lane & 15), a.o - 1) * a.row + 16 * (lane >> 4);
+  const int blocks = (int)(a.row / kRowUnit), row = (int)a.row, vectors = row / VEC;
+  int o0 = blockIdx.x * 16;
+  const int8_t* w;
   i32x4 wv[kTokenAhead][2] = {};
+  auto ask = [&]() {
+    w = a.w_codes + (int64_t)min(o0 + (lane & 15), a.o - 1) * a.row + 16 * (lane >> 4);
 #pragma unroll
-  for (int i = 0; i < kTokenAhead; ++i)
-    if (wave + i * waves < blocks) {
+    for (int i = 0; i < kTokenAhead; ++i)
+      if (wave + i * waves < blocks) {
 #pragma unroll
-      for (int h = 0; h < 2; ++h) wv[i][h] = *reinterpret_cast<const i32x4*>(w + (wave + i * waves) * kRowUnit + 64 * h);
-    }
+        for (int h = 0; h < 2; ++h) wv[i][h] = *reinterpret_cast<const i32x4*>(w + (wave + i * waves) * kRowUnit + 64 * h);
+      }
+  };
+  ask();
   auto load = [&](int n, int v) {
     const T* const from = static_cast<const T*>(x) + (int64_t)n * k;
     const int at = v * VEC;
@@ -334,25 +341,31 @@ __global__ __launch_bounds__(1024) void i8_token_kernel(FwdArgs a, const void* _
   }
   __syncthreads();
   const int8_t* const mine = rows + min(lane & 15, a.m - 1) * row + 16 * (lane >> 4);
-  i32x4 acc = {0, 0, 0, 0};
-  auto multiply = [&](int b, const i32x4(&v)[2]) {
-#pragma unroll
-    for (int h = 0; h < 2; ++h) acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(v[h], *reinterpret_cast<const i32x4*>(mine + b * kRowUnit + 64 * h), acc, 0, 0, 0);
-  };
-#pragma unroll
-  for (int i = 0; i < kTokenAhead; ++i)
-    if (wave + i * waves < blocks) multiply(wave + i * waves, wv[i]);
-  for (int b = wave + kTokenAhead * waves; b < blocks; b += waves) {
-    i32x4 v[2];
-#pragma unroll
-    for (int h = 0; h < 2; ++h) v[h] = *reinterpret_cast<const i32x4*>(w + b * kRowUnit + 64 * h);
-    multiply(b, v);
-  }
   int* const parts = reinterpret_cast<int*>(rows + a.m * row);
+  for (;;) {
+    i32x4 acc = {0, 0, 0, 0};
+    auto multiply = [&](int b, const i32x4(&v)[2]) {
 #pragma unroll
-  for (int r = 0; r < 4; ++r) parts[wave * 256 + r * 64 + lane] = acc[r];
-  __syncthreads();
-  join_waves<E, 1>(a, parts, waves, 0, o0, scale);
+      for (int h = 0; h < 2; ++h) acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(v[h], *reinterpret_cast<const i32x4*>(mine + b * kRowUnit + 64 * h), acc, 0, 0, 0);
+    };
+#pragma unroll
+    for (int i = 0; i < kTokenAhead; ++i)
+      if (wave + i * waves < blocks) multiply(wave + i * waves, wv[i]);
+    for (int b = wave + kTokenAhead * waves; b < blocks; b += waves) {
+      i32x4 v[2];
+#pragma unroll
+      for (int h = 0; h < 2; ++h) v[h] = *reinterpret_cast<const i32x4*>(w + b * kRowUnit + 64 * h);
+      multiply(b, v);
+    }
+#pragma unroll
+    for (int r = 0; r < 4; ++r) parts[wave * 256 + r * 64 + lane] = acc[r];
+    __syncthreads();
+    join_waves<E, 1>(a, parts, waves, 0, o0, scale);
+    if ((int64_t)o0 + (int64_t)gridDim.x * 16 >= a.o) break;
+    o0 += gridDim.x * 16;
+    ask();
+    __syncthreads();
+  }
 }
 
 typedef const __attribute__((address_space(1))) uint32_t* GlobalPtr;
@@ -461,7 +474,7 @@ template <int DTYPE>
 int launch_forward(const i8_desc* d, const FwdArgs& a, const void* x, int8_t* codes, float* scales, hipStream_t stream) {
   const int m = d->p.m, o = d->p.num_output;
   if (x && d->token) {
-    hipLaunchKernelGGL(i8_token_kernel<DTYPE>, dim3((o + 15) / 16), dim3(64 * d->waves), (size_t)(m * d->row + d->waves * 1024), stream, a, x, codes, scales, d->p.k);
+    hipLaunchKernelGGL(i8_token_kernel<DTYPE>, dim3(std::min((o + 15) / 16, kMostBlocks)), dim3(64 * d->waves), (size_t)(m * d->row + d->waves * 1024), stream, a, x, codes, scales, d->p.k);
     return (int)hipGetLastError();
   }
   if (x) {
@@ -474,7 +487,7 @@ int launch_forward(const i8_desc* d, const FwdArgs& a, const void* x, int8_t* co
     hipLaunchKernelGGL((i8_tile_kernel<DTYPE, 2, 2, 4>), dim3((m + 127) / 128 * ((o + 127) / 128)), dim3(256), 0, stream, a);
   } else {
     const int mt = std::min(4, (m + 15) / 16);
-    const dim3 grid((o + 15) / 16, std::min((m + 16 * mt - 1) / (16 * mt), 65535)), block(64 * d->waves);
+    const dim3 grid((uint32_t)std::min<int64_t>((int64_t)((o + 15) / 16) * ((m + 16 * mt - 1) / (16 * mt)), kMostBlocks)), block(64 * d->waves);
     const size_t lds = (size_t)d->waves * mt * 1024;  // at most 64 KB
     switch (mt) {
       case 1: hipLaunchKernelGGL((i8_rows_kernel<DTYPE, 1>), grid, block, lds, stream, a); break;

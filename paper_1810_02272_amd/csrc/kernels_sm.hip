@@ -613,7 +613,7 @@ struct Team {
     __syncthreads();
   }
 
-  __device__ __forceinline__ uint64_t fixed(double w) const { return (uint64_t)ldexp(w, shift); }
+  __device__ __forceinline__ uint64_t fixed(double w) const { return (uint64_t)rint(ldexp(w, shift)); }
 
   template <bool WEIGHT>
   __device__ __forceinline__ void count_in(int b, double w) {
@@ -696,6 +696,11 @@ struct Team {
         sort(inside);
         int place = (int)target - above - 1;
         if (WEIGHT) place = sorted_place(inside, sum, target);
+        if (WEIGHT && sum >= target && sum > 0.) {  // (a rounding of the whole numbers: what is above the bin reaches it)
+          cut.value = key_value((uint32_t)(memory().sorted[0] >> 32));
+          cut.last = -1;
+          return true;
+        }
         const uint64_t entry = memory().sorted[max(0, min(place, inside - 1))];
         cut.value = key_value((uint32_t)(entry >> 32));
         cut.last = (int)(0xFFFFFFFFu - (uint32_t)entry);
@@ -1061,7 +1066,8 @@ __global__ __launch_bounds__(THREADS) void sm_row_kernel(SmArgs a) {
   typename Rows::Lds& lds = Rows::memory();
   const int tid = threadIdx.x;
   fill_roots(lds.root, tid);
-  for (int r = blockIdx.x; r < a.rows; r += gridDim.x) {
+  for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
+    const int r = (int)row;
     Rows t;
     t.tid = tid;
     t.lane = tid & 63;

@@ -337,3 +337,25 @@ def test_other_streams_and_graphs(case):
         if i == 0:
             assert all(torch.equal(a, b) for a, b in zip(first, outs))
         check_filter(case, layer, codes, scale, dz, dw, db)
+
+
+def test_more_outputs_and_rows_than_a_launch_has_workgroups():
+    """2^25 + 37 outputs of two inputs: their pattern repeats, and so do codes, scales and results."""
+    o, some = (1 << 25) + 37, 1000
+    x, w, bias, _ = make((1, 2, some, BF16, 1, 0))
+    times = -(-o // some)
+    small, large = Layer((1, 2, some, BF16, 1, 0)), lib.i8_desc_create(lib.I8Params(1, 2, o, BF16, 1, 0))
+    codes, scale = small.eight(w, pack=True)
+    want, *_ = small.forward(x, codes, scale, bias)
+    w_codes, w_scale = torch.empty((o, 128), device=DEV, dtype=torch.int8), torch.empty(o, device=DEV)
+    lib.i8_pack(large, w.repeat(times, 1)[:o].contiguous(), w_codes, w_scale)
+    for first in range(0, o, 4000 * some):
+        part = w_codes[first:first + 4000 * some]
+        assert torch.equal(part, codes.repeat(-(-part.shape[0] // some), 1)[:part.shape[0]])
+    assert torch.equal(w_scale, scale.repeat(times)[:o])
+    y = torch.empty((1, o), device=DEV, dtype=BF16)
+    row, s = torch.empty((1, 128), device=DEV, dtype=torch.int8), torch.empty(1, device=DEV)
+    for x_or_none in (x, None):
+        y.fill_(math.nan)
+        lib.i8_forward(large, x_or_none, w_codes, w_scale, bias.repeat(times)[:o].contiguous(), y, row, s)
+        assert torch.equal(y[0], want[0].repeat(times)[:o])

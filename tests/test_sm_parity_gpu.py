@@ -233,3 +233,13 @@ def test_no_rows_and_far_rows():
     far[0, 11], far[1, 4999] = 50.0, 50.0
     token, _ = run(far, full(2, 0.5))
     assert token.tolist() == [11, 4999]
+
+
+def test_more_rows_than_a_launch_has_workgroups():
+    rows, vocab = (1 << 20) + 5, 3
+    x = torch.randn((1000, vocab), device=DEV).repeat(-(-rows // 1000), 1)[:rows].contiguous()
+    u = torch.rand(1000, device=DEV).repeat(-(-rows // 1000))[:rows].contiguous()
+    for limits in ((None, None, None, None), (None, full(rows, 2, I32), full(rows, 0.9), None)):
+        token, logp = run(x, u, *limits)
+        check((token[:1000], logp[:1000]), x[:1000], u[:1000], *(None if t is None else t[:1000] for t in limits))
+        assert torch.equal(token, token[:1000].repeat(-(-rows // 1000))[:rows])
