@@ -68,6 +68,7 @@ constexpr int kChunkVecs = 4;   // vectors of a lane of the first launch, and of
 constexpr int kMostSegments = 256;
 constexpr int kUnits = 256;     // compute units
 constexpr int kAhead = 8;        // vectors that a thread asks for at a time
+constexpr float kFew = 256.f;    // logits that are ranked for little; where a few weigh most, a share of the row does not show them
 constexpr float kNear = 8.f;    // nats below the maximum that the list holds: weights from 3e-4 on
 
 // 2^(i / 64), computed to 60 digits and rounded.
@@ -896,7 +897,7 @@ struct Team {
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
       const int bin = kBins - 1 - (tid * PER + i), up_to = total - beyond;  // logits up to this bin's end
-      const bool enough = k > 0 ? up_to * share >= 1.4f * k + 8.f * share : weight_beyond <= 0.7 * left;
+      const bool enough = (k > 0 ? up_to * share >= 1.4f * k + 8.f * share : weight_beyond <= 0.7 * left) && up_to * share >= kFew;
       const bool short_of = k > 0 ? up_to * share < 0.7f * k - 8.f * share : weight_beyond > 1.4 * left;
       if (!short_of) low = bin;
       if (!enough && high == 0) {
