@@ -546,9 +546,9 @@ __global__ __launch_bounds__(TILE == 256 ? 512 : 256, 2) void i8_gradient_kernel
   typedef typename E::T T;
   constexpr int THREADS = TILE == 256 ? 512 : 256, HALF = THREADS / 2, WN = TILE == 64 ? 1 : 2, MT = TILE == 64 ? 1 : 4, NT = TILE / (16 * WN);
   constexpr int TERMS = DTYPE == MI355_BF16 ? 2 : 3, STEP = step_of(TILE), GROUPS = STEP / 8;
-  // pieces of 16 bytes: [term][group of 8 terms of the sum][place], and the same of the codes; two are left out after every 16, and four
-  // after a group, so that the lanes that write meet no bank twice
-  constexpr int GROUP = TILE + TILE / 8 + 4, TERM = GROUPS * GROUP, BUFFER = (TERMS + 1) * TERM;
+  // pieces of 16 bytes: [term][group of 8 terms of the sum][place], and the same of the codes; a lane's place is its number modulo 16 in every
+  // access, so that the lanes that go together, eight of two neighbouring sixteens, meet no bank twice
+  constexpr int GROUP = TILE + 16, TERM = GROUPS * GROUP, BUFFER = (TERMS + 1) * TERM;
   __shared__ __attribute__((aligned(16))) u32x4 lds[2][BUFFER];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), wm = wave / WN, wn = wave % WN;
   const int rows = FILTER ? a.o : a.n, depth = FILTER ? a.n : a.o;
@@ -560,20 +560,21 @@ __global__ __launch_bounds__(TILE == 256 ? 512 : 256, 2) void i8_gradient_kernel
 
   const bool of_dz = wave < HALF / 64;
   const int half = of_dz ? tid : tid - HALF, g = half / (TILE / 4), p = half % (TILE / 4);  // group, four rows or columns 4 p ..
-  // the place of a row or column: of 64 neighbours, 4 l + q stands at 16 q + l (and the pieces left out)
-  auto place_of = [](int i) { return (i >> 6) * 72 + (i & 3) * 18 + (i >> 2 & 15); };
+  // the place of a row or column: of 64 neighbours, 4 l + q stands at 16 q + l
+  auto place_of = [](int i) { return (i & ~63) + (i & 3) * 16 + (i >> 2 & 15); };
   const int col = (int)min((int64_t)i0 + 4 * p, a.row - 4);
   const int out = SLOW ? r0 + 4 * p : min(r0 + 4 * p, rows - 4);  // filter
   int places[4];
 #pragma unroll
-  for (int q = 0; q < 4; ++q) places[q] = !FILTER || !of_dz ? place_of(4 * p + q) : out + q >= r0 ? place_of(out + q - r0) : GROUP - 1;  // (another tile's: nobody reads it)
+  for (int q = 0; q < 4; ++q) places[q] = !FILTER || !of_dz ? place_of(4 * p + q) : out + q >= r0 ? place_of(out + q - r0) : TILE;  // (another tile's: nobody reads it)
   // the first term of a group's 8 in a step, and how many of them are not the group's
   auto first_of = [&](int step, int group, int& skip) {
     const int d0 = (first + step) * STEP + 8 * group, from = max(0, min(d0, depth - 8));
     skip = d0 - from;
     return from;
   };
-  constexpr int DATA_ROWS = TILE * GROUPS / HALF;  // data: 8 terms of rows half / GROUPS and on, HALF / GROUPS apart
+  constexpr int DATA_ROWS = TILE * GROUPS / HALF;  // data: 8 terms of rows data_row and on, HALF / GROUPS apart
+  const int data_group = (half >> 4) % GROUPS, data_row = (half & 15) + (half >> 4) / GROUPS * 16;
   constexpr int WORDS = DTYPE == MI355_F32 ? 4 : 2;
   typedef typename std::conditional<DTYPE == MI355_F32, u32x4, u32x2>::type Four;
   struct __attribute__((packed, aligned(sizeof(T)))) FourMem {
@@ -602,7 +603,7 @@ __global__ __launch_bounds__(TILE == 256 ? 512 : 256, 2) void i8_gradient_kernel
     for (int j = 0; j < 8; ++j) way.c[j] = *reinterpret_cast<const uint32_t*>(at + (int64_t)(SLOW ? min(j, depth - 1 - from) : j) * a.row);
   };
   auto load_dz = [&](Way& way, int step) {
-    const int from = first_of(step, FILTER ? g : half % GROUPS, way.skip);
+    const int from = first_of(step, FILTER ? g : data_group, way.skip);
 #pragma unroll
     for (int j = 0; j < 8; ++j) way.s[j] = a.scale[SLOW ? min(from + j, depth - 1) : from + j];
     if constexpr (FILTER) {
@@ -624,7 +625,7 @@ __global__ __launch_bounds__(TILE == 256 ? 512 : 256, 2) void i8_gradient_kernel
     } else {
 #pragma unroll
       for (int i = 0; i < DATA_ROWS; ++i) {
-        const T* const z = static_cast<const T*>(a.dz) + (int64_t)min(r0 + half / GROUPS + i * (HALF / GROUPS), rows - 1) * a.o + from;
+        const T* const z = static_cast<const T*>(a.dz) + (int64_t)min(r0 + data_row + i * (HALF / GROUPS), rows - 1) * a.o + from;
         if constexpr (SLOW) {
           float f[8];
 #pragma unroll
@@ -705,9 +706,9 @@ __global__ __launch_bounds__(TILE == 256 ? 512 : 256, 2) void i8_gradient_kernel
         for (int j = 0; j < 8; ++j) v[j] = E::get(way.raw.z[i][j / E::VEC], j % E::VEC);
         u32x4 w[TERMS];
         terms_of(way, v, w);
-        const int row = half / GROUPS + i * (HALF / GROUPS);
+        const int row = data_row + i * (HALF / GROUPS);
 #pragma unroll
-        for (int t = 0; t < TERMS; ++t) buffer[t * TERM + half % GROUPS * GROUP + row + 2 * (row >> 4)] = w[t];
+        for (int t = 0; t < TERMS; ++t) buffer[t * TERM + data_group * GROUP + row] = w[t];
       }
     }
   };
@@ -716,16 +717,16 @@ __global__ __launch_bounds__(TILE == 256 ? 512 : 256, 2) void i8_gradient_kernel
   auto products = [&](int step, auto&& between) {
 #pragma unroll
     for (int part = 0; part < STEP / 32; ++part) {
-      const u32x4* const A = lds[step & 1] + (4 * part + (lane >> 4)) * GROUP + wm * MT * 18 + (lane & 15);
-      const u32x4* const B = lds[step & 1] + TERMS * TERM + (4 * part + (lane >> 4)) * GROUP + wn * NT * 18 + (lane & 15);
+      const u32x4* const A = lds[step & 1] + (4 * part + (lane >> 4)) * GROUP + wm * MT * 16 + (lane & 15);
+      const u32x4* const B = lds[step & 1] + TERMS * TERM + (4 * part + (lane >> 4)) * GROUP + wn * NT * 16 + (lane & 15);
       bf16x8 w[NT];
 #pragma unroll
-      for (int u = 0; u < NT; ++u) w[u] = __builtin_bit_cast(bf16x8, B[u * 18]);
+      for (int u = 0; u < NT; ++u) w[u] = __builtin_bit_cast(bf16x8, B[u * 16]);
 #pragma unroll
       for (int t = 0; t < TERMS; ++t) {
         bf16x8 x[MT];
 #pragma unroll
-        for (int i = 0; i < MT; ++i) x[i] = __builtin_bit_cast(bf16x8, A[t * TERM + 18 * i]);
+        for (int i = 0; i < MT; ++i) x[i] = __builtin_bit_cast(bf16x8, A[t * TERM + 16 * i]);
 #pragma unroll
         for (int i = 0; i < MT; ++i)
 #pragma unroll
