@@ -559,7 +559,8 @@ __global__ __launch_bounds__(TILE == 256 ? 512 : 256, 2) void i8_gradient_kernel
   const bool sum_bias = FILTER && a.db && tn == 0;
 
   const bool of_dz = wave < HALF / 64;
-  const int half = of_dz ? tid : tid - HALF, g = half / (TILE / 4), p = half % (TILE / 4);  // group, four rows or columns 4 p ..
+  const int half = of_dz ? tid : tid - HALF, p = half % (TILE / 4);  // four rows or columns 4 p ..
+  const int g = TILE == 256 ? __builtin_amdgcn_readfirstlane(half / (TILE / 4)) : half / (TILE / 4);  // group: a wave's
   // the place of a row or column: of 64 neighbours, 4 l + q stands at 16 q + l
   auto place_of = [](int i) { return (i & ~63) + (i & 3) * 16 + (i >> 2 & 15); };
   const int col = (int)min((int64_t)i0 + 4 * p, a.row - 4);
