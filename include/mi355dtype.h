@@ -1,4 +1,4 @@
-/* Element types of the entry points that take more than one (mi355lp.h, mi355gn.h, mi355q4.h). */
+/* Element types of the entry points that take more than one (mi355lp.h, mi355gn.h, mi355q4.h, mi355sm.h, mi355i8.h). */
 #ifndef MI355DTYPE_H
 #define MI355DTYPE_H
 
