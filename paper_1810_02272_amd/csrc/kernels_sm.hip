@@ -153,11 +153,11 @@ struct Exponential {
 
   static constexpr double kWhole = 0x1.8p52;
 
-  // The weights of N logits, none of which is below `low`, added to a sum one after the other.  Their steps go side by side, so that a wave waits
+  // The weights of N logits, none of which is below `low`, as a power of 2 and a factor, and added to a sum one after the other.  Their steps go side by side, so that a wave waits
   // once for N entries.  Ten operations in 64 bits a logit take most of the time.  (One of them is the difference, which makes the largest one's weight
   // 1 exactly, and so sums of equal ones exact.)
-  template <int N>
-  __device__ __forceinline__ double add(double sum, const float (&x)[N]) const {
+  template <int N, class F>
+  __device__ __forceinline__ void terms(const float (&x)[N], F&& f) const {
     constexpr double L = 0.69314718055994530942 / kRootCount;
     double r[N], entry[N];
     uint32_t at[N];
@@ -175,9 +175,23 @@ struct Exponential {
       words[1] += at[i] << (20 - kRootBits);
       double p = fma(L * L * L * L / 24, r[i], L * L * L / 6);
       p = fma(fma(fma(p, r[i], L * L / 2), r[i], L), r[i], 1.);
-      sum = fma(__builtin_bit_cast(double, words), p, sum);
+      f(i, __builtin_bit_cast(double, words), p);
     }
+  }
+
+  template <int N>
+  __device__ __forceinline__ double add(double sum, const float (&x)[N]) const {
+    terms(x, [&](int, double power, double rest) { sum = fma(power, rest, sum); });
     return sum;
+  }
+
+  // Those of any logits.
+  template <int N>
+  __device__ __forceinline__ void of(const float (&x)[N], double (&w)[N]) const {
+    float held[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) held[i] = __builtin_amdgcn_fmed3f(x[i], low, FLT_MAX);
+    terms(held, [&](int i, double power, double rest) { w[i] = x[i] >= low ? power * rest : 0.; });
   }
 
   __device__ __forceinline__ double near(float x) const { return add<1>(0., {x}); }
@@ -373,14 +387,16 @@ struct Team {
   float m, scale;  // the maximum
   Exponential weight;
   Cut cut;
+  bool parts_ready;
   int part_end[WAVES];  // of the list's parts, one after the other
+  int listed;           // in this wave's part
 
   __device__ __forceinline__ u32x4 vec(int v) const {
     if constexpr (HELD) return v < nv ? memory().held[v] : lowest_vec<E>();
     return long_row_vec<E>(row, v, nv, n);
   }
 
-  __device__ __forceinline__ bool keeps(float x, int at) const { return x > cut.value || (x == cut.value && at <= cut.last); }
+  __device__ __forceinline__ bool keeps(float x, int at) const { return (x > cut.value) | ((x == cut.value) & (at <= cut.last)); }
 
   __device__ __forceinline__ float distance(float x) const { return fminf((m - x) * scale, FLT_MAX); }
 
@@ -392,37 +408,85 @@ struct Team {
     return place;
   }
 
-  // f(logit, index) for the elements of a vector, in order; compactly, two at a time.
-  template <class F>
+  // f(logit, index, weight) for the elements of a vector, in order, four at a time; without weights (0 in their place) where they are not asked for.
+  template <bool WEIGHT, class F>
   __device__ __forceinline__ void elements(u32x4 x, int v, F&& f) const {
     const Slot<E> at = slot_of<E>(v, n);
+    constexpr int WORDS = 16 / VEC;  // of four elements
 #pragma unroll 1
-    for (int w = 0; w < 4; ++w) {
-      const u32x4 first = {x[0], 0, 0, 0};
+    for (int h = 0; h < VEC; h += 4) {
+      float logit[4];
+      double w[4] = {0., 0., 0., 0.};
 #pragma unroll
-      for (int i = 0; i < VEC / 4; ++i) f(E::get(first, i), at.base + w * (VEC / 4) + i);
-      x = u32x4{x[1], x[2], x[3], x[0]};
+      for (int i = 0; i < 4; ++i) logit[i] = E::get(x, i);
+      if constexpr (WEIGHT) weight.of(logit, w);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) f(logit[i], at.base + h + i, w[i]);
+      if constexpr (WORDS == 2) x = u32x4{x[2], x[3], x[0], x[1]};
     }
   }
 
-  // The same for the whole row (LIST: what the list holds, with places for indices), by all threads.
-  template <bool LIST, class F>
-  __device__ __forceinline__ void each(int entries, F&& f) const {
-    if constexpr (LIST) {
-      for (int i = tid; i < entries; i += THREADS) f(memory().value[place_of(i)], i);
-    } else {
-      for (int v0 = 0; v0 < nv; v0 += kAhead * THREADS) {
-        u32x4 x[kAhead];
+  // The same for turns [j0, j1) of the team over the vectors [from, to), -inf beyond, with after(turn) behind each.
+  template <bool WEIGHT, class F, class After>
+  __device__ __forceinline__ void turns(int from, int to, int j0, int j1, F&& f, After&& after) const {
+    constexpr int AHEAD = !LIMITED ? 1 : HELD ? 4 : kAhead;
+    for (int j = j0; j < j1; j += AHEAD) {
+      u32x4 x[AHEAD];
 #pragma unroll
-        for (int j = 0; j < kAhead; ++j) x[j] = vec(v0 + j * THREADS + tid);
+      for (int i = 0; i < AHEAD; ++i) {
+        const int v = from + (j + i) * THREADS + tid;
+        x[i] = vec(v < to ? v : nv);
+      }
 #pragma unroll 1
-        for (int j = 0; j < min(kAhead, (nv - v0 + THREADS - 1) / THREADS); ++j) {
-          elements(x[0], v0 + j * THREADS + tid, f);
+      for (int i = 0; i < min(AHEAD, j1 - j); ++i) {
+        elements<WEIGHT>(x[0], from + (j + i) * THREADS + tid, f);
+        after(j + i);
 #pragma unroll
-          for (int i = 0; i + 1 < kAhead; ++i) x[i] = x[i + 1];
-        }
+        for (int o = 0; o + 1 < AHEAD; ++o) x[o] = x[o + 1];
       }
     }
+  }
+
+  // For the whole row (LIST: what the list holds, with places for indices, whose order is the same; each wave its part), by all threads; -inf in the place of
+  // what is not there.
+  template <bool LIST, bool WEIGHT, class F, class After>
+  __device__ __forceinline__ void each(F&& f, After&& after) const {
+    if constexpr (LIST) {
+      const int first = wave * SHARE, end = first + listed;
+#pragma unroll 1
+      for (int i0 = first + lane; i0 - lane < end; i0 += 256) {
+        float logit[4];
+        double w[4] = {0., 0., 0., 0.};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) logit[i] = i0 + i * 64 < end ? memory().value[i0 + i * 64] : -INFINITY;
+        if constexpr (WEIGHT) weight.of(logit, w);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) f(logit[i], i0 + i * 64, w[i]);
+      }
+    } else {
+      turns<WEIGHT>(0, nv, 0, (nv + THREADS - 1) / THREADS, f, after);
+    }
+  }
+  template <bool LIST, bool WEIGHT, class F>
+  __device__ __forceinline__ void each(F&& f) const {
+    each<LIST, WEIGHT>(f, [](int) {});
+  }
+
+  // Turns that are added up together, so that a sum over `length` of them is known in at most kGroups parts.
+  static __device__ __forceinline__ int group_of(int length) { return length <= 4 ? 1 : max(4, (length + kGroups - 1) / kGroups); }
+
+  // Sums of(...) over the turns of a group, each wave's into memory().part.
+  struct GroupSum {
+    double s = 0.;
+    int g = 0, in = 0;
+  };
+  __device__ __forceinline__ void group_after(GroupSum& sums, int per, bool last) const {
+    if (++sums.in < per && !last) return;
+    const double s = wave_sum(sums.s);
+    if (lane == 0) memory().part[sums.g][wave] = s;
+    sums.s = 0.;
+    sums.in = 0;
+    ++sums.g;
   }
 
   // The groups' sums stand in the lanes: the first group with which they pass `target`, or the last one of any weight; target becomes what is left of
@@ -452,27 +516,21 @@ struct Team {
     return chosen;
   }
 
-  // The index of the first logit of the vectors [from, to) with which the sum of of(logit, index) passes the target: u times the whole
-  // (FRACTION), or as given.
-  template <bool FRACTION, class W>
-  __device__ __forceinline__ int locate(int from, int to, double target, W&& of, double& whole) {
+  // The index of the first logit of the vectors [from, to) with which the sum of of(logit, index, weight) passes the target: u times the whole
+  // (FRACTION), or as given.  ready: the first round's parts stand in memory().part.
+  template <bool FRACTION, bool WEIGHT, class W>
+  __device__ __forceinline__ int locate(int from, int to, double target, W&& of, double& whole, bool ready = false) {
     int j0 = 0, j1 = (to - from + THREADS - 1) / THREADS, place = 0;
-    auto of_vec = [&](int v) {
-      double s = 0.;
-      if (v < to) elements(vec(v), v, [&](float x, int at) { s += of(x, at); });
-      return s;
-    };
     bool first = FRACTION;
     for (;;) {
-      const int length = j1 - j0, per = length <= 4 ? 1 : max(4, (length + kGroups - 1) / kGroups), groups = (length + per - 1) / per;
+      const int length = j1 - j0, per = group_of(length), groups = (length + per - 1) / per;
       __syncthreads();
-      for (int g = 0; g < groups; ++g) {
-        double s = 0.;
-        for (int j = j0 + g * per; j < min(j0 + (g + 1) * per, j1); ++j) s += of_vec(from + j * THREADS + tid);
-        s = wave_sum(s);
-        if (lane == 0) memory().part[g][wave] = s;
+      if (!ready) {
+        GroupSum sums;
+        turns<WEIGHT>(from, to, j0, j1, [&](float x, int at, double w) { sums.s += of(x, at, w); }, [&](int j) { group_after(sums, per, j + 1 == j1); });
+        __syncthreads();
       }
-      __syncthreads();
+      ready = false;
       double s = 0.;
       if (lane < groups)
         for (int w = 0; w < WAVES; ++w) s += memory().part[lane][w];
@@ -491,13 +549,16 @@ struct Team {
     }
     if (wave == place) {
       const int v = from + j0 * THREADS + tid;
-      const int at_lane = pick_lane(of_vec(v), target);
+      const u32x4 mine = vec(v < to ? v : nv);
+      double here = 0.;
+      elements<WEIGHT>(mine, v, [&](float x, int at, double w) { here += of(x, at, w); });
+      const int at_lane = pick_lane(here, target);
       if (lane == at_lane) {
         double sum = 0.;
         int index = 0;
         bool done = false;
-        elements(vec(v), v, [&](float x, int at) {
-          const double w = of(x, at);
+        elements<WEIGHT>(mine, v, [&](float x, int at, double weight_of) {
+          const double w = of(x, at, weight_of);
           sum += w;
           if (w > 0. && !done) {
             index = at;
@@ -618,18 +679,24 @@ struct Team {
 
   __device__ __forceinline__ uint64_t fixed(double w) const { return (uint64_t)rint(ldexp(w, shift)); }
 
+  // The same of a weight, up to 1: 2^shift of it are at most 2^50, which 2^52 rounds and shows as a whole number.
   template <bool WEIGHT>
   __device__ __forceinline__ void count_in(int b, double w) {
     atomicAdd(&memory().count[b], 1);
-    if (WEIGHT) atomicAdd((unsigned long long*)&memory().weights[b], (unsigned long long)fixed(w));
+    if (WEIGHT) {
+      const double placed = fma(w, __builtin_bit_cast(double, (uint64_t)(1023 + shift) << 52), 0x1p52);
+      atomicAdd((unsigned long long*)&memory().weights[b], (unsigned long long)(__builtin_bit_cast(uint64_t, placed) & 0xFFFFFFFFFFFFFull));
+    }
   }
 
-  // Moves the cut to where the counts (WEIGHT: the weights) of what it keeps reach the target, in descending order.  least: the least finite logit.
+  // Moves the cut to where the counts (WEIGHT: the weights) of what it keeps reach the target, in descending order.  LIST: none is below `least`.
   // [bracket.x, bracket.y]: distances between which it is likely to be (bracket.y = 0: not known).  False where they do not reach it.
-  template <bool WEIGHT, bool LIST>
-  __device__ __forceinline__ bool find_cut(double target, float least, int entries, float2 bracket) {
+  // PARTS: the sums of the weights from q on of what it then keeps are left for locate(), if parts_ready says so.
+  template <bool WEIGHT, bool LIST, bool PARTS = false>
+  __device__ __forceinline__ bool find_cut(double target, float least, float2 bracket, double q = 0.) {
     // histograms by distance: of the bracket, then near the maximum, then beyond; d of (from, to]
-    const float end = distance(least);
+    float end = LIST ? distance(least) : FLT_MAX;
+    parts_ready = false;
     float from = -1.f, to = -1.f, start = 0.f, per = 0.f;
     double above_sum = 0.;
     int bin = -1, count_carry = 0;
@@ -637,22 +704,22 @@ struct Team {
     for (int phase = bracket.y > 0.f ? 0 : 1; phase < 3 && bin < 0; ++phase) {
       from = phase == 0 ? bracket.x : phase == 1 ? -1.f : kNear;
       to = phase == 0 ? bracket.y : phase == 1 ? fminf(kNear, end) : end;
-      if (phase == 2 && end <= kNear) break;
+      if (phase == 2) {
+        if (!LIST) to = end = distance(least_finite());
+        if (end <= kNear) break;
+      }
       start = fmaxf(from, 0.f);
       per = to > start ? fminf(kBins / (to - start), FLT_MAX) : 0.f;
       clear_bins();
       double sum = 0.;
       int count = 0;
-      each<LIST>(entries, [&](float logit, int at) {
+      each<LIST, WEIGHT>([&](float logit, int at, double w) {
+        // (one branch: conditions side by side cost less)
         const float d = distance(logit);
-        if (!(d <= to) || !(logit > -INFINITY) || !keeps(logit, at)) return;
-        const double w = WEIGHT ? weight(logit) : 0.;
-        if (d > from) {
-          count_in<WEIGHT>(min((int)((d - start) * per), kBins - 1), w);
-        } else {
-          ++count;
-          sum += w;
-        }
+        const bool in = (d <= to) & (logit > -INFINITY) & keeps(logit, at), above = in & !(d > from);
+        count += above ? 1 : 0;
+        sum += above ? w : 0.;
+        if (in & (d > from)) count_in<WEIGHT>(min((int)((d - start) * per), kBins - 1), w);
       });
       above_sum = 0.;
       count_carry = 0;
@@ -673,19 +740,24 @@ struct Team {
       // what the bin holds: to be sorted if it is few; their range; the weight above them
       float most = -INFINITY, least_in = INFINITY;
       double sum = 0.;
-      each<LIST>(entries, [&](float logit, int at) {
-        if (!(logit > -INFINITY) || !keeps(logit, at)) return;
+      GroupSum sums;
+      const int length = (nv + THREADS - 1) / THREADS, per_group = group_of(length);
+      each<LIST, WEIGHT || PARTS>([&](float logit, int at, double w) {
+        const bool in = (logit > -INFINITY) & keeps(logit, at);
         int side;  // below 0: above the bin
         if (by_key) {
           const uint32_t key = order_key(logit);
-          side = key > high ? -1 : key < low ? 1 : (int)((high - key) >> bits) - bin;
+          side = (int)((high - min(max(key, low), high)) >> bits) - bin;
+          side = key > high ? -1 : key < low ? 1 : side;
         } else {
           const float d = distance(logit);
-          if (d <= from) return;  // these are in above_sum
-          side = d > to ? 1 : min((int)((d - start) * per), kBins - 1) - bin;
+          side = min((int)((fminf(d, to) - start) * per), kBins - 1) - bin;
+          side = d <= from ? -1 : d > to ? 1 : side;
         }
-        if (WEIGHT && side < 0) sum += weight(logit);
-        if (side == 0) {
+        const bool above = in & (side < 0);
+        if (WEIGHT) sum += above ? w : 0.;
+        if (PARTS) sums.s += above & (w >= q) ? w : 0.;
+        if (in & (side == 0)) {
           most = fmaxf(most, logit);
           least_in = fminf(least_in, logit);
           if (inside <= kSorted) {
@@ -693,8 +765,10 @@ struct Team {
             if (place < (uint32_t)kSorted) memory().sorted[place] = entry_of(logit, at);
           }
         }
+      }, [&](int j) {
+        if (PARTS) group_after(sums, per_group, j + 1 == length);
       });
-      if (WEIGHT) sum = team_sum<THREADS>(memory(), sum) + (by_key ? 0. : above_sum);
+      if (WEIGHT) sum = team_sum<THREADS>(memory(), sum);
       if (inside <= kSorted) {
         sort(inside);
         int place = (int)target - above - 1;
@@ -702,11 +776,17 @@ struct Team {
         if (WEIGHT && sum >= target && sum > 0.) {  // (a rounding of the whole numbers: what is above the bin reaches it)
           cut.value = key_value((uint32_t)(memory().sorted[0] >> 32));
           cut.last = -1;
+          parts_ready = PARTS;
           return true;
         }
-        const uint64_t entry = memory().sorted[max(0, min(place, inside - 1))];
+        place = max(0, min(place, inside - 1));
+        const uint64_t entry = memory().sorted[place];
         cut.value = key_value((uint32_t)(entry >> 32));
         cut.last = (int)(0xFFFFFFFFu - (uint32_t)entry);
+        if constexpr (PARTS) {
+          add_sorted(place + 1, per_group, q);
+          parts_ready = true;
+        }
         return true;
       }
       most = team_most<THREADS>(memory(), most);
@@ -715,7 +795,7 @@ struct Team {
         double order = target - above;
         if (WEIGHT) order = fmin(fmax(ceil((target - sum) / weight(most)), 1.), (double)inside);
         const Cut kept = cut;
-        cut.last = nth_equal<LIST>(most, (int)order, entries);
+        cut.last = nth_equal<LIST>(most, (int)order);
         cut.value = most;
         if (most == kept.value) cut.last = min(cut.last, kept.last);
         return true;
@@ -725,9 +805,9 @@ struct Team {
       low = order_key(least_in);
       bits = max(0, 32 - __builtin_clz(high - low) - 10);
       clear_bins();
-      each<LIST>(entries, [&](float logit, int at) {
+      each<LIST, WEIGHT>([&](float logit, int at, double w) {
         const uint32_t key = order_key(logit);
-        if (key <= high && key >= low && keeps(logit, at)) count_in<WEIGHT>((int)((high - key) >> bits), WEIGHT ? weight(logit) : 0.);
+        if ((key <= high) & (key >= low) & keeps(logit, at)) count_in<WEIGHT>((int)((high - key) >> bits), w);
       });
       uint64_t before = WEIGHT ? 0 : (uint64_t)above;
       int count_before = above;
@@ -738,30 +818,48 @@ struct Team {
     }
   }
 
+  // The weights from q on of the first of memory().sorted to the parts of their groups and waves, in their order.
+  __device__ __forceinline__ void add_sorted(int entries, int per, double q) {
+    double* const weights = reinterpret_cast<double*>(memory().weights);
+    for (int i = tid; i < entries; i += THREADS) {
+      const uint64_t entry = memory().sorted[i];
+      const double w = weight(key_value((uint32_t)(entry >> 32)));
+      const int v = (int)(0xFFFFFFFFu - (uint32_t)entry) / VEC, turn = v / THREADS;
+      weights[i] = w >= q ? w : 0.;
+      memory().count[i] = turn / per * WAVES + (v - turn * THREADS) / 64;
+    }
+    __syncthreads();
+    if (tid < kGroups * WAVES) {
+      double s = 0.;
+      for (int i = 0; i < entries; ++i) s += memory().count[i] == tid ? weights[i] : 0.;
+      if (s > 0.) memory().part[tid / WAVES][tid % WAVES] += s;
+    }
+    __syncthreads();
+  }
+
   // The index of the order-th (from 1) of the logits that equal x, all of which the cut keeps.
   template <bool LIST>
-  __device__ __forceinline__ int nth_equal(float x, int order, int entries) {
-    if constexpr (LIST) {  // places in turns of the team
-      int before = 0;
-      for (int i0 = 0; i0 < entries; i0 += THREADS) {
-        const bool mine = i0 + tid < entries && memory().value[place_of(i0 + tid)] == x;
-        const uint64_t mask = __ballot(mine);
-        __syncthreads();
-        if (lane == 0) memory().number[wave] = (int)__builtin_popcountll(mask);
-        __syncthreads();
-        int here = before + (int)__builtin_popcountll(mask & ((2ull << lane) - 1));
-#pragma unroll
-        for (int w = 0; w < WAVES; ++w) {
-          if (w < wave) here += memory().number[w];
-          before += memory().number[w];
+  __device__ __forceinline__ int nth_equal(float x, int order) {
+    if constexpr (LIST) {  // places, part by part
+      int mine = 0;
+      for (int i = lane; i - lane < listed; i += 64) mine += (int)__builtin_popcountll(__ballot(i < listed && memory().value[wave * SHARE + i] == x));
+      __syncthreads();
+      if (lane == 0) memory().number[wave] = mine;
+      __syncthreads();
+      for (int w = 0; w < wave; ++w) order -= memory().number[w];
+      if (order >= 1 && order <= mine) {
+        for (int i = lane; i - lane < listed; i += 64) {
+          const bool equal = i < listed && memory().value[wave * SHARE + i] == x;
+          const uint64_t mask = __ballot(equal);
+          if (equal && (int)__builtin_popcountll(mask & ((2ull << lane) - 1)) == order) memory().found = wave * SHARE + i;
+          order -= (int)__builtin_popcountll(mask);
         }
-        if (mine && here == order) memory().found = i0 + tid;
       }
       __syncthreads();
       return memory().found;
     } else {
       double whole;
-      return locate<false>(0, nv, order - 0.5, [&](float logit, int at) { return logit == x && keeps(logit, at) ? 1. : 0.; }, whole);
+      return locate<false, false>(0, nv, order - 0.5, [&](float logit, int at, double) { return (logit == x) & keeps(logit, at) ? 1. : 0.; }, whole);
     }
   }
 
@@ -801,38 +899,54 @@ struct Team {
     return memory().found;
   }
 
+  // Those of a wave's vectors from v on into its part of the list, which holds `mine` already; how many it then holds, more than SHARE if that is too many.
+  __device__ __forceinline__ int list_vec(u32x4 x, int v, float bound, int mine) const {
+    if (v + 64 >= nv) {  // where the row ends
+      if constexpr (HELD)
+        x = v + lane < nv ? x : lowest_vec<E>();
+      else
+        x = end_row_vec<E>(x, v + lane, nv, n);
+    }
+    uint32_t own = 0;
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) own |= E::get(x, i) >= bound ? 1u << i : 0u;
+    if (__ballot(own != 0) == 0) return mine;
+    const int count = __builtin_popcount(own), up_to = wave_scan(count), all = read_lane(up_to, 63);
+    if (mine + all > SHARE) return SHARE + 1;
+    int place = wave * SHARE + mine + up_to - count;
+    const int at = slot_of<E>(v + lane, n).base;
+#pragma unroll
+    for (int i = 0; i < VEC; ++i)
+      if (own >> i & 1) {
+        memory().value[place] = E::get(x, i);
+        memory().index[place] = at + i;
+        ++place;
+      }
+    return mine + all;
+  }
+
   // Logits from `bound` on into the list, in the order of their indices: each wave takes a part of the row and fills a part of the list.  The number of them, or -1 where a wave found more than its part holds.
   __device__ __forceinline__ int fill_list(float bound) {
     const int per = ((nv + WAVES - 1) / WAVES + 63) / 64 * 64, to = min(nv, (wave + 1) * per);
     int mine = 0;
     __syncthreads();
-    constexpr int AHEAD = HELD ? 4 : 16;
+    constexpr int AHEAD = HELD ? 4 : 8;
     for (int v0 = wave * per; v0 < to && mine <= SHARE; v0 += AHEAD * 64) {
       u32x4 x[AHEAD];
 #pragma unroll
-      for (int j = 0; j < AHEAD; ++j) x[j] = vec(v0 + j * 64 + lane < to ? v0 + j * 64 + lane : nv);
-#pragma unroll
       for (int j = 0; j < AHEAD; ++j) {
-        uint32_t mask = 0;
-#pragma unroll
-        for (int i = 0; i < VEC; ++i) mask |= E::get(x[j], i) >= bound ? 1u << i : 0u;
-        if (__ballot(mask != 0) == 0) continue;
-        const int count = __builtin_popcount(mask), up_to = wave_scan(count);
-        int place = mine + up_to - count;
-        const Slot<E> at = slot_of<E>(v0 + j * 64 + lane, n);
-#pragma unroll
-        for (int i = 0; i < VEC; ++i)
-          if (mask >> i & 1) {
-            if (place < SHARE) {
-              memory().value[wave * SHARE + place] = E::get(x[j], i);
-              memory().index[wave * SHARE + place] = at.base + i;
-            }
-            ++place;
-          }
-        mine += read_lane(up_to, 63);
+        const int v = v0 + j * 64 + lane;
+        if constexpr (HELD)
+          x[j] = memory().held[min(v, nv - 1)];
+        else
+          x[j] = begin_row_vec<E>(row, v, nv, n);
       }
+#pragma unroll
+      for (int j = 0; j < AHEAD; ++j)
+        if (v0 + j * 64 < to && mine <= SHARE) mine = list_vec(x[j], v0 + j * 64, bound, mine);
     }
     if (lane == 0) memory().number[wave] = mine;
+    listed = min(mine, SHARE);
     __syncthreads();
     int all = 0;
     bool over = false;
@@ -855,7 +969,7 @@ struct Team {
     const float share = (float)nv / (float)min(THREADS, (nv + stride - 1) / stride);
     clear_bins();
     if (v < nv)
-      elements(vec(v), v, [&](float logit, int) {
+      elements<false>(vec(v), v, [&](float logit, int, double) {
         if (logit > -INFINITY) atomicAdd(&memory().count[(int)fminf(distance(logit) * kPer, kBins - 1.f)], 1);
       });
     __syncthreads();
@@ -921,31 +1035,35 @@ struct Team {
 
   __device__ __forceinline__ float least_finite() const {
     float least = INFINITY;
-    each<false>(0, [&](float logit, int) { least = logit > -INFINITY ? fminf(least, logit) : least; });
+    each<false, false>([&](float logit, int, double) { least = logit > -INFINITY ? fminf(least, logit) : least; });
     return -team_most<THREADS>(memory(), -least);
   }
 
   // The sum of the weights that the cut keeps.
   template <bool LIST>
-  __device__ __forceinline__ double kept_sum(int entries) {
+  __device__ __forceinline__ double kept_sum() {
     double sum = 0.;
-    each<LIST>(entries, [&](float logit, int at) {
-      if (keeps(logit, at)) sum += weight(logit);
+    each<LIST, true>([&](float logit, int at, double w) {
+      sum += keeps(logit, at) ? w : 0.;
     });
     return team_sum<THREADS>(memory(), sum);
   }
 
   // The place in the list of the token.
-  __device__ __forceinline__ int locate_in_list(double u, double q, int entries, double& whole) {
-    // each thread a run of the list
-    const int per = (entries + THREADS - 1) / THREADS, from = min(tid * per, entries), to = min(from + per, entries);
-    auto of = [&](int i) {
-      const float x = memory().value[place_of(i)];
-      const double w = keeps(x, i) ? weight(x) : 0.;
-      return w >= q ? w : 0.;
-    };
+  __device__ __forceinline__ int locate_in_list(double u, double q, double& whole) {
+    // each lane a run of its wave's part
+    const int first = wave * SHARE, per = (listed + 63) / 64, from = first + min(lane * per, listed), to = first + min((lane + 1) * per, listed);
+    auto of = [&](int i, double w) { return (w >= q) & keeps(memory().value[i], i) ? w : 0.; };
     double mine = 0.;
-    for (int i = from; i < to; ++i) mine += of(i);
+    for (int i = from; i < to; i += 4) {
+      float x[4];
+      double w[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) x[j] = memory().value[min(i + j, to - 1)];
+      weight.of(x, w);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) mine += i + j < to ? of(i + j, w[j]) : 0.;
+    }
     const double sum = wave_sum(mine);
     __syncthreads();
     if (lane == 0) memory().part[0][wave] = sum;
@@ -960,7 +1078,7 @@ struct Team {
         double reached = 0.;
         int chosen = from;
         for (int i = from; i < to; ++i) {
-          const double w = of(i);
+          const double w = of(i, weight(memory().value[i]));
           reached += w;
           if (w > 0.) {
             chosen = i;
@@ -1162,40 +1280,42 @@ __global__ __launch_bounds__(THREADS) void sm_row_kernel(SmArgs a) {
         const float lowest = bound;
         if (by_count) {
           if (k < entries)
-            enough = t.template find_cut<false, true>((double)k, lowest, entries, make_float2(0.f, 0.f));
+            enough = t.template find_cut<false, true>((double)k, lowest, make_float2(0.f, 0.f));
           else
             enough = k == entries || complete;
         }
         if (enough && by_weight) {
-          const double kept = t.template kept_sum<true>(entries), target = fmax((by_count ? kept : all) * (double)p, 0.);
+          const double kept = t.template kept_sum<true>(), target = fmax((by_count ? kept : all) * (double)p, 0.);
           if (by_count && k > entries)
             enough = false;  // (the weight of k logits is not known)
           else if (target <= kept)
-            t.template find_cut<true, true>(target, lowest, entries, make_float2(0.f, 0.f));
+            t.template find_cut<true, true>(target, lowest, make_float2(0.f, 0.f));
           else
             enough = complete;
         }
         if (enough)
-          token = lds.index[t.place_of(t.locate_in_list((double)u, least_weight, entries, whole))];
+          token = lds.index[t.locate_in_list((double)u, least_weight, whole)];
         else
           t.cut = Cut{-INFINITY, INT_MAX};
       }
       if (token < 0) {
-        const float least = t.least_finite();
-        if (by_count) t.template find_cut<false, false>((double)k, least, 0, bracket);
-        if (by_weight) t.template find_cut<true, false>(fmax((by_count ? t.template kept_sum<false>(0) : all) * (double)p, 0.), least, 0, by_count ? make_float2(0.f, 0.f) : bracket);
-        token = t.template locate<true>(
-            0, t.nv, (double)u,
-            [&](float logit, int at) {
-              const double w = t.keeps(logit, at) ? t.weight(logit) : 0.;
-              return w >= least_weight ? w : 0.;
-            },
-            whole);
+        if (by_count) {
+          if (by_weight)
+            t.template find_cut<false, false>((double)k, 0.f, bracket);
+          else
+            t.template find_cut<false, false, true>((double)k, 0.f, bracket, least_weight);
+        }
+        if (by_weight)
+          t.template find_cut<true, false, true>(fmax((by_count ? t.template kept_sum<false>() : all) * (double)p, 0.), 0.f,
+                                                 by_count ? make_float2(0.f, 0.f) : bracket, least_weight);
+        token = t.template locate<true, true>(
+            0, t.nv, (double)u, [&](float logit, int at, double w) { return (w >= least_weight) & t.keeps(logit, at) ? w : 0.; }, whole,
+            (by_count || by_weight) && t.parts_ready);
       }
     } else {
-      auto plain = [&](float logit, int) { return t.weight(logit); };
+      auto plain = [](float, int, double w) { return w; };
       if constexpr (HELD) {
-        token = t.template locate<true>(0, t.nv, (double)u, plain, whole);
+        token = t.template locate<true, true>(0, t.nv, (double)u, plain, whole);
       } else {
         if (tid < kMostSegments) lds.segment[tid] = tid < a.segments ? part.sum * t.weight(part.most) : 0.;
         __syncthreads();
@@ -1223,7 +1343,7 @@ __global__ __launch_bounds__(THREADS) void sm_row_kernel(SmArgs a) {
         }
         const int per = a.chunks * 64 * kChunkVecs, from = (4 * lane + chosen) * per;
         double ignored;
-        token = t.template locate<false>(from, min(from + per, t.nv), target - before, plain, ignored);
+        token = t.template locate<false, true>(from, min(from + per, t.nv), target - before, plain, ignored);
       }
     }
     if (tid == 0) {
@@ -1275,7 +1395,7 @@ int sm_desc_create(sm_desc_t** out, const sm_params_t* pp) {
   d->held = chunks <= 4;
   int bits = 0;
   while (((int64_t)1 << bits) < p.vocab) ++bits;
-  d->shift = 61 - bits;
+  d->shift = std::min(50, 61 - bits);
   if (!d->held) d->ws_bytes = (size_t)p.rows * d->segments * (sizeof(Part) + kTops * sizeof(float));
   snprintf(d->names, sizeof(d->names), d->held ? "sample=sm_row" : "sample=sm_sums+sm_row");
   *out = d;
