@@ -45,7 +45,7 @@ constexpr int kUnits = 256;            // compute units
 constexpr int64_t kMaxElems = (int64_t)1 << 30;
 constexpr int kMostBlocks = 1 << 21;   // of up to 1024 threads: a launch has fewer than 2^32
 
-enum FwdForm { kRows, kTile128, kTile256 };
+enum FwdForm { kRows, kTile64By4, kTile64By2, kTile128By2, kTile128, kTile256 };  // by: groups of waves that share the sums
 
 // ---- rows to 8 bits ----
 
@@ -212,10 +212,10 @@ __device__ __forceinline__ float finish(int sum, float s, float t, float bias, i
 
 // What the waves of a workgroup have found for 16 MT rows and 16 outputs, [waves][MT * 256] in `parts`, into the results.
 template <class E, int MT>
-__device__ __forceinline__ void join_waves(const FwdArgs& a, const int* parts, int waves, int m0, int o0, const float* scale) {
+__device__ __forceinline__ void join_waves(const FwdArgs& a, const int* parts, int waves, int o0, const float* scale) {
   for (int i = threadIdx.x; i < MT * 256; i += blockDim.x) {
     // (consecutive threads: consecutive outputs of a row)
-    const int t = i >> 8, n = m0 + 16 * t + (i >> 4 & 15), out = o0 + (i & 15);
+    const int t = i >> 8, n = 16 * t + (i >> 4 & 15), out = o0 + (i & 15);
     if (n >= a.m || out >= a.o) continue;
     const int at = t * 256 + (i & 3) * 64 + ((i & 15) >> 2) * 16 + (i >> 4 & 15);
     int sum = 0;
@@ -226,22 +226,23 @@ __device__ __forceinline__ void join_waves(const FwdArgs& a, const int* parts, i
   }
 }
 
-// 16 MT rows by 16 outputs in a workgroup, whose waves take the inputs in turn, 128 at a time, and add up through shared memory: nothing is used by two
+// Up to 16 MT rows by 16 outputs in a workgroup, whose waves take the inputs in turn, 128 at a time, and add up through shared memory: nothing is used by two
 // waves, and operands come from memory as the instructions take them, 16 inputs of a row or an output a lane, those of AHEAD turns at a time.
-// Bound by the L2 caches, from which every workgroup reads all its rows' codes: 48 x 9216 -> 4096 20 us, 41 MB of memory and 150 of L2.
+// Bound by the L2 caches, from which every workgroup reads all its rows' codes: 32 x 4096 -> 4096 9 us (and 4 to bring the rows to 8 bits), 17 MB of memory
+// and 50 of L2.
 template <int DTYPE, int MT>
 __global__ __launch_bounds__(1024) void i8_rows_kernel(FwdArgs a) {
   typedef Elem<DTYPE> E;
   constexpr int AHEAD = MT == 1 ? 4 : 2;
   extern __shared__ int parts[];  // [waves][MT * 256]
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), waves = blockDim.x >> 6;
-  const int blocks = (int)(a.row / kRowUnit), tiles = (a.o + 15) / 16, groups = (a.m + 16 * MT - 1) / (16 * MT);
-  for (int64_t item = blockIdx.x; item < (int64_t)tiles * groups; item += gridDim.x) {
-    const int o0 = (int)(item % tiles) * 16, m0 = (int)(item / tiles) * 16 * MT;
+  const int blocks = (int)(a.row / kRowUnit), tiles = (a.o + 15) / 16;
+  for (int64_t item = blockIdx.x; item < tiles; item += gridDim.x) {
+    const int o0 = (int)item * 16;
     const int8_t* const w = a.w_codes + (int64_t)min(o0 + (lane & 15), a.o - 1) * a.row + 16 * (lane >> 4);
     const int8_t* x[MT];
 #pragma unroll
-    for (int t = 0; t < MT; ++t) x[t] = a.codes + (int64_t)min(m0 + 16 * t + (lane & 15), a.m - 1) * a.row + 16 * (lane >> 4);
+    for (int t = 0; t < MT; ++t) x[t] = a.codes + (int64_t)min(16 * t + (lane & 15), a.m - 1) * a.row + 16 * (lane >> 4);
     i32x4 acc[MT] = {};
     auto turn = [&](int b0, auto count) {
       constexpr int N = decltype(count)::value;
@@ -275,7 +276,7 @@ __global__ __launch_bounds__(1024) void i8_rows_kernel(FwdArgs a) {
 #pragma unroll
       for (int r = 0; r < 4; ++r) parts[(wave * MT + t) * 256 + r * 64 + lane] = acc[t][r];  // output 4 (lane / 16) + r, row lane % 16
     __syncthreads();
-    join_waves<E, MT>(a, parts, waves, m0, o0, a.scale);
+    join_waves<E, MT>(a, parts, waves, o0, a.scale);
   }
 }
 
@@ -362,7 +363,7 @@ __global__ __launch_bounds__(1024) void i8_token_kernel(FwdArgs a, const void* _
 #pragma unroll
     for (int r = 0; r < 4; ++r) parts[wave * 256 + r * 64 + lane] = acc[r];
     __syncthreads();
-    join_waves<E, 1>(a, parts, waves, 0, o0, scale);
+    join_waves<E, 1>(a, parts, waves, o0, scale);
     if ((int64_t)o0 + (int64_t)gridDim.x * 16 >= a.o) break;
     o0 += gridDim.x * 16;
     ask();
@@ -399,34 +400,39 @@ __device__ __forceinline__ int column_at(int p) { return (p & ~63) + 4 * (p & 15
 
 // WM x WN waves, each 64 rows of x by 16 NT outputs.  128 inputs at a time go straight into shared memory, one step ahead, as rows of 8 pieces of 16
 // bytes whose order is turned from row to row, so that neither side meets a bank twice.  Bound by the matrix units, 51 % busy: 8192 x 4096 -> 4096 130 us,
-// 2.1 POP/s.  (Three buffers for tiles of 128: the same there, 60 against 44 us for 3000 x 4096 -> 2000, as a compute unit then holds one workgroup.)
-template <int DTYPE, int WM, int WN, int NT>
-__global__ __launch_bounds__(WM * WN * 64, 2) void i8_tile_kernel(FwdArgs a) {
+// 2.1 POP/s; of few tiles by what a group of waves waits for in each step, 48 x 9216 -> 4096 18 us by four groups.  (Three or four buffers: no change where
+// there are few tiles, 60 against 44 us for 3000 x 4096 -> 2000, as a compute unit then holds one workgroup.)
+// DEPTH: groups of such waves in a workgroup that take the steps in turn, each with shared memory of its own, and add up in the end: where there are few tiles a
+// compute unit has more than a wave for each of its matrix units.
+template <int DTYPE, int WM, int WN, int NT, int DEPTH = 1>
+__global__ __launch_bounds__(WM * WN * DEPTH * 64, DEPTH > 1 ? 1 : 2) void i8_tile_kernel(FwdArgs a) {
   typedef Elem<DTYPE> E;
   constexpr int THREADS = WM * WN * 64, BM = WM * 64, BN = WN * NT * 16, ROWS = BM + BN, LOADS = ROWS * 8 / THREADS;
-  __shared__ __attribute__((aligned(16))) int8_t lds[2][ROWS * kRowUnit];
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), wm = wave / WN, wn = wave % WN;
+  __shared__ __attribute__((aligned(16))) int8_t lds[2 * DEPTH][ROWS * kRowUnit];
+  const int lane = threadIdx.x & 63, tid = (int)threadIdx.x % THREADS, wave = __builtin_amdgcn_readfirstlane(tid >> 6), wm = wave / WN, wn = wave % WN;
+  const int part = DEPTH > 1 ? __builtin_amdgcn_readfirstlane((int)threadIdx.x / THREADS) : 0;
   int tm, tn;
   tile_place((a.m + BM - 1) / BM, (a.o + BN - 1) / BN, tm, tn);
   const int m0 = tm * BM, o0 = tn * BN, steps = (int)(a.row / kRowUnit);
   const int8_t* from[LOADS];
 #pragma unroll
   for (int j = 0; j < LOADS; ++j) {
-    const int at = j * THREADS + (int)threadIdx.x, r = at >> 3, piece = (at & 7) ^ (r & 7);
+    const int at = j * THREADS + tid, r = at >> 3, piece = (at & 7) ^ (r & 7);
     from[j] = (r < BM ? a.codes + (int64_t)min(m0 + r, a.m - 1) * a.row : a.w_codes + (int64_t)min(o0 + column_at(r - BM), a.o - 1) * a.row) + 16 * piece;
   }
   auto load = [&](int step, int buffer) {
 #pragma unroll
     for (int j = 0; j < LOADS; ++j)
-      __builtin_amdgcn_global_load_lds((GlobalPtr)(from[j] + (int64_t)step * kRowUnit), (LdsPtr)&lds[buffer][(j * THREADS + wave * 64) * 16], 16, 0, 0);
+      __builtin_amdgcn_global_load_lds((GlobalPtr)(from[j] + (int64_t)step * kRowUnit), (LdsPtr)&lds[2 * part + buffer][(j * THREADS + wave * 64) * 16], 16, 0, 0);
   };
   i32x4 acc[4][NT] = {};
-  load(0, 0);
-  for (int s = 0; s < steps; ++s) {
+  if (part < steps) load(part, 0);
+  for (int s = part, buffer = 0; s - part < steps; s += DEPTH, buffer ^= 1) {
     __builtin_amdgcn_s_waitcnt(0x0F70);  // vmcnt(0): this wave's pieces are in shared memory
     __syncthreads();                     // everybody's are, and nobody reads the other buffer any more
-    if (s + 1 < steps) load(s + 1, (s + 1) & 1);
-    const int8_t* const base = lds[s & 1];
+    if (s + DEPTH < steps) load(s + DEPTH, buffer ^ 1);
+    if (DEPTH > 1 && s >= steps) continue;
+    const int8_t* const base = lds[2 * part + buffer];
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
       i32x4 x[4], w[NT];
@@ -441,6 +447,26 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void i8_tile_kernel(FwdArgs a) {
 #pragma unroll
         for (int u = 0; u < NT; ++u) acc[t][u] = __builtin_amdgcn_mfma_i32_16x16x64_i8(x[t], w[u], acc[t][u], 0, 0, 0);
     }
+  }
+  if constexpr (DEPTH > 1) {  // each group adds up some of the rows
+    static_assert(4 % DEPTH == 0 && WM * WN * 4 * NT * 1024 <= 2 * ROWS * kRowUnit, "");
+    i32x4* const sums = reinterpret_cast<i32x4*>(lds);
+    __syncthreads();
+#pragma unroll
+    for (int t = 0; t < 4; ++t)
+#pragma unroll
+      for (int u = 0; u < NT; ++u) sums[(((part * WM * WN + wave) * 4 + t) * NT + u) * 64 + lane] = acc[t][u];
+    __syncthreads();
+#pragma unroll
+    for (int t = 0; t < 4; ++t)
+      if (t / (4 / DEPTH) == part) {
+#pragma unroll
+        for (int u = 0; u < NT; ++u) {
+          acc[t][u] = sums[((wave * 4 + t) * NT + u) * 64 + lane];
+#pragma unroll
+          for (int p = 1; p < DEPTH; ++p) acc[t][u] += sums[(((p * WM * WN + wave) * 4 + t) * NT + u) * 64 + lane];
+        }
+      }
   }
 #pragma unroll
   for (int g = 0; g < NT / 4; ++g) {
@@ -458,7 +484,7 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void i8_tile_kernel(FwdArgs a) {
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
         const int n = m0 + wm * 64 + i * 16 + 4 * (lane >> 4) + r;
-        if (n >= a.m) continue;
+        if (n >= a.m || (DEPTH > 1 && i / (4 / DEPTH) != part)) continue;
         const float s = a.scale[n];
         float v[4];
 #pragma unroll
@@ -484,20 +510,25 @@ int launch_forward(const i8_desc* d, const FwdArgs& a, const void* x, int8_t* co
     const int e = launch_quantise<DTYPE>(x, codes, scales, m, d->p.k, d->row, stream);
     if (e) return e;
   }
+  const auto tiles = [&](int tile) { return dim3((uint32_t)((int64_t)((m + tile - 1) / tile) * ((o + tile - 1) / tile))); };
   if (d->fwd == kTile256) {
-    hipLaunchKernelGGL((i8_tile_kernel<DTYPE, 4, 2, 8>), dim3((m + 255) / 256 * ((o + 255) / 256)), dim3(512), 0, stream, a);
+    hipLaunchKernelGGL((i8_tile_kernel<DTYPE, 4, 2, 8>), tiles(256), dim3(512), 0, stream, a);
   } else if (d->fwd == kTile128) {
-    hipLaunchKernelGGL((i8_tile_kernel<DTYPE, 2, 2, 4>), dim3((m + 127) / 128 * ((o + 127) / 128)), dim3(256), 0, stream, a);
+    hipLaunchKernelGGL((i8_tile_kernel<DTYPE, 2, 2, 4>), tiles(128), dim3(256), 0, stream, a);
+  } else if (d->fwd == kTile128By2) {
+    hipLaunchKernelGGL((i8_tile_kernel<DTYPE, 2, 2, 4, 2>), tiles(128), dim3(512), 0, stream, a);
+  } else if (d->fwd == kTile64By4) {
+    hipLaunchKernelGGL((i8_tile_kernel<DTYPE, 1, 1, 4, 4>), tiles(64), dim3(256), 0, stream, a);
+  } else if (d->fwd == kTile64By2) {
+    hipLaunchKernelGGL((i8_tile_kernel<DTYPE, 1, 1, 4, 2>), tiles(64), dim3(128), 0, stream, a);
   } else {
-    const int mt = std::min(4, (m + 15) / 16);
-    const dim3 grid((uint32_t)std::min<int64_t>((int64_t)((o + 15) / 16) * ((m + 16 * mt - 1) / (16 * mt)), kMostBlocks)), block(64 * d->waves);
-    const size_t lds = (size_t)d->waves * mt * 1024;  // at most 64 KB
-    switch (mt) {
-      case 1: hipLaunchKernelGGL((i8_rows_kernel<DTYPE, 1>), grid, block, lds, stream, a); break;
-      case 2: hipLaunchKernelGGL((i8_rows_kernel<DTYPE, 2>), grid, block, lds, stream, a); break;
-      case 3: hipLaunchKernelGGL((i8_rows_kernel<DTYPE, 3>), grid, block, lds, stream, a); break;
-      default: hipLaunchKernelGGL((i8_rows_kernel<DTYPE, 4>), grid, block, lds, stream, a);
-    }
+    const int mt = m > 16 ? 2 : 1;
+    const dim3 grid((uint32_t)std::min((o + 15) / 16, kMostBlocks)), block(64 * d->waves);
+    const size_t lds = (size_t)d->waves * mt * 1024;  // at most 32 KB
+    if (mt == 1)
+      hipLaunchKernelGGL((i8_rows_kernel<DTYPE, 1>), grid, block, lds, stream, a);
+    else
+      hipLaunchKernelGGL((i8_rows_kernel<DTYPE, 2>), grid, block, lds, stream, a);
   }
   return (int)hipGetLastError();
 }
@@ -937,12 +968,27 @@ int clear(float* to, int64_t count, hipStream_t stream) {
 
 int64_t tiles_of(int64_t rows, int64_t columns, int tile) { return (rows + tile - 1) / tile * ((columns + tile - 1) / tile); }
 
+// The forward pass.  More rows than two tiles of 16 share weights better in tiles; where there are few tiles, small ones whose sums several groups of waves share:
+// a step of 128 inputs takes 0.7 us in a group, whatever its tile is, as every group waits for its own reads of shared memory (us, rows, 64 by 4, 64 by 2,
+// 128 by 2, 128, 256: 32 x 4096 -> 4096 13.4, 14.8; 64 rows 17.7, 15.5, 18.2; 64 x 4096 -> 16384 43.7, 20.2, 19.8; 300 rows -, -, 19.6, 25.0, 28.5; 512 rows
+// -, 26.1, 21.5, 26.1, 29.5; 700 rows -, -, 33.5, 26.4, 29.9; 1024 rows -, 46, 35.4, 28.9, 32.0, 60; 1300 rows -, -, 48.8, 47.9, 38.9, 61.7).  From then on a tile of 256
+// has a compute unit to itself, of 128 half of one, and a round of the former takes 1.5 times as long (2048 rows 45.6, with 256 64.8; 2500 rows 64.2, 65.9;
+// 4096 rows 85.3, 75.0; 6000 rows 128, 132).
+int32_t plan_forward(int64_t m, int64_t o) {
+  if (m <= 16 || (m <= 32 && o <= 96 * 64)) return kRows;
+  if (tiles_of(m, o, 64) <= kUnits) return kTile64By4;
+  if (tiles_of(m, o, 64) <= 2 * kUnits) return kTile64By2;
+  if (tiles_of(m, o, 128) <= kUnits) return kTile128By2;
+  const int64_t large = (tiles_of(m, o, 256) + kUnits - 1) / kUnits, medium = (tiles_of(m, o, 128) + 2 * kUnits - 1) / (2 * kUnits);  // rounds
+  return 3 * large < 2 * medium ? kTile256 : kTile128;
+}
+
 // The tile of a gradient, and the workgroups that share a sum.  A tile of 256 has a compute unit to itself, of 128 half of one; a round of the former takes
-// 1.4 times as long as one of the latter where dz is two terms, 1.7 to 1.9 where it is three, 2.3 for dx in fp32, whose kernel keeps 152 bytes a lane in
-// scratch memory (us, 256 and 128: dw of 8192 x 4096 -> 4096 bf16 483, 683, fp16 812, 961, fp32 1124, 1199; dx of the same 451, 630; 852, 903; 1232, 1083; dw of
-// 8192 x 4096 -> 2048 bf16, half a round, 456, 359).  Where a tile of 128 leaves half of the units without work, 64: dx of 100 x 999 <- 333 fp32 10.3, with
-// 128 17.4; of 512 x 333 <- 150 fp32 6.8, 12.5; dw of 2000 x 512 -> 512 bf16 17.0, 18.7, of 1999 x 1111 -> 777 fp16 40.4, 38.3; of 1000 x 2000 -> 1000 bf16, 128 tiles of
-// 128, 30.0, 30.7; of 64 x 4096 -> 4096 bf16 33.1, 21.8.
+// 1.4 times as long as one of the latter where dz is two terms, 1.6 to 2.0 where it is three, 2.5 for dx in fp32, whose kernel of 256 was built only to
+// measure it (us, 256 and 128: dw of 8192 x 4096 -> 4096 bf16 460, 674, fp16 738, 949, fp32 1146, 1145; dx of the same 434, 606; 759, 877; 1177, 944; dw of
+// 8192 x 4096 -> 2048 bf16, half a round, 436, 356).  Where a tile of 128 leaves half of the units without work, 64: dx of 100 x 999 <- 333 fp32 10.1, with
+// 128 16.4; of 512 x 333 <- 150 fp32 6.7, 11.8; dw of 2000 x 512 -> 512 bf16 17.0, 18.4, of 1999 x 1111 -> 777 fp16 40.3, 38.1; of 1000 x 2000 -> 1000 bf16, 128 tiles of
+// 128, 29.7, 30.6; of 64 x 4096 -> 4096 bf16 32.8, 22.0.
 void plan_gradient(int64_t rows, int64_t k, int64_t depth, int dtype, bool filter, int32_t& tile, int32_t& splits, int32_t& per) {
   const int64_t large = (tiles_of(rows, k, 256) + kUnits - 1) / kUnits, medium = (tiles_of(rows, k, 128) + 2 * kUnits - 1) / (2 * kUnits);  // rounds
   const double round = dtype == MI355_BF16 ? 1.43 : filter || dtype == MI355_F16 ? 1.85 : 2.3;
@@ -982,7 +1028,7 @@ int i8_desc_create(i8_desc_t** out, const i8_params_t* pp) {
   memset(d, 0, sizeof(*d));
   d->p = p;
   d->row = (K + kRowUnit - 1) / kRowUnit * kRowUnit;
-  d->fwd = M <= 64 || tiles_of(M, O, 128) < kUnits / 4 ? kRows : tiles_of(M, O, 256) >= kUnits / 2 ? kTile256 : kTile128;
+  d->fwd = plan_forward(M, O);
   d->waves = (int32_t)std::max<int64_t>(1, std::min<int64_t>(tiles_of(M, O, 16) > 4 * kUnits ? 4 : 16, d->row / kRowUnit));
   d->token = d->fwd == kRows && M <= kTokenRows && M * d->row <= kTokenBytes;
   plan_gradient(O, K, M, p.dtype, true, d->filter_tile, d->filter_splits, d->filter_per);
@@ -993,9 +1039,9 @@ int i8_desc_create(i8_desc_t** out, const i8_params_t* pp) {
   }
   char fwd[48];
   if (d->fwd == kRows)
-    snprintf(fwd, sizeof(fwd), "%si8_rows[m%d](W=%d)", d->token ? "i8_token/" : "", 16 * std::max(1, std::min(4, (p.m + 15) / 16)), d->waves);
+    snprintf(fwd, sizeof(fwd), "%si8_rows[m%d](W=%d)", d->token ? "i8_token/" : "", p.m > 16 ? 32 : 16, d->waves);
   else
-    snprintf(fwd, sizeof(fwd), "i8_tile[%d]", d->fwd == kTile256 ? 256 : 128);
+    snprintf(fwd, sizeof(fwd), "i8_tile[%s]", d->fwd == kTile256 ? "256" : d->fwd == kTile128 ? "128" : d->fwd == kTile128By2 ? "128,by2" : d->fwd == kTile64By2 ? "64,by2" : "64,by4");
   snprintf(d->names, sizeof(d->names), "fwd=%s;bwd_filter=i8_gradient[%d%s](S=%d);bwd_data=i8_gradient[%d%s](S=%d)", fwd, d->filter_tile, slow(O, M, true) ? ",slow" : "",
            d->filter_splits, d->data_tile, slow(M, O, false) ? ",slow" : "", d->data_splits);
   *out = d;
