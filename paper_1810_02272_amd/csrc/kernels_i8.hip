@@ -968,14 +968,15 @@ int clear(float* to, int64_t count, hipStream_t stream) {
 
 int64_t tiles_of(int64_t rows, int64_t columns, int tile) { return (rows + tile - 1) / tile * ((columns + tile - 1) / tile); }
 
-// The forward pass.  More rows than two tiles of 16 share weights better in tiles; where there are few tiles, small ones whose sums several groups of waves share:
+// The forward pass.  A few rows by themselves (16 x 4096 -> 8192 14.3 us, in tiles 14.8, -> 16384 21.7, 18.7; 32 x 4096 -> 4096 13.1, 14.8, -> 6000 18.3, 14.9); more of them
+// share weights better in tiles; where there are few tiles, small ones whose sums several groups of waves share:
 // a step of 128 inputs takes 0.7 us in a group, whatever its tile is, as every group waits for its own reads of shared memory (us, rows, 64 by 4, 64 by 2,
-// 128 by 2, 128, 256: 32 x 4096 -> 4096 13.4, 14.8; 64 rows 17.7, 15.5, 18.2; 64 x 4096 -> 16384 43.7, 20.2, 19.8; 300 rows -, -, 19.6, 25.0, 28.5; 512 rows
+// 128 by 2, 128, 256: 64 x 4096 -> 4096 17.7, 15.5, 18.2; 64 x 4096 -> 16384 43.7, 20.2, 19.8; 300 rows -, -, 19.6, 25.0, 28.5; 512 rows
 // -, 26.1, 21.5, 26.1, 29.5; 700 rows -, -, 33.5, 26.4, 29.9; 1024 rows -, 46, 35.4, 28.9, 32.0, 60; 1300 rows -, -, 48.8, 47.9, 38.9, 61.7).  From then on a tile of 256
 // has a compute unit to itself, of 128 half of one, and a round of the former takes 1.5 times as long (2048 rows 45.6, with 256 64.8; 2500 rows 64.2, 65.9;
 // 4096 rows 85.3, 75.0; 6000 rows 128, 132).
 int32_t plan_forward(int64_t m, int64_t o) {
-  if (m <= 16 || (m <= 32 && o <= 96 * 64)) return kRows;
+  if (m <= kTokenRows || (m <= 32 && (m > 16 ? 2 : 1) * o <= 8192)) return kRows;
   if (tiles_of(m, o, 64) <= kUnits) return kTile64By4;
   if (tiles_of(m, o, 64) <= 2 * kUnits) return kTile64By2;
   if (tiles_of(m, o, 128) <= kUnits) return kTile128By2;

@@ -31,7 +31,7 @@ CASES = [
     (3001, 140, 1, BF16, 1, 0), (8, 300, 8, BF16, 1, 0), (9, 257, 9, F16, 1, 0), (130, 129, 259, BF16, 1, 0), (131, 200, 387, F16, 1, 0), (133, 64, 130, F32, 1, 0),
     (150, 8200, 8, BF16, 0, 0), (140, 8200, 9, F16, 1, 0), (130, 8201, 520, F32, 0, 0), (520, 1025, 1999, BF16, 1, 0), (530, 1030, 2001, F16, 1, 0), (540, 1026, 2000, F32, 1, 0),
     (16, 1024, 2000, F16, 1, 0), (1001, 260, 3001, F32, 1, 1), (999, 130, 3005, F16, 1, 0), (1000, 385, 3002, BF16, 0, 0), (2300, 140, 2301, F32, 1, 0),
-    (2301, 129, 2300, BF16, 1, 1), (2299, 257, 2303, F16, 0, 0),
+    (2301, 129, 2300, BF16, 1, 1), (2299, 257, 2303, F16, 0, 0), (7, 300, 9001, BF16, 1, 0),
 ]
 
 
