@@ -751,7 +751,7 @@ struct Team {
           side = key > high ? -1 : key < low ? 1 : side;
         } else {
           const float d = distance(logit);
-          side = min((int)((fminf(d, to) - start) * per), kBins - 1) - bin;
+          side = min((int)((__builtin_amdgcn_fmed3f(d, start, to) - start) * per), kBins - 1) - bin;
           side = d <= from ? -1 : d > to ? 1 : side;
         }
         const bool above = in & (side < 0);

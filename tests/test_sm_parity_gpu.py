@@ -171,6 +171,21 @@ def test_limits_that_keep_few_many_and_most(vocab, spread, dtype):
         check(run(x, u, None, *limits), x, u, None, *limits)
 
 
+@pytest.mark.parametrize("dtype", [F32, F16, BF16])
+@pytest.mark.parametrize("vocab", [9000, 50001, 140000])
+def test_rows_in_order_and_in_steps(vocab, dtype):
+    """The largest logits lie together, at either end or in the middle, or a few hundred of them are equal, where the limits keep thousands."""
+    g = torch.Generator(device=DEV).manual_seed(vocab)
+    z = torch.randn(vocab, generator=g, device=DEV).mul_(0.7).sort()[0]
+    kinds = [z, z.flip(0), torch.roll(z, vocab // 2), (z[torch.randperm(vocab, generator=g, device=DEV)] * 64).round() / 64]
+    limits = [(0, 0.5, 0.0), (0, 0.97, 0.0), (0, 0.999999, 0.0), (0, 0.97, 0.2), (vocab // 3, 1.0, 0.0), (vocab // 2, 0.9, 0.0), (vocab // 2, 0.9, 0.3), (0, 1.0, 0.1), (700, 0.9, 0.0)]
+    rows = len(kinds) * len(limits)
+    x = torch.stack([kinds[i // len(limits)] for i in range(rows)]).to(dtype)
+    pick = lambda at, t=F32: torch.tensor([limits[i % len(limits)][at] for i in range(rows)], device=DEV, dtype=t)
+    args = torch.rand(rows, generator=g, device=DEV), full(rows, 0.8), pick(0, I32), pick(1), pick(2)
+    check(run(x, *args), x, *args)
+
+
 @pytest.mark.parametrize("vocab", [50, 5000, 100000])
 def test_logits_that_differ_in_their_last_bits(vocab):
     """fp32 logits closer to each other than their distance from the maximum can tell; and far apart."""
