@@ -139,16 +139,22 @@ __device__ __forceinline__ uint64_t wave_scan(uint64_t v) {
 }
 
 // exp of the difference to the row's or segment's largest logit: 2^((64 n + i + r) / 64), |r| <= 1/2.  The number 1.5 2^52 brings 64 n + i
-// into the lower word; the polynomial's next term is below 2^-44.5.  What is below 2^-995 counts as 0.
+// into the lower word; the polynomial's next term is below 2^-44.5.  What is below 2^-995 counts as 0: from 2^-1022 on the power would run out of its
+// exponent.
 struct Exponential {
   const double* root;  // in shared memory
   double top, c;
-  float low;
+  float low;    // the smallest number that is at most 690 nats below the largest logit: rounded up, as a step of that one may be hundreds of nats
+  bool steep;   // `low` itself weighs something beside 1, so that it cannot stand for what is below it
 
   __device__ __forceinline__ void set(float largest, float scale) {
     top = largest;
     c = (double)scale * (kRootCount * 1.44269504088896340736);
-    low = fmaxf(largest - 690.f / scale, -FLT_MAX);
+    const double border = (double)largest - (double)(690.f / scale);
+    const float near = (float)border;
+    const int bits = __builtin_bit_cast(int, near);
+    low = fmaxf((double)near < border ? __builtin_bit_cast(float, bits < 0 ? bits - 1 : bits + 1) : near, -FLT_MAX);
+    steep = !((largest - low) * scale >= 600.f);
   }
 
   static constexpr double kWhole = 0x1.8p52;
@@ -262,11 +268,29 @@ __device__ __forceinline__ float chunk_most(const u32x4 (&x)[kChunkVecs]) {
 template <class E>
 __device__ __forceinline__ double chunk_sum(const u32x4 (&x)[kChunkVecs], const Exponential& weight) {
   double s = 0.;
+  if (weight.steep) {  // (hardly ever: by a loop, so that the usual way keeps its registers)
+    u32x4 left[kChunkVecs];
+#pragma unroll
+    for (int j = 0; j < kChunkVecs; ++j) left[j] = x[j];
+#pragma unroll 1
+    for (int i = 0; i < kChunkVecs * E::VEC / 4; ++i) {
+      const float logit[4] = {E::get(left[0], 0), E::get(left[0], 1), E::get(left[0], 2), E::get(left[0], 3)};
+      double w[4];
+      weight.of(logit, w);
+      s += (w[0] + w[1]) + (w[2] + w[3]);
+#pragma unroll
+      for (int j = 0; j < kChunkVecs; ++j) {
+        const u32x4 next = left[min(j + 1, kChunkVecs - 1)];
+        left[j] = E::VEC == 4 ? next : u32x4{left[j][2], left[j][3], next[0], next[1]};
+      }
+    }
+    return s;
+  }
 #pragma unroll
   for (int j = 0; j < kChunkVecs; ++j) {
 #pragma unroll
     for (int h = 0; h < E::VEC; h += 4) {
-      float logit[4];  // (2^-995 in the place of less: nothing beside 1)
+      float logit[4];  // (`low`, e^-600 or less, in the place of less: nothing beside 1)
 #pragma unroll
       for (int i = 0; i < 4; ++i) logit[i] = __builtin_amdgcn_fmed3f(E::get(x[j], h + i), weight.low, FLT_MAX);
       s = weight.add(s, logit);

@@ -200,6 +200,48 @@ def test_logits_that_differ_in_their_last_bits(vocab):
         check(run(x, u, *limits), x, u, *limits)
 
 
+def far_above(rows, vocab, dtype, seed):
+    """Rows whose logits lie 0 to 40 of the type's steps below a maximum that several share, the rest far below it or banned."""
+    g = torch.Generator(device=DEV).manual_seed(seed)
+    top = torch.tensor([3.0, 10.0, 20.0, 100.0, 600.0, 1000.0, 0.0, -7.0, -0.001, -2000.0], device=DEV)[torch.arange(rows, device=DEV) % 10][:, None]
+    steps = torch.randint(0, 41, (rows, vocab), generator=g, device=DEV) * torch.randint(0, 2, (rows, vocab), generator=g, device=DEV)
+    size = torch.where(top == 0, 2.0 ** -149, torch.exp2(torch.floor(torch.log2(top.abs())))) * torch.finfo(dtype).eps
+    x = top.double() - steps * size.double()
+    kind = torch.rand((rows, vocab), generator=g, device=DEV)
+    x = torch.where(kind < 0.5, top.double() - 1.0 - 50.0 * torch.rand((rows, vocab), generator=g, device=DEV), x)
+    x = torch.where(kind < 0.2, -math.inf, x)
+    few = torch.arange(rows, device=DEV) % 3 == 0  # the maximum once, near the end
+    x = torch.where(few[:, None] & (x >= top), -math.inf, x)
+    x[:, vocab - 2 if vocab > 2 else 0] = top[:, 0].double()
+    return x.to(dtype), torch.rand(rows, generator=g, device=DEV)
+
+
+@pytest.mark.parametrize("dtype", [F32, F16, BF16])
+@pytest.mark.parametrize("vocab", [7, 300, 5000, 9000, 128256])
+def test_scales_at_which_a_step_of_the_largest_logit_is_many_nats(vocab, dtype):
+    """A tiny temperature: the numbers next to the largest logit weigh something, nothing, or less than 64 bits hold; with and without limits."""
+    scales = [1e6, 2e6, 2.0 ** 24, 2.0 ** 27, 1e8, 2.0 ** 28, 1e9, 2.0 ** 30, 1e10, 2.0 ** 35, 2.0 ** 40, 2.0 ** 60, 1e3, 1e4, 1e5, 3e5]
+    rows = 10 * len(scales)
+    x, u = far_above(rows, vocab, dtype, seed=vocab)
+    scale = torch.tensor(scales, device=DEV).repeat_interleave(10)
+    k, p, q = full(rows, max(2, vocab // 9), I32), full(rows, 0.83), full(rows, 0.01)
+    for limits in ((None, None, None), (None, None, q), (None, p, None), (k, None, None), (k, p, None), (k, p, q)):
+        check(run(x, u, scale, *limits), x, u, scale, *limits)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("vocab", [6, 700, 9000, 70000])
+def test_rows_of_the_lowest_number(vocab, dtype):
+    """Nothing is below the largest logit but what is banned, which weighs nothing all the same."""
+    rows = 8
+    x = torch.full((rows, vocab), torch.finfo(dtype).min, device=DEV, dtype=dtype)
+    x[:, ::3] = -math.inf
+    u = torch.linspace(0.03, 0.97, rows, device=DEV)
+    for scale in (1.0, 2.0 ** -60, 2.0 ** 60):
+        for limits in ((None, None, None), (full(rows, 3, I32), full(rows, 0.9), None), (None, full(rows, 0.6), full(rows, 0.2))):
+            check(run(x, u, full(rows, scale), *limits), x, u, full(rows, scale), *limits)
+
+
 def test_every_token_comes_as_often_as_it_should():
     vocab, rows = 10, 4096
     row = torch.randn(vocab, device=DEV)
