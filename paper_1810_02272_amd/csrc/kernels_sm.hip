@@ -144,17 +144,22 @@ __device__ __forceinline__ uint64_t wave_scan(uint64_t v) {
 struct Exponential {
   const double* root;  // in shared memory
   double top, c;
-  float low;    // the smallest number that is at most 690 nats below the largest logit: rounded up, as a step of that one may be hundreds of nats
+  float low;    // the smallest number that is at most 690 nats below the largest logit; rounded up where a step of that one may be many nats
   bool steep;   // `low` itself weighs something beside 1, so that it cannot stand for what is below it
 
   __device__ __forceinline__ void set(float largest, float scale) {
     top = largest;
     c = (double)scale * (kRootCount * 1.44269504088896340736);
-    const double border = (double)largest - (double)(690.f / scale);
-    const float near = (float)border;
-    const int bits = __builtin_bit_cast(int, near);
-    low = fmaxf((double)near < border ? __builtin_bit_cast(float, bits < 0 ? bits - 1 : bits + 1) : near, -FLT_MAX);
-    steep = !((largest - low) * scale >= 600.f);
+    const float span = 690.f * __builtin_amdgcn_rcpf(scale);
+    low = largest - span;  // within a sixteenth of a nat, where neither number has more than 2^20 of them
+    steep = fabsf(largest) * scale >= 0x1p20f;
+    if (steep) {
+      const double border = (double)largest - (double)span;
+      const float near = (float)border;
+      const int bits = __builtin_bit_cast(int, near);
+      low = fmaxf((double)near < border ? __builtin_bit_cast(float, bits < 0 ? bits - 1 : bits + 1) : near, -FLT_MAX);
+      steep = !((largest - low) * scale >= 600.f);
+    }
   }
 
   static constexpr double kWhole = 0x1.8p52;
