@@ -204,9 +204,11 @@ struct FwdArgs {
   int32_t m, o, relu;
 };
 
-// One result: the scales one after the other, as their product may leave fp32 where the result does not.
+// One result: the scales one after the other, as their product may leave fp32 where the result does not; so would the sum's, below 2^31, with
+// a scale of 2^97 and more, which therefore comes last.  (Scales are 2^-126 at least: nothing falls below fp32's normal numbers on the way.)
 __device__ __forceinline__ float finish(int sum, float s, float t, float bias, int relu) {
-  const float z = fmaf((float)sum * s, t, bias);
+  const bool large = s >= 0x1p96f;
+  const float z = fmaf((float)sum * (large ? t : s), large ? s : t, bias);
   return relu ? (z > 0.f ? z : 0.f) : z;
 }
 

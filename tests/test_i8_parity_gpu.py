@@ -251,6 +251,30 @@ def test_not_a_number_and_infinity_stay_in_their_rows(dtype, m):
     assert torch.isnan(dx[4]).all() and torch.isfinite(dx[torch.arange(m, device=DEV) != 4]).all()
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("m,k,o", [(3, 4096, 40), (12, 900, 70), (30, 4096, 300), (300, 1000, 500), (1200, 500, 900)])
+def test_forward_of_the_largest_and_smallest_rows(m, k, o, dtype):
+    """Rows up to the type's largest number under small weights, and the other way round: the sum of the codes' products with one scale leaves fp32, or is
+    small, where the result is neither."""
+    x, w, bias, _ = make((m, k, o, dtype, 1, 0))
+    size = torch.tensor([1e38, 1e37, 1e34, 1e30, 1e20, 1.0, 1e-20, 1e-30, 1e-35], device=DEV, dtype=torch.float64)
+    unit = lambda t: t.double() / t.double().abs().amax(1, keepdim=True)
+    layer = Layer((m, k, o, dtype, 1, 0))
+    rows = size[4 * torch.arange(m, device=DEV) % 9][:, None]
+    for weights in (1e-38, 1e-30, 1e-3, 1.0, 1e30, 1e38):
+        xs, ws = (unit(x) * rows).to(dtype), (unit(w) * weights).to(dtype)
+        w_codes, w_scale = layer.eight(ws, pack=True)
+        y, codes, scale = layer.forward(xs, w_codes, w_scale, bias)
+        want = tokens.i8_forward(codes[:, :k], scale, w_codes[:, :k], w_scale, bias, 0)
+        product = tokens.i8_forward(codes[:, :k], scale, w_codes[:, :k], w_scale, None, 0).abs()
+        fits = product < torch.finfo(dtype).max * 0.9
+        assert bool(fits.any())
+        # as check_forward
+        tol = product * 2.01 * U + want.abs() * 1.01 * U + half_step(want, dtype) * 1.01
+        within(torch.where(fits, y.double(), 0.0), torch.where(fits, want, 0.0), tol)
+        assert not bool(torch.isfinite(y[product > torch.finfo(dtype).max * 1.1]).any())
+
+
 @pytest.mark.parametrize("dtype", [F32, F16, BF16])
 def test_gradients_take_all_bits_of_dz(dtype):
     """Two rows whose dz differ in the last bit, under codes 1 and -1 and a scale of 255 / 128: what is left comes out exactly."""
