@@ -15,8 +15,8 @@
  * A logit of -inf is a banned token and is never drawn.  A row of nothing but -inf has nothing to draw: token -1, logp -inf.  A row that holds a NaN or
  * +inf, or whose scale is not in [2^-60, 2^60], u not in [0, 1], p or q NaN, has token -1 and logp NaN.  (A token of -1 counts for
  * nothing in mi355lp.h.)
- * Weights and their sums are held in 64 bits: a token differs from the formula's only where u or p meets a border within some 2^-45 of
- * the whole.  A weight below some 2^-995 counts as 0.
+ * Weights and their sums are held in 64 bits: a token differs from the formula's only where u or p meets a border within some 2^-44 of
+ * the whole (vocab 2^-62 of it in rows of more than 2^18 logits), or q a weight within 2^-44 of it.  A weight below some 2^-995 counts as 0.
  *
  * Types and layouts: logits in the descriptor's type (fp32, fp16, bf16), rows `stride` elements apart (stride >= vocab where there is more than one
  * row) and dense inside, on the element's own alignment; dense [rows]: u, scale, top_p, min_p, logp fp32, top_k, token int32.  scale, top_k, top_p

@@ -719,7 +719,8 @@ struct Team {
   }
 
   // Moves the cut to where the counts (WEIGHT: the weights) of what it keeps reach the target, in descending order.  LIST: none is below `least`.
-  // [bracket.x, bracket.y]: distances between which it is likely to be (bracket.y = 0: not known).  False where they do not reach it.
+  // [bracket.x, bracket.y]: distances between which it is likely to be (bracket.y = 0: not known).  False where the counts do not reach it, or whole numbers
+  // of weights pick a bin that the weights' own sums do not end in: then the cut is as it was, and halve() finds it.
   // PARTS: the sums of the weights from q on of what it then keeps are left for locate(), if parts_ready says so.
   template <bool WEIGHT, bool LIST, bool PARTS = false>
   __device__ __forceinline__ bool find_cut(double target, float least, float2 bracket, double q = 0.) {
@@ -797,16 +798,16 @@ struct Team {
       }, [&](int j) {
         if (PARTS) group_after(sums, per_group, j + 1 == length);
       });
-      if (WEIGHT) sum = team_sum<THREADS>(memory(), sum);
+      if constexpr (WEIGHT) {
+        sum = team_sum<THREADS>(memory(), sum);
+        if (sum >= target && sum > 0.) return false;  // what is above the bin reaches it
+      }
       if (inside <= kSorted) {
         sort(inside);
         int place = (int)target - above - 1;
-        if (WEIGHT) place = sorted_place(inside, sum, target);
-        if (WEIGHT && sum >= target && sum > 0.) {  // (a rounding of the whole numbers: what is above the bin reaches it)
-          cut.value = key_value((uint32_t)(memory().sorted[0] >> 32));
-          cut.last = -1;
-          parts_ready = PARTS;
-          return true;
+        if constexpr (WEIGHT) {
+          place = sorted_place(inside, sum, target);
+          if (place < 0) return false;
         }
         place = max(0, min(place, inside - 1));
         const uint64_t entry = memory().sorted[place];
@@ -822,7 +823,10 @@ struct Team {
       least_in = -team_most<THREADS>(memory(), -least_in);
       if (most == least_in) {  // equal ones: by their indices
         double order = target - above;
-        if (WEIGHT) order = fmin(fmax(ceil((target - sum) / weight(most)), 1.), (double)inside);
+        if constexpr (WEIGHT) {
+          order = fmax(ceil((target - sum) / weight(most)), 1.);
+          if (order > (double)inside) return false;
+        }
         const Cut kept = cut;
         cut.last = nth_equal<LIST>(most, (int)order);
         cut.value = most;
@@ -845,6 +849,39 @@ struct Team {
       above = memory().before;
       inside = memory().inside;
     }
+  }
+
+  // Moves the cut to where the weights of what it keeps reach the target, in descending order, by the sums of the weights alone: a pass for each bit of
+  // the logits' order.  For the rows where find_cut's whole numbers are not enough: equal logits are rounded alike, and those of a row of millions that
+  // weigh little each may all be rounded to nothing.  (Hardly ever: 1.2 ms for a row of 128256, 13 for a million.)
+  template <bool LIST>
+  __device__ __forceinline__ void halve(double target) {
+    uint32_t high = order_key(m), low = order_key(-FLT_MAX);  // the sum from `low` on reaches the target, the one above `high` does not
+    double above = 0.;                                        // the latter
+    while (low < high) {
+      const uint32_t middle = high - (high - low) / 2;
+      double sum = 0.;
+      each<LIST, false>([&](float logit, int at, double) {
+        const uint32_t key = order_key(logit);
+        if ((key >= middle) & (key <= high) & keeps(logit, at)) sum += weight(logit);
+      });
+      sum = above + team_sum<THREADS>(memory(), sum);
+      if (sum >= target) {
+        low = middle;
+      } else {
+        above = sum;
+        high = middle - 1;
+      }
+    }
+    const float value = key_value(high);
+    int count = 0;
+    each<LIST, false>([&](float logit, int at, double) { count += (logit == value) & keeps(logit, at) ? 1 : 0; });
+    const double equal = team_sum<THREADS>(memory(), (double)count);
+    const Cut kept = cut;
+    int last = INT_MAX;
+    if (equal > 0.) last = nth_equal<LIST>(value, (int)fmin(fmax(ceil((target - above) / weight(value)), 1.), equal));
+    cut = Cut{value, value == kept.value ? min(last, kept.last) : last};
+    parts_ready = false;
   }
 
   // The weights from q on of the first of memory().sorted to the parts of their groups and waves, in their order.
@@ -892,12 +929,12 @@ struct Team {
     }
   }
 
-  // The first place of memory().sorted with which the weights reach the target, counted from `sum` on.
+  // The first place of memory().sorted with which the weights reach the target, counted from `sum` on; -1 where there is none.
   __device__ __forceinline__ int sorted_place(int entries, double sum, double target) {
     if (entries <= 64) {
       const double w = lane < entries ? weight(key_value((uint32_t)(memory().sorted[lane] >> 32))) : 0.;
       const uint64_t reached = __ballot(lane < entries && sum + wave_scan(w) >= target);
-      return reached ? __builtin_ctzll(reached) : entries - 1;
+      return reached ? __builtin_ctzll(reached) : -1;
     }
     constexpr int PER = kSorted / THREADS;
     double w[PER], mine = 0.;
@@ -908,7 +945,7 @@ struct Team {
       mine += w[i];
     }
     const double to = wave_scan(mine);
-    if (tid == 0) memory().found = entries - 1;
+    if (tid == 0) memory().found = INT_MAX;
     if (lane == 63) memory().sum[wave] = to;
     __syncthreads();
 #pragma unroll
@@ -925,7 +962,7 @@ struct Team {
       }
     }
     __syncthreads();
-    return memory().found;
+    return memory().found == INT_MAX ? -1 : memory().found;
   }
 
   // Those of a wave's vectors from v on into its part of the list, which holds `mine` already; how many it then holds, more than SHARE if that is too many.
@@ -1317,10 +1354,10 @@ __global__ __launch_bounds__(THREADS) void sm_row_kernel(SmArgs a) {
           const double kept = t.template kept_sum<true>(), target = fmax((by_count ? kept : all) * (double)p, 0.);
           if (by_count && k > entries)
             enough = false;  // (the weight of k logits is not known)
-          else if (target <= kept)
-            t.template find_cut<true, true>(target, lowest, make_float2(0.f, 0.f));
-          else
+          else if (target > kept)
             enough = complete;
+          else if (!t.template find_cut<true, true>(target, lowest, make_float2(0.f, 0.f)))
+            t.template halve<true>(target);
         }
         if (enough)
           token = lds.index[t.locate_in_list((double)u, least_weight, whole)];
@@ -1334,9 +1371,10 @@ __global__ __launch_bounds__(THREADS) void sm_row_kernel(SmArgs a) {
           else
             t.template find_cut<false, false, true>((double)k, 0.f, bracket, least_weight);
         }
-        if (by_weight)
-          t.template find_cut<true, false, true>(fmax((by_count ? t.template kept_sum<false>() : all) * (double)p, 0.), 0.f,
-                                                 by_count ? make_float2(0.f, 0.f) : bracket, least_weight);
+        if (by_weight) {
+          const double target = fmax((by_count ? t.template kept_sum<false>() : all) * (double)p, 0.);
+          if (!t.template find_cut<true, false, true>(target, 0.f, by_count ? make_float2(0.f, 0.f) : bracket, least_weight)) t.template halve<false>(target);
+        }
         token = t.template locate<true, true>(
             0, t.nv, (double)u, [&](float logit, int at, double w) { return (w >= least_weight) & t.keeps(logit, at) ? w : 0.; }, whole,
             (by_count || by_weight) && t.parts_ready);

@@ -242,6 +242,55 @@ def test_rows_of_the_lowest_number(vocab, dtype):
             check(run(x, u, full(rows, scale), *limits), x, u, full(rows, scale), *limits)
 
 
+def tail(n, x, scale, p, k):
+    """One token of weight 1 and n[0], n[1] of logits x[0] > x[1]: how many of the latter top-p keeps of the first k, as a number whose next whole one it is."""
+    w = [math.exp(scale * v) for v in x]
+    n = [min(n[0], k - 1), min(n[1], max(0, k - 1 - n[0]))]
+    left = (1.0 - p) * (1.0 + n[0] * w[0] + n[1] * w[1])  # what may be left out (1 - p is exact)
+    first = n[1] - left / w[1]
+    return n[0] + first if first > 0 else n[0] - (left - n[1] * w[1]) / w[0]
+
+
+@pytest.mark.parametrize("vocab,dtype,n", [(4096, F32, 2000), (8192, BF16, 4000), (50257, F32, 20000), (128256, BF16, 5000), (128256, F16, 60000), (1048571, BF16, 500000)],
+                         ids=lambda v: str(v))
+def test_top_p_next_to_one_over_many_equal_logits_that_weigh_little(vocab, dtype, n):
+    """What top-p leaves out are some of two kinds of equal logits of 2^-35 to 2^-43 each: a sum that loses a part of each of them ends elsewhere.  The
+    number that is kept follows from the definition, and is never within a tenth of a whole one.  A thread adds vocab / 512 weights one after the other,
+    one of which may be the 1: a sum is off by vocab / 512 2^-53 of the whole at most, which is less than a tenth of a token but in the longest row,
+    where tokens of 2^-43 are two of them apart."""
+    x, rows = (-28.0, -28.125), []
+    for steps in (1, 2, 3):
+        p = 1.0 - steps * 2.0 ** -24
+        for offset in (-5.5, -1.5, -0.5, 0.5, 4.5, 0.4 * n):  # tokens beyond those of the first kind
+            for k in (0, 1 + 2 * n - n // 3):
+                count = k if k else vocab
+                low, high = 0.5, 3.0  # the more scale, the fewer are kept
+                for _ in range(80):
+                    scale = 0.5 * (low + high)
+                    low, high = (scale, high) if tail((n, n), x, scale, p, count) > n + offset else (low, scale)
+                scale = torch.tensor(scale)
+                kept = tail((n, n), x, float(scale), p, count)
+                while not 0.1 < kept % 1.0 < 0.9:
+                    scale = torch.nextafter(scale, torch.tensor(0.0))
+                    kept = tail((n, n), x, float(scale), p, count)
+                rows.append((p, float(scale), k, math.ceil(kept)))
+    off = torch.tensor([math.ceil(max(0.0, vocab * 2.0 ** -62 / math.exp(r[1] * x[1]) - 0.1)) for r in rows], device=DEV)
+    assert vocab > 1 << 18 or int(off.max()) == 0
+    values = torch.full((2, vocab), -math.inf, device=DEV)
+    values[0, 0], values[0, 1:n + 1], values[0, n + 1:2 * n + 1] = 0.0, x[0], x[1]
+    values[1, vocab - 1], values[1, 7:n + 7], values[1, n + 7:2 * n + 7] = 0.0, x[1], x[0]
+    pick = lambda at, t=F32: torch.tensor([r[at] for r in rows], device=DEV, dtype=t)
+    p, scale, k, want = pick(0), pick(1), pick(2, I32), pick(3, I32)
+    logits = values[0].to(dtype).expand(len(rows), vocab).contiguous()
+    for limits in ((k, p, None), (k, p, full(len(rows), 1e-30))):
+        token, logp = run(logits, full(len(rows), 1.0), scale, *limits)  # the last one that is kept
+        assert bool(((token - want).abs() <= off).all()), (token - want).tolist()
+        assert bool(((logp.double() - torch.where(want > n, x[1], x[0]) * scale.double()).abs() <= 30 * 2.0 ** -23).all())
+    logits = values[1].to(dtype).expand(len(rows), vocab).contiguous()
+    token, _ = run(logits, full(len(rows), 0.0), scale, k, p)  # the first one: of the second kind where any of them is kept
+    assert bool((((want - n).abs() <= off) & (off > 0) | (token == torch.where(want > n, 7, n + 7))).all())
+
+
 def test_every_token_comes_as_often_as_it_should():
     vocab, rows = 10, 4096
     row = torch.randn(vocab, device=DEV)
