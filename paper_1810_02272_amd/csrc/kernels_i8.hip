@@ -934,7 +934,10 @@ int launch_gradient(const BwdArgs& a, int tile, int splits, hipStream_t stream) 
   if (slow(rows, FILTER ? a.n : a.o, FILTER))
     hipLaunchKernelGGL((i8_gradient_kernel<DTYPE, FILTER, 128, true>), grid, dim3(256), 0, stream, a);
   else if (tile == 256) {
-    if constexpr (FILTER || DTYPE != MI355_F32) hipLaunchKernelGGL((i8_gradient_kernel<DTYPE, FILTER, 256, false>), grid, dim3(512), 0, stream, a);
+    if constexpr (FILTER || DTYPE != MI355_F32)
+      hipLaunchKernelGGL((i8_gradient_kernel<DTYPE, FILTER, 256, false>), grid, dim3(512), 0, stream, a);
+    else
+      return (int)hipErrorInvalidDeviceFunction;  // not built: plan_gradient never asks for it
   } else if (tile == 64)
     hipLaunchKernelGGL((i8_gradient_kernel<DTYPE, FILTER, 64, false>), grid, dim3(256), 0, stream, a);
   else
@@ -988,9 +991,10 @@ int32_t plan_forward(int64_t m, int64_t o) {
 
 // The tile of a gradient, and the workgroups that share a sum.  A tile of 256 has a compute unit to itself, of 128 half of one; a round of the former takes
 // 1.4 times as long as one of the latter where dz is two terms, 1.6 to 2.0 where it is three, 2.5 for dx in fp32, whose kernel of 256 was built only to
-// measure it (us, 256 and 128: dw of 8192 x 4096 -> 4096 bf16 460, 674, fp16 738, 949, fp32 1146, 1145; dx of the same 434, 606; 759, 877; 1177, 944; dw of
+// measure it (and is never taken: a tile of 256 is four of 128 at most, so that there are at least half as many rounds of them) (us, 256 and 128: dw of 8192 x 4096 -> 4096 bf16 460, 674, fp16 738, 949, fp32 1146, 1145; dx of the same 434, 606; 759, 877; 1177, 944; dw of
 // 8192 x 4096 -> 2048 bf16, half a round, 436, 356).  Where a tile of 128 leaves half of the units without work, 64: dx of 100 x 999 <- 333 fp32 10.1, with
-// 128 16.4; of 512 x 333 <- 150 fp32 6.7, 11.8; dw of 2000 x 512 -> 512 bf16 17.0, 18.4, of 1999 x 1111 -> 777 fp16 40.3, 38.1; of 1000 x 2000 -> 1000 bf16, 128 tiles of
+// 128 16.4; of 512 x 333 <- 150 fp32 6.7, 11.8; dw of 2000 x 512 -> 512 bf16 17.0, 18.4, of 1999 x 1111 -> 777 fp16 40.3, 38.1 (the one of these that the rule
+// makes 5 % slower); of 1000 x 2000 -> 1000 bf16, 128 tiles of
 // 128, 29.7, 30.6; of 64 x 4096 -> 4096 bf16 32.8, 22.0.
 void plan_gradient(int64_t rows, int64_t k, int64_t depth, int dtype, bool filter, int32_t& tile, int32_t& splits, int32_t& per) {
   const int64_t large = (tiles_of(rows, k, 256) + kUnits - 1) / kUnits, medium = (tiles_of(rows, k, 128) + 2 * kUnits - 1) / (2 * kUnits);  // rounds

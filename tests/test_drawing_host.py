@@ -158,6 +158,17 @@ def test_i8_variants_have_parity_cases():
                     assert key(m, k, o, dtype) <= seen, (m, k, o, key(m, k, o, dtype) - seen)
 
 
+def test_i8_input_gradients_of_fp32_never_take_the_tile_that_is_not_built():
+    """Whatever the sizes: a round of tiles of 256 counts for 2.3 of those of 128, of which there are twice as many at most."""
+    sizes = (4, 8, 100, 255, 256, 257, 512, 1000, 2047, 2048, 4096, 8192, 12000, 16384, 40000, 100000, 130000)
+    for m in sizes:
+        for k in sizes:
+            if m * k < 1 << 30:
+                for o in (8, 1000):
+                    if max(k, m) * o < 1 << 30:
+                        assert "bwd_data=i8_gradient[256" not in lib.i8_desc_kernel_names(lib.i8_desc_create(lib.I8Params(m, k, o, F32)))
+
+
 def test_sm_variants_have_parity_cases():
     import test_sm_parity_gpu as t
     key = lambda rows, vocab, dtype: (re.sub(r"S=\d+", "S", lib.sm_desc_kernel_names(lib.sm_desc_create(lib.SmParams(rows, vocab, dtype)))), dtype)
