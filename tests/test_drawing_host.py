@@ -169,6 +169,26 @@ def test_i8_input_gradients_of_fp32_never_take_the_tile_that_is_not_built():
                         assert "bwd_data=i8_gradient[256" not in lib.i8_desc_kernel_names(lib.i8_desc_create(lib.I8Params(m, k, o, F32)))
 
 
+def test_sm_layouts_have_parity_cases():
+    """What the kernels of a type tell apart: rows that a team holds, rows in segments of one chunk, and of several; each with limits and without, as
+    every parity case runs."""
+    import inspect
+
+    import test_sm_parity_gpu as t
+
+    def layout(rows, vocab, dtype):
+        chunk = 1024 if dtype is F32 else 2048
+        size = lib.sm_desc_workspace_bytes(lib.sm_desc_create(lib.SmParams(rows, vocab, dtype)))
+        assert size % rows == 0
+        segments = size // rows // 32  # 16 bytes and four maxima each
+        return ("held" if not size else "one chunk" if segments * chunk >= vocab else "several chunks"), dtype
+    want = {(kind, dtype) for kind in ("held", "one chunk", "several chunks") for dtype in (F32, F16, BF16)}
+    assert {layout(rows, vocab, dtype) for rows in (1, 500) for vocab in (1, 4096, 8193, 160000, 600000, 1 << 24) for dtype in (F32, F16, BF16)} == want
+    assert {layout(*c[:3]) for c in t.CASES + t.LONG_CASES} == want
+    runs = inspect.getsource(t.test_parity)
+    assert "(None, None, None, None)" in runs and "(scale, k, p, q)" in runs and "test_parity(case)" in inspect.getsource(t.test_parity_of_the_longest_rows)
+
+
 def test_sm_variants_have_parity_cases():
     import test_sm_parity_gpu as t
     key = lambda rows, vocab, dtype: (re.sub(r"S=\d+", "S", lib.sm_desc_kernel_names(lib.sm_desc_create(lib.SmParams(rows, vocab, dtype)))), dtype)

@@ -1,5 +1,6 @@
 """The oracle of drawing tokens and of layers in 8 bits against hand-worked values and definitions; and planted mistakes that these checks have to notice."""
 import math
+import operator
 
 import pytest
 import torch
@@ -67,6 +68,72 @@ def test_planted_mistakes_in_draws_are_noticed():
         return [w[i] if i in kept[:k] else 0.0 for i in range(len(w))]
     full = tokens.kept_weights(ROW)
     assert top_p_first(full, 3, 0.7) != pytest.approx(tokens.kept_weights(ROW, top_k=3, top_p=0.7))
+
+
+def limits_by(row, p, q, u, reached, least, passed):
+    """Tokens that top-p and min-p keep and the token drawn, with the three borders' comparisons given; equal logits, whose sums are exact."""
+    order, kept, w = range(len(row)), [], 0.0
+    for _ in order:
+        if kept and reached(w, p * len(row)):
+            break
+        kept.append(len(kept))
+        w += 1.0
+    kept = [i for i in kept if least(1.0, q)]
+    drawn, sums = (kept or [-1])[-1], 0.0
+    for i in kept:
+        sums += 1.0
+        if passed(sums, u * len(kept)):
+            drawn = i
+            break
+    return kept, drawn
+
+
+@pytest.mark.parametrize("which", [None, "top_p", "min_p", "u"])
+def test_planted_strict_borders_are_noticed(which):
+    """Eight equal logits under borders that their sums meet exactly: top-p is reached by as much as it asks for, min-p keeps what is equal, u is to be passed."""
+    row = torch.zeros(8, dtype=torch.float64)
+    got = limits_by(row, 0.5, 1.0, 0.5, operator.gt if which == "top_p" else operator.ge, operator.gt if which == "min_p" else operator.ge,
+                    operator.ge if which == "u" else operator.gt)
+    w = tokens.kept_weights(row, top_p=0.5, min_p=1.0)
+    want = [i for i, v in enumerate(w) if v > 0], tokens.draw_row(row, 0.5, top_p=0.5, min_p=1.0)[0]
+    assert want == ([0, 1, 2, 3], 2)
+    assert (got == want) == (which is None)
+    full = lambda v, t=torch.float32: torch.full((1,), v, dtype=t)
+    token, logp = tokens.draw(row[None], full(0.5), full(1.0), full(0, torch.int32), full(0.5), full(1.0))
+    assert (int(token), float(logp)) == (2, pytest.approx(math.log(1 / 4)))
+
+
+def eight_bits_by(x, scale_of, nearest):
+    scale = torch.tensor([scale_of(float(v)) for v in x.abs().amax(1)], dtype=torch.float64)
+    return nearest(x.double() / scale[:, None]), scale
+
+
+@pytest.mark.parametrize("which", [None, "scale of 24 bits", "scale rounded to nearest", "halves up", "halves away from 0"])
+def test_planted_mistakes_in_eight_bits_are_noticed(which):
+    def up(most):
+        fraction, exponent = math.frexp(most / 127)
+        return math.ldexp(math.ceil(fraction * 256), exponent - 8)
+
+    def near(most):
+        fraction, exponent = math.frexp(most / 127)
+        return math.ldexp(round(fraction * 256), exponent - 8)
+    scale_of = {"scale of 24 bits": lambda most: most / 127, "scale rounded to nearest": near}.get(which, up)
+    nearest = {"halves up": lambda t: torch.floor(t + 0.5), "halves away from 0": lambda t: torch.sign(t) * torch.floor(t.abs() + 0.5)}.get(which, torch.round)
+    x = torch.tensor([[127.0, 0.5, 1.5, -2.5, -3.5], [254.0, 1.0, -3.0, 3.1, 0.0], [128.25, 1.0, 64.0, -7.0, 0.0]])
+    codes, scale = tokens.eight_bits(x)
+    got_codes, got_scale = eight_bits_by(x, scale_of, nearest)
+    assert (torch.equal(got_codes, codes) and torch.equal(got_scale, scale)) == (which is None)
+
+
+@pytest.mark.parametrize("which", [None, "scale of the row left out", "scale of the output left out", "scale taken twice", "bias gradient with the scale"])
+def test_planted_mistakes_in_gradients_of_eight_bits_are_noticed(which):
+    x, w, dz = rand(5, 12), rand(7, 12, seed=1), rand(5, 7, seed=2)
+    (c, s), (v, t) = tokens.eight_bits(x), tokens.eight_bits(w)
+    wanted = tokens.i8_backward_filter(c, s, dz) + (tokens.i8_backward_data(v, t, dz),)
+    row = {"scale of the row left out": torch.ones_like(s), "scale taken twice": s * s}.get(which, s)
+    out = torch.ones_like(t) if which == "scale of the output left out" else t
+    got = (dz * row[:, None]).t() @ c, (dz * s[:, None] if which == "bias gradient with the scale" else dz).sum(0), (dz * out[None]) @ v
+    assert all(torch.allclose(a, b, rtol=1e-12) for a, b in zip(got, wanted)) == (which is None)
 
 
 def test_worked_rows_in_eight_bits():

@@ -291,6 +291,31 @@ def test_gradients_take_all_bits_of_dz(dtype):
     assert float(dx) == step * float(scale[0])
 
 
+@pytest.mark.parametrize("dtype", [F32, F16, BF16])
+@pytest.mark.parametrize("m,k,o", [(3, 40, 2), (40, 64, 70), (300, 700, 900), (3000, 2100, 2200)])
+def test_gradients_of_the_smallest_dz(m, k, o, dtype):
+    """Products with the scale down to fp32's smallest: what a bf16 term rounds away there is half of 2^-133 at most, as often as a code counts it."""
+    x, w, _, dz = make((m, k, o, dtype, 0, 0))
+    layer = Layer((m, k, o, dtype, 0, 0))
+    codes, scale = layer.eight(x)
+    w_codes, w_scale = layer.eight(w, pack=True)
+    size = torch.tensor([1e-30, 2.0 ** -116, 2.0 ** -121, 2.0 ** -126, 2.0 ** -131, 2.0 ** -134], device=DEV, dtype=torch.float64)
+    z = dz.double() * (size[torch.arange(o, device=DEV) % 6] if dtype is not F16 else 2.0 ** -24)
+    if dtype is F16:  # whose smallest number is 2^-24: the scales make the products small
+        scale, w_scale = scale * 2.0 ** -104, w_scale * 2.0 ** -104
+    dz = z.to(dtype)
+    dw, _ = layer.filter(codes, scale, dz)
+    want, _ = tokens.i8_backward_filter(codes[:, :k], scale, dz)
+    some, _ = tokens.i8_backward_filter(codes[:, :k].abs(), scale, dz.abs())
+    lost = codes[:, :k].double().abs().sum(0)[None] * 1.01 * 2.0 ** -134
+    within(dw, want, some * (36 + terms(dtype) * m / 32 + layer.splits("bwd_filter")) * U * 1.02 + lost + 2.0 ** -148)
+    dx = layer.data(w_codes, w_scale, dz)
+    want = tokens.i8_backward_data(w_codes[:, :k], w_scale, dz)
+    some = tokens.i8_backward_data(w_codes[:, :k].abs(), w_scale, dz.abs())
+    lost = w_codes[:, :k].double().abs().sum(0)[None] * 1.01 * 2.0 ** -134
+    within(dx, want, some * (36 + terms(dtype) * o / 32 + layer.splits("bwd_data")) * U * 1.02 + half_step(want, dtype) * 1.02 + lost + 2.0 ** -148)
+
+
 def test_gradients_agree_with_differences():
     """fp32: of a sum of outputs of the layer, by the codes' and the bias's change."""
     case = (6, 20, 5, F32, 1, 0)

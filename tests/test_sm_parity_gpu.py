@@ -74,6 +74,15 @@ def test_parity(case):
         check(run(x, u, *limits), x, u, *limits)
 
 
+# segments of several chunks
+LONG_CASES = [(2, 300001, F32, 300001, 2.0), (3, 262145, F32, 262147, 0.5), (2, 540001, F16, 540004, 3.0), (2, 1600003, BF16, 1600003, 1.0)]
+
+
+@pytest.mark.parametrize("case", LONG_CASES, ids=["%dx%d-%s" % (c[0], c[1], str(c[2])[6:]) for c in LONG_CASES])
+def test_parity_of_the_longest_rows(case):
+    test_parity(case)
+
+
 @pytest.mark.parametrize("dtype", [F32, F16, BF16])
 def test_against_the_definition_token_by_token(dtype):
     x, u, scale, k, p, q = make((120, 37, dtype, 40, 2.0), seed=4)
