@@ -300,6 +300,43 @@ def test_top_p_next_to_one_over_many_equal_logits_that_weigh_little(vocab, dtype
     assert bool((((want - n).abs() <= off) & (off > 0) | (token == torch.where(want > n, 7, n + 7))).all())
 
 
+@pytest.mark.parametrize("vocab,dtype,n", [(4096, F32, 900), (8192, BF16, 1000), (4096, F32, 2000), (8192, F16, 4000), (20000, BF16, 4000), (9000, F32, 4400)],
+                         ids=lambda v: str(v))
+def test_top_p_a_small_part_of_a_token_from_the_end_of_equal_logits(vocab, dtype, n):
+    """As above, with fewer tokens: the border is a small part of a token before or behind the last one of the first kind, where sums of weights rounded to
+    2^-shift end on its other side in some rows.  (The parts are four times what sums may be off or more.)"""
+    x, rows, missed = (-28.0, -28.125), [], 0
+    unit = 2.0 ** min(50, 61 - (vocab - 1).bit_length())
+    for steps in range(1, 13):
+        p = 1.0 - steps * 2.0 ** -24
+        for before in (True, False):
+            low, high = 0.5, 3.0
+            for _ in range(80):
+                scale = 0.5 * (low + high)
+                low, high = (scale, high) if tail((n, n), x, scale, p, vocab) > n else (low, scale)
+            scale = torch.tensor(scale)
+            part = 0.1 * min(1.0, n * unit ** -1 / math.exp(float(scale) * x[0]) * 4)
+            for _ in range(1000):
+                kept = tail((n, n), x, float(scale), p, vocab) - n
+                if part / 5 < (-kept if before else kept) < part:
+                    break
+                scale = torch.nextafter(scale, torch.tensor(0.0 if kept < (-0.6 if before else 0.6) * part else 9.0))
+            else:
+                continue
+            w, whole = [math.exp(float(scale) * v) for v in x], 1.0
+            whole += n * w[0] + n * w[1]
+            missed += (unit + n * round(w[0] * unit) >= round(p * whole * unit)) != before
+            assert vocab * 2.0 ** -62 < part / 20 * w[1]
+            rows.append((p, float(scale), n if before else n + 1))
+    assert len(rows) >= 6 and missed >= 2, (len(rows), missed)
+    values = torch.full((vocab,), -math.inf, device=DEV)
+    values[0], values[1:n + 1], values[n + 1:2 * n + 1] = 0.0, x[0], x[1]
+    pick = lambda at, t=F32: torch.tensor([r[at] for r in rows], device=DEV, dtype=t)
+    logits = values.to(dtype).expand(len(rows), vocab).contiguous()
+    token, _ = run(logits, full(len(rows), 1.0), pick(1), None, pick(0))
+    assert torch.equal(token, pick(2, I32)), (token - pick(2, I32)).tolist()
+
+
 def test_every_token_comes_as_often_as_it_should():
     vocab, rows = 10, 4096
     row = torch.randn(vocab, device=DEV)
