@@ -83,6 +83,31 @@ def test_parity_of_the_longest_rows(case):
     test_parity(case)
 
 
+@pytest.mark.parametrize("case", CASES + LONG_CASES, ids=["%dx%d-%s" % (c[0], c[1], str(c[2])[6:]) for c in CASES + LONG_CASES])
+def test_no_case_has_a_border_within_what_the_arithmetic_may_be_off(case):
+    """Of the whole, u and p are 2^-40 or more away from every sum that decides about them, and of q every weight that is not equal to it."""
+    x, u, scale, k, p, q = make(case)
+    rows, vocab = x.shape
+    for limits in ((None, None, None, None), (scale, None, None, None), (scale, k, None, None), (scale, None, p, None), (None, None, None, q),
+                   (scale, k, p, None), (scale, k, p, q)):
+        s, kk, pp, qq = (t if t is not None else full(rows, v, d) for t, v, d in zip(limits, (1.0, 0, 1.0, 0.0), (F32, I32, F32, F32)))
+        by, index = torch.sort(x.double(), dim=1, descending=True, stable=True)
+        by = torch.exp((by - by[:, :1]) * s.double()[:, None])
+        place = torch.arange(vocab, device=DEV)[None]
+        by = torch.where((place < kk[:, None]) | (kk <= 0)[:, None], by, 0.0)
+        sums = by.cumsum(1)
+        target = pp.double()[:, None] * sums[:, -1:]
+        limited = ((pp > 0) & (pp < 1))[:, None] & (place < vocab)
+        assert bool(((sums - target).abs() > sums[:, -1:] * 2.0 ** -40)[limited].all())
+        by = torch.where((place <= (sums < target).sum(1, keepdim=True)) | (pp >= 1)[:, None], by, 0.0)
+        least = qq.double().clamp(max=1.0)[:, None]
+        assert bool(((by == least) | ((by - least).abs() > least * 2.0 ** -40))[(qq > 0)[:, None] & (by > 0)].all())
+        kept = torch.zeros_like(by).scatter_(1, index, torch.where((by >= least) | (qq <= 0)[:, None], by, 0.0))
+        sums = kept.cumsum(1)
+        near = ((sums - u.double()[:, None] * sums[:, -1:]).abs() <= sums[:, -1:] * 2.0 ** -40) & (kept > 0)
+        assert not bool(near.any())
+
+
 @pytest.mark.parametrize("dtype", [F32, F16, BF16])
 def test_against_the_definition_token_by_token(dtype):
     x, u, scale, k, p, q = make((120, 37, dtype, 40, 2.0), seed=4)
