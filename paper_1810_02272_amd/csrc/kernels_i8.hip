@@ -402,7 +402,7 @@ __device__ __forceinline__ int column_at(int p) { return (p & ~63) + 4 * (p & 15
 
 // WM x WN waves, each 64 rows of x by 16 NT outputs.  128 inputs at a time go straight into shared memory, one step ahead, as rows of 8 pieces of 16
 // bytes whose order is turned from row to row, so that neither side meets a bank twice.  Bound by the matrix units, 51 % busy: 8192 x 4096 -> 4096 130 us,
-// 2.1 POP/s; of few tiles by what a group of waves waits for in each step, 48 x 9216 -> 4096 18 us by four groups.  (Three or four buffers: no change where
+// 2.1 POP/s; of few tiles by what a group of waves waits for in each step, 48 x 9216 -> 4096 20 us by four groups, 64 workgroups on 256 units.  (Three or four buffers: no change where
 // there are few tiles, 60 against 44 us for 3000 x 4096 -> 2000, as a compute unit then holds one workgroup.)
 // DEPTH: groups of such waves in a workgroup that take the steps in turn, each with shared memory of its own, and add up in the end: where there are few tiles a
 // compute unit has more than a wave for each of its matrix units.
